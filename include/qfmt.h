@@ -458,6 +458,112 @@ int qfmt_conv_fmac8(int32_t op, const qfmt_conv_t* geom, const float* d_p, const
                     const qfmt_format_t* fmt, qfmt_stats_t* d_stats, int accumulate, int path, void* stream);
 
 /*
+ * What follows a product inside a transformer layer (the paper pre-trains BERT models; their layers end
+ * both halves with it): dropout, the residual addition and layer normalisation, forward and backward.
+ * The tensors are rows x cols matrices, row-major, all of one storage type:
+ *   QFMT_F32   fp32 containers, as qfmt_quantize_stats and the products write them
+ *   QFMT_F16   packed 1/5/10 codes (IEEE binary16), QFMT_BF16  packed 1/8/7 codes (bfloat16)
+ * Weights, biases, their gradients and the row statistics are fp32.  All arithmetic is in 32 bits; each
+ * stored value is rounded once.  In every call below a leading dimension of 0 stands for cols; rows = 0 or
+ * cols = 0 is valid; rows and cols are below 2^31.  Any alignment of an element is accepted.  Tensors whose
+ * granules of eight columns are aligned (32 bytes for containers, 16 for codes, leading dimensions
+ * multiples of 8) move by whole granules.
+ */
+enum { QFMT_F32 = 0, QFMT_F16 = 1, QFMT_BF16 = 2 };
+
+/*
+ * A dropout mask that is recomputed from these numbers wherever it is needed and never stored.  Element
+ * (row, col) has 16 random bits u and is dropped when u < t, t = round(65536 p); what is kept is multiplied by
+ * 65536 / (65536 - t), so that the mean stays what it was for the t in use.  u are bits 16 (col mod 8) and up
+ * (word 0 first) of the 128-bit block that the generator Philox4x32-10 (Salmon, Moraes, Dror, Shaw, SC 2011)
+ * gives for the counter (col / 8, row, offset mod 2^32, offset / 2^32) under the key seed.  The mask depends on
+ * nothing else: not on the storage type, the leading dimensions or the alignment.
+ */
+typedef struct {
+    float p;                  /* probability to drop, 0 .. 1; p < 2^-17 drops nothing                  */
+    int32_t reserved;
+    uint64_t seed;            /* one per run                                                         */
+    uint64_t offset;          /* one per layer and step: another offset gives another mask           */
+    const uint64_t* d_offset; /* device, 8-byte aligned, or NULL: added to offset when the kernel runs, so that
+                                 a captured graph draws a new mask at every replay                    */
+} qfmt_dropout_t;
+
+/*
+ * out = residual + D(x) with D as above; out = D(x) if d_residual is NULL.  A dropped element counts as zero
+ * whatever it holds (infinities and NaN do not get through).  D is its own backward pass: call this on the
+ * gradient with the same *drop.  d_out may equal d_x or d_residual when their leading dimensions agree; other
+ * overlap is an error the library cannot detect.
+ * Errors: QFMT_ERR_BAD_ARG, QFMT_ERR_UNSUPPORTED_ARCH, QFMT_ERR_CUDA.
+ */
+int qfmt_dropout(const void* d_x, int64_t ld_x, const void* d_residual, int64_t ld_residual, void* d_out, int64_t ld_out,
+                 int64_t rows, int64_t cols, int32_t dtype, const qfmt_dropout_t* drop, void* stream);
+
+/* Geometry of a normalisation; ld_t is the leading dimension of the tensor d_t below, 0 for cols. */
+typedef struct {
+    int64_t rows, cols;
+    int64_t ld_x, ld_residual, ld_h, ld_y;
+    int64_t ld_dy, ld_dh, ld_dx, ld_dresidual;
+    int32_t dtype;            /* QFMT_F32, QFMT_F16 or QFMT_BF16                                      */
+    float eps;                /* finite, >= 0                                                        */
+} qfmt_norm_t;
+
+/*
+ * Layer normalisation of every row: with n = cols,
+ *     mean = sum x / n,  rstd = 1 / sqrt(sum (x - mean)^2 / n + eps),  y = (x - mean) rstd weight + bias.
+ *   d_weight, d_bias   device, cols floats, or NULL for 1 and 0
+ *   d_mean, d_rstd     device, rows floats, or NULL: what the backward pass needs
+ *   fmt      NULL: y is rounded to its storage type only.  Otherwise y is rounded to *fmt, so that the next
+ *            product can read it (Section IV-A rounds at the output of every layer): the values of
+ *            qfmt_quantize_stats (containers) or the codes of qfmt_quantize_stats_pack16 on the 32-bit results.
+ *            loss_scale must be 1, and QFMT_F16 / QFMT_BF16 take {5, 10} / {8, 7} only (QFMT_ERR_BAD_FORMAT)
+ *   d_stats  device, 8-byte aligned, or NULL: statistics of that rounding (fmt is then required);
+ *            accumulate as in qfmt_quantize_stats
+ * d_y may equal d_x when their leading dimensions agree; other overlap is an error the library cannot detect.
+ * The backward pass, from dy = dL/dy, with xhat = (x - mean) rstd and g = weight dy:
+ *     dx = rstd (g - sum g / n - xhat sum (g xhat) / n),  dweight = sum over rows of dy xhat,  dbias = ... of dy.
+ *   d_dx, d_dweight, d_dbias   each may be NULL where it is not wanted; dweight and dbias are overwritten (zeros
+ *            for rows = 0) and do not depend on the order in which blocks run
+ *   fmt, d_stats, accumulate   as above, for dx (d_stats requires d_dx)
+ *   d_workspace  device, 16-byte aligned, at least qfmt_layer_norm_workspace_bytes(norm) bytes; may be NULL if
+ *            neither d_dweight nor d_dbias is wanted.  Calls that share a workspace must be ordered on one stream
+ * d_dx may equal d_dy when their leading dimensions agree.
+ * Errors: QFMT_ERR_BAD_FORMAT, QFMT_ERR_BAD_ARG, QFMT_ERR_UNSUPPORTED_ARCH, QFMT_ERR_CUDA.
+ */
+int qfmt_layer_norm(const qfmt_norm_t* norm, const void* d_x, const float* d_weight, const float* d_bias, void* d_y,
+                    float* d_mean, float* d_rstd, const qfmt_format_t* fmt, qfmt_stats_t* d_stats, int accumulate, void* stream);
+int qfmt_layer_norm_backward(const qfmt_norm_t* norm, const void* d_dy, const void* d_x, const float* d_mean,
+                             const float* d_rstd, const float* d_weight, void* d_dx, float* d_dweight, float* d_dbias,
+                             const qfmt_format_t* fmt, qfmt_stats_t* d_stats, int accumulate, void* d_workspace,
+                             size_t workspace_bytes, void* stream);
+size_t qfmt_layer_norm_workspace_bytes(const qfmt_norm_t* norm);  /* 0 if rows or cols is out of range */
+
+/*
+ * The output of a transformer sub-layer in one pass: h = residual + D(x), y = LN(h), with D as in qfmt_dropout and
+ * LN as in qfmt_layer_norm (which takes the 32-bit h, before it is rounded to its storage type).
+ *   drop        NULL or p = 0: nothing is dropped (inference)
+ *   d_residual  NULL: h = D(x)
+ *   d_h         receives h, which the backward pass reads; NULL where there will be none
+ *   fmt, d_stats, accumulate   as in qfmt_layer_norm, for y
+ * d_h may equal d_x or d_residual, and d_y may equal d_x or d_residual, when the leading dimensions agree.
+ * The backward pass, with the forward pass's *drop:
+ *     dresidual = dh + (what qfmt_layer_norm_backward gives for dy at h),   dx = D(dresidual).
+ *   d_dh        a gradient that reaches h by another path (the next residual addition of a pre-norm layer), or NULL
+ *   d_dx, d_dresidual, d_dweight, d_dbias   each may be NULL where it is not wanted
+ *   fmt, d_stats, accumulate   as above, for dx (the operand of the next two products); dresidual is rounded to
+ *               its storage type only
+ * D is applied to the 32-bit dresidual.  d_dx or d_dresidual may equal d_dy or d_dh when the leading dimensions
+ * agree; d_dx and d_dresidual must differ.  Workspace and errors as in qfmt_layer_norm_backward.
+ */
+int qfmt_dropout_add_layer_norm(const qfmt_norm_t* norm, const qfmt_dropout_t* drop, const void* d_x, const void* d_residual,
+                                const float* d_weight, const float* d_bias, void* d_h, void* d_y, float* d_mean, float* d_rstd,
+                                const qfmt_format_t* fmt, qfmt_stats_t* d_stats, int accumulate, void* stream);
+int qfmt_dropout_add_layer_norm_backward(const qfmt_norm_t* norm, const qfmt_dropout_t* drop, const void* d_dy, const void* d_dh,
+                                         const void* d_h, const float* d_mean, const float* d_rstd, const float* d_weight,
+                                         void* d_dx, void* d_dresidual, float* d_dweight, float* d_dbias,
+                                         const qfmt_format_t* fmt, qfmt_stats_t* d_stats, int accumulate, void* d_workspace,
+                                         size_t workspace_bytes, void* stream);
+
+/*
  * qfmt_gemm for callers that cannot allocate device memory.  (The paper has no counterpart of
  * this call; it exists for the way the library gets embedded.)
  *

@@ -66,6 +66,20 @@ class qfmt_dls_t(ctypes.Structure):
                 ("reserved", ctypes.c_int32), ("n_steps", ctypes.c_uint64), ("n_skipped", ctypes.c_uint64)]
 
 
+class qfmt_dropout_t(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_float), ("reserved", ctypes.c_int32), ("seed", ctypes.c_uint64),
+                ("offset", ctypes.c_uint64), ("d_offset", ctypes.c_void_p)]
+
+
+class qfmt_norm_t(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int64) for k in ("rows", "cols", "ld_x", "ld_residual", "ld_h", "ld_y", "ld_dy", "ld_dh",
+                                              "ld_dx", "ld_dresidual")] + [("dtype", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+QFMT_F32, QFMT_F16, QFMT_BF16 = 0, 1, 2
+_STORAGE = {"torch.float32": QFMT_F32, "torch.float16": QFMT_F16, "torch.bfloat16": QFMT_BF16}
+
+
 _lib: Optional[ctypes.CDLL] = None
 
 
@@ -145,6 +159,20 @@ def _bind_optional(L: ctypes.CDLL) -> None:
     L.qfmt_conv_workspace_bytes.restype = sz
     L.qfmt_conv_fmac8.argtypes = [ctypes.c_int32, convp, vp, vp, vp, ctypes.POINTER(qfmt_format_t), vp, ci, ci, vp]
     L.qfmt_conv_fmac8.restype = ci
+    normp, dropp, fmtp = ctypes.POINTER(qfmt_norm_t), ctypes.POINTER(qfmt_dropout_t), ctypes.POINTER(qfmt_format_t)
+    L.qfmt_dropout.argtypes = [vp, i64, vp, i64, vp, i64, i64, i64, ctypes.c_int32, dropp, vp]
+    L.qfmt_dropout.restype = ci
+    L.qfmt_layer_norm.argtypes = [normp, vp, vp, vp, vp, vp, vp, fmtp, vp, ci, vp]
+    L.qfmt_layer_norm.restype = ci
+    L.qfmt_layer_norm_backward.argtypes = [normp, vp, vp, vp, vp, vp, vp, vp, vp, fmtp, vp, ci, vp, sz, vp]
+    L.qfmt_layer_norm_backward.restype = ci
+    L.qfmt_layer_norm_workspace_bytes.argtypes = [normp]
+    L.qfmt_layer_norm_workspace_bytes.restype = sz
+    L.qfmt_dropout_add_layer_norm.argtypes = [normp, dropp, vp, vp, vp, vp, vp, vp, vp, vp, fmtp, vp, ci, vp]
+    L.qfmt_dropout_add_layer_norm.restype = ci
+    L.qfmt_dropout_add_layer_norm_backward.argtypes = [normp, dropp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, fmtp, vp, ci,
+                                                       vp, sz, vp]
+    L.qfmt_dropout_add_layer_norm_backward.restype = ci
     L.qfmt_gemm_builtin_scratch.argtypes = [matp, matp, vp, ctypes.c_int64, ctypes.POINTER(qfmt_format_t), vp, vp]
     L.qfmt_gemm_builtin_scratch.restype = ci
     L.qfmt_selftest_bounded_wait.argtypes = [vp, ctypes.c_uint32, vp, vp]
@@ -378,3 +406,74 @@ def qfmt_gemm_tile_policy(policy: int) -> None:
     """0 automatic, 1 single-CTA tiles, 2 CTA-pair tiles, 3 CTA-pair tiles under the balanced schedule; see
     include/qfmt.h."""
     _check(lib().qfmt_gemm_tile_policy(int(policy)), "qfmt_gemm_tile_policy")
+
+
+def _storage(dtype) -> int:
+    """Storage type of a tensor: QFMT_F32 / QFMT_F16 / QFMT_BF16, or the torch dtype of the same words."""
+    return dtype if isinstance(dtype, int) else _STORAGE[str(dtype)]
+
+
+def make_dropout(p: float, seed: int, offset: int = 0, d_offset=None) -> qfmt_dropout_t:
+    """A mask: probability, seed of the run, offset of the layer and step; see qfmt_dropout_t in include/qfmt.h."""
+    return qfmt_dropout_t(p, 0, seed, offset, _ptr(d_offset))
+
+
+def make_norm(rows: int, cols: int, dtype, eps: float = 1e-5, ld_x: int = 0, ld_residual: int = 0, ld_h: int = 0, ld_y: int = 0,
+              ld_dy: int = 0, ld_dh: int = 0, ld_dx: int = 0, ld_dresidual: int = 0) -> qfmt_norm_t:
+    """Geometry of a normalisation (a leading dimension of 0 is a dense tensor's); see qfmt_norm_t in include/qfmt.h."""
+    return qfmt_norm_t(rows, cols, ld_x, ld_residual, ld_h, ld_y, ld_dy, ld_dh, ld_dx, ld_dresidual, _storage(dtype), eps)
+
+
+def _ref(record):
+    """A record's address for a call, or NULL."""
+    return None if record is None else ctypes.byref(record)
+
+
+def qfmt_dropout(d_x, ld_x: int, d_residual, ld_residual: int, d_out, ld_out: int, rows: int, cols: int, dtype,
+                 drop: qfmt_dropout_t, stream=None) -> None:
+    """out = residual + D(x), and D's own backward pass; see qfmt_dropout in include/qfmt.h."""
+    _check(lib().qfmt_dropout(_ptr(d_x), ld_x, _ptr(d_residual), ld_residual, _ptr(d_out), ld_out, rows, cols,
+                              _storage(dtype), _ref(drop), _stream_handle(stream)), "qfmt_dropout")
+
+
+def qfmt_layer_norm(norm: qfmt_norm_t, d_x, d_weight, d_bias, d_y, d_mean=None, d_rstd=None,
+                    fmt: Optional[qfmt_format_t] = None, d_stats=None, accumulate: int = 0, stream=None) -> None:
+    """y = LN(x), rounded to fmt with statistics if one is given; see qfmt_layer_norm in include/qfmt.h."""
+    _check(lib().qfmt_layer_norm(_ref(norm), _ptr(d_x), _ptr(d_weight), _ptr(d_bias), _ptr(d_y), _ptr(d_mean), _ptr(d_rstd),
+                                 _ref(fmt), _ptr(d_stats), accumulate, _stream_handle(stream)), "qfmt_layer_norm")
+
+
+def qfmt_layer_norm_workspace_bytes(norm: qfmt_norm_t) -> int:
+    return int(lib().qfmt_layer_norm_workspace_bytes(ctypes.byref(norm)))
+
+
+def qfmt_layer_norm_backward(norm: qfmt_norm_t, d_dy, d_x, d_mean, d_rstd, d_weight, d_dx, d_dweight, d_dbias, d_workspace,
+                             workspace_bytes: int, fmt: Optional[qfmt_format_t] = None, d_stats=None, accumulate: int = 0,
+                             stream=None) -> None:
+    """Gradients of LN's input, weight and bias; see qfmt_layer_norm_backward in include/qfmt.h."""
+    _check(lib().qfmt_layer_norm_backward(_ref(norm), _ptr(d_dy), _ptr(d_x), _ptr(d_mean), _ptr(d_rstd), _ptr(d_weight),
+                                          _ptr(d_dx), _ptr(d_dweight), _ptr(d_dbias), _ref(fmt), _ptr(d_stats), accumulate,
+                                          _ptr(d_workspace), workspace_bytes, _stream_handle(stream)),
+           "qfmt_layer_norm_backward")
+
+
+def qfmt_dropout_add_layer_norm(norm: qfmt_norm_t, drop: Optional[qfmt_dropout_t], d_x, d_residual, d_weight, d_bias, d_h, d_y,
+                                d_mean=None, d_rstd=None, fmt: Optional[qfmt_format_t] = None, d_stats=None,
+                                accumulate: int = 0, stream=None) -> None:
+    """h = residual + D(x), y = LN(h) in one pass; see qfmt_dropout_add_layer_norm in include/qfmt.h."""
+    _check(lib().qfmt_dropout_add_layer_norm(_ref(norm), _ref(drop), _ptr(d_x), _ptr(d_residual), _ptr(d_weight), _ptr(d_bias),
+                                             _ptr(d_h), _ptr(d_y), _ptr(d_mean), _ptr(d_rstd), _ref(fmt), _ptr(d_stats),
+                                             accumulate, _stream_handle(stream)), "qfmt_dropout_add_layer_norm")
+
+
+def qfmt_dropout_add_layer_norm_backward(norm: qfmt_norm_t, drop: Optional[qfmt_dropout_t], d_dy, d_dh, d_h, d_mean, d_rstd,
+                                         d_weight, d_dx, d_dresidual, d_dweight, d_dbias, d_workspace, workspace_bytes: int,
+                                         fmt: Optional[qfmt_format_t] = None, d_stats=None, accumulate: int = 0,
+                                         stream=None) -> None:
+    """dresidual = dh + LN's gradient, dx = D(dresidual), dweight, dbias; see
+    qfmt_dropout_add_layer_norm_backward in include/qfmt.h."""
+    _check(lib().qfmt_dropout_add_layer_norm_backward(_ref(norm), _ref(drop), _ptr(d_dy), _ptr(d_dh), _ptr(d_h), _ptr(d_mean),
+                                                      _ptr(d_rstd), _ptr(d_weight), _ptr(d_dx), _ptr(d_dresidual),
+                                                      _ptr(d_dweight), _ptr(d_dbias), _ref(fmt), _ptr(d_stats), accumulate,
+                                                      _ptr(d_workspace), workspace_bytes, _stream_handle(stream)),
+           "qfmt_dropout_add_layer_norm_backward")

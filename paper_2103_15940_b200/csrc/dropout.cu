@@ -1,0 +1,100 @@
+// Dropout from a counter-based generator: out = residual + D(x), with the mask recomputed from (seed, offset,
+// row, column) wherever it is needed and never stored.
+//
+// One read and one write per element (two reads with a residual) and, per granule of eight columns, one
+// Philox block: 20 wide products, against 32 bytes of traffic for 16-bit codes.
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "common.cuh"
+#include "elements.cuh"
+
+namespace qfmt {
+namespace {
+
+constexpr int kDropThreads = 256;
+
+template <int kType>
+struct DropArgs {
+    using W = typename Word<kType>::type;
+    const W* x;
+    const W* residual;  // or NULL
+    W* out;
+    int64_t ld_x, ld_residual, ld_out;
+    int64_t rows, cols;
+    uint32_t granules;  // per row
+    bool vec;
+    DropParams drop;
+};
+
+template <int kType>
+__global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropArgs<kType> a) {
+    const uint64_t total = (uint64_t)a.rows * a.granules;
+    const uint64_t offset = drop_offset(a.drop);
+    for (uint64_t i = (uint64_t)blockIdx.x * kDropThreads + threadIdx.x; i < total; i += (uint64_t)gridDim.x * kDropThreads) {
+        const uint64_t row = i / a.granules;
+        const uint32_t g = (uint32_t)(i - row * a.granules);
+        const int64_t col = (int64_t)g * kGranule;
+        const int n = a.cols - col < kGranule ? (int)(a.cols - col) : kGranule;
+        float v[kGranule];
+        load_granule<kType>(a.x + row * a.ld_x + col, n, a.vec, v);
+        if (a.drop.threshold != 0u) drop_granule(a.drop, offset, (uint32_t)row, g, v);
+        if (a.residual != nullptr) {
+            float r[kGranule];
+            load_granule<kType>(a.residual + row * a.ld_residual + col, n, a.vec, r);
+#pragma unroll
+            for (int j = 0; j < kGranule; ++j) v[j] = add_ieee(r[j], v[j]);
+        }
+        store_granule<kType>(a.out + row * a.ld_out + col, n, a.vec, finish<kType, false>(v, n, QuantParams{}, nullptr));
+    }
+}
+
+template <int kType>
+int launch_dropout(const void* d_x, int64_t ld_x, const void* d_residual, int64_t ld_residual, void* d_out, int64_t ld_out,
+                   int64_t rows, int64_t cols, const DropParams& drop, const DeviceInfo& dev, cudaStream_t stream) {
+    using W = typename Word<kType>::type;
+    DropArgs<kType> a;
+    a.x = static_cast<const W*>(d_x);
+    a.residual = static_cast<const W*>(d_residual);
+    a.out = static_cast<W*>(d_out);
+    a.ld_x = ld_x;
+    a.ld_residual = ld_residual;
+    a.ld_out = ld_out;
+    a.rows = rows;
+    a.cols = cols;
+    a.granules = (uint32_t)((cols + kGranule - 1) / kGranule);
+    a.vec = granule_aligned(d_x, ld_x, kType) && granule_aligned(d_residual, ld_residual, kType) &&
+            granule_aligned(d_out, ld_out, kType);
+    a.drop = drop;
+    const uint64_t blocks = ((uint64_t)rows * a.granules + kDropThreads - 1) / kDropThreads;
+    const uint64_t cap = (uint64_t)dev.sm_count * 16;
+    dropout_kernel<kType><<<(unsigned)(blocks < cap ? blocks : cap), kDropThreads, 0, stream>>>(a);
+    QFMT_CUDA_TRY(cudaGetLastError());
+    return QFMT_OK;
+}
+
+}  // namespace
+}  // namespace qfmt
+
+extern "C" int qfmt_dropout(const void* d_x, int64_t ld_x, const void* d_residual, int64_t ld_residual, void* d_out,
+                            int64_t ld_out, int64_t rows, int64_t cols, int32_t dtype, const qfmt_dropout_t* drop,
+                            void* stream) {
+    using namespace qfmt;
+    if (drop == nullptr || dtype < QFMT_F32 || dtype > QFMT_BF16) return QFMT_ERR_BAD_ARG;
+    DropParams params;
+    int rc = make_drop_params(drop, &params);
+    if (rc != QFMT_OK) return rc;
+    if (rows < 0 || cols < 0 || rows > 0x7FFFFFFF || cols > 0x7FFFFFFF) return QFMT_ERR_BAD_ARG;
+    ld_x = ld_x ? ld_x : cols;
+    ld_residual = ld_residual ? ld_residual : cols;
+    ld_out = ld_out ? ld_out : cols;
+    if (ld_x < cols || ld_out < cols || (d_residual != nullptr && ld_residual < cols)) return QFMT_ERR_BAD_ARG;
+    if (rows != 0 && cols != 0 && (d_x == nullptr || d_out == nullptr)) return QFMT_ERR_BAD_ARG;
+    if (!element_aligned(d_x, dtype) || !element_aligned(d_residual, dtype) || !element_aligned(d_out, dtype)) return QFMT_ERR_BAD_ARG;
+    DeviceInfo dev;
+    rc = current_device(&dev);
+    if (rc != QFMT_OK) return rc;
+    if (rows == 0 || cols == 0) return QFMT_OK;
+    const auto launch = dtype == QFMT_F32 ? launch_dropout<QFMT_F32> : dtype == QFMT_F16 ? launch_dropout<QFMT_F16> : launch_dropout<QFMT_BF16>;
+    return launch(d_x, ld_x, d_residual, ld_residual, d_out, ld_out, rows, cols, params, dev, (cudaStream_t)stream);
+}

@@ -1,0 +1,222 @@
+// Typed access to rows of fp32 containers, binary16 codes and bfloat16 codes in granules of eight
+// columns, the dropout mask, and the rounding of finished values, shared by the passes that work on
+// whole layer outputs (dropout, layer normalisation).
+//
+// A granule is the unit everything here is laid out by: eight 16-bit codes are one 128-bit access, eight
+// containers one 256-bit access, and eight columns take the 128 random bits of one Philox block, so a
+// thread that owns a granule never shares a block of random bits with another one.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "qfmt.h"
+#include "round.cuh"
+
+namespace qfmt {
+namespace {
+
+constexpr int kGranule = 8;
+
+template <int kType>
+struct Word {
+    using type = uint16_t;
+};
+template <>
+struct Word<QFMT_F32> {
+    using type = uint32_t;
+};
+
+template <int kType>
+__device__ __forceinline__ float widen(typename Word<kType>::type w) {
+    if constexpr (kType == QFMT_F32) {
+        return __uint_as_float(w);
+    } else if constexpr (kType == QFMT_BF16) {
+        return __uint_as_float((uint32_t)w << 16);
+    } else {
+        float f;
+        asm("cvt.f32.f16 %0, %1;" : "=f"(f) : "h"(w));
+        return f;
+    }
+}
+
+// The words of a granule as they lie in memory: eight for containers, four for codes.
+template <int kType>
+struct Raw {
+    uint32_t w[kType == QFMT_F32 ? 8 : 4];
+};
+
+template <int kType>
+__device__ __forceinline__ Raw<kType> load_raw(const typename Word<kType>::type* p) {
+    Raw<kType> r;
+    if constexpr (kType == QFMT_F32) {
+        asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                     : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]), "=r"(r.w[5]), "=r"(r.w[6]),
+                       "=r"(r.w[7])
+                     : "l"(p));
+    } else {
+        asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];"
+                     : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]) : "l"(p));
+    }
+    return r;
+}
+
+template <int kType>
+__device__ __forceinline__ void store_raw(typename Word<kType>::type* p, const Raw<kType>& r) {
+    if constexpr (kType == QFMT_F32) {
+        asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                     :: "l"(p), "r"(r.w[0]), "r"(r.w[1]), "r"(r.w[2]), "r"(r.w[3]), "r"(r.w[4]), "r"(r.w[5]), "r"(r.w[6]),
+                     "r"(r.w[7]) : "memory");
+    } else {
+        asm volatile("st.global.v4.b32 [%0], {%1,%2,%3,%4};"
+                     :: "l"(p), "r"(r.w[0]), "r"(r.w[1]), "r"(r.w[2]), "r"(r.w[3]) : "memory");
+    }
+}
+
+template <int kType>
+__device__ __forceinline__ void widen_raw(const Raw<kType>& r, float (&v)[kGranule]) {
+#pragma unroll
+    for (int j = 0; j < kGranule; ++j) {
+        if constexpr (kType == QFMT_F32) v[j] = __uint_as_float(r.w[j]);
+        else v[j] = widen<kType>((uint16_t)(j & 1 ? r.w[j / 2] >> 16 : r.w[j / 2] & 0xFFFFu));
+    }
+}
+
+// `n` columns (1..8) of a granule at p as 32-bit values, the others zero.  vec: p is aligned to a full granule.
+template <int kType>
+__device__ __forceinline__ void load_granule(const typename Word<kType>::type* p, int n, bool vec, float (&v)[kGranule]) {
+    if (vec && n == kGranule) {
+        widen_raw<kType>(load_raw<kType>(p), v);
+    } else {
+#pragma unroll
+        for (int j = 0; j < kGranule; ++j) v[j] = j < n ? widen<kType>(p[j]) : 0.0f;
+    }
+}
+
+// Eight finished values to words: rounded once to the storage type (nearest, ties to even), or with kFmt to
+// the format *p, whose statistics are counted in the per-lane histogram `hist` when there is one.
+template <int kType, bool kFmt>
+__device__ __forceinline__ Raw<kType> finish(const float (&v)[kGranule], int n, const QuantParams& p, uint32_t* hist) {
+    Raw<kType> r;
+    int bin[kGranule];
+    if constexpr (kType == QFMT_F32) {
+#pragma unroll
+        for (int j = 0; j < kGranule; ++j)
+            r.w[j] = kFmt ? quantize_one<false>(__float_as_uint(v[j]), p, bin[j]) : __float_as_uint(v[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < kGranule / 2; ++j) {
+            if constexpr (kFmt)
+                r.w[j] = quantize_pack_pair_native<false, kType == QFMT_BF16>(__float_as_uint(v[2 * j]), __float_as_uint(v[2 * j + 1]),
+                                                                              p, bin[2 * j], bin[2 * j + 1]);
+            else if constexpr (kType == QFMT_BF16)
+                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r.w[j]) : "f"(v[2 * j + 1]), "f"(v[2 * j]));
+            else
+                asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r.w[j]) : "f"(v[2 * j + 1]), "f"(v[2 * j]));
+        }
+    }
+    if constexpr (kFmt) {
+        if (hist != nullptr) {
+            const int lane = threadIdx.x & 31;
+#pragma unroll
+            for (int j = 0; j < kGranule; ++j)
+                if (j < n) atomicAdd(&hist[bin[j] * 32 + lane], 1u);
+        }
+    }
+    return r;
+}
+
+template <int kType>
+__device__ __forceinline__ void store_granule(typename Word<kType>::type* p, int n, bool vec, const Raw<kType>& r) {
+    if (vec && n == kGranule) {
+        store_raw<kType>(p, r);
+    } else {
+#pragma unroll
+        for (int j = 0; j < kGranule; ++j) {
+            if (j < n) {
+                if constexpr (kType == QFMT_F32) p[j] = r.w[j];
+                else p[j] = (uint16_t)(j & 1 ? r.w[j / 2] >> 16 : r.w[j / 2] & 0xFFFFu);
+            }
+        }
+    }
+}
+
+// Philox4x32-10 (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3", SC 2011): ten
+// rounds of two 32 x 32 -> 64-bit products on a counter of four words under a key of two.
+__device__ __forceinline__ uint4 philox4x32_10(uint4 c, uint32_t k0, uint32_t k1) {
+#pragma unroll
+    for (int r = 0; r < 10; ++r) {
+        const uint64_t a = (uint64_t)c.x * 0xD2511F53u, b = (uint64_t)c.z * 0xCD9E8D57u;
+        c = make_uint4((uint32_t)(b >> 32) ^ c.y ^ k0, (uint32_t)b, (uint32_t)(a >> 32) ^ c.w ^ k1, (uint32_t)a);
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    return c;
+}
+
+struct DropParams {
+    uint32_t threshold;  // 16 random bits below this drop their element; 65536 drops every one, 0 none
+    float scale;         // 65536 / (65536 - threshold): the mean is kept exactly for the threshold in use
+    uint32_t key0, key1;
+    uint64_t offset;
+    const uint64_t* d_offset;  // added to offset when the kernel runs, or NULL
+};
+
+__device__ __forceinline__ uint64_t drop_offset(const DropParams& d) {
+    return d.offset + (d.d_offset != nullptr ? *d.d_offset : 0ull);
+}
+
+// D(v) of the granule of columns 8 * granule .. of a row.  A dropped element is zero whatever it held (a
+// selection, not a product: inf and NaN do not get through).
+__device__ __forceinline__ void drop_granule(const DropParams& d, uint64_t offset, uint32_t row, uint32_t granule,
+                                             float (&v)[kGranule]) {
+    const uint4 r = philox4x32_10(make_uint4(granule, row, (uint32_t)offset, (uint32_t)(offset >> 32)), d.key0, d.key1);
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int j = 0; j < kGranule; ++j) {
+        const uint32_t u = j & 1 ? w[j / 2] >> 16 : w[j / 2] & 0xFFFFu;
+        v[j] = u >= d.threshold ? mul_ieee(v[j], d.scale) : 0.0f;
+    }
+}
+
+// Per-lane histogram [bin][lane] in shared memory: cleared by the whole block, merged into the device
+// record by the whole block at the end (round.cuh).
+__device__ __forceinline__ void clear_hist(uint32_t* hist, const QuantParams& p) {
+    for (int i = threadIdx.x; i < (p.top + kExtraBins) * 32; i += blockDim.x) hist[i] = 0u;
+    __syncthreads();
+}
+__device__ __forceinline__ void flush_hist(const uint32_t* hist, const QuantParams& p, qfmt_stats_t* stats, uint64_t n_total) {
+    __syncthreads();
+    const int lane = threadIdx.x & 31;
+    for (int b = (threadIdx.x >> 5) + 1; b < p.top + kExtraBins; b += blockDim.x >> 5) {  // bin 0 is never used
+        const uint32_t c = __reduce_add_sync(0xFFFFFFFFu, hist[b * 32 + lane]);
+        if (lane == 0 && c != 0u) merge_bin(stats, p, b, c);
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) atomicAdd((unsigned long long*)&stats->n_total, (unsigned long long)n_total);
+}
+
+// Host side -----------------------------------------------------------------------------------------------
+
+inline size_t element_size(int32_t dtype) { return dtype == QFMT_F32 ? 4 : 2; }
+inline size_t granule_bytes(int32_t dtype) { return kGranule * element_size(dtype); }
+inline bool element_aligned(const void* p, int32_t dtype) { return (reinterpret_cast<uintptr_t>(p) & (element_size(dtype) - 1)) == 0; }
+// Whether every full granule of every row of a matrix may be moved by one access.
+inline bool granule_aligned(const void* p, int64_t ld, int32_t dtype) {
+    return p == nullptr || ((reinterpret_cast<uintptr_t>(p) & (granule_bytes(dtype) - 1)) == 0 && ld % kGranule == 0);
+}
+
+inline int make_drop_params(const qfmt_dropout_t* d, DropParams* out) {
+    *out = DropParams{0u, 1.0f, 0u, 0u, 0ull, nullptr};
+    if (d == nullptr) return QFMT_OK;
+    if (!(d->p >= 0.0f && d->p <= 1.0f) || (reinterpret_cast<uintptr_t>(d->d_offset) & 7u)) return QFMT_ERR_BAD_ARG;
+    out->threshold = (uint32_t)((double)d->p * 65536.0 + 0.5);
+    out->scale = out->threshold < 65536u ? (float)(65536.0 / (65536.0 - (double)out->threshold)) : 0.0f;
+    out->key0 = (uint32_t)d->seed;
+    out->key1 = (uint32_t)(d->seed >> 32);
+    out->offset = d->offset;
+    out->d_offset = d->d_offset;
+    return QFMT_OK;
+}
+
+}  // namespace
+}  // namespace qfmt
