@@ -93,6 +93,13 @@ __device__ __forceinline__ void load_granule(const typename Word<kType>::type* p
     }
 }
 
+// The same for a row whose granules are all whole and aligned (kVec), or for any row.
+template <int kType, bool kVec>
+__device__ __forceinline__ void load_granule(const typename Word<kType>::type* p, int n, float (&v)[kGranule]) {
+    if constexpr (kVec) widen_raw<kType>(load_raw<kType>(p), v);
+    else load_granule<kType>(p, n, false, v);
+}
+
 // Eight finished values to words: rounded once to the storage type (nearest, ties to even), or with kFmt to
 // the format *p, whose statistics are counted in the per-lane histogram `hist` when there is one.
 template <int kType, bool kFmt>
@@ -139,6 +146,12 @@ __device__ __forceinline__ void store_granule(typename Word<kType>::type* p, int
             }
         }
     }
+}
+
+template <int kType, bool kVec>
+__device__ __forceinline__ void store_granule(typename Word<kType>::type* p, int n, const Raw<kType>& r) {
+    if constexpr (kVec) store_raw<kType>(p, r);
+    else store_granule<kType>(p, n, false, r);
 }
 
 // Philox4x32-10 (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3", SC 2011): ten

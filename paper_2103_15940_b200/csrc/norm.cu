@@ -33,6 +33,7 @@ struct ForwardArgs {
     int64_t rows, cols;
     float eps;
     bool vec;
+    bool fmt;  // quant holds a format to round to
     DropParams drop;
     QuantParams quant;
     qfmt_stats_t* stats;
@@ -53,6 +54,7 @@ struct BackwardArgs {
     int64_t ld_dy, ld_dh, ld_h, ld_dx, ld_dresidual;
     int64_t rows, cols;
     bool vec;
+    bool fmt;  // quant holds a format to round to
     DropParams drop;
     QuantParams quant;
     qfmt_stats_t* stats;
@@ -80,10 +82,17 @@ __device__ __forceinline__ void load_h(const ForwardArgs<kType>& a, int64_t row,
     }
 }
 
-// `n` entries of a vector of one value per column, or `fill` where there is none.
+// `n` entries of a vector of one value per column, or `fill` where there is none.  kVec: all eight, aligned.
+template <bool kVec>
 __device__ __forceinline__ void load_columns(const float* p, int64_t col, int n, float fill, float (&v)[kGranule]) {
+    if (kVec && p != nullptr) {
+        const float4 lo = __ldg(reinterpret_cast<const float4*>(p + col)), hi = __ldg(reinterpret_cast<const float4*>(p + col) + 1);
+        v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w;
+        v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
+    } else {
 #pragma unroll
-    for (int j = 0; j < kGranule; ++j) v[j] = p != nullptr && j < n ? p[col + j] : fill;
+        for (int j = 0; j < kGranule; ++j) v[j] = p != nullptr && j < n ? __ldg(p + col + j) : fill;
+    }
 }
 
 // Sum over the block in every thread, in a fixed order.  `scratch` holds one entry per warp.
@@ -151,11 +160,124 @@ __global__ void __launch_bounds__(kLoopThreads) norm_forward_loop_kernel(const F
             load_h<kType, kFused>(a, row, g, n, offset, v);
             if (kFused && a.h != nullptr)
                 store_granule<kType>(a.h + row * a.ld_h + col, n, a.vec, finish<kType, false>(v, n, a.quant, nullptr));
-            load_columns(a.weight, col, n, 1.0f, w);
-            load_columns(a.bias, col, n, 0.0f, b);
+            load_columns<false>(a.weight, col, n, 1.0f, w);
+            load_columns<false>(a.bias, col, n, 0.0f, b);
 #pragma unroll
             for (int j = 0; j < kGranule; ++j) v[j] = __fmaf_rn((v[j] - mean) * rstd, w[j], b[j]);
             store_granule<kType>(a.y + row * a.ld_y + col, n, a.vec, finish<kType, kFmt>(v, n, a.quant, hist));
+        }
+    }
+    if (hist != nullptr) flush_hist(hist, a.quant, a.stats, (uint64_t)a.rows * (uint64_t)a.cols);
+}
+
+// Teams: the threads that share a row.  A team of up to 32 threads is an aligned part of a warp; a larger
+// one is whole warps.  Granule k * team + t of the row is thread t's k-th.
+
+// Sum over a team in every thread, in a fixed order.  scratch: 16 entries per team, of which those past the
+// team's warps are zero; one barrier, so the next sum needs another scratch.
+__device__ __forceinline__ float2 team_sum(float2 s, int team, int t, int barrier, float2* scratch) {
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) {
+        if (off < team) {
+            s.x += __shfl_xor_sync(0xFFFFFFFFu, s.x, off);
+            s.y += __shfl_xor_sync(0xFFFFFFFFu, s.y, off);
+        }
+    }
+    if (team > 32) {
+        if ((t & 31) == 0) scratch[t >> 5] = s;
+        asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(team) : "memory");
+        const float4* q = reinterpret_cast<const float4*>(scratch);
+        s = make_float2(0.0f, 0.0f);
+        for (int i = 0; i < team; i += 128) {  // four warps' entries
+            const float4 u = q[i / 64], v = q[i / 64 + 1];
+            s.x += (u.x + u.z) + (v.x + v.z);
+            s.y += (u.y + u.w) + (v.y + v.w);
+        }
+    }
+    return s;
+}
+
+constexpr int kRowThreads = 512;
+
+// A row is read once and stays in its team's registers.
+template <int kType, int V, bool kFused, bool kVec>
+__global__ void __launch_bounds__(kRowThreads) norm_forward_rows_kernel(const ForwardArgs<kType> a, int team) {
+    extern __shared__ uint32_t lane_hist[];
+    __shared__ float2 scratch[2][16];
+    uint32_t* hist = a.stats != nullptr ? lane_hist : nullptr;
+    if (team > 32) {
+        if (threadIdx.x < 32) scratch[threadIdx.x >> 4][threadIdx.x & 15] = make_float2(0.0f, 0.0f);
+        __syncthreads();
+    }
+    if (hist != nullptr) clear_hist(hist, a.quant);
+    const int t = team > 32 ? (int)threadIdx.x : (int)threadIdx.x & (team - 1);
+    const int teams = blockDim.x / team;
+    const float inverse = 1.0f / (float)a.cols;
+    const uint64_t offset = kFused ? drop_offset(a.drop) : 0ull;
+    // the last teams of a warp may have no row while its other teams have one: they go through the motions
+    for (int64_t base = (int64_t)blockIdx.x * teams; base < a.rows; base += (int64_t)gridDim.x * teams) {
+        const int64_t row = base + threadIdx.x / team;
+        float v[V][kGranule];
+        float2 s = make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const int64_t col = (int64_t)(k * team + t) * kGranule;
+            const int n = row < a.rows && col < a.cols ? granule_columns(a.cols, col) : 0;
+#pragma unroll
+            for (int j = 0; j < kGranule; ++j) v[k][j] = 0.0f;
+            if (n > 0) load_granule<kType, kVec>(a.x + row * a.ld_x + col, n, v[k]);
+        }
+        if constexpr (kFused) {
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                const int64_t col = (int64_t)(k * team + t) * kGranule;
+                const int n = row < a.rows && col < a.cols ? granule_columns(a.cols, col) : 0;
+                if (n > 0) {
+                    float r[kGranule];
+                    if (a.residual != nullptr) load_granule<kType, kVec>(a.residual + row * a.ld_residual + col, n, r);
+                    if (a.drop.threshold != 0u) drop_granule(a.drop, offset, (uint32_t)row, k * team + t, v[k]);
+                    if (a.residual != nullptr) {
+#pragma unroll
+                        for (int j = 0; j < kGranule; ++j) v[k][j] = add_ieee(r[j], v[k][j]);
+                    }
+                    if (a.h != nullptr)
+                        store_granule<kType, kVec>(a.h + row * a.ld_h + col, n, finish<kType, false>(v[k], n, a.quant, nullptr));
+                }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+#pragma unroll
+            for (int j = 0; j < kGranule; ++j) s.x += v[k][j];
+        const float mean = team_sum(s, team, t, 1, scratch[0]).x * inverse;
+        s.x = 0.0f;
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const int64_t col = (int64_t)(k * team + t) * kGranule;
+#pragma unroll
+            for (int j = 0; j < kGranule; ++j) {
+                v[k][j] = col + j < a.cols ? v[k][j] - mean : 0.0f;
+                s.x = __fmaf_rn(v[k][j], v[k][j], s.x);
+            }
+        }
+        const float rstd = 1.0f / sqrtf(team_sum(s, team, t, 1, scratch[1]).x * inverse + a.eps);
+        if (t == 0 && row < a.rows) {
+            if (a.mean != nullptr) a.mean[row] = mean;
+            if (a.rstd != nullptr) a.rstd[row] = rstd;
+        }
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const int64_t col = (int64_t)(k * team + t) * kGranule;
+            const int n = row < a.rows && col < a.cols ? granule_columns(a.cols, col) : 0;
+            if (n > 0) {
+                float w[kGranule], b[kGranule];
+                load_columns<kVec>(a.weight, col, n, 1.0f, w);
+                load_columns<kVec>(a.bias, col, n, 0.0f, b);
+#pragma unroll
+                for (int j = 0; j < kGranule; ++j) v[k][j] = __fmaf_rn(v[k][j] * rstd, w[j], b[j]);
+                store_granule<kType, kVec>(a.y + row * a.ld_y + col, n,
+                                           a.fmt ? finish<kType, true>(v[k], n, a.quant, hist) : finish<kType, false>(v[k], n, a.quant, nullptr));
+            }
         }
     }
     if (hist != nullptr) flush_hist(hist, a.quant, a.stats, (uint64_t)a.rows * (uint64_t)a.cols);
@@ -188,7 +310,7 @@ __global__ void __launch_bounds__(kLoopThreads) norm_backward_loop_kernel(const 
             const int n = granule_columns(a.cols, col);
             float xhat[kGranule], dy[kGranule], w[kGranule];
             load_xhat_dy<kType>(a, row, col, n, mean, rstd, xhat, dy);
-            load_columns(a.weight, col, n, 1.0f, w);
+            load_columns<false>(a.weight, col, n, 1.0f, w);
 #pragma unroll
             for (int j = 0; j < kGranule; ++j) {
                 const float t = dy[j] * w[j];
@@ -203,7 +325,7 @@ __global__ void __launch_bounds__(kLoopThreads) norm_backward_loop_kernel(const 
             const int n = granule_columns(a.cols, col);
             float xhat[kGranule], dy[kGranule], w[kGranule];
             load_xhat_dy<kType>(a, row, col, n, mean, rstd, xhat, dy);
-            load_columns(a.weight, col, n, 1.0f, w);
+            load_columns<false>(a.weight, col, n, 1.0f, w);
 #pragma unroll
             for (int j = 0; j < kGranule; ++j) dy[j] = rstd * (__fmaf_rn(dy[j], w[j], -c1) - xhat[j] * c2);
             if (kFused) {
@@ -330,10 +452,44 @@ int prepare_call(const qfmt_norm_t* norm, const qfmt_dropout_t* drop, const qfmt
 
 bool float_aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
-template <int kType, bool kFused, bool kFmt>
+// Threads that share a row and the granules each of them holds: the fewest that cover it with at most four
+// granules a thread (fewer barriers and shuffles per element than one granule a thread).
+struct Team {
+    int threads, granules;
+};
+Team forward_team(int64_t cols) {
+    const int64_t g = (cols + kGranule - 1) / kGranule;
+    if (g > 4 * kRowThreads) return {0, 0};
+    if (g <= 32) {
+        int threads = 1;
+        while (threads < g) threads *= 2;
+        return {threads, 1};
+    }
+    if (g <= 64) return {32, 2};
+    return {(int)((g + 127) / 128) * 32, 4};
+}
+
+bool column_aligned(const float* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+template <int kType, bool kFused>
 int launch_forward(const Call& c, const ForwardArgs<kType>& a, cudaStream_t stream) {
-    const int64_t cap = (int64_t)c.dev.sm_count * 4;
-    norm_forward_loop_kernel<kType, kFused, kFmt><<<(unsigned)(a.rows < cap ? a.rows : cap), kLoopThreads, c.hist_bytes, stream>>>(a);
+    const Team team = forward_team(a.cols);
+    if (team.threads != 0) {
+        const bool vec = a.vec && a.cols % kGranule == 0 && column_aligned(a.weight) && column_aligned(a.bias);
+        const unsigned block = team.threads > 32 ? team.threads : 128;
+        const int64_t want = (a.rows * team.threads + block - 1) / block, cap = (int64_t)c.dev.sm_count * 32;
+        const auto kern = vec ? (team.granules == 1   ? norm_forward_rows_kernel<kType, 1, kFused, true>
+                                 : team.granules == 2 ? norm_forward_rows_kernel<kType, 2, kFused, true>
+                                                      : norm_forward_rows_kernel<kType, 4, kFused, true>)
+                              : (team.granules == 1   ? norm_forward_rows_kernel<kType, 1, kFused, false>
+                                 : team.granules == 2 ? norm_forward_rows_kernel<kType, 2, kFused, false>
+                                                      : norm_forward_rows_kernel<kType, 4, kFused, false>);
+        kern<<<(unsigned)(want < cap ? want : cap), block, c.hist_bytes, stream>>>(a, team.threads);
+    } else {
+        const int64_t cap = (int64_t)c.dev.sm_count * 4;
+        const auto kern = c.fmt ? norm_forward_loop_kernel<kType, kFused, true> : norm_forward_loop_kernel<kType, kFused, false>;
+        kern<<<(unsigned)(a.rows < cap ? a.rows : cap), kLoopThreads, c.hist_bytes, stream>>>(a);
+    }
     QFMT_CUDA_TRY(cudaGetLastError());
     return QFMT_OK;
 }
@@ -360,10 +516,11 @@ int forward(const Call& c, const void* d_x, const void* d_residual, const float*
     a.eps = c.norm.eps;
     a.vec = granule_aligned(d_x, a.ld_x, kType) && granule_aligned(d_residual, a.ld_residual, kType) &&
             granule_aligned(d_h, a.ld_h, kType) && granule_aligned(d_y, a.ld_y, kType);
+    a.fmt = c.fmt;
     a.drop = c.drop;
     a.quant = c.quant;
     a.stats = d_stats;
-    return c.fmt ? launch_forward<kType, kFused, true>(c, a, stream) : launch_forward<kType, kFused, false>(c, a, stream);
+    return launch_forward<kType, kFused>(c, a, stream);
 }
 
 int forward_entry(const qfmt_norm_t* norm, const qfmt_dropout_t* drop, bool fused, const void* d_x, const void* d_residual,
@@ -429,6 +586,7 @@ int backward(const Call& c, const void* d_dy, const void* d_dh, const void* d_h,
     a.cols = c.norm.cols;
     a.vec = granule_aligned(d_dy, a.ld_dy, kType) && granule_aligned(d_dh, a.ld_dh, kType) && granule_aligned(d_h, a.ld_h, kType) &&
             granule_aligned(d_dx, a.ld_dx, kType) && granule_aligned(d_dresidual, a.ld_dresidual, kType);
+    a.fmt = c.fmt;
     a.drop = c.drop;
     a.quant = c.quant;
     a.stats = d_stats;
