@@ -196,8 +196,9 @@ def _ptr(x) -> Optional[int]:
 
 def _stream_handle(stream) -> Optional[int]:
     if stream is None:
+        # the raw handle: building torch's stream object for it takes 3 us, as long as a launch
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream

@@ -29,6 +29,8 @@ struct DropArgs {
 
 template <int kType>
 __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropArgs<kType> a) {
+    grid_launch_dependents();
+    grid_dependency_wait();
     const uint64_t total = (uint64_t)a.rows * a.granules;
     const uint64_t offset = drop_offset(a.drop);
     for (uint64_t i = (uint64_t)blockIdx.x * kDropThreads + threadIdx.x; i < total; i += (uint64_t)gridDim.x * kDropThreads) {
@@ -36,16 +38,14 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropArgs<kT
         const uint32_t g = (uint32_t)(i - row * a.granules);
         const int64_t col = (int64_t)g * kGranule;
         const int n = a.cols - col < kGranule ? (int)(a.cols - col) : kGranule;
-        float v[kGranule];
-        load_granule<kType>(a.x + row * a.ld_x + col, n, a.vec, v);
-        if (a.drop.threshold != 0u) drop_granule(a.drop, offset, (uint32_t)row, g, v);
+        Granule v = widen_raw<kType>(load_words<kType>(a.x + row * a.ld_x + col, n, a.vec));
+        if (a.drop.active) drop_granule(a.drop, offset, (uint32_t)row, g, v);
         if (a.residual != nullptr) {
-            float r[kGranule];
-            load_granule<kType>(a.residual + row * a.ld_residual + col, n, a.vec, r);
+            const Granule r = widen_raw<kType>(load_words<kType>(a.residual + row * a.ld_residual + col, n, a.vec));
 #pragma unroll
-            for (int j = 0; j < kGranule; ++j) v[j] = add_ieee(r[j], v[j]);
+            for (int j = 0; j < 4; ++j) v.p[j] = add2(r.p[j], v.p[j]);
         }
-        store_granule<kType>(a.out + row * a.ld_out + col, n, a.vec, finish<kType, false>(v, n, QuantParams{}, nullptr));
+        store_words<kType>(a.out + row * a.ld_out + col, n, a.vec, finish<kType>(v));
     }
 }
 
@@ -68,8 +68,7 @@ int launch_dropout(const void* d_x, int64_t ld_x, const void* d_residual, int64_
     a.drop = drop;
     const uint64_t blocks = ((uint64_t)rows * a.granules + kDropThreads - 1) / kDropThreads;
     const uint64_t cap = (uint64_t)dev.sm_count * 16;
-    dropout_kernel<kType><<<(unsigned)(blocks < cap ? blocks : cap), kDropThreads, 0, stream>>>(a);
-    QFMT_CUDA_TRY(cudaGetLastError());
+    QFMT_CUDA_TRY(launch_overlapping(dropout_kernel<kType>, (unsigned)(blocks < cap ? blocks : cap), kDropThreads, 0, stream, a));
     return QFMT_OK;
 }
 

@@ -73,68 +73,118 @@ __device__ __forceinline__ void store_raw(typename Word<kType>::type* p, const R
     }
 }
 
+// The eight columns of a granule as four pairs: additions and products on pairs issue as one instruction each
+// (two IEEE results), which halves what the passes issue per element.
+struct Granule {
+    float2 p[4];
+    __device__ __forceinline__ float& at(int j) { return j & 1 ? p[j / 2].y : p[j / 2].x; }
+    __device__ __forceinline__ float at(int j) const { return j & 1 ? p[j / 2].y : p[j / 2].x; }
+};
+
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 r;
+    asm("{ .reg .b64 a, b, r; mov.b64 a, {%2, %3}; mov.b64 b, {%4, %5}; add.rn.f32x2 r, a, b; mov.b64 {%0, %1}, r; }"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 r;
+    asm("{ .reg .b64 a, b, r; mov.b64 a, {%2, %3}; mov.b64 b, {%4, %5}; mul.rn.f32x2 r, a, b; mov.b64 {%0, %1}, r; }"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 r;
+    asm("{ .reg .b64 a, b, c, r; mov.b64 a, {%2, %3}; mov.b64 b, {%4, %5}; mov.b64 c, {%6, %7}; fma.rn.f32x2 r, a, b, c;"
+        " mov.b64 {%0, %1}, r; }"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return r;
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+__device__ __forceinline__ Granule splat(float v) {
+    Granule g;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) g.p[j] = both(v);
+    return g;
+}
+
 template <int kType>
-__device__ __forceinline__ void widen_raw(const Raw<kType>& r, float (&v)[kGranule]) {
+__device__ __forceinline__ Granule widen_raw(const Raw<kType>& r) {
+    Granule g;
 #pragma unroll
-    for (int j = 0; j < kGranule; ++j) {
-        if constexpr (kType == QFMT_F32) v[j] = __uint_as_float(r.w[j]);
-        else v[j] = widen<kType>((uint16_t)(j & 1 ? r.w[j / 2] >> 16 : r.w[j / 2] & 0xFFFFu));
-    }
-}
-
-// `n` columns (1..8) of a granule at p as 32-bit values, the others zero.  vec: p is aligned to a full granule.
-template <int kType>
-__device__ __forceinline__ void load_granule(const typename Word<kType>::type* p, int n, bool vec, float (&v)[kGranule]) {
-    if (vec && n == kGranule) {
-        widen_raw<kType>(load_raw<kType>(p), v);
-    } else {
-#pragma unroll
-        for (int j = 0; j < kGranule; ++j) v[j] = j < n ? widen<kType>(p[j]) : 0.0f;
-    }
-}
-
-// The same for a row whose granules are all whole and aligned (kVec), or for any row.
-template <int kType, bool kVec>
-__device__ __forceinline__ void load_granule(const typename Word<kType>::type* p, int n, float (&v)[kGranule]) {
-    if constexpr (kVec) widen_raw<kType>(load_raw<kType>(p), v);
-    else load_granule<kType>(p, n, false, v);
-}
-
-// Eight finished values to words: rounded once to the storage type (nearest, ties to even), or with kFmt to
-// the format *p, whose statistics are counted in the per-lane histogram `hist` when there is one.
-template <int kType, bool kFmt>
-__device__ __forceinline__ Raw<kType> finish(const float (&v)[kGranule], int n, const QuantParams& p, uint32_t* hist) {
-    Raw<kType> r;
-    int bin[kGranule];
-    if constexpr (kType == QFMT_F32) {
-#pragma unroll
-        for (int j = 0; j < kGranule; ++j)
-            r.w[j] = kFmt ? quantize_one<false>(__float_as_uint(v[j]), p, bin[j]) : __float_as_uint(v[j]);
-    } else {
-#pragma unroll
-        for (int j = 0; j < kGranule / 2; ++j) {
-            if constexpr (kFmt)
-                r.w[j] = quantize_pack_pair_native<false, kType == QFMT_BF16>(__float_as_uint(v[2 * j]), __float_as_uint(v[2 * j + 1]),
-                                                                              p, bin[2 * j], bin[2 * j + 1]);
-            else if constexpr (kType == QFMT_BF16)
-                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r.w[j]) : "f"(v[2 * j + 1]), "f"(v[2 * j]));
-            else
-                asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r.w[j]) : "f"(v[2 * j + 1]), "f"(v[2 * j]));
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (kType == QFMT_F32) {
+            g.p[j] = make_float2(__uint_as_float(r.w[2 * j]), __uint_as_float(r.w[2 * j + 1]));
+        } else if constexpr (kType == QFMT_BF16) {
+            g.p[j] = make_float2(__uint_as_float(r.w[j] << 16), __uint_as_float(r.w[j] & 0xFFFF0000u));
+        } else {
+            asm("{ .reg .b16 lo, hi; mov.b32 {lo, hi}, %2; cvt.f32.f16 %0, lo; cvt.f32.f16 %1, hi; }"
+                : "=f"(g.p[j].x), "=f"(g.p[j].y) : "r"(r.w[j]));
         }
     }
-    if constexpr (kFmt) {
-        if (hist != nullptr) {
-            const int lane = threadIdx.x & 31;
+    return g;
+}
+
+// The words of `n` columns (1..8) of a granule at p, the others zero.  vec: p is aligned to a whole granule.
+template <int kType>
+__device__ __forceinline__ Raw<kType> load_words(const typename Word<kType>::type* p, int n, bool vec) {
+    if (vec && n == kGranule) return load_raw<kType>(p);
+    Raw<kType> r;
 #pragma unroll
-            for (int j = 0; j < kGranule; ++j)
-                if (j < n) atomicAdd(&hist[bin[j] * 32 + lane], 1u);
+    for (int j = 0; j < kGranule; ++j) {
+        const uint32_t w = j < n ? (uint32_t)p[j] : 0u;
+        if constexpr (kType == QFMT_F32) r.w[j] = w;
+        else r.w[j / 2] = j & 1 ? r.w[j / 2] | (w << 16) : w;
+    }
+    return r;
+}
+
+// Eight finished values to words, rounded once to the storage type (nearest, ties to even).
+template <int kType>
+__device__ __forceinline__ Raw<kType> finish(const Granule& v) {
+    Raw<kType> r;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (kType == QFMT_F32) {
+            r.w[2 * j] = __float_as_uint(v.p[j].x);
+            r.w[2 * j + 1] = __float_as_uint(v.p[j].y);
+        } else if constexpr (kType == QFMT_BF16) {
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r.w[j]) : "f"(v.p[j].y), "f"(v.p[j].x));
+        } else {
+            asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r.w[j]) : "f"(v.p[j].y), "f"(v.p[j].x));
         }
     }
     return r;
 }
 
+// The same rounded to the format *p (for codes, the one of their storage type); the bins of the first `n`
+// columns are counted in the per-lane histogram `hist` when there is one.
 template <int kType>
-__device__ __forceinline__ void store_granule(typename Word<kType>::type* p, int n, bool vec, const Raw<kType>& r) {
+__device__ __forceinline__ Raw<kType> finish_format(const Granule& v, int n, const QuantParams& p, uint32_t* hist) {
+    Raw<kType> r;
+    int bin[kGranule];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t x = __float_as_uint(v.p[j].x), y = __float_as_uint(v.p[j].y);
+        if constexpr (kType == QFMT_F32) {
+            r.w[2 * j] = quantize_one<false>(x, p, bin[2 * j]);
+            r.w[2 * j + 1] = quantize_one<false>(y, p, bin[2 * j + 1]);
+        } else {
+            r.w[j] = quantize_pack_pair_native<false, kType == QFMT_BF16>(x, y, p, bin[2 * j], bin[2 * j + 1]);
+        }
+    }
+    if (hist != nullptr) {
+        const int lane = threadIdx.x & 31;
+#pragma unroll
+        for (int j = 0; j < kGranule; ++j)
+            if (j < n) atomicAdd(&hist[bin[j] * 32 + lane], 1u);
+    }
+    return r;
+}
+
+template <int kType>
+__device__ __forceinline__ void store_words(typename Word<kType>::type* p, int n, bool vec, const Raw<kType>& r) {
     if (vec && n == kGranule) {
         store_raw<kType>(p, r);
     } else {
@@ -146,12 +196,6 @@ __device__ __forceinline__ void store_granule(typename Word<kType>::type* p, int
             }
         }
     }
-}
-
-template <int kType, bool kVec>
-__device__ __forceinline__ void store_granule(typename Word<kType>::type* p, int n, const Raw<kType>& r) {
-    if constexpr (kVec) store_raw<kType>(p, r);
-    else store_granule<kType>(p, n, false, r);
 }
 
 // Philox4x32-10 (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3", SC 2011): ten
@@ -168,8 +212,9 @@ __device__ __forceinline__ uint4 philox4x32_10(uint4 c, uint32_t k0, uint32_t k1
 }
 
 struct DropParams {
-    uint32_t threshold;  // 16 random bits below this drop their element; 65536 drops every one, 0 none
-    float scale;         // 65536 / (65536 - threshold): the mean is kept exactly for the threshold in use
+    uint32_t active;  // 0: nothing is dropped
+    uint32_t limit;   // 65536 t - 1: 16 random bits, moved to the top of a word, at or below this drop their element
+    float scale;      // 65536 / (65536 - t): the mean is kept exactly for the threshold in use
     uint32_t key0, key1;
     uint64_t offset;
     const uint64_t* d_offset;  // added to offset when the kernel runs, or NULL
@@ -180,15 +225,16 @@ __device__ __forceinline__ uint64_t drop_offset(const DropParams& d) {
 }
 
 // D(v) of the granule of columns 8 * granule .. of a row.  A dropped element is zero whatever it held (a
-// selection, not a product: inf and NaN do not get through).
-__device__ __forceinline__ void drop_granule(const DropParams& d, uint64_t offset, uint32_t row, uint32_t granule,
-                                             float (&v)[kGranule]) {
+// selection, not a product: inf and NaN do not get through).  The upper half of a random word is compared in
+// place (its lower half cannot reach the limit's ones), the lower half after a shift.
+__device__ __forceinline__ void drop_granule(const DropParams& d, uint64_t offset, uint32_t row, uint32_t granule, Granule& v) {
     const uint4 r = philox4x32_10(make_uint4(granule, row, (uint32_t)offset, (uint32_t)(offset >> 32)), d.key0, d.key1);
     const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-    for (int j = 0; j < kGranule; ++j) {
-        const uint32_t u = j & 1 ? w[j / 2] >> 16 : w[j / 2] & 0xFFFFu;
-        v[j] = u >= d.threshold ? mul_ieee(v[j], d.scale) : 0.0f;
+    for (int j = 0; j < 4; ++j) {
+        const float2 s = mul2(v.p[j], both(d.scale));
+        v.p[j].x = (w[j] << 16) > d.limit ? s.x : 0.0f;
+        v.p[j].y = w[j] > d.limit ? s.y : 0.0f;
     }
 }
 
@@ -219,11 +265,13 @@ inline bool granule_aligned(const void* p, int64_t ld, int32_t dtype) {
 }
 
 inline int make_drop_params(const qfmt_dropout_t* d, DropParams* out) {
-    *out = DropParams{0u, 1.0f, 0u, 0u, 0ull, nullptr};
+    *out = DropParams{};
     if (d == nullptr) return QFMT_OK;
     if (!(d->p >= 0.0f && d->p <= 1.0f) || (reinterpret_cast<uintptr_t>(d->d_offset) & 7u)) return QFMT_ERR_BAD_ARG;
-    out->threshold = (uint32_t)((double)d->p * 65536.0 + 0.5);
-    out->scale = out->threshold < 65536u ? (float)(65536.0 / (65536.0 - (double)out->threshold)) : 0.0f;
+    const uint32_t t = (uint32_t)((double)d->p * 65536.0 + 0.5);
+    out->active = t != 0u;
+    out->limit = (t << 16) - 1u;  // t = 65536: all ones, which nothing exceeds
+    out->scale = t < 65536u ? (float)(65536.0 / (65536.0 - (double)t)) : 0.0f;
     out->key0 = (uint32_t)d->seed;
     out->key1 = (uint32_t)(d->seed >> 32);
     out->offset = d->offset;

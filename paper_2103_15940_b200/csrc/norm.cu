@@ -10,6 +10,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
 #include <cmath>
 
 #include "common.cuh"
@@ -32,7 +33,7 @@ struct ForwardArgs {
     int64_t ld_x, ld_residual, ld_h, ld_y;
     int64_t rows, cols;
     float eps;
-    bool vec;
+    bool vec;  // every granule whole and aligned
     bool fmt;  // quant holds a format to round to
     DropParams drop;
     QuantParams quant;
@@ -53,46 +54,93 @@ struct BackwardArgs {
     float* partial;  // [parts][2][cols] sums of dy xhat and dy over a part of the rows, or NULL
     int64_t ld_dy, ld_dh, ld_h, ld_dx, ld_dresidual;
     int64_t rows, cols;
-    bool vec;
+    bool vec;  // every granule whole and aligned
     bool fmt;  // quant holds a format to round to
     DropParams drop;
     QuantParams quant;
     qfmt_stats_t* stats;
 };
 
-__device__ __forceinline__ int granule_columns(int64_t cols, int64_t col) {
-    const int64_t left = cols - col;
-    return left < kGranule ? (int)left : kGranule;
+// Columns of granule g that exist, 0..8.
+__device__ __forceinline__ int granule_columns(int64_t cols, int64_t g) {
+    const int64_t left = cols - g * kGranule;
+    return left >= kGranule ? kGranule : left > 0 ? (int)left : 0;
 }
 
-// h of one granule: x, or residual + D(x).
-template <int kType, bool kFused>
-__device__ __forceinline__ void load_h(const ForwardArgs<kType>& a, int64_t row, uint32_t g, int n, uint64_t offset,
-                                       float (&v)[kGranule]) {
-    const int64_t col = (int64_t)g * kGranule;
-    load_granule<kType>(a.x + row * a.ld_x + col, n, a.vec, v);
-    if constexpr (kFused) {
-        if (a.drop.threshold != 0u) drop_granule(a.drop, offset, (uint32_t)row, g, v);
-        if (a.residual != nullptr) {
-            float r[kGranule];
-            load_granule<kType>(a.residual + row * a.ld_residual + col, n, a.vec, r);
-#pragma unroll
-            for (int j = 0; j < kGranule; ++j) v[j] = add_ieee(r[j], v[j]);
-        }
-    }
-}
-
-// `n` entries of a vector of one value per column, or `fill` where there is none.  kVec: all eight, aligned.
-template <bool kVec>
-__device__ __forceinline__ void load_columns(const float* p, int64_t col, int n, float fill, float (&v)[kGranule]) {
-    if (kVec && p != nullptr) {
-        const float4 lo = __ldg(reinterpret_cast<const float4*>(p + col)), hi = __ldg(reinterpret_cast<const float4*>(p + col) + 1);
-        v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w;
-        v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
+// `n` entries of granule g of a vector of one value per column, or `fill` where there is none.
+__device__ __forceinline__ Granule load_columns(const float* p, int64_t g, int n, float fill) {
+    Granule v = splat(fill);
+    if (p == nullptr) return v;
+    p += g * kGranule;
+    if (n == kGranule && (reinterpret_cast<uintptr_t>(p) & 15u) == 0) {
+        const float4 lo = __ldg(reinterpret_cast<const float4*>(p)), hi = __ldg(reinterpret_cast<const float4*>(p) + 1);
+        v.p[0] = make_float2(lo.x, lo.y), v.p[1] = make_float2(lo.z, lo.w);
+        v.p[2] = make_float2(hi.x, hi.y), v.p[3] = make_float2(hi.z, hi.w);
     } else {
 #pragma unroll
-        for (int j = 0; j < kGranule; ++j) v[j] = p != nullptr && j < n ? __ldg(p + col + j) : fill;
+        for (int j = 0; j < kGranule; ++j)
+            if (j < n) v.at(j) = __ldg(p + j);
     }
+    return v;
+}
+
+// Granule g (of n columns) of a row.  kVec: whole and aligned.
+template <int kType, bool kVec>
+__device__ __forceinline__ Raw<kType> fetch(const typename Word<kType>::type* row, uint32_t g, int n, bool vec) {
+    const typename Word<kType>::type* p = row + (int64_t)g * kGranule;
+    if constexpr (kVec) return load_raw<kType>(p);
+    else return load_words<kType>(p, n, vec);
+}
+template <int kType, bool kVec>
+__device__ __forceinline__ void put(typename Word<kType>::type* row, uint32_t g, int n, bool vec, const Raw<kType>& r) {
+    typename Word<kType>::type* p = row + (int64_t)g * kGranule;
+    if constexpr (kVec) store_raw<kType>(p, r);
+    else store_words<kType>(p, n, vec, r);
+}
+template <int kType>
+__device__ __forceinline__ Raw<kType> no_words() {
+    Raw<kType> r;
+#pragma unroll
+    for (uint32_t& w : r.w) w = 0u;
+    return r;
+}
+
+// residual + D(x)
+template <int kType, bool kFused>
+__device__ __forceinline__ Granule join_h(const ForwardArgs<kType>& a, const Raw<kType>& x, const Raw<kType>& r, uint64_t offset, int64_t row,
+                                          uint32_t g) {
+    Granule v = widen_raw<kType>(x);
+    if constexpr (kFused) {
+        if (a.drop.active) drop_granule(a.drop, offset, (uint32_t)row, g, v);
+        if (a.residual != nullptr) {
+            const Granule u = widen_raw<kType>(r);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v.p[j] = add2(u.p[j], v.p[j]);
+        }
+    }
+    return v;
+}
+
+template <int kType, typename Args>
+__device__ __forceinline__ Raw<kType> finish_output(const Args& a, const Granule& v, int n, uint32_t* hist) {
+    return a.fmt ? finish_format<kType>(v, n, a.quant, hist) : finish<kType>(v);
+}
+
+__device__ __forceinline__ float sum8(const Granule& v) {
+    const float2 s = add2(add2(v.p[0], v.p[1]), add2(v.p[2], v.p[3]));
+    return s.x + s.y;
+}
+// v - mean where a column exists, 0 elsewhere; the sum of its squares.
+__device__ __forceinline__ float centre(Granule& v, float mean, int n) {
+    float2 s = make_float2(0.0f, 0.0f);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        v.p[j] = add2(v.p[j], both(-mean));
+        if (2 * j >= n) v.p[j].x = 0.0f;
+        if (2 * j + 1 >= n) v.p[j].y = 0.0f;
+        s = fma2(v.p[j], v.p[j], s);
+    }
+    return s.x + s.y;
 }
 
 // Sum over the block in every thread, in a fixed order.  `scratch` holds one entry per warp.
@@ -117,260 +165,273 @@ __device__ __forceinline__ float2 block_sum(float2 s, float2* scratch) {
 
 constexpr int kLoopThreads = 512;
 
-// A block takes a row at a time and reads it three times: for the mean, for the variance, for the result.
-template <int kType, bool kFused, bool kFmt>
+// Rows too long for a team's registers: a block takes a row at a time and reads it three times, for the mean,
+// for the variance and for the result.
+template <int kType, bool kFused>
 __global__ void __launch_bounds__(kLoopThreads) norm_forward_loop_kernel(const ForwardArgs<kType> a) {
     extern __shared__ uint32_t lane_hist[];
     __shared__ float2 scratch[32];
-    uint32_t* hist = kFmt && a.stats != nullptr ? lane_hist : nullptr;
+    grid_dependency_wait();
+    uint32_t* hist = a.stats != nullptr ? lane_hist : nullptr;
     if (hist != nullptr) clear_hist(hist, a.quant);
     const uint32_t granules = (uint32_t)((a.cols + kGranule - 1) / kGranule);
     const float count = (float)a.cols;
     const uint64_t offset = kFused ? drop_offset(a.drop) : 0ull;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const auto* x = a.x + row * a.ld_x;
+        const auto* r = a.residual + row * a.ld_residual;
+        const auto h = [&](uint32_t g, int n) {
+            const Raw<kType> res = kFused && a.residual != nullptr ? fetch<kType, false>(r, g, n, a.vec) : no_words<kType>();
+            return join_h<kType, kFused>(a, fetch<kType, false>(x, g, n, a.vec), res, offset, row, g);
+        };
         float sum = 0.0f;
         for (uint32_t g = threadIdx.x; g < granules; g += kLoopThreads) {
-            const int n = granule_columns(a.cols, (int64_t)g * kGranule);
-            float v[kGranule];
-            load_h<kType, kFused>(a, row, g, n, offset, v);
-#pragma unroll
-            for (int j = 0; j < kGranule; ++j) sum += v[j];
+            const int n = granule_columns(a.cols, g);
+            sum += sum8(h(g, n));
         }
         const float mean = block_sum(make_float2(sum, 0.0f), scratch).x / count;
-        float square = 0.0f;
+        sum = 0.0f;
         for (uint32_t g = threadIdx.x; g < granules; g += kLoopThreads) {
-            const int n = granule_columns(a.cols, (int64_t)g * kGranule);
-            float v[kGranule];
-            load_h<kType, kFused>(a, row, g, n, offset, v);
-#pragma unroll
-            for (int j = 0; j < kGranule; ++j) {
-                const float d = j < n ? v[j] - mean : 0.0f;
-                square = __fmaf_rn(d, d, square);
-            }
+            const int n = granule_columns(a.cols, g);
+            Granule v = h(g, n);
+            sum += centre(v, mean, n);
         }
-        const float rstd = 1.0f / sqrtf(block_sum(make_float2(square, 0.0f), scratch).x / count + a.eps);
+        const float rstd = 1.0f / sqrtf(block_sum(make_float2(sum, 0.0f), scratch).x / count + a.eps);
         if (threadIdx.x == 0) {
             if (a.mean != nullptr) a.mean[row] = mean;
             if (a.rstd != nullptr) a.rstd[row] = rstd;
         }
         for (uint32_t g = threadIdx.x; g < granules; g += kLoopThreads) {
-            const int64_t col = (int64_t)g * kGranule;
-            const int n = granule_columns(a.cols, col);
-            float v[kGranule], w[kGranule], b[kGranule];
-            load_h<kType, kFused>(a, row, g, n, offset, v);
-            if (kFused && a.h != nullptr)
-                store_granule<kType>(a.h + row * a.ld_h + col, n, a.vec, finish<kType, false>(v, n, a.quant, nullptr));
-            load_columns<false>(a.weight, col, n, 1.0f, w);
-            load_columns<false>(a.bias, col, n, 0.0f, b);
+            const int n = granule_columns(a.cols, g);
+            Granule v = h(g, n);
+            if (kFused && a.h != nullptr) put<kType, false>(a.h + row * a.ld_h, g, n, a.vec, finish<kType>(v));
+            const Granule w = load_columns(a.weight, g, n, 1.0f), b = load_columns(a.bias, g, n, 0.0f);
 #pragma unroll
-            for (int j = 0; j < kGranule; ++j) v[j] = __fmaf_rn((v[j] - mean) * rstd, w[j], b[j]);
-            store_granule<kType>(a.y + row * a.ld_y + col, n, a.vec, finish<kType, kFmt>(v, n, a.quant, hist));
+            for (int j = 0; j < 4; ++j) v.p[j] = fma2(mul2(add2(v.p[j], both(-mean)), both(rstd)), w.p[j], b.p[j]);
+            put<kType, false>(a.y + row * a.ld_y, g, n, a.vec, finish_output<kType>(a, v, n, hist));
         }
     }
     if (hist != nullptr) flush_hist(hist, a.quant, a.stats, (uint64_t)a.rows * (uint64_t)a.cols);
 }
 
 // Teams: the threads that share a row.  A team of up to 32 threads is an aligned part of a warp; a larger
-// one is whole warps.  Granule k * team + t of the row is thread t's k-th.
+// one is whole warps.  Granule k * team + t of the row is thread t's k-th, k < V.
+constexpr int kMaxTeam = 512;
 
-// Sum over a team in every thread, in a fixed order.  scratch: 16 entries per team, of which those past the
-// team's warps are zero; one barrier, so the next sum needs another scratch.
-__device__ __forceinline__ float2 team_sum(float2 s, int team, int t, int barrier, float2* scratch) {
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
-        if (off < team) {
-            s.x += __shfl_xor_sync(0xFFFFFFFFu, s.x, off);
-            s.y += __shfl_xor_sync(0xFFFFFFFFu, s.y, off);
-        }
-    }
+// Sum over a team in every thread, in a fixed order.  scratch: 16 entries, those past the team's warps zero;
+// one barrier, so the team's next sum needs another scratch.
+template <typename T, typename Add>
+__device__ __forceinline__ T team_sum(T s, int team, int t, int barrier, T* scratch, Add add) {
+    for (int off = team < 32 ? team / 2 : 16; off > 0; off >>= 1) s = add(s, add.other(s, off));
     if (team > 32) {
         if ((t & 31) == 0) scratch[t >> 5] = s;
         asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(team) : "memory");
-        const float4* q = reinterpret_cast<const float4*>(scratch);
-        s = make_float2(0.0f, 0.0f);
-        for (int i = 0; i < team; i += 128) {  // four warps' entries
-            const float4 u = q[i / 64], v = q[i / 64 + 1];
-            s.x += (u.x + u.z) + (v.x + v.z);
-            s.y += (u.y + u.w) + (v.y + v.w);
-        }
+        s = add(add(scratch[0], scratch[1]), add(scratch[2], scratch[3]));
+        for (int i = 4; i < team / 32; i += 4) s = add(s, add(add(scratch[i], scratch[i + 1]), add(scratch[i + 2], scratch[i + 3])));
     }
     return s;
 }
+struct AddOne {
+    __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
+    __device__ __forceinline__ float other(float s, int off) const { return __shfl_xor_sync(0xFFFFFFFFu, s, off); }
+};
+struct AddTwo {
+    __device__ __forceinline__ float2 operator()(float2 a, float2 b) const { return add2(a, b); }
+    __device__ __forceinline__ float2 other(float2 s, int off) const {
+        return make_float2(__shfl_xor_sync(0xFFFFFFFFu, s.x, off), __shfl_xor_sync(0xFFFFFFFFu, s.y, off));
+    }
+};
 
-constexpr int kRowThreads = 512;
-
-// A row is read once and stays in its team's registers.
+// A row is read once and stays in its team's registers.  V <= 2: so do the team's weight and bias, from row to
+// row, and the next row is on its way while this one is worked on.  V = 4: longer rows, without either.
 template <int kType, int V, bool kFused, bool kVec>
-__global__ void __launch_bounds__(kRowThreads) norm_forward_rows_kernel(const ForwardArgs<kType> a, int team) {
+__global__ void __launch_bounds__(kMaxTeam) norm_forward_rows_kernel(const ForwardArgs<kType> a, int team) {
+    constexpr bool kKeep = V <= 2;
+    constexpr bool kAhead = kKeep && kVec;
     extern __shared__ uint32_t lane_hist[];
-    __shared__ float2 scratch[2][16];
+    __shared__ float scratch[kMaxTeam / 32][2][16];
+    grid_launch_dependents();
+    grid_dependency_wait();
     uint32_t* hist = a.stats != nullptr ? lane_hist : nullptr;
     if (team > 32) {
-        if (threadIdx.x < 32) scratch[threadIdx.x >> 4][threadIdx.x & 15] = make_float2(0.0f, 0.0f);
+        for (int i = threadIdx.x; i < kMaxTeam; i += blockDim.x) (&scratch[0][0][0])[i] = 0.0f;
         __syncthreads();
     }
     if (hist != nullptr) clear_hist(hist, a.quant);
-    const int t = team > 32 ? (int)threadIdx.x : (int)threadIdx.x & (team - 1);
-    const int teams = blockDim.x / team;
+    const int mine = threadIdx.x / team, t = threadIdx.x - mine * team, teams = blockDim.x / team;
+    const int slot = team > 32 ? mine : 0;
     const float inverse = 1.0f / (float)a.cols;
     const uint64_t offset = kFused ? drop_offset(a.drop) : 0ull;
-    // the last teams of a warp may have no row while its other teams have one: they go through the motions
-    for (int64_t base = (int64_t)blockIdx.x * teams; base < a.rows; base += (int64_t)gridDim.x * teams) {
-        const int64_t row = base + threadIdx.x / team;
-        float v[V][kGranule];
-        float2 s = make_float2(0.0f, 0.0f);
+    const bool residual = kFused && a.residual != nullptr;
+    const int64_t step = (int64_t)gridDim.x * teams;
+    int n[V];  // columns of each granule
+#pragma unroll
+    for (int k = 0; k < V; ++k) n[k] = granule_columns(a.cols, k * team + t);
+
+    // A team past the last row, whose warp has teams with one, keeps in step with them and stores nothing.
+    int64_t base = (int64_t)blockIdx.x * teams, row = base + mine;
+    Raw<kType> x[V], r[V];
+    const auto fetch_row = [&](int64_t at) {
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            const int64_t col = (int64_t)(k * team + t) * kGranule;
-            const int n = row < a.rows && col < a.cols ? granule_columns(a.cols, col) : 0;
-#pragma unroll
-            for (int j = 0; j < kGranule; ++j) v[k][j] = 0.0f;
-            if (n > 0) load_granule<kType, kVec>(a.x + row * a.ld_x + col, n, v[k]);
+            const bool there = at < a.rows && n[k] > 0;
+            x[k] = there ? fetch<kType, kVec>(a.x + at * a.ld_x, k * team + t, n[k], a.vec) : no_words<kType>();
+            r[k] = there && residual ? fetch<kType, kVec>(a.residual + at * a.ld_residual, k * team + t, n[k], a.vec) : no_words<kType>();
         }
-        if constexpr (kFused) {
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-                const int64_t col = (int64_t)(k * team + t) * kGranule;
-                const int n = row < a.rows && col < a.cols ? granule_columns(a.cols, col) : 0;
-                if (n > 0) {
-                    float r[kGranule];
-                    if (a.residual != nullptr) load_granule<kType, kVec>(a.residual + row * a.ld_residual + col, n, r);
-                    if (a.drop.threshold != 0u) drop_granule(a.drop, offset, (uint32_t)row, k * team + t, v[k]);
-                    if (a.residual != nullptr) {
-#pragma unroll
-                        for (int j = 0; j < kGranule; ++j) v[k][j] = add_ieee(r[j], v[k][j]);
-                    }
-                    if (a.h != nullptr)
-                        store_granule<kType, kVec>(a.h + row * a.ld_h + col, n, finish<kType, false>(v[k], n, a.quant, nullptr));
-                }
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < V; ++k)
-#pragma unroll
-            for (int j = 0; j < kGranule; ++j) s.x += v[k][j];
-        const float mean = team_sum(s, team, t, 1, scratch[0]).x * inverse;
-        s.x = 0.0f;
+    };
+    if (kAhead) fetch_row(row);
+    Granule w[kKeep ? V : 1], b[kKeep ? V : 1];
+    if constexpr (kKeep) {
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            const int64_t col = (int64_t)(k * team + t) * kGranule;
-#pragma unroll
-            for (int j = 0; j < kGranule; ++j) {
-                v[k][j] = col + j < a.cols ? v[k][j] - mean : 0.0f;
-                s.x = __fmaf_rn(v[k][j], v[k][j], s.x);
-            }
+            w[k] = load_columns(a.weight, k * team + t, n[k], 1.0f);
+            b[k] = load_columns(a.bias, k * team + t, n[k], 0.0f);
         }
-        const float rstd = 1.0f / sqrtf(team_sum(s, team, t, 1, scratch[1]).x * inverse + a.eps);
-        if (t == 0 && row < a.rows) {
+    }
+    for (; base < a.rows; base += step, row += step) {
+        const bool live = row < a.rows;
+        if (!kAhead) fetch_row(row);
+        Granule v[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] = join_h<kType, kFused>(a, x[k], r[k], offset, row, k * team + t);
+        if (kAhead) fetch_row(row + step);
+        if (kFused && a.h != nullptr) {
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                if (live && n[k] > 0) put<kType, kVec>(a.h + row * a.ld_h, k * team + t, n[k], a.vec, finish<kType>(v[k]));
+        }
+        float s = 0.0f;
+#pragma unroll
+        for (int k = 0; k < V; ++k) s += sum8(v[k]);
+        const float mean = team_sum(s, team, t, 1 + slot, scratch[slot][0], AddOne()) * inverse;
+        s = 0.0f;
+#pragma unroll
+        for (int k = 0; k < V; ++k) s += kVec ? (n[k] > 0 ? centre(v[k], mean, kGranule) : 0.0f) : centre(v[k], mean, n[k]);
+        const float rstd = 1.0f / sqrtf(team_sum(s, team, t, 1 + slot, scratch[slot][1], AddOne()) * inverse + a.eps);
+        if (t == 0 && live) {
             if (a.mean != nullptr) a.mean[row] = mean;
             if (a.rstd != nullptr) a.rstd[row] = rstd;
         }
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            const int64_t col = (int64_t)(k * team + t) * kGranule;
-            const int n = row < a.rows && col < a.cols ? granule_columns(a.cols, col) : 0;
-            if (n > 0) {
-                float w[kGranule], b[kGranule];
-                load_columns<kVec>(a.weight, col, n, 1.0f, w);
-                load_columns<kVec>(a.bias, col, n, 0.0f, b);
+            if (live && n[k] > 0) {
+                if constexpr (!kKeep) {
+                    w[0] = load_columns(a.weight, k * team + t, n[k], 1.0f);
+                    b[0] = load_columns(a.bias, k * team + t, n[k], 0.0f);
+                }
+                const Granule& wk = w[kKeep ? k : 0];
+                const Granule& bk = b[kKeep ? k : 0];
 #pragma unroll
-                for (int j = 0; j < kGranule; ++j) v[k][j] = __fmaf_rn(v[k][j] * rstd, w[j], b[j]);
-                store_granule<kType, kVec>(a.y + row * a.ld_y + col, n,
-                                           a.fmt ? finish<kType, true>(v[k], n, a.quant, hist) : finish<kType, false>(v[k], n, a.quant, nullptr));
+                for (int j = 0; j < 4; ++j) v[k].p[j] = fma2(mul2(v[k].p[j], both(rstd)), wk.p[j], bk.p[j]);
+                put<kType, kVec>(a.y + row * a.ld_y, k * team + t, n[k], a.vec, finish_output<kType>(a, v[k], n[k], hist));
             }
         }
     }
     if (hist != nullptr) flush_hist(hist, a.quant, a.stats, (uint64_t)a.rows * (uint64_t)a.cols);
 }
 
-template <int kType>
-__device__ __forceinline__ void load_xhat_dy(const BackwardArgs<kType>& a, int64_t row, int64_t col, int n, float mean, float rstd,
-                                             float (&xhat)[kGranule], float (&dy)[kGranule]) {
-    load_granule<kType>(a.h + row * a.ld_h + col, n, a.vec, xhat);
-    load_granule<kType>(a.dy + row * a.ld_dy + col, n, a.vec, dy);
+// xhat of a granule; 0 where there is no column.
+__device__ __forceinline__ Granule normalise(Granule v, float mean, float rstd, int n) {
 #pragma unroll
-    for (int j = 0; j < kGranule; ++j) xhat[j] = j < n ? (xhat[j] - mean) * rstd : 0.0f;
+    for (int j = 0; j < 4; ++j) {
+        v.p[j] = mul2(add2(v.p[j], both(-mean)), both(rstd));
+        if (2 * j >= n) v.p[j].x = 0.0f;
+        if (2 * j + 1 >= n) v.p[j].y = 0.0f;
+    }
+    return v;
 }
 
-// The gradient of h, and D of it: a block takes a row at a time and reads it twice.
-template <int kType, bool kFused, bool kFmt>
+// The row's two sums over one granule: g = w dy and g xhat.
+__device__ __forceinline__ float2 row_sums(const Granule& dy, const Granule& xhat, const Granule& w) {
+    float2 s = make_float2(0.0f, 0.0f), q = s;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float2 g = mul2(dy.p[j], w.p[j]);
+        s = add2(s, g);
+        q = fma2(g, xhat.p[j], q);
+    }
+    return make_float2(s.x + s.y, q.x + q.y);
+}
+
+// What a granule's gradients become: dh (with what arrives by another path) to dresidual, D of it to dx.
+template <int kType, bool kFused, bool kVec>
+__device__ __forceinline__ void store_gradients(const BackwardArgs<kType>& a, const Granule& dy, const Granule& xhat, const Granule& w,
+                                                float rstd, float c1, float c2, int64_t row, uint32_t g, int n, uint64_t offset,
+                                                uint32_t* hist) {
+    Granule d;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        d.p[j] = mul2(fma2(xhat.p[j], both(-c2), fma2(dy.p[j], w.p[j], both(-c1))), both(rstd));
+    if constexpr (kFused) {
+        if (a.dh != nullptr) {
+            const Granule more = widen_raw<kType>(fetch<kType, kVec>(a.dh + row * a.ld_dh, g, n, a.vec));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) d.p[j] = add2(d.p[j], more.p[j]);
+        }
+        if (a.dresidual != nullptr) put<kType, kVec>(a.dresidual + row * a.ld_dresidual, g, n, a.vec, finish<kType>(d));
+        if (a.drop.active && a.dx != nullptr) drop_granule(a.drop, offset, (uint32_t)row, g, d);
+    }
+    if (a.dx != nullptr) put<kType, kVec>(a.dx + row * a.ld_dx, g, n, a.vec, finish_output<kType>(a, d, n, hist));
+}
+
+// Long rows: a block takes a row at a time and reads it twice.
+template <int kType, bool kFused>
 __global__ void __launch_bounds__(kLoopThreads) norm_backward_loop_kernel(const BackwardArgs<kType> a) {
     extern __shared__ uint32_t lane_hist[];
     __shared__ float2 scratch[32];
-    uint32_t* hist = kFmt && a.stats != nullptr ? lane_hist : nullptr;
+    uint32_t* hist = a.stats != nullptr ? lane_hist : nullptr;
     if (hist != nullptr) clear_hist(hist, a.quant);
     const uint32_t granules = (uint32_t)((a.cols + kGranule - 1) / kGranule);
     const float count = (float)a.cols;
     const uint64_t offset = kFused ? drop_offset(a.drop) : 0ull;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const float mean = a.mean[row], rstd = a.rstd[row];
+        const auto load = [&](uint32_t g, int n, Granule& dy, Granule& xhat, Granule& w) {
+            dy = widen_raw<kType>(fetch<kType, false>(a.dy + row * a.ld_dy, g, n, a.vec));
+            xhat = normalise(widen_raw<kType>(fetch<kType, false>(a.h + row * a.ld_h, g, n, a.vec)), mean, rstd, n);
+            w = load_columns(a.weight, g, n, 1.0f);
+        };
         float2 s = make_float2(0.0f, 0.0f);
+        Granule dy, xhat, w;
         for (uint32_t g = threadIdx.x; g < granules; g += kLoopThreads) {
-            const int64_t col = (int64_t)g * kGranule;
-            const int n = granule_columns(a.cols, col);
-            float xhat[kGranule], dy[kGranule], w[kGranule];
-            load_xhat_dy<kType>(a, row, col, n, mean, rstd, xhat, dy);
-            load_columns<false>(a.weight, col, n, 1.0f, w);
-#pragma unroll
-            for (int j = 0; j < kGranule; ++j) {
-                const float t = dy[j] * w[j];
-                s.x += t;
-                s.y = __fmaf_rn(t, xhat[j], s.y);
-            }
+            load(g, granule_columns(a.cols, g), dy, xhat, w);
+            s = add2(s, row_sums(dy, xhat, w));
         }
         s = block_sum(s, scratch);
-        const float c1 = s.x / count, c2 = s.y / count;
         for (uint32_t g = threadIdx.x; g < granules; g += kLoopThreads) {
-            const int64_t col = (int64_t)g * kGranule;
-            const int n = granule_columns(a.cols, col);
-            float xhat[kGranule], dy[kGranule], w[kGranule];
-            load_xhat_dy<kType>(a, row, col, n, mean, rstd, xhat, dy);
-            load_columns<false>(a.weight, col, n, 1.0f, w);
-#pragma unroll
-            for (int j = 0; j < kGranule; ++j) dy[j] = rstd * (__fmaf_rn(dy[j], w[j], -c1) - xhat[j] * c2);
-            if (kFused) {
-                if (a.dh != nullptr) {
-                    float more[kGranule];
-                    load_granule<kType>(a.dh + row * a.ld_dh + col, n, a.vec, more);
-#pragma unroll
-                    for (int j = 0; j < kGranule; ++j) dy[j] += more[j];
-                }
-                if (a.dresidual != nullptr)
-                    store_granule<kType>(a.dresidual + row * a.ld_dresidual + col, n, a.vec, finish<kType, false>(dy, n, a.quant, nullptr));
-                if (a.drop.threshold != 0u && a.dx != nullptr) drop_granule(a.drop, offset, (uint32_t)row, g, dy);
-            }
-            if (a.dx != nullptr)
-                store_granule<kType>(a.dx + row * a.ld_dx + col, n, a.vec, finish<kType, kFmt>(dy, n, a.quant, hist));
+            const int n = granule_columns(a.cols, g);
+            load(g, n, dy, xhat, w);
+            store_gradients<kType, kFused, false>(a, dy, xhat, w, rstd, s.x / count, s.y / count, row, g, n, offset, hist);
         }
     }
     if (hist != nullptr) flush_hist(hist, a.quant, a.stats, (uint64_t)a.rows * (uint64_t)a.cols);
 }
 
-// Sums over rows for the gradients of weight and bias: a block takes 32 granules of columns and one part of
-// the rows, its eight warps every eighth row; their sums are joined in a fixed order.
+// Sums over rows for the gradients of weight and bias of long rows: a block takes 32 granules of columns and
+// one part of the rows, its eight warps every eighth row; their sums are joined in a fixed order.
 constexpr int kColumnWarps = 8;
 template <int kType>
 __global__ void __launch_bounds__(32 * kColumnWarps) norm_column_sums_kernel(const BackwardArgs<kType> a) {
     __shared__ float part[kColumnWarps][2][kGranule][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t col = ((int64_t)blockIdx.x * 32 + lane) * kGranule;
-    const int n = col < a.cols ? granule_columns(a.cols, col) : 0;
-    float dw[kGranule] = {}, db[kGranule] = {};
+    const uint32_t g = blockIdx.x * 32 + lane;
+    const int n = granule_columns(a.cols, g);
+    Granule dw = splat(0.0f), db = splat(0.0f);
     if (n > 0) {
         for (int64_t row = (int64_t)blockIdx.y * kColumnWarps + warp; row < a.rows; row += (int64_t)gridDim.y * kColumnWarps) {
-            float xhat[kGranule], dy[kGranule];
-            load_xhat_dy<kType>(a, row, col, n, a.mean[row], a.rstd[row], xhat, dy);
+            const Granule dy = widen_raw<kType>(fetch<kType, false>(a.dy + row * a.ld_dy, g, n, a.vec));
+            const Granule xhat = normalise(widen_raw<kType>(fetch<kType, false>(a.h + row * a.ld_h, g, n, a.vec)), a.mean[row], a.rstd[row], n);
 #pragma unroll
-            for (int j = 0; j < kGranule; ++j) {
-                dw[j] = __fmaf_rn(dy[j], xhat[j], dw[j]);
-                db[j] += dy[j];
+            for (int j = 0; j < 4; ++j) {
+                dw.p[j] = fma2(dy.p[j], xhat.p[j], dw.p[j]);
+                db.p[j] = add2(db.p[j], dy.p[j]);
             }
         }
     }
 #pragma unroll
     for (int j = 0; j < kGranule; ++j) {
-        part[warp][0][j][lane] = dw[j];
-        part[warp][1][j][lane] = db[j];
+        part[warp][0][j][lane] = dw.at(j);
+        part[warp][1][j][lane] = db.at(j);
     }
     __syncthreads();
     for (int i = threadIdx.x; i < 2 * kGranule * 32; i += 32 * kColumnWarps) {
@@ -383,17 +444,130 @@ __global__ void __launch_bounds__(32 * kColumnWarps) norm_column_sums_kernel(con
     }
 }
 
+// The backward pass of rows that a team holds in registers: dy and h are read once, the sums over rows stay in
+// the registers of the thread that owns their columns from row to row, and a block leaves one part.
+template <int kType, int V, bool kFused, bool kVec>
+__global__ void __launch_bounds__(kMaxTeam) norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int hist_words) {
+    constexpr bool kAhead = kVec && kType != QFMT_F32;
+    extern __shared__ uint32_t dynamic[];  // [hist_words] histogram, then the sums of a block's teams
+    __shared__ float2 scratch[kMaxTeam / 32][2][16];
+    grid_launch_dependents();
+    grid_dependency_wait();
+    uint32_t* hist = a.stats != nullptr ? dynamic : nullptr;
+    if (team > 32) {
+        for (int i = threadIdx.x; i < kMaxTeam; i += blockDim.x) (&scratch[0][0][0])[i] = make_float2(0.0f, 0.0f);
+        __syncthreads();
+    }
+    if (hist != nullptr) clear_hist(hist, a.quant);
+    const int mine = threadIdx.x / team, t = threadIdx.x - mine * team, teams = blockDim.x / team;
+    const int slot = team > 32 ? mine : 0;
+    const float inverse = 1.0f / (float)a.cols;
+    const uint64_t offset = kFused ? drop_offset(a.drop) : 0ull;
+    const int64_t step = (int64_t)gridDim.x * teams;
+    int n[V];
+    Granule w[V], dw[V], db[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        n[k] = granule_columns(a.cols, k * team + t);
+        dw[k] = db[k] = splat(0.0f);
+    }
+    int64_t base = (int64_t)blockIdx.x * teams, row = base + mine;
+    Raw<kType> raw_dy[V], raw_h[V];
+    float mean = 0.0f, rstd = 0.0f;
+    const auto fetch_row = [&](int64_t at) {
+        if (at < a.rows) mean = a.mean[at], rstd = a.rstd[at];
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const bool there = at < a.rows && n[k] > 0;
+            raw_dy[k] = there ? fetch<kType, kVec>(a.dy + at * a.ld_dy, k * team + t, n[k], a.vec) : no_words<kType>();
+            raw_h[k] = there ? fetch<kType, kVec>(a.h + at * a.ld_h, k * team + t, n[k], a.vec) : no_words<kType>();
+        }
+    };
+    if (kAhead) fetch_row(row);
+#pragma unroll
+    for (int k = 0; k < V; ++k) w[k] = load_columns(a.weight, k * team + t, n[k], 1.0f);
+    int parity = 0;
+    for (; base < a.rows; base += step, row += step, parity ^= 1) {
+        const bool live = row < a.rows;
+        if (!kAhead) fetch_row(row);
+        Granule dy[V], xhat[V];
+        float2 s = make_float2(0.0f, 0.0f);
+        const float this_rstd = rstd;
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            dy[k] = widen_raw<kType>(raw_dy[k]);
+            xhat[k] = normalise(widen_raw<kType>(raw_h[k]), mean, rstd, live ? (kVec && n[k] > 0 ? kGranule : n[k]) : 0);
+            s = add2(s, row_sums(dy[k], xhat[k], w[k]));
+        }
+        if (kAhead) fetch_row(row + step);
+        s = team_sum(s, team, t, 1 + slot, scratch[slot][parity], AddTwo());
+        const float c1 = s.x * inverse, c2 = s.y * inverse;
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                dw[k].p[j] = fma2(dy[k].p[j], xhat[k].p[j], dw[k].p[j]);
+                db[k].p[j] = add2(db[k].p[j], dy[k].p[j]);
+            }
+            if (live && n[k] > 0)
+                store_gradients<kType, kFused, kVec>(a, dy[k], xhat[k], w[k], this_rstd, c1, c2, row, k * team + t, n[k], offset, hist);
+        }
+    }
+    if (hist != nullptr) flush_hist(hist, a.quant, a.stats, (uint64_t)a.rows * (uint64_t)a.cols);
+    if (a.partial == nullptr) return;
+    // the teams of a warp by shuffles, those of the block one after the other through shared memory
+    for (int off = 16; off >= team; off >>= 1) {
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                dw[k].p[j] = add2(dw[k].p[j], AddTwo().other(dw[k].p[j], off));
+                db[k].p[j] = add2(db[k].p[j], AddTwo().other(db[k].p[j], off));
+            }
+    }
+    const int unit = team < 32 ? 32 : team, units = blockDim.x / unit;  // threads that still hold a sum of their own
+    float* const sums = reinterpret_cast<float*>(dynamic + hist_words);
+    const int u = threadIdx.x / unit;
+    const bool holds = threadIdx.x - u * unit < team;
+    for (int turn = 0; turn < units; ++turn) {
+        if (turn > 0) __syncthreads();
+        if (u != turn || !holds) continue;
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const int64_t col = (int64_t)(k * team + t) * kGranule;
+#pragma unroll
+            for (int j = 0; j < kGranule; ++j) {
+                if (j < n[k]) {
+                    float p = dw[k].at(j), q = db[k].at(j);
+                    if (turn > 0) p += sums[col + j], q += sums[a.cols + col + j];
+                    if (turn == units - 1) {
+                        a.partial[(int64_t)blockIdx.x * 2 * a.cols + col + j] = p;
+                        a.partial[((int64_t)blockIdx.x * 2 + 1) * a.cols + col + j] = q;
+                    } else {
+                        sums[col + j] = p, sums[a.cols + col + j] = q;
+                    }
+                }
+            }
+        }
+    }
+}
+
 // Joins the parts in a fixed order: a block takes 32 columns, its eight warps every eighth part.
 __global__ void __launch_bounds__(32 * kColumnWarps)
-norm_join_parts_kernel(const float* __restrict__ partial, int parts, int64_t cols, float* dweight, float* dbias) {
+norm_join_parts_kernel(const float* partial, int parts, int64_t cols, float* dweight, float* dbias) {
     __shared__ float sums[kColumnWarps][32];
+    grid_launch_dependents();
+    grid_dependency_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t c = (int64_t)blockIdx.x * 32 + lane;
-    float* const out = blockIdx.y == 0 ? dweight : dbias;
+    const int which = blockIdx.x & 1;
+    const int64_t c = (int64_t)(blockIdx.x >> 1) * 32 + lane;
+    float* const out = which == 0 ? dweight : dbias;
     if (out == nullptr) return;
     float s = 0.0f;
-    if (c < cols)
-        for (int k = warp; k < parts; k += kColumnWarps) s += partial[((int64_t)k * 2 + blockIdx.y) * cols + c];
+    if (c < cols) {
+#pragma unroll 8
+        for (int k = warp; k < parts; k += kColumnWarps) s += partial[((int64_t)k * 2 + which) * cols + c];
+    }
     sums[warp][lane] = s;
     __syncthreads();
     if (warp == 0 && c < cols) {
@@ -403,9 +577,44 @@ norm_join_parts_kernel(const float* __restrict__ partial, int parts, int64_t col
     }
 }
 
-// Parts the rows are summed in for the gradients of weight and bias.
-int row_parts(int64_t rows) {
-    const int64_t want = (rows + 8 * kColumnWarps - 1) / (8 * kColumnWarps);
+// How a pass runs.  The team is the fewest threads that cover a row with V granules each: with V = 2 a team's
+// weights fit in registers beside the row and the one on its way.
+struct Plan {
+    int team, granules;  // team 0: the row does not fit a team
+};
+Plan make_plan(int64_t cols, int most) {
+    const int64_t g = (cols + kGranule - 1) / kGranule;
+    if (g <= 32) {
+        int team = 1;
+        while (team < g) team *= 2;
+        return {team, 1};
+    }
+    for (int v = 2; v <= most; v *= 2)
+        if (g <= (int64_t)v * kMaxTeam) return {(int)((g + 32 * v - 1) / (32 * v)) * 32, v};
+    return {0, 0};
+}
+constexpr int kForwardGranules = 4, kBackwardGranules = 2;
+
+// Blocks of a kernel that an SM holds at once; asked for once per block size.
+template <typename K>
+int resident_blocks(K kernel, unsigned block, size_t smem, std::atomic<int>* known, int* out) {
+    std::atomic<int>& slot = known[block / 32];
+    if (smem == 0 && slot.load() > 0) {
+        *out = slot.load();
+        return QFMT_OK;
+    }
+    QFMT_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(out, kernel, (int)block, smem));
+    if (*out < 1) *out = 1;
+    if (smem == 0) slot.store(*out);
+    return QFMT_OK;
+}
+
+// Parts that the backward pass leaves for the gradients of weight and bias: one per block of the rows kernel (at
+// most one block per SM of a B200), or a share of the rows for long rows.
+constexpr int kMaxParts = 148;
+int row_parts(const qfmt_norm_t& s) {
+    if (make_plan(s.cols, kBackwardGranules).team != 0) return kMaxParts;
+    const int64_t want = (s.rows + 8 * kColumnWarps - 1) / (8 * kColumnWarps);
     return (int)(want < 64 ? (want > 0 ? want : 1) : 64);
 }
 
@@ -452,45 +661,34 @@ int prepare_call(const qfmt_norm_t* norm, const qfmt_dropout_t* drop, const qfmt
 
 bool float_aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
-// Threads that share a row and the granules each of them holds: the fewest that cover it with at most four
-// granules a thread (fewer barriers and shuffles per element than one granule a thread).
-struct Team {
-    int threads, granules;
-};
-Team forward_team(int64_t cols) {
-    const int64_t g = (cols + kGranule - 1) / kGranule;
-    if (g > 4 * kRowThreads) return {0, 0};
-    if (g <= 32) {
-        int threads = 1;
-        while (threads < g) threads *= 2;
-        return {threads, 1};
-    }
-    if (g <= 64) return {32, 2};
-    return {(int)((g + 127) / 128) * 32, 4};
+template <int kType, int V, bool kFused, bool kVec>
+int launch_forward_rows(const Call& c, const ForwardArgs<kType>& a, int team, cudaStream_t stream) {
+    static std::atomic<int> known[kMaxTeam / 32 + 1];
+    const auto kern = norm_forward_rows_kernel<kType, V, kFused, kVec>;
+    const unsigned teams = team < 128 ? 128 / team : 1, block = teams * team;
+    int resident = 0;
+    const int rc = resident_blocks(kern, block, c.hist_bytes, known, &resident);
+    if (rc != QFMT_OK) return rc;
+    const int64_t want = (a.rows + teams - 1) / teams, cap = (int64_t)c.dev.sm_count * resident;
+    QFMT_CUDA_TRY(launch_overlapping(kern, (unsigned)(want < cap ? want : cap), block, c.hist_bytes, stream, a, team));
+    return QFMT_OK;
 }
-
-bool column_aligned(const float* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 template <int kType, bool kFused>
 int launch_forward(const Call& c, const ForwardArgs<kType>& a, cudaStream_t stream) {
-    const Team team = forward_team(a.cols);
-    if (team.threads != 0) {
-        const bool vec = a.vec && a.cols % kGranule == 0 && column_aligned(a.weight) && column_aligned(a.bias);
-        const unsigned block = team.threads > 32 ? team.threads : 128;
-        const int64_t want = (a.rows * team.threads + block - 1) / block, cap = (int64_t)c.dev.sm_count * 32;
-        const auto kern = vec ? (team.granules == 1   ? norm_forward_rows_kernel<kType, 1, kFused, true>
-                                 : team.granules == 2 ? norm_forward_rows_kernel<kType, 2, kFused, true>
-                                                      : norm_forward_rows_kernel<kType, 4, kFused, true>)
-                              : (team.granules == 1   ? norm_forward_rows_kernel<kType, 1, kFused, false>
-                                 : team.granules == 2 ? norm_forward_rows_kernel<kType, 2, kFused, false>
-                                                      : norm_forward_rows_kernel<kType, 4, kFused, false>);
-        kern<<<(unsigned)(want < cap ? want : cap), block, c.hist_bytes, stream>>>(a, team.threads);
-    } else {
-        const int64_t cap = (int64_t)c.dev.sm_count * 4;
-        const auto kern = c.fmt ? norm_forward_loop_kernel<kType, kFused, true> : norm_forward_loop_kernel<kType, kFused, false>;
-        kern<<<(unsigned)(a.rows < cap ? a.rows : cap), kLoopThreads, c.hist_bytes, stream>>>(a);
+    const Plan plan = make_plan(a.cols, kForwardGranules);
+    if (plan.team != 0) {
+        const auto run = a.vec ? (plan.granules == 1   ? launch_forward_rows<kType, 1, kFused, true>
+                                  : plan.granules == 2 ? launch_forward_rows<kType, 2, kFused, true>
+                                                       : launch_forward_rows<kType, 4, kFused, true>)
+                               : (plan.granules == 1   ? launch_forward_rows<kType, 1, kFused, false>
+                                  : plan.granules == 2 ? launch_forward_rows<kType, 2, kFused, false>
+                                                       : launch_forward_rows<kType, 4, kFused, false>);
+        return run(c, a, plan.team, stream);
     }
-    QFMT_CUDA_TRY(cudaGetLastError());
+    const int64_t cap = (int64_t)c.dev.sm_count * 4;
+    QFMT_CUDA_TRY(launch_overlapping(norm_forward_loop_kernel<kType, kFused>, (unsigned)(a.rows < cap ? a.rows : cap), kLoopThreads,
+                                     c.hist_bytes, stream, a));
     return QFMT_OK;
 }
 
@@ -514,7 +712,7 @@ int forward(const Call& c, const void* d_x, const void* d_residual, const float*
     a.rows = c.norm.rows;
     a.cols = c.norm.cols;
     a.eps = c.norm.eps;
-    a.vec = granule_aligned(d_x, a.ld_x, kType) && granule_aligned(d_residual, a.ld_residual, kType) &&
+    a.vec = a.cols % kGranule == 0 && granule_aligned(d_x, a.ld_x, kType) && granule_aligned(d_residual, a.ld_residual, kType) &&
             granule_aligned(d_h, a.ld_h, kType) && granule_aligned(d_y, a.ld_y, kType);
     a.fmt = c.fmt;
     a.drop = c.drop;
@@ -537,26 +735,55 @@ int forward_entry(const qfmt_norm_t* norm, const qfmt_dropout_t* drop, bool fuse
         return QFMT_ERR_BAD_ARG;
     rc = current_device(&c.dev);
     if (rc != QFMT_OK) return rc;
-    if (d_stats != nullptr && accumulate == 0) QFMT_CUDA_TRY(cudaMemsetAsync(d_stats, 0, sizeof(qfmt_stats_t), stream));
+    if (d_stats != nullptr && accumulate == 0)
+        QFMT_CUDA_TRY(launch_overlapping(zero_words_kernel, 1u, 256u, 0, stream, reinterpret_cast<int*>(d_stats),
+                                         (int)(sizeof(qfmt_stats_t) / sizeof(int))));
     if (empty) return QFMT_OK;
     const auto run = fused ? (t == QFMT_F32 ? forward<QFMT_F32, true> : t == QFMT_F16 ? forward<QFMT_F16, true> : forward<QFMT_BF16, true>)
                            : (t == QFMT_F32 ? forward<QFMT_F32, false> : t == QFMT_F16 ? forward<QFMT_F16, false> : forward<QFMT_BF16, false>);
     return run(c, d_x, d_residual, d_weight, d_bias, d_h, d_y, d_mean, d_rstd, d_stats, stream);
 }
 
-template <int kType, bool kFused, bool kFmt>
+int join_parts(const float* partial, int parts, int64_t cols, float* d_dweight, float* d_dbias, cudaStream_t stream) {
+    QFMT_CUDA_TRY(launch_overlapping(norm_join_parts_kernel, 2u * (unsigned)((cols + 31) / 32), 32u * kColumnWarps, 0, stream, partial, parts,
+                                     cols, d_dweight, d_dbias));
+    return QFMT_OK;
+}
+
+template <int kType, int V, bool kFused, bool kVec>
+int launch_backward_rows(const Call& c, const BackwardArgs<kType>& a, int team, float* d_dweight, float* d_dbias, cudaStream_t stream) {
+    const auto kern = norm_backward_rows_kernel<kType, V, kFused, kVec>;
+    const unsigned teams = kMaxTeam / team, block = teams * team;
+    const unsigned units = team < 32 ? block / 32 : teams;
+    const size_t smem = c.hist_bytes + (units > 1 && a.partial != nullptr ? 2 * (size_t)a.cols * sizeof(float) : 0);
+    if (smem > 32 * 1024) QFMT_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    const int64_t want = (a.rows + teams - 1) / teams;
+    const int cap = c.dev.sm_count < kMaxParts ? c.dev.sm_count : kMaxParts;
+    const unsigned blocks = (unsigned)(want < cap ? want : cap);
+    QFMT_CUDA_TRY(launch_overlapping(kern, blocks, block, smem, stream, a, team, (int)(c.hist_bytes / sizeof(uint32_t))));
+    return a.partial != nullptr ? join_parts(a.partial, (int)blocks, a.cols, d_dweight, d_dbias, stream) : QFMT_OK;
+}
+
+template <int kType, bool kFused>
 int launch_backward(const Call& c, const BackwardArgs<kType>& a, float* d_dweight, float* d_dbias, cudaStream_t stream) {
+    if (a.rows == 0) return join_parts(a.partial, 0, a.cols, d_dweight, d_dbias, stream);  // zeros
+    const Plan plan = make_plan(a.cols, kBackwardGranules);
+    if (plan.team != 0) {
+        const auto run = a.vec ? (plan.granules == 1 ? launch_backward_rows<kType, 1, kFused, true> : launch_backward_rows<kType, 2, kFused, true>)
+                               : (plan.granules == 1 ? launch_backward_rows<kType, 1, kFused, false> : launch_backward_rows<kType, 2, kFused, false>);
+        return run(c, a, plan.team, d_dweight, d_dbias, stream);
+    }
     if (a.partial != nullptr) {  // before the row pass, which may overwrite dy
-        const int parts = row_parts(a.rows);
+        const int parts = row_parts(c.norm);
         const dim3 grid((unsigned)((a.cols + 32 * kGranule - 1) / (32 * kGranule)), (unsigned)parts);
         norm_column_sums_kernel<kType><<<grid, 32 * kColumnWarps, 0, stream>>>(a);
-        const dim3 join((unsigned)((a.cols + 31) / 32), 2);
-        norm_join_parts_kernel<<<join, 32 * kColumnWarps, 0, stream>>>(a.partial, parts, a.cols, d_dweight, d_dbias);
         QFMT_CUDA_TRY(cudaGetLastError());
+        const int rc = join_parts(a.partial, parts, a.cols, d_dweight, d_dbias, stream);
+        if (rc != QFMT_OK) return rc;
     }
-    if (a.rows != 0 && (a.dx != nullptr || a.dresidual != nullptr)) {
+    if (a.dx != nullptr || a.dresidual != nullptr) {
         const int64_t cap = (int64_t)c.dev.sm_count * 4;
-        norm_backward_loop_kernel<kType, kFused, kFmt><<<(unsigned)(a.rows < cap ? a.rows : cap), kLoopThreads, c.hist_bytes, stream>>>(a);
+        norm_backward_loop_kernel<kType, kFused><<<(unsigned)(a.rows < cap ? a.rows : cap), kLoopThreads, c.hist_bytes, stream>>>(a);
         QFMT_CUDA_TRY(cudaGetLastError());
     }
     return QFMT_OK;
@@ -584,14 +811,13 @@ int backward(const Call& c, const void* d_dy, const void* d_dh, const void* d_h,
     a.ld_dresidual = c.norm.ld_dresidual;
     a.rows = c.norm.rows;
     a.cols = c.norm.cols;
-    a.vec = granule_aligned(d_dy, a.ld_dy, kType) && granule_aligned(d_dh, a.ld_dh, kType) && granule_aligned(d_h, a.ld_h, kType) &&
+    a.vec = a.cols % kGranule == 0 && granule_aligned(d_dy, a.ld_dy, kType) && granule_aligned(d_dh, a.ld_dh, kType) && granule_aligned(d_h, a.ld_h, kType) &&
             granule_aligned(d_dx, a.ld_dx, kType) && granule_aligned(d_dresidual, a.ld_dresidual, kType);
     a.fmt = c.fmt;
     a.drop = c.drop;
     a.quant = c.quant;
     a.stats = d_stats;
-    return c.fmt ? launch_backward<kType, kFused, true>(c, a, d_dweight, d_dbias, stream)
-                 : launch_backward<kType, kFused, false>(c, a, d_dweight, d_dbias, stream);
+    return launch_backward<kType, kFused>(c, a, d_dweight, d_dbias, stream);
 }
 
 int backward_entry(const qfmt_norm_t* norm, const qfmt_dropout_t* drop, bool fused, const void* d_dy, const void* d_dh,
@@ -616,7 +842,9 @@ int backward_entry(const qfmt_norm_t* norm, const qfmt_dropout_t* drop, bool fus
         return QFMT_ERR_BAD_ARG;
     rc = current_device(&c.dev);
     if (rc != QFMT_OK) return rc;
-    if (d_stats != nullptr && accumulate == 0) QFMT_CUDA_TRY(cudaMemsetAsync(d_stats, 0, sizeof(qfmt_stats_t), stream));
+    if (d_stats != nullptr && accumulate == 0)
+        QFMT_CUDA_TRY(launch_overlapping(zero_words_kernel, 1u, 256u, 0, stream, reinterpret_cast<int*>(d_stats),
+                                         (int)(sizeof(qfmt_stats_t) / sizeof(int))));
     if (c.norm.cols == 0 || (empty && !columns)) return QFMT_OK;
     const int64_t ld_h = fused ? c.norm.ld_h : c.norm.ld_x;
     const auto run = fused ? (t == QFMT_F32 ? backward<QFMT_F32, true> : t == QFMT_F16 ? backward<QFMT_F16, true> : backward<QFMT_BF16, true>)
@@ -630,7 +858,7 @@ int backward_entry(const qfmt_norm_t* norm, const qfmt_dropout_t* drop, bool fus
 
 extern "C" size_t qfmt_layer_norm_workspace_bytes(const qfmt_norm_t* norm) {
     if (norm == nullptr || norm->rows < 0 || norm->cols < 0 || norm->rows > 0x7FFFFFFF || norm->cols > 0x7FFFFFFF) return 0;
-    return (size_t)qfmt::row_parts(norm->rows) * 2 * (size_t)norm->cols * sizeof(float);
+    return (size_t)qfmt::row_parts(*norm) * 2 * (size_t)norm->cols * sizeof(float);
 }
 
 extern "C" int qfmt_layer_norm(const qfmt_norm_t* norm, const void* d_x, const float* d_weight, const float* d_bias, void* d_y,
