@@ -84,16 +84,14 @@ __device__ __forceinline__ Granule load_columns(const float* p, int64_t g, int n
     return v;
 }
 
-// Granule g (of n columns) of a row.  kVec: whole and aligned.
+// A granule of n columns at p.  kVec: whole and aligned.
 template <int kType, bool kVec>
-__device__ __forceinline__ Raw<kType> fetch(const typename Word<kType>::type* row, uint32_t g, int n, bool vec) {
-    const typename Word<kType>::type* p = row + (int64_t)g * kGranule;
+__device__ __forceinline__ Raw<kType> fetch(const typename Word<kType>::type* p, int n, bool vec) {
     if constexpr (kVec) return load_raw<kType>(p);
     else return load_words<kType>(p, n, vec);
 }
 template <int kType, bool kVec>
-__device__ __forceinline__ void put(typename Word<kType>::type* row, uint32_t g, int n, bool vec, const Raw<kType>& r) {
-    typename Word<kType>::type* p = row + (int64_t)g * kGranule;
+__device__ __forceinline__ void put(typename Word<kType>::type* p, int n, bool vec, const Raw<kType>& r) {
     if constexpr (kVec) store_raw<kType>(p, r);
     else store_words<kType>(p, n, vec, r);
 }
@@ -107,11 +105,11 @@ __device__ __forceinline__ Raw<kType> no_words() {
 
 // residual + D(x)
 template <int kType, bool kFused>
-__device__ __forceinline__ Granule join_h(const ForwardArgs<kType>& a, const Raw<kType>& x, const Raw<kType>& r, uint64_t offset, int64_t row,
+__device__ __forceinline__ Granule join_h(const ForwardArgs<kType>& a, const Raw<kType>& x, const Raw<kType>& r, uint64_t offset, uint32_t row,
                                           uint32_t g) {
     Granule v = widen_raw<kType>(x);
     if constexpr (kFused) {
-        if (a.drop.active) drop_granule(a.drop, offset, (uint32_t)row, g, v);
+        if (a.drop.active) drop_granule(a.drop, offset, row, g, v);
         if (a.residual != nullptr) {
             const Granule u = widen_raw<kType>(r);
 #pragma unroll
@@ -141,6 +139,13 @@ __device__ __forceinline__ float centre(Granule& v, float mean, int n) {
         s = fma2(v.p[j], v.p[j], s);
     }
     return s.x + s.y;
+}
+
+// 1 / sqrt(v): the hardware's approximation, within 2^-22.9 of it.
+__device__ __forceinline__ float inverse_root(float v) {
+    float r;
+    asm("rsqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
 }
 
 // Sum over the block in every thread, in a fixed order.  `scratch` holds one entry per warp.
@@ -181,8 +186,8 @@ __global__ void __launch_bounds__(kLoopThreads) norm_forward_loop_kernel(const F
         const auto* x = a.x + row * a.ld_x;
         const auto* r = a.residual + row * a.ld_residual;
         const auto h = [&](uint32_t g, int n) {
-            const Raw<kType> res = kFused && a.residual != nullptr ? fetch<kType, false>(r, g, n, a.vec) : no_words<kType>();
-            return join_h<kType, kFused>(a, fetch<kType, false>(x, g, n, a.vec), res, offset, row, g);
+            const Raw<kType> res = kFused && a.residual != nullptr ? fetch<kType, false>(r + (int64_t)g * kGranule, n, a.vec) : no_words<kType>();
+            return join_h<kType, kFused>(a, fetch<kType, false>(x + (int64_t)g * kGranule, n, a.vec), res, offset, (uint32_t)row, g);
         };
         float sum = 0.0f;
         for (uint32_t g = threadIdx.x; g < granules; g += kLoopThreads) {
@@ -196,7 +201,7 @@ __global__ void __launch_bounds__(kLoopThreads) norm_forward_loop_kernel(const F
             Granule v = h(g, n);
             sum += centre(v, mean, n);
         }
-        const float rstd = 1.0f / sqrtf(block_sum(make_float2(sum, 0.0f), scratch).x / count + a.eps);
+        const float rstd = inverse_root(block_sum(make_float2(sum, 0.0f), scratch).x / count + a.eps);
         if (threadIdx.x == 0) {
             if (a.mean != nullptr) a.mean[row] = mean;
             if (a.rstd != nullptr) a.rstd[row] = rstd;
@@ -204,11 +209,11 @@ __global__ void __launch_bounds__(kLoopThreads) norm_forward_loop_kernel(const F
         for (uint32_t g = threadIdx.x; g < granules; g += kLoopThreads) {
             const int n = granule_columns(a.cols, g);
             Granule v = h(g, n);
-            if (kFused && a.h != nullptr) put<kType, false>(a.h + row * a.ld_h, g, n, a.vec, finish<kType>(v));
+            if (kFused && a.h != nullptr) put<kType, false>(a.h + row * a.ld_h + (int64_t)g * kGranule, n, a.vec, finish<kType>(v));
             const Granule w = load_columns(a.weight, g, n, 1.0f), b = load_columns(a.bias, g, n, 0.0f);
 #pragma unroll
             for (int j = 0; j < 4; ++j) v.p[j] = fma2(mul2(add2(v.p[j], both(-mean)), both(rstd)), w.p[j], b.p[j]);
-            put<kType, false>(a.y + row * a.ld_y, g, n, a.vec, finish_output<kType>(a, v, n, hist));
+            put<kType, false>(a.y + row * a.ld_y + (int64_t)g * kGranule, n, a.vec, finish_output<kType>(a, v, n, hist));
         }
     }
     if (hist != nullptr) flush_hist(hist, a.quant, a.stats, (uint64_t)a.rows * (uint64_t)a.cols);
@@ -218,29 +223,45 @@ __global__ void __launch_bounds__(kLoopThreads) norm_forward_loop_kernel(const F
 // one is whole warps.  Granule k * team + t of the row is thread t's k-th, k < V.
 constexpr int kMaxTeam = 512;
 
-// Sum over a team in every thread, in a fixed order.  scratch: 16 entries, those past the team's warps zero;
-// one barrier, so the team's next sum needs another scratch.
-template <typename T, typename Add>
-__device__ __forceinline__ T team_sum(T s, int team, int t, int barrier, T* scratch, Add add) {
-    for (int off = team < 32 ? team / 2 : 16; off > 0; off >>= 1) s = add(s, add.other(s, off));
-    if (team > 32) {
-        if ((t & 31) == 0) scratch[t >> 5] = s;
-        asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(team) : "memory");
-        s = add(add(scratch[0], scratch[1]), add(scratch[2], scratch[3]));
-        for (int i = 4; i < team / 32; i += 4) s = add(s, add(add(scratch[i], scratch[i + 1]), add(scratch[i + 2], scratch[i + 3])));
+struct AddOne {
+    using T = float;
+    __device__ __forceinline__ static float add(float a, float b) { return a + b; }
+    __device__ __forceinline__ static float across(float s, int off) { return add(s, __shfl_xor_sync(0xFFFFFFFFu, s, off)); }
+    __device__ __forceinline__ static float four(const float* p) {
+        const float4 q = *reinterpret_cast<const float4*>(p);
+        return (q.x + q.y) + (q.z + q.w);
+    }
+};
+struct AddTwo {
+    using T = float2;
+    __device__ __forceinline__ static float2 add(float2 a, float2 b) { return add2(a, b); }
+    __device__ __forceinline__ static float2 across(float2 s, int off) {
+        return add2(s, make_float2(__shfl_xor_sync(0xFFFFFFFFu, s.x, off), __shfl_xor_sync(0xFFFFFFFFu, s.y, off)));
+    }
+    __device__ __forceinline__ static float2 four(const float2* p) {
+        const float4 q = reinterpret_cast<const float4*>(p)[0], r = reinterpret_cast<const float4*>(p)[1];
+        return add2(add2(make_float2(q.x, q.y), make_float2(q.z, q.w)), add2(make_float2(r.x, r.y), make_float2(r.z, r.w)));
+    }
+};
+
+// Sum over a team in every thread, in a fixed order.  kWarps: the team is whole warps.  scratch: 16 entries, those
+// past the team's warps zero; one barrier, so the team's next sum needs another scratch.
+template <typename Add, bool kWarps>
+__device__ __forceinline__ typename Add::T team_sum(typename Add::T s, int team, int t, int barrier, typename Add::T* scratch) {
+    if constexpr (!kWarps) {
+        for (int off = team >> 1; off > 0; off >>= 1) s = Add::across(s, off);
+    } else {
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) s = Add::across(s, off);
+        if (team > 32) {
+            if ((t & 31) == 0) scratch[t >> 5] = s;
+            asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(team) : "memory");
+            s = Add::four(scratch);
+            for (int i = 4; i * 32 < team; i += 4) s = Add::add(s, Add::four(scratch + i));
+        }
     }
     return s;
 }
-struct AddOne {
-    __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
-    __device__ __forceinline__ float other(float s, int off) const { return __shfl_xor_sync(0xFFFFFFFFu, s, off); }
-};
-struct AddTwo {
-    __device__ __forceinline__ float2 operator()(float2 a, float2 b) const { return add2(a, b); }
-    __device__ __forceinline__ float2 other(float2 s, int off) const {
-        return make_float2(__shfl_xor_sync(0xFFFFFFFFu, s.x, off), __shfl_xor_sync(0xFFFFFFFFu, s.y, off));
-    }
-};
 
 // A row is read once and stays in its team's registers.  V <= 2: so do the team's weight and bias, from row to
 // row, and the next row is on its way while this one is worked on.  V = 4: longer rows, without either.
@@ -249,7 +270,7 @@ __global__ void __launch_bounds__(kMaxTeam) norm_forward_rows_kernel(const Forwa
     constexpr bool kKeep = V <= 2;
     constexpr bool kAhead = kKeep && kVec;
     extern __shared__ uint32_t lane_hist[];
-    __shared__ float scratch[kMaxTeam / 32][2][16];
+    __shared__ __align__(16) float scratch[kMaxTeam / 32][2][16];
     grid_launch_dependents();
     grid_dependency_wait();
     uint32_t* hist = a.stats != nullptr ? lane_hist : nullptr;
@@ -264,22 +285,28 @@ __global__ void __launch_bounds__(kMaxTeam) norm_forward_rows_kernel(const Forwa
     const uint64_t offset = kFused ? drop_offset(a.drop) : 0ull;
     const bool residual = kFused && a.residual != nullptr;
     const int64_t step = (int64_t)gridDim.x * teams;
-    int n[V];  // columns of each granule
+    const int next = team * kGranule;  // elements between a thread's granules
+    int n[V];                          // columns of each granule
 #pragma unroll
     for (int k = 0; k < V; ++k) n[k] = granule_columns(a.cols, k * team + t);
 
     // A team past the last row, whose warp has teams with one, keeps in step with them and stores nothing.
-    int64_t base = (int64_t)blockIdx.x * teams, row = base + mine;
+    int64_t row = (int64_t)blockIdx.x * teams + mine;
+    const auto* px = a.x + row * a.ld_x + t * kGranule;
+    const auto* pr = a.residual + row * a.ld_residual + t * kGranule;
+    auto* ph = a.h + row * a.ld_h + t * kGranule;
+    auto* py = a.y + row * a.ld_y + t * kGranule;
     Raw<kType> x[V], r[V];
-    const auto fetch_row = [&](int64_t at) {
+    const auto fetch_row = [&](bool there) {
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            const bool there = at < a.rows && n[k] > 0;
-            x[k] = there ? fetch<kType, kVec>(a.x + at * a.ld_x, k * team + t, n[k], a.vec) : no_words<kType>();
-            r[k] = there && residual ? fetch<kType, kVec>(a.residual + at * a.ld_residual, k * team + t, n[k], a.vec) : no_words<kType>();
+            x[k] = there && n[k] > 0 ? fetch<kType, kVec>(px + k * next, n[k], a.vec) : no_words<kType>();
+            if (residual) r[k] = there && n[k] > 0 ? fetch<kType, kVec>(pr + k * next, n[k], a.vec) : no_words<kType>();
         }
+        px += step * a.ld_x;
+        pr += step * a.ld_residual;
     };
-    if (kAhead) fetch_row(row);
+    if (kAhead) fetch_row(row < a.rows);
     Granule w[kKeep ? V : 1], b[kKeep ? V : 1];
     if constexpr (kKeep) {
 #pragma unroll
@@ -288,26 +315,28 @@ __global__ void __launch_bounds__(kMaxTeam) norm_forward_rows_kernel(const Forwa
             b[k] = load_columns(a.bias, k * team + t, n[k], 0.0f);
         }
     }
-    for (; base < a.rows; base += step, row += step) {
+    for (; row - mine < a.rows; row += step) {
         const bool live = row < a.rows;
-        if (!kAhead) fetch_row(row);
+        if (!kAhead) fetch_row(live);
         Granule v[V];
 #pragma unroll
-        for (int k = 0; k < V; ++k) v[k] = join_h<kType, kFused>(a, x[k], r[k], offset, row, k * team + t);
-        if (kAhead) fetch_row(row + step);
+        for (int k = 0; k < V; ++k) v[k] = join_h<kType, kFused>(a, x[k], r[k], offset, (uint32_t)row, k * team + t);
+        if (kAhead) fetch_row(row + step < a.rows);
         if (kFused && a.h != nullptr) {
 #pragma unroll
             for (int k = 0; k < V; ++k)
-                if (live && n[k] > 0) put<kType, kVec>(a.h + row * a.ld_h, k * team + t, n[k], a.vec, finish<kType>(v[k]));
+                if (live && n[k] > 0) put<kType, kVec>(ph + k * next, n[k], a.vec, finish<kType>(v[k]));
         }
         float s = 0.0f;
 #pragma unroll
         for (int k = 0; k < V; ++k) s += sum8(v[k]);
-        const float mean = team_sum(s, team, t, 1 + slot, scratch[slot][0], AddOne()) * inverse;
+        const float mean = team_sum<AddOne, (V > 1)>(s, team, t, 1 + slot, scratch[slot][0]) * inverse;
         s = 0.0f;
 #pragma unroll
-        for (int k = 0; k < V; ++k) s += kVec ? (n[k] > 0 ? centre(v[k], mean, kGranule) : 0.0f) : centre(v[k], mean, n[k]);
-        const float rstd = 1.0f / sqrtf(team_sum(s, team, t, 1 + slot, scratch[slot][1], AddOne()) * inverse + a.eps);
+        for (int k = 0; k < V; ++k) {
+            if (n[k] > 0) s += centre(v[k], mean, kVec ? kGranule : n[k]);
+        }
+        const float rstd = inverse_root(team_sum<AddOne, (V > 1)>(s, team, t, 1 + slot, scratch[slot][1]) * inverse + a.eps);
         if (t == 0 && live) {
             if (a.mean != nullptr) a.mean[row] = mean;
             if (a.rstd != nullptr) a.rstd[row] = rstd;
@@ -323,9 +352,11 @@ __global__ void __launch_bounds__(kMaxTeam) norm_forward_rows_kernel(const Forwa
                 const Granule& bk = b[kKeep ? k : 0];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[k].p[j] = fma2(mul2(v[k].p[j], both(rstd)), wk.p[j], bk.p[j]);
-                put<kType, kVec>(a.y + row * a.ld_y, k * team + t, n[k], a.vec, finish_output<kType>(a, v[k], n[k], hist));
+                put<kType, kVec>(py + k * next, n[k], a.vec, finish_output<kType>(a, v[k], n[k], hist));
             }
         }
+        ph += step * a.ld_h;
+        py += step * a.ld_y;
     }
     if (hist != nullptr) flush_hist(hist, a.quant, a.stats, (uint64_t)a.rows * (uint64_t)a.cols);
 }
@@ -353,25 +384,40 @@ __device__ __forceinline__ float2 row_sums(const Granule& dy, const Granule& xha
     return make_float2(s.x + s.y, q.x + q.y);
 }
 
+// Where the gradients of one row go, at a thread's first granule.
+template <int kType>
+struct GradientRow {
+    const typename Word<kType>::type* dh;
+    typename Word<kType>::type* dx;
+    typename Word<kType>::type* dresidual;
+    __device__ __forceinline__ GradientRow(const BackwardArgs<kType>& a, int64_t row, int64_t col)
+        : dh(a.dh + row * a.ld_dh + col), dx(a.dx + row * a.ld_dx + col), dresidual(a.dresidual + row * a.ld_dresidual + col) {}
+    __device__ __forceinline__ void advance(const BackwardArgs<kType>& a, int64_t rows) {
+        dh += rows * a.ld_dh;
+        dx += rows * a.ld_dx;
+        dresidual += rows * a.ld_dresidual;
+    }
+};
+
 // What a granule's gradients become: dh (with what arrives by another path) to dresidual, D of it to dx.
 template <int kType, bool kFused, bool kVec>
-__device__ __forceinline__ void store_gradients(const BackwardArgs<kType>& a, const Granule& dy, const Granule& xhat, const Granule& w,
-                                                float rstd, float c1, float c2, int64_t row, uint32_t g, int n, uint64_t offset,
-                                                uint32_t* hist) {
+__device__ __forceinline__ void store_gradients(const BackwardArgs<kType>& a, const GradientRow<kType>& to, int64_t at, const Granule& dy,
+                                                const Granule& xhat, const Granule& w, float rstd, float c1, float c2, uint32_t row,
+                                                uint32_t g, int n, uint64_t offset, uint32_t* hist) {
     Granule d;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
         d.p[j] = mul2(fma2(xhat.p[j], both(-c2), fma2(dy.p[j], w.p[j], both(-c1))), both(rstd));
     if constexpr (kFused) {
         if (a.dh != nullptr) {
-            const Granule more = widen_raw<kType>(fetch<kType, kVec>(a.dh + row * a.ld_dh, g, n, a.vec));
+            const Granule more = widen_raw<kType>(fetch<kType, kVec>(to.dh + at, n, a.vec));
 #pragma unroll
             for (int j = 0; j < 4; ++j) d.p[j] = add2(d.p[j], more.p[j]);
         }
-        if (a.dresidual != nullptr) put<kType, kVec>(a.dresidual + row * a.ld_dresidual, g, n, a.vec, finish<kType>(d));
-        if (a.drop.active && a.dx != nullptr) drop_granule(a.drop, offset, (uint32_t)row, g, d);
+        if (a.dresidual != nullptr) put<kType, kVec>(to.dresidual + at, n, a.vec, finish<kType>(d));
+        if (a.drop.active && a.dx != nullptr) drop_granule(a.drop, offset, row, g, d);
     }
-    if (a.dx != nullptr) put<kType, kVec>(a.dx + row * a.ld_dx, g, n, a.vec, finish_output<kType>(a, d, n, hist));
+    if (a.dx != nullptr) put<kType, kVec>(to.dx + at, n, a.vec, finish_output<kType>(a, d, n, hist));
 }
 
 // Long rows: a block takes a row at a time and reads it twice.
@@ -387,8 +433,8 @@ __global__ void __launch_bounds__(kLoopThreads) norm_backward_loop_kernel(const 
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const float mean = a.mean[row], rstd = a.rstd[row];
         const auto load = [&](uint32_t g, int n, Granule& dy, Granule& xhat, Granule& w) {
-            dy = widen_raw<kType>(fetch<kType, false>(a.dy + row * a.ld_dy, g, n, a.vec));
-            xhat = normalise(widen_raw<kType>(fetch<kType, false>(a.h + row * a.ld_h, g, n, a.vec)), mean, rstd, n);
+            dy = widen_raw<kType>(fetch<kType, false>(a.dy + row * a.ld_dy + (int64_t)g * kGranule, n, a.vec));
+            xhat = normalise(widen_raw<kType>(fetch<kType, false>(a.h + row * a.ld_h + (int64_t)g * kGranule, n, a.vec)), mean, rstd, n);
             w = load_columns(a.weight, g, n, 1.0f);
         };
         float2 s = make_float2(0.0f, 0.0f);
@@ -401,7 +447,8 @@ __global__ void __launch_bounds__(kLoopThreads) norm_backward_loop_kernel(const 
         for (uint32_t g = threadIdx.x; g < granules; g += kLoopThreads) {
             const int n = granule_columns(a.cols, g);
             load(g, n, dy, xhat, w);
-            store_gradients<kType, kFused, false>(a, dy, xhat, w, rstd, s.x / count, s.y / count, row, g, n, offset, hist);
+            store_gradients<kType, kFused, false>(a, GradientRow<kType>(a, row, 0), (int64_t)g * kGranule, dy, xhat, w, rstd, s.x / count,
+                                                  s.y / count, (uint32_t)row, g, n, offset, hist);
         }
     }
     if (hist != nullptr) flush_hist(hist, a.quant, a.stats, (uint64_t)a.rows * (uint64_t)a.cols);
@@ -419,8 +466,8 @@ __global__ void __launch_bounds__(32 * kColumnWarps) norm_column_sums_kernel(con
     Granule dw = splat(0.0f), db = splat(0.0f);
     if (n > 0) {
         for (int64_t row = (int64_t)blockIdx.y * kColumnWarps + warp; row < a.rows; row += (int64_t)gridDim.y * kColumnWarps) {
-            const Granule dy = widen_raw<kType>(fetch<kType, false>(a.dy + row * a.ld_dy, g, n, a.vec));
-            const Granule xhat = normalise(widen_raw<kType>(fetch<kType, false>(a.h + row * a.ld_h, g, n, a.vec)), a.mean[row], a.rstd[row], n);
+            const Granule dy = widen_raw<kType>(fetch<kType, false>(a.dy + row * a.ld_dy + (int64_t)g * kGranule, n, a.vec));
+            const Granule xhat = normalise(widen_raw<kType>(fetch<kType, false>(a.h + row * a.ld_h + (int64_t)g * kGranule, n, a.vec)), a.mean[row], a.rstd[row], n);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 dw.p[j] = fma2(dy.p[j], xhat.p[j], dw.p[j]);
@@ -450,7 +497,7 @@ template <int kType, int V, bool kFused, bool kVec>
 __global__ void __launch_bounds__(kMaxTeam) norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int hist_words) {
     constexpr bool kAhead = kVec && kType != QFMT_F32;
     extern __shared__ uint32_t dynamic[];  // [hist_words] histogram, then the sums of a block's teams
-    __shared__ float2 scratch[kMaxTeam / 32][2][16];
+    __shared__ __align__(16) float2 scratch[kMaxTeam / 32][2][16];
     grid_launch_dependents();
     grid_dependency_wait();
     uint32_t* hist = a.stats != nullptr ? dynamic : nullptr;
@@ -464,6 +511,7 @@ __global__ void __launch_bounds__(kMaxTeam) norm_backward_rows_kernel(const Back
     const float inverse = 1.0f / (float)a.cols;
     const uint64_t offset = kFused ? drop_offset(a.drop) : 0ull;
     const int64_t step = (int64_t)gridDim.x * teams;
+    const int next = team * kGranule;  // elements between a thread's granules
     int n[V];
     Granule w[V], dw[V], db[V];
 #pragma unroll
@@ -471,23 +519,28 @@ __global__ void __launch_bounds__(kMaxTeam) norm_backward_rows_kernel(const Back
         n[k] = granule_columns(a.cols, k * team + t);
         dw[k] = db[k] = splat(0.0f);
     }
-    int64_t base = (int64_t)blockIdx.x * teams, row = base + mine;
+    int64_t row = (int64_t)blockIdx.x * teams + mine;
+    const auto* pdy = a.dy + row * a.ld_dy + t * kGranule;
+    const auto* ph = a.h + row * a.ld_h + t * kGranule;
+    GradientRow<kType> to(a, row, t * kGranule);
     Raw<kType> raw_dy[V], raw_h[V];
     float mean = 0.0f, rstd = 0.0f;
     const auto fetch_row = [&](int64_t at) {
-        if (at < a.rows) mean = a.mean[at], rstd = a.rstd[at];
+        const bool there = at < a.rows;
+        if (there) mean = a.mean[at], rstd = a.rstd[at];
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            const bool there = at < a.rows && n[k] > 0;
-            raw_dy[k] = there ? fetch<kType, kVec>(a.dy + at * a.ld_dy, k * team + t, n[k], a.vec) : no_words<kType>();
-            raw_h[k] = there ? fetch<kType, kVec>(a.h + at * a.ld_h, k * team + t, n[k], a.vec) : no_words<kType>();
+            raw_dy[k] = there && n[k] > 0 ? fetch<kType, kVec>(pdy + k * next, n[k], a.vec) : no_words<kType>();
+            raw_h[k] = there && n[k] > 0 ? fetch<kType, kVec>(ph + k * next, n[k], a.vec) : no_words<kType>();
         }
+        pdy += step * a.ld_dy;
+        ph += step * a.ld_h;
     };
     if (kAhead) fetch_row(row);
 #pragma unroll
     for (int k = 0; k < V; ++k) w[k] = load_columns(a.weight, k * team + t, n[k], 1.0f);
     int parity = 0;
-    for (; base < a.rows; base += step, row += step, parity ^= 1) {
+    for (; row - mine < a.rows; row += step, parity ^= 1) {
         const bool live = row < a.rows;
         if (!kAhead) fetch_row(row);
         Granule dy[V], xhat[V];
@@ -496,22 +549,24 @@ __global__ void __launch_bounds__(kMaxTeam) norm_backward_rows_kernel(const Back
 #pragma unroll
         for (int k = 0; k < V; ++k) {
             dy[k] = widen_raw<kType>(raw_dy[k]);
-            xhat[k] = normalise(widen_raw<kType>(raw_h[k]), mean, rstd, live ? (kVec && n[k] > 0 ? kGranule : n[k]) : 0);
+            xhat[k] = splat(0.0f);
+            if (live && n[k] > 0) xhat[k] = normalise(widen_raw<kType>(raw_h[k]), mean, rstd, kVec ? kGranule : n[k]);
             s = add2(s, row_sums(dy[k], xhat[k], w[k]));
-        }
-        if (kAhead) fetch_row(row + step);
-        s = team_sum(s, team, t, 1 + slot, scratch[slot][parity], AddTwo());
-        const float c1 = s.x * inverse, c2 = s.y * inverse;
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 dw[k].p[j] = fma2(dy[k].p[j], xhat[k].p[j], dw[k].p[j]);
                 db[k].p[j] = add2(db[k].p[j], dy[k].p[j]);
             }
-            if (live && n[k] > 0)
-                store_gradients<kType, kFused, kVec>(a, dy[k], xhat[k], w[k], this_rstd, c1, c2, row, k * team + t, n[k], offset, hist);
         }
+        if (kAhead) fetch_row(row + step);
+        s = team_sum<AddTwo, (V > 1)>(s, team, t, 1 + slot, scratch[slot][parity]);
+        const float c1 = s.x * inverse, c2 = s.y * inverse;
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            if (live && n[k] > 0)
+                store_gradients<kType, kFused, kVec>(a, to, k * next, dy[k], xhat[k], w[k], this_rstd, c1, c2, (uint32_t)row, k * team + t,
+                                                     n[k], offset, hist);
+        to.advance(a, step);
     }
     if (hist != nullptr) flush_hist(hist, a.quant, a.stats, (uint64_t)a.rows * (uint64_t)a.cols);
     if (a.partial == nullptr) return;
@@ -521,8 +576,8 @@ __global__ void __launch_bounds__(kMaxTeam) norm_backward_rows_kernel(const Back
         for (int k = 0; k < V; ++k)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                dw[k].p[j] = add2(dw[k].p[j], AddTwo().other(dw[k].p[j], off));
-                db[k].p[j] = add2(db[k].p[j], AddTwo().other(db[k].p[j], off));
+                dw[k].p[j] = AddTwo::across(dw[k].p[j], off);
+                db[k].p[j] = AddTwo::across(db[k].p[j], off);
             }
     }
     const int unit = team < 32 ? 32 : team, units = blockDim.x / unit;  // threads that still hold a sum of their own
