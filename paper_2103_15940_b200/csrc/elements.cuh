@@ -46,17 +46,21 @@ struct Raw {
     uint32_t w[kType == QFMT_F32 ? 8 : 4];
 };
 
+// A whole granule, or zeros where `there` is false (a predicate on the load, not a branch around it).
 template <int kType>
-__device__ __forceinline__ Raw<kType> load_raw(const typename Word<kType>::type* p) {
+__device__ __forceinline__ Raw<kType> load_raw(const typename Word<kType>::type* p, bool there = true) {
     Raw<kType> r;
+#pragma unroll
+    for (uint32_t& w : r.w) w = 0u;
     if constexpr (kType == QFMT_F32) {
-        asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                     : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]), "=r"(r.w[5]), "=r"(r.w[6]),
-                       "=r"(r.w[7])
-                     : "l"(p));
+        asm volatile("{ .reg .pred q; setp.ne.u32 q, %9, 0;"
+                     " @q ld.global.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8]; }"
+                     : "+r"(r.w[0]), "+r"(r.w[1]), "+r"(r.w[2]), "+r"(r.w[3]), "+r"(r.w[4]), "+r"(r.w[5]), "+r"(r.w[6]),
+                       "+r"(r.w[7])
+                     : "l"(p), "r"((uint32_t)there));
     } else {
-        asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];"
-                     : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]) : "l"(p));
+        asm volatile("{ .reg .pred q; setp.ne.u32 q, %5, 0; @q ld.global.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4]; }"
+                     : "+r"(r.w[0]), "+r"(r.w[1]), "+r"(r.w[2]), "+r"(r.w[3]) : "l"(p), "r"((uint32_t)there));
     }
     return r;
 }

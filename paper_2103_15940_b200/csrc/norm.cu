@@ -35,6 +35,7 @@ struct ForwardArgs {
     float eps;
     bool vec;  // every granule whole and aligned
     bool fmt;  // quant holds a format to round to
+    float inverse;  // 1 / cols
     DropParams drop;
     QuantParams quant;
     qfmt_stats_t* stats;
@@ -56,6 +57,7 @@ struct BackwardArgs {
     int64_t rows, cols;
     bool vec;  // every granule whole and aligned
     bool fmt;  // quant holds a format to round to
+    float inverse;  // 1 / cols
     DropParams drop;
     QuantParams quant;
     qfmt_stats_t* stats;
@@ -84,23 +86,19 @@ __device__ __forceinline__ Granule load_columns(const float* p, int64_t g, int n
     return v;
 }
 
-// A granule of n columns at p.  kVec: whole and aligned.
-template <int kType, bool kVec>
+// A granule of n columns at p, zeros where there are none.  kPlain: whole and aligned, or not there at all.
+template <int kType, bool kPlain>
 __device__ __forceinline__ Raw<kType> fetch(const typename Word<kType>::type* p, int n, bool vec) {
-    if constexpr (kVec) return load_raw<kType>(p);
+    if constexpr (kPlain) return load_raw<kType>(p, n > 0);
     else return load_words<kType>(p, n, vec);
 }
-template <int kType, bool kVec>
+template <int kType, bool kPlain>
 __device__ __forceinline__ void put(typename Word<kType>::type* p, int n, bool vec, const Raw<kType>& r) {
-    if constexpr (kVec) store_raw<kType>(p, r);
-    else store_words<kType>(p, n, vec, r);
-}
-template <int kType>
-__device__ __forceinline__ Raw<kType> no_words() {
-    Raw<kType> r;
-#pragma unroll
-    for (uint32_t& w : r.w) w = 0u;
-    return r;
+    if constexpr (kPlain) {
+        if (n > 0) store_raw<kType>(p, r);
+    } else {
+        store_words<kType>(p, n, vec, r);
+    }
 }
 
 // residual + D(x)
@@ -119,23 +117,25 @@ __device__ __forceinline__ Granule join_h(const ForwardArgs<kType>& a, const Raw
     return v;
 }
 
-template <int kType, typename Args>
+template <int kType, bool kPlain, typename Args>
 __device__ __forceinline__ Raw<kType> finish_output(const Args& a, const Granule& v, int n, uint32_t* hist) {
-    return a.fmt ? finish_format<kType>(v, n, a.quant, hist) : finish<kType>(v);
+    return !kPlain && a.fmt ? finish_format<kType>(v, n, a.quant, hist) : finish<kType>(v);
 }
 
 __device__ __forceinline__ float sum8(const Granule& v) {
     const float2 s = add2(add2(v.p[0], v.p[1]), add2(v.p[2], v.p[3]));
     return s.x + s.y;
 }
-// v - mean where a column exists, 0 elsewhere; the sum of its squares.
+// v - mean where a column exists, 0 elsewhere; the sum of its squares.  kPlain: all eight exist or (v = 0) none.
+template <bool kPlain>
 __device__ __forceinline__ float centre(Granule& v, float mean, int n) {
+    const float2 shift = both(kPlain && n == 0 ? 0.0f : -mean);
     float2 s = make_float2(0.0f, 0.0f);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        v.p[j] = add2(v.p[j], both(-mean));
-        if (2 * j >= n) v.p[j].x = 0.0f;
-        if (2 * j + 1 >= n) v.p[j].y = 0.0f;
+        v.p[j] = add2(v.p[j], shift);
+        if (!kPlain && 2 * j >= n) v.p[j].x = 0.0f;
+        if (!kPlain && 2 * j + 1 >= n) v.p[j].y = 0.0f;
         s = fma2(v.p[j], v.p[j], s);
     }
     return s.x + s.y;
@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(kLoopThreads) norm_forward_loop_kernel(const F
         const auto* x = a.x + row * a.ld_x;
         const auto* r = a.residual + row * a.ld_residual;
         const auto h = [&](uint32_t g, int n) {
-            const Raw<kType> res = kFused && a.residual != nullptr ? fetch<kType, false>(r + (int64_t)g * kGranule, n, a.vec) : no_words<kType>();
+            const Raw<kType> res = kFused && a.residual != nullptr ? fetch<kType, false>(r + (int64_t)g * kGranule, n, a.vec) : Raw<kType>();
             return join_h<kType, kFused>(a, fetch<kType, false>(x + (int64_t)g * kGranule, n, a.vec), res, offset, (uint32_t)row, g);
         };
         float sum = 0.0f;
@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(kLoopThreads) norm_forward_loop_kernel(const F
         for (uint32_t g = threadIdx.x; g < granules; g += kLoopThreads) {
             const int n = granule_columns(a.cols, g);
             Granule v = h(g, n);
-            sum += centre(v, mean, n);
+            sum += centre<false>(v, mean, n);
         }
         const float rstd = inverse_root(block_sum(make_float2(sum, 0.0f), scratch).x / count + a.eps);
         if (threadIdx.x == 0) {
@@ -213,7 +213,7 @@ __global__ void __launch_bounds__(kLoopThreads) norm_forward_loop_kernel(const F
             const Granule w = load_columns(a.weight, g, n, 1.0f), b = load_columns(a.bias, g, n, 0.0f);
 #pragma unroll
             for (int j = 0; j < 4; ++j) v.p[j] = fma2(mul2(add2(v.p[j], both(-mean)), both(rstd)), w.p[j], b.p[j]);
-            put<kType, false>(a.y + row * a.ld_y + (int64_t)g * kGranule, n, a.vec, finish_output<kType>(a, v, n, hist));
+            put<kType, false>(a.y + row * a.ld_y + (int64_t)g * kGranule, n, a.vec, finish_output<kType, false>(a, v, n, hist));
         }
     }
     if (hist != nullptr) flush_hist(hist, a.quant, a.stats, (uint64_t)a.rows * (uint64_t)a.cols);
@@ -223,90 +223,114 @@ __global__ void __launch_bounds__(kLoopThreads) norm_forward_loop_kernel(const F
 // one is whole warps.  Granule k * team + t of the row is thread t's k-th, k < V.
 constexpr int kMaxTeam = 512;
 
-struct AddOne {
-    using T = float;
-    __device__ __forceinline__ static float add(float a, float b) { return a + b; }
-    __device__ __forceinline__ static float across(float s, int off) { return add(s, __shfl_xor_sync(0xFFFFFFFFu, s, off)); }
-    __device__ __forceinline__ static float four(const float* p) {
-        const float4 q = *reinterpret_cast<const float4*>(p);
-        return (q.x + q.y) + (q.z + q.w);
-    }
-};
-struct AddTwo {
-    using T = float2;
-    __device__ __forceinline__ static float2 add(float2 a, float2 b) { return add2(a, b); }
-    __device__ __forceinline__ static float2 across(float2 s, int off) {
-        return add2(s, make_float2(__shfl_xor_sync(0xFFFFFFFFu, s.x, off), __shfl_xor_sync(0xFFFFFFFFu, s.y, off)));
-    }
-    __device__ __forceinline__ static float2 four(const float2* p) {
-        const float4 q = reinterpret_cast<const float4*>(p)[0], r = reinterpret_cast<const float4*>(p)[1];
-        return add2(add2(make_float2(q.x, q.y), make_float2(q.z, q.w)), add2(make_float2(r.x, r.y), make_float2(r.z, r.w)));
-    }
-};
-
-// Sum over a team in every thread, in a fixed order.  kWarps: the team is whole warps.  scratch: 16 entries, those
-// past the team's warps zero; one barrier, so the team's next sum needs another scratch.
-template <typename Add, bool kWarps>
-__device__ __forceinline__ typename Add::T team_sum(typename Add::T s, int team, int t, int barrier, typename Add::T* scratch) {
-    if constexpr (!kWarps) {
-        for (int off = team >> 1; off > 0; off >>= 1) s = Add::across(s, off);
-    } else {
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1) s = Add::across(s, off);
-        if (team > 32) {
-            if ((t & 31) == 0) scratch[t >> 5] = s;
-            asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(team) : "memory");
-            s = Add::four(scratch);
-            for (int i = 4; i * 32 < team; i += 4) s = Add::add(s, Add::four(scratch + i));
-        }
+// Sums over a team, in every thread and in a fixed order: of one value, or of two at once.  kWarps: the team is
+// whole warps.  kBlock: it is the block.  scratch: 16 entries, or two times 16, of which those past the team's
+// warps are zero; one barrier, so the team's next sum needs another scratch.
+template <bool kBlock>
+__device__ __forceinline__ void team_barrier(int team, int slot) {
+    if constexpr (kBlock) __syncthreads();
+    else asm volatile("bar.sync %0, %1;" ::"r"(1 + slot), "r"(team) : "memory");
+}
+__device__ __forceinline__ float sum_entries(const float* scratch, int team) {
+    float s = 0.0f;
+    for (int i = 0; i * 32 < team; i += 4) {
+        const float4 q = *reinterpret_cast<const float4*>(scratch + i);
+        const float u = (q.x + q.y) + (q.z + q.w);
+        s = i == 0 ? u : s + u;
     }
     return s;
 }
+__device__ __forceinline__ float across(float s, int off) { return s + __shfl_xor_sync(0xFFFFFFFFu, s, off); }
 
-// A row is read once and stays in its team's registers.  V <= 2: so do the team's weight and bias, from row to
-// row, and the next row is on its way while this one is worked on.  V = 4: longer rows, without either.
-template <int kType, int V, bool kFused, bool kVec>
-__global__ void __launch_bounds__(kMaxTeam) norm_forward_rows_kernel(const ForwardArgs<kType> a, int team) {
+template <bool kWarps, bool kBlock>
+__device__ __forceinline__ float team_sum(float s, int team, int t, int slot, float* scratch) {
+    if constexpr (!kWarps) {
+        for (int off = team >> 1; off > 0; off >>= 1) s = across(s, off);
+        return s;
+    } else {
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) s = across(s, off);
+        if (team == 32) return s;
+        if ((t & 31) == 0) scratch[t >> 5] = s;
+        team_barrier<kBlock>(team, slot);
+        return sum_entries(scratch, team);
+    }
+}
+
+// Two values: after one exchange the lower half of a warp holds the first value's partial sums and the upper half
+// the second's, so five shuffles do for both.
+template <bool kWarps, bool kBlock>
+__device__ __forceinline__ float2 team_sum(float2 s, int team, int t, int slot, float* scratch) {
+    if constexpr (!kWarps) {
+        for (int off = team >> 1; off > 0; off >>= 1) s = make_float2(across(s.x, off), across(s.y, off));
+        return s;
+    } else {
+        const bool upper = t & 16;
+        float u = (upper ? s.y : s.x) + __shfl_xor_sync(0xFFFFFFFFu, upper ? s.x : s.y, 16);
+#pragma unroll
+        for (int off = 8; off > 0; off >>= 1) u = across(u, off);
+        if (team == 32) {
+            const float v = __shfl_xor_sync(0xFFFFFFFFu, u, 16);
+            return upper ? make_float2(v, u) : make_float2(u, v);
+        }
+        if ((t & 15) == 0) scratch[(t & 16) + (t >> 5)] = u;
+        team_barrier<kBlock>(team, slot);
+        return make_float2(sum_entries(scratch, team), sum_entries(scratch + 16, team));
+    }
+}
+
+// Elements from a row of a team to its next one.
+struct ForwardSteps {
+    int64_t x, residual, h, y;
+};
+
+// R rows at a time are read once and stay in their team's registers.  V <= 2: so do the team's weight and bias,
+// from row to row, and with kPlain the next rows are on their way while these are worked on.  V = 4: longer rows,
+// without either.  kPlain: every granule whole and aligned, no format; otherwise any layout and an optional format.
+template <int kType, int V, int R, bool kFused, bool kPlain>
+__global__ void __launch_bounds__(kMaxTeam) norm_forward_rows_kernel(const ForwardArgs<kType> a, int team, const ForwardSteps step) {
     constexpr bool kKeep = V <= 2;
-    constexpr bool kAhead = kKeep && kVec;
+    constexpr bool kAhead = kKeep && kPlain;
     extern __shared__ uint32_t lane_hist[];
-    __shared__ __align__(16) float scratch[kMaxTeam / 32][2][16];
+    __shared__ __align__(16) float scratch[2][R][16];
     grid_launch_dependents();
     grid_dependency_wait();
-    uint32_t* hist = a.stats != nullptr ? lane_hist : nullptr;
+    uint32_t* hist = !kPlain && a.stats != nullptr ? lane_hist : nullptr;
     if (team > 32) {
-        for (int i = threadIdx.x; i < kMaxTeam; i += blockDim.x) (&scratch[0][0][0])[i] = 0.0f;
+        for (int i = threadIdx.x; i < 2 * R * 16; i += blockDim.x) (&scratch[0][0][0])[i] = 0.0f;
         __syncthreads();
     }
     if (hist != nullptr) clear_hist(hist, a.quant);
     const int mine = threadIdx.x / team, t = threadIdx.x - mine * team, teams = blockDim.x / team;
-    const int slot = team > 32 ? mine : 0;
-    const float inverse = 1.0f / (float)a.cols;
     const uint64_t offset = kFused ? drop_offset(a.drop) : 0ull;
     const bool residual = kFused && a.residual != nullptr;
-    const int64_t step = (int64_t)gridDim.x * teams;
     const int next = team * kGranule;  // elements between a thread's granules
     int n[V];                          // columns of each granule
 #pragma unroll
     for (int k = 0; k < V; ++k) n[k] = granule_columns(a.cols, k * team + t);
 
     // A team past the last row, whose warp has teams with one, keeps in step with them and stores nothing.
-    int64_t row = (int64_t)blockIdx.x * teams + mine;
+    const uint32_t rows = (uint32_t)a.rows, stride = gridDim.x * teams * R;
+    uint32_t row = (blockIdx.x * teams + mine) * R;
     const auto* px = a.x + row * a.ld_x + t * kGranule;
     const auto* pr = a.residual + row * a.ld_residual + t * kGranule;
     auto* ph = a.h + row * a.ld_h + t * kGranule;
     auto* py = a.y + row * a.ld_y + t * kGranule;
-    Raw<kType> x[V], r[V];
-    const auto fetch_row = [&](bool there) {
+    Raw<kType> x[R][V], r[R][V];
+    const auto fetch_rows = [&](uint32_t at) {
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-            x[k] = there && n[k] > 0 ? fetch<kType, kVec>(px + k * next, n[k], a.vec) : no_words<kType>();
-            if (residual) r[k] = there && n[k] > 0 ? fetch<kType, kVec>(pr + k * next, n[k], a.vec) : no_words<kType>();
+        for (int i = 0; i < R; ++i) {
+            const bool there = at + i < rows;
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                x[i][k] = fetch<kType, kPlain>(px + i * a.ld_x + k * next, there ? n[k] : 0, a.vec);
+                if (kFused) r[i][k] = fetch<kType, kPlain>(pr + i * a.ld_residual + k * next, there && residual ? n[k] : 0, a.vec);
+            }
         }
-        px += step * a.ld_x;
-        pr += step * a.ld_residual;
+        px += step.x;
+        pr += step.residual;
     };
-    if (kAhead) fetch_row(row < a.rows);
+    if (kAhead) fetch_rows(row);
     Granule w[kKeep ? V : 1], b[kKeep ? V : 1];
     if constexpr (kKeep) {
 #pragma unroll
@@ -315,59 +339,84 @@ __global__ void __launch_bounds__(kMaxTeam) norm_forward_rows_kernel(const Forwa
             b[k] = load_columns(a.bias, k * team + t, n[k], 0.0f);
         }
     }
-    for (; row - mine < a.rows; row += step) {
-        const bool live = row < a.rows;
-        if (!kAhead) fetch_row(live);
-        Granule v[V];
+    for (; row - mine * R < rows; row += stride) {
+        if (!kAhead) fetch_rows(row);
+        Granule v[R][V];
+        float s[R] = {}, mean[R], rstd[R];
 #pragma unroll
-        for (int k = 0; k < V; ++k) v[k] = join_h<kType, kFused>(a, x[k], r[k], offset, (uint32_t)row, k * team + t);
-        if (kAhead) fetch_row(row + step < a.rows);
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int k = 0; k < V; ++k) v[i][k] = join_h<kType, kFused>(a, x[i][k], r[i][k], offset, row + i, k * team + t);
+        if (kAhead) fetch_rows(row + stride);
         if (kFused && a.h != nullptr) {
 #pragma unroll
-            for (int k = 0; k < V; ++k)
-                if (live && n[k] > 0) put<kType, kVec>(ph + k * next, n[k], a.vec, finish<kType>(v[k]));
+            for (int i = 0; i < R; ++i)
+#pragma unroll
+                for (int k = 0; k < V; ++k)
+                    put<kType, kPlain>(ph + i * a.ld_h + k * next, row + i < rows ? n[k] : 0, a.vec, finish<kType>(v[i][k]));
         }
-        float s = 0.0f;
+        const auto total = [&](float (&out)[R], float* space) {
+            if constexpr (R == 2) {
+                const float2 q = team_sum<(V > 1), true>(make_float2(s[0], s[1]), team, t, 0, space);
+                out[0] = q.x * a.inverse;
+                out[1] = q.y * a.inverse;
+            } else {
+                out[0] = team_sum<(V > 1), true>(s[0], team, t, 0, space) * a.inverse;
+            }
+        };
 #pragma unroll
-        for (int k = 0; k < V; ++k) s += sum8(v[k]);
-        const float mean = team_sum<AddOne, (V > 1)>(s, team, t, 1 + slot, scratch[slot][0]) * inverse;
-        s = 0.0f;
+        for (int i = 0; i < R; ++i) {
+            s[i] = sum8(v[i][0]);
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-            if (n[k] > 0) s += centre(v[k], mean, kVec ? kGranule : n[k]);
+            for (int k = 1; k < V; ++k) s[i] += sum8(v[i][k]);
         }
-        const float rstd = inverse_root(team_sum<AddOne, (V > 1)>(s, team, t, 1 + slot, scratch[slot][1]) * inverse + a.eps);
-        if (t == 0 && live) {
-            if (a.mean != nullptr) a.mean[row] = mean;
-            if (a.rstd != nullptr) a.rstd[row] = rstd;
+        total(mean, scratch[0][0]);
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            s[i] = centre<kPlain>(v[i][0], mean[i], n[0]);
+#pragma unroll
+            for (int k = 1; k < V; ++k) s[i] += centre<kPlain>(v[i][k], mean[i], n[k]);
         }
+        total(rstd, scratch[1][0]);
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-            if (live && n[k] > 0) {
-                if constexpr (!kKeep) {
-                    w[0] = load_columns(a.weight, k * team + t, n[k], 1.0f);
-                    b[0] = load_columns(a.bias, k * team + t, n[k], 0.0f);
-                }
-                const Granule& wk = w[kKeep ? k : 0];
-                const Granule& bk = b[kKeep ? k : 0];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) v[k].p[j] = fma2(mul2(v[k].p[j], both(rstd)), wk.p[j], bk.p[j]);
-                put<kType, kVec>(py + k * next, n[k], a.vec, finish_output<kType>(a, v[k], n[k], hist));
+        for (int i = 0; i < R; ++i) {
+            rstd[i] = inverse_root(rstd[i] + a.eps);
+            if (t == 0 && row + i < rows) {
+                if (a.mean != nullptr) a.mean[row + i] = mean[i];
+                if (a.rstd != nullptr) a.rstd[row + i] = rstd[i];
             }
         }
-        ph += step * a.ld_h;
-        py += step * a.ld_y;
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            if constexpr (!kKeep) {
+                w[0] = load_columns(a.weight, k * team + t, n[k], 1.0f);
+                b[0] = load_columns(a.bias, k * team + t, n[k], 0.0f);
+            }
+            const Granule& wk = w[kKeep ? k : 0];
+            const Granule& bk = b[kKeep ? k : 0];
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[i][k].p[j] = fma2(mul2(v[i][k].p[j], both(rstd[i])), wk.p[j], bk.p[j]);
+                const int there = row + i < rows ? n[k] : 0;
+                put<kType, kPlain>(py + i * a.ld_y + k * next, there, a.vec, finish_output<kType, kPlain>(a, v[i][k], there, hist));
+            }
+        }
+        ph += step.h;
+        py += step.y;
     }
     if (hist != nullptr) flush_hist(hist, a.quant, a.stats, (uint64_t)a.rows * (uint64_t)a.cols);
 }
 
-// xhat of a granule; 0 where there is no column.
+// xhat of a granule; 0 where there is no column.  kPlain: all eight exist or (v = 0) none.
+template <bool kPlain>
 __device__ __forceinline__ Granule normalise(Granule v, float mean, float rstd, int n) {
+    const float2 shift = both(kPlain && n == 0 ? 0.0f : -mean);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        v.p[j] = mul2(add2(v.p[j], both(-mean)), both(rstd));
-        if (2 * j >= n) v.p[j].x = 0.0f;
-        if (2 * j + 1 >= n) v.p[j].y = 0.0f;
+        v.p[j] = mul2(add2(v.p[j], shift), both(rstd));
+        if (!kPlain && 2 * j >= n) v.p[j].x = 0.0f;
+        if (!kPlain && 2 * j + 1 >= n) v.p[j].y = 0.0f;
     }
     return v;
 }
@@ -392,15 +441,10 @@ struct GradientRow {
     typename Word<kType>::type* dresidual;
     __device__ __forceinline__ GradientRow(const BackwardArgs<kType>& a, int64_t row, int64_t col)
         : dh(a.dh + row * a.ld_dh + col), dx(a.dx + row * a.ld_dx + col), dresidual(a.dresidual + row * a.ld_dresidual + col) {}
-    __device__ __forceinline__ void advance(const BackwardArgs<kType>& a, int64_t rows) {
-        dh += rows * a.ld_dh;
-        dx += rows * a.ld_dx;
-        dresidual += rows * a.ld_dresidual;
-    }
 };
 
 // What a granule's gradients become: dh (with what arrives by another path) to dresidual, D of it to dx.
-template <int kType, bool kFused, bool kVec>
+template <int kType, bool kFused, bool kPlain>
 __device__ __forceinline__ void store_gradients(const BackwardArgs<kType>& a, const GradientRow<kType>& to, int64_t at, const Granule& dy,
                                                 const Granule& xhat, const Granule& w, float rstd, float c1, float c2, uint32_t row,
                                                 uint32_t g, int n, uint64_t offset, uint32_t* hist) {
@@ -410,14 +454,14 @@ __device__ __forceinline__ void store_gradients(const BackwardArgs<kType>& a, co
         d.p[j] = mul2(fma2(xhat.p[j], both(-c2), fma2(dy.p[j], w.p[j], both(-c1))), both(rstd));
     if constexpr (kFused) {
         if (a.dh != nullptr) {
-            const Granule more = widen_raw<kType>(fetch<kType, kVec>(to.dh + at, n, a.vec));
+            const Granule more = widen_raw<kType>(fetch<kType, kPlain>(to.dh + at, n, a.vec));
 #pragma unroll
             for (int j = 0; j < 4; ++j) d.p[j] = add2(d.p[j], more.p[j]);
         }
-        if (a.dresidual != nullptr) put<kType, kVec>(to.dresidual + at, n, a.vec, finish<kType>(d));
+        if (a.dresidual != nullptr) put<kType, kPlain>(to.dresidual + at, n, a.vec, finish<kType>(d));
         if (a.drop.active && a.dx != nullptr) drop_granule(a.drop, offset, row, g, d);
     }
-    if (a.dx != nullptr) put<kType, kVec>(to.dx + at, n, a.vec, finish_output<kType>(a, d, n, hist));
+    if (a.dx != nullptr) put<kType, kPlain>(to.dx + at, n, a.vec, finish_output<kType, kPlain>(a, d, n, hist));
 }
 
 // Long rows: a block takes a row at a time and reads it twice.
@@ -434,7 +478,7 @@ __global__ void __launch_bounds__(kLoopThreads) norm_backward_loop_kernel(const 
         const float mean = a.mean[row], rstd = a.rstd[row];
         const auto load = [&](uint32_t g, int n, Granule& dy, Granule& xhat, Granule& w) {
             dy = widen_raw<kType>(fetch<kType, false>(a.dy + row * a.ld_dy + (int64_t)g * kGranule, n, a.vec));
-            xhat = normalise(widen_raw<kType>(fetch<kType, false>(a.h + row * a.ld_h + (int64_t)g * kGranule, n, a.vec)), mean, rstd, n);
+            xhat = normalise<false>(widen_raw<kType>(fetch<kType, false>(a.h + row * a.ld_h + (int64_t)g * kGranule, n, a.vec)), mean, rstd, n);
             w = load_columns(a.weight, g, n, 1.0f);
         };
         float2 s = make_float2(0.0f, 0.0f);
@@ -467,7 +511,7 @@ __global__ void __launch_bounds__(32 * kColumnWarps) norm_column_sums_kernel(con
     if (n > 0) {
         for (int64_t row = (int64_t)blockIdx.y * kColumnWarps + warp; row < a.rows; row += (int64_t)gridDim.y * kColumnWarps) {
             const Granule dy = widen_raw<kType>(fetch<kType, false>(a.dy + row * a.ld_dy + (int64_t)g * kGranule, n, a.vec));
-            const Granule xhat = normalise(widen_raw<kType>(fetch<kType, false>(a.h + row * a.ld_h + (int64_t)g * kGranule, n, a.vec)), a.mean[row], a.rstd[row], n);
+            const Granule xhat = normalise<false>(widen_raw<kType>(fetch<kType, false>(a.h + row * a.ld_h + (int64_t)g * kGranule, n, a.vec)), a.mean[row], a.rstd[row], n);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 dw.p[j] = fma2(dy.p[j], xhat.p[j], dw.p[j]);
@@ -491,26 +535,31 @@ __global__ void __launch_bounds__(32 * kColumnWarps) norm_column_sums_kernel(con
     }
 }
 
+// Elements from a row of a team to its next one.
+struct BackwardSteps {
+    int64_t dy, h, dh, dx, dresidual;
+};
+
 // The backward pass of rows that a team holds in registers: dy and h are read once, the sums over rows stay in
 // the registers of the thread that owns their columns from row to row, and a block leaves one part.
-template <int kType, int V, bool kFused, bool kVec>
-__global__ void __launch_bounds__(kMaxTeam) norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int hist_words) {
-    constexpr bool kAhead = kVec && kType != QFMT_F32;
+// kPlain as in the forward pass.
+template <int kType, int V, bool kFused, bool kPlain>
+__global__ void __launch_bounds__(kMaxTeam)
+norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, const BackwardSteps step, int hist_words) {
+    constexpr bool kAhead = kPlain && kType != QFMT_F32;
     extern __shared__ uint32_t dynamic[];  // [hist_words] histogram, then the sums of a block's teams
-    __shared__ __align__(16) float2 scratch[kMaxTeam / 32][2][16];
+    __shared__ __align__(16) float scratch[kMaxTeam / 64][2][32];  // a slot for each team of more than a warp
     grid_launch_dependents();
     grid_dependency_wait();
-    uint32_t* hist = a.stats != nullptr ? dynamic : nullptr;
+    uint32_t* hist = !kPlain && a.stats != nullptr ? dynamic : nullptr;
     if (team > 32) {
-        for (int i = threadIdx.x; i < kMaxTeam; i += blockDim.x) (&scratch[0][0][0])[i] = make_float2(0.0f, 0.0f);
+        for (int i = threadIdx.x; i < kMaxTeam; i += blockDim.x) (&scratch[0][0][0])[i] = 0.0f;
         __syncthreads();
     }
     if (hist != nullptr) clear_hist(hist, a.quant);
     const int mine = threadIdx.x / team, t = threadIdx.x - mine * team, teams = blockDim.x / team;
     const int slot = team > 32 ? mine : 0;
-    const float inverse = 1.0f / (float)a.cols;
     const uint64_t offset = kFused ? drop_offset(a.drop) : 0ull;
-    const int64_t step = (int64_t)gridDim.x * teams;
     const int next = team * kGranule;  // elements between a thread's granules
     int n[V];
     Granule w[V], dw[V], db[V];
@@ -519,29 +568,30 @@ __global__ void __launch_bounds__(kMaxTeam) norm_backward_rows_kernel(const Back
         n[k] = granule_columns(a.cols, k * team + t);
         dw[k] = db[k] = splat(0.0f);
     }
-    int64_t row = (int64_t)blockIdx.x * teams + mine;
+    const uint32_t rows = (uint32_t)a.rows, stride = gridDim.x * teams;
+    uint32_t row = blockIdx.x * teams + mine;
     const auto* pdy = a.dy + row * a.ld_dy + t * kGranule;
     const auto* ph = a.h + row * a.ld_h + t * kGranule;
     GradientRow<kType> to(a, row, t * kGranule);
     Raw<kType> raw_dy[V], raw_h[V];
     float mean = 0.0f, rstd = 0.0f;
-    const auto fetch_row = [&](int64_t at) {
-        const bool there = at < a.rows;
+    const auto fetch_row = [&](uint32_t at) {
+        const bool there = at < rows;
         if (there) mean = a.mean[at], rstd = a.rstd[at];
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            raw_dy[k] = there && n[k] > 0 ? fetch<kType, kVec>(pdy + k * next, n[k], a.vec) : no_words<kType>();
-            raw_h[k] = there && n[k] > 0 ? fetch<kType, kVec>(ph + k * next, n[k], a.vec) : no_words<kType>();
+            raw_dy[k] = fetch<kType, kPlain>(pdy + k * next, there ? n[k] : 0, a.vec);
+            raw_h[k] = fetch<kType, kPlain>(ph + k * next, there ? n[k] : 0, a.vec);
         }
-        pdy += step * a.ld_dy;
-        ph += step * a.ld_h;
+        pdy += step.dy;
+        ph += step.h;
     };
     if (kAhead) fetch_row(row);
 #pragma unroll
     for (int k = 0; k < V; ++k) w[k] = load_columns(a.weight, k * team + t, n[k], 1.0f);
     int parity = 0;
-    for (; row - mine < a.rows; row += step, parity ^= 1) {
-        const bool live = row < a.rows;
+    for (; row - mine < rows; row += stride, parity ^= 1) {
+        const bool live = row < rows;
         if (!kAhead) fetch_row(row);
         Granule dy[V], xhat[V];
         float2 s = make_float2(0.0f, 0.0f);
@@ -549,8 +599,7 @@ __global__ void __launch_bounds__(kMaxTeam) norm_backward_rows_kernel(const Back
 #pragma unroll
         for (int k = 0; k < V; ++k) {
             dy[k] = widen_raw<kType>(raw_dy[k]);
-            xhat[k] = splat(0.0f);
-            if (live && n[k] > 0) xhat[k] = normalise(widen_raw<kType>(raw_h[k]), mean, rstd, kVec ? kGranule : n[k]);
+            xhat[k] = normalise<kPlain>(widen_raw<kType>(raw_h[k]), mean, rstd, live ? n[k] : 0);
             s = add2(s, row_sums(dy[k], xhat[k], w[k]));
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -558,15 +607,16 @@ __global__ void __launch_bounds__(kMaxTeam) norm_backward_rows_kernel(const Back
                 db[k].p[j] = add2(db[k].p[j], dy[k].p[j]);
             }
         }
-        if (kAhead) fetch_row(row + step);
-        s = team_sum<AddTwo, (V > 1)>(s, team, t, 1 + slot, scratch[slot][parity]);
-        const float c1 = s.x * inverse, c2 = s.y * inverse;
+        if (kAhead) fetch_row(row + stride);
+        s = team_sum<(V > 1), false>(s, team, t, slot, scratch[slot][parity]);
+        const float c1 = s.x * a.inverse, c2 = s.y * a.inverse;
 #pragma unroll
         for (int k = 0; k < V; ++k)
-            if (live && n[k] > 0)
-                store_gradients<kType, kFused, kVec>(a, to, k * next, dy[k], xhat[k], w[k], this_rstd, c1, c2, (uint32_t)row, k * team + t,
-                                                     n[k], offset, hist);
-        to.advance(a, step);
+            store_gradients<kType, kFused, kPlain>(a, to, k * next, dy[k], xhat[k], w[k], this_rstd, c1, c2, row, k * team + t,
+                                                   live ? n[k] : 0, offset, hist);
+        to.dh += step.dh;
+        to.dx += step.dx;
+        to.dresidual += step.dresidual;
     }
     if (hist != nullptr) flush_hist(hist, a.quant, a.stats, (uint64_t)a.rows * (uint64_t)a.cols);
     if (a.partial == nullptr) return;
@@ -576,8 +626,8 @@ __global__ void __launch_bounds__(kMaxTeam) norm_backward_rows_kernel(const Back
         for (int k = 0; k < V; ++k)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                dw[k].p[j] = AddTwo::across(dw[k].p[j], off);
-                db[k].p[j] = AddTwo::across(db[k].p[j], off);
+                dw[k].p[j] = make_float2(across(dw[k].p[j].x, off), across(dw[k].p[j].y, off));
+                db[k].p[j] = make_float2(across(db[k].p[j].x, off), across(db[k].p[j].y, off));
             }
     }
     const int unit = team < 32 ? 32 : team, units = blockDim.x / unit;  // threads that still hold a sum of their own
@@ -716,16 +766,23 @@ int prepare_call(const qfmt_norm_t* norm, const qfmt_dropout_t* drop, const qfmt
 
 bool float_aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
-template <int kType, int V, bool kFused, bool kVec>
+template <int kType, int V, int R, bool kFused, bool kPlain>
 int launch_forward_rows(const Call& c, const ForwardArgs<kType>& a, int team, cudaStream_t stream) {
     static std::atomic<int> known[kMaxTeam / 32 + 1];
-    const auto kern = norm_forward_rows_kernel<kType, V, kFused, kVec>;
-    const unsigned teams = team < 128 ? 128 / team : 1, block = teams * team;
+    const auto kern = norm_forward_rows_kernel<kType, V, R, kFused, kPlain>;
+    const unsigned teams = team > 32 ? 1 : 128 / team, block = teams * team;
     int resident = 0;
     const int rc = resident_blocks(kern, block, c.hist_bytes, known, &resident);
     if (rc != QFMT_OK) return rc;
-    const int64_t want = (a.rows + teams - 1) / teams, cap = (int64_t)c.dev.sm_count * resident;
-    QFMT_CUDA_TRY(launch_overlapping(kern, (unsigned)(want < cap ? want : cap), block, c.hist_bytes, stream, a, team));
+    const int64_t want = (a.rows + teams * R - 1) / (teams * R), cap = (int64_t)c.dev.sm_count * resident;
+    // two rows at a time only where every team has them
+    if constexpr (R == 2) {
+        if (want < cap) return launch_forward_rows<kType, V, 1, kFused, kPlain>(c, a, team, stream);
+    }
+    const unsigned blocks = (unsigned)(want < cap ? want : cap);
+    const int64_t stride = (int64_t)blocks * teams * R;
+    const ForwardSteps step = {stride * a.ld_x, stride * a.ld_residual, stride * a.ld_h, stride * a.ld_y};
+    QFMT_CUDA_TRY(launch_overlapping(kern, blocks, block, c.hist_bytes, stream, a, team, step));
     return QFMT_OK;
 }
 
@@ -733,12 +790,12 @@ template <int kType, bool kFused>
 int launch_forward(const Call& c, const ForwardArgs<kType>& a, cudaStream_t stream) {
     const Plan plan = make_plan(a.cols, kForwardGranules);
     if (plan.team != 0) {
-        const auto run = a.vec ? (plan.granules == 1   ? launch_forward_rows<kType, 1, kFused, true>
-                                  : plan.granules == 2 ? launch_forward_rows<kType, 2, kFused, true>
-                                                       : launch_forward_rows<kType, 4, kFused, true>)
-                               : (plan.granules == 1   ? launch_forward_rows<kType, 1, kFused, false>
-                                  : plan.granules == 2 ? launch_forward_rows<kType, 2, kFused, false>
-                                                       : launch_forward_rows<kType, 4, kFused, false>);
+        const auto run = a.vec && !a.fmt ? (plan.granules == 1   ? launch_forward_rows<kType, 1, 2, kFused, true>
+                                            : plan.granules == 2 ? launch_forward_rows<kType, 2, kFused && kType == QFMT_F32 ? 1 : 2, kFused, true>
+                                                                 : launch_forward_rows<kType, 4, 1, kFused, true>)
+                                         : (plan.granules == 1   ? launch_forward_rows<kType, 1, 1, kFused, false>
+                                            : plan.granules == 2 ? launch_forward_rows<kType, 2, 1, kFused, false>
+                                                                 : launch_forward_rows<kType, 4, 1, kFused, false>);
         return run(c, a, plan.team, stream);
     }
     const int64_t cap = (int64_t)c.dev.sm_count * 4;
@@ -770,6 +827,7 @@ int forward(const Call& c, const void* d_x, const void* d_residual, const float*
     a.vec = a.cols % kGranule == 0 && granule_aligned(d_x, a.ld_x, kType) && granule_aligned(d_residual, a.ld_residual, kType) &&
             granule_aligned(d_h, a.ld_h, kType) && granule_aligned(d_y, a.ld_y, kType);
     a.fmt = c.fmt;
+    a.inverse = 1.0f / (float)a.cols;
     a.drop = c.drop;
     a.quant = c.quant;
     a.stats = d_stats;
@@ -805,9 +863,9 @@ int join_parts(const float* partial, int parts, int64_t cols, float* d_dweight, 
     return QFMT_OK;
 }
 
-template <int kType, int V, bool kFused, bool kVec>
+template <int kType, int V, bool kFused, bool kPlain>
 int launch_backward_rows(const Call& c, const BackwardArgs<kType>& a, int team, float* d_dweight, float* d_dbias, cudaStream_t stream) {
-    const auto kern = norm_backward_rows_kernel<kType, V, kFused, kVec>;
+    const auto kern = norm_backward_rows_kernel<kType, V, kFused, kPlain>;
     const unsigned teams = kMaxTeam / team, block = teams * team;
     const unsigned units = team < 32 ? block / 32 : teams;
     const size_t smem = c.hist_bytes + (units > 1 && a.partial != nullptr ? 2 * (size_t)a.cols * sizeof(float) : 0);
@@ -815,7 +873,9 @@ int launch_backward_rows(const Call& c, const BackwardArgs<kType>& a, int team, 
     const int64_t want = (a.rows + teams - 1) / teams;
     const int cap = c.dev.sm_count < kMaxParts ? c.dev.sm_count : kMaxParts;
     const unsigned blocks = (unsigned)(want < cap ? want : cap);
-    QFMT_CUDA_TRY(launch_overlapping(kern, blocks, block, smem, stream, a, team, (int)(c.hist_bytes / sizeof(uint32_t))));
+    const int64_t stride = (int64_t)blocks * teams;
+    const BackwardSteps step = {stride * a.ld_dy, stride * a.ld_h, stride * a.ld_dh, stride * a.ld_dx, stride * a.ld_dresidual};
+    QFMT_CUDA_TRY(launch_overlapping(kern, blocks, block, smem, stream, a, team, step, (int)(c.hist_bytes / sizeof(uint32_t))));
     return a.partial != nullptr ? join_parts(a.partial, (int)blocks, a.cols, d_dweight, d_dbias, stream) : QFMT_OK;
 }
 
@@ -824,7 +884,7 @@ int launch_backward(const Call& c, const BackwardArgs<kType>& a, float* d_dweigh
     if (a.rows == 0) return join_parts(a.partial, 0, a.cols, d_dweight, d_dbias, stream);  // zeros
     const Plan plan = make_plan(a.cols, kBackwardGranules);
     if (plan.team != 0) {
-        const auto run = a.vec ? (plan.granules == 1 ? launch_backward_rows<kType, 1, kFused, true> : launch_backward_rows<kType, 2, kFused, true>)
+        const auto run = a.vec && !a.fmt ? (plan.granules == 1 ? launch_backward_rows<kType, 1, kFused, true> : launch_backward_rows<kType, 2, kFused, true>)
                                : (plan.granules == 1 ? launch_backward_rows<kType, 1, kFused, false> : launch_backward_rows<kType, 2, kFused, false>);
         return run(c, a, plan.team, d_dweight, d_dbias, stream);
     }
@@ -869,6 +929,7 @@ int backward(const Call& c, const void* d_dy, const void* d_dh, const void* d_h,
     a.vec = a.cols % kGranule == 0 && granule_aligned(d_dy, a.ld_dy, kType) && granule_aligned(d_dh, a.ld_dh, kType) && granule_aligned(d_h, a.ld_h, kType) &&
             granule_aligned(d_dx, a.ld_dx, kType) && granule_aligned(d_dresidual, a.ld_dresidual, kType);
     a.fmt = c.fmt;
+    a.inverse = 1.0f / (float)a.cols;
     a.drop = c.drop;
     a.quant = c.quant;
     a.stats = d_stats;
