@@ -219,18 +219,14 @@ __global__ void __launch_bounds__(kLoopThreads) norm_forward_loop_kernel(const F
     if (hist != nullptr) flush_hist(hist, a.quant, a.stats, (uint64_t)a.rows * (uint64_t)a.cols);
 }
 
-// Teams: the threads that share a row.  A team of up to 32 threads is an aligned part of a warp; a larger
-// one is whole warps.  Granule k * team + t of the row is thread t's k-th, k < V.
+// Teams: the threads that share a row.  With V = 1 granule a thread a team is an aligned part of a warp (or all of
+// it), otherwise it is the whole block, which keeps row numbers and addresses uniform.  Granule k * team + t of the
+// row is thread t's k-th, k < V.
 constexpr int kMaxTeam = 512;
 
-// Sums over a team, in every thread and in a fixed order: of one value, or of two at once.  kWarps: the team is
-// whole warps.  kBlock: it is the block.  scratch: 16 entries, or two times 16, of which those past the team's
-// warps are zero; one barrier, so the team's next sum needs another scratch.
-template <bool kBlock>
-__device__ __forceinline__ void team_barrier(int team, int slot) {
-    if constexpr (kBlock) __syncthreads();
-    else asm volatile("bar.sync %0, %1;" ::"r"(1 + slot), "r"(team) : "memory");
-}
+// Sums over a team, in every thread and in a fixed order: of one value, or of two at once.  kBlock: the team is the
+// block.  scratch: 16 entries, or two times 16, of which those past the team's warps are zero; one barrier, so the
+// next sum needs another scratch.
 __device__ __forceinline__ float sum_entries(const float* scratch, int team) {
     float s = 0.0f;
     for (int i = 0; i * 32 < team; i += 4) {
@@ -242,9 +238,9 @@ __device__ __forceinline__ float sum_entries(const float* scratch, int team) {
 }
 __device__ __forceinline__ float across(float s, int off) { return s + __shfl_xor_sync(0xFFFFFFFFu, s, off); }
 
-template <bool kWarps, bool kBlock>
-__device__ __forceinline__ float team_sum(float s, int team, int t, int slot, float* scratch) {
-    if constexpr (!kWarps) {
+template <bool kBlock>
+__device__ __forceinline__ float team_sum(float s, int team, int t, float* scratch) {
+    if constexpr (!kBlock) {
         for (int off = team >> 1; off > 0; off >>= 1) s = across(s, off);
         return s;
     } else {
@@ -252,16 +248,16 @@ __device__ __forceinline__ float team_sum(float s, int team, int t, int slot, fl
         for (int off = 16; off > 0; off >>= 1) s = across(s, off);
         if (team == 32) return s;
         if ((t & 31) == 0) scratch[t >> 5] = s;
-        team_barrier<kBlock>(team, slot);
+        __syncthreads();
         return sum_entries(scratch, team);
     }
 }
 
 // Two values: after one exchange the lower half of a warp holds the first value's partial sums and the upper half
 // the second's, so five shuffles do for both.
-template <bool kWarps, bool kBlock>
-__device__ __forceinline__ float2 team_sum(float2 s, int team, int t, int slot, float* scratch) {
-    if constexpr (!kWarps) {
+template <bool kBlock>
+__device__ __forceinline__ float2 team_sum(float2 s, int team, int t, float* scratch) {
+    if constexpr (!kBlock) {
         for (int off = team >> 1; off > 0; off >>= 1) s = make_float2(across(s.x, off), across(s.y, off));
         return s;
     } else {
@@ -274,7 +270,7 @@ __device__ __forceinline__ float2 team_sum(float2 s, int team, int t, int slot, 
             return upper ? make_float2(v, u) : make_float2(u, v);
         }
         if ((t & 15) == 0) scratch[(t & 16) + (t >> 5)] = u;
-        team_barrier<kBlock>(team, slot);
+        __syncthreads();
         return make_float2(sum_entries(scratch, team), sum_entries(scratch + 16, team));
     }
 }
@@ -296,12 +292,12 @@ __global__ void __launch_bounds__(kMaxTeam) norm_forward_rows_kernel(const Forwa
     grid_launch_dependents();
     grid_dependency_wait();
     uint32_t* hist = !kPlain && a.stats != nullptr ? lane_hist : nullptr;
-    if (team > 32) {
+    if (V > 1) {
         for (int i = threadIdx.x; i < 2 * R * 16; i += blockDim.x) (&scratch[0][0][0])[i] = 0.0f;
         __syncthreads();
     }
     if (hist != nullptr) clear_hist(hist, a.quant);
-    const int mine = threadIdx.x / team, t = threadIdx.x - mine * team, teams = blockDim.x / team;
+    const int mine = V > 1 ? 0 : threadIdx.x / team, t = threadIdx.x - mine * team, teams = V > 1 ? 1 : blockDim.x / team;
     const uint64_t offset = kFused ? drop_offset(a.drop) : 0ull;
     const bool residual = kFused && a.residual != nullptr;
     const int next = team * kGranule;  // elements between a thread's granules
@@ -357,11 +353,11 @@ __global__ void __launch_bounds__(kMaxTeam) norm_forward_rows_kernel(const Forwa
         }
         const auto total = [&](float (&out)[R], float* space) {
             if constexpr (R == 2) {
-                const float2 q = team_sum<(V > 1), true>(make_float2(s[0], s[1]), team, t, 0, space);
+                const float2 q = team_sum<(V > 1)>(make_float2(s[0], s[1]), team, t, space);
                 out[0] = q.x * a.inverse;
                 out[1] = q.y * a.inverse;
             } else {
-                out[0] = team_sum<(V > 1), true>(s[0], team, t, 0, space) * a.inverse;
+                out[0] = team_sum<(V > 1)>(s[0], team, t, space) * a.inverse;
             }
         };
 #pragma unroll
@@ -540,6 +536,27 @@ struct BackwardSteps {
     int64_t dy, h, dh, dx, dresidual;
 };
 
+// Blocks of a cluster: how many, which one this is, a barrier over all of them, a word of another one's shared memory.
+__device__ __forceinline__ uint32_t cluster_blocks() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctaid.x;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_barrier() {
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+__device__ __forceinline__ float load_cluster(const float* p, int rank) {
+    float v;
+    asm volatile("{ .reg .u32 a; mapa.shared::cluster.u32 a, %1, %2; ld.shared::cluster.f32 %0, [a]; }"
+                 : "=f"(v) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank) : "memory");
+    return v;
+}
+
 // The backward pass of rows that a team holds in registers: dy and h are read once, the sums over rows stay in
 // the registers of the thread that owns their columns from row to row, and a block leaves one part.
 // kPlain as in the forward pass.
@@ -548,17 +565,16 @@ __global__ void __launch_bounds__(kMaxTeam)
 norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, const BackwardSteps step, int hist_words) {
     constexpr bool kAhead = kPlain && kType != QFMT_F32;
     extern __shared__ uint32_t dynamic[];  // [hist_words] histogram, then the sums of a block's teams
-    __shared__ __align__(16) float scratch[kMaxTeam / 64][2][32];  // a slot for each team of more than a warp
+    __shared__ __align__(16) float scratch[2][32];
     grid_launch_dependents();
     grid_dependency_wait();
     uint32_t* hist = !kPlain && a.stats != nullptr ? dynamic : nullptr;
-    if (team > 32) {
-        for (int i = threadIdx.x; i < kMaxTeam; i += blockDim.x) (&scratch[0][0][0])[i] = 0.0f;
+    if (V > 1) {
+        for (int i = threadIdx.x; i < 64; i += blockDim.x) (&scratch[0][0])[i] = 0.0f;
         __syncthreads();
     }
     if (hist != nullptr) clear_hist(hist, a.quant);
-    const int mine = threadIdx.x / team, t = threadIdx.x - mine * team, teams = blockDim.x / team;
-    const int slot = team > 32 ? mine : 0;
+    const int mine = V > 1 ? 0 : threadIdx.x / team, t = threadIdx.x - mine * team, teams = V > 1 ? 1 : blockDim.x / team;
     const uint64_t offset = kFused ? drop_offset(a.drop) : 0ull;
     const int next = team * kGranule;  // elements between a thread's granules
     int n[V];
@@ -608,7 +624,7 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, const BackwardS
             }
         }
         if (kAhead) fetch_row(row + stride);
-        s = team_sum<(V > 1), false>(s, team, t, slot, scratch[slot][parity]);
+        s = team_sum<(V > 1)>(s, team, t, scratch[parity]);
         const float c1 = s.x * a.inverse, c2 = s.y * a.inverse;
 #pragma unroll
         for (int k = 0; k < V; ++k)
@@ -620,39 +636,55 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, const BackwardS
     }
     if (hist != nullptr) flush_hist(hist, a.quant, a.stats, (uint64_t)a.rows * (uint64_t)a.cols);
     if (a.partial == nullptr) return;
-    // the teams of a warp by shuffles, those of the block one after the other through shared memory
-    for (int off = 16; off >= team; off >>= 1) {
-#pragma unroll
-        for (int k = 0; k < V; ++k)
+    float* const sums = reinterpret_cast<float*>(dynamic + hist_words);  // [2][cols]
+    const int64_t cols = a.cols;
+    if constexpr (V == 1) {
+        // the teams of a warp by shuffles, the warps one after the other through shared memory
+        for (int off = 16; off >= team; off >>= 1) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                dw[k].p[j] = make_float2(across(dw[k].p[j].x, off), across(dw[k].p[j].y, off));
-                db[k].p[j] = make_float2(across(db[k].p[j].x, off), across(db[k].p[j].y, off));
+                dw[0].p[j] = make_float2(across(dw[0].p[j].x, off), across(dw[0].p[j].y, off));
+                db[0].p[j] = make_float2(across(db[0].p[j].x, off), across(db[0].p[j].y, off));
             }
-    }
-    const int unit = team < 32 ? 32 : team, units = blockDim.x / unit;  // threads that still hold a sum of their own
-    float* const sums = reinterpret_cast<float*>(dynamic + hist_words);
-    const int u = threadIdx.x / unit;
-    const bool holds = threadIdx.x - u * unit < team;
-    for (int turn = 0; turn < units; ++turn) {
-        if (turn > 0) __syncthreads();
-        if (u != turn || !holds) continue;
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-            const int64_t col = (int64_t)(k * team + t) * kGranule;
+        }
+        const int warps = blockDim.x / 32, lane = threadIdx.x & 31;
+        for (int turn = 0; turn < warps; ++turn) {
+            if (turn > 0) __syncthreads();
+            if (threadIdx.x / 32 != turn || lane >= team) continue;
 #pragma unroll
             for (int j = 0; j < kGranule; ++j) {
-                if (j < n[k]) {
-                    float p = dw[k].at(j), q = db[k].at(j);
-                    if (turn > 0) p += sums[col + j], q += sums[a.cols + col + j];
-                    if (turn == units - 1) {
-                        a.partial[(int64_t)blockIdx.x * 2 * a.cols + col + j] = p;
-                        a.partial[((int64_t)blockIdx.x * 2 + 1) * a.cols + col + j] = q;
-                    } else {
-                        sums[col + j] = p, sums[a.cols + col + j] = q;
-                    }
-                }
+                if (j >= n[0]) continue;
+                const int c = t * kGranule + j;
+                float p = dw[0].at(j), q = db[0].at(j);
+                if (turn > 0) p += sums[c], q += sums[cols + c];
+                sums[c] = p, sums[cols + c] = q;
             }
+        }
+        __syncthreads();
+        float* const part = a.partial + (int64_t)blockIdx.x * 2 * cols;
+        for (int c = threadIdx.x; c < 2 * (int)cols; c += blockDim.x) part[c] = sums[c];
+    } else {
+        // the blocks of a cluster leave one part: each adds up its share of the columns from all of them
+        const int ranks = (int)cluster_blocks();
+        float* const part = a.partial + (int64_t)(blockIdx.x / ranks) * 2 * cols;
+        float* const own = ranks > 1 ? sums : part;
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+#pragma unroll
+            for (int j = 0; j < kGranule; ++j) {
+                if (j >= n[k]) continue;
+                const int c = (k * team + t) * kGranule + j;
+                own[c] = dw[k].at(j), own[cols + c] = db[k].at(j);
+            }
+        }
+        if (ranks > 1) {
+            cluster_barrier();
+            for (int c = (int)cluster_rank() * team + t; c < 2 * (int)cols; c += ranks * team) {
+                float s = load_cluster(sums + c, 0);
+                for (int i = 1; i < ranks; ++i) s += load_cluster(sums + c, i);
+                part[c] = s;
+            }
+            cluster_barrier();  // the others may still be reading this block's sums
         }
     }
 }
@@ -714,9 +746,9 @@ int resident_blocks(K kernel, unsigned block, size_t smem, std::atomic<int>* kno
     return QFMT_OK;
 }
 
-// Parts that the backward pass leaves for the gradients of weight and bias: one per block of the rows kernel (at
-// most one block per SM of a B200), or a share of the rows for long rows.
-constexpr int kMaxParts = 148;
+// Parts that the backward pass leaves for the gradients of weight and bias: one per block or cluster of the rows
+// kernel (512 threads on each SM of a B200 make at most two), or a share of the rows for long rows.
+constexpr int kMaxParts = 2 * 148;
 int row_parts(const qfmt_norm_t& s) {
     if (make_plan(s.cols, kBackwardGranules).team != 0) return kMaxParts;
     const int64_t want = (s.rows + 8 * kColumnWarps - 1) / (8 * kColumnWarps);
@@ -770,7 +802,7 @@ template <int kType, int V, int R, bool kFused, bool kPlain>
 int launch_forward_rows(const Call& c, const ForwardArgs<kType>& a, int team, cudaStream_t stream) {
     static std::atomic<int> known[kMaxTeam / 32 + 1];
     const auto kern = norm_forward_rows_kernel<kType, V, R, kFused, kPlain>;
-    const unsigned teams = team > 32 ? 1 : 128 / team, block = teams * team;
+    const unsigned teams = V > 1 ? 1 : 128 / team, block = teams * team;
     int resident = 0;
     const int rc = resident_blocks(kern, block, c.hist_bytes, known, &resident);
     if (rc != QFMT_OK) return rc;
@@ -866,17 +898,20 @@ int join_parts(const float* partial, int parts, int64_t cols, float* d_dweight, 
 template <int kType, int V, bool kFused, bool kPlain>
 int launch_backward_rows(const Call& c, const BackwardArgs<kType>& a, int team, float* d_dweight, float* d_dbias, cudaStream_t stream) {
     const auto kern = norm_backward_rows_kernel<kType, V, kFused, kPlain>;
-    const unsigned teams = kMaxTeam / team, block = teams * team;
-    const unsigned units = team < 32 ? block / 32 : teams;
-    const size_t smem = c.hist_bytes + (units > 1 && a.partial != nullptr ? 2 * (size_t)a.cols * sizeof(float) : 0);
-    if (smem > 32 * 1024) QFMT_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    const int64_t want = (a.rows + teams - 1) / teams;
-    const int cap = c.dev.sm_count < kMaxParts ? c.dev.sm_count : kMaxParts;
-    const unsigned blocks = (unsigned)(want < cap ? want : cap);
+    // 512 threads an SM: one block of small teams, or as many blocks of one team, clustered so that they leave one part
+    const unsigned block = V > 1 ? team : kMaxTeam, teams = V > 1 ? 1 : block / team;
+    unsigned cluster = 1;
+    while (V > 1 && cluster < 8 && 2 * cluster * block <= kMaxTeam) cluster *= 2;
+    const size_t smem = c.hist_bytes + (V == 1 || cluster > 1 ? 2 * (size_t)a.cols * sizeof(float) : 0);
+    if (smem > 40 * 1024) QFMT_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    const int64_t want = (a.rows + (int64_t)teams * cluster - 1) / ((int64_t)teams * cluster);
+    const int64_t cap = (int64_t)c.dev.sm_count * kMaxTeam / (block * cluster);
+    const unsigned parts = (unsigned)(want < cap ? want < kMaxParts ? want : kMaxParts : cap < kMaxParts ? cap : kMaxParts);
+    const unsigned blocks = parts * cluster;
     const int64_t stride = (int64_t)blocks * teams;
     const BackwardSteps step = {stride * a.ld_dy, stride * a.ld_h, stride * a.ld_dh, stride * a.ld_dx, stride * a.ld_dresidual};
-    QFMT_CUDA_TRY(launch_overlapping(kern, blocks, block, smem, stream, a, team, step, (int)(c.hist_bytes / sizeof(uint32_t))));
-    return a.partial != nullptr ? join_parts(a.partial, (int)blocks, a.cols, d_dweight, d_dbias, stream) : QFMT_OK;
+    QFMT_CUDA_TRY(launch_overlapping_clusters(kern, blocks, block, cluster, smem, stream, a, team, step, (int)(c.hist_bytes / sizeof(uint32_t))));
+    return a.partial != nullptr ? join_parts(a.partial, (int)parts, a.cols, d_dweight, d_dbias, stream) : QFMT_OK;
 }
 
 template <int kType, bool kFused>
