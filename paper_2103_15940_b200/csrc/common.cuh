@@ -49,27 +49,19 @@ __device__ __forceinline__ void grid_launch_dependents() { asm volatile("griddep
 // first access to global memory (the GEMM kernels, the split-K reduction, the layer-output pass).  After anything else in the
 // stream (a copy, a memset, a kernel without grid_launch_dependents) it is an ordinary launch.
 template <typename... P, typename... A>
-cudaError_t launch_overlapping_clusters(void (*kernel)(P...), unsigned grid, unsigned block, unsigned cluster, size_t smem,
-                                        cudaStream_t stream, A&&... args) {
+cudaError_t launch_overlapping(void (*kernel)(P...), unsigned grid, unsigned block, size_t smem, cudaStream_t stream,
+                               A&&... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(grid, 1, 1);
     cfg.blockDim = dim3(block, 1, 1);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[2];
+    cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = cluster;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...);
-}
-template <typename... P, typename... A>
-cudaError_t launch_overlapping(void (*kernel)(P...), unsigned grid, unsigned block, size_t smem, cudaStream_t stream,
-                               A&&... args) {
-    return launch_overlapping_clusters(kernel, grid, block, 1u, smem, stream, std::forward<A>(args)...);
 }
 
 // Zeroes a few words (the hand-over words of the balanced schedule, a statistics record).  A kernel rather than a memset so that the launches

@@ -10,6 +10,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 
@@ -429,7 +430,7 @@ __device__ __forceinline__ float2 row_sums(const Granule& dy, const Granule& xha
     return make_float2(s.x + s.y, q.x + q.y);
 }
 
-// Where the gradients of one row go, at a thread's first granule.
+// Where the gradients of a row go, at a thread's first granule (and, i rows on, those of the next ones).
 template <int kType>
 struct GradientRow {
     const typename Word<kType>::type* dh;
@@ -441,7 +442,7 @@ struct GradientRow {
 
 // What a granule's gradients become: dh (with what arrives by another path) to dresidual, D of it to dx.
 template <int kType, bool kFused, bool kPlain>
-__device__ __forceinline__ void store_gradients(const BackwardArgs<kType>& a, const GradientRow<kType>& to, int64_t at, const Granule& dy,
+__device__ __forceinline__ void store_gradients(const BackwardArgs<kType>& a, const GradientRow<kType>& to, int i, int64_t at, const Granule& dy,
                                                 const Granule& xhat, const Granule& w, float rstd, float c1, float c2, uint32_t row,
                                                 uint32_t g, int n, uint64_t offset, uint32_t* hist) {
     Granule d;
@@ -450,14 +451,14 @@ __device__ __forceinline__ void store_gradients(const BackwardArgs<kType>& a, co
         d.p[j] = mul2(fma2(xhat.p[j], both(-c2), fma2(dy.p[j], w.p[j], both(-c1))), both(rstd));
     if constexpr (kFused) {
         if (a.dh != nullptr) {
-            const Granule more = widen_raw<kType>(fetch<kType, kPlain>(to.dh + at, n, a.vec));
+            const Granule more = widen_raw<kType>(fetch<kType, kPlain>(to.dh + i * a.ld_dh + at, n, a.vec));
 #pragma unroll
             for (int j = 0; j < 4; ++j) d.p[j] = add2(d.p[j], more.p[j]);
         }
-        if (a.dresidual != nullptr) put<kType, kPlain>(to.dresidual + at, n, a.vec, finish<kType>(d));
+        if (a.dresidual != nullptr) put<kType, kPlain>(to.dresidual + i * a.ld_dresidual + at, n, a.vec, finish<kType>(d));
         if (a.drop.active && a.dx != nullptr) drop_granule(a.drop, offset, row, g, d);
     }
-    if (a.dx != nullptr) put<kType, kPlain>(to.dx + at, n, a.vec, finish_output<kType, kPlain>(a, d, n, hist));
+    if (a.dx != nullptr) put<kType, kPlain>(to.dx + i * a.ld_dx + at, n, a.vec, finish_output<kType, kPlain>(a, d, n, hist));
 }
 
 // Long rows: a block takes a row at a time and reads it twice.
@@ -487,7 +488,7 @@ __global__ void __launch_bounds__(kLoopThreads) norm_backward_loop_kernel(const 
         for (uint32_t g = threadIdx.x; g < granules; g += kLoopThreads) {
             const int n = granule_columns(a.cols, g);
             load(g, n, dy, xhat, w);
-            store_gradients<kType, kFused, false>(a, GradientRow<kType>(a, row, 0), (int64_t)g * kGranule, dy, xhat, w, rstd, s.x / count,
+            store_gradients<kType, kFused, false>(a, GradientRow<kType>(a, row, 0), 0, (int64_t)g * kGranule, dy, xhat, w, rstd, s.x / count,
                                                   s.y / count, (uint32_t)row, g, n, offset, hist);
         }
     }
@@ -527,7 +528,7 @@ __global__ void __launch_bounds__(32 * kColumnWarps) norm_column_sums_kernel(con
         float s = 0.0f;
 #pragma unroll
         for (int w = 0; w < kColumnWarps; ++w) s += part[w][which][j][l];
-        if (c < a.cols) a.partial[((int64_t)blockIdx.y * 2 + which) * a.cols + c] = s;
+        if (c < a.cols) a.partial[((int64_t)blockIdx.y * 2 + which) * ((a.cols + kGranule - 1) / kGranule * kGranule) + c] = s;
     }
 }
 
@@ -536,45 +537,48 @@ struct BackwardSteps {
     int64_t dy, h, dh, dx, dresidual;
 };
 
-// Blocks of a cluster: how many, which one this is, a barrier over all of them, a word of another one's shared memory.
-__device__ __forceinline__ uint32_t cluster_blocks() {
-    uint32_t r;
-    asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm("mov.u32 %0, %%cluster_ctaid.x;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void cluster_barrier() {
-    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
-}
-__device__ __forceinline__ float load_cluster(const float* p, int rank) {
+// Two sums of each of R rows over a team of whole warps that is one of several in its block, in every thread and in
+// a fixed order.  With every exchange a lane gives up half of the values it holds, so six shuffles do for four values.
+// scratch: 16 entries for each of the 2 R values, those past the team's warps zero.
+template <int R>
+__device__ __forceinline__ void team_sums(float2 (&s)[R], int team, int t, int barrier, float* scratch) {
+    const bool upper = t & 16, odd = t & 8;
+    float u[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) u[i] = (upper ? s[i].y : s[i].x) + __shfl_xor_sync(0xFFFFFFFFu, upper ? s[i].x : s[i].y, 16);
     float v;
-    asm volatile("{ .reg .u32 a; mapa.shared::cluster.u32 a, %1, %2; ld.shared::cluster.f32 %0, [a]; }"
-                 : "=f"(v) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank) : "memory");
-    return v;
+    if constexpr (R == 2) v = (odd ? u[1] : u[0]) + __shfl_xor_sync(0xFFFFFFFFu, odd ? u[0] : u[1], 8);
+    else v = across(u[0], 8);
+#pragma unroll
+    for (int off = 4; off > 0; off >>= 1) v = across(v, off);
+    // value 0 of row 0, 0 of row 1, 1 of row 0, 1 of row 1 in lanes 0, 8, 16, 24
+    if ((t & 7) == 0 && (R == 2 || !odd)) scratch[(t & 24) * 2 + (t >> 5)] = v;
+    asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(team) : "memory");
+#pragma unroll
+    for (int i = 0; i < R; ++i) s[i] = make_float2(sum_entries(scratch + 16 * i, team), sum_entries(scratch + 32 + 16 * i, team));
 }
 
-// The backward pass of rows that a team holds in registers: dy and h are read once, the sums over rows stay in
-// the registers of the thread that owns their columns from row to row, and a block leaves one part.
-// kPlain as in the forward pass.
-template <int kType, int V, bool kFused, bool kPlain>
+// The backward pass of rows that a team holds in registers, R at a time: dy and h are read once, the sums over rows
+// stay in the registers of the thread that owns their columns from row to row, and a block leaves one part.
+// kParts: a team is a part of a warp (or all of it), otherwise whole warps; a block has 512 threads' worth of teams.
+// kPlain as in the forward pass; the next rows are then on their way while these are worked on.
+template <int kType, int V, int R, bool kParts, bool kFused, bool kPlain>
 __global__ void __launch_bounds__(kMaxTeam)
 norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, const BackwardSteps step, int hist_words) {
-    constexpr bool kAhead = kPlain && kType != QFMT_F32;
-    extern __shared__ uint32_t dynamic[];  // [hist_words] histogram, then the sums of a block's teams
-    __shared__ __align__(16) float scratch[2][32];
+    constexpr bool kAhead = kPlain && V == 1;
+    extern __shared__ __align__(16) uint32_t dynamic[];  // [hist_words] histogram, then the sums of the block's teams
+    __shared__ __align__(16) float scratch[kParts ? 1 : kMaxTeam / 64][2][64];
     grid_launch_dependents();
     grid_dependency_wait();
     uint32_t* hist = !kPlain && a.stats != nullptr ? dynamic : nullptr;
-    if (V > 1) {
-        for (int i = threadIdx.x; i < 64; i += blockDim.x) (&scratch[0][0])[i] = 0.0f;
+    if constexpr (!kParts) {
+        for (int i = threadIdx.x; i < kMaxTeam * 2; i += blockDim.x) (&scratch[0][0][0])[i] = 0.0f;
         __syncthreads();
     }
     if (hist != nullptr) clear_hist(hist, a.quant);
-    const int mine = V > 1 ? 0 : threadIdx.x / team, t = threadIdx.x - mine * team, teams = V > 1 ? 1 : blockDim.x / team;
+    // (the shuffle tells the compiler that a warp belongs to one team)
+    const int mine = kParts ? threadIdx.x / team : __shfl_sync(0xFFFFFFFFu, threadIdx.x / team, 0);
+    const int t = threadIdx.x - mine * team, teams = blockDim.x / team;
     const uint64_t offset = kFused ? drop_offset(a.drop) : 0ull;
     const int next = team * kGranule;  // elements between a thread's granules
     int n[V];
@@ -584,153 +588,156 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, const BackwardS
         n[k] = granule_columns(a.cols, k * team + t);
         dw[k] = db[k] = splat(0.0f);
     }
-    const uint32_t rows = (uint32_t)a.rows, stride = gridDim.x * teams;
-    uint32_t row = blockIdx.x * teams + mine;
+    const uint32_t rows = (uint32_t)a.rows, stride = gridDim.x * teams * R;
+    uint32_t row = (blockIdx.x * teams + mine) * R;
     const auto* pdy = a.dy + row * a.ld_dy + t * kGranule;
     const auto* ph = a.h + row * a.ld_h + t * kGranule;
     GradientRow<kType> to(a, row, t * kGranule);
-    Raw<kType> raw_dy[V], raw_h[V];
-    float mean = 0.0f, rstd = 0.0f;
-    const auto fetch_row = [&](uint32_t at) {
-        const bool there = at < rows;
-        if (there) mean = a.mean[at], rstd = a.rstd[at];
+    Raw<kType> raw_dy[R][V], raw_h[R][V];
+    float mean[R], rstd[R];
+    const auto fetch_rows = [&](uint32_t at) {
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-            raw_dy[k] = fetch<kType, kPlain>(pdy + k * next, there ? n[k] : 0, a.vec);
-            raw_h[k] = fetch<kType, kPlain>(ph + k * next, there ? n[k] : 0, a.vec);
+        for (int i = 0; i < R; ++i) {
+            const bool there = at + i < rows;
+            mean[i] = there ? __ldg(a.mean + at + i) : 0.0f;
+            rstd[i] = there ? __ldg(a.rstd + at + i) : 0.0f;
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                raw_dy[i][k] = fetch<kType, kPlain>(pdy + i * a.ld_dy + k * next, there ? n[k] : 0, a.vec);
+                raw_h[i][k] = fetch<kType, kPlain>(ph + i * a.ld_h + k * next, there ? n[k] : 0, a.vec);
+            }
         }
         pdy += step.dy;
         ph += step.h;
     };
-    if (kAhead) fetch_row(row);
+    if (kAhead) fetch_rows(row);
 #pragma unroll
     for (int k = 0; k < V; ++k) w[k] = load_columns(a.weight, k * team + t, n[k], 1.0f);
     int parity = 0;
-    for (; row - mine < rows; row += stride, parity ^= 1) {
-        const bool live = row < rows;
-        if (!kAhead) fetch_row(row);
-        Granule dy[V], xhat[V];
-        float2 s = make_float2(0.0f, 0.0f);
-        const float this_rstd = rstd;
+    for (; row - mine * R < rows; row += stride, parity ^= 1) {
+        if (!kAhead) fetch_rows(row);
+        Granule dy[R][V], xhat[R][V];
+        float2 s[R];
+        float this_rstd[R];
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-            dy[k] = widen_raw<kType>(raw_dy[k]);
-            xhat[k] = normalise<kPlain>(widen_raw<kType>(raw_h[k]), mean, rstd, live ? n[k] : 0);
-            s = add2(s, row_sums(dy[k], xhat[k], w[k]));
+        for (int i = 0; i < R; ++i) {
+            this_rstd[i] = rstd[i];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                dw[k].p[j] = fma2(dy[k].p[j], xhat[k].p[j], dw[k].p[j]);
-                db[k].p[j] = add2(db[k].p[j], dy[k].p[j]);
+            for (int k = 0; k < V; ++k) {
+                dy[i][k] = widen_raw<kType>(raw_dy[i][k]);
+                xhat[i][k] = normalise<kPlain>(widen_raw<kType>(raw_h[i][k]), mean[i], rstd[i], row + i < rows ? n[k] : 0);
+                const float2 q = row_sums(dy[i][k], xhat[i][k], w[k]);
+                s[i] = k == 0 ? q : add2(s[i], q);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    dw[k].p[j] = fma2(dy[i][k].p[j], xhat[i][k].p[j], dw[k].p[j]);
+                    db[k].p[j] = add2(db[k].p[j], dy[i][k].p[j]);
+                }
             }
         }
-        if (kAhead) fetch_row(row + stride);
-        s = team_sum<(V > 1)>(s, team, t, scratch[parity]);
-        const float c1 = s.x * a.inverse, c2 = s.y * a.inverse;
+        if (kAhead) fetch_rows(row + stride);
+        if constexpr (kParts) {
+            for (int off = team >> 1; off > 0; off >>= 1) {
 #pragma unroll
-        for (int k = 0; k < V; ++k)
-            store_gradients<kType, kFused, kPlain>(a, to, k * next, dy[k], xhat[k], w[k], this_rstd, c1, c2, row, k * team + t,
-                                                   live ? n[k] : 0, offset, hist);
+                for (int i = 0; i < R; ++i) s[i] = make_float2(across(s[i].x, off), across(s[i].y, off));
+            }
+        } else {
+            team_sums<R>(s, team, t, 1 + mine, scratch[mine][parity]);
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const float c1 = s[i].x * a.inverse, c2 = s[i].y * a.inverse;
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                store_gradients<kType, kFused, kPlain>(a, to, i, k * next, dy[i][k], xhat[i][k], w[k], this_rstd[i], c1, c2, row + i,
+                                                       k * team + t, row + i < rows ? n[k] : 0, offset, hist);
+        }
         to.dh += step.dh;
         to.dx += step.dx;
         to.dresidual += step.dresidual;
     }
     if (hist != nullptr) flush_hist(hist, a.quant, a.stats, (uint64_t)a.rows * (uint64_t)a.cols);
     if (a.partial == nullptr) return;
-    float* const sums = reinterpret_cast<float*>(dynamic + hist_words);  // [2][cols]
-    const int64_t cols = a.cols;
-    if constexpr (V == 1) {
-        // the teams of a warp by shuffles, the warps one after the other through shared memory
-        for (int off = 16; off >= team; off >>= 1) {
+    // [dweight, dbias][padded columns] of every warp of small teams, or of every team; then their sum
+    const int padded = ((int)a.cols + kGranule - 1) / kGranule * kGranule, quads = padded / 2;
+    const int units = kParts ? blockDim.x / 32 : teams;
+    float4* const part = reinterpret_cast<float4*>(a.partial) + (int64_t)blockIdx.x * quads;
+    float4* const sums = units > 1 ? reinterpret_cast<float4*>(dynamic + hist_words) : part;
+    float4* const own = sums + (kParts ? threadIdx.x / 32 : mine) * quads;
+    if constexpr (kParts) {
+        for (int off = 16; off >= team; off >>= 1) {  // the teams of a warp
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 dw[0].p[j] = make_float2(across(dw[0].p[j].x, off), across(dw[0].p[j].y, off));
                 db[0].p[j] = make_float2(across(db[0].p[j].x, off), across(db[0].p[j].y, off));
             }
         }
-        const int warps = blockDim.x / 32, lane = threadIdx.x & 31;
-        for (int turn = 0; turn < warps; ++turn) {
-            if (turn > 0) __syncthreads();
-            if (threadIdx.x / 32 != turn || lane >= team) continue;
+    }
 #pragma unroll
-            for (int j = 0; j < kGranule; ++j) {
-                if (j >= n[0]) continue;
-                const int c = t * kGranule + j;
-                float p = dw[0].at(j), q = db[0].at(j);
-                if (turn > 0) p += sums[c], q += sums[cols + c];
-                sums[c] = p, sums[cols + c] = q;
-            }
+    for (int k = 0; k < V; ++k) {
+        if ((kParts && (threadIdx.x & 31) >= team) || n[k] == 0) continue;
+        float4* const q = own + (k * team + t) * 2;
+        q[0] = make_float4(dw[k].p[0].x, dw[k].p[0].y, dw[k].p[1].x, dw[k].p[1].y);
+        q[1] = make_float4(dw[k].p[2].x, dw[k].p[2].y, dw[k].p[3].x, dw[k].p[3].y);
+        q[quads / 2] = make_float4(db[k].p[0].x, db[k].p[0].y, db[k].p[1].x, db[k].p[1].y);
+        q[quads / 2 + 1] = make_float4(db[k].p[2].x, db[k].p[2].y, db[k].p[3].x, db[k].p[3].y);
+    }
+    if (units == 1) return;
+    __syncthreads();
+    for (int i = threadIdx.x; i < quads; i += blockDim.x) {
+        float4 s = sums[i];
+        for (int u = 1; u < units; ++u) {
+            const float4 q = sums[u * quads + i];
+            s = make_float4(s.x + q.x, s.y + q.y, s.z + q.z, s.w + q.w);
         }
-        __syncthreads();
-        float* const part = a.partial + (int64_t)blockIdx.x * 2 * cols;
-        for (int c = threadIdx.x; c < 2 * (int)cols; c += blockDim.x) part[c] = sums[c];
-    } else {
-        // the blocks of a cluster leave one part: each adds up its share of the columns from all of them
-        const int ranks = (int)cluster_blocks();
-        float* const part = a.partial + (int64_t)(blockIdx.x / ranks) * 2 * cols;
-        float* const own = ranks > 1 ? sums : part;
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-#pragma unroll
-            for (int j = 0; j < kGranule; ++j) {
-                if (j >= n[k]) continue;
-                const int c = (k * team + t) * kGranule + j;
-                own[c] = dw[k].at(j), own[cols + c] = db[k].at(j);
-            }
-        }
-        if (ranks > 1) {
-            cluster_barrier();
-            for (int c = (int)cluster_rank() * team + t; c < 2 * (int)cols; c += ranks * team) {
-                float s = load_cluster(sums + c, 0);
-                for (int i = 1; i < ranks; ++i) s += load_cluster(sums + c, i);
-                part[c] = s;
-            }
-            cluster_barrier();  // the others may still be reading this block's sums
-        }
+        part[i] = s;
     }
 }
 
-// Joins the parts in a fixed order: a block takes 32 columns, its eight warps every eighth part.
-__global__ void __launch_bounds__(32 * kColumnWarps)
-norm_join_parts_kernel(const float* partial, int parts, int64_t cols, float* dweight, float* dbias) {
-    __shared__ float sums[kColumnWarps][32];
+// Joins the parts in a fixed order: a block takes 32 columns, its warps every 32nd part.
+constexpr int kJoinWarps = 32;
+__global__ void __launch_bounds__(32 * kJoinWarps)
+norm_join_parts_kernel(const float* partial, int parts, int64_t padded, int64_t cols, float* dweight, float* dbias) {
+    __shared__ float sums[kJoinWarps][33];
     grid_launch_dependents();
     grid_dependency_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int which = blockIdx.x & 1;
-    const int64_t c = (int64_t)(blockIdx.x >> 1) * 32 + lane;
+    const int64_t first = (int64_t)(blockIdx.x >> 1) * 32, c = first + lane;
     float* const out = which == 0 ? dweight : dbias;
     if (out == nullptr) return;
     float s = 0.0f;
     if (c < cols) {
-#pragma unroll 8
-        for (int k = warp; k < parts; k += kColumnWarps) s += partial[((int64_t)k * 2 + which) * cols + c];
+#pragma unroll 10
+        for (int k = warp; k < parts; k += kJoinWarps) s += partial[((int64_t)k * 2 + which) * padded + c];
     }
     sums[warp][lane] = s;
     __syncthreads();
-    if (warp == 0 && c < cols) {
+    s = sums[lane][warp];  // a warp joins one column
 #pragma unroll
-        for (int w = 1; w < kColumnWarps; ++w) s += sums[w][lane];
-        out[c] = s;
-    }
+    for (int off = 16; off > 0; off >>= 1) s = across(s, off);
+    if (lane == 0 && first + warp < cols) out[first + warp] = s;
 }
 
-// How a pass runs.  The team is the fewest threads that cover a row with V granules each: with V = 2 a team's
-// weights fit in registers beside the row and the one on its way.
+// How a pass runs: the threads that share a row and the granules each of them holds.  The fewest granules a thread
+// with which a team of at most 512 covers the row, but in the forward pass two rather than one beyond a warp (fewer
+// shuffles and barriers per element; the backward pass has no registers for that beside the column sums of its rows).
 struct Plan {
     int team, granules;  // team 0: the row does not fit a team
 };
-Plan make_plan(int64_t cols, int most) {
+Plan make_plan(int64_t cols, int least, int most) {
     const int64_t g = (cols + kGranule - 1) / kGranule;
     if (g <= 32) {
         int team = 1;
         while (team < g) team *= 2;
         return {team, 1};
     }
-    for (int v = 2; v <= most; v *= 2)
+    for (int v = least; v <= most; v *= 2)
         if (g <= (int64_t)v * kMaxTeam) return {(int)((g + 32 * v - 1) / (32 * v)) * 32, v};
     return {0, 0};
 }
-constexpr int kForwardGranules = 4, kBackwardGranules = 2;
+Plan forward_plan(int64_t cols) { return make_plan(cols, 2, 4); }
+Plan backward_plan(int64_t cols) { return make_plan(cols, 1, 2); }
 
 // Blocks of a kernel that an SM holds at once; asked for once per block size.
 template <typename K>
@@ -746,11 +753,11 @@ int resident_blocks(K kernel, unsigned block, size_t smem, std::atomic<int>* kno
     return QFMT_OK;
 }
 
-// Parts that the backward pass leaves for the gradients of weight and bias: one per block or cluster of the rows
-// kernel (512 threads on each SM of a B200 make at most two), or a share of the rows for long rows.
-constexpr int kMaxParts = 2 * 148;
+// Parts that the backward pass leaves for the gradients of weight and bias: one per block of the rows kernel,
+// which has a block on each of a B200's SMs, or a share of the rows for long rows.
+constexpr int kMaxParts = 148;
 int row_parts(const qfmt_norm_t& s) {
-    if (make_plan(s.cols, kBackwardGranules).team != 0) return kMaxParts;
+    if (backward_plan(s.cols).team != 0) return kMaxParts;
     const int64_t want = (s.rows + 8 * kColumnWarps - 1) / (8 * kColumnWarps);
     return (int)(want < 64 ? (want > 0 ? want : 1) : 64);
 }
@@ -820,7 +827,7 @@ int launch_forward_rows(const Call& c, const ForwardArgs<kType>& a, int team, cu
 
 template <int kType, bool kFused>
 int launch_forward(const Call& c, const ForwardArgs<kType>& a, cudaStream_t stream) {
-    const Plan plan = make_plan(a.cols, kForwardGranules);
+    const Plan plan = forward_plan(a.cols);
     if (plan.team != 0) {
         const auto run = a.vec && !a.fmt ? (plan.granules == 1   ? launch_forward_rows<kType, 1, 2, kFused, true>
                                             : plan.granules == 2 ? launch_forward_rows<kType, 2, kFused && kType == QFMT_F32 ? 1 : 2, kFused, true>
@@ -889,38 +896,49 @@ int forward_entry(const qfmt_norm_t* norm, const qfmt_dropout_t* drop, bool fuse
     return run(c, d_x, d_residual, d_weight, d_bias, d_h, d_y, d_mean, d_rstd, d_stats, stream);
 }
 
+int64_t padded_columns(int64_t cols) { return (cols + kGranule - 1) / kGranule * kGranule; }
+
 int join_parts(const float* partial, int parts, int64_t cols, float* d_dweight, float* d_dbias, cudaStream_t stream) {
-    QFMT_CUDA_TRY(launch_overlapping(norm_join_parts_kernel, 2u * (unsigned)((cols + 31) / 32), 32u * kColumnWarps, 0, stream, partial, parts,
-                                     cols, d_dweight, d_dbias));
+    QFMT_CUDA_TRY(launch_overlapping(norm_join_parts_kernel, 2u * (unsigned)((cols + 31) / 32), 32u * kJoinWarps, 0, stream, partial, parts,
+                                     padded_columns(cols), cols, d_dweight, d_dbias));
     return QFMT_OK;
 }
 
-template <int kType, int V, bool kFused, bool kPlain>
+template <int kType, int V, int R, bool kParts, bool kFused, bool kPlain>
 int launch_backward_rows(const Call& c, const BackwardArgs<kType>& a, int team, float* d_dweight, float* d_dbias, cudaStream_t stream) {
-    const auto kern = norm_backward_rows_kernel<kType, V, kFused, kPlain>;
-    // 512 threads an SM: one block of small teams, or as many blocks of one team, clustered so that they leave one part
-    const unsigned block = V > 1 ? team : kMaxTeam, teams = V > 1 ? 1 : block / team;
-    unsigned cluster = 1;
-    while (V > 1 && cluster < 8 && 2 * cluster * block <= kMaxTeam) cluster *= 2;
-    const size_t smem = c.hist_bytes + (V == 1 || cluster > 1 ? 2 * (size_t)a.cols * sizeof(float) : 0);
-    if (smem > 40 * 1024) QFMT_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    const int64_t want = (a.rows + (int64_t)teams * cluster - 1) / ((int64_t)teams * cluster);
-    const int64_t cap = (int64_t)c.dev.sm_count * kMaxTeam / (block * cluster);
-    const unsigned parts = (unsigned)(want < cap ? want < kMaxParts ? want : kMaxParts : cap < kMaxParts ? cap : kMaxParts);
-    const unsigned blocks = parts * cluster;
-    const int64_t stride = (int64_t)blocks * teams;
+    const unsigned teams = kMaxTeam / team, block = teams * team;
+    const int64_t cap = std::min(c.dev.sm_count, kMaxParts), want = (a.rows + teams * R - 1) / (teams * R);
+    // two rows at a time only where every team has them (a rule on sizes alone: it decides the order of the sums over rows)
+    if constexpr (R == 2) {
+        if (want < cap) return launch_backward_rows<kType, V, 1, kParts, kFused, kPlain>(c, a, team, d_dweight, d_dbias, stream);
+    }
+    const auto kern = norm_backward_rows_kernel<kType, V, R, kParts, kFused, kPlain>;
+    const unsigned units = kParts ? block / 32 : teams;
+    const size_t smem = c.hist_bytes + (units > 1 ? 2 * sizeof(float) * (size_t)padded_columns(a.cols) * units : 0);
+    static std::atomic<bool> allowed[64];
+    if (c.dev.ordinal < 0 || c.dev.ordinal >= 64 || !allowed[c.dev.ordinal].load()) {
+        QFMT_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 72 * 1024));  // histogram and sums
+        if (c.dev.ordinal >= 0 && c.dev.ordinal < 64) allowed[c.dev.ordinal].store(true);
+    }
+    const unsigned blocks = (unsigned)std::min(want, cap);
+    const int64_t stride = (int64_t)blocks * teams * R;
     const BackwardSteps step = {stride * a.ld_dy, stride * a.ld_h, stride * a.ld_dh, stride * a.ld_dx, stride * a.ld_dresidual};
-    QFMT_CUDA_TRY(launch_overlapping_clusters(kern, blocks, block, cluster, smem, stream, a, team, step, (int)(c.hist_bytes / sizeof(uint32_t))));
-    return a.partial != nullptr ? join_parts(a.partial, (int)parts, a.cols, d_dweight, d_dbias, stream) : QFMT_OK;
+    QFMT_CUDA_TRY(launch_overlapping(kern, blocks, block, smem, stream, a, team, step, (int)(c.hist_bytes / sizeof(uint32_t))));
+    return a.partial != nullptr ? join_parts(a.partial, (int)blocks, a.cols, d_dweight, d_dbias, stream) : QFMT_OK;
 }
 
 template <int kType, bool kFused>
 int launch_backward(const Call& c, const BackwardArgs<kType>& a, float* d_dweight, float* d_dbias, cudaStream_t stream) {
     if (a.rows == 0) return join_parts(a.partial, 0, a.cols, d_dweight, d_dbias, stream);  // zeros
-    const Plan plan = make_plan(a.cols, kBackwardGranules);
+    const Plan plan = backward_plan(a.cols);
     if (plan.team != 0) {
-        const auto run = a.vec && !a.fmt ? (plan.granules == 1 ? launch_backward_rows<kType, 1, kFused, true> : launch_backward_rows<kType, 2, kFused, true>)
-                               : (plan.granules == 1 ? launch_backward_rows<kType, 1, kFused, false> : launch_backward_rows<kType, 2, kFused, false>);
+        const bool plain = a.vec && !a.fmt;
+        const auto run = plan.granules == 2 ? (plain ? launch_backward_rows<kType, 2, 1, false, kFused, true>
+                                                     : launch_backward_rows<kType, 2, 1, false, kFused, false>)
+                         : plan.team > 32   ? (plain ? launch_backward_rows<kType, 1, 2, false, kFused, true>
+                                                     : launch_backward_rows<kType, 1, 2, false, kFused, false>)
+                                            : (plain ? launch_backward_rows<kType, 1, 2, true, kFused, true>
+                                                     : launch_backward_rows<kType, 1, 2, true, kFused, false>);
         return run(c, a, plan.team, d_dweight, d_dbias, stream);
     }
     if (a.partial != nullptr) {  // before the row pass, which may overwrite dy
@@ -1009,7 +1027,7 @@ int backward_entry(const qfmt_norm_t* norm, const qfmt_dropout_t* drop, bool fus
 
 extern "C" size_t qfmt_layer_norm_workspace_bytes(const qfmt_norm_t* norm) {
     if (norm == nullptr || norm->rows < 0 || norm->cols < 0 || norm->rows > 0x7FFFFFFF || norm->cols > 0x7FFFFFFF) return 0;
-    return (size_t)qfmt::row_parts(*norm) * 2 * (size_t)norm->cols * sizeof(float);
+    return (size_t)qfmt::row_parts(*norm) * 2 * (size_t)qfmt::padded_columns(norm->cols) * sizeof(float);
 }
 
 extern "C" int qfmt_layer_norm(const qfmt_norm_t* norm, const void* d_x, const float* d_weight, const float* d_bias, void* d_y,
