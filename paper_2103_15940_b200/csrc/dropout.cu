@@ -16,14 +16,11 @@ constexpr int kDropThreads = 256;
 
 template <int kType>
 struct DropArgs {
-    using W = typename Word<kType>::type;
-    const W* x;
-    const W* residual;  // or NULL
-    W* out;
-    int64_t ld_x, ld_residual, ld_out;
-    int64_t rows, cols;
+    Source<kType> x, residual;  // residual.p may be NULL
+    Target<kType> out;
+    int64_t cols;
     uint32_t granules;  // per row
-    bool vec;
+    uint64_t total;     // rows * granules
     DropParams drop;
 };
 
@@ -31,42 +28,38 @@ template <int kType>
 __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropArgs<kType> a) {
     grid_launch_dependents();
     grid_dependency_wait();
-    const uint64_t total = (uint64_t)a.rows * a.granules;
     const uint64_t offset = drop_offset(a.drop);
-    for (uint64_t i = (uint64_t)blockIdx.x * kDropThreads + threadIdx.x; i < total; i += (uint64_t)gridDim.x * kDropThreads) {
+    const int lane = threadIdx.x & 31;
+    const uint64_t step = (uint64_t)gridDim.x * kDropThreads;
+    for (uint64_t base = (uint64_t)blockIdx.x * kDropThreads; base < a.total; base += step) {  // whole warps
+        const uint64_t i = base + threadIdx.x;
         const uint64_t row = i / a.granules;
         const uint32_t g = (uint32_t)(i - row * a.granules);
         const int64_t col = (int64_t)g * kGranule;
-        const int n = a.cols - col < kGranule ? (int)(a.cols - col) : kGranule;
-        Granule v = widen_raw<kType>(load_words<kType>(a.x + row * a.ld_x + col, n, a.vec));
+        const int n = i < a.total ? (int)(a.cols - col < kGranule ? a.cols - col : kGranule) : 0;
+        Granule v = widen_raw<kType>(load_any<kType>(a.x.p + row * a.x.ld + col, n, a.x));
         if (a.drop.active) drop_granule(a.drop, offset, (uint32_t)row, g, v);
-        if (a.residual != nullptr) {
-            const Granule r = widen_raw<kType>(load_words<kType>(a.residual + row * a.ld_residual + col, n, a.vec));
+        if (a.residual.p != nullptr) {
+            const Granule r = widen_raw<kType>(load_any<kType>(a.residual.p + row * a.residual.ld + col, n, a.residual));
 #pragma unroll
             for (int j = 0; j < 4; ++j) v.p[j] = add2(r.p[j], v.p[j]);
         }
-        store_words<kType>(a.out + row * a.ld_out + col, n, a.vec, finish<kType>(v));
+        store_any<kType>(a.out.p + row * a.out.ld + col, n, a.out, finish<kType>(v), lane != 0 && g != 0, lane != 31 && g + 1 < a.granules);
     }
 }
 
 template <int kType>
 int launch_dropout(const void* d_x, int64_t ld_x, const void* d_residual, int64_t ld_residual, void* d_out, int64_t ld_out,
                    int64_t rows, int64_t cols, const DropParams& drop, const DeviceInfo& dev, cudaStream_t stream) {
-    using W = typename Word<kType>::type;
     DropArgs<kType> a;
-    a.x = static_cast<const W*>(d_x);
-    a.residual = static_cast<const W*>(d_residual);
-    a.out = static_cast<W*>(d_out);
-    a.ld_x = ld_x;
-    a.ld_residual = ld_residual;
-    a.ld_out = ld_out;
-    a.rows = rows;
+    a.x = make_source<kType>(d_x, ld_x, rows, cols);
+    a.residual = make_source<kType>(d_residual, ld_residual, rows, cols);
+    a.out = make_target<kType>(d_out, ld_out);
     a.cols = cols;
     a.granules = (uint32_t)((cols + kGranule - 1) / kGranule);
-    a.vec = granule_aligned(d_x, ld_x, kType) && granule_aligned(d_residual, ld_residual, kType) &&
-            granule_aligned(d_out, ld_out, kType);
+    a.total = (uint64_t)rows * a.granules;
     a.drop = drop;
-    const uint64_t blocks = ((uint64_t)rows * a.granules + kDropThreads - 1) / kDropThreads;
+    const uint64_t blocks = (a.total + kDropThreads - 1) / kDropThreads;
     const uint64_t cap = (uint64_t)dev.sm_count * 16;
     QFMT_CUDA_TRY(launch_overlapping(dropout_kernel<kType>, (unsigned)(blocks < cap ? blocks : cap), kDropThreads, 0, stream, a));
     return QFMT_OK;

@@ -130,18 +130,160 @@ __device__ __forceinline__ Granule widen_raw(const Raw<kType>& r) {
     return g;
 }
 
-// The words of `n` columns (1..8) of a granule at p, the others zero.  vec: p is aligned to a whole granule.
+// A matrix that is read or written in granules.  whole: every row starts on a granule boundary of memory.  last: one
+// past the matrix's last element.
 template <int kType>
-__device__ __forceinline__ Raw<kType> load_words(const typename Word<kType>::type* p, int n, bool vec) {
-    if (vec && n == kGranule) return load_raw<kType>(p);
+struct Source {
+    const typename Word<kType>::type* p;
+    const typename Word<kType>::type* last;
+    int64_t ld;
+    bool whole;
+};
+template <int kType>
+struct Target {
+    typename Word<kType>::type* p;
+    int64_t ld;
+    bool whole;
+};
+
+template <int kType>
+__device__ __forceinline__ uint32_t word_of(const Raw<kType>& r, int j) {
+    if constexpr (kType == QFMT_F32) return r.w[j];
+    else return j & 1 ? r.w[j / 2] >> 16 : r.w[j / 2] & 0xFFFFu;
+}
+
+// A granule's words from element `first` of w on; the elements are 32 or 16 bits wide.
+template <int kType, int kFrom>
+__device__ __forceinline__ Raw<kType> shifted(uint32_t (&w)[kFrom], uint32_t first) {
     Raw<kType> r;
+    constexpr int kWords = sizeof(r.w) / 4;
+    uint32_t word = kType == QFMT_F32 ? first : first >> 1;
 #pragma unroll
-    for (int j = 0; j < kGranule; ++j) {
-        const uint32_t w = j < n ? (uint32_t)p[j] : 0u;
-        if constexpr (kType == QFMT_F32) r.w[j] = w;
-        else r.w[j / 2] = j & 1 ? r.w[j / 2] | (w << 16) : w;
+    for (int by = 4; by > 0; by /= 2) {
+        if (by + kWords > kFrom) continue;  // no shift that far is asked for
+        const bool on = word & by;
+#pragma unroll
+        for (int i = 0; i + by < kFrom; ++i) w[i] = on ? w[i + by] : w[i];
+    }
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+        r.w[i] = w[i];
+        if (kType != QFMT_F32 && i + 1 < kFrom) r.w[i] = __funnelshift_r(w[i], w[i + 1], (first & 1) * 16);
     }
     return r;
+}
+
+// Four words of w from word `first` (0..4) on.
+struct Four {
+    uint32_t w[4];
+};
+__device__ __forceinline__ Four shifted_words(const uint32_t (&v)[8], int first) {
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = v[i];
+#pragma unroll
+    for (int by = 4; by > 0; by /= 2) {
+#pragma unroll
+        for (int i = 0; i + by < 8; ++i) w[i] = first & by ? w[i + by] : w[i];
+    }
+    return {{w[0], w[1], w[2], w[3]}};
+}
+
+// The words of `n` columns (0..8) of a granule at p, the others zero.  A granule that does not start on a boundary is
+// put together from the aligned 16-byte pieces it touches, where those lie inside the matrix (what they hold beyond
+// the row is thrown away); at the matrix's two ends it is read by elements.
+template <int kType>
+__device__ __forceinline__ Raw<kType> load_any(const typename Word<kType>::type* p, int n, const Source<kType>& m) {
+    if (m.whole && n == kGranule) return load_raw<kType>(p);
+    constexpr int kPer = kType == QFMT_F32 ? 4 : 8, kPieces = kType == QFMT_F32 ? 3 : 2;
+    Raw<kType> r;
+    const uint32_t first = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15u) / (16 / kPer);
+    const auto* base = p - first;
+    if (n > 0 && base >= m.p && base + kPieces * kPer <= m.last) {
+        uint32_t w[kPieces * 4];
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i)
+            asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];"
+                         : "=r"(w[4 * i]), "=r"(w[4 * i + 1]), "=r"(w[4 * i + 2]), "=r"(w[4 * i + 3]) : "l"(base + i * kPer));
+        r = shifted<kType>(w, first);
+        if (n < kGranule) {
+#pragma unroll
+            for (int i = 0; i < (int)(sizeof(r.w) / 4); ++i) {
+                if (kType == QFMT_F32) r.w[i] = i < n ? r.w[i] : 0u;
+                else r.w[i] = 2 * i + 1 < n ? r.w[i] : 2 * i < n ? r.w[i] & 0xFFFFu : 0u;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < kGranule; ++j) {
+            const uint32_t w = j < n ? (uint32_t)p[j] : 0u;
+            if constexpr (kType == QFMT_F32) r.w[j] = w;
+            else r.w[j / 2] = j & 1 ? r.w[j / 2] | (w << 16) : w;
+        }
+    }
+    return r;
+}
+
+// Writes `n` columns (0..8) of a granule at p.  Called by whole warps.  `from` and `to`: the lane before this one holds
+// the granule before this one, the lane after it the next.  Where rows do not start on granule boundaries a lane
+// writes the aligned 16-byte pieces that begin inside its granule, the last one with words of the next lane, and only
+// the ends of a warp's stretch are written by elements.
+template <int kType>
+__device__ __forceinline__ void store_any(typename Word<kType>::type* p, int n, const Target<kType>& m, const Raw<kType>& r, bool from,
+                                          bool to) {
+    constexpr int kPer = kType == QFMT_F32 ? 4 : 8;
+    bool head = false, body = false, tail = false;  // parts that an aligned piece covers
+    int first = kPer;                               // elements before the first piece that begins here
+    if (m.whole) {
+        if (n == kGranule) store_raw<kType>(p, r);
+        head = n == kGranule;
+        first = kGranule;
+    } else {
+        uint32_t w[8];
+        const int following = __shfl_down_sync(0xFFFFFFFFu, n, 1);
+        if constexpr (kType == QFMT_F32) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                w[i] = r.w[4 + i];
+                w[4 + i] = __shfl_down_sync(0xFFFFFFFFu, r.w[i], 1);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                w[i] = r.w[i];
+                w[4 + i] = __shfl_down_sync(0xFFFFFFFFu, r.w[i], 1);
+            }
+        }
+        const int skew = (int)(reinterpret_cast<uintptr_t>(p) & 15u) / (16 / kPer);
+        first = (kPer - skew) & (kPer - 1);
+        head = first == 0 || (from && n >= first);
+        tail = skew != 0 && to && following >= first;
+        if constexpr (kType == QFMT_F32) {
+            body = n == kGranule;
+            if (body) {  // the piece in the middle is all this lane's
+                uint32_t own[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) own[i] = r.w[i];
+                const Four q = shifted_words(own, first);
+                asm volatile("st.global.v4.b32 [%0], {%1,%2,%3,%4};" ::"l"(p + first), "r"(q.w[0]), "r"(q.w[1]), "r"(q.w[2]), "r"(q.w[3]) : "memory");
+            }
+            if (first == 0) tail = body;
+            if (tail) {
+                const Four q = shifted_words(w, first);
+                asm volatile("st.global.v4.b32 [%0], {%1,%2,%3,%4};" ::"l"(p + first + 4), "r"(q.w[0]), "r"(q.w[1]), "r"(q.w[2]), "r"(q.w[3]) : "memory");
+            }
+        } else {
+            if (first == 0) tail = n == kGranule;
+            if (tail) {
+                const Raw<kType> q = shifted<kType>(w, first);
+                asm volatile("st.global.v4.b32 [%0], {%1,%2,%3,%4};" ::"l"(p + first), "r"(q.w[0]), "r"(q.w[1]), "r"(q.w[2]), "r"(q.w[3]) : "memory");
+            }
+        }
+    }
+    const int second = kType == QFMT_F32 ? first + 4 : first;
+#pragma unroll
+    for (int j = 0; j < kGranule; ++j)
+        if (j < n && !(j < first ? head : j < second ? body : tail)) p[j] = (typename Word<kType>::type)word_of<kType>(r, j);
 }
 
 // Eight finished values to words, rounded once to the storage type (nearest, ties to even).
@@ -185,21 +327,6 @@ __device__ __forceinline__ Raw<kType> finish_format(const Granule& v, int n, con
             if (j < n) atomicAdd(&hist[bin[j] * 32 + lane], 1u);
     }
     return r;
-}
-
-template <int kType>
-__device__ __forceinline__ void store_words(typename Word<kType>::type* p, int n, bool vec, const Raw<kType>& r) {
-    if (vec && n == kGranule) {
-        store_raw<kType>(p, r);
-    } else {
-#pragma unroll
-        for (int j = 0; j < kGranule; ++j) {
-            if (j < n) {
-                if constexpr (kType == QFMT_F32) p[j] = r.w[j];
-                else p[j] = (uint16_t)(j & 1 ? r.w[j / 2] >> 16 : r.w[j / 2] & 0xFFFFu);
-            }
-        }
-    }
 }
 
 // Philox4x32-10 (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3", SC 2011): ten
@@ -263,9 +390,18 @@ __device__ __forceinline__ void flush_hist(const uint32_t* hist, const QuantPara
 inline size_t element_size(int32_t dtype) { return dtype == QFMT_F32 ? 4 : 2; }
 inline size_t granule_bytes(int32_t dtype) { return kGranule * element_size(dtype); }
 inline bool element_aligned(const void* p, int32_t dtype) { return (reinterpret_cast<uintptr_t>(p) & (element_size(dtype) - 1)) == 0; }
-// Whether every full granule of every row of a matrix may be moved by one access.
+// Whether every row of a matrix starts on a granule boundary.
 inline bool granule_aligned(const void* p, int64_t ld, int32_t dtype) {
-    return p == nullptr || ((reinterpret_cast<uintptr_t>(p) & (granule_bytes(dtype) - 1)) == 0 && ld % kGranule == 0);
+    return (reinterpret_cast<uintptr_t>(p) & (granule_bytes(dtype) - 1)) == 0 && ld % kGranule == 0;
+}
+template <int kType>
+Source<kType> make_source(const void* p, int64_t ld, int64_t rows, int64_t cols) {
+    const auto* q = static_cast<const typename Word<kType>::type*>(p);
+    return {q, p == nullptr || rows == 0 ? q : q + (rows - 1) * ld + cols, ld, granule_aligned(p, ld, kType)};
+}
+template <int kType>
+Target<kType> make_target(void* p, int64_t ld) {
+    return {static_cast<typename Word<kType>::type*>(p), ld, granule_aligned(p, ld, kType)};
 }
 
 inline int make_drop_params(const qfmt_dropout_t* d, DropParams* out) {

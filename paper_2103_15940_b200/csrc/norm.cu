@@ -13,6 +13,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <initializer_list>
 
 #include "common.cuh"
 #include "elements.cuh"
@@ -22,21 +23,16 @@ namespace {
 
 template <int kType>
 struct ForwardArgs {
-    using W = typename Word<kType>::type;
-    const W* x;
-    const W* residual;  // or NULL
+    Source<kType> x, residual;  // residual.p may be NULL
     const float* weight;
     const float* bias;
-    W* h;  // or NULL
-    W* y;
+    Target<kType> h, y;  // h.p may be NULL
     float* mean;
     float* rstd;
-    int64_t ld_x, ld_residual, ld_h, ld_y;
     int64_t rows, cols;
     float eps;
-    bool vec;  // every granule whole and aligned
-    bool fmt;  // quant holds a format to round to
     float inverse;  // 1 / cols
+    bool fmt;       // quant holds a format to round to
     DropParams drop;
     QuantParams quant;
     qfmt_stats_t* stats;
@@ -44,21 +40,15 @@ struct ForwardArgs {
 
 template <int kType>
 struct BackwardArgs {
-    using W = typename Word<kType>::type;
-    const W* dy;
-    const W* dh;  // gradient that reaches h by another path, or NULL
-    const W* h;
+    Source<kType> dy, dh, h;  // dh: gradient that reaches h by another path, or NULL
     const float* mean;
     const float* rstd;
     const float* weight;
-    W* dx;         // or NULL
-    W* dresidual;  // or NULL
-    float* partial;  // [parts][2][cols] sums of dy xhat and dy over a part of the rows, or NULL
-    int64_t ld_dy, ld_dh, ld_h, ld_dx, ld_dresidual;
+    Target<kType> dx, dresidual;  // or NULL
+    float* partial;  // [parts][2][padded columns] sums of dy xhat and dy over a part of the rows, or NULL
     int64_t rows, cols;
-    bool vec;  // every granule whole and aligned
-    bool fmt;  // quant holds a format to round to
-    float inverse;  // 1 / cols
+    float inverse;
+    bool fmt;
     DropParams drop;
     QuantParams quant;
     qfmt_stats_t* stats;
@@ -89,16 +79,16 @@ __device__ __forceinline__ Granule load_columns(const float* p, int64_t g, int n
 
 // A granule of n columns at p, zeros where there are none.  kPlain: whole and aligned, or not there at all.
 template <int kType, bool kPlain>
-__device__ __forceinline__ Raw<kType> fetch(const typename Word<kType>::type* p, int n, bool vec) {
+__device__ __forceinline__ Raw<kType> fetch(const typename Word<kType>::type* p, int n, const Source<kType>& m) {
     if constexpr (kPlain) return load_raw<kType>(p, n > 0);
-    else return load_words<kType>(p, n, vec);
+    else return load_any<kType>(p, n, m);
 }
 template <int kType, bool kPlain>
-__device__ __forceinline__ void put(typename Word<kType>::type* p, int n, bool vec, const Raw<kType>& r) {
+__device__ __forceinline__ void put(typename Word<kType>::type* p, int n, const Target<kType>& m, const Raw<kType>& r, bool from, bool to) {
     if constexpr (kPlain) {
         if (n > 0) store_raw<kType>(p, r);
     } else {
-        store_words<kType>(p, n, vec, r);
+        store_any<kType>(p, n, m, r, from, to);
     }
 }
 
@@ -109,7 +99,7 @@ __device__ __forceinline__ Granule join_h(const ForwardArgs<kType>& a, const Raw
     Granule v = widen_raw<kType>(x);
     if constexpr (kFused) {
         if (a.drop.active) drop_granule(a.drop, offset, row, g, v);
-        if (a.residual != nullptr) {
+        if (a.residual.p != nullptr) {
             const Granule u = widen_raw<kType>(r);
 #pragma unroll
             for (int j = 0; j < 4; ++j) v.p[j] = add2(u.p[j], v.p[j]);
@@ -183,18 +173,16 @@ __global__ void __launch_bounds__(kLoopThreads) norm_forward_loop_kernel(const F
     const uint32_t granules = (uint32_t)((a.cols + kGranule - 1) / kGranule);
     const float count = (float)a.cols;
     const uint64_t offset = kFused ? drop_offset(a.drop) : 0ull;
+    const bool from = threadIdx.x & 31, to = (threadIdx.x & 31) != 31;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const auto* x = a.x + row * a.ld_x;
-        const auto* r = a.residual + row * a.ld_residual;
         const auto h = [&](uint32_t g, int n) {
-            const Raw<kType> res = kFused && a.residual != nullptr ? fetch<kType, false>(r + (int64_t)g * kGranule, n, a.vec) : Raw<kType>();
-            return join_h<kType, kFused>(a, fetch<kType, false>(x + (int64_t)g * kGranule, n, a.vec), res, offset, (uint32_t)row, g);
+            const int64_t col = (int64_t)g * kGranule;
+            const Raw<kType> res = kFused && a.residual.p != nullptr
+                                       ? load_any<kType>(a.residual.p + row * a.residual.ld + col, n, a.residual) : Raw<kType>();
+            return join_h<kType, kFused>(a, load_any<kType>(a.x.p + row * a.x.ld + col, n, a.x), res, offset, (uint32_t)row, g);
         };
         float sum = 0.0f;
-        for (uint32_t g = threadIdx.x; g < granules; g += kLoopThreads) {
-            const int n = granule_columns(a.cols, g);
-            sum += sum8(h(g, n));
-        }
+        for (uint32_t g = threadIdx.x; g < granules; g += kLoopThreads) sum += sum8(h(g, granule_columns(a.cols, g)));
         const float mean = block_sum(make_float2(sum, 0.0f), scratch).x / count;
         sum = 0.0f;
         for (uint32_t g = threadIdx.x; g < granules; g += kLoopThreads) {
@@ -207,14 +195,16 @@ __global__ void __launch_bounds__(kLoopThreads) norm_forward_loop_kernel(const F
             if (a.mean != nullptr) a.mean[row] = mean;
             if (a.rstd != nullptr) a.rstd[row] = rstd;
         }
-        for (uint32_t g = threadIdx.x; g < granules; g += kLoopThreads) {
+        for (uint32_t g0 = 0; g0 < granules; g0 += kLoopThreads) {  // whole warps
+            const uint32_t g = g0 + threadIdx.x;
+            const int64_t col = (int64_t)g * kGranule;
             const int n = granule_columns(a.cols, g);
             Granule v = h(g, n);
-            if (kFused && a.h != nullptr) put<kType, false>(a.h + row * a.ld_h + (int64_t)g * kGranule, n, a.vec, finish<kType>(v));
+            if (kFused && a.h.p != nullptr) store_any<kType>(a.h.p + row * a.h.ld + col, n, a.h, finish<kType>(v), from, to);
             const Granule w = load_columns(a.weight, g, n, 1.0f), b = load_columns(a.bias, g, n, 0.0f);
 #pragma unroll
             for (int j = 0; j < 4; ++j) v.p[j] = fma2(mul2(add2(v.p[j], both(-mean)), both(rstd)), w.p[j], b.p[j]);
-            put<kType, false>(a.y + row * a.ld_y + (int64_t)g * kGranule, n, a.vec, finish_output<kType, false>(a, v, n, hist));
+            store_any<kType>(a.y.p + row * a.y.ld + col, n, a.y, finish_output<kType, false>(a, v, n, hist), from, to);
         }
     }
     if (hist != nullptr) flush_hist(hist, a.quant, a.stats, (uint64_t)a.rows * (uint64_t)a.cols);
@@ -299,8 +289,9 @@ __global__ void __launch_bounds__(kMaxTeam) norm_forward_rows_kernel(const Forwa
     }
     if (hist != nullptr) clear_hist(hist, a.quant);
     const int mine = V > 1 ? 0 : threadIdx.x / team, t = threadIdx.x - mine * team, teams = V > 1 ? 1 : blockDim.x / team;
+    const bool from = (t & 31) != 0, to = (t & 31) != 31 && t + 1 < team;  // the lanes before and after hold neighbours
     const uint64_t offset = kFused ? drop_offset(a.drop) : 0ull;
-    const bool residual = kFused && a.residual != nullptr;
+    const bool residual = kFused && a.residual.p != nullptr;
     const int next = team * kGranule;  // elements between a thread's granules
     int n[V];                          // columns of each granule
 #pragma unroll
@@ -309,10 +300,10 @@ __global__ void __launch_bounds__(kMaxTeam) norm_forward_rows_kernel(const Forwa
     // A team past the last row, whose warp has teams with one, keeps in step with them and stores nothing.
     const uint32_t rows = (uint32_t)a.rows, stride = gridDim.x * teams * R;
     uint32_t row = (blockIdx.x * teams + mine) * R;
-    const auto* px = a.x + row * a.ld_x + t * kGranule;
-    const auto* pr = a.residual + row * a.ld_residual + t * kGranule;
-    auto* ph = a.h + row * a.ld_h + t * kGranule;
-    auto* py = a.y + row * a.ld_y + t * kGranule;
+    const auto* px = a.x.p + row * a.x.ld + t * kGranule;
+    const auto* pr = a.residual.p + row * a.residual.ld + t * kGranule;
+    auto* ph = a.h.p + row * a.h.ld + t * kGranule;
+    auto* py = a.y.p + row * a.y.ld + t * kGranule;
     Raw<kType> x[R][V], r[R][V];
     const auto fetch_rows = [&](uint32_t at) {
 #pragma unroll
@@ -320,8 +311,8 @@ __global__ void __launch_bounds__(kMaxTeam) norm_forward_rows_kernel(const Forwa
             const bool there = at + i < rows;
 #pragma unroll
             for (int k = 0; k < V; ++k) {
-                x[i][k] = fetch<kType, kPlain>(px + i * a.ld_x + k * next, there ? n[k] : 0, a.vec);
-                if (kFused) r[i][k] = fetch<kType, kPlain>(pr + i * a.ld_residual + k * next, there && residual ? n[k] : 0, a.vec);
+                x[i][k] = fetch<kType, kPlain>(px + i * a.x.ld + k * next, there ? n[k] : 0, a.x);
+                if (kFused) r[i][k] = fetch<kType, kPlain>(pr + i * a.residual.ld + k * next, there && residual ? n[k] : 0, a.residual);
             }
         }
         px += step.x;
@@ -345,12 +336,12 @@ __global__ void __launch_bounds__(kMaxTeam) norm_forward_rows_kernel(const Forwa
 #pragma unroll
             for (int k = 0; k < V; ++k) v[i][k] = join_h<kType, kFused>(a, x[i][k], r[i][k], offset, row + i, k * team + t);
         if (kAhead) fetch_rows(row + stride);
-        if (kFused && a.h != nullptr) {
+        if (kFused && a.h.p != nullptr) {
 #pragma unroll
             for (int i = 0; i < R; ++i)
 #pragma unroll
                 for (int k = 0; k < V; ++k)
-                    put<kType, kPlain>(ph + i * a.ld_h + k * next, row + i < rows ? n[k] : 0, a.vec, finish<kType>(v[i][k]));
+                    put<kType, kPlain>(ph + i * a.h.ld + k * next, row + i < rows ? n[k] : 0, a.h, finish<kType>(v[i][k]), from, to);
         }
         const auto total = [&](float (&out)[R], float* space) {
             if constexpr (R == 2) {
@@ -396,7 +387,7 @@ __global__ void __launch_bounds__(kMaxTeam) norm_forward_rows_kernel(const Forwa
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[i][k].p[j] = fma2(mul2(v[i][k].p[j], both(rstd[i])), wk.p[j], bk.p[j]);
                 const int there = row + i < rows ? n[k] : 0;
-                put<kType, kPlain>(py + i * a.ld_y + k * next, there, a.vec, finish_output<kType, kPlain>(a, v[i][k], there, hist));
+                put<kType, kPlain>(py + i * a.y.ld + k * next, there, a.y, finish_output<kType, kPlain>(a, v[i][k], there, hist), from, to);
             }
         }
         ph += step.h;
@@ -437,28 +428,29 @@ struct GradientRow {
     typename Word<kType>::type* dx;
     typename Word<kType>::type* dresidual;
     __device__ __forceinline__ GradientRow(const BackwardArgs<kType>& a, int64_t row, int64_t col)
-        : dh(a.dh + row * a.ld_dh + col), dx(a.dx + row * a.ld_dx + col), dresidual(a.dresidual + row * a.ld_dresidual + col) {}
+        : dh(a.dh.p + row * a.dh.ld + col), dx(a.dx.p + row * a.dx.ld + col), dresidual(a.dresidual.p + row * a.dresidual.ld + col) {}
 };
 
 // What a granule's gradients become: dh (with what arrives by another path) to dresidual, D of it to dx.
 template <int kType, bool kFused, bool kPlain>
 __device__ __forceinline__ void store_gradients(const BackwardArgs<kType>& a, const GradientRow<kType>& to, int i, int64_t at, const Granule& dy,
                                                 const Granule& xhat, const Granule& w, float rstd, float c1, float c2, uint32_t row,
-                                                uint32_t g, int n, uint64_t offset, uint32_t* hist) {
+                                                uint32_t g, int n, bool from, bool after, uint64_t offset,
+                                                uint32_t* hist) {
     Granule d;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
         d.p[j] = mul2(fma2(xhat.p[j], both(-c2), fma2(dy.p[j], w.p[j], both(-c1))), both(rstd));
     if constexpr (kFused) {
-        if (a.dh != nullptr) {
-            const Granule more = widen_raw<kType>(fetch<kType, kPlain>(to.dh + i * a.ld_dh + at, n, a.vec));
+        if (a.dh.p != nullptr) {
+            const Granule more = widen_raw<kType>(fetch<kType, kPlain>(to.dh + i * a.dh.ld + at, n, a.dh));
 #pragma unroll
             for (int j = 0; j < 4; ++j) d.p[j] = add2(d.p[j], more.p[j]);
         }
-        if (a.dresidual != nullptr) put<kType, kPlain>(to.dresidual + i * a.ld_dresidual + at, n, a.vec, finish<kType>(d));
-        if (a.drop.active && a.dx != nullptr) drop_granule(a.drop, offset, row, g, d);
+        if (a.dresidual.p != nullptr) put<kType, kPlain>(to.dresidual + i * a.dresidual.ld + at, n, a.dresidual, finish<kType>(d), from, after);
+        if (a.drop.active && a.dx.p != nullptr) drop_granule(a.drop, offset, row, g, d);
     }
-    if (a.dx != nullptr) put<kType, kPlain>(to.dx + i * a.ld_dx + at, n, a.vec, finish_output<kType, kPlain>(a, d, n, hist));
+    if (a.dx.p != nullptr) put<kType, kPlain>(to.dx + i * a.dx.ld + at, n, a.dx, finish_output<kType, kPlain>(a, d, n, hist), from, after);
 }
 
 // Long rows: a block takes a row at a time and reads it twice.
@@ -474,8 +466,8 @@ __global__ void __launch_bounds__(kLoopThreads) norm_backward_loop_kernel(const 
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const float mean = a.mean[row], rstd = a.rstd[row];
         const auto load = [&](uint32_t g, int n, Granule& dy, Granule& xhat, Granule& w) {
-            dy = widen_raw<kType>(fetch<kType, false>(a.dy + row * a.ld_dy + (int64_t)g * kGranule, n, a.vec));
-            xhat = normalise<false>(widen_raw<kType>(fetch<kType, false>(a.h + row * a.ld_h + (int64_t)g * kGranule, n, a.vec)), mean, rstd, n);
+            dy = widen_raw<kType>(load_any<kType>(a.dy.p + row * a.dy.ld + (int64_t)g * kGranule, n, a.dy));
+            xhat = normalise<false>(widen_raw<kType>(load_any<kType>(a.h.p + row * a.h.ld + (int64_t)g * kGranule, n, a.h)), mean, rstd, n);
             w = load_columns(a.weight, g, n, 1.0f);
         };
         float2 s = make_float2(0.0f, 0.0f);
@@ -485,11 +477,12 @@ __global__ void __launch_bounds__(kLoopThreads) norm_backward_loop_kernel(const 
             s = add2(s, row_sums(dy, xhat, w));
         }
         s = block_sum(s, scratch);
-        for (uint32_t g = threadIdx.x; g < granules; g += kLoopThreads) {
+        for (uint32_t g0 = 0; g0 < granules; g0 += kLoopThreads) {  // whole warps
+            const uint32_t g = g0 + threadIdx.x;
             const int n = granule_columns(a.cols, g);
             load(g, n, dy, xhat, w);
             store_gradients<kType, kFused, false>(a, GradientRow<kType>(a, row, 0), 0, (int64_t)g * kGranule, dy, xhat, w, rstd, s.x / count,
-                                                  s.y / count, (uint32_t)row, g, n, offset, hist);
+                                                  s.y / count, (uint32_t)row, g, n, threadIdx.x & 31, (threadIdx.x & 31) != 31, offset, hist);
         }
     }
     if (hist != nullptr) flush_hist(hist, a.quant, a.stats, (uint64_t)a.rows * (uint64_t)a.cols);
@@ -507,8 +500,8 @@ __global__ void __launch_bounds__(32 * kColumnWarps) norm_column_sums_kernel(con
     Granule dw = splat(0.0f), db = splat(0.0f);
     if (n > 0) {
         for (int64_t row = (int64_t)blockIdx.y * kColumnWarps + warp; row < a.rows; row += (int64_t)gridDim.y * kColumnWarps) {
-            const Granule dy = widen_raw<kType>(fetch<kType, false>(a.dy + row * a.ld_dy + (int64_t)g * kGranule, n, a.vec));
-            const Granule xhat = normalise<false>(widen_raw<kType>(fetch<kType, false>(a.h + row * a.ld_h + (int64_t)g * kGranule, n, a.vec)), a.mean[row], a.rstd[row], n);
+            const Granule dy = widen_raw<kType>(load_any<kType>(a.dy.p + row * a.dy.ld + (int64_t)g * kGranule, n, a.dy));
+            const Granule xhat = normalise<false>(widen_raw<kType>(load_any<kType>(a.h.p + row * a.h.ld + (int64_t)g * kGranule, n, a.h)), a.mean[row], a.rstd[row], n);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 dw.p[j] = fma2(dy.p[j], xhat.p[j], dw.p[j]);
@@ -579,6 +572,7 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, const BackwardS
     // (the shuffle tells the compiler that a warp belongs to one team)
     const int mine = kParts ? threadIdx.x / team : __shfl_sync(0xFFFFFFFFu, threadIdx.x / team, 0);
     const int t = threadIdx.x - mine * team, teams = blockDim.x / team;
+    const bool from = (t & 31) != 0, after = (t & 31) != 31 && t + 1 < team;
     const uint64_t offset = kFused ? drop_offset(a.drop) : 0ull;
     const int next = team * kGranule;  // elements between a thread's granules
     int n[V];
@@ -590,8 +584,8 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, const BackwardS
     }
     const uint32_t rows = (uint32_t)a.rows, stride = gridDim.x * teams * R;
     uint32_t row = (blockIdx.x * teams + mine) * R;
-    const auto* pdy = a.dy + row * a.ld_dy + t * kGranule;
-    const auto* ph = a.h + row * a.ld_h + t * kGranule;
+    const auto* pdy = a.dy.p + row * a.dy.ld + t * kGranule;
+    const auto* ph = a.h.p + row * a.h.ld + t * kGranule;
     GradientRow<kType> to(a, row, t * kGranule);
     Raw<kType> raw_dy[R][V], raw_h[R][V];
     float mean[R], rstd[R];
@@ -603,8 +597,8 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, const BackwardS
             rstd[i] = there ? __ldg(a.rstd + at + i) : 0.0f;
 #pragma unroll
             for (int k = 0; k < V; ++k) {
-                raw_dy[i][k] = fetch<kType, kPlain>(pdy + i * a.ld_dy + k * next, there ? n[k] : 0, a.vec);
-                raw_h[i][k] = fetch<kType, kPlain>(ph + i * a.ld_h + k * next, there ? n[k] : 0, a.vec);
+                raw_dy[i][k] = fetch<kType, kPlain>(pdy + i * a.dy.ld + k * next, there ? n[k] : 0, a.dy);
+                raw_h[i][k] = fetch<kType, kPlain>(ph + i * a.h.ld + k * next, there ? n[k] : 0, a.h);
             }
         }
         pdy += step.dy;
@@ -650,7 +644,7 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, const BackwardS
 #pragma unroll
             for (int k = 0; k < V; ++k)
                 store_gradients<kType, kFused, kPlain>(a, to, i, k * next, dy[i][k], xhat[i][k], w[k], this_rstd[i], c1, c2, row + i,
-                                                       k * team + t, row + i < rows ? n[k] : 0, offset, hist);
+                                                       k * team + t, row + i < rows ? n[k] : 0, from, after, offset, hist);
         }
         to.dh += step.dh;
         to.dx += step.dx;
@@ -805,6 +799,11 @@ int prepare_call(const qfmt_norm_t* norm, const qfmt_dropout_t* drop, const qfmt
 
 bool float_aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
+// Whether every granule of every tensor is whole and aligned.
+bool plain_layout(int64_t cols, std::initializer_list<bool> whole) {
+    return cols % kGranule == 0 && std::all_of(whole.begin(), whole.end(), [](bool w) { return w; });
+}
+
 template <int kType, int V, int R, bool kFused, bool kPlain>
 int launch_forward_rows(const Call& c, const ForwardArgs<kType>& a, int team, cudaStream_t stream) {
     static std::atomic<int> known[kMaxTeam / 32 + 1];
@@ -820,7 +819,7 @@ int launch_forward_rows(const Call& c, const ForwardArgs<kType>& a, int team, cu
     }
     const unsigned blocks = (unsigned)(want < cap ? want : cap);
     const int64_t stride = (int64_t)blocks * teams * R;
-    const ForwardSteps step = {stride * a.ld_x, stride * a.ld_residual, stride * a.ld_h, stride * a.ld_y};
+    const ForwardSteps step = {stride * a.x.ld, stride * a.residual.ld, stride * a.h.ld, stride * a.y.ld};
     QFMT_CUDA_TRY(launch_overlapping(kern, blocks, block, c.hist_bytes, stream, a, team, step));
     return QFMT_OK;
 }
@@ -829,7 +828,8 @@ template <int kType, bool kFused>
 int launch_forward(const Call& c, const ForwardArgs<kType>& a, cudaStream_t stream) {
     const Plan plan = forward_plan(a.cols);
     if (plan.team != 0) {
-        const auto run = a.vec && !a.fmt ? (plan.granules == 1   ? launch_forward_rows<kType, 1, 2, kFused, true>
+        const bool plain = plain_layout(a.cols, {a.x.whole, a.residual.whole, a.h.whole, a.y.whole}) && !a.fmt;
+        const auto run = plain ? (plan.granules == 1   ? launch_forward_rows<kType, 1, 2, kFused, true>
                                             : plan.granules == 2 ? launch_forward_rows<kType, 2, kFused && kType == QFMT_F32 ? 1 : 2, kFused, true>
                                                                  : launch_forward_rows<kType, 4, 1, kFused, true>)
                                          : (plan.granules == 1   ? launch_forward_rows<kType, 1, 1, kFused, false>
@@ -846,27 +846,21 @@ int launch_forward(const Call& c, const ForwardArgs<kType>& a, cudaStream_t stre
 template <int kType, bool kFused>
 int forward(const Call& c, const void* d_x, const void* d_residual, const float* d_weight, const float* d_bias, void* d_h,
             void* d_y, float* d_mean, float* d_rstd, qfmt_stats_t* d_stats, cudaStream_t stream) {
-    using W = typename Word<kType>::type;
+    const qfmt_norm_t& s = c.norm;
     ForwardArgs<kType> a;
-    a.x = static_cast<const W*>(d_x);
-    a.residual = static_cast<const W*>(d_residual);
+    a.x = make_source<kType>(d_x, s.ld_x, s.rows, s.cols);
+    a.residual = make_source<kType>(d_residual, s.ld_residual, s.rows, s.cols);
     a.weight = d_weight;
     a.bias = d_bias;
-    a.h = static_cast<W*>(d_h);
-    a.y = static_cast<W*>(d_y);
+    a.h = make_target<kType>(d_h, s.ld_h);
+    a.y = make_target<kType>(d_y, s.ld_y);
     a.mean = d_mean;
     a.rstd = d_rstd;
-    a.ld_x = c.norm.ld_x;
-    a.ld_residual = c.norm.ld_residual;
-    a.ld_h = c.norm.ld_h;
-    a.ld_y = c.norm.ld_y;
-    a.rows = c.norm.rows;
-    a.cols = c.norm.cols;
-    a.eps = c.norm.eps;
-    a.vec = a.cols % kGranule == 0 && granule_aligned(d_x, a.ld_x, kType) && granule_aligned(d_residual, a.ld_residual, kType) &&
-            granule_aligned(d_h, a.ld_h, kType) && granule_aligned(d_y, a.ld_y, kType);
-    a.fmt = c.fmt;
+    a.rows = s.rows;
+    a.cols = s.cols;
+    a.eps = s.eps;
     a.inverse = 1.0f / (float)a.cols;
+    a.fmt = c.fmt;
     a.drop = c.drop;
     a.quant = c.quant;
     a.stats = d_stats;
@@ -922,7 +916,7 @@ int launch_backward_rows(const Call& c, const BackwardArgs<kType>& a, int team, 
     }
     const unsigned blocks = (unsigned)std::min(want, cap);
     const int64_t stride = (int64_t)blocks * teams * R;
-    const BackwardSteps step = {stride * a.ld_dy, stride * a.ld_h, stride * a.ld_dh, stride * a.ld_dx, stride * a.ld_dresidual};
+    const BackwardSteps step = {stride * a.dy.ld, stride * a.h.ld, stride * a.dh.ld, stride * a.dx.ld, stride * a.dresidual.ld};
     QFMT_CUDA_TRY(launch_overlapping(kern, blocks, block, smem, stream, a, team, step, (int)(c.hist_bytes / sizeof(uint32_t))));
     return a.partial != nullptr ? join_parts(a.partial, (int)blocks, a.cols, d_dweight, d_dbias, stream) : QFMT_OK;
 }
@@ -932,7 +926,7 @@ int launch_backward(const Call& c, const BackwardArgs<kType>& a, float* d_dweigh
     if (a.rows == 0) return join_parts(a.partial, 0, a.cols, d_dweight, d_dbias, stream);  // zeros
     const Plan plan = backward_plan(a.cols);
     if (plan.team != 0) {
-        const bool plain = a.vec && !a.fmt;
+        const bool plain = plain_layout(a.cols, {a.dy.whole, a.dh.whole, a.h.whole, a.dx.whole, a.dresidual.whole}) && !a.fmt;
         const auto run = plan.granules == 2 ? (plain ? launch_backward_rows<kType, 2, 1, false, kFused, true>
                                                      : launch_backward_rows<kType, 2, 1, false, kFused, false>)
                          : plan.team > 32   ? (plain ? launch_backward_rows<kType, 1, 2, false, kFused, true>
@@ -949,7 +943,7 @@ int launch_backward(const Call& c, const BackwardArgs<kType>& a, float* d_dweigh
         const int rc = join_parts(a.partial, parts, a.cols, d_dweight, d_dbias, stream);
         if (rc != QFMT_OK) return rc;
     }
-    if (a.dx != nullptr || a.dresidual != nullptr) {
+    if (a.dx.p != nullptr || a.dresidual.p != nullptr) {
         const int64_t cap = (int64_t)c.dev.sm_count * 4;
         norm_backward_loop_kernel<kType, kFused><<<(unsigned)(a.rows < cap ? a.rows : cap), kLoopThreads, c.hist_bytes, stream>>>(a);
         QFMT_CUDA_TRY(cudaGetLastError());
@@ -961,28 +955,21 @@ template <int kType, bool kFused>
 int backward(const Call& c, const void* d_dy, const void* d_dh, const void* d_h, int64_t ld_h, const float* d_mean,
              const float* d_rstd, const float* d_weight, void* d_dx, void* d_dresidual, float* d_dweight, float* d_dbias,
              qfmt_stats_t* d_stats, float* partial, cudaStream_t stream) {
-    using W = typename Word<kType>::type;
+    const qfmt_norm_t& s = c.norm;
     BackwardArgs<kType> a;
-    a.dy = static_cast<const W*>(d_dy);
-    a.dh = static_cast<const W*>(d_dh);
-    a.h = static_cast<const W*>(d_h);
+    a.dy = make_source<kType>(d_dy, s.ld_dy, s.rows, s.cols);
+    a.dh = make_source<kType>(d_dh, s.ld_dh, s.rows, s.cols);
+    a.h = make_source<kType>(d_h, ld_h, s.rows, s.cols);
     a.mean = d_mean;
     a.rstd = d_rstd;
     a.weight = d_weight;
-    a.dx = static_cast<W*>(d_dx);
-    a.dresidual = static_cast<W*>(d_dresidual);
+    a.dx = make_target<kType>(d_dx, s.ld_dx);
+    a.dresidual = make_target<kType>(d_dresidual, s.ld_dresidual);
     a.partial = partial;
-    a.ld_dy = c.norm.ld_dy;
-    a.ld_dh = c.norm.ld_dh;
-    a.ld_h = ld_h;
-    a.ld_dx = c.norm.ld_dx;
-    a.ld_dresidual = c.norm.ld_dresidual;
-    a.rows = c.norm.rows;
-    a.cols = c.norm.cols;
-    a.vec = a.cols % kGranule == 0 && granule_aligned(d_dy, a.ld_dy, kType) && granule_aligned(d_dh, a.ld_dh, kType) && granule_aligned(d_h, a.ld_h, kType) &&
-            granule_aligned(d_dx, a.ld_dx, kType) && granule_aligned(d_dresidual, a.ld_dresidual, kType);
-    a.fmt = c.fmt;
+    a.rows = s.rows;
+    a.cols = s.cols;
     a.inverse = 1.0f / (float)a.cols;
+    a.fmt = c.fmt;
     a.drop = c.drop;
     a.quant = c.quant;
     a.stats = d_stats;
