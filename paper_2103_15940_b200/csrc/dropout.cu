@@ -16,35 +16,65 @@ constexpr int kDropThreads = 256;
 
 template <int kType>
 struct DropArgs {
-    Source<kType> x, residual;  // residual.p may be NULL
+    Source<kType> x, residual;
     Target<kType> out;
     int64_t cols;
-    uint32_t granules;  // per row
-    uint64_t total;     // rows * granules
+    uint32_t granules;    // per row
+    uint64_t total;       // rows * granules
+    uint32_t step_rows, step_granules;  // the grid's threads as whole rows and granules beyond them
     DropParams drop;
 };
 
-template <int kType>
+// A thread takes granules a grid's width apart, kAhead of them at a time.  kPlain: every granule whole and aligned.
+template <int kType, bool kResidual, bool kPlain>
 __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropArgs<kType> a) {
+    constexpr int kAhead = !kPlain ? 1 : (kType == QFMT_F32) + kResidual == 2 ? 2 : 4;
     grid_launch_dependents();
     grid_dependency_wait();
     const uint64_t offset = drop_offset(a.drop);
     const int lane = threadIdx.x & 31;
     const uint64_t step = (uint64_t)gridDim.x * kDropThreads;
-    for (uint64_t base = (uint64_t)blockIdx.x * kDropThreads; base < a.total; base += step) {  // whole warps
-        const uint64_t i = base + threadIdx.x;
-        const uint64_t row = i / a.granules;
-        const uint32_t g = (uint32_t)(i - row * a.granules);
-        const int64_t col = (int64_t)g * kGranule;
-        const int n = i < a.total ? (int)(a.cols - col < kGranule ? a.cols - col : kGranule) : 0;
-        Granule v = widen_raw<kType>(load_any<kType>(a.x.p + row * a.x.ld + col, n, a.x));
-        if (a.drop.active) drop_granule(a.drop, offset, (uint32_t)row, g, v);
-        if (a.residual.p != nullptr) {
-            const Granule r = widen_raw<kType>(load_any<kType>(a.residual.p + row * a.residual.ld + col, n, a.residual));
+    uint64_t at = (uint64_t)blockIdx.x * kDropThreads + threadIdx.x;
+    uint32_t row = (uint32_t)(at / a.granules), g = (uint32_t)(at - (uint64_t)row * a.granules);
+    for (; at - lane < a.total; at += kAhead * step) {  // whole warps
+        Raw<kType> x[kAhead], r[kAhead];
+        uint32_t rows[kAhead], gs[kAhead];
+        int n[kAhead];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v.p[j] = add2(r.p[j], v.p[j]);
+        for (int i = 0; i < kAhead; ++i) {
+            rows[i] = row;
+            gs[i] = g;
+            const int64_t col = (int64_t)g * kGranule, left = a.cols - col;
+            n[i] = at + i * step < a.total ? (kPlain || left > kGranule ? kGranule : (int)left) : 0;
+            const auto* px = a.x.p + row * a.x.ld + col;
+            if constexpr (kPlain) x[i] = load_raw<kType>(px, n[i] > 0);
+            else x[i] = load_any<kType>(px, n[i], a.x);
+            if constexpr (kResidual) {
+                const auto* pr = a.residual.p + row * a.residual.ld + col;
+                if constexpr (kPlain) r[i] = load_raw<kType>(pr, n[i] > 0);
+                else r[i] = load_any<kType>(pr, n[i], a.residual);
+            }
+            row += a.step_rows;
+            g += a.step_granules;
+            if (g >= a.granules) {
+                g -= a.granules;
+                ++row;
+            }
         }
-        store_any<kType>(a.out.p + row * a.out.ld + col, n, a.out, finish<kType>(v), lane != 0 && g != 0, lane != 31 && g + 1 < a.granules);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (kPlain && n[i] == 0) continue;
+            Granule v = widen_raw<kType>(x[i]);
+            if (a.drop.active) drop_granule(a.drop, offset, rows[i], gs[i], v);
+            if constexpr (kResidual) {
+                const Granule u = widen_raw<kType>(r[i]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v.p[j] = add2(u.p[j], v.p[j]);
+            }
+            auto* po = a.out.p + rows[i] * a.out.ld + (int64_t)gs[i] * kGranule;
+            if constexpr (kPlain) store_raw<kType>(po, finish<kType>(v));
+            else store_any<kType>(po, n[i], a.out, finish<kType>(v), lane != 0 && gs[i] != 0, lane != 31 && gs[i] + 1 < a.granules);
+        }
     }
 }
 
@@ -59,9 +89,15 @@ int launch_dropout(const void* d_x, int64_t ld_x, const void* d_residual, int64_
     a.granules = (uint32_t)((cols + kGranule - 1) / kGranule);
     a.total = (uint64_t)rows * a.granules;
     a.drop = drop;
-    const uint64_t blocks = (a.total + kDropThreads - 1) / kDropThreads;
-    const uint64_t cap = (uint64_t)dev.sm_count * 16;
-    QFMT_CUDA_TRY(launch_overlapping(dropout_kernel<kType>, (unsigned)(blocks < cap ? blocks : cap), kDropThreads, 0, stream, a));
+    const uint64_t want = (a.total + kDropThreads - 1) / kDropThreads, cap = (uint64_t)dev.sm_count * 8;
+    const unsigned blocks = (unsigned)(want < cap ? want : cap);
+    const uint64_t threads = (uint64_t)blocks * kDropThreads;
+    a.step_rows = (uint32_t)(threads / a.granules);
+    a.step_granules = (uint32_t)(threads % a.granules);
+    const bool plain = cols % kGranule == 0 && a.x.whole && a.residual.whole && a.out.whole;
+    const auto kern = d_residual != nullptr ? (plain ? dropout_kernel<kType, true, true> : dropout_kernel<kType, true, false>)
+                                            : (plain ? dropout_kernel<kType, false, true> : dropout_kernel<kType, false, false>);
+    QFMT_CUDA_TRY(launch_overlapping(kern, blocks, kDropThreads, 0, stream, a));
     return QFMT_OK;
 }
 
