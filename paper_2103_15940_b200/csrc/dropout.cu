@@ -19,61 +19,60 @@ struct DropArgs {
     Source<kType> x, residual;
     Target<kType> out;
     int64_t cols;
-    uint32_t granules;    // per row
-    uint64_t total;       // rows * granules
-    uint32_t step_rows, step_granules;  // the grid's threads as whole rows and granules beyond them
+    uint32_t rows, granules;  // per row
+    uint32_t step;            // rows from a thread's granule to its next one
+    uint32_t turns;           // granules of a thread down the rows
+    int64_t step_x, step_residual, step_out;  // the same step in elements
     DropParams drop;
 };
 
-// A thread takes granules a grid's width apart, kAhead of them at a time.  kPlain: every granule whole and aligned.
+// A thread keeps its granule of columns and walks down the rows, so that the first round of the generator and half of
+// the second are the same all the way; kAhead granules are loaded at a time.  kPlain: every granule whole and aligned.
 template <int kType, bool kResidual, bool kPlain>
 __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropArgs<kType> a) {
-    constexpr int kAhead = !kPlain ? 1 : (kType == QFMT_F32) + kResidual == 2 ? 2 : 4;
+    constexpr int kAhead = !kPlain || (kType == QFMT_F32 && kResidual) ? 2 : 4;
     grid_launch_dependents();
     grid_dependency_wait();
     const uint64_t offset = drop_offset(a.drop);
+    const uint32_t threads = gridDim.x * kDropThreads, id = blockIdx.x * kDropThreads + threadIdx.x;
     const int lane = threadIdx.x & 31;
-    const uint64_t step = (uint64_t)gridDim.x * kDropThreads;
-    uint64_t at = (uint64_t)blockIdx.x * kDropThreads + threadIdx.x;
-    uint32_t row = (uint32_t)(at / a.granules), g = (uint32_t)(at - (uint64_t)row * a.granules);
-    for (; at - lane < a.total; at += kAhead * step) {  // whole warps
-        Raw<kType> x[kAhead], r[kAhead];
-        uint32_t rows[kAhead], gs[kAhead];
-        int n[kAhead];
+    const uint32_t row0 = id / a.granules, g0 = id - row0 * a.granules;
+    for (uint32_t g = g0; g - g0 < a.granules; g += threads) {  // once, unless a row is longer than the grid
+        const int64_t col = (int64_t)g * kGranule, left = a.cols - col;
+        const int columns = row0 >= a.step || left <= 0 ? 0 : kPlain || left > kGranule ? kGranule : (int)left;
+        const auto* px = a.x.p + row0 * a.x.ld + col;
+        const auto* pr = a.residual.p + row0 * a.residual.ld + col;
+        auto* po = a.out.p + row0 * a.out.ld + col;
+        uint32_t row = row0;
+        for (uint32_t turn = 0; turn < a.turns; turn += kAhead) {  // whole warps
+            Raw<kType> x[kAhead], r[kAhead];
+            int n[kAhead];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            rows[i] = row;
-            gs[i] = g;
-            const int64_t col = (int64_t)g * kGranule, left = a.cols - col;
-            n[i] = at + i * step < a.total ? (kPlain || left > kGranule ? kGranule : (int)left) : 0;
-            const auto* px = a.x.p + row * a.x.ld + col;
-            if constexpr (kPlain) x[i] = load_raw<kType>(px, n[i] > 0);
-            else x[i] = load_any<kType>(px, n[i], a.x);
-            if constexpr (kResidual) {
-                const auto* pr = a.residual.p + row * a.residual.ld + col;
-                if constexpr (kPlain) r[i] = load_raw<kType>(pr, n[i] > 0);
-                else r[i] = load_any<kType>(pr, n[i], a.residual);
+            for (int i = 0; i < kAhead; ++i) {
+                n[i] = row + i * a.step < a.rows ? columns : 0;
+                if constexpr (kPlain) x[i] = load_raw<kType>(px, n[i] > 0);
+                else x[i] = load_any<kType>(px, n[i], a.x);
+                px += a.step_x;
+                if constexpr (kResidual) {
+                    if constexpr (kPlain) r[i] = load_raw<kType>(pr, n[i] > 0);
+                    else r[i] = load_any<kType>(pr, n[i], a.residual);
+                    pr += a.step_residual;
+                }
             }
-            row += a.step_rows;
-            g += a.step_granules;
-            if (g >= a.granules) {
-                g -= a.granules;
-                ++row;
-            }
-        }
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            if (kPlain && n[i] == 0) continue;
-            Granule v = widen_raw<kType>(x[i]);
-            if (a.drop.active) drop_granule(a.drop, offset, rows[i], gs[i], v);
-            if constexpr (kResidual) {
-                const Granule u = widen_raw<kType>(r[i]);
+            for (int i = 0; i < kAhead; ++i) {
+                Granule v = widen_raw<kType>(x[i]);
+                if (a.drop.active) drop_granule(a.drop, offset, row, g, v);
+                if constexpr (kResidual) {
+                    const Granule u = widen_raw<kType>(r[i]);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v.p[j] = add2(u.p[j], v.p[j]);
+                    for (int j = 0; j < 4; ++j) v.p[j] = add2(u.p[j], v.p[j]);
+                }
+                if constexpr (!kPlain) store_any<kType>(po, n[i], a.out, finish<kType>(v), lane != 0 && g != 0, lane != 31 && g + 1 < a.granules);
+                else if (n[i] > 0) store_raw<kType>(po, finish<kType>(v));
+                po += a.step_out;
+                row += a.step;
             }
-            auto* po = a.out.p + rows[i] * a.out.ld + (int64_t)gs[i] * kGranule;
-            if constexpr (kPlain) store_raw<kType>(po, finish<kType>(v));
-            else store_any<kType>(po, n[i], a.out, finish<kType>(v), lane != 0 && gs[i] != 0, lane != 31 && gs[i] + 1 < a.granules);
         }
     }
 }
@@ -86,17 +85,27 @@ int launch_dropout(const void* d_x, int64_t ld_x, const void* d_residual, int64_
     a.residual = make_source<kType>(d_residual, ld_residual, rows, cols);
     a.out = make_target<kType>(d_out, ld_out);
     a.cols = cols;
+    a.rows = (uint32_t)rows;
     a.granules = (uint32_t)((cols + kGranule - 1) / kGranule);
-    a.total = (uint64_t)rows * a.granules;
     a.drop = drop;
-    const uint64_t want = (a.total + kDropThreads - 1) / kDropThreads, cap = (uint64_t)dev.sm_count * 8;
-    const unsigned blocks = (unsigned)(want < cap ? want : cap);
-    const uint64_t threads = (uint64_t)blocks * kDropThreads;
-    a.step_rows = (uint32_t)(threads / a.granules);
-    a.step_granules = (uint32_t)(threads % a.granules);
     const bool plain = cols % kGranule == 0 && a.x.whole && a.residual.whole && a.out.whole;
-    const auto kern = d_residual != nullptr ? (plain ? dropout_kernel<kType, true, true> : dropout_kernel<kType, true, false>)
-                                            : (plain ? dropout_kernel<kType, false, true> : dropout_kernel<kType, false, false>);
+    const int variant = 2 * (d_residual != nullptr) + plain;
+    const auto kern = variant == 3   ? dropout_kernel<kType, true, true>
+                      : variant == 2 ? dropout_kernel<kType, true, false>
+                      : variant == 1 ? dropout_kernel<kType, false, true>
+                                     : dropout_kernel<kType, false, false>;
+    static std::atomic<int> known[4][kDropThreads / 32 + 1];
+    int resident = 0;
+    const int rc = resident_blocks(kern, kDropThreads, 0, known[variant], &resident);
+    if (rc != QFMT_OK) return rc;
+    const uint64_t want = ((uint64_t)rows * a.granules + kDropThreads - 1) / kDropThreads, cap = (uint64_t)dev.sm_count * resident;
+    const unsigned blocks = (unsigned)(want < cap ? want : cap);
+    const uint32_t step = blocks * kDropThreads / a.granules;
+    a.step = step > 0 ? step : 1;
+    a.turns = (a.rows + a.step - 1) / a.step;
+    a.step_x = a.step * ld_x;
+    a.step_residual = a.step * ld_residual;
+    a.step_out = a.step * ld_out;
     QFMT_CUDA_TRY(launch_overlapping(kern, blocks, kDropThreads, 0, stream, a));
     return QFMT_OK;
 }

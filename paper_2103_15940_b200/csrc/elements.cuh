@@ -10,6 +10,9 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
+#include "common.cuh"
 #include "qfmt.h"
 #include "round.cuh"
 
@@ -329,27 +332,25 @@ __device__ __forceinline__ Raw<kType> finish_format(const Granule& v, int n, con
     return r;
 }
 
-// Philox4x32-10 (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3", SC 2011): ten
-// rounds of two 32 x 32 -> 64-bit products on a counter of four words under a key of two.
-__device__ __forceinline__ uint4 philox4x32_10(uint4 c, uint32_t k0, uint32_t k1) {
-#pragma unroll
-    for (int r = 0; r < 10; ++r) {
-        const uint64_t a = (uint64_t)c.x * 0xD2511F53u, b = (uint64_t)c.z * 0xCD9E8D57u;
-        c = make_uint4((uint32_t)(b >> 32) ^ c.y ^ k0, (uint32_t)b, (uint32_t)(a >> 32) ^ c.w ^ k1, (uint32_t)a);
-        k0 += 0x9E3779B9u;
-        k1 += 0xBB67AE85u;
-    }
-    return c;
-}
-
 struct DropParams {
     uint32_t active;  // 0: nothing is dropped
     uint32_t limit;   // 65536 t - 1: 16 random bits, moved to the top of a word, at or below this drop their element
     float scale;      // 65536 / (65536 - t): the mean is kept exactly for the threshold in use
-    uint32_t key0, key1;
+    uint32_t key[10][2];  // of every round
     uint64_t offset;
     const uint64_t* d_offset;  // added to offset when the kernel runs, or NULL
 };
+
+// Philox4x32-10 (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3", SC 2011): ten
+// rounds of two 32 x 32 -> 64-bit products on a counter of four words, each with its key.
+__device__ __forceinline__ uint4 philox4x32_10(uint4 c, const DropParams& d) {
+#pragma unroll
+    for (int r = 0; r < 10; ++r) {
+        const uint64_t a = (uint64_t)c.x * 0xD2511F53u, b = (uint64_t)c.z * 0xCD9E8D57u;
+        c = make_uint4((uint32_t)(b >> 32) ^ c.y ^ d.key[r][0], (uint32_t)b, (uint32_t)(a >> 32) ^ c.w ^ d.key[r][1], (uint32_t)a);
+    }
+    return c;
+}
 
 __device__ __forceinline__ uint64_t drop_offset(const DropParams& d) {
     return d.offset + (d.d_offset != nullptr ? *d.d_offset : 0ull);
@@ -359,7 +360,7 @@ __device__ __forceinline__ uint64_t drop_offset(const DropParams& d) {
 // selection, not a product: inf and NaN do not get through).  The upper half of a random word is compared in
 // place (its lower half cannot reach the limit's ones), the lower half after a shift.
 __device__ __forceinline__ void drop_granule(const DropParams& d, uint64_t offset, uint32_t row, uint32_t granule, Granule& v) {
-    const uint4 r = philox4x32_10(make_uint4(granule, row, (uint32_t)offset, (uint32_t)(offset >> 32)), d.key0, d.key1);
+    const uint4 r = philox4x32_10(make_uint4(granule, row, (uint32_t)offset, (uint32_t)(offset >> 32)), d);
     const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -412,10 +413,26 @@ inline int make_drop_params(const qfmt_dropout_t* d, DropParams* out) {
     out->active = t != 0u;
     out->limit = (t << 16) - 1u;  // t = 65536: all ones, which nothing exceeds
     out->scale = t < 65536u ? (float)(65536.0 / (65536.0 - (double)t)) : 0.0f;
-    out->key0 = (uint32_t)d->seed;
-    out->key1 = (uint32_t)(d->seed >> 32);
+    for (int r = 0; r < 10; ++r) {
+        out->key[r][0] = (uint32_t)d->seed + (uint32_t)r * 0x9E3779B9u;
+        out->key[r][1] = (uint32_t)(d->seed >> 32) + (uint32_t)r * 0xBB67AE85u;
+    }
     out->offset = d->offset;
     out->d_offset = d->d_offset;
+    return QFMT_OK;
+}
+
+// Blocks of a kernel that an SM holds at once; asked for once per block size.
+template <typename K>
+int resident_blocks(K kernel, unsigned block, size_t smem, std::atomic<int>* known, int* out) {
+    std::atomic<int>& slot = known[block / 32];
+    if (smem == 0 && slot.load() > 0) {
+        *out = slot.load();
+        return QFMT_OK;
+    }
+    QFMT_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(out, kernel, (int)block, smem));
+    if (*out < 1) *out = 1;
+    if (smem == 0) slot.store(*out);
     return QFMT_OK;
 }
 

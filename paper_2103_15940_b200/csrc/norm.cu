@@ -733,20 +733,6 @@ Plan make_plan(int64_t cols, int least, int most) {
 Plan forward_plan(int64_t cols) { return make_plan(cols, 2, 4); }
 Plan backward_plan(int64_t cols) { return make_plan(cols, 1, 2); }
 
-// Blocks of a kernel that an SM holds at once; asked for once per block size.
-template <typename K>
-int resident_blocks(K kernel, unsigned block, size_t smem, std::atomic<int>* known, int* out) {
-    std::atomic<int>& slot = known[block / 32];
-    if (smem == 0 && slot.load() > 0) {
-        *out = slot.load();
-        return QFMT_OK;
-    }
-    QFMT_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(out, kernel, (int)block, smem));
-    if (*out < 1) *out = 1;
-    if (smem == 0) slot.store(*out);
-    return QFMT_OK;
-}
-
 // Parts that the backward pass leaves for the gradients of weight and bias: one per block of the rows kernel,
 // which has a block on each of a B200's SMs, or a share of the rows for long rows.
 constexpr int kMaxParts = 148;
