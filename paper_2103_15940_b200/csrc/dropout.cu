@@ -20,58 +20,57 @@ struct DropArgs {
     Target<kType> out;
     int64_t cols;
     uint32_t rows, granules;  // per row
-    uint32_t step;            // rows from a thread's granule to its next one
-    uint32_t turns;           // granules of a thread down the rows
+    uint32_t turns;           // granules that a thread takes one after the other ...
+    uint32_t step;            // ... this many rows apart, or in rows longer than the grid this many granules
     int64_t step_x, step_residual, step_out;  // the same step in elements
     DropParams drop;
 };
 
-// A thread keeps its granule of columns and walks down the rows, so that the first round of the generator and half of
-// the second are the same all the way; kAhead granules are loaded at a time.  kPlain: every granule whole and aligned.
-template <int kType, bool kResidual, bool kPlain>
+// kDown: a thread keeps its granule of columns and walks down the rows, so that the first round of the generator and
+// half of the second are the same all the way.  Otherwise (rows longer than the grid, a flat tensor) it walks along
+// one row after the other.  kAhead granules are loaded at a time.  kPlain: every granule whole and aligned.
+template <int kType, bool kResidual, bool kDown, bool kPlain>
 __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropArgs<kType> a) {
     constexpr int kAhead = !kPlain || (kType == QFMT_F32 && kResidual) ? 2 : 4;
     grid_launch_dependents();
     grid_dependency_wait();
     const uint64_t offset = drop_offset(a.drop);
-    const uint32_t threads = gridDim.x * kDropThreads, id = blockIdx.x * kDropThreads + threadIdx.x;
+    const uint32_t id = blockIdx.x * kDropThreads + threadIdx.x;
     const int lane = threadIdx.x & 31;
-    const uint32_t row0 = id / a.granules, g0 = id - row0 * a.granules;
-    for (uint32_t g = g0; g - g0 < a.granules; g += threads) {  // once, unless a row is longer than the grid
-        const int64_t col = (int64_t)g * kGranule, left = a.cols - col;
-        const int columns = row0 >= a.step || left <= 0 ? 0 : kPlain || left > kGranule ? kGranule : (int)left;
-        const auto* px = a.x.p + row0 * a.x.ld + col;
-        const auto* pr = a.residual.p + row0 * a.residual.ld + col;
-        auto* po = a.out.p + row0 * a.out.ld + col;
-        uint32_t row = row0;
+    uint32_t row = kDown ? id / a.granules : 0u;
+    const uint32_t g0 = id - row * a.granules;
+    const bool mine = !kDown || row < a.step;
+    for (uint32_t first = 0; first < (kDown ? 1u : a.rows); ++first, row = first) {
+        uint32_t g = g0;
+        const auto* px = a.x.p + row * a.x.ld + (int64_t)g * kGranule;
+        const auto* pr = a.residual.p + row * a.residual.ld + (int64_t)g * kGranule;
+        auto* po = a.out.p + row * a.out.ld + (int64_t)g * kGranule;
         for (uint32_t turn = 0; turn < a.turns; turn += kAhead) {  // whole warps
-            Raw<kType> x[kAhead], r[kAhead];
+            OnItsWay<kType, kPlain> x[kAhead], r[kAhead];
             int n[kAhead];
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                n[i] = row + i * a.step < a.rows ? columns : 0;
-                if constexpr (kPlain) x[i] = load_raw<kType>(px, n[i] > 0);
-                else x[i] = load_any<kType>(px, n[i], a.x);
-                px += a.step_x;
-                if constexpr (kResidual) {
-                    if constexpr (kPlain) r[i] = load_raw<kType>(pr, n[i] > 0);
-                    else r[i] = load_any<kType>(pr, n[i], a.residual);
-                    pr += a.step_residual;
-                }
+                const uint32_t at_row = kDown ? row + i * a.step : row, at_g = kDown ? g : g + i * a.step;
+                const int64_t left = a.cols - (int64_t)at_g * kGranule;
+                n[i] = !mine || at_row >= a.rows || left <= 0 ? 0 : kPlain || left > kGranule ? kGranule : (int)left;
+                x[i] = start<kType, kPlain>(px + i * a.step_x, n[i], a.x);
+                if (kResidual) r[i] = start<kType, kPlain>(pr + i * a.step_residual, n[i], a.residual);
             }
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                Granule v = widen_raw<kType>(x[i]);
+                Granule v = widen_raw<kType>(words<kType, kPlain>(x[i], px, n[i], a.x));
                 if (a.drop.active) drop_granule(a.drop, offset, row, g, v);
                 if constexpr (kResidual) {
-                    const Granule u = widen_raw<kType>(r[i]);
+                    const Granule u = widen_raw<kType>(words<kType, kPlain>(r[i], pr, n[i], a.residual));
 #pragma unroll
                     for (int j = 0; j < 4; ++j) v.p[j] = add2(u.p[j], v.p[j]);
                 }
-                if constexpr (!kPlain) store_any<kType>(po, n[i], a.out, finish<kType>(v), lane != 0 && g != 0, lane != 31 && g + 1 < a.granules);
-                else if (n[i] > 0) store_raw<kType>(po, finish<kType>(v));
+                put<kType, kPlain>(po, n[i], a.out, finish<kType>(v), lane != 0 && g != 0, lane != 31 && g + 1 < a.granules);
+                px += a.step_x;
+                pr += a.step_residual;
                 po += a.step_out;
-                row += a.step;
+                if (kDown) row += a.step;
+                else g += a.step;
             }
         }
     }
@@ -89,24 +88,26 @@ int launch_dropout(const void* d_x, int64_t ld_x, const void* d_residual, int64_
     a.granules = (uint32_t)((cols + kGranule - 1) / kGranule);
     a.drop = drop;
     const bool plain = cols % kGranule == 0 && a.x.whole && a.residual.whole && a.out.whole;
-    const int variant = 2 * (d_residual != nullptr) + plain;
-    const auto kern = variant == 3   ? dropout_kernel<kType, true, true>
-                      : variant == 2 ? dropout_kernel<kType, true, false>
-                      : variant == 1 ? dropout_kernel<kType, false, true>
-                                     : dropout_kernel<kType, false, false>;
-    static std::atomic<int> known[4][kDropThreads / 32 + 1];
+    const bool down = a.granules <= (uint32_t)dev.sm_count * kDropThreads;  // a row is no longer than the smallest grid
+    const int variant = 4 * (d_residual != nullptr) + 2 * down + plain;
+    void (*const kernels[8])(DropArgs<kType>) = {
+        dropout_kernel<kType, false, false, false>, dropout_kernel<kType, false, false, true>,
+        dropout_kernel<kType, false, true, false>,  dropout_kernel<kType, false, true, true>,
+        dropout_kernel<kType, true, false, false>,  dropout_kernel<kType, true, false, true>,
+        dropout_kernel<kType, true, true, false>,   dropout_kernel<kType, true, true, true>};
+    static std::atomic<int> known[8][kDropThreads / 32 + 1];
     int resident = 0;
-    const int rc = resident_blocks(kern, kDropThreads, 0, known[variant], &resident);
+    const int rc = resident_blocks(kernels[variant], kDropThreads, 0, known[variant], &resident);
     if (rc != QFMT_OK) return rc;
     const uint64_t want = ((uint64_t)rows * a.granules + kDropThreads - 1) / kDropThreads, cap = (uint64_t)dev.sm_count * resident;
     const unsigned blocks = (unsigned)(want < cap ? want : cap);
-    const uint32_t step = blocks * kDropThreads / a.granules;
-    a.step = step > 0 ? step : 1;
-    a.turns = (a.rows + a.step - 1) / a.step;
-    a.step_x = a.step * ld_x;
-    a.step_residual = a.step * ld_residual;
-    a.step_out = a.step * ld_out;
-    QFMT_CUDA_TRY(launch_overlapping(kern, blocks, kDropThreads, 0, stream, a));
+    const uint32_t threads = blocks * kDropThreads;
+    a.step = down ? threads / a.granules : threads;
+    a.turns = down ? (a.rows + a.step - 1) / a.step : (a.granules + threads - 1) / threads;
+    a.step_x = (int64_t)a.step * (down ? ld_x : kGranule);
+    a.step_residual = (int64_t)a.step * (down ? ld_residual : kGranule);
+    a.step_out = (int64_t)a.step * (down ? ld_out : kGranule);
+    QFMT_CUDA_TRY(launch_overlapping(kernels[variant], blocks, kDropThreads, 0, stream, a));
     return QFMT_OK;
 }
 

@@ -11,6 +11,7 @@
 #include <stdint.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "common.cuh"
 #include "qfmt.h"
@@ -192,39 +193,69 @@ __device__ __forceinline__ Four shifted_words(const uint32_t (&v)[8], int first)
     return {{w[0], w[1], w[2], w[3]}};
 }
 
-// The words of `n` columns (0..8) of a granule at p, the others zero.  A granule that does not start on a boundary is
-// put together from the aligned 16-byte pieces it touches, where those lie inside the matrix (what they hold beyond
-// the row is thrown away); at the matrix's two ends it is read by elements.
+// A granule of any alignment on its way: the aligned 16-byte pieces that hold it.
 template <int kType>
-__device__ __forceinline__ Raw<kType> load_any(const typename Word<kType>::type* p, int n, const Source<kType>& m) {
-    if (m.whole && n == kGranule) return load_raw<kType>(p);
-    constexpr int kPer = kType == QFMT_F32 ? 4 : 8, kPieces = kType == QFMT_F32 ? 3 : 2;
-    Raw<kType> r;
-    const uint32_t first = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15u) / (16 / kPer);
-    const auto* base = p - first;
-    if (n > 0 && base >= m.p && base + kPieces * kPer <= m.last) {
-        uint32_t w[kPieces * 4];
+struct Pieces {
+    uint32_t w[kType == QFMT_F32 ? 12 : 8];
+};
+
+// Starts to load `n` columns (0..8) of a granule at p: loads under a predicate, nothing waits and nothing branches.
+// What the pieces hold beyond the row is thrown away later; a granule whose pieces reach beyond the matrix (at its two
+// ends only) is left to arrive().
+template <int kType>
+__device__ __forceinline__ bool inside(const typename Word<kType>::type* p, int n, const Source<kType>& m, const typename Word<kType>::type*& base,
+                                       int& pieces) {
+    constexpr int kPer = kType == QFMT_F32 ? 4 : 8;
+    const int first = (int)(reinterpret_cast<uintptr_t>(p) & 15u) / (16 / kPer);
+    base = p - first;
+    pieces = (first + n + kPer - 1) / kPer;
+    return n > 0 && base >= m.p && base + pieces * kPer <= m.last;
+}
+template <int kType>
+__device__ __forceinline__ Pieces<kType> start_any(const typename Word<kType>::type* p, int n, const Source<kType>& m) {
+    constexpr int kPer = kType == QFMT_F32 ? 4 : 8;
+    Pieces<kType> r;
+    const typename Word<kType>::type* base;
+    int pieces;
+    const bool ok = inside<kType>(p, n, m, base, pieces);
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i)
-            asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];"
-                         : "=r"(w[4 * i]), "=r"(w[4 * i + 1]), "=r"(w[4 * i + 2]), "=r"(w[4 * i + 3]) : "l"(base + i * kPer));
-        r = shifted<kType>(w, first);
-        if (n < kGranule) {
+    for (int i = 0; i < (int)(sizeof(r.w) / 16); ++i) {
 #pragma unroll
-            for (int i = 0; i < (int)(sizeof(r.w) / 4); ++i) {
-                if (kType == QFMT_F32) r.w[i] = i < n ? r.w[i] : 0u;
-                else r.w[i] = 2 * i + 1 < n ? r.w[i] : 2 * i < n ? r.w[i] & 0xFFFFu : 0u;
-            }
-        }
-    } else {
+        for (int j = 0; j < 4; ++j) r.w[4 * i + j] = 0u;
+        asm volatile("{ .reg .pred q; setp.ne.u32 q, %5, 0; @q ld.global.v4.b32 {%0,%1,%2,%3}, [%4]; }"
+                     : "+r"(r.w[4 * i]), "+r"(r.w[4 * i + 1]), "+r"(r.w[4 * i + 2]), "+r"(r.w[4 * i + 3])
+                     : "l"(base + i * kPer), "r"((uint32_t)(ok && i < pieces)));
+    }
+    return r;
+}
+// Its words, zero where there is no column.
+template <int kType>
+__device__ __forceinline__ Raw<kType> arrive(Pieces<kType>& q, const typename Word<kType>::type* p, int n, const Source<kType>& m) {
+    constexpr int kPer = kType == QFMT_F32 ? 4 : 8;
+    const typename Word<kType>::type* base;
+    int pieces;
+    const bool ok = inside<kType>(p, n, m, base, pieces);
+    Raw<kType> r = shifted<kType>(q.w, (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15u) / (16 / kPer));
+    if (n > 0 && !ok) {
 #pragma unroll
         for (int j = 0; j < kGranule; ++j) {
             const uint32_t w = j < n ? (uint32_t)p[j] : 0u;
             if constexpr (kType == QFMT_F32) r.w[j] = w;
             else r.w[j / 2] = j & 1 ? r.w[j / 2] | (w << 16) : w;
         }
+    } else if (n < kGranule) {
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(r.w) / 4); ++i) {
+            if (kType == QFMT_F32) r.w[i] = i < n ? r.w[i] : 0u;
+            else r.w[i] = 2 * i + 1 < n ? r.w[i] : 2 * i < n ? r.w[i] & 0xFFFFu : 0u;
+        }
     }
     return r;
+}
+template <int kType>
+__device__ __forceinline__ Raw<kType> load_any(const typename Word<kType>::type* p, int n, const Source<kType>& m) {
+    Pieces<kType> q = start_any<kType>(p, n, m);
+    return arrive<kType>(q, p, n, m);
 }
 
 // Writes `n` columns (0..8) of a granule at p.  Called by whole warps.  `from` and `to`: the lane before this one holds
@@ -330,6 +361,29 @@ __device__ __forceinline__ Raw<kType> finish_format(const Granule& v, int n, con
             if (j < n) atomicAdd(&hist[bin[j] * 32 + lane], 1u);
     }
     return r;
+}
+
+// A granule of n columns at p on its way, and its words, zeros where there are none.  kPlain: whole and aligned, or
+// not there at all.
+template <int kType, bool kPlain>
+using OnItsWay = std::conditional_t<kPlain, Raw<kType>, Pieces<kType>>;
+template <int kType, bool kPlain>
+__device__ __forceinline__ OnItsWay<kType, kPlain> start(const typename Word<kType>::type* p, int n, const Source<kType>& m) {
+    if constexpr (kPlain) return load_raw<kType>(p, n > 0);
+    else return start_any<kType>(p, n, m);
+}
+template <int kType, bool kPlain>
+__device__ __forceinline__ Raw<kType> words(OnItsWay<kType, kPlain>& q, const typename Word<kType>::type* p, int n, const Source<kType>& m) {
+    if constexpr (kPlain) return q;
+    else return arrive<kType>(q, p, n, m);
+}
+template <int kType, bool kPlain>
+__device__ __forceinline__ void put(typename Word<kType>::type* p, int n, const Target<kType>& m, const Raw<kType>& r, bool from, bool to) {
+    if constexpr (kPlain) {
+        if (n > 0) store_raw<kType>(p, r);
+    } else {
+        store_any<kType>(p, n, m, r, from, to);
+    }
 }
 
 struct DropParams {

@@ -77,21 +77,6 @@ __device__ __forceinline__ Granule load_columns(const float* p, int64_t g, int n
     return v;
 }
 
-// A granule of n columns at p, zeros where there are none.  kPlain: whole and aligned, or not there at all.
-template <int kType, bool kPlain>
-__device__ __forceinline__ Raw<kType> fetch(const typename Word<kType>::type* p, int n, const Source<kType>& m) {
-    if constexpr (kPlain) return load_raw<kType>(p, n > 0);
-    else return load_any<kType>(p, n, m);
-}
-template <int kType, bool kPlain>
-__device__ __forceinline__ void put(typename Word<kType>::type* p, int n, const Target<kType>& m, const Raw<kType>& r, bool from, bool to) {
-    if constexpr (kPlain) {
-        if (n > 0) store_raw<kType>(p, r);
-    } else {
-        store_any<kType>(p, n, m, r, from, to);
-    }
-}
-
 // residual + D(x)
 template <int kType, bool kFused>
 __device__ __forceinline__ Granule join_h(const ForwardArgs<kType>& a, const Raw<kType>& x, const Raw<kType>& r, uint64_t offset, uint32_t row,
@@ -304,19 +289,18 @@ __global__ void __launch_bounds__(kMaxTeam) norm_forward_rows_kernel(const Forwa
     const auto* pr = a.residual.p + row * a.residual.ld + t * kGranule;
     auto* ph = a.h.p + row * a.h.ld + t * kGranule;
     auto* py = a.y.p + row * a.y.ld + t * kGranule;
-    Raw<kType> x[R][V], r[R][V];
+    OnItsWay<kType, kPlain> x[R][V], r[R][V];
     const auto fetch_rows = [&](uint32_t at) {
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             const bool there = at + i < rows;
 #pragma unroll
             for (int k = 0; k < V; ++k) {
-                x[i][k] = fetch<kType, kPlain>(px + i * a.x.ld + k * next, there ? n[k] : 0, a.x);
-                if (kFused) r[i][k] = fetch<kType, kPlain>(pr + i * a.residual.ld + k * next, there && residual ? n[k] : 0, a.residual);
+                x[i][k] = start<kType, kPlain>(px + i * a.x.ld + k * next, there ? n[k] : 0, a.x);
+                if (kFused) r[i][k] = start<kType, kPlain>(pr + i * a.residual.ld + k * next, there && residual ? n[k] : 0, a.residual);
             }
         }
-        px += step.x;
-        pr += step.residual;
+        if (kAhead) px += step.x, pr += step.residual;
     };
     if (kAhead) fetch_rows(row);
     Granule w[kKeep ? V : 1], b[kKeep ? V : 1];
@@ -334,8 +318,15 @@ __global__ void __launch_bounds__(kMaxTeam) norm_forward_rows_kernel(const Forwa
 #pragma unroll
         for (int i = 0; i < R; ++i)
 #pragma unroll
-            for (int k = 0; k < V; ++k) v[i][k] = join_h<kType, kFused>(a, x[i][k], r[i][k], offset, row + i, k * team + t);
+            for (int k = 0; k < V; ++k) {
+                const int there = row + i < rows ? n[k] : 0;
+                const Raw<kType> xs = words<kType, kPlain>(x[i][k], px + i * a.x.ld + k * next, there, a.x);
+                const Raw<kType> rs = kFused ? words<kType, kPlain>(r[i][k], pr + i * a.residual.ld + k * next, residual ? there : 0, a.residual)
+                                             : Raw<kType>();
+                v[i][k] = join_h<kType, kFused>(a, xs, rs, offset, row + i, k * team + t);
+            }
         if (kAhead) fetch_rows(row + stride);
+        else px += step.x, pr += step.residual;
         if (kFused && a.h.p != nullptr) {
 #pragma unroll
             for (int i = 0; i < R; ++i)
@@ -443,7 +434,9 @@ __device__ __forceinline__ void store_gradients(const BackwardArgs<kType>& a, co
         d.p[j] = mul2(fma2(xhat.p[j], both(-c2), fma2(dy.p[j], w.p[j], both(-c1))), both(rstd));
     if constexpr (kFused) {
         if (a.dh.p != nullptr) {
-            const Granule more = widen_raw<kType>(fetch<kType, kPlain>(to.dh + i * a.dh.ld + at, n, a.dh));
+            const auto* p = to.dh + i * a.dh.ld + at;
+            OnItsWay<kType, kPlain> q = start<kType, kPlain>(p, n, a.dh);
+            const Granule more = widen_raw<kType>(words<kType, kPlain>(q, p, n, a.dh));
 #pragma unroll
             for (int j = 0; j < 4; ++j) d.p[j] = add2(d.p[j], more.p[j]);
         }
@@ -587,7 +580,7 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, const BackwardS
     const auto* pdy = a.dy.p + row * a.dy.ld + t * kGranule;
     const auto* ph = a.h.p + row * a.h.ld + t * kGranule;
     GradientRow<kType> to(a, row, t * kGranule);
-    Raw<kType> raw_dy[R][V], raw_h[R][V];
+    OnItsWay<kType, kPlain> raw_dy[R][V], raw_h[R][V];
     float mean[R], rstd[R];
     const auto fetch_rows = [&](uint32_t at) {
 #pragma unroll
@@ -597,12 +590,11 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, const BackwardS
             rstd[i] = there ? __ldg(a.rstd + at + i) : 0.0f;
 #pragma unroll
             for (int k = 0; k < V; ++k) {
-                raw_dy[i][k] = fetch<kType, kPlain>(pdy + i * a.dy.ld + k * next, there ? n[k] : 0, a.dy);
-                raw_h[i][k] = fetch<kType, kPlain>(ph + i * a.h.ld + k * next, there ? n[k] : 0, a.h);
+                raw_dy[i][k] = start<kType, kPlain>(pdy + i * a.dy.ld + k * next, there ? n[k] : 0, a.dy);
+                raw_h[i][k] = start<kType, kPlain>(ph + i * a.h.ld + k * next, there ? n[k] : 0, a.h);
             }
         }
-        pdy += step.dy;
-        ph += step.h;
+        if (kAhead) pdy += step.dy, ph += step.h;
     };
     if (kAhead) fetch_rows(row);
 #pragma unroll
@@ -618,8 +610,10 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, const BackwardS
             this_rstd[i] = rstd[i];
 #pragma unroll
             for (int k = 0; k < V; ++k) {
-                dy[i][k] = widen_raw<kType>(raw_dy[i][k]);
-                xhat[i][k] = normalise<kPlain>(widen_raw<kType>(raw_h[i][k]), mean[i], rstd[i], row + i < rows ? n[k] : 0);
+                const int there = row + i < rows ? n[k] : 0;
+                dy[i][k] = widen_raw<kType>(words<kType, kPlain>(raw_dy[i][k], pdy + i * a.dy.ld + k * next, there, a.dy));
+                xhat[i][k] = normalise<kPlain>(widen_raw<kType>(words<kType, kPlain>(raw_h[i][k], ph + i * a.h.ld + k * next, there, a.h)),
+                                               mean[i], rstd[i], there);
                 const float2 q = row_sums(dy[i][k], xhat[i][k], w[k]);
                 s[i] = k == 0 ? q : add2(s[i], q);
 #pragma unroll
@@ -630,6 +624,7 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, const BackwardS
             }
         }
         if (kAhead) fetch_rows(row + stride);
+        else pdy += step.dy, ph += step.h;
         if constexpr (kParts) {
             for (int off = team >> 1; off > 0; off >>= 1) {
 #pragma unroll
