@@ -158,13 +158,15 @@ __device__ __forceinline__ uint32_t word_of(const Raw<kType>& r, int j) {
 
 // A granule's words from element `first` of w on; the elements are 32 or 16 bits wide.
 template <int kType, int kFrom>
-__device__ __forceinline__ Raw<kType> shifted(uint32_t (&w)[kFrom], uint32_t first) {
+__device__ __forceinline__ Raw<kType> shifted(const uint32_t (&v)[kFrom], uint32_t first) {
     Raw<kType> r;
     constexpr int kWords = sizeof(r.w) / 4;
-    uint32_t word = kType == QFMT_F32 ? first : first >> 1;
+    uint32_t w[kFrom];
 #pragma unroll
-    for (int by = 4; by > 0; by /= 2) {
-        if (by + kWords > kFrom) continue;  // no shift that far is asked for
+    for (int i = 0; i < kFrom; ++i) w[i] = v[i];
+    const uint32_t word = kType == QFMT_F32 ? first : first >> 1;
+#pragma unroll
+    for (int by = (kFrom - kWords) / 2; by > 0; by /= 2) {  // a shift by less than kFrom - kWords words is asked for
         const bool on = word & by;
 #pragma unroll
         for (int i = 0; i + by < kFrom; ++i) w[i] = on ? w[i + by] : w[i];
@@ -177,7 +179,7 @@ __device__ __forceinline__ Raw<kType> shifted(uint32_t (&w)[kFrom], uint32_t fir
     return r;
 }
 
-// Four words of w from word `first` (0..4) on.
+// Four words of w from word `first` (0..3) on.
 struct Four {
     uint32_t w[4];
 };
@@ -186,7 +188,7 @@ __device__ __forceinline__ Four shifted_words(const uint32_t (&v)[8], int first)
 #pragma unroll
     for (int i = 0; i < 8; ++i) w[i] = v[i];
 #pragma unroll
-    for (int by = 4; by > 0; by /= 2) {
+    for (int by = 2; by > 0; by /= 2) {
 #pragma unroll
         for (int i = 0; i + by < 8; ++i) w[i] = first & by ? w[i + by] : w[i];
     }
@@ -197,65 +199,52 @@ __device__ __forceinline__ Four shifted_words(const uint32_t (&v)[8], int first)
 template <int kType>
 struct Pieces {
     uint32_t w[kType == QFMT_F32 ? 12 : 8];
+    bool inside;  // they lie in the matrix
 };
 
 // Starts to load `n` columns (0..8) of a granule at p: loads under a predicate, nothing waits and nothing branches.
-// What the pieces hold beyond the row is thrown away later; a granule whose pieces reach beyond the matrix (at its two
-// ends only) is left to arrive().
-template <int kType>
-__device__ __forceinline__ bool inside(const typename Word<kType>::type* p, int n, const Source<kType>& m, const typename Word<kType>::type*& base,
-                                       int& pieces) {
-    constexpr int kPer = kType == QFMT_F32 ? 4 : 8;
-    const int first = (int)(reinterpret_cast<uintptr_t>(p) & 15u) / (16 / kPer);
-    base = p - first;
-    pieces = (first + n + kPer - 1) / kPer;
-    return n > 0 && base >= m.p && base + pieces * kPer <= m.last;
-}
+// What the pieces hold beyond the columns is thrown away later; a granule whose pieces reach beyond the matrix (at its
+// two ends only) is left to arrive().
 template <int kType>
 __device__ __forceinline__ Pieces<kType> start_any(const typename Word<kType>::type* p, int n, const Source<kType>& m) {
     constexpr int kPer = kType == QFMT_F32 ? 4 : 8;
     Pieces<kType> r;
-    const typename Word<kType>::type* base;
-    int pieces;
-    const bool ok = inside<kType>(p, n, m, base, pieces);
+    const int first = (int)(reinterpret_cast<uintptr_t>(p) & 15u) / (16 / kPer);
+    const auto* base = p - first;
+    const int pieces = (first + n + kPer - 1) / kPer;
+    r.inside = n > 0 && base >= m.p && base + pieces * kPer <= m.last;
 #pragma unroll
-    for (int i = 0; i < (int)(sizeof(r.w) / 16); ++i) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) r.w[4 * i + j] = 0u;
+    for (int i = 0; i < (int)(sizeof(r.w) / 16); ++i)
         asm volatile("{ .reg .pred q; setp.ne.u32 q, %5, 0; @q ld.global.v4.b32 {%0,%1,%2,%3}, [%4]; }"
-                     : "+r"(r.w[4 * i]), "+r"(r.w[4 * i + 1]), "+r"(r.w[4 * i + 2]), "+r"(r.w[4 * i + 3])
-                     : "l"(base + i * kPer), "r"((uint32_t)(ok && i < pieces)));
-    }
+                     : "=r"(r.w[4 * i]), "=r"(r.w[4 * i + 1]), "=r"(r.w[4 * i + 2]), "=r"(r.w[4 * i + 3])
+                     : "l"(base + i * kPer), "r"((uint32_t)(r.inside && i < pieces)));
     return r;
 }
 // Its words, zero where there is no column.
 template <int kType>
-__device__ __forceinline__ Raw<kType> arrive(Pieces<kType>& q, const typename Word<kType>::type* p, int n, const Source<kType>& m) {
+__device__ __forceinline__ Raw<kType> arrive(const Pieces<kType>& q, const typename Word<kType>::type* p, int n, const Source<kType>& m) {
     constexpr int kPer = kType == QFMT_F32 ? 4 : 8;
-    const typename Word<kType>::type* base;
-    int pieces;
-    const bool ok = inside<kType>(p, n, m, base, pieces);
-    Raw<kType> r = shifted<kType>(q.w, (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15u) / (16 / kPer));
-    if (n > 0 && !ok) {
+    const uint32_t first = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15u) / (16 / kPer);
+    Raw<kType> r;
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(r.w) / 4); ++i) r.w[i] = q.w[i];
+    if (first != 0) r = shifted<kType>(q.w, first);
+    if (n != kGranule || !q.inside) {
+        const bool read = n > 0 && !q.inside;
 #pragma unroll
         for (int j = 0; j < kGranule; ++j) {
-            const uint32_t w = j < n ? (uint32_t)p[j] : 0u;
+            uint32_t w = word_of<kType>(r, j);
+            if (read && j < n) w = (uint32_t)p[j];
+            if (j >= n) w = 0u;
             if constexpr (kType == QFMT_F32) r.w[j] = w;
-            else r.w[j / 2] = j & 1 ? r.w[j / 2] | (w << 16) : w;
-        }
-    } else if (n < kGranule) {
-#pragma unroll
-        for (int i = 0; i < (int)(sizeof(r.w) / 4); ++i) {
-            if (kType == QFMT_F32) r.w[i] = i < n ? r.w[i] : 0u;
-            else r.w[i] = 2 * i + 1 < n ? r.w[i] : 2 * i < n ? r.w[i] & 0xFFFFu : 0u;
+            else r.w[j / 2] = j & 1 ? (r.w[j / 2] & 0xFFFFu) | (w << 16) : (r.w[j / 2] & 0xFFFF0000u) | w;
         }
     }
     return r;
 }
 template <int kType>
 __device__ __forceinline__ Raw<kType> load_any(const typename Word<kType>::type* p, int n, const Source<kType>& m) {
-    Pieces<kType> q = start_any<kType>(p, n, m);
-    return arrive<kType>(q, p, n, m);
+    return arrive<kType>(start_any<kType>(p, n, m), p, n, m);
 }
 
 // Writes `n` columns (0..8) of a granule at p.  Called by whole warps.  `from` and `to`: the lane before this one holds
@@ -266,58 +255,50 @@ template <int kType>
 __device__ __forceinline__ void store_any(typename Word<kType>::type* p, int n, const Target<kType>& m, const Raw<kType>& r, bool from,
                                           bool to) {
     constexpr int kPer = kType == QFMT_F32 ? 4 : 8;
-    bool head = false, body = false, tail = false;  // parts that an aligned piece covers
-    int first = kPer;                               // elements before the first piece that begins here
+    uint32_t left = (1u << n) - 1u;  // columns that no aligned piece covers
     if (m.whole) {
-        if (n == kGranule) store_raw<kType>(p, r);
-        head = n == kGranule;
-        first = kGranule;
+        if (n == kGranule) {
+            store_raw<kType>(p, r);
+            left = 0u;
+        }
     } else {
-        uint32_t w[8];
         const int following = __shfl_down_sync(0xFFFFFFFFu, n, 1);
-        if constexpr (kType == QFMT_F32) {
+        uint32_t w[8];  // the last 16 bytes of this granule and the first 16 of the next
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                w[i] = r.w[4 + i];
-                w[4 + i] = __shfl_down_sync(0xFFFFFFFFu, r.w[i], 1);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                w[i] = r.w[i];
-                w[4 + i] = __shfl_down_sync(0xFFFFFFFFu, r.w[i], 1);
-            }
+        for (int i = 0; i < 4; ++i) {
+            w[i] = r.w[kType == QFMT_F32 ? 4 + i : i];
+            w[4 + i] = __shfl_down_sync(0xFFFFFFFFu, r.w[i], 1);
         }
         const int skew = (int)(reinterpret_cast<uintptr_t>(p) & 15u) / (16 / kPer);
-        first = (kPer - skew) & (kPer - 1);
-        head = first == 0 || (from && n >= first);
-        tail = skew != 0 && to && following >= first;
+        const int first = (kPer - skew) & (kPer - 1);  // columns before the first piece that begins here
+        const uint32_t before = (1u << first) - 1u;
+        if (from && n >= first) left &= ~before;
+        const bool full = n == kGranule;
+        const bool last = skew != 0 ? to && following >= first : full;  // the piece that may need the next lane's words
+        Four q;
         if constexpr (kType == QFMT_F32) {
-            body = n == kGranule;
-            if (body) {  // the piece in the middle is all this lane's
-                uint32_t own[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) own[i] = r.w[i];
-                const Four q = shifted_words(own, first);
+            if (full) {  // a piece in the middle is all this lane's
+                const uint32_t own[8] = {r.w[0], r.w[1], r.w[2], r.w[3], r.w[4], r.w[5], r.w[6], r.w[7]};
+                q = shifted_words(own, first);
                 asm volatile("st.global.v4.b32 [%0], {%1,%2,%3,%4};" ::"l"(p + first), "r"(q.w[0]), "r"(q.w[1]), "r"(q.w[2]), "r"(q.w[3]) : "memory");
+                left &= ~(0xFu << first);
             }
-            if (first == 0) tail = body;
-            if (tail) {
-                const Four q = shifted_words(w, first);
-                asm volatile("st.global.v4.b32 [%0], {%1,%2,%3,%4};" ::"l"(p + first + 4), "r"(q.w[0]), "r"(q.w[1]), "r"(q.w[2]), "r"(q.w[3]) : "memory");
-            }
+            q = shifted_words(w, first);
         } else {
-            if (first == 0) tail = n == kGranule;
-            if (tail) {
-                const Raw<kType> q = shifted<kType>(w, first);
-                asm volatile("st.global.v4.b32 [%0], {%1,%2,%3,%4};" ::"l"(p + first), "r"(q.w[0]), "r"(q.w[1]), "r"(q.w[2]), "r"(q.w[3]) : "memory");
-            }
+            const Raw<kType> s = shifted<kType>(w, first);
+            q = {{s.w[0], s.w[1], s.w[2], s.w[3]}};
+        }
+        if (last) {
+            constexpr int kMiddle = kType == QFMT_F32 ? 4 : 0;
+            asm volatile("st.global.v4.b32 [%0], {%1,%2,%3,%4};" ::"l"(p + first + kMiddle), "r"(q.w[0]), "r"(q.w[1]), "r"(q.w[2]), "r"(q.w[3]) : "memory");
+            left &= (1u << (first + kMiddle)) - 1u;
         }
     }
-    const int second = kType == QFMT_F32 ? first + 4 : first;
+    if (left != 0u) {
 #pragma unroll
-    for (int j = 0; j < kGranule; ++j)
-        if (j < n && !(j < first ? head : j < second ? body : tail)) p[j] = (typename Word<kType>::type)word_of<kType>(r, j);
+        for (int j = 0; j < kGranule; ++j)
+            if (left >> j & 1u) p[j] = (typename Word<kType>::type)word_of<kType>(r, j);
+    }
 }
 
 // Eight finished values to words, rounded once to the storage type (nearest, ties to even).
@@ -373,7 +354,7 @@ __device__ __forceinline__ OnItsWay<kType, kPlain> start(const typename Word<kTy
     else return start_any<kType>(p, n, m);
 }
 template <int kType, bool kPlain>
-__device__ __forceinline__ Raw<kType> words(OnItsWay<kType, kPlain>& q, const typename Word<kType>::type* p, int n, const Source<kType>& m) {
+__device__ __forceinline__ Raw<kType> words(const OnItsWay<kType, kPlain>& q, const typename Word<kType>::type* p, int n, const Source<kType>& m) {
     if constexpr (kPlain) return q;
     else return arrive<kType>(q, p, n, m);
 }
