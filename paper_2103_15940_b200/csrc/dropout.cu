@@ -31,7 +31,7 @@ struct DropArgs {
 // one row after the other.  kAhead granules are loaded at a time.  kPlain: every granule whole and aligned.
 template <int kType, bool kResidual, bool kDown, bool kPlain>
 __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropArgs<kType> a) {
-    constexpr int kAhead = !kPlain || (kType == QFMT_F32 && kResidual) ? 2 : 4;
+    constexpr int kAhead = !kPlain ? 1 : kType == QFMT_F32 && kResidual ? 2 : 4;
     grid_launch_dependents();
     grid_dependency_wait();
     const uint64_t offset = drop_offset(a.drop);

@@ -547,11 +547,12 @@ __device__ __forceinline__ void team_sums(float2 (&s)[R], int team, int t, int b
 // The backward pass of rows that a team holds in registers, R at a time: dy and h are read once, the sums over rows
 // stay in the registers of the thread that owns their columns from row to row, and a block leaves one part.
 // kParts: a team is a part of a warp (or all of it), otherwise whole warps; a block has 512 threads' worth of teams.
-// kPlain as in the forward pass; the next rows are then on their way while these are worked on.
+// kPlain as in the forward pass.  With registers to spare (kAhead) the next rows are on their way while these are
+// worked on.  A team takes `group` neighbouring rows (R, or R = 1 at a time), then the group that is a step away.
 template <int kType, int V, int R, bool kParts, bool kFused, bool kPlain>
 __global__ void __launch_bounds__(kMaxTeam)
-norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, const BackwardSteps step, int hist_words) {
-    constexpr bool kAhead = kPlain && V == 1;
+norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, const BackwardSteps step, int hist_words) {
+    constexpr bool kAhead = V == 1 || (kPlain && kType != QFMT_F32);
     extern __shared__ __align__(16) uint32_t dynamic[];  // [hist_words] histogram, then the sums of the block's teams
     __shared__ __align__(16) float scratch[kParts ? 1 : kMaxTeam / 64][2][64];
     grid_launch_dependents();
@@ -575,8 +576,8 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, const BackwardS
         n[k] = granule_columns(a.cols, k * team + t);
         dw[k] = db[k] = splat(0.0f);
     }
-    const uint32_t rows = (uint32_t)a.rows, stride = gridDim.x * teams * R;
-    uint32_t row = (blockIdx.x * teams + mine) * R;
+    const uint32_t rows = (uint32_t)a.rows, stride = gridDim.x * teams * group;
+    uint32_t row = (blockIdx.x * teams + mine) * group;
     const auto* pdy = a.dy.p + row * a.dy.ld + t * kGranule;
     const auto* ph = a.h.p + row * a.h.ld + t * kGranule;
     GradientRow<kType> to(a, row, t * kGranule);
@@ -594,13 +595,16 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, const BackwardS
                 raw_h[i][k] = start<kType, kPlain>(ph + i * a.h.ld + k * next, there ? n[k] : 0, a.h);
             }
         }
-        if (kAhead) pdy += step.dy, ph += step.h;
     };
+    // rows to the next one: a step, or with R = 1 one row within a group
+    const bool pairs = R == 1 && group == 2;
+    const auto advance = [&](bool second, auto*& p, int64_t ld, int64_t by) { p += pairs ? (second ? by - ld : ld) : by; };
     if (kAhead) fetch_rows(row);
 #pragma unroll
     for (int k = 0; k < V; ++k) w[k] = load_columns(a.weight, k * team + t, n[k], 1.0f);
     int parity = 0;
-    for (; row - mine * R < rows; row += stride, parity ^= 1) {
+    bool second = false;
+    for (uint32_t first = blockIdx.x * teams * group; first < rows; parity ^= 1) {  // the row of the block's first team
         if (!kAhead) fetch_rows(row);
         Granule dy[R][V], xhat[R][V];
         float2 s[R];
@@ -623,8 +627,10 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, const BackwardS
                 }
             }
         }
-        if (kAhead) fetch_rows(row + stride);
-        else pdy += step.dy, ph += step.h;
+        const uint32_t by = pairs ? (second ? stride - 1 : 1) : stride;
+        advance(second, pdy, a.dy.ld, step.dy);
+        advance(second, ph, a.h.ld, step.h);
+        if (kAhead) fetch_rows(row + by);
         if constexpr (kParts) {
             for (int off = team >> 1; off > 0; off >>= 1) {
 #pragma unroll
@@ -641,9 +647,12 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, const BackwardS
                 store_gradients<kType, kFused, kPlain>(a, to, i, k * next, dy[i][k], xhat[i][k], w[k], this_rstd[i], c1, c2, row + i,
                                                        k * team + t, row + i < rows ? n[k] : 0, from, after, offset, hist);
         }
-        to.dh += step.dh;
-        to.dx += step.dx;
-        to.dresidual += step.dresidual;
+        advance(second, to.dh, a.dh.ld, step.dh);
+        advance(second, to.dx, a.dx.ld, step.dx);
+        advance(second, to.dresidual, a.dresidual.ld, step.dresidual);
+        row += by;
+        first += by;
+        second = pairs && !second;
     }
     if (hist != nullptr) flush_hist(hist, a.quant, a.stats, (uint64_t)a.rows * (uint64_t)a.cols);
     if (a.partial == nullptr) return;
@@ -880,13 +889,9 @@ int join_parts(const float* partial, int parts, int64_t cols, float* d_dweight, 
 }
 
 template <int kType, int V, int R, bool kParts, bool kFused, bool kPlain>
-int launch_backward_rows(const Call& c, const BackwardArgs<kType>& a, int team, float* d_dweight, float* d_dbias, cudaStream_t stream) {
+int launch_backward_rows(const Call& c, const BackwardArgs<kType>& a, int team, int group, float* d_dweight, float* d_dbias, cudaStream_t stream) {
     const unsigned teams = kMaxTeam / team, block = teams * team;
-    const int64_t cap = std::min(c.dev.sm_count, kMaxParts), want = (a.rows + teams * R - 1) / (teams * R);
-    // two rows at a time only where every team has them (a rule on sizes alone: it decides the order of the sums over rows)
-    if constexpr (R == 2) {
-        if (want < cap) return launch_backward_rows<kType, V, 1, kParts, kFused, kPlain>(c, a, team, d_dweight, d_dbias, stream);
-    }
+    const int64_t cap = std::min(c.dev.sm_count, kMaxParts), want = (a.rows + teams * group - 1) / (teams * group);
     const auto kern = norm_backward_rows_kernel<kType, V, R, kParts, kFused, kPlain>;
     const unsigned units = kParts ? block / 32 : teams;
     const size_t smem = c.hist_bytes + (units > 1 ? 2 * sizeof(float) * (size_t)padded_columns(a.cols) * units : 0);
@@ -896,9 +901,9 @@ int launch_backward_rows(const Call& c, const BackwardArgs<kType>& a, int team, 
         if (c.dev.ordinal >= 0 && c.dev.ordinal < 64) allowed[c.dev.ordinal].store(true);
     }
     const unsigned blocks = (unsigned)std::min(want, cap);
-    const int64_t stride = (int64_t)blocks * teams * R;
+    const int64_t stride = (int64_t)blocks * teams * group;
     const BackwardSteps step = {stride * a.dy.ld, stride * a.h.ld, stride * a.dh.ld, stride * a.dx.ld, stride * a.dresidual.ld};
-    QFMT_CUDA_TRY(launch_overlapping(kern, blocks, block, smem, stream, a, team, step, (int)(c.hist_bytes / sizeof(uint32_t))));
+    QFMT_CUDA_TRY(launch_overlapping(kern, blocks, block, smem, stream, a, team, group, step, (int)(c.hist_bytes / sizeof(uint32_t))));
     return a.partial != nullptr ? join_parts(a.partial, (int)blocks, a.cols, d_dweight, d_dbias, stream) : QFMT_OK;
 }
 
@@ -908,13 +913,19 @@ int launch_backward(const Call& c, const BackwardArgs<kType>& a, float* d_dweigh
     const Plan plan = backward_plan(a.cols);
     if (plan.team != 0) {
         const bool plain = plain_layout(a.cols, {a.dy.whole, a.dh.whole, a.h.whole, a.dx.whole, a.dresidual.whole}) && !a.fmt;
+        // Two neighbouring rows to a team where every team gets some: a rule on sizes alone, since it decides the order
+        // of the sums over rows.  Whether the two are worked on at once does not.
+        const int64_t teams = (int64_t)(kMaxTeam / plan.team) * std::min(c.dev.sm_count, kMaxParts);
+        const int group = plan.granules == 1 && a.rows > 2 * (teams - 1) ? 2 : 1;
         const auto run = plan.granules == 2 ? (plain ? launch_backward_rows<kType, 2, 1, false, kFused, true>
                                                      : launch_backward_rows<kType, 2, 1, false, kFused, false>)
-                         : plan.team > 32   ? (plain ? launch_backward_rows<kType, 1, 2, false, kFused, true>
-                                                     : launch_backward_rows<kType, 1, 2, false, kFused, false>)
-                                            : (plain ? launch_backward_rows<kType, 1, 2, true, kFused, true>
-                                                     : launch_backward_rows<kType, 1, 2, true, kFused, false>);
-        return run(c, a, plan.team, d_dweight, d_dbias, stream);
+                         : plan.team > 32   ? (!plain       ? launch_backward_rows<kType, 1, 1, false, kFused, false>
+                                               : group == 2 ? launch_backward_rows<kType, 1, 2, false, kFused, true>
+                                                            : launch_backward_rows<kType, 1, 1, false, kFused, true>)
+                                            : (!plain       ? launch_backward_rows<kType, 1, 1, true, kFused, false>
+                                               : group == 2 ? launch_backward_rows<kType, 1, 2, true, kFused, true>
+                                                            : launch_backward_rows<kType, 1, 1, true, kFused, true>);
+        return run(c, a, plan.team, group, d_dweight, d_dbias, stream);
     }
     if (a.partial != nullptr) {  // before the row pass, which may overwrite dy
         const int parts = row_parts(c.norm);
