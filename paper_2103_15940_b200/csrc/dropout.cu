@@ -53,8 +53,8 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropArgs<kT
                 const uint32_t at_row = kDown ? row + i * a.step : row, at_g = kDown ? g : g + i * a.step;
                 const int64_t left = a.cols - (int64_t)at_g * kGranule;
                 n[i] = !mine || at_row >= a.rows || left <= 0 ? 0 : kPlain || left > kGranule ? kGranule : (int)left;
-                x[i] = start<kType, kPlain>(px + i * a.step_x, n[i], a.x);
-                if (kResidual) r[i] = start<kType, kPlain>(pr + i * a.step_residual, n[i], a.residual);
+                x[i] = start<kType, kPlain>(px + i * a.step_x, n[i], 0, 1, a.x);
+                if (kResidual) r[i] = start<kType, kPlain>(pr + i * a.step_residual, n[i], 0, 1, a.residual);
             }
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {

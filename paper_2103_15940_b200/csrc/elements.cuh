@@ -50,21 +50,23 @@ struct Raw {
     uint32_t w[kType == QFMT_F32 ? 8 : 4];
 };
 
-// A whole granule, or zeros where `there` is false (a predicate on the load, not a branch around it).
+// A whole granule where it is there (n > 0) and its row is one (row < rows), zeros elsewhere.  A predicate on the load,
+// not a branch around it.
 template <int kType>
-__device__ __forceinline__ Raw<kType> load_raw(const typename Word<kType>::type* p, bool there = true) {
+__device__ __forceinline__ Raw<kType> load_raw(const typename Word<kType>::type* p, int n, uint32_t row, uint32_t rows) {
     Raw<kType> r;
 #pragma unroll
     for (uint32_t& w : r.w) w = 0u;
     if constexpr (kType == QFMT_F32) {
-        asm volatile("{ .reg .pred q; setp.ne.u32 q, %9, 0;"
+        asm volatile("{ .reg .pred q, s; setp.lt.u32 s, %10, %11; setp.ne.and.s32 q, %9, 0, s;"
                      " @q ld.global.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8]; }"
                      : "+r"(r.w[0]), "+r"(r.w[1]), "+r"(r.w[2]), "+r"(r.w[3]), "+r"(r.w[4]), "+r"(r.w[5]), "+r"(r.w[6]),
                        "+r"(r.w[7])
-                     : "l"(p), "r"((uint32_t)there));
+                     : "l"(p), "r"(n), "r"(row), "r"(rows));
     } else {
-        asm volatile("{ .reg .pred q; setp.ne.u32 q, %5, 0; @q ld.global.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4]; }"
-                     : "+r"(r.w[0]), "+r"(r.w[1]), "+r"(r.w[2]), "+r"(r.w[3]) : "l"(p), "r"((uint32_t)there));
+        asm volatile("{ .reg .pred q, s; setp.lt.u32 s, %6, %7; setp.ne.and.s32 q, %5, 0, s;"
+                     " @q ld.global.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4]; }"
+                     : "+r"(r.w[0]), "+r"(r.w[1]), "+r"(r.w[2]), "+r"(r.w[3]) : "l"(p), "r"(n), "r"(row), "r"(rows));
     }
     return r;
 }
@@ -344,14 +346,15 @@ __device__ __forceinline__ Raw<kType> finish_format(const Granule& v, int n, con
     return r;
 }
 
-// A granule of n columns at p on its way, and its words, zeros where there are none.  kPlain: whole and aligned, or
-// not there at all.
+// A granule of n columns at p, in row `row` of `rows`, on its way, and its words: zeros where there is nothing.
+// kPlain: whole and aligned, or not there at all.
 template <int kType, bool kPlain>
 using OnItsWay = std::conditional_t<kPlain, Raw<kType>, Pieces<kType>>;
 template <int kType, bool kPlain>
-__device__ __forceinline__ OnItsWay<kType, kPlain> start(const typename Word<kType>::type* p, int n, const Source<kType>& m) {
-    if constexpr (kPlain) return load_raw<kType>(p, n > 0);
-    else return start_any<kType>(p, n, m);
+__device__ __forceinline__ OnItsWay<kType, kPlain> start(const typename Word<kType>::type* p, int n, uint32_t row, uint32_t rows,
+                                                         const Source<kType>& m) {
+    if constexpr (kPlain) return load_raw<kType>(p, n, row, rows);
+    else return start_any<kType>(p, row < rows ? n : 0, m);
 }
 template <int kType, bool kPlain>
 __device__ __forceinline__ Raw<kType> words(const OnItsWay<kType, kPlain>& q, const typename Word<kType>::type* p, int n, const Source<kType>& m) {

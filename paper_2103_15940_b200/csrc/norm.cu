@@ -200,54 +200,72 @@ __global__ void __launch_bounds__(kLoopThreads) norm_forward_loop_kernel(const F
 // row is thread t's k-th, k < V.
 constexpr int kMaxTeam = 512;
 
-// Sums over a team, in every thread and in a fixed order: of one value, or of two at once.  kBlock: the team is the
-// block.  scratch: 16 entries, or two times 16, of which those past the team's warps are zero; one barrier, so the
-// next sum needs another scratch.
-__device__ __forceinline__ float sum_entries(const float* scratch, int team) {
-    float s = 0.0f;
-    for (int i = 0; i * 32 < team; i += 4) {
-        const float4 q = *reinterpret_cast<const float4*>(scratch + i);
-        const float u = (q.x + q.y) + (q.z + q.w);
-        s = i == 0 ? u : s + u;
-    }
-    return s;
-}
 __device__ __forceinline__ float across(float s, int off) { return s + __shfl_xor_sync(0xFFFFFFFFu, s, off); }
 
-template <bool kBlock>
-__device__ __forceinline__ float team_sum(float s, int team, int t, float* scratch) {
-    if constexpr (!kBlock) {
-        for (int off = team >> 1; off > 0; off >>= 1) s = across(s, off);
-        return s;
+// What the warps of a team left in scratch, 16 entries for each of kValues values, those past the team's warps zero.
+// Up to four warps every thread adds the entries up; more would be 15 additions a value in every thread, so the lanes
+// of each warp share them (always in the order of the shuffles, whatever kValues is).
+template <int kValues>
+__device__ __forceinline__ void sum_entries(const float* scratch, int team, float (&s)[kValues]) {
+    if (team <= 128) {
+#pragma unroll
+        for (int i = 0; i < kValues; ++i) {
+            const float4 q = *reinterpret_cast<const float4*>(scratch + 16 * i);
+            s[i] = (q.x + q.y) + (q.z + q.w);
+        }
+        return;
+    }
+    const int lane = threadIdx.x & 31;
+    constexpr int kLanes = kValues == 4 ? 8 : 16;  // that share a value
+    const int value = lane / kLanes % kValues;
+    float u = scratch[16 * value + lane % kLanes];
+    if (kLanes == 8) u += scratch[16 * value + 8 + lane % 8];
+    else u = across(u, 8);
+#pragma unroll
+    for (int off = 4; off > 0; off >>= 1) u = across(u, off);
+    if constexpr (kValues == 1) {
+        s[0] = u;
     } else {
 #pragma unroll
-        for (int off = 16; off > 0; off >>= 1) s = across(s, off);
-        if (team == 32) return s;
-        if ((t & 31) == 0) scratch[t >> 5] = s;
-        __syncthreads();
-        return sum_entries(scratch, team);
+        for (int i = 0; i < kValues; ++i) s[i] = __shfl_sync(0xFFFFFFFFu, u, i * kLanes);
     }
 }
 
+// Sums over a team, in every thread and in a fixed order: of one value, or of two at once.  kBlock: the team is the
+// block.  One barrier, so the next sum needs another scratch.
+template <bool kBlock>
+__device__ __forceinline__ void team_sum(float (&s)[1], int team, int t, float* scratch) {
+    if constexpr (!kBlock) {
+        for (int off = team >> 1; off > 0; off >>= 1) s[0] = across(s[0], off);
+    } else {
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) s[0] = across(s[0], off);
+        if (team == 32) return;
+        if ((t & 31) == 0) scratch[t >> 5] = s[0];
+        __syncthreads();
+        sum_entries<1>(scratch, team, s);
+    }
+}
 // Two values: after one exchange the lower half of a warp holds the first value's partial sums and the upper half
 // the second's, so five shuffles do for both.
 template <bool kBlock>
-__device__ __forceinline__ float2 team_sum(float2 s, int team, int t, float* scratch) {
+__device__ __forceinline__ void team_sum(float (&s)[2], int team, int t, float* scratch) {
     if constexpr (!kBlock) {
-        for (int off = team >> 1; off > 0; off >>= 1) s = make_float2(across(s.x, off), across(s.y, off));
-        return s;
+        for (int off = team >> 1; off > 0; off >>= 1) s[0] = across(s[0], off), s[1] = across(s[1], off);
     } else {
         const bool upper = t & 16;
-        float u = (upper ? s.y : s.x) + __shfl_xor_sync(0xFFFFFFFFu, upper ? s.x : s.y, 16);
+        float u = (upper ? s[1] : s[0]) + __shfl_xor_sync(0xFFFFFFFFu, upper ? s[0] : s[1], 16);
 #pragma unroll
         for (int off = 8; off > 0; off >>= 1) u = across(u, off);
         if (team == 32) {
             const float v = __shfl_xor_sync(0xFFFFFFFFu, u, 16);
-            return upper ? make_float2(v, u) : make_float2(u, v);
+            s[0] = upper ? v : u;
+            s[1] = upper ? u : v;
+            return;
         }
         if ((t & 15) == 0) scratch[(t & 16) + (t >> 5)] = u;
         __syncthreads();
-        return make_float2(sum_entries(scratch, team), sum_entries(scratch + 16, team));
+        sum_entries<2>(scratch, team, s);
     }
 }
 
@@ -293,11 +311,10 @@ __global__ void __launch_bounds__(kMaxTeam) norm_forward_rows_kernel(const Forwa
     const auto fetch_rows = [&](uint32_t at) {
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            const bool there = at + i < rows;
 #pragma unroll
             for (int k = 0; k < V; ++k) {
-                x[i][k] = start<kType, kPlain>(px + i * a.x.ld + k * next, there ? n[k] : 0, a.x);
-                if (kFused) r[i][k] = start<kType, kPlain>(pr + i * a.residual.ld + k * next, there && residual ? n[k] : 0, a.residual);
+                x[i][k] = start<kType, kPlain>(px + i * a.x.ld + k * next, n[k], at + i, rows, a.x);
+                if (kFused) r[i][k] = start<kType, kPlain>(pr + i * a.residual.ld + k * next, residual ? n[k] : 0, at + i, rows, a.residual);
             }
         }
         if (kAhead) px += step.x, pr += step.residual;
@@ -314,7 +331,7 @@ __global__ void __launch_bounds__(kMaxTeam) norm_forward_rows_kernel(const Forwa
     for (; row - mine * R < rows; row += stride) {
         if (!kAhead) fetch_rows(row);
         Granule v[R][V];
-        float s[R] = {}, mean[R], rstd[R];
+        float mean[R], rstd[R];
 #pragma unroll
         for (int i = 0; i < R; ++i)
 #pragma unroll
@@ -334,32 +351,24 @@ __global__ void __launch_bounds__(kMaxTeam) norm_forward_rows_kernel(const Forwa
                 for (int k = 0; k < V; ++k)
                     put<kType, kPlain>(ph + i * a.h.ld + k * next, row + i < rows ? n[k] : 0, a.h, finish<kType>(v[i][k]), from, to);
         }
-        const auto total = [&](float (&out)[R], float* space) {
-            if constexpr (R == 2) {
-                const float2 q = team_sum<(V > 1)>(make_float2(s[0], s[1]), team, t, space);
-                out[0] = q.x * a.inverse;
-                out[1] = q.y * a.inverse;
-            } else {
-                out[0] = team_sum<(V > 1)>(s[0], team, t, space) * a.inverse;
-            }
-        };
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            s[i] = sum8(v[i][0]);
+            mean[i] = sum8(v[i][0]);
 #pragma unroll
-            for (int k = 1; k < V; ++k) s[i] += sum8(v[i][k]);
+            for (int k = 1; k < V; ++k) mean[i] += sum8(v[i][k]);
         }
-        total(mean, scratch[0][0]);
+        team_sum<(V > 1)>(mean, team, t, scratch[0][0]);
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            s[i] = centre<kPlain>(v[i][0], mean[i], n[0]);
+            mean[i] *= a.inverse;
+            rstd[i] = centre<kPlain>(v[i][0], mean[i], n[0]);
 #pragma unroll
-            for (int k = 1; k < V; ++k) s[i] += centre<kPlain>(v[i][k], mean[i], n[k]);
+            for (int k = 1; k < V; ++k) rstd[i] += centre<kPlain>(v[i][k], mean[i], n[k]);
         }
-        total(rstd, scratch[1][0]);
+        team_sum<(V > 1)>(rstd, team, t, scratch[1][0]);
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            rstd[i] = inverse_root(rstd[i] + a.eps);
+            rstd[i] = inverse_root(rstd[i] * a.inverse + a.eps);
             if (t == 0 && row + i < rows) {
                 if (a.mean != nullptr) a.mean[row + i] = mean[i];
                 if (a.rstd != nullptr) a.rstd[row + i] = rstd[i];
@@ -435,7 +444,7 @@ __device__ __forceinline__ void store_gradients(const BackwardArgs<kType>& a, co
     if constexpr (kFused) {
         if (a.dh.p != nullptr) {
             const auto* p = to.dh + i * a.dh.ld + at;
-            OnItsWay<kType, kPlain> q = start<kType, kPlain>(p, n, a.dh);
+            const OnItsWay<kType, kPlain> q = start<kType, kPlain>(p, n, 0, 1, a.dh);
             const Granule more = widen_raw<kType>(words<kType, kPlain>(q, p, n, a.dh));
 #pragma unroll
             for (int j = 0; j < 4; ++j) d.p[j] = add2(d.p[j], more.p[j]);
@@ -525,7 +534,6 @@ struct BackwardSteps {
 
 // Two sums of each of R rows over a team of whole warps that is one of several in its block, in every thread and in
 // a fixed order.  With every exchange a lane gives up half of the values it holds, so six shuffles do for four values.
-// scratch: 16 entries for each of the 2 R values, those past the team's warps zero.
 template <int R>
 __device__ __forceinline__ void team_sums(float2 (&s)[R], int team, int t, int barrier, float* scratch) {
     const bool upper = t & 16, odd = t & 8;
@@ -537,11 +545,13 @@ __device__ __forceinline__ void team_sums(float2 (&s)[R], int team, int t, int b
     else v = across(u[0], 8);
 #pragma unroll
     for (int off = 4; off > 0; off >>= 1) v = across(v, off);
-    // value 0 of row 0, 0 of row 1, 1 of row 0, 1 of row 1 in lanes 0, 8, 16, 24
-    if ((t & 7) == 0 && (R == 2 || !odd)) scratch[(t & 24) * 2 + (t >> 5)] = v;
+    // value 0 of row 0, 0 of row 1, 1 of row 0, 1 of row 1 in lanes 0, 8, 16, 24; with one row in lanes 0 and 16
+    if ((t & 7) == 0 && (R == 2 || !odd)) scratch[(t & 24) * R + (t >> 5)] = v;
     asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(team) : "memory");
+    float total[2 * R];
+    sum_entries<2 * R>(scratch, team, total);
 #pragma unroll
-    for (int i = 0; i < R; ++i) s[i] = make_float2(sum_entries(scratch + 16 * i, team), sum_entries(scratch + 32 + 16 * i, team));
+    for (int i = 0; i < R; ++i) s[i] = make_float2(total[i], total[R + i]);
 }
 
 // The backward pass of rows that a team holds in registers, R at a time: dy and h are read once, the sums over rows
@@ -591,8 +601,8 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
             rstd[i] = there ? __ldg(a.rstd + at + i) : 0.0f;
 #pragma unroll
             for (int k = 0; k < V; ++k) {
-                raw_dy[i][k] = start<kType, kPlain>(pdy + i * a.dy.ld + k * next, there ? n[k] : 0, a.dy);
-                raw_h[i][k] = start<kType, kPlain>(ph + i * a.h.ld + k * next, there ? n[k] : 0, a.h);
+                raw_dy[i][k] = start<kType, kPlain>(pdy + i * a.dy.ld + k * next, n[k], at + i, rows, a.dy);
+                raw_h[i][k] = start<kType, kPlain>(ph + i * a.h.ld + k * next, n[k], at + i, rows, a.h);
             }
         }
     };
@@ -612,14 +622,14 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             this_rstd[i] = rstd[i];
+            s[i] = make_float2(0.0f, 0.0f);
 #pragma unroll
             for (int k = 0; k < V; ++k) {
-                const int there = row + i < rows ? n[k] : 0;
+                const int there = row + i < rows ? n[k] : 0;  // a row that does not exist adds nothing to the column sums
                 dy[i][k] = widen_raw<kType>(words<kType, kPlain>(raw_dy[i][k], pdy + i * a.dy.ld + k * next, there, a.dy));
                 xhat[i][k] = normalise<kPlain>(widen_raw<kType>(words<kType, kPlain>(raw_h[i][k], ph + i * a.h.ld + k * next, there, a.h)),
                                                mean[i], rstd[i], there);
-                const float2 q = row_sums(dy[i][k], xhat[i][k], w[k]);
-                s[i] = k == 0 ? q : add2(s[i], q);
+                s[i] = add2(s[i], row_sums(dy[i][k], xhat[i][k], w[k]));
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     dw[k].p[j] = fma2(dy[i][k].p[j], xhat[i][k].p[j], dw[k].p[j]);
