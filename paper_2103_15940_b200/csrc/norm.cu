@@ -554,16 +554,31 @@ __device__ __forceinline__ void team_sums(float2 (&s)[R], int team, int t, int b
     for (int i = 0; i < R; ++i) s[i] = make_float2(total[i], total[R + i]);
 }
 
+// Column sums of one more row: dweight += dy xhat, dbias += dy.
+__device__ __forceinline__ void add_columns(Granule& dw, Granule& db, const Granule& dy, const Granule& xhat) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        dw.p[j] = fma2(dy.p[j], xhat.p[j], dw.p[j]);
+        db.p[j] = add2(db.p[j], dy.p[j]);
+    }
+}
+__device__ __forceinline__ float4 quad(const Granule& v, int i) { return make_float4(v.p[2 * i].x, v.p[2 * i].y, v.p[2 * i + 1].x, v.p[2 * i + 1].y); }
+__device__ __forceinline__ Granule from_quads(float4 a, float4 b) {
+    return {{make_float2(a.x, a.y), make_float2(a.z, a.w), make_float2(b.x, b.y), make_float2(b.z, b.w)}};
+}
+
 // The backward pass of rows that a team holds in registers, R at a time: dy and h are read once, the sums over rows
 // stay in the registers of the thread that owns their columns from row to row, and a block leaves one part.
 // kParts: a team is a part of a warp (or all of it), otherwise whole warps; a block has 512 threads' worth of teams.
+// V > 1 (wide rows): the team is the block, and the column sums lie in shared memory, each thread's its own, since the
+// registers hold V granules of dy and h; with V = 4 the weight is read from the cache as well.
 // kPlain as in the forward pass.  With registers to spare (kAhead) the next rows are on their way while these are
 // worked on.  A team takes `group` neighbouring rows (R, or R = 1 at a time), then the group that is a step away.
 template <int kType, int V, int R, bool kParts, bool kFused, bool kPlain>
 __global__ void __launch_bounds__(kMaxTeam)
 norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, const BackwardSteps step, int hist_words) {
-    constexpr bool kAhead = V == 1 || (kPlain && kType != QFMT_F32);
-    extern __shared__ __align__(16) uint32_t dynamic[];  // [hist_words] histogram, then the sums of the block's teams
+    constexpr bool kAhead = V == 1 || (V == 2 && kPlain);
+    extern __shared__ __align__(16) uint32_t dynamic[];  // [hist_words] histogram, then the column sums of the block
     __shared__ __align__(16) float scratch[kParts ? 1 : kMaxTeam / 64][2][64];
     grid_launch_dependents();
     grid_dependency_wait();
@@ -574,17 +589,21 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
     }
     if (hist != nullptr) clear_hist(hist, a.quant);
     // (the shuffle tells the compiler that a warp belongs to one team)
-    const int mine = kParts ? threadIdx.x / team : __shfl_sync(0xFFFFFFFFu, threadIdx.x / team, 0);
-    const int t = threadIdx.x - mine * team, teams = blockDim.x / team;
+    const int mine = V > 1 ? 0 : kParts ? threadIdx.x / team : __shfl_sync(0xFFFFFFFFu, threadIdx.x / team, 0);
+    const int t = threadIdx.x - mine * team, teams = V > 1 ? 1 : blockDim.x / team;
     const bool from = (t & 31) != 0, after = (t & 31) != 31 && t + 1 < team;
     const uint64_t offset = kFused ? drop_offset(a.drop) : 0ull;
     const int next = team * kGranule;  // elements between a thread's granules
     int n[V];
-    Granule w[V], dw[V], db[V];
+    Granule w[V < 4 ? V : 1], dw = splat(0.0f), db = splat(0.0f);  // the sums with V = 1
+    float4* const sums_in_shared = reinterpret_cast<float4*>(dynamic + hist_words);  // with V > 1: [V][4][team]
 #pragma unroll
     for (int k = 0; k < V; ++k) {
         n[k] = granule_columns(a.cols, k * team + t);
-        dw[k] = db[k] = splat(0.0f);
+        if (V > 1) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sums_in_shared[(4 * k + i) * team + t] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        }
     }
     const uint32_t rows = (uint32_t)a.rows, stride = gridDim.x * teams * group;
     uint32_t row = (blockIdx.x * teams + mine) * group;
@@ -611,7 +630,7 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
     const auto advance = [&](bool second, auto*& p, int64_t ld, int64_t by) { p += pairs ? (second ? by - ld : ld) : by; };
     if (kAhead) fetch_rows(row);
 #pragma unroll
-    for (int k = 0; k < V; ++k) w[k] = load_columns(a.weight, k * team + t, n[k], 1.0f);
+    for (int k = 0; k < (V < 4 ? V : 0); ++k) w[k] = load_columns(a.weight, k * team + t, n[k], 1.0f);
     int parity = 0;
     bool second = false;
     for (uint32_t first = blockIdx.x * teams * group; first < rows; parity ^= 1) {  // the row of the block's first team
@@ -629,11 +648,15 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
                 dy[i][k] = widen_raw<kType>(words<kType, kPlain>(raw_dy[i][k], pdy + i * a.dy.ld + k * next, there, a.dy));
                 xhat[i][k] = normalise<kPlain>(widen_raw<kType>(words<kType, kPlain>(raw_h[i][k], ph + i * a.h.ld + k * next, there, a.h)),
                                                mean[i], rstd[i], there);
-                s[i] = add2(s[i], row_sums(dy[i][k], xhat[i][k], w[k]));
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    dw[k].p[j] = fma2(dy[i][k].p[j], xhat[i][k].p[j], dw[k].p[j]);
-                    db[k].p[j] = add2(db[k].p[j], dy[i][k].p[j]);
+                if (V == 4) w[0] = load_columns(a.weight, k * team + t, n[k], 1.0f);
+                s[i] = add2(s[i], row_sums(dy[i][k], xhat[i][k], w[V < 4 ? k : 0]));
+                if constexpr (V == 1) {
+                    add_columns(dw, db, dy[i][k], xhat[i][k]);
+                } else {
+                    float4* const q = sums_in_shared + 4 * k * team + t;
+                    Granule u = from_quads(q[0], q[team]), v = from_quads(q[2 * team], q[3 * team]);
+                    add_columns(u, v, dy[i][k], xhat[i][k]);
+                    q[0] = quad(u, 0), q[team] = quad(u, 1), q[2 * team] = quad(v, 0), q[3 * team] = quad(v, 1);
                 }
             }
         }
@@ -653,9 +676,11 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
         for (int i = 0; i < R; ++i) {
             const float c1 = s[i].x * a.inverse, c2 = s[i].y * a.inverse;
 #pragma unroll
-            for (int k = 0; k < V; ++k)
-                store_gradients<kType, kFused, kPlain>(a, to, i, k * next, dy[i][k], xhat[i][k], w[k], this_rstd[i], c1, c2, row + i,
+            for (int k = 0; k < V; ++k) {
+                if (V == 4) w[0] = load_columns(a.weight, k * team + t, n[k], 1.0f);
+                store_gradients<kType, kFused, kPlain>(a, to, i, k * next, dy[i][k], xhat[i][k], w[V < 4 ? k : 0], this_rstd[i], c1, c2, row + i,
                                                        k * team + t, row + i < rows ? n[k] : 0, from, after, offset, hist);
+            }
         }
         advance(second, to.dh, a.dh.ld, step.dh);
         advance(second, to.dx, a.dx.ld, step.dx);
@@ -676,19 +701,22 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
         for (int off = 16; off >= team; off >>= 1) {  // the teams of a warp
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                dw[0].p[j] = make_float2(across(dw[0].p[j].x, off), across(dw[0].p[j].y, off));
-                db[0].p[j] = make_float2(across(db[0].p[j].x, off), across(db[0].p[j].y, off));
+                dw.p[j] = make_float2(across(dw.p[j].x, off), across(dw.p[j].y, off));
+                db.p[j] = make_float2(across(db.p[j].x, off), across(db.p[j].y, off));
             }
         }
     }
 #pragma unroll
     for (int k = 0; k < V; ++k) {
         if ((kParts && (threadIdx.x & 31) >= team) || n[k] == 0) continue;
+        if (V > 1) {
+            const float4* const q = sums_in_shared + 4 * k * team + t;
+            dw = from_quads(q[0], q[team]);
+            db = from_quads(q[2 * team], q[3 * team]);
+        }
         float4* const q = own + (k * team + t) * 2;
-        q[0] = make_float4(dw[k].p[0].x, dw[k].p[0].y, dw[k].p[1].x, dw[k].p[1].y);
-        q[1] = make_float4(dw[k].p[2].x, dw[k].p[2].y, dw[k].p[3].x, dw[k].p[3].y);
-        q[quads / 2] = make_float4(db[k].p[0].x, db[k].p[0].y, db[k].p[1].x, db[k].p[1].y);
-        q[quads / 2 + 1] = make_float4(db[k].p[2].x, db[k].p[2].y, db[k].p[3].x, db[k].p[3].y);
+        q[0] = quad(dw, 0), q[1] = quad(dw, 1);
+        q[quads / 2] = quad(db, 0), q[quads / 2 + 1] = quad(db, 1);
     }
     if (units == 1) return;
     __syncthreads();
@@ -745,7 +773,7 @@ Plan make_plan(int64_t cols, int least, int most) {
     return {0, 0};
 }
 Plan forward_plan(int64_t cols) { return make_plan(cols, 2, 4); }
-Plan backward_plan(int64_t cols) { return make_plan(cols, 1, 2); }
+Plan backward_plan(int64_t cols) { return make_plan(cols, 1, 4); }
 
 // Parts that the backward pass leaves for the gradients of weight and bias: one per block of the rows kernel,
 // which has a block on each of a B200's SMs, or a share of the rows for long rows.
@@ -904,10 +932,12 @@ int launch_backward_rows(const Call& c, const BackwardArgs<kType>& a, int team, 
     const int64_t cap = std::min(c.dev.sm_count, kMaxParts), want = (a.rows + teams * group - 1) / (teams * group);
     const auto kern = norm_backward_rows_kernel<kType, V, R, kParts, kFused, kPlain>;
     const unsigned units = kParts ? block / 32 : teams;
-    const size_t smem = c.hist_bytes + (units > 1 ? 2 * sizeof(float) * (size_t)padded_columns(a.cols) * units : 0);
+    const size_t smem = c.hist_bytes + (V > 1       ? (size_t)block * V * 64
+                                        : units > 1 ? 2 * sizeof(float) * (size_t)padded_columns(a.cols) * units : 0);
     static std::atomic<bool> allowed[64];
     if (c.dev.ordinal < 0 || c.dev.ordinal >= 64 || !allowed[c.dev.ordinal].load()) {
-        QFMT_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 72 * 1024));  // histogram and sums
+        QFMT_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                           (V > 1 ? V * 32 + 40 : 72) * 1024));  // histogram and sums
         if (c.dev.ordinal >= 0 && c.dev.ordinal < 64) allowed[c.dev.ordinal].store(true);
     }
     const unsigned blocks = (unsigned)std::min(want, cap);
@@ -927,8 +957,10 @@ int launch_backward(const Call& c, const BackwardArgs<kType>& a, float* d_dweigh
         // of the sums over rows.  Whether the two are worked on at once does not.
         const int64_t teams = (int64_t)(kMaxTeam / plan.team) * std::min(c.dev.sm_count, kMaxParts);
         const int group = plan.granules == 1 && a.rows > 2 * (teams - 1) ? 2 : 1;
-        const auto run = plan.granules == 2 ? (plain ? launch_backward_rows<kType, 2, 1, false, kFused, true>
-                                                     : launch_backward_rows<kType, 2, 1, false, kFused, false>)
+        const auto run = plan.granules == 4   ? (plain ? launch_backward_rows<kType, 4, 1, false, kFused, true>
+                                                       : launch_backward_rows<kType, 4, 1, false, kFused, false>)
+                         : plan.granules == 2 ? (plain ? launch_backward_rows<kType, 2, 1, false, kFused, true>
+                                                       : launch_backward_rows<kType, 2, 1, false, kFused, false>)
                          : plan.team > 32   ? (!plain       ? launch_backward_rows<kType, 1, 1, false, kFused, false>
                                                : group == 2 ? launch_backward_rows<kType, 1, 2, false, kFused, true>
                                                             : launch_backward_rows<kType, 1, 1, false, kFused, true>)
