@@ -730,29 +730,34 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
     }
 }
 
-// Joins the parts in a fixed order: a block takes 32 columns, its warps every 32nd part.
+// Joins the parts in a fixed order: a block takes 128 columns of dweight and dbias side by side, its warps every 32nd
+// part, four columns a lane.
 constexpr int kJoinWarps = 32;
 __global__ void __launch_bounds__(32 * kJoinWarps)
-norm_join_parts_kernel(const float* partial, int parts, int64_t padded, int64_t cols, float* dweight, float* dbias) {
-    __shared__ float sums[kJoinWarps][33];
+norm_join_parts_kernel(const float4* partial, int parts, int padded, int cols, float* dweight, float* dbias) {
+    __shared__ float4 sums[kJoinWarps][32];
     grid_launch_dependents();
     grid_dependency_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int which = blockIdx.x & 1;
-    const int64_t first = (int64_t)(blockIdx.x >> 1) * 32, c = first + lane;
-    float* const out = which == 0 ? dweight : dbias;
-    if (out == nullptr) return;
-    float s = 0.0f;
-    if (c < cols) {
-#pragma unroll 10
-        for (int k = warp; k < parts; k += kJoinWarps) s += partial[((int64_t)k * 2 + which) * padded + c];
+    const int quads = padded / 2, q = blockIdx.x * 32 + lane;
+    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (q < quads) {
+#pragma unroll 5
+        for (int k = warp; k < parts; k += kJoinWarps) {
+            const float4 v = partial[(int64_t)k * quads + q];
+            s = make_float4(s.x + v.x, s.y + v.y, s.z + v.z, s.w + v.w);
+        }
     }
     sums[warp][lane] = s;
     __syncthreads();
-    s = sums[lane][warp];  // a warp joins one column
+    if (threadIdx.x >= 128) return;
+    float u = 0.0f;
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) s = across(s, off);
-    if (lane == 0 && first + warp < cols) out[first + warp] = s;
+    for (int w = 0; w < kJoinWarps; ++w) u += reinterpret_cast<const float*>(sums[w])[threadIdx.x];
+    int c = blockIdx.x * 128 + threadIdx.x;
+    float* out = dweight;
+    if (c >= padded) c -= padded, out = dbias;
+    if (out != nullptr && c < cols) out[c] = u;
 }
 
 // How a pass runs: the threads that share a row and the granules each of them holds.  The fewest granules a thread
@@ -921,8 +926,9 @@ int forward_entry(const qfmt_norm_t* norm, const qfmt_dropout_t* drop, bool fuse
 int64_t padded_columns(int64_t cols) { return (cols + kGranule - 1) / kGranule * kGranule; }
 
 int join_parts(const float* partial, int parts, int64_t cols, float* d_dweight, float* d_dbias, cudaStream_t stream) {
-    QFMT_CUDA_TRY(launch_overlapping(norm_join_parts_kernel, 2u * (unsigned)((cols + 31) / 32), 32u * kJoinWarps, 0, stream, partial, parts,
-                                     padded_columns(cols), cols, d_dweight, d_dbias));
+    const int64_t padded = padded_columns(cols);
+    QFMT_CUDA_TRY(launch_overlapping(norm_join_parts_kernel, (unsigned)((2 * padded + 127) / 128), 32u * kJoinWarps, 0, stream,
+                                     reinterpret_cast<const float4*>(partial), parts, (int)padded, (int)cols, d_dweight, d_dbias));
     return QFMT_OK;
 }
 
