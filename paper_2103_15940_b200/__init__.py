@@ -183,12 +183,12 @@ def _bind_optional(L: ctypes.CDLL) -> None:
 
 def _ptr(x) -> Optional[int]:
     """Address of a torch tensor / numpy array / int / None."""
-    if x is None:
-        return None
-    if isinstance(x, int):
+    if x is None or type(x) is int:
         return x
     if hasattr(x, "data_ptr"):
         return x.data_ptr()
+    if isinstance(x, int):
+        return x
     if hasattr(x, "ctypes"):
         return x.ctypes.data
     raise TypeError(type(x))

@@ -53,15 +53,16 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropArgs<kT
                 const uint32_t at_row = kDown ? row + i * a.step : row, at_g = kDown ? g : g + i * a.step;
                 const int64_t left = a.cols - (int64_t)at_g * kGranule;
                 n[i] = !mine || at_row >= a.rows || left <= 0 ? 0 : kPlain || left > kGranule ? kGranule : (int)left;
-                x[i] = start<kType, kPlain>(px + i * a.step_x, n[i], 0, 1, a.x);
-                if (kResidual) r[i] = start<kType, kPlain>(pr + i * a.step_residual, n[i], 0, 1, a.residual);
+                const bool edge = at_edge(a.cols, at_g);
+                x[i] = start<kType, kPlain>(px + i * a.step_x, n[i], at_row, a.rows, edge);
+                if (kResidual) r[i] = start<kType, kPlain>(pr + i * a.step_residual, n[i], at_row, a.rows, edge);
             }
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                Granule v = widen_raw<kType>(words<kType, kPlain>(x[i], px, n[i], a.x));
+                Granule v = widen_raw<kType>(words<kType, kPlain>(x[i], px, n[i]));
                 if (a.drop.active) drop_granule(a.drop, offset, row, g, v);
                 if constexpr (kResidual) {
-                    const Granule u = widen_raw<kType>(words<kType, kPlain>(r[i], pr, n[i], a.residual));
+                    const Granule u = widen_raw<kType>(words<kType, kPlain>(r[i], pr, n[i]));
 #pragma unroll
                     for (int j = 0; j < 4; ++j) v.p[j] = add2(u.p[j], v.p[j]);
                 }
@@ -80,8 +81,8 @@ template <int kType>
 int launch_dropout(const void* d_x, int64_t ld_x, const void* d_residual, int64_t ld_residual, void* d_out, int64_t ld_out,
                    int64_t rows, int64_t cols, const DropParams& drop, const DeviceInfo& dev, cudaStream_t stream) {
     DropArgs<kType> a;
-    a.x = make_source<kType>(d_x, ld_x, rows, cols);
-    a.residual = make_source<kType>(d_residual, ld_residual, rows, cols);
+    a.x = make_source<kType>(d_x, ld_x);
+    a.residual = make_source<kType>(d_residual, ld_residual);
     a.out = make_target<kType>(d_out, ld_out);
     a.cols = cols;
     a.rows = (uint32_t)rows;

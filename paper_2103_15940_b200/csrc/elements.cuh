@@ -136,12 +136,10 @@ __device__ __forceinline__ Granule widen_raw(const Raw<kType>& r) {
     return g;
 }
 
-// A matrix that is read or written in granules.  whole: every row starts on a granule boundary of memory.  last: one
-// past the matrix's last element.
+// A matrix that is read or written in granules.  whole: every row starts on a granule boundary of memory.
 template <int kType>
 struct Source {
     const typename Word<kType>::type* p;
-    const typename Word<kType>::type* last;
     int64_t ld;
     bool whole;
 };
@@ -204,27 +202,30 @@ struct Pieces {
     bool inside;  // they lie in the matrix
 };
 
+// Whether the pieces of granule g can reach beyond the matrix in its first or last row.
+__device__ __forceinline__ bool at_edge(int64_t cols, int64_t g) { return g == 0 || (g + 2) * kGranule > cols + 1; }
+
 // Starts to load `n` columns (0..8) of a granule at p: loads under a predicate, nothing waits and nothing branches.
-// What the pieces hold beyond the columns is thrown away later; a granule whose pieces reach beyond the matrix (at its
-// two ends only) is left to arrive().
+// What the pieces hold beyond the columns is thrown away later; where they could reach beyond the matrix (`inside`
+// false: at the edges of its first and last row) the granule is left to arrive().
 template <int kType>
-__device__ __forceinline__ Pieces<kType> start_any(const typename Word<kType>::type* p, int n, const Source<kType>& m) {
+__device__ __forceinline__ Pieces<kType> start_any(const typename Word<kType>::type* p, int n, bool inside) {
     constexpr int kPer = kType == QFMT_F32 ? 4 : 8;
     Pieces<kType> r;
     const int first = (int)(reinterpret_cast<uintptr_t>(p) & 15u) / (16 / kPer);
     const auto* base = p - first;
-    const int pieces = (first + n + kPer - 1) / kPer;
-    r.inside = n > 0 && base >= m.p && base + pieces * kPer <= m.last;
+    const int reach = inside && n > 0 ? first + n : 0;
+    r.inside = inside;
 #pragma unroll
     for (int i = 0; i < (int)(sizeof(r.w) / 16); ++i)
-        asm volatile("{ .reg .pred q; setp.ne.u32 q, %5, 0; @q ld.global.v4.b32 {%0,%1,%2,%3}, [%4]; }"
+        asm volatile("{ .reg .pred q; setp.gt.s32 q, %5, %6; @q ld.global.v4.b32 {%0,%1,%2,%3}, [%4]; }"
                      : "=r"(r.w[4 * i]), "=r"(r.w[4 * i + 1]), "=r"(r.w[4 * i + 2]), "=r"(r.w[4 * i + 3])
-                     : "l"(base + i * kPer), "r"((uint32_t)(r.inside && i < pieces)));
+                     : "l"(base + i * kPer), "r"(reach), "r"(i * kPer));
     return r;
 }
 // Its words, zero where there is no column.
 template <int kType>
-__device__ __forceinline__ Raw<kType> arrive(const Pieces<kType>& q, const typename Word<kType>::type* p, int n, const Source<kType>& m) {
+__device__ __forceinline__ Raw<kType> arrive(const Pieces<kType>& q, const typename Word<kType>::type* p, int n) {
     constexpr int kPer = kType == QFMT_F32 ? 4 : 8;
     const uint32_t first = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15u) / (16 / kPer);
     Raw<kType> r;
@@ -245,8 +246,8 @@ __device__ __forceinline__ Raw<kType> arrive(const Pieces<kType>& q, const typen
     return r;
 }
 template <int kType>
-__device__ __forceinline__ Raw<kType> load_any(const typename Word<kType>::type* p, int n, const Source<kType>& m) {
-    return arrive<kType>(start_any<kType>(p, n, m), p, n, m);
+__device__ __forceinline__ Raw<kType> load_any(const typename Word<kType>::type* p, int n, bool inside) {
+    return arrive<kType>(start_any<kType>(p, n, inside), p, n);
 }
 
 // Writes `n` columns (0..8) of a granule at p.  Called by whole warps.  `from` and `to`: the lane before this one holds
@@ -347,19 +348,18 @@ __device__ __forceinline__ Raw<kType> finish_format(const Granule& v, int n, con
 }
 
 // A granule of n columns at p, in row `row` of `rows`, on its way, and its words: zeros where there is nothing.
-// kPlain: whole and aligned, or not there at all.
+// kPlain: whole and aligned, or not there at all.  edge: at_edge() of the granule.
 template <int kType, bool kPlain>
 using OnItsWay = std::conditional_t<kPlain, Raw<kType>, Pieces<kType>>;
 template <int kType, bool kPlain>
-__device__ __forceinline__ OnItsWay<kType, kPlain> start(const typename Word<kType>::type* p, int n, uint32_t row, uint32_t rows,
-                                                         const Source<kType>& m) {
+__device__ __forceinline__ OnItsWay<kType, kPlain> start(const typename Word<kType>::type* p, int n, uint32_t row, uint32_t rows, bool edge) {
     if constexpr (kPlain) return load_raw<kType>(p, n, row, rows);
-    else return start_any<kType>(p, row < rows ? n : 0, m);
+    else return start_any<kType>(p, row < rows ? n : 0, !(edge && (row == 0 || row + 1 >= rows)));
 }
 template <int kType, bool kPlain>
-__device__ __forceinline__ Raw<kType> words(const OnItsWay<kType, kPlain>& q, const typename Word<kType>::type* p, int n, const Source<kType>& m) {
+__device__ __forceinline__ Raw<kType> words(const OnItsWay<kType, kPlain>& q, const typename Word<kType>::type* p, int n) {
     if constexpr (kPlain) return q;
-    else return arrive<kType>(q, p, n, m);
+    else return arrive<kType>(q, p, n);
 }
 template <int kType, bool kPlain>
 __device__ __forceinline__ void put(typename Word<kType>::type* p, int n, const Target<kType>& m, const Raw<kType>& r, bool from, bool to) {
@@ -434,9 +434,8 @@ inline bool granule_aligned(const void* p, int64_t ld, int32_t dtype) {
     return (reinterpret_cast<uintptr_t>(p) & (granule_bytes(dtype) - 1)) == 0 && ld % kGranule == 0;
 }
 template <int kType>
-Source<kType> make_source(const void* p, int64_t ld, int64_t rows, int64_t cols) {
-    const auto* q = static_cast<const typename Word<kType>::type*>(p);
-    return {q, p == nullptr || rows == 0 ? q : q + (rows - 1) * ld + cols, ld, granule_aligned(p, ld, kType)};
+Source<kType> make_source(const void* p, int64_t ld) {
+    return {static_cast<const typename Word<kType>::type*>(p), ld, granule_aligned(p, ld, kType)};
 }
 template <int kType>
 Target<kType> make_target(void* p, int64_t ld) {

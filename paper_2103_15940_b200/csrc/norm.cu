@@ -46,6 +46,8 @@ struct BackwardArgs {
     const float* weight;
     Target<kType> dx, dresidual;  // or NULL
     float* partial;  // [parts][2][padded columns] sums of dy xhat and dy over a part of the rows, or NULL
+    float* dweight;  // where a single part goes at once; both NULL with several parts
+    float* dbias;
     int64_t rows, cols;
     float inverse;
     bool fmt;
@@ -162,9 +164,10 @@ __global__ void __launch_bounds__(kLoopThreads) norm_forward_loop_kernel(const F
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const auto h = [&](uint32_t g, int n) {
             const int64_t col = (int64_t)g * kGranule;
+            const bool inside = (row != 0 && row + 1 != a.rows) || !at_edge(a.cols, g);
             const Raw<kType> res = kFused && a.residual.p != nullptr
-                                       ? load_any<kType>(a.residual.p + row * a.residual.ld + col, n, a.residual) : Raw<kType>();
-            return join_h<kType, kFused>(a, load_any<kType>(a.x.p + row * a.x.ld + col, n, a.x), res, offset, (uint32_t)row, g);
+                                       ? load_any<kType>(a.residual.p + row * a.residual.ld + col, n, inside) : Raw<kType>();
+            return join_h<kType, kFused>(a, load_any<kType>(a.x.p + row * a.x.ld + col, n, inside), res, offset, (uint32_t)row, g);
         };
         float sum = 0.0f;
         for (uint32_t g = threadIdx.x; g < granules; g += kLoopThreads) sum += sum8(h(g, granule_columns(a.cols, g)));
@@ -275,7 +278,7 @@ struct ForwardSteps {
 };
 
 // R rows at a time are read once and stay in their team's registers.  V <= 2: so do the team's weight and bias,
-// from row to row, and with kPlain the next rows are on their way while these are worked on.  V = 4: longer rows,
+// from row to row, and with kPlain the next rows are on their way while these are worked on.  V > 2: longer rows,
 // without either.  kPlain: every granule whole and aligned, no format; otherwise any layout and an optional format.
 template <int kType, int V, int R, bool kFused, bool kPlain>
 __global__ void __launch_bounds__(kMaxTeam) norm_forward_rows_kernel(const ForwardArgs<kType> a, int team, const ForwardSteps step) {
@@ -297,8 +300,12 @@ __global__ void __launch_bounds__(kMaxTeam) norm_forward_rows_kernel(const Forwa
     const bool residual = kFused && a.residual.p != nullptr;
     const int next = team * kGranule;  // elements between a thread's granules
     int n[V];                          // columns of each granule
+    bool edge[V];
 #pragma unroll
-    for (int k = 0; k < V; ++k) n[k] = granule_columns(a.cols, k * team + t);
+    for (int k = 0; k < V; ++k) {
+        n[k] = granule_columns(a.cols, k * team + t);
+        edge[k] = at_edge(a.cols, k * team + t);
+    }
 
     // A team past the last row, whose warp has teams with one, keeps in step with them and stores nothing.
     const uint32_t rows = (uint32_t)a.rows, stride = gridDim.x * teams * R;
@@ -313,8 +320,8 @@ __global__ void __launch_bounds__(kMaxTeam) norm_forward_rows_kernel(const Forwa
         for (int i = 0; i < R; ++i) {
 #pragma unroll
             for (int k = 0; k < V; ++k) {
-                x[i][k] = start<kType, kPlain>(px + i * a.x.ld + k * next, n[k], at + i, rows, a.x);
-                if (kFused) r[i][k] = start<kType, kPlain>(pr + i * a.residual.ld + k * next, residual ? n[k] : 0, at + i, rows, a.residual);
+                x[i][k] = start<kType, kPlain>(px + i * a.x.ld + k * next, n[k], at + i, rows, edge[k]);
+                if (kFused) r[i][k] = start<kType, kPlain>(pr + i * a.residual.ld + k * next, residual ? n[k] : 0, at + i, rows, edge[k]);
             }
         }
         if (kAhead) px += step.x, pr += step.residual;
@@ -337,8 +344,8 @@ __global__ void __launch_bounds__(kMaxTeam) norm_forward_rows_kernel(const Forwa
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 const int there = row + i < rows ? n[k] : 0;
-                const Raw<kType> xs = words<kType, kPlain>(x[i][k], px + i * a.x.ld + k * next, there, a.x);
-                const Raw<kType> rs = kFused ? words<kType, kPlain>(r[i][k], pr + i * a.residual.ld + k * next, residual ? there : 0, a.residual)
+                const Raw<kType> xs = words<kType, kPlain>(x[i][k], px + i * a.x.ld + k * next, there);
+                const Raw<kType> rs = kFused ? words<kType, kPlain>(r[i][k], pr + i * a.residual.ld + k * next, residual ? there : 0)
                                              : Raw<kType>();
                 v[i][k] = join_h<kType, kFused>(a, xs, rs, offset, row + i, k * team + t);
             }
@@ -444,8 +451,8 @@ __device__ __forceinline__ void store_gradients(const BackwardArgs<kType>& a, co
     if constexpr (kFused) {
         if (a.dh.p != nullptr) {
             const auto* p = to.dh + i * a.dh.ld + at;
-            const OnItsWay<kType, kPlain> q = start<kType, kPlain>(p, n, 0, 1, a.dh);
-            const Granule more = widen_raw<kType>(words<kType, kPlain>(q, p, n, a.dh));
+            const OnItsWay<kType, kPlain> q = start<kType, kPlain>(p, n, row, (uint32_t)a.rows, at_edge(a.cols, g));
+            const Granule more = widen_raw<kType>(words<kType, kPlain>(q, p, n));
 #pragma unroll
             for (int j = 0; j < 4; ++j) d.p[j] = add2(d.p[j], more.p[j]);
         }
@@ -468,8 +475,9 @@ __global__ void __launch_bounds__(kLoopThreads) norm_backward_loop_kernel(const 
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const float mean = a.mean[row], rstd = a.rstd[row];
         const auto load = [&](uint32_t g, int n, Granule& dy, Granule& xhat, Granule& w) {
-            dy = widen_raw<kType>(load_any<kType>(a.dy.p + row * a.dy.ld + (int64_t)g * kGranule, n, a.dy));
-            xhat = normalise<false>(widen_raw<kType>(load_any<kType>(a.h.p + row * a.h.ld + (int64_t)g * kGranule, n, a.h)), mean, rstd, n);
+            const bool inside = (row != 0 && row + 1 != a.rows) || !at_edge(a.cols, g);
+            dy = widen_raw<kType>(load_any<kType>(a.dy.p + row * a.dy.ld + (int64_t)g * kGranule, n, inside));
+            xhat = normalise<false>(widen_raw<kType>(load_any<kType>(a.h.p + row * a.h.ld + (int64_t)g * kGranule, n, inside)), mean, rstd, n);
             w = load_columns(a.weight, g, n, 1.0f);
         };
         float2 s = make_float2(0.0f, 0.0f);
@@ -502,8 +510,9 @@ __global__ void __launch_bounds__(32 * kColumnWarps) norm_column_sums_kernel(con
     Granule dw = splat(0.0f), db = splat(0.0f);
     if (n > 0) {
         for (int64_t row = (int64_t)blockIdx.y * kColumnWarps + warp; row < a.rows; row += (int64_t)gridDim.y * kColumnWarps) {
-            const Granule dy = widen_raw<kType>(load_any<kType>(a.dy.p + row * a.dy.ld + (int64_t)g * kGranule, n, a.dy));
-            const Granule xhat = normalise<false>(widen_raw<kType>(load_any<kType>(a.h.p + row * a.h.ld + (int64_t)g * kGranule, n, a.h)), a.mean[row], a.rstd[row], n);
+            const bool inside = (row != 0 && row + 1 != a.rows) || !at_edge(a.cols, g);
+            const Granule dy = widen_raw<kType>(load_any<kType>(a.dy.p + row * a.dy.ld + (int64_t)g * kGranule, n, inside));
+            const Granule xhat = normalise<false>(widen_raw<kType>(load_any<kType>(a.h.p + row * a.h.ld + (int64_t)g * kGranule, n, inside)), a.mean[row], a.rstd[row], n);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 dw.p[j] = fma2(dy.p[j], xhat.p[j], dw.p[j]);
@@ -567,11 +576,23 @@ __device__ __forceinline__ Granule from_quads(float4 a, float4 b) {
     return {{make_float2(a.x, a.y), make_float2(a.z, a.w), make_float2(b.x, b.y), make_float2(b.z, b.w)}};
 }
 
+// Four columns of dweight and dbias laid side by side, from column 4 i on.
+__device__ __forceinline__ void put_columns(int i, float4 s, int padded, int cols, float* dweight, float* dbias) {
+    const bool second = 4 * i >= padded;
+    float* const out = second ? dbias : dweight;
+    const int c = 4 * i - (second ? padded : 0);
+    const float v[4] = {s.x, s.y, s.z, s.w};
+    if (out == nullptr) return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (c + j < cols) out[c + j] = v[j];
+}
+
 // The backward pass of rows that a team holds in registers, R at a time: dy and h are read once, the sums over rows
 // stay in the registers of the thread that owns their columns from row to row, and a block leaves one part.
 // kParts: a team is a part of a warp (or all of it), otherwise whole warps; a block has 512 threads' worth of teams.
 // V > 1 (wide rows): the team is the block, and the column sums lie in shared memory, each thread's its own, since the
-// registers hold V granules of dy and h; with V = 4 the weight is read from the cache as well.
+// registers hold V granules of dy and h; with V > 2 the weight is read from the cache as well.
 // kPlain as in the forward pass.  With registers to spare (kAhead) the next rows are on their way while these are
 // worked on.  A team takes `group` neighbouring rows (R, or R = 1 at a time), then the group that is a step away.
 template <int kType, int V, int R, bool kParts, bool kFused, bool kPlain>
@@ -595,11 +616,13 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
     const uint64_t offset = kFused ? drop_offset(a.drop) : 0ull;
     const int next = team * kGranule;  // elements between a thread's granules
     int n[V];
-    Granule w[V < 4 ? V : 1], dw = splat(0.0f), db = splat(0.0f);  // the sums with V = 1
+    bool edge[V];
+    Granule w[V <= 2 ? V : 1], dw = splat(0.0f), db = splat(0.0f);  // the sums with V = 1
     float4* const sums_in_shared = reinterpret_cast<float4*>(dynamic + hist_words);  // with V > 1: [V][4][team]
 #pragma unroll
     for (int k = 0; k < V; ++k) {
         n[k] = granule_columns(a.cols, k * team + t);
+        edge[k] = at_edge(a.cols, k * team + t);
         if (V > 1) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) sums_in_shared[(4 * k + i) * team + t] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -620,8 +643,8 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
             rstd[i] = there ? __ldg(a.rstd + at + i) : 0.0f;
 #pragma unroll
             for (int k = 0; k < V; ++k) {
-                raw_dy[i][k] = start<kType, kPlain>(pdy + i * a.dy.ld + k * next, n[k], at + i, rows, a.dy);
-                raw_h[i][k] = start<kType, kPlain>(ph + i * a.h.ld + k * next, n[k], at + i, rows, a.h);
+                raw_dy[i][k] = start<kType, kPlain>(pdy + i * a.dy.ld + k * next, n[k], at + i, rows, edge[k]);
+                raw_h[i][k] = start<kType, kPlain>(ph + i * a.h.ld + k * next, n[k], at + i, rows, edge[k]);
             }
         }
     };
@@ -630,7 +653,7 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
     const auto advance = [&](bool second, auto*& p, int64_t ld, int64_t by) { p += pairs ? (second ? by - ld : ld) : by; };
     if (kAhead) fetch_rows(row);
 #pragma unroll
-    for (int k = 0; k < (V < 4 ? V : 0); ++k) w[k] = load_columns(a.weight, k * team + t, n[k], 1.0f);
+    for (int k = 0; k < (V <= 2 ? V : 0); ++k) w[k] = load_columns(a.weight, k * team + t, n[k], 1.0f);
     int parity = 0;
     bool second = false;
     for (uint32_t first = blockIdx.x * teams * group; first < rows; parity ^= 1) {  // the row of the block's first team
@@ -645,11 +668,11 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 const int there = row + i < rows ? n[k] : 0;  // a row that does not exist adds nothing to the column sums
-                dy[i][k] = widen_raw<kType>(words<kType, kPlain>(raw_dy[i][k], pdy + i * a.dy.ld + k * next, there, a.dy));
-                xhat[i][k] = normalise<kPlain>(widen_raw<kType>(words<kType, kPlain>(raw_h[i][k], ph + i * a.h.ld + k * next, there, a.h)),
+                dy[i][k] = widen_raw<kType>(words<kType, kPlain>(raw_dy[i][k], pdy + i * a.dy.ld + k * next, there));
+                xhat[i][k] = normalise<kPlain>(widen_raw<kType>(words<kType, kPlain>(raw_h[i][k], ph + i * a.h.ld + k * next, there)),
                                                mean[i], rstd[i], there);
-                if (V == 4) w[0] = load_columns(a.weight, k * team + t, n[k], 1.0f);
-                s[i] = add2(s[i], row_sums(dy[i][k], xhat[i][k], w[V < 4 ? k : 0]));
+                if (V > 2) w[0] = load_columns(a.weight, k * team + t, n[k], 1.0f);
+                s[i] = add2(s[i], row_sums(dy[i][k], xhat[i][k], w[V <= 2 ? k : 0]));
                 if constexpr (V == 1) {
                     add_columns(dw, db, dy[i][k], xhat[i][k]);
                 } else {
@@ -677,8 +700,8 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
             const float c1 = s[i].x * a.inverse, c2 = s[i].y * a.inverse;
 #pragma unroll
             for (int k = 0; k < V; ++k) {
-                if (V == 4) w[0] = load_columns(a.weight, k * team + t, n[k], 1.0f);
-                store_gradients<kType, kFused, kPlain>(a, to, i, k * next, dy[i][k], xhat[i][k], w[V < 4 ? k : 0], this_rstd[i], c1, c2, row + i,
+                if (V > 2) w[0] = load_columns(a.weight, k * team + t, n[k], 1.0f);
+                store_gradients<kType, kFused, kPlain>(a, to, i, k * next, dy[i][k], xhat[i][k], w[V <= 2 ? k : 0], this_rstd[i], c1, c2, row + i,
                                                        k * team + t, row + i < rows ? n[k] : 0, from, after, offset, hist);
             }
         }
@@ -690,12 +713,13 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
         second = pairs && !second;
     }
     if (hist != nullptr) flush_hist(hist, a.quant, a.stats, (uint64_t)a.rows * (uint64_t)a.cols);
+    const bool alone = a.dweight != nullptr || a.dbias != nullptr;  // this block's part is the result
     if (a.partial == nullptr) return;
     // [dweight, dbias][padded columns] of every warp of small teams, or of every team; then their sum
     const int padded = ((int)a.cols + kGranule - 1) / kGranule * kGranule, quads = padded / 2;
     const int units = kParts ? blockDim.x / 32 : teams;
     float4* const part = reinterpret_cast<float4*>(a.partial) + (int64_t)blockIdx.x * quads;
-    float4* const sums = units > 1 ? reinterpret_cast<float4*>(dynamic + hist_words) : part;
+    float4* const sums = units > 1 ? reinterpret_cast<float4*>(dynamic + hist_words) : part;  // (a wide row's own sums stay where they are)
     float4* const own = sums + (kParts ? threadIdx.x / 32 : mine) * quads;
     if constexpr (kParts) {
         for (int off = 16; off >= team; off >>= 1) {  // the teams of a warp
@@ -718,7 +742,7 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
         q[0] = quad(dw, 0), q[1] = quad(dw, 1);
         q[quads / 2] = quad(db, 0), q[quads / 2 + 1] = quad(db, 1);
     }
-    if (units == 1) return;
+    if (units == 1 && !alone) return;
     __syncthreads();
     for (int i = threadIdx.x; i < quads; i += blockDim.x) {
         float4 s = sums[i];
@@ -726,7 +750,8 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
             const float4 q = sums[u * quads + i];
             s = make_float4(s.x + q.x, s.y + q.y, s.z + q.z, s.w + q.w);
         }
-        part[i] = s;
+        if (alone) put_columns(i, s, padded, (int)a.cols, a.dweight, a.dbias);
+        else part[i] = s;
     }
 }
 
@@ -773,7 +798,7 @@ Plan make_plan(int64_t cols, int least, int most) {
         while (team < g) team *= 2;
         return {team, 1};
     }
-    for (int v = least; v <= most; v *= 2)
+    for (int v = least; v <= most; ++v)
         if (g <= (int64_t)v * kMaxTeam) return {(int)((g + 32 * v - 1) / (32 * v)) * 32, v};
     return {0, 0};
 }
@@ -862,12 +887,15 @@ int launch_forward(const Call& c, const ForwardArgs<kType>& a, cudaStream_t stre
     const Plan plan = forward_plan(a.cols);
     if (plan.team != 0) {
         const bool plain = plain_layout(a.cols, {a.x.whole, a.residual.whole, a.h.whole, a.y.whole}) && !a.fmt;
+        constexpr int kRows = kFused && kType == QFMT_F32 ? 1 : 2;  // two wide fp32 rows of x and residual do not fit
         const auto run = plain ? (plan.granules == 1   ? launch_forward_rows<kType, 1, 2, kFused, true>
-                                            : plan.granules == 2 ? launch_forward_rows<kType, 2, kFused && kType == QFMT_F32 ? 1 : 2, kFused, true>
-                                                                 : launch_forward_rows<kType, 4, 1, kFused, true>)
-                                         : (plan.granules == 1   ? launch_forward_rows<kType, 1, 1, kFused, false>
-                                            : plan.granules == 2 ? launch_forward_rows<kType, 2, 1, kFused, false>
-                                                                 : launch_forward_rows<kType, 4, 1, kFused, false>);
+                                  : plan.granules == 2 ? launch_forward_rows<kType, 2, kRows, kFused, true>
+                                  : plan.granules == 3 ? launch_forward_rows<kType, 3, 1, kFused, true>
+                                                       : launch_forward_rows<kType, 4, 1, kFused, true>)
+                               : (plan.granules == 1   ? launch_forward_rows<kType, 1, 1, kFused, false>
+                                  : plan.granules == 2 ? launch_forward_rows<kType, 2, 1, kFused, false>
+                                  : plan.granules == 3 ? launch_forward_rows<kType, 3, 1, kFused, false>
+                                                       : launch_forward_rows<kType, 4, 1, kFused, false>);
         return run(c, a, plan.team, stream);
     }
     const int64_t cap = (int64_t)c.dev.sm_count * 4;
@@ -881,8 +909,8 @@ int forward(const Call& c, const void* d_x, const void* d_residual, const float*
             void* d_y, float* d_mean, float* d_rstd, qfmt_stats_t* d_stats, cudaStream_t stream) {
     const qfmt_norm_t& s = c.norm;
     ForwardArgs<kType> a;
-    a.x = make_source<kType>(d_x, s.ld_x, s.rows, s.cols);
-    a.residual = make_source<kType>(d_residual, s.ld_residual, s.rows, s.cols);
+    a.x = make_source<kType>(d_x, s.ld_x);
+    a.residual = make_source<kType>(d_residual, s.ld_residual);
     a.weight = d_weight;
     a.bias = d_bias;
     a.h = make_target<kType>(d_h, s.ld_h);
@@ -933,9 +961,12 @@ int join_parts(const float* partial, int parts, int64_t cols, float* d_dweight, 
 }
 
 template <int kType, int V, int R, bool kParts, bool kFused, bool kPlain>
-int launch_backward_rows(const Call& c, const BackwardArgs<kType>& a, int team, int group, float* d_dweight, float* d_dbias, cudaStream_t stream) {
+int launch_backward_rows(const Call& c, BackwardArgs<kType> a, int team, int group, float* d_dweight, float* d_dbias, cudaStream_t stream) {
     const unsigned teams = kMaxTeam / team, block = teams * team;
     const int64_t cap = std::min(c.dev.sm_count, kMaxParts), want = (a.rows + teams * group - 1) / (teams * group);
+    const unsigned blocks = (unsigned)std::min(want, cap);
+    const bool alone = a.partial != nullptr && blocks == 1;
+    if (alone) a.dweight = d_dweight, a.dbias = d_dbias;
     const auto kern = norm_backward_rows_kernel<kType, V, R, kParts, kFused, kPlain>;
     const unsigned units = kParts ? block / 32 : teams;
     const size_t smem = c.hist_bytes + (V > 1       ? (size_t)block * V * 64
@@ -946,11 +977,10 @@ int launch_backward_rows(const Call& c, const BackwardArgs<kType>& a, int team, 
                                            (V > 1 ? V * 32 + 40 : 72) * 1024));  // histogram and sums
         if (c.dev.ordinal >= 0 && c.dev.ordinal < 64) allowed[c.dev.ordinal].store(true);
     }
-    const unsigned blocks = (unsigned)std::min(want, cap);
     const int64_t stride = (int64_t)blocks * teams * group;
     const BackwardSteps step = {stride * a.dy.ld, stride * a.h.ld, stride * a.dh.ld, stride * a.dx.ld, stride * a.dresidual.ld};
     QFMT_CUDA_TRY(launch_overlapping(kern, blocks, block, smem, stream, a, team, group, step, (int)(c.hist_bytes / sizeof(uint32_t))));
-    return a.partial != nullptr ? join_parts(a.partial, (int)blocks, a.cols, d_dweight, d_dbias, stream) : QFMT_OK;
+    return a.partial != nullptr && !alone ? join_parts(a.partial, (int)blocks, a.cols, d_dweight, d_dbias, stream) : QFMT_OK;
 }
 
 template <int kType, bool kFused>
@@ -962,8 +992,12 @@ int launch_backward(const Call& c, const BackwardArgs<kType>& a, float* d_dweigh
         // Two neighbouring rows to a team where every team gets some: a rule on sizes alone, since it decides the order
         // of the sums over rows.  Whether the two are worked on at once does not.
         const int64_t teams = (int64_t)(kMaxTeam / plan.team) * std::min(c.dev.sm_count, kMaxParts);
-        const int group = plan.granules == 1 && a.rows > 2 * (teams - 1) ? 2 : 1;
-        const auto run = plan.granules == 4   ? (plain ? launch_backward_rows<kType, 4, 1, false, kFused, true>
+        // So is a single block where that takes one turn of pairs: its part is the result, and no second kernel runs.
+        const bool few = a.partial != nullptr && a.rows <= 2 * (kMaxTeam / plan.team);
+        const int group = plan.granules == 1 && (few || a.rows > 2 * (teams - 1)) ? 2 : 1;
+        const auto run = plan.granules == 3   ? (plain ? launch_backward_rows<kType, 3, 1, false, kFused, true>
+                                                       : launch_backward_rows<kType, 3, 1, false, kFused, false>)
+                         : plan.granules == 4 ? (plain ? launch_backward_rows<kType, 4, 1, false, kFused, true>
                                                        : launch_backward_rows<kType, 4, 1, false, kFused, false>)
                          : plan.granules == 2 ? (plain ? launch_backward_rows<kType, 2, 1, false, kFused, true>
                                                        : launch_backward_rows<kType, 2, 1, false, kFused, false>)
@@ -997,15 +1031,16 @@ int backward(const Call& c, const void* d_dy, const void* d_dh, const void* d_h,
              qfmt_stats_t* d_stats, float* partial, cudaStream_t stream) {
     const qfmt_norm_t& s = c.norm;
     BackwardArgs<kType> a;
-    a.dy = make_source<kType>(d_dy, s.ld_dy, s.rows, s.cols);
-    a.dh = make_source<kType>(d_dh, s.ld_dh, s.rows, s.cols);
-    a.h = make_source<kType>(d_h, ld_h, s.rows, s.cols);
+    a.dy = make_source<kType>(d_dy, s.ld_dy);
+    a.dh = make_source<kType>(d_dh, s.ld_dh);
+    a.h = make_source<kType>(d_h, ld_h);
     a.mean = d_mean;
     a.rstd = d_rstd;
     a.weight = d_weight;
     a.dx = make_target<kType>(d_dx, s.ld_dx);
     a.dresidual = make_target<kType>(d_dresidual, s.ld_dresidual);
     a.partial = partial;
+    a.dweight = a.dbias = nullptr;
     a.rows = s.rows;
     a.cols = s.cols;
     a.inverse = 1.0f / (float)a.cols;
