@@ -8,6 +8,7 @@ import glob
 import os
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -17,7 +18,7 @@ LIB = os.path.join(HERE, "libqfmt.so")
 NVCC_FLAGS = [
     "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
     "-ftz=false", "-prec-div=true", "-prec-sqrt=true", "-fmad=false",
-    "-Xcompiler", "-fPIC", "-shared", "-cudart", "static",
+    "-Xcompiler", "-fPIC", "-cudart", "static",
 ]
 
 
@@ -37,9 +38,16 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not needs_build():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + [
-        "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-o", LIB] + sources()
-    subprocess.check_call(cmd)
+    flags = NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-I", os.path.join(ROOT, "include"), "-I", CSRC]
+    # one nvcc per source, side by side; the objects are linked into the library and go
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, os.path.basename(s) + ".o") for s in sources()]
+        running = [subprocess.Popen([nvcc] + flags + ["-c", "-o", o, s]) for s, o in zip(sources(), objects)]
+        codes = [p.wait() for p in running]
+        for src, code in zip(sources(), codes):
+            if code != 0:
+                raise subprocess.CalledProcessError(code, f"{nvcc} -c {src}")
+        subprocess.check_call([nvcc] + NVCC_FLAGS + ["-shared", "-o", LIB] + objects)
     return LIB
 
 
