@@ -96,7 +96,7 @@ int launch_dropout(const void* d_x, int64_t ld_x, const void* d_residual, int64_
         dropout_kernel<kType, false, true, false>,  dropout_kernel<kType, false, true, true>,
         dropout_kernel<kType, true, false, false>,  dropout_kernel<kType, true, false, true>,
         dropout_kernel<kType, true, true, false>,   dropout_kernel<kType, true, true, true>};
-    static std::atomic<int> known[8][kDropThreads / 32 + 1];
+    static std::atomic<uint64_t> known[8][kDropThreads / 32 + 1];
     int resident = 0;
     const int rc = resident_blocks(kernels[variant], kDropThreads, 0, known[variant], &resident);
     if (rc != QFMT_OK) return rc;

@@ -379,6 +379,40 @@ struct DropParams {
     const uint64_t* d_offset;  // added to offset when the kernel runs, or NULL
 };
 
+// Rows of containers of any alignment through shared memory: a team copies a row there word by word (16-byte pieces
+// where it starts on one), asynchronously and in whole lines, so that its columns lie on granule boundaries.
+__device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+inline __host__ __device__ uint32_t staged_row_bytes(int64_t cols) { return (uint32_t)((cols + kGranule - 1) / kGranule * kGranule * 4); }
+__device__ __forceinline__ void stage_row(uint32_t shared, const uint32_t* row, int cols, int t, int team) {
+    int done = 0;
+    if ((reinterpret_cast<uintptr_t>(row) & 15u) == 0) {
+        done = cols / 4 * 4;
+        for (int i = 4 * t; i < done; i += 4 * team)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(shared + 4 * i), "l"(row + i) : "memory");
+    }
+    for (int i = done + t; i < cols; i += team)
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(shared + 4 * i), "l"(row + i) : "memory");
+}
+__device__ __forceinline__ void stage_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kPending>  // of this thread's copies all but the last kPending groups have arrived
+__device__ __forceinline__ void stage_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kPending) : "memory"); }
+
+// n columns (0..8) of granule g of a staged row, zeros where there are none.
+__device__ __forceinline__ Raw<QFMT_F32> staged_granule(uint32_t shared, int g, int n) {
+    Raw<QFMT_F32> r;
+#pragma unroll
+    for (uint32_t& w : r.w) w = 0u;
+    if (n <= 0) return r;
+    const uint32_t at = shared + (uint32_t)g * 32;
+#pragma unroll
+    for (int i = 0; i < 8; i += 4)
+        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];"
+                     : "=r"(r.w[i]), "=r"(r.w[i + 1]), "=r"(r.w[i + 2]), "=r"(r.w[i + 3]) : "r"(at + 4 * i) : "memory");
+#pragma unroll
+    for (int j = 0; j < kGranule; ++j) r.w[j] = j < n ? r.w[j] : 0u;
+    return r;
+}
+
 // Philox4x32-10 (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3", SC 2011): ten
 // rounds of two 32 x 32 -> 64-bit products on a counter of four words, each with its key.
 __device__ __forceinline__ uint4 philox4x32_10(uint4 c, const DropParams& d) {
@@ -459,17 +493,19 @@ inline int make_drop_params(const qfmt_dropout_t* d, DropParams* out) {
     return QFMT_OK;
 }
 
-// Blocks of a kernel that an SM holds at once; asked for once per block size.
+// Blocks of a kernel that an SM holds at once.  `known` remembers the last answer for every block size (with the bytes
+// of shared memory it was for), since asking takes as long as a launch.
 template <typename K>
-int resident_blocks(K kernel, unsigned block, size_t smem, std::atomic<int>* known, int* out) {
-    std::atomic<int>& slot = known[block / 32];
-    if (smem == 0 && slot.load() > 0) {
-        *out = slot.load();
+int resident_blocks(K kernel, unsigned block, size_t smem, std::atomic<uint64_t>* known, int* out) {
+    std::atomic<uint64_t>& slot = known[block / 32];
+    const uint64_t seen = slot.load(), key = (uint64_t)smem << 8 | 0x80u;
+    if ((seen & ~(uint64_t)0x7Fu) == key) {
+        *out = (int)(seen & 0x7Fu);
         return QFMT_OK;
     }
     QFMT_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(out, kernel, (int)block, smem));
     if (*out < 1) *out = 1;
-    if (smem == 0) slot.store(*out);
+    slot.store(key | (uint64_t)*out);
     return QFMT_OK;
 }
 

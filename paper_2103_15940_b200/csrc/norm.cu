@@ -278,17 +278,22 @@ struct ForwardSteps {
 };
 
 // R rows at a time are read once and stay in their team's registers.  V <= 2: so do the team's weight and bias,
-// from row to row, and with kPlain the next rows are on their way while these are worked on.  V > 2: longer rows,
-// without either.  kPlain: every granule whole and aligned, no format; otherwise any layout and an optional format.
+// from row to row.  V > 2: longer rows, without them.
+// kPlain: every granule whole and aligned, no format; granules go straight to registers, with V <= 2 those of the next
+// rows while these are worked on.  Otherwise any layout and an optional format: codes come as aligned pieces that are
+// shifted into place; rows of containers (kStaged) go through shared memory behind the histogram, in `slots` places a
+// team (twice the tensors that are read: the next row is copied meanwhile).  Each way is the faster one for its type:
+// 16384 rows of 1021 take 28 us as shifted bfloat16 pieces and 31 us staged, as fp32 39 us shifted and 33 us staged.
 template <int kType, int V, int R, bool kFused, bool kPlain>
-__global__ void __launch_bounds__(kMaxTeam) norm_forward_rows_kernel(const ForwardArgs<kType> a, int team, const ForwardSteps step) {
+__global__ void __launch_bounds__(kMaxTeam)
+norm_forward_rows_kernel(const ForwardArgs<kType> a, int team, const ForwardSteps step, int hist_words, int slots) {
     constexpr bool kKeep = V <= 2;
-    constexpr bool kAhead = kKeep && kPlain;
-    extern __shared__ uint32_t lane_hist[];
+    constexpr bool kAhead = kKeep && kPlain, kStaged = !kPlain && kType == QFMT_F32;
+    extern __shared__ __align__(16) uint32_t dynamic[];
     __shared__ __align__(16) float scratch[2][R][16];
     grid_launch_dependents();
     grid_dependency_wait();
-    uint32_t* hist = !kPlain && a.stats != nullptr ? lane_hist : nullptr;
+    uint32_t* hist = !kPlain && a.stats != nullptr ? dynamic : nullptr;
     if (V > 1) {
         for (int i = threadIdx.x; i < 2 * R * 16; i += blockDim.x) (&scratch[0][0][0])[i] = 0.0f;
         __syncthreads();
@@ -300,33 +305,47 @@ __global__ void __launch_bounds__(kMaxTeam) norm_forward_rows_kernel(const Forwa
     const bool residual = kFused && a.residual.p != nullptr;
     const int next = team * kGranule;  // elements between a thread's granules
     int n[V];                          // columns of each granule
-    bool edge[V];
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
-        n[k] = granule_columns(a.cols, k * team + t);
-        edge[k] = at_edge(a.cols, k * team + t);
-    }
+    for (int k = 0; k < V; ++k) n[k] = granule_columns(a.cols, k * team + t);
 
     // A team past the last row, whose warp has teams with one, keeps in step with them and stores nothing.
     const uint32_t rows = (uint32_t)a.rows, stride = gridDim.x * teams * R;
     uint32_t row = (blockIdx.x * teams + mine) * R;
-    const auto* px = a.x.p + row * a.x.ld + t * kGranule;
-    const auto* pr = a.residual.p + row * a.residual.ld + t * kGranule;
+    const auto* px = a.x.p + row * a.x.ld + (kStaged ? 0 : t * kGranule);
+    const auto* pr = a.residual.p + row * a.residual.ld + (kStaged ? 0 : t * kGranule);
     auto* ph = a.h.p + row * a.h.ld + t * kGranule;
     auto* py = a.y.p + row * a.y.ld + t * kGranule;
-    OnItsWay<kType, kPlain> x[R][V], r[R][V];
+    OnItsWay<kType, kPlain || kStaged> x[R][V], r[R][V];
     const auto fetch_rows = [&](uint32_t at) {
 #pragma unroll
         for (int i = 0; i < R; ++i) {
 #pragma unroll
             for (int k = 0; k < V; ++k) {
-                x[i][k] = start<kType, kPlain>(px + i * a.x.ld + k * next, n[k], at + i, rows, edge[k]);
-                if (kFused) r[i][k] = start<kType, kPlain>(pr + i * a.residual.ld + k * next, residual ? n[k] : 0, at + i, rows, edge[k]);
+                const bool edge = at_edge(a.cols, k * team + t);
+                x[i][k] = start<kType, kPlain || kStaged>(px + i * a.x.ld + k * next, n[k], at + i, rows, edge);
+                if (kFused)
+                    r[i][k] = start<kType, kPlain || kStaged>(pr + i * a.residual.ld + k * next, residual ? n[k] : 0, at + i, rows, edge);
             }
         }
         if (kAhead) px += step.x, pr += step.residual;
     };
+    const uint32_t row_bytes = staged_row_bytes(a.cols);
+    const uint32_t places = shared_address(dynamic + hist_words) + mine * slots * row_bytes;
+    const int tensors = kFused ? 2 : 1;
+    uint32_t half = 0;
+    const auto stage_rows = [&]([[maybe_unused]] uint32_t at, [[maybe_unused]] uint32_t to_half) {  // the next row through shared memory
+        if constexpr (kStaged) if (at < rows) {
+            const uint32_t place = places + to_half * tensors * row_bytes;
+            stage_row(place, px, (int)a.cols, t, team);
+            if (residual) stage_row(place + row_bytes, pr, (int)a.cols, t, team);
+        }
+        stage_end();
+        px += step.x;
+        pr += step.residual;
+    };
+    const bool ahead = slots > tensors;
     if (kAhead) fetch_rows(row);
+    if (kStaged && ahead) stage_rows(row, 0);
     Granule w[kKeep ? V : 1], b[kKeep ? V : 1];
     if constexpr (kKeep) {
 #pragma unroll
@@ -336,7 +355,23 @@ __global__ void __launch_bounds__(kMaxTeam) norm_forward_rows_kernel(const Forwa
         }
     }
     for (; row - mine * R < rows; row += stride) {
-        if (!kAhead) fetch_rows(row);
+        if constexpr (kStaged) {
+            stage_rows(ahead ? row + stride : row, ahead ? half ^ 1u : 0u);
+            if (ahead) stage_wait<1>();
+            else stage_wait<0>();
+            if (V > 1) __syncthreads();
+            else __syncwarp();
+            const uint32_t place = places + half * tensors * row_bytes;
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                const int there = row < rows ? n[k] : 0;
+                x[0][k] = staged_granule(place, k * team + t, there);
+                if (kFused) r[0][k] = staged_granule(place + row_bytes, k * team + t, residual ? there : 0);
+            }
+            if (ahead) half ^= 1u;
+        } else if (!kAhead) {
+            fetch_rows(row);
+        }
         Granule v[R][V];
         float mean[R], rstd[R];
 #pragma unroll
@@ -344,13 +379,13 @@ __global__ void __launch_bounds__(kMaxTeam) norm_forward_rows_kernel(const Forwa
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 const int there = row + i < rows ? n[k] : 0;
-                const Raw<kType> xs = words<kType, kPlain>(x[i][k], px + i * a.x.ld + k * next, there);
-                const Raw<kType> rs = kFused ? words<kType, kPlain>(r[i][k], pr + i * a.residual.ld + k * next, residual ? there : 0)
+                const Raw<kType> xs = words<kType, kPlain || kStaged>(x[i][k], px + i * a.x.ld + k * next, there);
+                const Raw<kType> rs = kFused ? words<kType, kPlain || kStaged>(r[i][k], pr + i * a.residual.ld + k * next, residual ? there : 0)
                                              : Raw<kType>();
                 v[i][k] = join_h<kType, kFused>(a, xs, rs, offset, row + i, k * team + t);
             }
         if (kAhead) fetch_rows(row + stride);
-        else px += step.x, pr += step.residual;
+        else if (!kStaged) px += step.x, pr += step.residual;
         if (kFused && a.h.p != nullptr) {
 #pragma unroll
             for (int i = 0; i < R; ++i)
@@ -451,8 +486,8 @@ __device__ __forceinline__ void store_gradients(const BackwardArgs<kType>& a, co
     if constexpr (kFused) {
         if (a.dh.p != nullptr) {
             const auto* p = to.dh + i * a.dh.ld + at;
-            const OnItsWay<kType, kPlain> q = start<kType, kPlain>(p, n, row, (uint32_t)a.rows, at_edge(a.cols, g));
-            const Granule more = widen_raw<kType>(words<kType, kPlain>(q, p, n));
+            const Granule more = widen_raw<kType>(kPlain ? load_raw<kType>(p, n, 0, 1)
+                                                         : load_any<kType>(p, n, !(at_edge(a.cols, g) && (row == 0 || row + 1 >= (uint32_t)a.rows))));
 #pragma unroll
             for (int j = 0; j < 4; ++j) d.p[j] = add2(d.p[j], more.p[j]);
         }
@@ -593,13 +628,16 @@ __device__ __forceinline__ void put_columns(int i, float4 s, int padded, int col
 // kParts: a team is a part of a warp (or all of it), otherwise whole warps; a block has 512 threads' worth of teams.
 // V > 1 (wide rows): the team is the block, and the column sums lie in shared memory, each thread's its own, since the
 // registers hold V granules of dy and h; with V > 2 the weight is read from the cache as well.
-// kPlain as in the forward pass.  With registers to spare (kAhead) the next rows are on their way while these are
-// worked on.  A team takes `group` neighbouring rows (R, or R = 1 at a time), then the group that is a step away.
+// kPlain and kStaged as in the forward pass (staged bfloat16 rows took 75 us where shifted pieces take 44); with
+// registers to spare (kAhead) the next rows are on their way while these are worked on.  Staged rows have `slots` places
+// a team: 4 with the next row copied meanwhile, 2, or 1 for dy and h in turn.  A team takes `group` neighbouring rows (R, or R = 1 at a time), then the group that is a step away.
 template <int kType, int V, int R, bool kParts, bool kFused, bool kPlain>
 __global__ void __launch_bounds__(kMaxTeam)
-norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, const BackwardSteps step, int hist_words) {
-    constexpr bool kAhead = V == 1 || (V == 2 && kPlain);
-    extern __shared__ __align__(16) uint32_t dynamic[];  // [hist_words] histogram, then the column sums of the block
+norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, const BackwardSteps step, int hist_words, int sum_words,
+                          int slots) {
+    constexpr bool kStaged = !kPlain && kType == QFMT_F32;
+    constexpr bool kAhead = (kPlain && V <= 2) || (!kPlain && !kStaged && V == 1);
+    extern __shared__ __align__(16) uint32_t dynamic[];  // [hist_words] histogram, [sum_words] the block's column sums, places for rows
     __shared__ __align__(16) float scratch[kParts ? 1 : kMaxTeam / 64][2][64];
     grid_launch_dependents();
     grid_dependency_wait();
@@ -616,13 +654,11 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
     const uint64_t offset = kFused ? drop_offset(a.drop) : 0ull;
     const int next = team * kGranule;  // elements between a thread's granules
     int n[V];
-    bool edge[V];
     Granule w[V <= 2 ? V : 1], dw = splat(0.0f), db = splat(0.0f);  // the sums with V = 1
     float4* const sums_in_shared = reinterpret_cast<float4*>(dynamic + hist_words);  // with V > 1: [V][4][team]
 #pragma unroll
     for (int k = 0; k < V; ++k) {
         n[k] = granule_columns(a.cols, k * team + t);
-        edge[k] = at_edge(a.cols, k * team + t);
         if (V > 1) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) sums_in_shared[(4 * k + i) * team + t] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -630,10 +666,10 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
     }
     const uint32_t rows = (uint32_t)a.rows, stride = gridDim.x * teams * group;
     uint32_t row = (blockIdx.x * teams + mine) * group;
-    const auto* pdy = a.dy.p + row * a.dy.ld + t * kGranule;
-    const auto* ph = a.h.p + row * a.h.ld + t * kGranule;
+    const auto* pdy = a.dy.p + row * a.dy.ld + (kStaged ? 0 : t * kGranule);
+    const auto* ph = a.h.p + row * a.h.ld + (kStaged ? 0 : t * kGranule);
     GradientRow<kType> to(a, row, t * kGranule);
-    OnItsWay<kType, kPlain> raw_dy[R][V], raw_h[R][V];
+    OnItsWay<kType, kPlain || kStaged> raw_dy[R][V], raw_h[R][V];
     float mean[R], rstd[R];
     const auto fetch_rows = [&](uint32_t at) {
 #pragma unroll
@@ -641,23 +677,75 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
             const bool there = at + i < rows;
             mean[i] = there ? __ldg(a.mean + at + i) : 0.0f;
             rstd[i] = there ? __ldg(a.rstd + at + i) : 0.0f;
+            if constexpr (!kStaged) {
 #pragma unroll
-            for (int k = 0; k < V; ++k) {
-                raw_dy[i][k] = start<kType, kPlain>(pdy + i * a.dy.ld + k * next, n[k], at + i, rows, edge[k]);
-                raw_h[i][k] = start<kType, kPlain>(ph + i * a.h.ld + k * next, n[k], at + i, rows, edge[k]);
+                for (int k = 0; k < V; ++k) {
+                    const bool edge = at_edge(a.cols, k * team + t);
+                    raw_dy[i][k] = start<kType, kPlain>(pdy + i * a.dy.ld + k * next, n[k], at + i, rows, edge);
+                    raw_h[i][k] = start<kType, kPlain>(ph + i * a.h.ld + k * next, n[k], at + i, rows, edge);
+                }
             }
         }
     };
+    const uint32_t row_bytes = staged_row_bytes(a.cols);
+    const uint32_t places = shared_address(dynamic + hist_words + sum_words) + mine * slots * row_bytes;
+    const auto stage = [&](uint32_t at, uint32_t place, const auto* p) {
+        if constexpr (kStaged) if (at < rows) stage_row(place, p, (int)a.cols, t, team);
+    };
+    const auto arrived = [&]() {  // every thread's copies, for the whole team
+        if constexpr (V > 1) __syncthreads();
+        else if constexpr (kParts) __syncwarp();
+        else asm volatile("bar.sync %0, %1;" ::"r"(1 + mine), "r"(team) : "memory");
+    };
+    uint32_t half = 0;
     // rows to the next one: a step, or with R = 1 one row within a group
     const bool pairs = R == 1 && group == 2;
     const auto advance = [&](bool second, auto*& p, int64_t ld, int64_t by) { p += pairs ? (second ? by - ld : ld) : by; };
     if (kAhead) fetch_rows(row);
+    if (kStaged && slots == 4) {
+        stage(row, places, pdy);
+        stage(row, places + row_bytes, ph);
+        stage_end();
+    }
 #pragma unroll
     for (int k = 0; k < (V <= 2 ? V : 0); ++k) w[k] = load_columns(a.weight, k * team + t, n[k], 1.0f);
     int parity = 0;
     bool second = false;
     for (uint32_t first = blockIdx.x * teams * group; first < rows; parity ^= 1) {  // the row of the block's first team
+        const uint32_t by = pairs ? (second ? stride - 1 : 1) : stride;
         if (!kAhead) fetch_rows(row);
+        if constexpr (kStaged) {
+            const bool there = row < rows;
+            if (slots == 4) {
+                advance(second, pdy, a.dy.ld, step.dy);
+                advance(second, ph, a.h.ld, step.h);
+                const uint32_t place = places + (half ^ 1u) * 2 * row_bytes;
+                stage(row + by, place, pdy);
+                stage(row + by, place + row_bytes, ph);
+                stage_end();
+                stage_wait<1>();
+            } else {
+                stage(row, places, ph);
+                if (slots == 2) stage(row, places + row_bytes, pdy);
+                stage_end();
+                stage_wait<0>();
+            }
+            arrived();
+            const uint32_t place_h = slots == 4 ? places + (2 * half + 1) * row_bytes : places;
+            const uint32_t place_dy = slots == 4 ? places + 2 * half * row_bytes : slots == 2 ? places + row_bytes : places;
+#pragma unroll
+            for (int k = 0; k < V; ++k) raw_h[0][k] = staged_granule(place_h, k * team + t, there ? n[k] : 0);
+            if (slots == 1) {
+                arrived();  // h has been read by everyone
+                stage(row, places, pdy);
+                stage_end();
+                stage_wait<0>();
+                arrived();
+            }
+#pragma unroll
+            for (int k = 0; k < V; ++k) raw_dy[0][k] = staged_granule(place_dy, k * team + t, there ? n[k] : 0);
+            if (slots == 4) half ^= 1u;
+        }
         Granule dy[R][V], xhat[R][V];
         float2 s[R];
         float this_rstd[R];
@@ -668,9 +756,10 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 const int there = row + i < rows ? n[k] : 0;  // a row that does not exist adds nothing to the column sums
-                dy[i][k] = widen_raw<kType>(words<kType, kPlain>(raw_dy[i][k], pdy + i * a.dy.ld + k * next, there));
-                xhat[i][k] = normalise<kPlain>(widen_raw<kType>(words<kType, kPlain>(raw_h[i][k], ph + i * a.h.ld + k * next, there)),
-                                               mean[i], rstd[i], there);
+                const Raw<kType> ds = words<kType, kPlain || kStaged>(raw_dy[i][k], pdy + i * a.dy.ld + k * next, there);
+                const Raw<kType> hs = words<kType, kPlain || kStaged>(raw_h[i][k], ph + i * a.h.ld + k * next, there);
+                dy[i][k] = widen_raw<kType>(ds);
+                xhat[i][k] = normalise<kPlain>(widen_raw<kType>(hs), mean[i], rstd[i], there);
                 if (V > 2) w[0] = load_columns(a.weight, k * team + t, n[k], 1.0f);
                 s[i] = add2(s[i], row_sums(dy[i][k], xhat[i][k], w[V <= 2 ? k : 0]));
                 if constexpr (V == 1) {
@@ -683,9 +772,10 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
                 }
             }
         }
-        const uint32_t by = pairs ? (second ? stride - 1 : 1) : stride;
-        advance(second, pdy, a.dy.ld, step.dy);
-        advance(second, ph, a.h.ld, step.h);
+        if (!kStaged || slots != 4) {
+            advance(second, pdy, a.dy.ld, step.dy);
+            advance(second, ph, a.h.ld, step.h);
+        }
         if (kAhead) fetch_rows(row + by);
         if constexpr (kParts) {
             for (int off = team >> 1; off > 0; off >>= 1) {
@@ -714,6 +804,7 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
     }
     if (hist != nullptr) flush_hist(hist, a.quant, a.stats, (uint64_t)a.rows * (uint64_t)a.cols);
     const bool alone = a.dweight != nullptr || a.dbias != nullptr;  // this block's part is the result
+    if (kStaged) stage_wait<0>();
     if (a.partial == nullptr) return;
     // [dweight, dbias][padded columns] of every warp of small teams, or of every team; then their sum
     const int padded = ((int)a.cols + kGranule - 1) / kGranule * kGranule, quads = padded / 2;
@@ -809,7 +900,7 @@ Plan backward_plan(int64_t cols) { return make_plan(cols, 1, 4); }
 // which has a block on each of a B200's SMs, or a share of the rows for long rows.
 constexpr int kMaxParts = 148;
 int row_parts(const qfmt_norm_t& s) {
-    if (backward_plan(s.cols).team != 0) return kMaxParts;
+    if (backward_plan(s.cols).team != 0) return kMaxParts;  // more than the loop would need
     const int64_t want = (s.rows + 8 * kColumnWarps - 1) / (8 * kColumnWarps);
     return (int)(want < 64 ? (want > 0 ? want : 1) : 64);
 }
@@ -862,13 +953,36 @@ bool plain_layout(int64_t cols, std::initializer_list<bool> whole) {
     return cols % kGranule == 0 && std::all_of(whole.begin(), whole.end(), [](bool w) { return w; });
 }
 
+constexpr size_t kMostShared = 216 * 1024;  // dynamic, beside the kernels' own few KiB
+
+// Raises a kernel's limit of dynamic shared memory, once on every GPU.
+template <typename K>
+int allow_shared(K kernel, size_t bytes, const DeviceInfo& dev, std::atomic<bool>* allowed) {
+    const bool known = dev.ordinal >= 0 && dev.ordinal < 64;
+    if (known && allowed[dev.ordinal].load()) return QFMT_OK;
+    QFMT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    if (known) allowed[dev.ordinal].store(true);
+    return QFMT_OK;
+}
+
 template <int kType, int V, int R, bool kFused, bool kPlain>
 int launch_forward_rows(const Call& c, const ForwardArgs<kType>& a, int team, cudaStream_t stream) {
-    static std::atomic<int> known[kMaxTeam / 32 + 1];
+    static std::atomic<uint64_t> known[kMaxTeam / 32 + 1];
     const auto kern = norm_forward_rows_kernel<kType, V, R, kFused, kPlain>;
     const unsigned teams = V > 1 ? 1 : 128 / team, block = teams * team;
+    // places for rows in shared memory: two for every tensor, one where two are too many
+    const int tensors = kFused ? 2 : 1;
+    constexpr bool kStaged = !kPlain && kType == QFMT_F32;
+    const size_t place = (size_t)teams * tensors * staged_row_bytes(a.cols);
+    const int slots = !kStaged ? 0 : c.hist_bytes + 2 * place <= kMostShared / 2 ? 2 * tensors : tensors;
+    const size_t smem = c.hist_bytes + place * slots / tensors;
+    static std::atomic<bool> allowed[64];
+    if (kStaged) {
+        const int rc = allow_shared(kern, kMostShared, c.dev, allowed);
+        if (rc != QFMT_OK) return rc;
+    }
     int resident = 0;
-    const int rc = resident_blocks(kern, block, c.hist_bytes, known, &resident);
+    const int rc = resident_blocks(kern, block, smem, known, &resident);
     if (rc != QFMT_OK) return rc;
     const int64_t want = (a.rows + teams * R - 1) / (teams * R), cap = (int64_t)c.dev.sm_count * resident;
     // two rows at a time only where every team has them
@@ -878,7 +992,7 @@ int launch_forward_rows(const Call& c, const ForwardArgs<kType>& a, int team, cu
     const unsigned blocks = (unsigned)(want < cap ? want : cap);
     const int64_t stride = (int64_t)blocks * teams * R;
     const ForwardSteps step = {stride * a.x.ld, stride * a.residual.ld, stride * a.h.ld, stride * a.y.ld};
-    QFMT_CUDA_TRY(launch_overlapping(kern, blocks, block, c.hist_bytes, stream, a, team, step));
+    QFMT_CUDA_TRY(launch_overlapping(kern, blocks, block, smem, stream, a, team, step, (int)(c.hist_bytes / 4), slots));
     return QFMT_OK;
 }
 
@@ -960,6 +1074,13 @@ int join_parts(const float* partial, int parts, int64_t cols, float* d_dweight, 
     return QFMT_OK;
 }
 
+// Shared memory for the column sums of a block of the backward pass.
+size_t backward_sum_bytes(int v, bool parts, int team, int64_t cols) {
+    if (v > 1) return (size_t)team * v * 64;
+    const int units = parts ? kMaxTeam / team * team / 32 : kMaxTeam / team;
+    return units > 1 ? 2 * sizeof(float) * (size_t)padded_columns(cols) * units : 0;
+}
+
 template <int kType, int V, int R, bool kParts, bool kFused, bool kPlain>
 int launch_backward_rows(const Call& c, BackwardArgs<kType> a, int team, int group, float* d_dweight, float* d_dbias, cudaStream_t stream) {
     const unsigned teams = kMaxTeam / team, block = teams * team;
@@ -968,18 +1089,19 @@ int launch_backward_rows(const Call& c, BackwardArgs<kType> a, int team, int gro
     const bool alone = a.partial != nullptr && blocks == 1;
     if (alone) a.dweight = d_dweight, a.dbias = d_dbias;
     const auto kern = norm_backward_rows_kernel<kType, V, R, kParts, kFused, kPlain>;
-    const unsigned units = kParts ? block / 32 : teams;
-    const size_t smem = c.hist_bytes + (V > 1       ? (size_t)block * V * 64
-                                        : units > 1 ? 2 * sizeof(float) * (size_t)padded_columns(a.cols) * units : 0);
+    constexpr bool kStaged = !kPlain && kType == QFMT_F32;
+    const size_t place = (size_t)teams * staged_row_bytes(a.cols);
+    const size_t sums = backward_sum_bytes(V, kParts, team, a.cols), rest = c.hist_bytes + sums;
+    const int slots = !kStaged ? 0 : rest + 4 * place <= kMostShared ? 4 : rest + 2 * place <= kMostShared ? 2 : 1;
+    // More than half of what an SM has: its one block must not be joined by a second of the same launch, which would
+    // leave another SM without work (launches overlap, so SMs come free at different times).
+    const size_t smem = std::max(rest + slots * place, (size_t)116 * 1024);
     static std::atomic<bool> allowed[64];
-    if (c.dev.ordinal < 0 || c.dev.ordinal >= 64 || !allowed[c.dev.ordinal].load()) {
-        QFMT_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                           (V > 1 ? V * 32 + 40 : 72) * 1024));  // histogram and sums
-        if (c.dev.ordinal >= 0 && c.dev.ordinal < 64) allowed[c.dev.ordinal].store(true);
-    }
+    const int rc = allow_shared(kern, kMostShared, c.dev, allowed);
+    if (rc != QFMT_OK) return rc;
     const int64_t stride = (int64_t)blocks * teams * group;
     const BackwardSteps step = {stride * a.dy.ld, stride * a.h.ld, stride * a.dh.ld, stride * a.dx.ld, stride * a.dresidual.ld};
-    QFMT_CUDA_TRY(launch_overlapping(kern, blocks, block, smem, stream, a, team, group, step, (int)(c.hist_bytes / sizeof(uint32_t))));
+    QFMT_CUDA_TRY(launch_overlapping(kern, blocks, block, smem, stream, a, team, group, step, (int)(c.hist_bytes / 4), (int)(sums / 4), slots));
     return a.partial != nullptr && !alone ? join_parts(a.partial, (int)blocks, a.cols, d_dweight, d_dbias, stream) : QFMT_OK;
 }
 
@@ -987,8 +1109,11 @@ template <int kType, bool kFused>
 int launch_backward(const Call& c, const BackwardArgs<kType>& a, float* d_dweight, float* d_dbias, cudaStream_t stream) {
     if (a.rows == 0) return join_parts(a.partial, 0, a.cols, d_dweight, d_dbias, stream);  // zeros
     const Plan plan = backward_plan(a.cols);
-    if (plan.team != 0) {
-        const bool plain = plain_layout(a.cols, {a.dy.whole, a.dh.whole, a.h.whole, a.dx.whole, a.dresidual.whole}) && !a.fmt;
+    const bool plain = plain_layout(a.cols, {a.dy.whole, a.dh.whole, a.h.whole, a.dx.whole, a.dresidual.whole}) && !a.fmt;
+    // (the widest rows with a histogram of 256 bins leave no place for a row)
+    const bool fits = plain || plan.granules < 3 || kType != QFMT_F32 ||
+                      c.hist_bytes + backward_sum_bytes(plan.granules, false, plan.team, a.cols) + staged_row_bytes(a.cols) <= kMostShared;
+    if (plan.team != 0 && fits) {
         // Two neighbouring rows to a team where every team gets some: a rule on sizes alone, since it decides the order
         // of the sums over rows.  Whether the two are worked on at once does not.
         const int64_t teams = (int64_t)(kMaxTeam / plan.team) * std::min(c.dev.sm_count, kMaxParts);
