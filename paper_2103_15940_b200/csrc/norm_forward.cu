@@ -1,0 +1,441 @@
+// Layer normalisation and its fused form, forward: y = LN(x), or h = residual + D(x) and y = LN(h) in one pass.
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "norm.cuh"
+
+namespace qfmt {
+namespace {
+
+template <int kType>
+struct ForwardArgs {
+    Source<kType> x, residual;  // residual.p may be NULL
+    const float* weight;
+    const float* bias;
+    Target<kType> h, y;  // h.p may be NULL
+    float* mean;
+    float* rstd;
+    int64_t rows, cols;
+    float eps;
+    float inverse;  // 1 / cols
+    bool fmt;       // quant holds a format to round to
+    DropParams drop;
+    QuantParams quant;
+    qfmt_stats_t* stats;
+};
+
+// residual + D(x)
+template <int kType, bool kFused>
+__device__ __forceinline__ Granule join_h(const ForwardArgs<kType>& a, const Raw<kType>& x, const Raw<kType>& r, uint64_t offset, uint32_t row,
+                                          uint32_t g) {
+    Granule v = widen_raw<kType>(x);
+    if constexpr (kFused) {
+        if (a.drop.active) drop_granule(a.drop, offset, row, g, v);
+        if (a.residual.p != nullptr) {
+            const Granule u = widen_raw<kType>(r);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v.p[j] = add2(u.p[j], v.p[j]);
+        }
+    }
+    return v;
+}
+
+__device__ __forceinline__ float sum8(const Granule& v) {
+    const float2 s = add2(add2(v.p[0], v.p[1]), add2(v.p[2], v.p[3]));
+    return s.x + s.y;
+}
+// v - mean where a column exists, 0 elsewhere; the sum of its squares.  kPlain: all eight exist or (v = 0) none.
+template <bool kPlain>
+__device__ __forceinline__ float centre(Granule& v, float mean, int n) {
+    const float2 shift = both(kPlain && n == 0 ? 0.0f : -mean);
+    float2 s = make_float2(0.0f, 0.0f);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        v.p[j] = add2(v.p[j], shift);
+        if (!kPlain && 2 * j >= n) v.p[j].x = 0.0f;
+        if (!kPlain && 2 * j + 1 >= n) v.p[j].y = 0.0f;
+        s = fma2(v.p[j], v.p[j], s);
+    }
+    return s.x + s.y;
+}
+
+// 1 / sqrt(v): the hardware's approximation, within 2^-22.9 of it.
+__device__ __forceinline__ float inverse_root(float v) {
+    float r;
+    asm("rsqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+
+// Rows too long for a team's registers: a block takes a row at a time and reads it three times, for the mean,
+// for the variance and for the result.
+template <int kType, bool kFused>
+__global__ void __launch_bounds__(kLoopThreads) norm_forward_loop_kernel(const ForwardArgs<kType> a) {
+    extern __shared__ uint32_t lane_hist[];
+    __shared__ float2 scratch[32];
+    grid_dependency_wait();
+    uint32_t* hist = a.stats != nullptr ? lane_hist : nullptr;
+    if (hist != nullptr) clear_hist(hist, a.quant);
+    const uint32_t granules = (uint32_t)((a.cols + kGranule - 1) / kGranule);
+    const float count = (float)a.cols;
+    const uint64_t offset = kFused ? drop_offset(a.drop) : 0ull;
+    const bool from = threadIdx.x & 31, to = (threadIdx.x & 31) != 31;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const auto h = [&](uint32_t g, int n) {
+            const int64_t col = (int64_t)g * kGranule;
+            const bool inside = (row != 0 && row + 1 != a.rows) || !at_edge(a.cols, g);
+            const Raw<kType> res = kFused && a.residual.p != nullptr
+                                       ? load_any<kType>(a.residual.p + row * a.residual.ld + col, n, inside) : Raw<kType>();
+            return join_h<kType, kFused>(a, load_any<kType>(a.x.p + row * a.x.ld + col, n, inside), res, offset, (uint32_t)row, g);
+        };
+        float sum = 0.0f;
+        for (uint32_t g = threadIdx.x; g < granules; g += kLoopThreads) sum += sum8(h(g, granule_columns(a.cols, g)));
+        const float mean = block_sum(make_float2(sum, 0.0f), scratch).x / count;
+        sum = 0.0f;
+        for (uint32_t g = threadIdx.x; g < granules; g += kLoopThreads) {
+            const int n = granule_columns(a.cols, g);
+            Granule v = h(g, n);
+            sum += centre<false>(v, mean, n);
+        }
+        const float rstd = inverse_root(block_sum(make_float2(sum, 0.0f), scratch).x / count + a.eps);
+        if (threadIdx.x == 0) {
+            if (a.mean != nullptr) a.mean[row] = mean;
+            if (a.rstd != nullptr) a.rstd[row] = rstd;
+        }
+        for (uint32_t g0 = 0; g0 < granules; g0 += kLoopThreads) {  // whole warps
+            const uint32_t g = g0 + threadIdx.x;
+            const int64_t col = (int64_t)g * kGranule;
+            const int n = granule_columns(a.cols, g);
+            Granule v = h(g, n);
+            if (kFused && a.h.p != nullptr) store_any<kType>(a.h.p + row * a.h.ld + col, n, a.h, finish<kType>(v), from, to);
+            const Granule w = load_columns(a.weight, g, n, 1.0f), b = load_columns(a.bias, g, n, 0.0f);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v.p[j] = fma2(mul2(add2(v.p[j], both(-mean)), both(rstd)), w.p[j], b.p[j]);
+            store_any<kType>(a.y.p + row * a.y.ld + col, n, a.y, finish_output<kType, false>(a, v, n, hist), from, to);
+        }
+    }
+    if (hist != nullptr) flush_hist(hist, a.quant, a.stats, (uint64_t)a.rows * (uint64_t)a.cols);
+}
+
+// Sums over a team, in every thread and in a fixed order: of one value, or of two at once.  kBlock: the team is the
+// block.  One barrier, so the next sum needs another scratch.
+template <bool kBlock>
+__device__ __forceinline__ void team_sum(float (&s)[1], int team, int t, float* scratch) {
+    if constexpr (!kBlock) {
+        for (int off = team >> 1; off > 0; off >>= 1) s[0] = across(s[0], off);
+    } else {
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) s[0] = across(s[0], off);
+        if (team == 32) return;
+        if ((t & 31) == 0) scratch[t >> 5] = s[0];
+        __syncthreads();
+        sum_entries<1>(scratch, team, s);
+    }
+}
+// Two values: after one exchange the lower half of a warp holds the first value's partial sums and the upper half
+// the second's, so five shuffles do for both.
+template <bool kBlock>
+__device__ __forceinline__ void team_sum(float (&s)[2], int team, int t, float* scratch) {
+    if constexpr (!kBlock) {
+        for (int off = team >> 1; off > 0; off >>= 1) s[0] = across(s[0], off), s[1] = across(s[1], off);
+    } else {
+        const bool upper = t & 16;
+        float u = (upper ? s[1] : s[0]) + __shfl_xor_sync(0xFFFFFFFFu, upper ? s[0] : s[1], 16);
+#pragma unroll
+        for (int off = 8; off > 0; off >>= 1) u = across(u, off);
+        if (team == 32) {
+            const float v = __shfl_xor_sync(0xFFFFFFFFu, u, 16);
+            s[0] = upper ? v : u;
+            s[1] = upper ? u : v;
+            return;
+        }
+        if ((t & 15) == 0) scratch[(t & 16) + (t >> 5)] = u;
+        __syncthreads();
+        sum_entries<2>(scratch, team, s);
+    }
+}
+
+// Elements from a row of a team to its next one.
+struct ForwardSteps {
+    int64_t x, residual, h, y;
+};
+
+// R rows at a time are read once and stay in their team's registers.  V <= 2: so do the team's weight and bias,
+// from row to row.  V > 2: longer rows, without them.
+// kPlain: every granule whole and aligned, no format; granules go straight to registers, with V <= 2 those of the next
+// rows while these are worked on.  Otherwise any layout and an optional format: codes come as aligned pieces that are
+// shifted into place; rows of containers (kStaged) go through shared memory behind the histogram, in `slots` places a
+// team (twice the tensors that are read: the next row is copied meanwhile).  Each way is the faster one for its type:
+// 16384 rows of 1021 take 28 us as shifted bfloat16 pieces and 31 us staged, as fp32 39 us shifted and 33 us staged.
+template <int kType, int V, int R, bool kFused, bool kPlain>
+__global__ void __launch_bounds__(kMaxTeam)
+norm_forward_rows_kernel(const ForwardArgs<kType> a, int team, const ForwardSteps step, int hist_words, int slots) {
+    constexpr bool kKeep = V <= 2;
+    constexpr bool kAhead = kKeep && kPlain, kStaged = !kPlain && kType == QFMT_F32;
+    extern __shared__ __align__(16) uint32_t dynamic[];
+    __shared__ __align__(16) float scratch[2][R][16];
+    grid_launch_dependents();
+    grid_dependency_wait();
+    uint32_t* hist = !kPlain && a.stats != nullptr ? dynamic : nullptr;
+    if (V > 1) {
+        for (int i = threadIdx.x; i < 2 * R * 16; i += blockDim.x) (&scratch[0][0][0])[i] = 0.0f;
+        __syncthreads();
+    }
+    if (hist != nullptr) clear_hist(hist, a.quant);
+    const int mine = V > 1 ? 0 : threadIdx.x / team, t = threadIdx.x - mine * team, teams = V > 1 ? 1 : blockDim.x / team;
+    const bool from = (t & 31) != 0, to = (t & 31) != 31 && t + 1 < team;  // the lanes before and after hold neighbours
+    const uint64_t offset = kFused ? drop_offset(a.drop) : 0ull;
+    const bool residual = kFused && a.residual.p != nullptr;
+    const int next = team * kGranule;  // elements between a thread's granules
+    int n[V];                          // columns of each granule
+#pragma unroll
+    for (int k = 0; k < V; ++k) n[k] = granule_columns(a.cols, k * team + t);
+
+    // A team past the last row, whose warp has teams with one, keeps in step with them and stores nothing.
+    const uint32_t rows = (uint32_t)a.rows, stride = gridDim.x * teams * R;
+    uint32_t row = (blockIdx.x * teams + mine) * R;
+    const auto* px = a.x.p + row * a.x.ld + (kStaged ? 0 : t * kGranule);
+    const auto* pr = a.residual.p + row * a.residual.ld + (kStaged ? 0 : t * kGranule);
+    auto* ph = a.h.p + row * a.h.ld + t * kGranule;
+    auto* py = a.y.p + row * a.y.ld + t * kGranule;
+    OnItsWay<kType, kPlain || kStaged> x[R][V], r[R][V];
+    const auto fetch_rows = [&](uint32_t at) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                const bool edge = at_edge(a.cols, k * team + t);
+                x[i][k] = start<kType, kPlain || kStaged>(px + i * a.x.ld + k * next, n[k], at + i, rows, edge);
+                if (kFused)
+                    r[i][k] = start<kType, kPlain || kStaged>(pr + i * a.residual.ld + k * next, residual ? n[k] : 0, at + i, rows, edge);
+            }
+        }
+        if (kAhead) px += step.x, pr += step.residual;
+    };
+    const uint32_t row_bytes = staged_row_bytes(a.cols);
+    const uint32_t places = shared_address(dynamic + hist_words) + mine * slots * row_bytes;
+    const int tensors = kFused ? 2 : 1;
+    uint32_t half = 0;
+    const auto stage_rows = [&]([[maybe_unused]] uint32_t at, [[maybe_unused]] uint32_t to_half) {  // the next row through shared memory
+        if constexpr (kStaged) if (at < rows) {
+            const uint32_t place = places + to_half * tensors * row_bytes;
+            stage_row(place, px, (int)a.cols, t, team);
+            if (residual) stage_row(place + row_bytes, pr, (int)a.cols, t, team);
+        }
+        stage_end();
+        px += step.x;
+        pr += step.residual;
+    };
+    const bool ahead = slots > tensors;
+    if (kAhead) fetch_rows(row);
+    if (kStaged && ahead) stage_rows(row, 0);
+    Granule w[kKeep ? V : 1], b[kKeep ? V : 1];
+    if constexpr (kKeep) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            w[k] = load_columns(a.weight, k * team + t, n[k], 1.0f);
+            b[k] = load_columns(a.bias, k * team + t, n[k], 0.0f);
+        }
+    }
+    for (; row - mine * R < rows; row += stride) {
+        if constexpr (kStaged) {
+            stage_rows(ahead ? row + stride : row, ahead ? half ^ 1u : 0u);
+            if (ahead) stage_wait<1>();
+            else stage_wait<0>();
+            if (V > 1) __syncthreads();
+            else __syncwarp();
+            const uint32_t place = places + half * tensors * row_bytes;
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                const int there = row < rows ? n[k] : 0;
+                x[0][k] = staged_granule(place, k * team + t, there);
+                if (kFused) r[0][k] = staged_granule(place + row_bytes, k * team + t, residual ? there : 0);
+            }
+            if (ahead) half ^= 1u;
+        } else if (!kAhead) {
+            fetch_rows(row);
+        }
+        Granule v[R][V];
+        float mean[R], rstd[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                const int there = row + i < rows ? n[k] : 0;
+                const Raw<kType> xs = words<kType, kPlain || kStaged>(x[i][k], px + i * a.x.ld + k * next, there);
+                const Raw<kType> rs = kFused ? words<kType, kPlain || kStaged>(r[i][k], pr + i * a.residual.ld + k * next, residual ? there : 0)
+                                             : Raw<kType>();
+                v[i][k] = join_h<kType, kFused>(a, xs, rs, offset, row + i, k * team + t);
+            }
+        if (kAhead) fetch_rows(row + stride);
+        else if (!kStaged) px += step.x, pr += step.residual;
+        if (kFused && a.h.p != nullptr) {
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+#pragma unroll
+                for (int k = 0; k < V; ++k)
+                    put<kType, kPlain>(ph + i * a.h.ld + k * next, row + i < rows ? n[k] : 0, a.h, finish<kType>(v[i][k]), from, to);
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            mean[i] = sum8(v[i][0]);
+#pragma unroll
+            for (int k = 1; k < V; ++k) mean[i] += sum8(v[i][k]);
+        }
+        team_sum<(V > 1)>(mean, team, t, scratch[0][0]);
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            mean[i] *= a.inverse;
+            rstd[i] = centre<kPlain>(v[i][0], mean[i], n[0]);
+#pragma unroll
+            for (int k = 1; k < V; ++k) rstd[i] += centre<kPlain>(v[i][k], mean[i], n[k]);
+        }
+        team_sum<(V > 1)>(rstd, team, t, scratch[1][0]);
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            rstd[i] = inverse_root(rstd[i] * a.inverse + a.eps);
+            if (t == 0 && row + i < rows) {
+                if (a.mean != nullptr) a.mean[row + i] = mean[i];
+                if (a.rstd != nullptr) a.rstd[row + i] = rstd[i];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            if constexpr (!kKeep) {
+                w[0] = load_columns(a.weight, k * team + t, n[k], 1.0f);
+                b[0] = load_columns(a.bias, k * team + t, n[k], 0.0f);
+            }
+            const Granule& wk = w[kKeep ? k : 0];
+            const Granule& bk = b[kKeep ? k : 0];
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[i][k].p[j] = fma2(mul2(v[i][k].p[j], both(rstd[i])), wk.p[j], bk.p[j]);
+                const int there = row + i < rows ? n[k] : 0;
+                put<kType, kPlain>(py + i * a.y.ld + k * next, there, a.y, finish_output<kType, kPlain>(a, v[i][k], there, hist), from, to);
+            }
+        }
+        ph += step.h;
+        py += step.y;
+    }
+    if (hist != nullptr) flush_hist(hist, a.quant, a.stats, (uint64_t)a.rows * (uint64_t)a.cols);
+}
+
+Plan forward_plan(int64_t cols) { return make_plan(cols, 2, 4); }
+
+template <int kType, int V, int R, bool kFused, bool kPlain>
+int launch_forward_rows(const Call& c, const ForwardArgs<kType>& a, int team, cudaStream_t stream) {
+    static std::atomic<uint64_t> known[kMaxTeam / 32 + 1];
+    const auto kern = norm_forward_rows_kernel<kType, V, R, kFused, kPlain>;
+    const unsigned teams = V > 1 ? 1 : 128 / team, block = teams * team;
+    // places for rows in shared memory: two for every tensor, one where two are too many
+    const int tensors = kFused ? 2 : 1;
+    constexpr bool kStaged = !kPlain && kType == QFMT_F32;
+    const size_t place = (size_t)teams * tensors * staged_row_bytes(a.cols);
+    const int slots = !kStaged ? 0 : c.hist_bytes + 2 * place <= kMostShared / 2 ? 2 * tensors : tensors;
+    const size_t smem = c.hist_bytes + place * slots / tensors;
+    static std::atomic<bool> allowed[64];
+    if (kStaged) {
+        const int rc = allow_shared(kern, kMostShared, c.dev, allowed);
+        if (rc != QFMT_OK) return rc;
+    }
+    int resident = 0;
+    const int rc = resident_blocks(kern, block, smem, known, &resident);
+    if (rc != QFMT_OK) return rc;
+    const int64_t want = (a.rows + teams * R - 1) / (teams * R), cap = (int64_t)c.dev.sm_count * resident;
+    // two rows at a time only where every team has them
+    if constexpr (R == 2) {
+        if (want < cap) return launch_forward_rows<kType, V, 1, kFused, kPlain>(c, a, team, stream);
+    }
+    const unsigned blocks = (unsigned)(want < cap ? want : cap);
+    const int64_t stride = (int64_t)blocks * teams * R;
+    const ForwardSteps step = {stride * a.x.ld, stride * a.residual.ld, stride * a.h.ld, stride * a.y.ld};
+    QFMT_CUDA_TRY(launch_overlapping(kern, blocks, block, smem, stream, a, team, step, (int)(c.hist_bytes / 4), slots));
+    return QFMT_OK;
+}
+
+template <int kType, bool kFused>
+int launch_forward(const Call& c, const ForwardArgs<kType>& a, cudaStream_t stream) {
+    const Plan plan = forward_plan(a.cols);
+    if (plan.team != 0) {
+        const bool plain = plain_layout(a.cols, {a.x.whole, a.residual.whole, a.h.whole, a.y.whole}) && !a.fmt;
+        constexpr int kRows = kFused && kType == QFMT_F32 ? 1 : 2;  // two wide fp32 rows of x and residual do not fit
+        const auto run = plain ? (plan.granules == 1   ? launch_forward_rows<kType, 1, 2, kFused, true>
+                                  : plan.granules == 2 ? launch_forward_rows<kType, 2, kRows, kFused, true>
+                                  : plan.granules == 3 ? launch_forward_rows<kType, 3, 1, kFused, true>
+                                                       : launch_forward_rows<kType, 4, 1, kFused, true>)
+                               : (plan.granules == 1   ? launch_forward_rows<kType, 1, 1, kFused, false>
+                                  : plan.granules == 2 ? launch_forward_rows<kType, 2, 1, kFused, false>
+                                  : plan.granules == 3 ? launch_forward_rows<kType, 3, 1, kFused, false>
+                                                       : launch_forward_rows<kType, 4, 1, kFused, false>);
+        return run(c, a, plan.team, stream);
+    }
+    const int64_t cap = (int64_t)c.dev.sm_count * 4;
+    QFMT_CUDA_TRY(launch_overlapping(norm_forward_loop_kernel<kType, kFused>, (unsigned)(a.rows < cap ? a.rows : cap), kLoopThreads,
+                                     c.hist_bytes, stream, a));
+    return QFMT_OK;
+}
+
+template <int kType, bool kFused>
+int forward(const Call& c, const void* d_x, const void* d_residual, const float* d_weight, const float* d_bias, void* d_h,
+            void* d_y, float* d_mean, float* d_rstd, qfmt_stats_t* d_stats, cudaStream_t stream) {
+    const qfmt_norm_t& s = c.norm;
+    ForwardArgs<kType> a;
+    a.x = make_source<kType>(d_x, s.ld_x);
+    a.residual = make_source<kType>(d_residual, s.ld_residual);
+    a.weight = d_weight;
+    a.bias = d_bias;
+    a.h = make_target<kType>(d_h, s.ld_h);
+    a.y = make_target<kType>(d_y, s.ld_y);
+    a.mean = d_mean;
+    a.rstd = d_rstd;
+    a.rows = s.rows;
+    a.cols = s.cols;
+    a.eps = s.eps;
+    a.inverse = 1.0f / (float)a.cols;
+    a.fmt = c.fmt;
+    a.drop = c.drop;
+    a.quant = c.quant;
+    a.stats = d_stats;
+    return launch_forward<kType, kFused>(c, a, stream);
+}
+
+int forward_entry(const qfmt_norm_t* norm, const qfmt_dropout_t* drop, bool fused, const void* d_x, const void* d_residual,
+                  const float* d_weight, const float* d_bias, void* d_h, void* d_y, float* d_mean, float* d_rstd,
+                  const qfmt_format_t* fmt, qfmt_stats_t* d_stats, int accumulate, cudaStream_t stream) {
+    Call c;
+    int rc = prepare_call(norm, drop, fmt, d_stats, accumulate, &c);
+    if (rc != QFMT_OK) return rc;
+    const int32_t t = c.norm.dtype;
+    const bool empty = c.norm.rows == 0 || c.norm.cols == 0;
+    if (!empty && (d_x == nullptr || d_y == nullptr)) return QFMT_ERR_BAD_ARG;
+    if (!element_aligned(d_x, t) || !element_aligned(d_residual, t) || !element_aligned(d_h, t) || !element_aligned(d_y, t) ||
+        !float_aligned(d_weight) || !float_aligned(d_bias) || !float_aligned(d_mean) || !float_aligned(d_rstd))
+        return QFMT_ERR_BAD_ARG;
+    rc = current_device(&c.dev);
+    if (rc != QFMT_OK) return rc;
+    if (d_stats != nullptr && accumulate == 0)
+        QFMT_CUDA_TRY(launch_overlapping(zero_words_kernel, 1u, 256u, 0, stream, reinterpret_cast<int*>(d_stats),
+                                         (int)(sizeof(qfmt_stats_t) / sizeof(int))));
+    if (empty) return QFMT_OK;
+    const auto run = fused ? (t == QFMT_F32 ? forward<QFMT_F32, true> : t == QFMT_F16 ? forward<QFMT_F16, true> : forward<QFMT_BF16, true>)
+                           : (t == QFMT_F32 ? forward<QFMT_F32, false> : t == QFMT_F16 ? forward<QFMT_F16, false> : forward<QFMT_BF16, false>);
+    return run(c, d_x, d_residual, d_weight, d_bias, d_h, d_y, d_mean, d_rstd, d_stats, stream);
+}
+
+}  // namespace
+}  // namespace qfmt
+
+extern "C" int qfmt_layer_norm(const qfmt_norm_t* norm, const void* d_x, const float* d_weight, const float* d_bias, void* d_y,
+                               float* d_mean, float* d_rstd, const qfmt_format_t* fmt, qfmt_stats_t* d_stats, int accumulate,
+                               void* stream) {
+    return qfmt::forward_entry(norm, nullptr, false, d_x, nullptr, d_weight, d_bias, nullptr, d_y, d_mean, d_rstd, fmt, d_stats,
+                               accumulate, (cudaStream_t)stream);
+}
+
+extern "C" int qfmt_dropout_add_layer_norm(const qfmt_norm_t* norm, const qfmt_dropout_t* drop, const void* d_x,
+                                           const void* d_residual, const float* d_weight, const float* d_bias, void* d_h,
+                                           void* d_y, float* d_mean, float* d_rstd, const qfmt_format_t* fmt,
+                                           qfmt_stats_t* d_stats, int accumulate, void* stream) {
+    return qfmt::forward_entry(norm, drop, true, d_x, d_residual, d_weight, d_bias, d_h, d_y, d_mean, d_rstd, fmt, d_stats,
+                               accumulate, (cudaStream_t)stream);
+}

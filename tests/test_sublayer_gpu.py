@@ -355,6 +355,31 @@ def test_norm_backward_parts(rows, cols, kind):
     assert torch.equal(got[1], full[1]) and torch.equal(got[2], full[2])
 
 
+@pytest.mark.parametrize("kind,e,m", FORMATS)
+@pytest.mark.parametrize("rows,cols", [(3, 8200), (5, 13001), (2, 16384)])
+def test_rounded_gradients_of_wide_rows(rows, cols, kind, e, m):
+    """Rows that take most of the shared memory, with the largest histograms beside them."""
+    gen = torch.Generator().manual_seed(cols)
+    x, dy = values(gen, rows, cols, kind), values(gen, rows, cols, kind)
+    mean, rstd = saved(x)
+    w, _ = vectors(gen, cols)
+    want = ref.backward(x.double(), dy.double(), mean.double(), rstd.double(), w.double())
+    stats = torch.full((qf.STATS_WORDS,), 5, dtype=torch.int64, device=DEV)
+    for off, pad in ((0, 0), (1, 3)):
+        got = run_norm_backward(x, dy, mean, rstd, w, kind, off, pad, fmt=qf.make_format(e, m, 0), stats=stats)
+        ref.close(got[1], want[1], want[4])
+        ref.close(got[2], want[2], want[5])
+        rounding = 2.0 ** -(m + 1) * want[0].abs() + 2.0 ** (2 - 2 ** (e - 1))   # half a last place, or flushed below 2^E_min
+        fine = want[0].abs() < 2.0 ** (2 ** (e - 1) - 1)                        # below overflow
+        err = (got[0].double() - want[0]).abs()
+        assert torch.all((err <= want[3] * (1 + 2.0 ** -m) + rounding)[fine])
+        st = stats.cpu()
+        assert int(st[qf.ST_TOTAL]) == rows * cols == int(st[:256].sum())
+    plain = run_norm_backward(x.float(), dy.float(), mean, rstd, w, "f32")[0]
+    st = oracle_rounding(plain, e, m, 0, kind)[1]
+    assert abs(int(st[qf.ST_DENORMAL]) - int(stats.cpu()[qf.ST_DENORMAL])) <= 2 + rows * cols // 1000
+
+
 def test_norm_backward_against_differences():
     """The gradients against central differences of the 64-bit forward pass along random directions.  With step s the
     difference is off by O(s^2) = 1e-8 of the gradient's scale, single precision by less than 1e-5 of it."""
