@@ -159,19 +159,18 @@ def _bind_optional(L: ctypes.CDLL) -> None:
     L.qfmt_conv_workspace_bytes.restype = sz
     L.qfmt_conv_fmac8.argtypes = [ctypes.c_int32, convp, vp, vp, vp, ctypes.POINTER(qfmt_format_t), vp, ci, ci, vp]
     L.qfmt_conv_fmac8.restype = ci
-    normp, dropp, fmtp = ctypes.POINTER(qfmt_norm_t), ctypes.POINTER(qfmt_dropout_t), ctypes.POINTER(qfmt_format_t)
-    L.qfmt_dropout.argtypes = [vp, i64, vp, i64, vp, i64, i64, i64, ctypes.c_int32, dropp, vp]
+    # records by address (see _ref), which converts faster than a pointer type
+    L.qfmt_dropout.argtypes = [vp, i64, vp, i64, vp, i64, i64, i64, ctypes.c_int32, vp, vp]
     L.qfmt_dropout.restype = ci
-    L.qfmt_layer_norm.argtypes = [normp, vp, vp, vp, vp, vp, vp, fmtp, vp, ci, vp]
+    L.qfmt_layer_norm.argtypes = [vp] * 9 + [ci, vp]
     L.qfmt_layer_norm.restype = ci
-    L.qfmt_layer_norm_backward.argtypes = [normp, vp, vp, vp, vp, vp, vp, vp, vp, fmtp, vp, ci, vp, sz, vp]
+    L.qfmt_layer_norm_backward.argtypes = [vp] * 11 + [ci, vp, sz, vp]
     L.qfmt_layer_norm_backward.restype = ci
-    L.qfmt_layer_norm_workspace_bytes.argtypes = [normp]
+    L.qfmt_layer_norm_workspace_bytes.argtypes = [vp]
     L.qfmt_layer_norm_workspace_bytes.restype = sz
-    L.qfmt_dropout_add_layer_norm.argtypes = [normp, dropp, vp, vp, vp, vp, vp, vp, vp, vp, fmtp, vp, ci, vp]
+    L.qfmt_dropout_add_layer_norm.argtypes = [vp] * 12 + [ci, vp]
     L.qfmt_dropout_add_layer_norm.restype = ci
-    L.qfmt_dropout_add_layer_norm_backward.argtypes = [normp, dropp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, fmtp, vp, ci,
-                                                       vp, sz, vp]
+    L.qfmt_dropout_add_layer_norm_backward.argtypes = [vp] * 14 + [ci, vp, sz, vp]
     L.qfmt_dropout_add_layer_norm_backward.restype = ci
     L.qfmt_gemm_builtin_scratch.argtypes = [matp, matp, vp, ctypes.c_int64, ctypes.POINTER(qfmt_format_t), vp, vp]
     L.qfmt_gemm_builtin_scratch.restype = ci
@@ -427,7 +426,7 @@ def make_norm(rows: int, cols: int, dtype, eps: float = 1e-5, ld_x: int = 0, ld_
 
 def _ref(record):
     """A record's address for a call, or NULL."""
-    return None if record is None else ctypes.byref(record)
+    return None if record is None else ctypes.addressof(record)
 
 
 def qfmt_dropout(d_x, ld_x: int, d_residual, ld_residual: int, d_out, ld_out: int, rows: int, cols: int, dtype,
@@ -445,7 +444,7 @@ def qfmt_layer_norm(norm: qfmt_norm_t, d_x, d_weight, d_bias, d_y, d_mean=None, 
 
 
 def qfmt_layer_norm_workspace_bytes(norm: qfmt_norm_t) -> int:
-    return int(lib().qfmt_layer_norm_workspace_bytes(ctypes.byref(norm)))
+    return int(lib().qfmt_layer_norm_workspace_bytes(_ref(norm)))
 
 
 def qfmt_layer_norm_backward(norm: qfmt_norm_t, d_dy, d_x, d_mean, d_rstd, d_weight, d_dx, d_dweight, d_dbias, d_workspace,

@@ -29,6 +29,13 @@ __device__ __forceinline__ int granule_columns(int64_t cols, int64_t g) {
     return left >= kGranule ? kGranule : left > 0 ? (int)left : 0;
 }
 
+// Zeros from column n of a granule on.
+__device__ __forceinline__ void clear_from(Granule& v, int n) {
+#pragma unroll
+    for (int j = 0; j < kGranule; ++j)
+        if (j >= n) v.at(j) = 0.0f;
+}
+
 // `n` entries of granule g of a vector of one value per column, or `fill` where there is none.
 __device__ __forceinline__ Granule load_columns(const float* p, int64_t g, int n, float fill) {
     Granule v = splat(fill);

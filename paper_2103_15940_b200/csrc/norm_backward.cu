@@ -30,11 +30,8 @@ template <bool kPlain>
 __device__ __forceinline__ Granule normalise(Granule v, float mean, float rstd, int n) {
     const float2 shift = both(kPlain && n == 0 ? 0.0f : -mean);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        v.p[j] = mul2(add2(v.p[j], shift), both(rstd));
-        if (!kPlain && 2 * j >= n) v.p[j].x = 0.0f;
-        if (!kPlain && 2 * j + 1 >= n) v.p[j].y = 0.0f;
-    }
+    for (int j = 0; j < 4; ++j) v.p[j] = mul2(add2(v.p[j], shift), both(rstd));
+    if (!kPlain && n < kGranule) clear_from(v, n);
     return v;
 }
 

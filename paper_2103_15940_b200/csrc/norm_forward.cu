@@ -48,14 +48,12 @@ __device__ __forceinline__ float sum8(const Granule& v) {
 template <bool kPlain>
 __device__ __forceinline__ float centre(Granule& v, float mean, int n) {
     const float2 shift = both(kPlain && n == 0 ? 0.0f : -mean);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v.p[j] = add2(v.p[j], shift);
+    if (!kPlain && n < kGranule) clear_from(v, n);
     float2 s = make_float2(0.0f, 0.0f);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        v.p[j] = add2(v.p[j], shift);
-        if (!kPlain && 2 * j >= n) v.p[j].x = 0.0f;
-        if (!kPlain && 2 * j + 1 >= n) v.p[j].y = 0.0f;
-        s = fma2(v.p[j], v.p[j], s);
-    }
+    for (int j = 0; j < 4; ++j) s = fma2(v.p[j], v.p[j], s);
     return s.x + s.y;
 }
 
