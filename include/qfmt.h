@@ -465,9 +465,9 @@ int qfmt_conv_fmac8(int32_t op, const qfmt_conv_t* geom, const float* d_p, const
  *   QFMT_F16   packed 1/5/10 codes (IEEE binary16), QFMT_BF16  packed 1/8/7 codes (bfloat16)
  * Weights, biases, their gradients and the row statistics are fp32.  All arithmetic is in 32 bits; each
  * stored value is rounded once.  In every call below a leading dimension of 0 stands for cols; rows = 0 or
- * cols = 0 is valid; rows and cols are below 2^31.  Any alignment of an element is accepted.  Tensors whose
- * granules of eight columns are aligned (32 bytes for containers, 16 for codes, leading dimensions
- * multiples of 8) move by whole granules.
+ * cols = 0 is valid; rows and cols are below 2^31.  Any alignment of an element is accepted, and no result depends on
+ * it; rows run fastest where cols and the leading dimensions are multiples of 8 and the tensors start on 32 bytes
+ * (containers) or 16 (codes).
  */
 enum { QFMT_F32 = 0, QFMT_F16 = 1, QFMT_BF16 = 2 };
 
