@@ -156,25 +156,25 @@ __device__ __forceinline__ uint32_t word_of(const Raw<kType>& r, int j) {
     else return j & 1 ? r.w[j / 2] >> 16 : r.w[j / 2] & 0xFFFFu;
 }
 
-// A granule's words from element `first` of w on; the elements are 32 or 16 bits wide.
-template <int kType, int kFrom>
-__device__ __forceinline__ Raw<kType> shifted(const uint32_t (&v)[kFrom], uint32_t first) {
-    Raw<kType> r;
-    constexpr int kWords = sizeof(r.w) / 4;
-    uint32_t w[kFrom];
+// A granule's words from element `first` of w on; the elements are 32 or 16 bits wide.  `first` is the same in all of a
+// row, so this branches on it: a selection per word and stage would keep the integer pipe four times as busy.
+template <int kType, int kWord, int kFrom>
+__device__ __forceinline__ void take_from(Raw<kType>& r, const uint32_t (&w)[kFrom], uint32_t odd) {
 #pragma unroll
-    for (int i = 0; i < kFrom; ++i) w[i] = v[i];
-    const uint32_t word = kType == QFMT_F32 ? first : first >> 1;
-#pragma unroll
-    for (int by = (kFrom - kWords) / 2; by > 0; by /= 2) {  // a shift by less than kFrom - kWords words is asked for
-        const bool on = word & by;
-#pragma unroll
-        for (int i = 0; i + by < kFrom; ++i) w[i] = on ? w[i + by] : w[i];
+    for (int i = 0; i < (int)(sizeof(r.w) / 4); ++i) {
+        if (kType == QFMT_F32) r.w[i] = w[kWord + i];
+        else asm volatile("shf.r.wrap.b32 %0, %1, %2, %3;" : "=r"(r.w[i]) : "r"(w[kWord + i]), "r"(w[(kWord + i + 1) % kFrom]), "r"(odd));
     }
-#pragma unroll
-    for (int i = 0; i < kWords; ++i) {
-        r.w[i] = w[i];
-        if (kType != QFMT_F32 && i + 1 < kFrom) r.w[i] = __funnelshift_r(w[i], w[i + 1], (first & 1) * 16);
+}
+template <int kType, int kFrom>
+__device__ __forceinline__ Raw<kType> shifted(const uint32_t (&w)[kFrom], uint32_t first) {
+    Raw<kType> r;
+    const uint32_t odd = kType == QFMT_F32 ? 0u : (first & 1u) * 16u;
+    switch (kType == QFMT_F32 ? first : first >> 1) {
+        case 0: take_from<kType, 0>(r, w, odd); break;
+        case 1: take_from<kType, 1>(r, w, odd); break;
+        case 2: take_from<kType, 2>(r, w, odd); break;
+        default: take_from<kType, 3>(r, w, odd); break;
     }
     return r;
 }
