@@ -3,7 +3,7 @@
 //
 // One read and one write per element (two reads with a residual): bound by memory, with the integer pipe not far
 // behind.  A granule of eight columns costs one generator block of 20 wide products and 20 three-way xors; with the
-// rest a warp issues 111 instructions for 32 granules of codes (137 before a thread kept its columns and the round keys
+// rest a warp issues 93 instructions for 32 granules of codes (137 before a thread kept its columns and the round keys
 // came as constants, 28 us against 24 on 8192 x 4096 bfloat16).  Sixteen bits an element, not 32, because two blocks a
 // granule would make the integer pipe the bound; so p is held in steps of 2^-16 and the scale belongs to the step taken.
 // Measured: 8192 x 4096 bfloat16 24.0 us (5.6 TB/s, 0.87 of the measured copy rate), 16384 x 4096 fp32 92 us (5.8 TB/s),

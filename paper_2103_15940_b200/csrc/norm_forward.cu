@@ -5,7 +5,7 @@
 // rows whose mean is large against their spread), so
 //   * a row stays in registers, two granules a thread, and additions and products issue in pairs: 118 instructions a
 //     granule and warp, against 186 with branches around loads and 64-bit row arithmetic (76 us -> 59 us on the case below);
-//   * two rows at a time share the barriers, and five shuffles reduce both rows' sums (59 -> 48 us);
+//   * two rows at a time share the barriers, and five shuffles reduce both rows' sums (79 instructions, 59 -> 48 us);
 //   * weight and bias stay in registers from row to row; four granules a thread without them took 75 us (their
 //     reads from L1 are four times the row's);
 //   * the next rows' granules are loaded while these are worked on.
