@@ -117,8 +117,21 @@ def lib() -> ctypes.CDLL:
         L.qfmt_version.argtypes = []
         L.qfmt_version.restype = ci
         _bind_optional(L)
+        _bind_calls(L)
         _lib = L
     return _lib
+
+
+def _bind_calls(L: ctypes.CDLL) -> None:
+    """The sub-layer calls go through a module of their own, since generic conversion takes as long as their GPU work."""
+    global _calls
+    try:
+        from . import _calls
+    except ImportError as e:
+        raise ImportError(f"{_HERE}/_calls.abi3.so is missing: build it with `python -m paper_2103_15940_b200.build`") from e
+    _calls.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+        L.qfmt_dropout, L.qfmt_layer_norm, L.qfmt_layer_norm_backward, L.qfmt_dropout_add_layer_norm,
+        L.qfmt_dropout_add_layer_norm_backward)))
 
 
 def _bind_optional(L: ctypes.CDLL) -> None:
@@ -193,11 +206,17 @@ def _ptr(x) -> Optional[int]:
     raise TypeError(type(x))
 
 
+_current_device = _current_stream = None
+
+
 def _stream_handle(stream) -> Optional[int]:
     if stream is None:
         # the raw handle: building torch's stream object for it takes 3 us, as long as a launch
-        import torch
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        global _current_device, _current_stream
+        if _current_stream is None:
+            import torch
+            _current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+        return _current_stream(_current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -408,9 +427,17 @@ def qfmt_gemm_tile_policy(policy: int) -> None:
     _check(lib().qfmt_gemm_tile_policy(int(policy)), "qfmt_gemm_tile_policy")
 
 
+_known_storage = {}
+
+
 def _storage(dtype) -> int:
     """Storage type of a tensor: QFMT_F32 / QFMT_F16 / QFMT_BF16, or the torch dtype of the same words."""
-    return dtype if isinstance(dtype, int) else _STORAGE[str(dtype)]
+    if type(dtype) is int:
+        return dtype
+    code = _known_storage.get(dtype)
+    if code is None:
+        code = _known_storage[dtype] = _STORAGE[str(dtype)]
+    return code
 
 
 def make_dropout(p: float, seed: int, offset: int = 0, d_offset=None) -> qfmt_dropout_t:
@@ -429,18 +456,27 @@ def _ref(record):
     return None if record is None else ctypes.addressof(record)
 
 
+def _sublayer(name: str, *args) -> None:
+    """One of the sub-layer calls: integers, tensors or None, in the order of include/qfmt.h."""
+    if _lib is None:
+        lib()
+    status = getattr(_calls, name)(*args)
+    if status != QFMT_OK:
+        raise QfmtError(status, "qfmt_" + name)
+
+
 def qfmt_dropout(d_x, ld_x: int, d_residual, ld_residual: int, d_out, ld_out: int, rows: int, cols: int, dtype,
                  drop: qfmt_dropout_t, stream=None) -> None:
     """out = residual + D(x), and D's own backward pass; see qfmt_dropout in include/qfmt.h."""
-    _check(lib().qfmt_dropout(_ptr(d_x), ld_x, _ptr(d_residual), ld_residual, _ptr(d_out), ld_out, rows, cols,
-                              _storage(dtype), _ref(drop), _stream_handle(stream)), "qfmt_dropout")
+    _sublayer("dropout", d_x, ld_x, d_residual, ld_residual, d_out, ld_out, rows, cols, _storage(dtype), _ref(drop),
+              _stream_handle(stream))
 
 
 def qfmt_layer_norm(norm: qfmt_norm_t, d_x, d_weight, d_bias, d_y, d_mean=None, d_rstd=None,
                     fmt: Optional[qfmt_format_t] = None, d_stats=None, accumulate: int = 0, stream=None) -> None:
     """y = LN(x), rounded to fmt with statistics if one is given; see qfmt_layer_norm in include/qfmt.h."""
-    _check(lib().qfmt_layer_norm(_ref(norm), _ptr(d_x), _ptr(d_weight), _ptr(d_bias), _ptr(d_y), _ptr(d_mean), _ptr(d_rstd),
-                                 _ref(fmt), _ptr(d_stats), accumulate, _stream_handle(stream)), "qfmt_layer_norm")
+    _sublayer("layer_norm", _ref(norm), d_x, d_weight, d_bias, d_y, d_mean, d_rstd, _ref(fmt), d_stats, accumulate,
+              _stream_handle(stream))
 
 
 def qfmt_layer_norm_workspace_bytes(norm: qfmt_norm_t) -> int:
@@ -451,19 +487,16 @@ def qfmt_layer_norm_backward(norm: qfmt_norm_t, d_dy, d_x, d_mean, d_rstd, d_wei
                              workspace_bytes: int, fmt: Optional[qfmt_format_t] = None, d_stats=None, accumulate: int = 0,
                              stream=None) -> None:
     """Gradients of LN's input, weight and bias; see qfmt_layer_norm_backward in include/qfmt.h."""
-    _check(lib().qfmt_layer_norm_backward(_ref(norm), _ptr(d_dy), _ptr(d_x), _ptr(d_mean), _ptr(d_rstd), _ptr(d_weight),
-                                          _ptr(d_dx), _ptr(d_dweight), _ptr(d_dbias), _ref(fmt), _ptr(d_stats), accumulate,
-                                          _ptr(d_workspace), workspace_bytes, _stream_handle(stream)),
-           "qfmt_layer_norm_backward")
+    _sublayer("layer_norm_backward", _ref(norm), d_dy, d_x, d_mean, d_rstd, d_weight, d_dx, d_dweight, d_dbias, _ref(fmt),
+              d_stats, accumulate, d_workspace, workspace_bytes, _stream_handle(stream))
 
 
 def qfmt_dropout_add_layer_norm(norm: qfmt_norm_t, drop: Optional[qfmt_dropout_t], d_x, d_residual, d_weight, d_bias, d_h, d_y,
                                 d_mean=None, d_rstd=None, fmt: Optional[qfmt_format_t] = None, d_stats=None,
                                 accumulate: int = 0, stream=None) -> None:
     """h = residual + D(x), y = LN(h) in one pass; see qfmt_dropout_add_layer_norm in include/qfmt.h."""
-    _check(lib().qfmt_dropout_add_layer_norm(_ref(norm), _ref(drop), _ptr(d_x), _ptr(d_residual), _ptr(d_weight), _ptr(d_bias),
-                                             _ptr(d_h), _ptr(d_y), _ptr(d_mean), _ptr(d_rstd), _ref(fmt), _ptr(d_stats),
-                                             accumulate, _stream_handle(stream)), "qfmt_dropout_add_layer_norm")
+    _sublayer("dropout_add_layer_norm", _ref(norm), _ref(drop), d_x, d_residual, d_weight, d_bias, d_h, d_y, d_mean, d_rstd,
+              _ref(fmt), d_stats, accumulate, _stream_handle(stream))
 
 
 def qfmt_dropout_add_layer_norm_backward(norm: qfmt_norm_t, drop: Optional[qfmt_dropout_t], d_dy, d_dh, d_h, d_mean, d_rstd,
@@ -472,8 +505,6 @@ def qfmt_dropout_add_layer_norm_backward(norm: qfmt_norm_t, drop: Optional[qfmt_
                                          stream=None) -> None:
     """dresidual = dh + LN's gradient, dx = D(dresidual), dweight, dbias; see
     qfmt_dropout_add_layer_norm_backward in include/qfmt.h."""
-    _check(lib().qfmt_dropout_add_layer_norm_backward(_ref(norm), _ref(drop), _ptr(d_dy), _ptr(d_dh), _ptr(d_h), _ptr(d_mean),
-                                                      _ptr(d_rstd), _ptr(d_weight), _ptr(d_dx), _ptr(d_dresidual),
-                                                      _ptr(d_dweight), _ptr(d_dbias), _ref(fmt), _ptr(d_stats), accumulate,
-                                                      _ptr(d_workspace), workspace_bytes, _stream_handle(stream)),
-           "qfmt_dropout_add_layer_norm_backward")
+    _sublayer("dropout_add_layer_norm_backward", _ref(norm), _ref(drop), d_dy, d_dh, d_h, d_mean, d_rstd, d_weight, d_dx,
+              d_dresidual, d_dweight, d_dbias, _ref(fmt), d_stats, accumulate, d_workspace, workspace_bytes,
+              _stream_handle(stream))

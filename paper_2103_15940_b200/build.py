@@ -1,6 +1,7 @@
 """Builds the CUDA library in-tree: ``python -m paper_2103_15940_b200.build``.
 
-One shared object, ``libqfmt.so``, next to this file, compiled by nvcc for sm_100a only.
+``libqfmt.so``, next to this file, compiled by nvcc for sm_100a only, and ``_calls.abi3.so``, the part of the Python
+binding that small passes need in C.
 """
 from __future__ import annotations
 
@@ -8,12 +9,14 @@ import glob
 import os
 import subprocess
 import sys
+import sysconfig
 import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libqfmt.so")
+CALLS = os.path.join(HERE, "_calls.abi3.so")
 
 NVCC_FLAGS = [
     "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
@@ -27,10 +30,10 @@ def sources():
 
 
 def needs_build() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(CALLS):
         return True
-    t = os.path.getmtime(LIB)
-    deps = sources() + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(ROOT, "include", "*.h"))
+    t = min(os.path.getmtime(LIB), os.path.getmtime(CALLS))
+    deps = sources() + glob.glob(os.path.join(CSRC, "*.c")) + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(ROOT, "include", "*.h"))
     return any(os.path.getmtime(d) > t for d in deps)
 
 
@@ -39,6 +42,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     flags = NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-I", os.path.join(ROOT, "include"), "-I", CSRC]
+    subprocess.check_call([os.environ.get("CC", "gcc"), "-O2", "-Wall", "-fPIC", "-shared", "-I", sysconfig.get_paths()["include"],
+                           "-I", os.path.join(ROOT, "include"), "-o", CALLS, os.path.join(CSRC, "calls.c")])
     # one nvcc per source, side by side; the objects are linked into the library and go
     with tempfile.TemporaryDirectory() as tmp:
         objects = [os.path.join(tmp, os.path.basename(s) + ".o") for s in sources()]

@@ -110,3 +110,25 @@ def test_records():
     assert ctypes.sizeof(qf.qfmt_dropout_t) == 32 and ctypes.sizeof(qf.qfmt_norm_t) == 88
     with pytest.raises(KeyError):
         qf.make_norm(1, 1, "torch.float64")
+
+
+def test_argument_types():
+    """Addresses come as integers, tensors or None; anything else, or another number of arguments, is a TypeError."""
+    norm = qf.make_norm(4, 16, qf.QFMT_F32)
+    for bad in ("text", 1.5, b"bytes", [P]):
+        with pytest.raises(TypeError):
+            qf.qfmt_layer_norm(norm, bad, P, P, P, stream=0)
+    with pytest.raises(TypeError):
+        qf.qfmt_layer_norm("norm", P, P, P, P, stream=0)
+    with pytest.raises(TypeError):
+        qf._calls.dropout(P, 16)
+    assert qf._calls.dropout(P, 16, None, 0, P, 16, 4, 16, 3, None, None) == BAD
+
+
+def test_tensors_pass_their_address():
+    """A tensor stands for its data_ptr(): a misaligned one is refused as its address is."""
+    import torch
+    buf = torch.zeros(64, dtype=torch.uint8)
+    odd = buf[1:] if buf.data_ptr() % 2 == 0 else buf
+    assert odd.data_ptr() % 2 == 1
+    assert forward(x=odd) == BAD == forward(x=odd.data_ptr())
