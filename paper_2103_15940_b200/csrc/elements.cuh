@@ -394,8 +394,7 @@ __device__ __forceinline__ void stage_row(uint32_t shared, const uint32_t* row, 
         asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(shared + 4 * i), "l"(row + i) : "memory");
 }
 __device__ __forceinline__ void stage_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int kPending>  // of this thread's copies all but the last kPending groups have arrived
-__device__ __forceinline__ void stage_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kPending) : "memory"); }
+__device__ __forceinline__ void stage_wait() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }  // this thread's copies
 
 // n columns (0..8) of granule g of a staged row, zeros where there are none.
 __device__ __forceinline__ Raw<QFMT_F32> staged_granule(uint32_t shared, int g, int n) {

@@ -226,8 +226,8 @@ __device__ __forceinline__ void put_columns(int i, float4 s, int padded, int col
 // V > 1 (wide rows): the team is the block, and the column sums lie in shared memory, each thread's its own, since the
 // registers hold V granules of dy and h; with V > 2 the weight is read from the cache as well.
 // kPlain and kStaged as in the forward pass (staged bfloat16 rows took 75 us where shifted pieces take 44); with
-// registers to spare (kAhead) the next rows are on their way while these are worked on.  Staged rows have `slots` places
-// a team: 4 with the next row copied meanwhile, 2, or 1 for dy and h in turn.  A team takes `group` neighbouring rows (R, or R = 1 at a time), then the group that is a step away.
+// registers to spare (kAhead) the next rows are on their way while these are worked on.  Staged rows have two
+// places a team, or one for h and dy in turn; the next ones are copied as soon as they have been read.  A team takes `group` neighbouring rows (R, or R = 1 at a time), then the group that is a step away.
 template <int kType, int V, int R, bool kParts, bool kFused, bool kPlain>
 __global__ void __launch_bounds__(kMaxTeam)
 norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, const BackwardSteps step, int hist_words, int sum_words,
@@ -294,16 +294,18 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
         else if constexpr (kParts) __syncwarp();
         else asm volatile("bar.sync %0, %1;" ::"r"(1 + mine), "r"(team) : "memory");
     };
-    uint32_t half = 0;
     // rows to the next one: a step, or with R = 1 one row within a group
     const bool pairs = R == 1 && group == 2;
     const auto advance = [&](bool second, auto*& p, int64_t ld, int64_t by) { p += pairs ? (second ? by - ld : ld) : by; };
     if (kAhead) fetch_rows(row);
-    if (kStaged && slots == 4) {
-        stage(row, places, pdy);
-        stage(row, places + row_bytes, ph);
-        stage_end();
-    }
+    const auto stage_next = [&](uint32_t at) {
+        if constexpr (kStaged) {
+            stage(at, places, ph);
+            if (slots == 2) stage(at, places + row_bytes, pdy);
+            stage_end();
+        }
+    };
+    stage_next(row);
 #pragma unroll
     for (int k = 0; k < (V <= 2 ? V : 0); ++k) w[k] = load_columns(a.weight, k * team + t, n[k], 1.0f);
     int parity = 0;
@@ -313,35 +315,20 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
         if (!kAhead) fetch_rows(row);
         if constexpr (kStaged) {
             const bool there = row < rows;
-            if (slots == 4) {
-                advance(second, pdy, a.dy.ld, step.dy);
-                advance(second, ph, a.h.ld, step.h);
-                const uint32_t place = places + (half ^ 1u) * 2 * row_bytes;
-                stage(row + by, place, pdy);
-                stage(row + by, place + row_bytes, ph);
-                stage_end();
-                stage_wait<1>();
-            } else {
-                stage(row, places, ph);
-                if (slots == 2) stage(row, places + row_bytes, pdy);
-                stage_end();
-                stage_wait<0>();
-            }
+            stage_wait();
             arrived();
-            const uint32_t place_h = slots == 4 ? places + (2 * half + 1) * row_bytes : places;
-            const uint32_t place_dy = slots == 4 ? places + 2 * half * row_bytes : slots == 2 ? places + row_bytes : places;
 #pragma unroll
-            for (int k = 0; k < V; ++k) raw_h[0][k] = staged_granule(place_h, k * team + t, there ? n[k] : 0);
+            for (int k = 0; k < V; ++k) raw_h[0][k] = staged_granule(places, k * team + t, there ? n[k] : 0);
             if (slots == 1) {
                 arrived();  // h has been read by everyone
                 stage(row, places, pdy);
                 stage_end();
-                stage_wait<0>();
+                stage_wait();
                 arrived();
             }
+            const uint32_t place = slots == 2 ? places + row_bytes : places;
 #pragma unroll
-            for (int k = 0; k < V; ++k) raw_dy[0][k] = staged_granule(place_dy, k * team + t, there ? n[k] : 0);
-            if (slots == 4) half ^= 1u;
+            for (int k = 0; k < V; ++k) raw_dy[0][k] = staged_granule(place, k * team + t, there ? n[k] : 0);
         }
         Granule dy[R][V], xhat[R][V];
         float2 s[R];
@@ -369,10 +356,8 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
                 }
             }
         }
-        if (!kStaged || slots != 4) {
-            advance(second, pdy, a.dy.ld, step.dy);
-            advance(second, ph, a.h.ld, step.h);
-        }
+        advance(second, pdy, a.dy.ld, step.dy);
+        advance(second, ph, a.h.ld, step.h);
         if (kAhead) fetch_rows(row + by);
         if constexpr (kParts) {
             for (int off = team >> 1; off > 0; off >>= 1) {
@@ -382,6 +367,8 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
         } else {
             team_sums<R>(s, team, t, 1 + mine, scratch[mine][parity]);
         }
+        if (kParts) __syncwarp();
+        stage_next(row + by);  // behind the sums' barrier: everyone has read the places
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             const float c1 = s[i].x * a.inverse, c2 = s[i].y * a.inverse;
@@ -401,7 +388,7 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
     }
     if (hist != nullptr) flush_hist(hist, a.quant, a.stats, (uint64_t)a.rows * (uint64_t)a.cols);
     const bool alone = a.dweight != nullptr || a.dbias != nullptr;  // this block's part is the result
-    if (kStaged) stage_wait<0>();
+    if (kStaged) stage_wait();
     if (a.partial == nullptr) return;
     // [dweight, dbias][padded columns] of every warp of small teams, or of every team; then their sum
     const int padded = ((int)a.cols + kGranule - 1) / kGranule * kGranule, quads = padded / 2;
@@ -511,7 +498,7 @@ int launch_backward_rows(const Call& c, BackwardArgs<kType> a, int team, int gro
     constexpr bool kStaged = !kPlain && kType == QFMT_F32;
     const size_t place = (size_t)teams * staged_row_bytes(a.cols);
     const size_t sums = backward_sum_bytes(V, kParts, team, a.cols), rest = c.hist_bytes + sums;
-    const int slots = !kStaged ? 0 : rest + 4 * place <= kMostShared ? 4 : rest + 2 * place <= kMostShared ? 2 : 1;
+    const int slots = !kStaged ? 0 : rest + 2 * place <= kMostShared ? 2 : 1;
     // More than half of what an SM has: its one block must not be joined by a second of the same launch, which would
     // leave another SM without work (launches overlap, so SMs come free at different times).
     const size_t smem = std::max(rest + slots * place, (size_t)116 * 1024);

@@ -173,12 +173,12 @@ struct ForwardSteps {
 // from row to row.  V > 2: longer rows, without them.
 // kPlain: every granule whole and aligned, no format; granules go straight to registers, with V <= 2 those of the next
 // rows while these are worked on.  Otherwise any layout and an optional format: codes come as aligned pieces that are
-// shifted into place; rows of containers (kStaged) go through shared memory behind the histogram, in `slots` places a
-// team (twice the tensors that are read: the next row is copied meanwhile).  Each way is the faster one for its type:
+// shifted into place; rows of containers (kStaged) go through shared memory behind the histogram, where the next row
+// is copied as soon as this one has been read from there by its whole team.  Each way is the faster one for its type:
 // 16384 rows of 1021 take 28 us as shifted bfloat16 pieces and 31 us staged, as fp32 39 us shifted and 33 us staged.
 template <int kType, int V, int R, bool kFused, bool kPlain>
 __global__ void __launch_bounds__(kMaxTeam)
-norm_forward_rows_kernel(const ForwardArgs<kType> a, int team, const ForwardSteps step, int hist_words, int slots) {
+norm_forward_rows_kernel(const ForwardArgs<kType> a, int team, const ForwardSteps step, int hist_words) {
     constexpr bool kKeep = V <= 2;
     constexpr bool kAhead = kKeep && kPlain, kStaged = !kPlain && kType == QFMT_F32;
     extern __shared__ __align__(16) uint32_t dynamic[];
@@ -222,22 +222,20 @@ norm_forward_rows_kernel(const ForwardArgs<kType> a, int team, const ForwardStep
         if (kAhead) px += step.x, pr += step.residual;
     };
     const uint32_t row_bytes = staged_row_bytes(a.cols);
-    const uint32_t places = shared_address(dynamic + hist_words) + mine * slots * row_bytes;
-    const int tensors = kFused ? 2 : 1;
-    uint32_t half = 0;
-    const auto stage_rows = [&]([[maybe_unused]] uint32_t at, [[maybe_unused]] uint32_t to_half) {  // the next row through shared memory
-        if constexpr (kStaged) if (at < rows) {
-            const uint32_t place = places + to_half * tensors * row_bytes;
-            stage_row(place, px, (int)a.cols, t, team);
-            if (residual) stage_row(place + row_bytes, pr, (int)a.cols, t, team);
+    const uint32_t place = shared_address(dynamic + hist_words) + mine * (kFused ? 2 : 1) * row_bytes;  // of the team
+    const auto stage_next = [&]([[maybe_unused]] uint32_t at) {  // the next row through shared memory
+        if constexpr (kStaged) {
+            if (at < rows) {
+                stage_row(place, px, (int)a.cols, t, team);
+                if (residual) stage_row(place + row_bytes, pr, (int)a.cols, t, team);
+            }
+            stage_end();
+            px += step.x;
+            pr += step.residual;
         }
-        stage_end();
-        px += step.x;
-        pr += step.residual;
     };
-    const bool ahead = slots > tensors;
     if (kAhead) fetch_rows(row);
-    if (kStaged && ahead) stage_rows(row, 0);
+    stage_next(row);
     Granule w[kKeep ? V : 1], b[kKeep ? V : 1];
     if constexpr (kKeep) {
 #pragma unroll
@@ -248,19 +246,15 @@ norm_forward_rows_kernel(const ForwardArgs<kType> a, int team, const ForwardStep
     }
     for (; row - mine * R < rows; row += stride) {
         if constexpr (kStaged) {
-            stage_rows(ahead ? row + stride : row, ahead ? half ^ 1u : 0u);
-            if (ahead) stage_wait<1>();
-            else stage_wait<0>();
+            stage_wait();
             if (V > 1) __syncthreads();
             else __syncwarp();
-            const uint32_t place = places + half * tensors * row_bytes;
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 const int there = row < rows ? n[k] : 0;
                 x[0][k] = staged_granule(place, k * team + t, there);
                 if (kFused) r[0][k] = staged_granule(place + row_bytes, k * team + t, residual ? there : 0);
             }
-            if (ahead) half ^= 1u;
         } else if (!kAhead) {
             fetch_rows(row);
         }
@@ -292,6 +286,8 @@ norm_forward_rows_kernel(const ForwardArgs<kType> a, int team, const ForwardStep
             for (int k = 1; k < V; ++k) mean[i] += sum8(v[i][k]);
         }
         team_sum<(V > 1)>(mean, team, t, scratch[0][0]);
+        if (V == 1) __syncwarp();
+        stage_next(row + stride);  // behind the sum's barrier: everyone has read the place
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             mean[i] *= a.inverse;
@@ -337,12 +333,8 @@ int launch_forward_rows(const Call& c, const ForwardArgs<kType>& a, int team, cu
     static std::atomic<uint64_t> known[kMaxTeam / 32 + 1];
     const auto kern = norm_forward_rows_kernel<kType, V, R, kFused, kPlain>;
     const unsigned teams = V > 1 ? 1 : 128 / team, block = teams * team;
-    // places for rows in shared memory: two for every tensor, one where two are too many
-    const int tensors = kFused ? 2 : 1;
     constexpr bool kStaged = !kPlain && kType == QFMT_F32;
-    const size_t place = (size_t)teams * tensors * staged_row_bytes(a.cols);
-    const int slots = !kStaged ? 0 : c.hist_bytes + 2 * place <= kMostShared / 2 ? 2 * tensors : tensors;
-    const size_t smem = c.hist_bytes + place * slots / tensors;
+    const size_t smem = c.hist_bytes + (kStaged ? (size_t)teams * (kFused ? 2 : 1) * staged_row_bytes(a.cols) : 0);
     static std::atomic<bool> allowed[64];
     if (kStaged) {
         const int rc = allow_shared(kern, kMostShared, c.dev, allowed);
@@ -360,7 +352,7 @@ int launch_forward_rows(const Call& c, const ForwardArgs<kType>& a, int team, cu
     const unsigned blocks = (unsigned)(want < cap ? want : cap);
     const int64_t stride = (int64_t)blocks * teams * R;
     const ForwardSteps step = {stride * a.x.ld, stride * a.residual.ld, stride * a.h.ld, stride * a.y.ld};
-    QFMT_CUDA_TRY(launch_overlapping(kern, blocks, block, smem, stream, a, team, step, (int)(c.hist_bytes / 4), slots));
+    QFMT_CUDA_TRY(launch_overlapping(kern, blocks, block, smem, stream, a, team, step, (int)(c.hist_bytes / 4)));
     return QFMT_OK;
 }
 
