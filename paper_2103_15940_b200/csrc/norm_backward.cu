@@ -224,10 +224,11 @@ __device__ __forceinline__ void put_columns(int i, float4 s, int padded, int col
 // stay in the registers of the thread that owns their columns from row to row, and a block leaves one part.
 // kParts: a team is a part of a warp (or all of it), otherwise whole warps; a block has 512 threads' worth of teams.
 // V > 1 (wide rows): the team is the block, and the column sums lie in shared memory, each thread's its own, since the
-// registers hold V granules of dy and h; with V > 2 the weight is read from the cache as well.
+// registers hold V granules of dy and h; with V = 4 the weight is read from the cache as well.
 // kPlain and kStaged as in the forward pass (staged bfloat16 rows took 75 us where shifted pieces take 44); with
 // registers to spare (kAhead) the next rows are on their way while these are worked on.  Staged rows have two
-// places a team, or one for h and dy in turn; the next ones are copied as soon as they have been read.  A team takes `group` neighbouring rows (R, or R = 1 at a time), then the group that is a step away.
+// places a team, or one for h and dy in turn; the next ones are copied as soon as they have been read.
+// A team takes `group` neighbouring rows (R, or R = 1 at a time), then the group that is a step away.
 template <int kType, int V, int R, bool kParts, bool kFused, bool kPlain>
 __global__ void __launch_bounds__(kMaxTeam)
 norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, const BackwardSteps step, int hist_words, int sum_words,
@@ -251,7 +252,7 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
     const uint64_t offset = kFused ? drop_offset(a.drop) : 0ull;
     const int next = team * kGranule;  // elements between a thread's granules
     int n[V];
-    Granule w[V <= 2 ? V : 1], dw = splat(0.0f), db = splat(0.0f);  // the sums with V = 1
+    Granule w[V <= 3 ? V : 1], dw = splat(0.0f), db = splat(0.0f);  // the sums with V = 1
     float4* const sums_in_shared = reinterpret_cast<float4*>(dynamic + hist_words);  // with V > 1: [V][4][team]
 #pragma unroll
     for (int k = 0; k < V; ++k) {
@@ -307,7 +308,7 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
     };
     stage_next(row);
 #pragma unroll
-    for (int k = 0; k < (V <= 2 ? V : 0); ++k) w[k] = load_columns(a.weight, k * team + t, n[k], 1.0f);
+    for (int k = 0; k < (V <= 3 ? V : 0); ++k) w[k] = load_columns(a.weight, k * team + t, n[k], 1.0f);
     int parity = 0;
     bool second = false;
     for (uint32_t first = blockIdx.x * teams * group; first < rows; parity ^= 1) {  // the row of the block's first team
@@ -344,8 +345,8 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
                 const Raw<kType> hs = words<kType, kPlain || kStaged>(raw_h[i][k], ph + i * a.h.ld + k * next, there);
                 dy[i][k] = widen_raw<kType>(ds);
                 xhat[i][k] = normalise<kPlain>(widen_raw<kType>(hs), mean[i], rstd[i], there);
-                if (V > 2) w[0] = load_columns(a.weight, k * team + t, n[k], 1.0f);
-                s[i] = add2(s[i], row_sums(dy[i][k], xhat[i][k], w[V <= 2 ? k : 0]));
+                if (V > 3) w[0] = load_columns(a.weight, k * team + t, n[k], 1.0f);
+                s[i] = add2(s[i], row_sums(dy[i][k], xhat[i][k], w[V <= 3 ? k : 0]));
                 if constexpr (V == 1) {
                     add_columns(dw, db, dy[i][k], xhat[i][k]);
                 } else {
@@ -374,8 +375,8 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
             const float c1 = s[i].x * a.inverse, c2 = s[i].y * a.inverse;
 #pragma unroll
             for (int k = 0; k < V; ++k) {
-                if (V > 2) w[0] = load_columns(a.weight, k * team + t, n[k], 1.0f);
-                store_gradients<kType, kFused, kPlain>(a, to, i, k * next, dy[i][k], xhat[i][k], w[V <= 2 ? k : 0], this_rstd[i], c1, c2, row + i,
+                if (V > 3) w[0] = load_columns(a.weight, k * team + t, n[k], 1.0f);
+                store_gradients<kType, kFused, kPlain>(a, to, i, k * next, dy[i][k], xhat[i][k], w[V <= 3 ? k : 0], this_rstd[i], c1, c2, row + i,
                                                        k * team + t, row + i < rows ? n[k] : 0, from, after, offset, hist);
             }
         }
