@@ -4,12 +4,11 @@
 // bias run along with the rows, in the registers of the thread that owns the columns, so nothing is read again for
 // them; each SM's one block of 512 threads leaves one part of 2 n sums and a second kernel joins the 148 parts, in an
 // order that depends on sizes alone.  Measured choices:
-//   * one granule a thread and two rows at a time: 31 us for dx and the sums of 16384 x 1024 fp32, where two granules
-//     and one row took 43;
+//   * up to 1280 columns one granule a thread and two rows at a time: 35.5 us for dx and the sums of 16384 x 1024 fp32; wider
+//     rows by the rule at backward_plan;
 //   * teams of one block, joined through its shared memory: small blocks in clusters that add up their sums through
 //     distributed shared memory took 4 to 5 us more at the end of every call;
-//   * at 4096 columns one team of 512 threads beats two of 256 with two granules (77 us against 100 on 16384 rows);
-//   * up to 4096 columns the sums are registers; beyond, the registers hold the row and the sums lie in shared memory.
+//   * with one granule a thread the sums are registers; with more, the registers hold the row and the sums lie in shared memory.
 // Measured: fused 8192 x 1024 fp32 26.5 us (5.1 TB/s, 0.78 of the measured copy rate), fused 8192 x 4096 bfloat16 52.7 us
 // (5.1 TB/s), fused 16384 x 4096 fp32 186 us (5.8 TB/s), 4096 x 768 binary16 7.6 us, of which joining takes 3.
 #include <cuda_runtime.h>
@@ -207,6 +206,7 @@ __device__ __forceinline__ float4 quad(const Granule& v, int i) { return make_fl
 __device__ __forceinline__ Granule from_quads(float4 a, float4 b) {
     return {{make_float2(a.x, a.y), make_float2(a.z, a.w), make_float2(b.x, b.y), make_float2(b.z, b.w)}};
 }
+__device__ __forceinline__ float4 sum_of(float4 a, float4 b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
 
 // Four columns of dweight and dbias laid side by side, from column 4 i on.
 __device__ __forceinline__ void put_columns(int i, float4 s, int padded, int cols, float* dweight, float* dbias) {
@@ -223,8 +223,8 @@ __device__ __forceinline__ void put_columns(int i, float4 s, int padded, int col
 // The backward pass of rows that a team holds in registers, R at a time: dy and h are read once, the sums over rows
 // stay in the registers of the thread that owns their columns from row to row, and a block leaves one part.
 // kParts: a team is a part of a warp (or all of it), otherwise whole warps; a block has 512 threads' worth of teams.
-// V > 1 (wide rows): the team is the block, and the column sums lie in shared memory, each thread's its own, since the
-// registers hold V granules of dy and h; with V = 4 the weight is read from the cache as well.
+// V > 1 (wide rows): the column sums lie in shared memory, each thread's its own, since the registers hold V granules of
+// dy and h; V > 2: the team is the block; with V = 4 the weight is read from the cache as well.
 // kPlain and kStaged as in the forward pass (staged bfloat16 rows took 75 us where shifted pieces take 44); with
 // registers to spare (kAhead) the next rows are on their way while these are worked on.  Staged rows have two
 // places a team, or one for h and dy in turn; the next ones are copied as soon as they have been read.
@@ -246,14 +246,14 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
     }
     if (hist != nullptr) clear_hist(hist, a.quant);
     // (the shuffle tells the compiler that a warp belongs to one team)
-    const int mine = V > 1 ? 0 : kParts ? threadIdx.x / team : __shfl_sync(0xFFFFFFFFu, threadIdx.x / team, 0);
-    const int t = threadIdx.x - mine * team, teams = V > 1 ? 1 : blockDim.x / team;
+    const int mine = V > 2 ? 0 : kParts ? threadIdx.x / team : __shfl_sync(0xFFFFFFFFu, threadIdx.x / team, 0);
+    const int t = threadIdx.x - mine * team, teams = V > 2 ? 1 : blockDim.x / team;
     const bool from = (t & 31) != 0, after = (t & 31) != 31 && t + 1 < team;
     const uint64_t offset = kFused ? drop_offset(a.drop) : 0ull;
     const int next = team * kGranule;  // elements between a thread's granules
     int n[V];
     Granule w[V <= 3 ? V : 1], dw = splat(0.0f), db = splat(0.0f);  // the sums with V = 1
-    float4* const sums_in_shared = reinterpret_cast<float4*>(dynamic + hist_words);  // with V > 1: [V][4][team]
+    float4* const sums_in_shared = reinterpret_cast<float4*>(dynamic + hist_words) + (V == 2 ? mine * V * 4 * team : 0);  // with V > 1: [teams][V][4][team]
 #pragma unroll
     for (int k = 0; k < V; ++k) {
         n[k] = granule_columns(a.cols, k * team + t);
@@ -291,7 +291,7 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
         if constexpr (kStaged) if (at < rows) stage_row(place, p, (int)a.cols, t, team);
     };
     const auto arrived = [&]() {  // every thread's copies, for the whole team
-        if constexpr (V > 1) __syncthreads();
+        if constexpr (V > 2) __syncthreads();
         else if constexpr (kParts) __syncwarp();
         else asm volatile("bar.sync %0, %1;" ::"r"(1 + mine), "r"(team) : "memory");
     };
@@ -391,11 +391,26 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
     const bool alone = a.dweight != nullptr || a.dbias != nullptr;  // this block's part is the result
     if (kStaged) stage_wait();
     if (a.partial == nullptr) return;
-    // [dweight, dbias][padded columns] of every warp of small teams, or of every team; then their sum
+    // [dweight, dbias][padded columns]
     const int padded = ((int)a.cols + kGranule - 1) / kGranule * kGranule, quads = padded / 2;
-    const int units = kParts ? blockDim.x / 32 : teams;
     float4* const part = reinterpret_cast<float4*>(a.partial) + (int64_t)blockIdx.x * quads;
-    float4* const sums = units > 1 ? reinterpret_cast<float4*>(dynamic + hist_words) : part;  // (a wide row's own sums stay where they are)
+    if constexpr (V > 1) {  // the sum of every team's
+        __syncthreads();
+        const float4* const sums = reinterpret_cast<const float4*>(dynamic + hist_words);
+        for (int i = threadIdx.x; i < V * 4 * team; i += blockDim.x) {
+            const int g = i / (4 * team) * team + i % team, which = i / team % 4;
+            if (g >= padded / kGranule) continue;
+            float4 s = sums[i];
+            for (int u = 1; u < teams; ++u) s = sum_of(s, sums[u * V * 4 * team + i]);
+            const int at = g * 2 + (which & 1) + (which >= 2 ? quads / 2 : 0);
+            if (alone) put_columns(at, s, padded, (int)a.cols, a.dweight, a.dbias);
+            else part[at] = s;
+        }
+        return;
+    }
+    // that of every warp of small teams, or of every team; then their sum
+    const int units = kParts ? blockDim.x / 32 : teams;
+    float4* const sums = units > 1 ? reinterpret_cast<float4*>(dynamic + hist_words) : part;
     float4* const own = sums + (kParts ? threadIdx.x / 32 : mine) * quads;
     if constexpr (kParts) {
         for (int off = 16; off >= team; off >>= 1) {  // the teams of a warp
@@ -406,15 +421,8 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
             }
         }
     }
-#pragma unroll
-    for (int k = 0; k < V; ++k) {
-        if ((kParts && (threadIdx.x & 31) >= team) || n[k] == 0) continue;
-        if (V > 1) {
-            const float4* const q = sums_in_shared + 4 * k * team + t;
-            dw = from_quads(q[0], q[team]);
-            db = from_quads(q[2 * team], q[3 * team]);
-        }
-        float4* const q = own + (k * team + t) * 2;
+    if (!(kParts && (threadIdx.x & 31) >= team) && n[0] != 0) {
+        float4* const q = own + t * 2;
         q[0] = quad(dw, 0), q[1] = quad(dw, 1);
         q[quads / 2] = quad(db, 0), q[quads / 2 + 1] = quad(db, 1);
     }
@@ -422,10 +430,7 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
     __syncthreads();
     for (int i = threadIdx.x; i < quads; i += blockDim.x) {
         float4 s = sums[i];
-        for (int u = 1; u < units; ++u) {
-            const float4 q = sums[u * quads + i];
-            s = make_float4(s.x + q.x, s.y + q.y, s.z + q.z, s.w + q.w);
-        }
+        for (int u = 1; u < units; ++u) s = sum_of(s, sums[u * quads + i]);
         if (alone) put_columns(i, s, padded, (int)a.cols, a.dweight, a.dbias);
         else part[i] = s;
     }
@@ -445,10 +450,7 @@ norm_join_parts_kernel(const float4* partial, int parts, int padded, int cols, f
     float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     if (q < quads) {
 #pragma unroll 5
-        for (int k = warp; k < parts; k += kJoinWarps) {
-            const float4 v = partial[(int64_t)k * quads + q];
-            s = make_float4(s.x + v.x, s.y + v.y, s.z + v.z, s.w + v.w);
-        }
+        for (int k = warp; k < parts; k += kJoinWarps) s = sum_of(s, partial[(int64_t)k * quads + q]);
     }
     sums[warp][lane] = s;
     __syncthreads();
@@ -462,13 +464,29 @@ norm_join_parts_kernel(const float4* partial, int parts, int padded, int cols, f
     if (out != nullptr && c < cols) out[c] = u;
 }
 
-Plan backward_plan(int64_t cols) { return make_plan(cols, 1, 4); }
+// One granule a thread; two and more, teams half as large, beyond 1280 columns where there are enough rows (16 a block of
+// containers, 32 of codes) and it pays: with containers (fused: unless the larger teams fill 512 threads), with codes where the
+// larger teams leave three eighths of 512 without work (2049 to 2560 columns).  dx and the sums / fused, two granules against
+// one, us: fp32 16384 x 1536 50 against 57 / 73 against 75, x 2048 64 against 68 / 97 against 90, x 2560 79 against 110 / 119
+// against 145, ragged x 2556 119 against 194 / 147 against 215, x 3496 110 against 136 / 158 against 177, x 4096 121 against 143
+// / 190 against 186, x 1024 36 against 36 / 49 against 46; 3000 x 2560 17 against 23 / 24 against 33, 2048 x 2560 13.7 against
+// 12.8 / 16.4 against 18.3, 400 x 2560 8.1 against 7.6 / 8.9 against 8.3.  bfloat16 16384 x 2560 54 against 62 / 67 against 76,
+// ragged x 2556 114 against 139 / 202 against 178 (registers spill), 9899 x 2816 41.7 against 40.1 / 52 against 50, 16384 x 4096
+// 79 against 77 / 100 against 99, 2000 x 2560 11.4 against 10.4 / 14.6 against 13.9.
+constexpr int kMaxParts = 148;  // the blocks of the rows kernel, one on each of a B200's SMs
+Plan backward_plan(const qfmt_norm_t& s, bool fused) {
+    const Plan one = make_plan(s.cols, 1, 4);
+    if (one.granules != 1 || one.team <= 160) return one;
+    const int used = kMaxTeam / one.team * one.team;
+    const bool containers = s.dtype == QFMT_F32;
+    const bool pays = containers ? !fused || used < kMaxTeam : used <= kMaxTeam - 3 * kMaxTeam / 8;
+    return pays && s.rows >= (containers ? 16 : 32) * kMaxParts ? make_plan(s.cols, 2, 4) : one;
+}
 
-// Parts that the backward pass leaves for the gradients of weight and bias: one per block of the rows kernel,
-// which has a block on each of a B200's SMs, or a share of the rows for long rows.
-constexpr int kMaxParts = 148;
+// Parts that the backward pass leaves for the gradients of weight and bias: one per block of the rows kernel, or a
+// share of the rows for long rows.
 int row_parts(const qfmt_norm_t& s) {
-    if (backward_plan(s.cols).team != 0) return kMaxParts;  // more than the loop would need
+    if (backward_plan(s, false).team != 0) return kMaxParts;  // more than the loop would need
     const int64_t want = (s.rows + 8 * kColumnWarps - 1) / (8 * kColumnWarps);
     return (int)(want < 64 ? (want > 0 ? want : 1) : 64);
 }
@@ -484,7 +502,7 @@ int join_parts(const float* partial, int parts, int64_t cols, float* d_dweight, 
 
 // Shared memory for the column sums of a block of the backward pass.
 size_t backward_sum_bytes(int v, bool parts, int team, int64_t cols) {
-    if (v > 1) return (size_t)team * v * 64;
+    if (v > 1) return (size_t)(kMaxTeam / team) * team * v * 64;
     const int units = parts ? kMaxTeam / team * team / 32 : kMaxTeam / team;
     return units > 1 ? 2 * sizeof(float) * (size_t)padded_columns(cols) * units : 0;
 }
@@ -515,7 +533,7 @@ int launch_backward_rows(const Call& c, BackwardArgs<kType> a, int team, int gro
 template <int kType, bool kFused>
 int launch_backward(const Call& c, const BackwardArgs<kType>& a, float* d_dweight, float* d_dbias, cudaStream_t stream) {
     if (a.rows == 0) return join_parts(a.partial, 0, a.cols, d_dweight, d_dbias, stream);  // zeros
-    const Plan plan = backward_plan(a.cols);
+    const Plan plan = backward_plan(c.norm, kFused);
     const bool plain = plain_layout(a.cols, {a.dy.whole, a.dh.whole, a.h.whole, a.dx.whole, a.dresidual.whole}) && !a.fmt;
     // (the widest rows with a histogram of 256 bins leave no place for a row)
     const bool fits = plain || plan.granules < 3 || kType != QFMT_F32 ||

@@ -564,6 +564,27 @@ def test_fused_backward_parts(rows, cols, kind):
     assert torch.equal(got[1], full[1]) and np.array_equal(stats.cpu().numpy().view(np.uint64), st)
 
 
+@pytest.mark.parametrize("kind", ref.KINDS)
+@pytest.mark.parametrize("rows,cols", [(2367, 1283), (2368, 1281), (2500, 1533), (2400, 2048), (2368, 2560), (4735, 2056), (4736, 2049), (2375, 3071)])
+def test_backward_of_several_teams_with_two_granules(rows, cols, kind):
+    """Widths at which several teams of a block hold two granules a thread where there are enough rows."""
+    test_norm_backward(rows, cols, kind)
+    test_fused_backward(rows, cols, kind)
+
+
+@pytest.mark.parametrize("kind", ref.KINDS)
+@pytest.mark.parametrize("rows,cols", [(4740, 2049)])
+def test_parts_of_several_teams_with_two_granules(rows, cols, kind):
+    test_norm_backward_parts(rows, cols, kind)
+    test_fused_backward_parts(rows, cols, kind)
+
+
+@pytest.mark.parametrize("kind,e,m", FORMATS)
+@pytest.mark.parametrize("rows,cols", [(2368, 1530), (4736, 2558)])
+def test_rounded_gradients_of_several_teams_with_two_granules(rows, cols, kind, e, m):
+    test_rounded_gradients_of_wide_rows(rows, cols, kind, e, m)
+
+
 # ---- how calls sit in a program ---------------------------------------------------------------------------------------
 
 
