@@ -547,7 +547,11 @@ int launch_backward(const Call& c, const BackwardArgs<kType>& a, float* d_dweigh
         const int teams = kMaxTeam / plan.team, cap = std::min(c.dev.sm_count, kMaxParts);
         const bool few = plan.granules == 1 && a.partial != nullptr && a.rows <= (plan.team <= 128 ? 4 : 2) * teams;
         const int group = plan.granules == 1 && (few || a.rows > 2 * ((int64_t)teams * cap - 1)) ? 2 : 1;
-        const int blocks = few ? 1 : (int)std::min<int64_t>((a.rows + (int64_t)teams * group - 1) / ((int64_t)teams * group), cap);
+        // With one granule as few blocks as take no more turns, so fewer parts are joined (5000 x 256 bfloat16 6.6 -> 5.8 us, 700 x
+        // 2048 6.9 -> 6.5, 400 x 4096 fp32 9.0 -> 8.7, 8192 x 1024 bfloat16 11.0 -> 11.2; wide rows mixed: 331 x 8192 11.4 -> 11.8).
+        const int64_t units = (a.rows + (int64_t)teams * group - 1) / ((int64_t)teams * group);
+        const int64_t turns = plan.granules == 1 ? (units + cap - 1) / cap : 1;
+        const int blocks = few ? 1 : (int)std::min<int64_t>((units + turns - 1) / turns, cap);
         const auto run = plan.granules == 3   ? (plain ? launch_backward_rows<kType, 3, 1, false, kFused, true>
                                                        : launch_backward_rows<kType, 3, 1, false, kFused, false>)
                          : plan.granules == 4 ? (plain ? launch_backward_rows<kType, 4, 1, false, kFused, true>
