@@ -299,8 +299,10 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
     const bool pairs = R == 1 && group == 2;
     const auto advance = [&](bool second, auto*& p, int64_t ld, int64_t by) { p += pairs ? (second ? by - ld : ld) : by; };
     if (kAhead) fetch_rows(row);
+    [[maybe_unused]] int skew_h = 0, skew_dy = 0;
     const auto stage_next = [&](uint32_t at) {
         if constexpr (kStaged) {
+            skew_h = row_skew(ph), skew_dy = row_skew(pdy);
             stage(at, places, ph);
             if (slots == 2) stage(at, places + row_bytes, pdy);
             stage_end();
@@ -319,7 +321,7 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
             stage_wait();
             arrived();
 #pragma unroll
-            for (int k = 0; k < V; ++k) raw_h[0][k] = staged_granule(places, k * team + t, there ? n[k] : 0);
+            for (int k = 0; k < V; ++k) raw_h[0][k] = staged_granule(places, skew_h, k * team + t, there ? n[k] : 0);
             if (slots == 1) {
                 arrived();  // h has been read by everyone
                 stage(row, places, pdy);
@@ -329,7 +331,7 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
             }
             const uint32_t place = slots == 2 ? places + row_bytes : places;
 #pragma unroll
-            for (int k = 0; k < V; ++k) raw_dy[0][k] = staged_granule(place, k * team + t, there ? n[k] : 0);
+            for (int k = 0; k < V; ++k) raw_dy[0][k] = staged_granule(place, skew_dy, k * team + t, there ? n[k] : 0);
         }
         Granule dy[R][V], xhat[R][V];
         float2 s[R];
@@ -468,7 +470,7 @@ norm_join_parts_kernel(const float4* partial, int parts, int padded, int cols, f
 // containers, 32 of codes) and it pays: with containers (fused: unless the larger teams fill 512 threads), with codes where the
 // larger teams leave three eighths of 512 without work (2049 to 2560 columns).  dx and the sums / fused, two granules against
 // one, us: fp32 16384 x 1536 50 against 57 / 73 against 75, x 2048 64 against 68 / 97 against 90, x 2560 79 against 110 / 119
-// against 145, ragged x 2556 119 against 194 / 147 against 215, x 3496 110 against 136 / 158 against 177, x 4096 121 against 143
+// against 145, ragged x 2556 121 against 194 / 159 against 215, x 3496 110 against 136 / 158 against 177, x 4096 121 against 143
 // / 190 against 186, x 1024 36 against 36 / 49 against 46; 3000 x 2560 17 against 23 / 24 against 33, 2048 x 2560 13.7 against
 // 12.8 / 16.4 against 18.3, 400 x 2560 8.1 against 7.6 / 8.9 against 8.3.  bfloat16 16384 x 2560 54 against 62 / 67 against 76,
 // ragged x 2556 114 against 139 / 202 against 178 (registers spill), 9899 x 2816 41.7 against 40.1 / 52 against 50, 16384 x 4096

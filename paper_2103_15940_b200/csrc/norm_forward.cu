@@ -175,7 +175,7 @@ struct ForwardSteps {
 // rows while these are worked on.  Otherwise any layout and an optional format: codes come as aligned pieces that are
 // shifted into place; rows of containers (kStaged) go through shared memory behind the histogram, where the next row
 // is copied as soon as this one has been read from there by its whole team.  Each way is the faster one for its type:
-// 16384 rows of 1021 take 25 us as shifted bfloat16 pieces and 31 us staged, as fp32 39 us shifted and 34 us staged.
+// 16384 rows of 1021 take 25 us as shifted bfloat16 pieces and 31 us staged, as fp32 39 us shifted and 31 us staged.
 template <int kType, int V, int R, bool kFused, bool kPlain>
 __global__ void __launch_bounds__(kMaxTeam)
 norm_forward_rows_kernel(const ForwardArgs<kType> a, int team, const ForwardSteps step, int hist_words) {
@@ -225,8 +225,10 @@ norm_forward_rows_kernel(const ForwardArgs<kType> a, int team, const ForwardStep
     };
     const uint32_t row_bytes = staged_row_bytes(a.cols);
     const uint32_t place = shared_address(dynamic + hist_words) + mine * (kFused ? 2 : 1) * row_bytes;  // of the team
+    [[maybe_unused]] int skew_x = 0, skew_r = 0;
     const auto stage_next = [&]([[maybe_unused]] uint32_t at) {  // the next row through shared memory
         if constexpr (kStaged) {
+            skew_x = row_skew(px), skew_r = row_skew(pr);
             if (at < rows) {
                 stage_row(place, px, (int)a.cols, t, team);
                 if (residual) stage_row(place + row_bytes, pr, (int)a.cols, t, team);
@@ -254,8 +256,8 @@ norm_forward_rows_kernel(const ForwardArgs<kType> a, int team, const ForwardStep
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 const int there = row < rows ? n[k] : 0;
-                x[0][k] = staged_granule(place, k * team + t, there);
-                if (kFused) r[0][k] = staged_granule(place + row_bytes, k * team + t, residual ? there : 0);
+                x[0][k] = staged_granule(place, skew_x, k * team + t, there);
+                if (kFused) r[0][k] = staged_granule(place + row_bytes, skew_r, k * team + t, residual ? there : 0);
             }
         } else if (!kAhead) {
             fetch_rows(row);
