@@ -175,9 +175,17 @@ struct ForwardSteps {
 // rows while these are worked on.  Otherwise any layout and an optional format: codes come as aligned pieces that are
 // shifted into place; rows of containers (kStaged) go through shared memory behind the histogram, where the next row
 // is copied as soon as this one has been read from there by its whole team.  Each way is the faster one for its type:
-// 16384 rows of 1021 take 25 us as shifted bfloat16 pieces and 31 us staged, as fp32 39 us shifted and 31 us staged.
+// 16384 rows of 1021 take 23 us as shifted bfloat16 pieces and 31 us staged, as fp32 39 us shifted and 30 us staged.
+// Registers: 128 for a team of 512; fewer where more blocks on an SM are worth more, the general variant without dropout
+// (fp32 16384 x 4093 at 81, 80, 72, 64: 144, 122, 125, 126 us; bfloat16 at 94, 96, 80, 72: 130, 120, 109, 127, but x 2049 67, 62,
+// 71, 74; 2048 x 10237 at 94, 72: 47, 39.  With dropout they spill: bfloat16 16384 x 4093 at 128, 80: 206, 240).
+constexpr int forward_registers(int type, int v, bool fused, bool plain) {
+    if (plain || fused || v == 4) return 128;
+    if (v == 1) return 64;
+    return type == QFMT_F32 ? (v == 2 ? 80 : 64) : (v == 2 ? 96 : 72);
+}
 template <int kType, int V, int R, bool kFused, bool kPlain>
-__global__ void __launch_bounds__(kMaxTeam)
+__global__ void __maxnreg__((forward_registers(kType, V, kFused, kPlain)))
 norm_forward_rows_kernel(const ForwardArgs<kType> a, int team, const ForwardSteps step, int hist_words) {
     // Wide rows keep the weights where that leaves the blocks of an SM as many as before (2048 rows of 16384 bfloat16: 39 us
     // against 50, fused fp32 100 against 90; of 12288: fused bfloat16 49 against 54, fp32 54 against 37).
