@@ -9,8 +9,8 @@
 //   * weight and bias stay in registers from row to row; four granules a thread without them took 75 us (their
 //     reads from L1 are four times the row's);
 //   * the next rows' granules are loaded while these are worked on.
-// Measured: 16384 x 4096 bfloat16 47.1 us (5.7 TB/s, 0.88 of the measured copy rate), 4096 x 768 fp32 4.8 us, fused
-// 8192 x 1024 bfloat16 14.6 us (4.6 TB/s), fused 16384 x 4096 bfloat16 87 us (6.1 TB/s), fp32 182 us (5.9 TB/s).
+// Measured: 16384 x 4096 bfloat16 46.8 us (5.7 TB/s, 0.89 of the measured copy rate), 4096 x 768 fp32 4.8 us, fused
+// 8192 x 1024 bfloat16 14.9 us (4.5 TB/s), fused 16384 x 4096 bfloat16 87 us (6.1 TB/s), fp32 182 us (5.9 TB/s).
 #include <cuda_runtime.h>
 #include <stdint.h>
 
