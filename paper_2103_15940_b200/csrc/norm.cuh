@@ -53,6 +53,14 @@ __device__ __forceinline__ Granule load_columns(const float* p, int64_t g, int n
     return v;
 }
 
+// Column i of dweight and dbias laid side by side, each padded to whole granules.  In 64 bits: i runs to twice the
+// padded columns, and a row may have 2^31 - 1.
+struct JoinedColumn {
+    bool second;  // of dbias
+    int64_t c;    // may lie in the padding
+};
+__host__ __device__ __forceinline__ JoinedColumn joined_column(int64_t i, int64_t padded) { return {i >= padded, i >= padded ? i - padded : i}; }
+
 template <int kType, bool kPlain, typename Args>
 __device__ __forceinline__ Raw<kType> finish_output(const Args& a, const Granule& v, int n, uint32_t* hist) {
     return !kPlain && a.fmt ? finish_format<kType>(v, n, a.quant, hist) : finish<kType>(v);

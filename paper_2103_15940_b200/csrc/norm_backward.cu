@@ -443,16 +443,16 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
 // kernel) is its launch and two dependent reads; one column a lane took 17 us instead of 10 at 16384 columns.
 constexpr int kJoinWarps = 32;
 __global__ void __launch_bounds__(32 * kJoinWarps)
-norm_join_parts_kernel(const float4* partial, int parts, int padded, int cols, float* dweight, float* dbias) {
+norm_join_parts_kernel(const float4* partial, int parts, int64_t padded, int64_t cols, float* dweight, float* dbias) {
     __shared__ float4 sums[kJoinWarps][32];
     grid_launch_dependents();
     grid_dependency_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int quads = padded / 2, q = blockIdx.x * 32 + lane;
+    const int64_t quads = padded / 2, q = (int64_t)blockIdx.x * 32 + lane;
     float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     if (q < quads) {
 #pragma unroll 5
-        for (int k = warp; k < parts; k += kJoinWarps) s = sum_of(s, partial[(int64_t)k * quads + q]);
+        for (int k = warp; k < parts; k += kJoinWarps) s = sum_of(s, partial[k * quads + q]);
     }
     sums[warp][lane] = s;
     __syncthreads();
@@ -460,10 +460,9 @@ norm_join_parts_kernel(const float4* partial, int parts, int padded, int cols, f
     float u = 0.0f;
 #pragma unroll
     for (int w = 0; w < kJoinWarps; ++w) u += reinterpret_cast<const float*>(sums[w])[threadIdx.x];
-    int c = blockIdx.x * 128 + threadIdx.x;
-    float* out = dweight;
-    if (c >= padded) c -= padded, out = dbias;
-    if (out != nullptr && c < cols) out[c] = u;
+    const JoinedColumn at = joined_column((int64_t)blockIdx.x * 128 + threadIdx.x, padded);
+    float* const out = at.second ? dbias : dweight;
+    if (out != nullptr && at.c < cols) out[at.c] = u;
 }
 
 // One granule a thread; two and more, teams half as large, beyond 1280 columns where there are enough rows (16 a block of
@@ -498,7 +497,7 @@ int64_t padded_columns(int64_t cols) { return (cols + kGranule - 1) / kGranule *
 int join_parts(const float* partial, int parts, int64_t cols, float* d_dweight, float* d_dbias, cudaStream_t stream) {
     const int64_t padded = padded_columns(cols);
     QFMT_CUDA_TRY(launch_overlapping(norm_join_parts_kernel, (unsigned)((2 * padded + 127) / 128), 32u * kJoinWarps, 0, stream,
-                                     reinterpret_cast<const float4*>(partial), parts, (int)padded, (int)cols, d_dweight, d_dbias));
+                                     reinterpret_cast<const float4*>(partial), parts, padded, cols, d_dweight, d_dbias));
     return QFMT_OK;
 }
 

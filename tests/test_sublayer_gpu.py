@@ -617,6 +617,37 @@ def test_offsets_beyond_32_bits():
     ref.close(db, want[2], want[5])
 
 
+def test_column_sums_of_more_than_two_to_the_thirty_columns():
+    """[dweight, dbias] side by side pass 2^31 places.  With one row dbias is dy and dweight is dy xhat, each rounding known."""
+    cols = (1 << 30) + 8
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    x, dy = (torch.empty(1, cols, dtype=torch.bfloat16, device=DEV).normal_(generator=gen) for _ in range(2))
+    norm = qf.make_norm(1, cols, torch.bfloat16, EPS)
+    ws = torch.empty(qf.qfmt_layer_norm_workspace_bytes(norm), dtype=torch.uint8, device=DEV)
+    grads = torch.full((2 * cols + 24,), SENTINEL, device=DEV)
+    dw, db = grads[8:8 + cols], grads[16 + cols:16 + 2 * cols]
+    mean, rstd = torch.tensor([0.25], device=DEV), torch.tensor([1.5], device=DEV)
+    qf.qfmt_layer_norm_backward(norm, dy, x, mean, rstd, None, None, dw, db, ws, ws.numel())
+    for i in range(0, cols, 1 << 28):
+        part = slice(i, min(cols, i + (1 << 28)))
+        assert torch.equal(db[part], dy[0, part].float())
+        assert torch.equal(dw[part], dy[0, part].float() * ((x[0, part].float() - mean) * rstd))
+    for edge in (grads[:8], grads[8 + cols:16 + cols], grads[16 + 2 * cols:]):
+        assert torch.all(edge == SENTINEL)
+
+
+def test_column_sums_of_no_rows_of_the_widest_matrix():
+    cols = (1 << 31) - 1
+    norm = qf.make_norm(0, cols, torch.bfloat16, EPS)
+    ws = torch.empty(qf.qfmt_layer_norm_workspace_bytes(norm), dtype=torch.uint8, device=DEV)
+    grads = torch.full((2 * cols + 16,), SENTINEL, device=DEV)
+    dw, db = grads[:cols], grads[8 + cols:8 + 2 * cols]
+    qf.qfmt_layer_norm_backward(norm, None, None, None, None, None, None, dw, db, ws, ws.numel())
+    for t in (dw, db):
+        assert all(float(t[i:i + (1 << 28)].abs().max()) == 0.0 for i in range(0, cols, 1 << 28))
+    assert torch.all(grads[cols:cols + 8] == SENTINEL) and torch.all(grads[8 + 2 * cols:] == SENTINEL)
+
+
 def test_long_single_row_dropout():
     """A flat tensor as one row: granule numbers beyond 2^16."""
     n = (1 << 22) + 3
