@@ -298,7 +298,7 @@ norm_forward_rows_kernel(const ForwardArgs<kType> a, int team, const ForwardStep
             for (int k = 1; k < V; ++k) mean[i] += sum8(v[i][k]);
         }
         team_sum<(V > 1)>(mean, team, t, scratch[0][0]);
-        if (V == 1) __syncwarp();
+        if (V == 1 || team == 32) __syncwarp();  // the sum of one warp or less is shuffles, which order no memory
         stage_next(row + stride);  // behind the sum's barrier: everyone has read the place
 #pragma unroll
         for (int i = 0; i < R; ++i) {

@@ -224,6 +224,22 @@ def test_norm_without_weight_bias_or_statistics_and_in_place(kind):
     assert torch.equal(run_norm(x, w, b, kind, in_place=True, off=3, pad=2)[0], plain[0])
 
 
+@pytest.mark.parametrize("cols", [31, 253, 257, 389, 511, 515])
+def test_places_of_one_warp_are_read_before_the_next_row_arrives(cols):
+    """Ragged containers go through a place in shared memory that the next row takes over; teams of a warp or less (up to 512
+    columns) have no block-wide barrier.  Many rows a team, against the aligned layout bit by bit."""
+    gen = torch.Generator().manual_seed(cols)
+    rows = 40000
+    x, r = torch.randn(rows, cols, generator=gen), torch.randn(rows, cols, generator=gen)
+    w, b = vectors(gen, cols)
+    pad = -cols % 8
+    aligned, fused = run_norm(x, w, b, "f32", 0, pad), run_fused(x, r, w, b, 0.1, 2, 3, "f32", 0, pad)
+    for off, more in ((1, 0), (2, 1), (3, 2)):
+        for got, want in ((run_norm(x, w, b, "f32", off, more), aligned), (run_fused(x, r, w, b, 0.1, 2, 3, "f32", off, more), fused)):
+            for u, v in zip(got, want):
+                assert torch.equal(u, v)
+
+
 @pytest.mark.parametrize("cols", [64, 1000, 1024, 8200, 70001])
 def test_large_centre_loses_nothing(cols):
     """Rows whose mean is 2^12 times their spread, and rows that begin with an outlier: the variance is taken about the mean."""
