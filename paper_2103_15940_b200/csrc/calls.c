@@ -1,13 +1,14 @@
 /*
  * The Python side of the sub-layer calls (dropout, layer normalisation and their fused form): small passes whose GPU
  * work takes 2 us, as long as generic argument conversion would.  Each function takes the arguments of its C
- * counterpart in include/qfmt.h, in order: integers (addresses of records, sizes, raw pointers, the stream), None for NULL,
- * or tensors, whose data_ptr() is taken.  It returns the status.  The C functions are those of the library that the
- * binding has loaded; it hands over their addresses with bind().
+ * counterpart in include/qfmt.h, in order: for a pointer (the address of a record, the stream) an integer, None for NULL or
+ * a tensor, whose data_ptr() is taken; for a size whatever converts to an integer.  It returns the status.  The C
+ * functions are those of the library that the binding has loaded; it hands over their addresses with bind().
  */
 #define PY_SSIZE_T_CLEAN
 #define Py_LIMITED_API 0x030A0000
 #include <Python.h>
+#include <string.h>
 
 #include "qfmt.h"
 
@@ -28,21 +29,23 @@ static struct {
 
 static PyObject* data_ptr;  /* the method's name */
 
-/* The arguments as 64-bit words; 0 and an exception set if one is neither an integer, None nor a tensor. */
-static int words(PyObject* const* args, Py_ssize_t n, Py_ssize_t want, uint64_t* v) {
+/* The arguments as 64-bit words; 0 and an exception set if one is not what `kinds` says: p a pointer, i an integer.  (A size is
+ * never taken from a tensor's address.) */
+static int words(PyObject* const* args, Py_ssize_t n, const char* kinds, uint64_t* v) {
+    const Py_ssize_t want = (Py_ssize_t)strlen(kinds);
     if (n != want) {
         PyErr_Format(PyExc_TypeError, "%zd arguments expected, got %zd", want, n);
         return 0;
     }
     for (Py_ssize_t i = 0; i < n; ++i) {
-        if (args[i] == Py_None) {
-            v[i] = 0;
-        } else if (PyLong_Check(args[i])) {
+        if (PyLong_Check(args[i])) {
             v[i] = PyLong_AsUnsignedLongLongMask(args[i]);
+        } else if (kinds[i] == 'p' && args[i] == Py_None) {
+            v[i] = 0;
         } else {
-            PyObject* p = PyObject_CallMethodObjArgs(args[i], data_ptr, NULL);
+            PyObject* p = kinds[i] == 'p' ? PyObject_CallMethodObjArgs(args[i], data_ptr, NULL) : PyNumber_Index(args[i]);
             if (p == NULL) {
-                PyErr_Format(PyExc_TypeError, "argument %zd: an address, a tensor or None expected", i);
+                if (kinds[i] == 'p') PyErr_Format(PyExc_TypeError, "argument %zd: an address, a tensor or None expected", i);
                 return 0;
             }
             v[i] = PyLong_AsUnsignedLongLongMask(p);
@@ -54,12 +57,12 @@ static int words(PyObject* const* args, Py_ssize_t n, Py_ssize_t want, uint64_t*
 }
 
 #define P(i) ((void*)(uintptr_t)v[i])
-#define CALL(function, count, ...)                                                                    \
+#define CALL(function, kinds, ...)                                                                    \
     static PyObject* py_##function(PyObject* self, PyObject* const* args, Py_ssize_t n) {             \
         uint64_t v[MOST];                                                                             \
         int status;                                                                                   \
         (void)self;                                                                                   \
-        if (!words(args, n, count, v)) return NULL;                                                   \
+        if (!words(args, n, kinds, v)) return NULL;                                                   \
         if (lib.function == NULL) {                                                                   \
             PyErr_SetString(PyExc_RuntimeError, "the library is not loaded");                         \
             return NULL;                                                                              \
@@ -70,17 +73,19 @@ static int words(PyObject* const* args, Py_ssize_t n, Py_ssize_t want, uint64_t*
         return PyLong_FromLong(status);                                                               \
     }
 
-CALL(dropout, 11, P(0), (int64_t)v[1], P(2), (int64_t)v[3], P(4), (int64_t)v[5], (int64_t)v[6], (int64_t)v[7], (int32_t)v[8], P(9), P(10))
-CALL(layer_norm, 11, P(0), P(1), P(2), P(3), P(4), P(5), P(6), P(7), P(8), (int)v[9], P(10))
-CALL(layer_norm_backward, 15, P(0), P(1), P(2), P(3), P(4), P(5), P(6), P(7), P(8), P(9), P(10), (int)v[11], P(12), (size_t)v[13], P(14))
-CALL(dropout_add_layer_norm, 14, P(0), P(1), P(2), P(3), P(4), P(5), P(6), P(7), P(8), P(9), P(10), P(11), (int)v[12], P(13))
-CALL(dropout_add_layer_norm_backward, 18, P(0), P(1), P(2), P(3), P(4), P(5), P(6), P(7), P(8), P(9), P(10), P(11), P(12), P(13), (int)v[14],
-     P(15), (size_t)v[16], P(17))
+CALL(dropout, "pipipiiiipp", P(0), (int64_t)v[1], P(2), (int64_t)v[3], P(4), (int64_t)v[5], (int64_t)v[6], (int64_t)v[7], (int32_t)v[8], P(9),
+     P(10))
+CALL(layer_norm, "pppppppppip", P(0), P(1), P(2), P(3), P(4), P(5), P(6), P(7), P(8), (int)v[9], P(10))
+CALL(layer_norm_backward, "pppppppppppipip", P(0), P(1), P(2), P(3), P(4), P(5), P(6), P(7), P(8), P(9), P(10), (int)v[11], P(12), (size_t)v[13],
+     P(14))
+CALL(dropout_add_layer_norm, "ppppppppppppip", P(0), P(1), P(2), P(3), P(4), P(5), P(6), P(7), P(8), P(9), P(10), P(11), (int)v[12], P(13))
+CALL(dropout_add_layer_norm_backward, "ppppppppppppppipip", P(0), P(1), P(2), P(3), P(4), P(5), P(6), P(7), P(8), P(9), P(10), P(11), P(12),
+     P(13), (int)v[14], P(15), (size_t)v[16], P(17))
 
 static PyObject* py_bind(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     uint64_t v[MOST];
     (void)self;
-    if (!words(args, n, 5, v)) return NULL;
+    if (!words(args, n, "ppppp", v)) return NULL;
     *(void**)&lib.dropout = P(0);
     *(void**)&lib.layer_norm = P(1);
     *(void**)&lib.layer_norm_backward = P(2);

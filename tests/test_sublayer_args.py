@@ -132,3 +132,36 @@ def test_tensors_pass_their_address():
     odd = buf[1:] if buf.data_ptr() % 2 == 0 else buf
     assert odd.data_ptr() % 2 == 1
     assert forward(x=odd) == BAD == forward(x=odd.data_ptr())
+
+
+@pytest.fixture
+def seen(lib):
+    """What the C side of qfmt_dropout and qfmt_layer_norm_backward is called with, instead of the library."""
+    calls = []
+    vp, i64 = ctypes.c_void_p, ctypes.c_int64
+    dropout = ctypes.CFUNCTYPE(ctypes.c_int, vp, i64, vp, i64, vp, i64, i64, i64, ctypes.c_int32, vp, vp)(lambda *a: calls.append(a) or 0)
+    backward = ctypes.CFUNCTYPE(ctypes.c_int, *[vp] * 11, ctypes.c_int, vp, ctypes.c_size_t, vp)(lambda *a: calls.append(a) or 0)
+    fake = [ctypes.cast(f, vp).value for f in (dropout, backward)]
+    qf._calls.bind(fake[0], 0, fake[1], 0, 0)
+    yield calls
+    qf._bind_calls(lib)
+
+
+def test_sizes_are_numbers_and_never_addresses(seen):
+    """Sizes convert as in the library's other calls (numpy integers, tensors of one integer); a tensor among them stands for
+    its value, not for its address."""
+    import numpy as np
+    import torch
+    drop, norm = qf.make_dropout(0.1, 1), qf.make_norm(4, 16, qf.QFMT_F32)
+    one = torch.tensor
+    for kind in (int, np.int64, np.uint32, one):
+        qf.qfmt_dropout(P, kind(24), P, kind(32), P, kind(40), kind(3), kind(17), qf.QFMT_F16, drop, stream=0)
+        assert seen.pop()[:9] == (P, 24, P, 32, P, 40, 3, 17, qf.QFMT_F16)
+        qf.qfmt_layer_norm_backward(norm, P, P, P, P, P, P, P, P, P, kind(4096), accumulate=kind(1), stream=0)
+        assert seen.pop()[11:14] == (1, P, 4096)
+    for bad in (None, "8", 8.0, torch.zeros(2), torch.zeros(1)):
+        with pytest.raises((TypeError, ValueError)):
+            qf.qfmt_dropout(P, bad, None, 0, P, 16, 4, 16, 0, drop, stream=0)
+        with pytest.raises((TypeError, ValueError)):
+            qf.qfmt_layer_norm_backward(norm, P, P, P, P, P, P, P, P, P, bad, stream=0)
+    assert not seen
