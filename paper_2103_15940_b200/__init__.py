@@ -451,9 +451,13 @@ def make_norm(rows: int, cols: int, dtype, eps: float = 1e-5, ld_x: int = 0, ld_
     return qfmt_norm_t(rows, cols, ld_x, ld_residual, ld_h, ld_y, ld_dy, ld_dh, ld_dx, ld_dresidual, _storage(dtype), eps)
 
 
-def _ref(record):
-    """A record's address for a call, or NULL."""
-    return None if record is None else ctypes.addressof(record)
+def _ref(record, kind):
+    """Address of a record of type `kind` for a call, or NULL."""
+    if record is None:
+        return None
+    if not isinstance(record, kind):
+        raise TypeError(f"a {kind.__name__} expected, got {type(record).__name__}")
+    return ctypes.addressof(record)
 
 
 def _sublayer(name: str, *args) -> None:
@@ -468,35 +472,35 @@ def _sublayer(name: str, *args) -> None:
 def qfmt_dropout(d_x, ld_x: int, d_residual, ld_residual: int, d_out, ld_out: int, rows: int, cols: int, dtype,
                  drop: qfmt_dropout_t, stream=None) -> None:
     """out = residual + D(x), and D's own backward pass; see qfmt_dropout in include/qfmt.h."""
-    _sublayer("dropout", d_x, ld_x, d_residual, ld_residual, d_out, ld_out, rows, cols, _storage(dtype), _ref(drop),
-              _stream_handle(stream))
+    _sublayer("dropout", d_x, ld_x, d_residual, ld_residual, d_out, ld_out, rows, cols, _storage(dtype),
+              _ref(drop, qfmt_dropout_t), _stream_handle(stream))
 
 
 def qfmt_layer_norm(norm: qfmt_norm_t, d_x, d_weight, d_bias, d_y, d_mean=None, d_rstd=None,
                     fmt: Optional[qfmt_format_t] = None, d_stats=None, accumulate: int = 0, stream=None) -> None:
     """y = LN(x), rounded to fmt with statistics if one is given; see qfmt_layer_norm in include/qfmt.h."""
-    _sublayer("layer_norm", _ref(norm), d_x, d_weight, d_bias, d_y, d_mean, d_rstd, _ref(fmt), d_stats, accumulate,
-              _stream_handle(stream))
+    _sublayer("layer_norm", _ref(norm, qfmt_norm_t), d_x, d_weight, d_bias, d_y, d_mean, d_rstd, _ref(fmt, qfmt_format_t),
+              d_stats, accumulate, _stream_handle(stream))
 
 
 def qfmt_layer_norm_workspace_bytes(norm: qfmt_norm_t) -> int:
-    return int(lib().qfmt_layer_norm_workspace_bytes(_ref(norm)))
+    return int(lib().qfmt_layer_norm_workspace_bytes(_ref(norm, qfmt_norm_t)))
 
 
 def qfmt_layer_norm_backward(norm: qfmt_norm_t, d_dy, d_x, d_mean, d_rstd, d_weight, d_dx, d_dweight, d_dbias, d_workspace,
                              workspace_bytes: int, fmt: Optional[qfmt_format_t] = None, d_stats=None, accumulate: int = 0,
                              stream=None) -> None:
     """Gradients of LN's input, weight and bias; see qfmt_layer_norm_backward in include/qfmt.h."""
-    _sublayer("layer_norm_backward", _ref(norm), d_dy, d_x, d_mean, d_rstd, d_weight, d_dx, d_dweight, d_dbias, _ref(fmt),
-              d_stats, accumulate, d_workspace, workspace_bytes, _stream_handle(stream))
+    _sublayer("layer_norm_backward", _ref(norm, qfmt_norm_t), d_dy, d_x, d_mean, d_rstd, d_weight, d_dx, d_dweight, d_dbias,
+              _ref(fmt, qfmt_format_t), d_stats, accumulate, d_workspace, workspace_bytes, _stream_handle(stream))
 
 
 def qfmt_dropout_add_layer_norm(norm: qfmt_norm_t, drop: Optional[qfmt_dropout_t], d_x, d_residual, d_weight, d_bias, d_h, d_y,
                                 d_mean=None, d_rstd=None, fmt: Optional[qfmt_format_t] = None, d_stats=None,
                                 accumulate: int = 0, stream=None) -> None:
     """h = residual + D(x), y = LN(h) in one pass; see qfmt_dropout_add_layer_norm in include/qfmt.h."""
-    _sublayer("dropout_add_layer_norm", _ref(norm), _ref(drop), d_x, d_residual, d_weight, d_bias, d_h, d_y, d_mean, d_rstd,
-              _ref(fmt), d_stats, accumulate, _stream_handle(stream))
+    _sublayer("dropout_add_layer_norm", _ref(norm, qfmt_norm_t), _ref(drop, qfmt_dropout_t), d_x, d_residual, d_weight, d_bias, d_h,
+              d_y, d_mean, d_rstd, _ref(fmt, qfmt_format_t), d_stats, accumulate, _stream_handle(stream))
 
 
 def qfmt_dropout_add_layer_norm_backward(norm: qfmt_norm_t, drop: Optional[qfmt_dropout_t], d_dy, d_dh, d_h, d_mean, d_rstd,
@@ -505,6 +509,6 @@ def qfmt_dropout_add_layer_norm_backward(norm: qfmt_norm_t, drop: Optional[qfmt_
                                          stream=None) -> None:
     """dresidual = dh + LN's gradient, dx = D(dresidual), dweight, dbias; see
     qfmt_dropout_add_layer_norm_backward in include/qfmt.h."""
-    _sublayer("dropout_add_layer_norm_backward", _ref(norm), _ref(drop), d_dy, d_dh, d_h, d_mean, d_rstd, d_weight, d_dx,
-              d_dresidual, d_dweight, d_dbias, _ref(fmt), d_stats, accumulate, d_workspace, workspace_bytes,
+    _sublayer("dropout_add_layer_norm_backward", _ref(norm, qfmt_norm_t), _ref(drop, qfmt_dropout_t), d_dy, d_dh, d_h, d_mean, d_rstd, d_weight,
+              d_dx, d_dresidual, d_dweight, d_dbias, _ref(fmt, qfmt_format_t), d_stats, accumulate, d_workspace, workspace_bytes,
               _stream_handle(stream))

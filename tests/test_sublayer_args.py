@@ -125,6 +125,29 @@ def test_argument_types():
     assert qf._calls.dropout(P, 16, None, 0, P, 16, 4, 16, 3, None, None) == BAD
 
 
+def test_records_of_another_type_are_refused():
+    """A call copies a record of the type it expects: a shorter one in its place would be read beyond its end."""
+    norm, drop, fmt = qf.make_norm(4, 16, qf.QFMT_F32), qf.make_dropout(0.1, 1), qf.make_format(6, 9)
+    for n, d, f in ((drop, drop, fmt), (norm, norm, fmt), (norm, drop, drop), (drop, norm, None), (fmt, drop, None), (norm, fmt, None),
+                    (norm, drop, norm), (P, drop, None), (norm, P, None), (norm, drop, P)):
+        with pytest.raises(TypeError):
+            qf.qfmt_dropout_add_layer_norm(n, d, None, None, P, P, None, None, fmt=f, stream=0)
+        with pytest.raises(TypeError):
+            qf.qfmt_dropout_add_layer_norm_backward(n, d, None, None, None, P, P, P, None, None, P, P, None, 0, fmt=f, stream=0)
+    for n, f in ((drop, fmt), (fmt, None), (norm, drop), (norm, norm)):
+        with pytest.raises(TypeError):
+            qf.qfmt_layer_norm(n, None, P, P, None, fmt=f, stream=0)
+        with pytest.raises(TypeError):
+            qf.qfmt_layer_norm_backward(n, None, None, P, P, P, None, P, P, None, 0, fmt=f, stream=0)
+    for d in (norm, fmt, P):
+        with pytest.raises(TypeError):
+            qf.qfmt_dropout(None, 16, None, 0, None, 16, 4, 16, 0, d, stream=0)
+    for n in (drop, fmt, P):
+        with pytest.raises(TypeError):
+            qf.qfmt_layer_norm_workspace_bytes(n)
+    assert qf.qfmt_layer_norm_workspace_bytes(None) == 0
+
+
 def test_tensors_pass_their_address():
     """A tensor stands for its data_ptr(): a misaligned one is refused as its address is."""
     import torch
