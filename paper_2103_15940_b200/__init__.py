@@ -122,13 +122,18 @@ def lib() -> ctypes.CDLL:
     return _lib
 
 
+_calls_error: Optional[ImportError] = None
+
+
 def _bind_calls(L: ctypes.CDLL) -> None:
-    """The sub-layer calls go through a module of their own, since generic conversion takes as long as their GPU work."""
-    global _calls
+    """The sub-layer calls go through a module of their own, since generic conversion takes as long as their GPU work.  Without
+    it they raise; nothing else needs it."""
+    global _calls, _calls_error
     try:
         from . import _calls
     except ImportError as e:
-        raise ImportError(f"{_HERE}/_calls.abi3.so is missing: build it with `python -m paper_2103_15940_b200.build`") from e
+        _calls, _calls_error = None, e
+        return
     _calls.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
         L.qfmt_dropout, L.qfmt_layer_norm, L.qfmt_layer_norm_backward, L.qfmt_dropout_add_layer_norm,
         L.qfmt_dropout_add_layer_norm_backward)))
@@ -464,6 +469,9 @@ def _sublayer(name: str, *args) -> None:
     """One of the sub-layer calls: integers, tensors or None, in the order of include/qfmt.h."""
     if _lib is None:
         lib()
+    if _calls is None:
+        raise ImportError(f"qfmt_{name} needs {_HERE}/_calls.abi3.so, which could not be loaded ({_calls_error}): build it with "
+                          "`python -m paper_2103_15940_b200.build`") from _calls_error
     status = getattr(_calls, name)(*args)
     if status != QFMT_OK:
         raise QfmtError(status, "qfmt_" + name)

@@ -29,21 +29,30 @@ def sources():
     return sorted(glob.glob(os.path.join(CSRC, "*.cu")))
 
 
+def headers():
+    return glob.glob(os.path.join(ROOT, "include", "*.h"))
+
+
+def older(target, deps) -> bool:
+    """Whether a target is missing or older than what it is made of."""
+    return not os.path.exists(target) or any(os.path.getmtime(d) > os.path.getmtime(target) for d in deps)
+
+
+def library_needs_build() -> bool:
+    return older(LIB, sources() + glob.glob(os.path.join(CSRC, "*.cuh")) + headers())
+
+
+def calls_need_build() -> bool:
+    return older(CALLS, glob.glob(os.path.join(CSRC, "*.c")) + headers())
+
+
 def needs_build() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(CALLS):
-        return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(CALLS))
-    deps = sources() + glob.glob(os.path.join(CSRC, "*.c")) + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(ROOT, "include", "*.h"))
-    return any(os.path.getmtime(d) > t for d in deps)
+    return library_needs_build() or calls_need_build()
 
 
-def build(force: bool = False, verbose: bool = False) -> str:
-    if not force and not needs_build():
-        return LIB
+def build_library(verbose: bool = False) -> None:
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     flags = NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-I", os.path.join(ROOT, "include"), "-I", CSRC]
-    subprocess.check_call([os.environ.get("CC", "gcc"), "-O2", "-Wall", "-fPIC", "-shared", "-I", sysconfig.get_paths()["include"],
-                           "-I", os.path.join(ROOT, "include"), "-o", CALLS, os.path.join(CSRC, "calls.c")])
     # one nvcc per source, side by side; the objects are linked into the library and go
     with tempfile.TemporaryDirectory() as tmp:
         objects = [os.path.join(tmp, os.path.basename(s) + ".o") for s in sources()]
@@ -53,6 +62,20 @@ def build(force: bool = False, verbose: bool = False) -> str:
             if code != 0:
                 raise subprocess.CalledProcessError(code, f"{nvcc} -c {src}")
         subprocess.check_call([nvcc] + NVCC_FLAGS + ["-shared", "-o", LIB] + objects)
+
+
+def build_calls() -> None:
+    subprocess.check_call([os.environ.get("CC", "gcc"), "-O2", "-Wall", "-fPIC", "-shared", "-I", sysconfig.get_paths()["include"],
+                           "-I", os.path.join(ROOT, "include"), "-o", CALLS, os.path.join(CSRC, "calls.c")])
+
+
+def build(force: bool = False, verbose: bool = False) -> str:
+    """Builds what is missing or out of date: the library first, since all calls but the sub-layer ones do without the module
+    (which needs the interpreter's headers)."""
+    if force or library_needs_build():
+        build_library(verbose)
+    if force or calls_need_build():
+        build_calls()
     return LIB
 
 
