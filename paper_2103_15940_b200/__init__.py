@@ -214,14 +214,28 @@ def _ptr(x) -> Optional[int]:
 _current_device = _current_stream = None
 
 
+def _forget_streams() -> None:
+    global _current_device, _current_stream
+    _current_device = _current_stream = None
+
+
+if hasattr(os, "register_at_fork"):
+    os.register_at_fork(after_in_child=_forget_streams)  # a forked child asks torch again, which says what it may not do
+
+
 def _stream_handle(stream) -> Optional[int]:
     if stream is None:
-        # the raw handle: building torch's stream object for it takes 3 us, as long as a launch
         global _current_device, _current_stream
-        if _current_stream is None:
-            import torch
-            _current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
-        return _current_stream(_current_device())
+        if _current_stream is not None:
+            return _current_stream(_current_device())
+        # The first call initialises torch's CUDA state.  Later ones take the raw handle where torch offers it: building its
+        # stream object takes 3 us, as long as a launch.
+        import torch
+        handle = torch.cuda.current_stream().cuda_stream
+        device, raw = (getattr(torch._C, name, None) for name in ("_cuda_getDevice", "_cuda_getCurrentRawStream"))
+        if device is not None and raw is not None:
+            _current_device, _current_stream = device, raw
+        return handle
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
