@@ -324,7 +324,7 @@ __device__ __forceinline__ Raw<kType> finish(const Granule& v) {
 
 // The same rounded to the format *p (for codes, the one of their storage type); the bins of the first `n`
 // columns are counted in the per-lane histogram `hist` when there is one.
-template <int kType>
+template <int kType, int kLanes>
 __device__ __forceinline__ Raw<kType> finish_format(const Granule& v, int n, const QuantParams& p, uint32_t* hist) {
     Raw<kType> r;
     int bin[kGranule];
@@ -339,10 +339,10 @@ __device__ __forceinline__ Raw<kType> finish_format(const Granule& v, int n, con
         }
     }
     if (hist != nullptr) {
-        const int lane = threadIdx.x & 31;
+        const int lane = threadIdx.x & (kLanes - 1);
 #pragma unroll
         for (int j = 0; j < kGranule; ++j)
-            if (j < n) atomicAdd(&hist[bin[j] * 32 + lane], 1u);
+            if (j < n) atomicAdd(&hist[bin[j] * kLanes + lane], 1u);
     }
     return r;
 }
@@ -457,16 +457,20 @@ __device__ __forceinline__ void drop_granule(const DropParams& d, uint64_t offse
 }
 
 // Per-lane histogram [bin][lane] in shared memory: cleared by the whole block, merged into the device
-// record by the whole block at the end (round.cuh).
+// record by the whole block at the end (round.cuh).  kLanes: counters of a bin, 32 (no two lanes of a warp meet) or 16 where
+// shared memory is short.
+constexpr int kHistLanes = 32;
+template <int kLanes = kHistLanes>
 __device__ __forceinline__ void clear_hist(uint32_t* hist, const QuantParams& p) {
-    for (int i = threadIdx.x; i < (p.top + kExtraBins) * 32; i += blockDim.x) hist[i] = 0u;
+    for (int i = threadIdx.x; i < (p.top + kExtraBins) * kLanes; i += blockDim.x) hist[i] = 0u;
     __syncthreads();
 }
+template <int kLanes = kHistLanes>
 __device__ __forceinline__ void flush_hist(const uint32_t* hist, const QuantParams& p, qfmt_stats_t* stats, uint64_t n_total) {
     __syncthreads();
     const int lane = threadIdx.x & 31;
     for (int b = (threadIdx.x >> 5) + 1; b < p.top + kExtraBins; b += blockDim.x >> 5) {  // bin 0 is never used
-        const uint32_t c = __reduce_add_sync(0xFFFFFFFFu, hist[b * 32 + lane]);
+        const uint32_t c = __reduce_add_sync(0xFFFFFFFFu, lane < kLanes ? hist[b * kLanes + lane] : 0u);
         if (lane == 0 && c != 0u) merge_bin(stats, p, b, c);
     }
     if (blockIdx.x == 0 && threadIdx.x == 0) atomicAdd((unsigned long long*)&stats->n_total, (unsigned long long)n_total);

@@ -61,9 +61,9 @@ struct JoinedColumn {
 };
 __host__ __device__ __forceinline__ JoinedColumn joined_column(int64_t i, int64_t padded) { return {i >= padded, i >= padded ? i - padded : i}; }
 
-template <int kType, bool kPlain, typename Args>
+template <int kType, bool kPlain, int kLanes = kHistLanes, typename Args>
 __device__ __forceinline__ Raw<kType> finish_output(const Args& a, const Granule& v, int n, uint32_t* hist) {
-    return !kPlain && a.fmt ? finish_format<kType>(v, n, a.quant, hist) : finish<kType>(v);
+    return !kPlain && a.fmt ? finish_format<kType, kLanes>(v, n, a.quant, hist) : finish<kType>(v);
 }
 
 constexpr int kLoopThreads = 512;
@@ -174,7 +174,7 @@ inline int prepare_call(const qfmt_norm_t* norm, const qfmt_dropout_t* drop, con
         if (s.dtype == QFMT_F16 && (fmt->e != 5 || fmt->m != 10)) return QFMT_ERR_BAD_FORMAT;
         if (s.dtype == QFMT_BF16 && (fmt->e != 8 || fmt->m != 7)) return QFMT_ERR_BAD_FORMAT;
         c->quant = make_params(*fmt);
-        if (d_stats != nullptr) c->hist_bytes = (size_t)(c->quant.top + kExtraBins) * 32 * sizeof(uint32_t);
+        if (d_stats != nullptr) c->hist_bytes = (size_t)(c->quant.top + kExtraBins) * kHistLanes * sizeof(uint32_t);
     } else if (d_stats != nullptr) {
         return QFMT_ERR_BAD_ARG;  // bins are those of a format
     }

@@ -70,7 +70,7 @@ struct GradientRow {
 };
 
 // What a granule's gradients become: dh (with what arrives by another path) to dresidual, D of it to dx.
-template <int kType, bool kFused, bool kPlain>
+template <int kType, bool kFused, bool kPlain, int kLanes = kHistLanes>
 __device__ __forceinline__ void store_gradients(const BackwardArgs<kType>& a, const GradientRow<kType>& to, int i, int64_t at, const Granule& dy,
                                                 const Granule& xhat, const Granule& w, float rstd, float c1, float c2, uint32_t row,
                                                 uint32_t g, int n, bool from, bool after, uint64_t offset,
@@ -90,7 +90,8 @@ __device__ __forceinline__ void store_gradients(const BackwardArgs<kType>& a, co
         if (a.dresidual.p != nullptr) put<kType, kPlain>(to.dresidual + i * a.dresidual.ld + at, n, a.dresidual, finish<kType>(d), from, after);
         if (a.drop.active && a.dx.p != nullptr) drop_granule(a.drop, offset, row, g, d);
     }
-    if (a.dx.p != nullptr) put<kType, kPlain>(to.dx + i * a.dx.ld + at, n, a.dx, finish_output<kType, kPlain>(a, d, n, hist), from, after);
+    if (a.dx.p != nullptr)
+        put<kType, kPlain>(to.dx + i * a.dx.ld + at, n, a.dx, finish_output<kType, kPlain, kLanes>(a, d, n, hist), from, after);
 }
 
 // Long rows: a block takes a row at a time and reads it twice.
@@ -220,6 +221,12 @@ __device__ __forceinline__ void put_columns(int i, float4 s, int padded, int col
         if (c + j < cols) out[c + j] = v[j];
 }
 
+// Counters of a bin.  The sums of the widest containers and a place for one row leave 24 KB for the histogram, whose 262 bins
+// of 32 would take 33: a call with statistics would have to add up in the order of another kernel.
+__host__ __device__ constexpr int backward_hist_lanes(int type, int v) { return type == QFMT_F32 && v == 4 ? kHistLanes / 2 : kHistLanes; }
+static_assert((255 + kExtraBins) * backward_hist_lanes(QFMT_F32, 4) * 4 + 4 * kMaxTeam * 64 + 4 * kMaxTeam * kGranule * 4 + 16 <= kMostShared,
+              "histogram, column sums and one place of the widest rows");
+
 // The backward pass of rows that a team holds in registers, R at a time: dy and h are read once, the sums over rows
 // stay in the registers of the thread that owns their columns from row to row, and a block leaves one part.
 // kParts: a team is a part of a warp (or all of it), otherwise whole warps; a block has 512 threads' worth of teams.
@@ -235,6 +242,7 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
                           int slots) {
     constexpr bool kStaged = !kPlain && kType == QFMT_F32;
     constexpr bool kAhead = (kPlain && V <= 2) || (!kPlain && !kStaged && V == 1);
+    constexpr int kLanes = backward_hist_lanes(kType, V);
     extern __shared__ __align__(16) uint32_t dynamic[];  // [hist_words] histogram, [sum_words] the block's column sums, places for rows
     __shared__ __align__(16) float scratch[kParts ? 1 : kMaxTeam / 64][2][64];
     grid_launch_dependents();
@@ -244,7 +252,7 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
         for (int i = threadIdx.x; i < kMaxTeam * 2; i += blockDim.x) (&scratch[0][0][0])[i] = 0.0f;
         __syncthreads();
     }
-    if (hist != nullptr) clear_hist(hist, a.quant);
+    if (hist != nullptr) clear_hist<kLanes>(hist, a.quant);
     // (the shuffle tells the compiler that a warp belongs to one team)
     const int mine = V > 2 ? 0 : kParts ? threadIdx.x / team : __shfl_sync(0xFFFFFFFFu, threadIdx.x / team, 0);
     const int t = threadIdx.x - mine * team, teams = V > 2 ? 1 : blockDim.x / team;
@@ -378,8 +386,8 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 if (V > 3) w[0] = load_columns(a.weight, k * team + t, n[k], 1.0f);
-                store_gradients<kType, kFused, kPlain>(a, to, i, k * next, dy[i][k], xhat[i][k], w[V <= 3 ? k : 0], this_rstd[i], c1, c2, row + i,
-                                                       k * team + t, row + i < rows ? n[k] : 0, from, after, offset, hist);
+                store_gradients<kType, kFused, kPlain, kLanes>(a, to, i, k * next, dy[i][k], xhat[i][k], w[V <= 3 ? k : 0], this_rstd[i], c1, c2,
+                                                               row + i, k * team + t, row + i < rows ? n[k] : 0, from, after, offset, hist);
             }
         }
         advance(second, to.dh, a.dh.ld, step.dh);
@@ -389,7 +397,7 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
         first += by;
         second = pairs && !second;
     }
-    if (hist != nullptr) flush_hist(hist, a.quant, a.stats, (uint64_t)a.rows * (uint64_t)a.cols);
+    if (hist != nullptr) flush_hist<kLanes>(hist, a.quant, a.stats, (uint64_t)a.rows * (uint64_t)a.cols);
     const bool alone = a.dweight != nullptr || a.dbias != nullptr;  // this block's part is the result
     if (kStaged) stage_wait();
     if (a.partial == nullptr) return;
@@ -516,8 +524,8 @@ int launch_backward_rows(const Call& c, BackwardArgs<kType> a, int team, int gro
     if (alone) a.dweight = d_dweight, a.dbias = d_dbias;
     const auto kern = norm_backward_rows_kernel<kType, V, R, kParts, kFused, kPlain>;
     constexpr bool kStaged = !kPlain && kType == QFMT_F32;
-    const size_t place = (size_t)teams * staged_row_bytes(a.cols);
-    const size_t sums = backward_sum_bytes(V, kParts, team, a.cols), rest = c.hist_bytes + sums;
+    const size_t place = (size_t)teams * staged_row_bytes(a.cols), hist = c.hist_bytes / kHistLanes * backward_hist_lanes(kType, V);
+    const size_t sums = backward_sum_bytes(V, kParts, team, a.cols), rest = hist + sums;
     const int slots = !kStaged ? 0 : rest + 2 * place <= kMostShared ? 2 : 1;
     // More than half of what an SM has: its one block must not be joined by a second of the same launch, which would
     // leave another SM without work (launches overlap, so SMs come free at different times).
@@ -527,7 +535,7 @@ int launch_backward_rows(const Call& c, BackwardArgs<kType> a, int team, int gro
     if (rc != QFMT_OK) return rc;
     const int64_t stride = (int64_t)blocks * teams * group;
     const BackwardSteps step = {stride * a.dy.ld, stride * a.h.ld, stride * a.dh.ld, stride * a.dx.ld, stride * a.dresidual.ld};
-    QFMT_CUDA_TRY(launch_overlapping(kern, blocks, block, smem, stream, a, team, group, step, (int)(c.hist_bytes / 4), (int)(sums / 4), slots));
+    QFMT_CUDA_TRY(launch_overlapping(kern, blocks, block, smem, stream, a, team, group, step, (int)(hist / 4), (int)(sums / 4), slots));
     return a.partial != nullptr && !alone ? join_parts(a.partial, (int)blocks, a.cols, d_dweight, d_dbias, stream) : QFMT_OK;
 }
 
@@ -536,10 +544,7 @@ int launch_backward(const Call& c, const BackwardArgs<kType>& a, float* d_dweigh
     if (a.rows == 0) return join_parts(a.partial, 0, a.cols, d_dweight, d_dbias, stream);  // zeros
     const Plan plan = backward_plan(c.norm, kFused);
     const bool plain = plain_layout(a.cols, {a.dy.whole, a.dh.whole, a.h.whole, a.dx.whole, a.dresidual.whole}) && !a.fmt;
-    // (the widest rows with a histogram of 256 bins leave no place for a row)
-    const bool fits = plain || plan.granules < 3 || kType != QFMT_F32 ||
-                      c.hist_bytes + backward_sum_bytes(plan.granules, false, plan.team, a.cols) + staged_row_bytes(a.cols) <= kMostShared;
-    if (plan.team != 0 && fits) {
+    if (plan.team != 0) {
         // Two neighbouring rows to a team where every team gets some: a rule on sizes alone, since it decides the order
         // of the sums over rows.  Whether the two are worked on at once does not.
         // So is a single block where that takes one turn of pairs, or two of narrow rows: its part is the result, and no

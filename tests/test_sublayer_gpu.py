@@ -396,6 +396,27 @@ def test_rounded_gradients_of_wide_rows(rows, cols, kind, e, m):
     assert abs(int(st[qf.ST_DENORMAL]) - int(stats.cpu()[qf.ST_DENORMAL])) <= 2 + rows * cols // 1000
 
 
+@pytest.mark.parametrize("kind,e,m", FORMATS)
+@pytest.mark.parametrize("rows,cols", [(37, 1000), (5, 12289), (7, 13001), (300, 16384), (2, 20001)])
+def test_gradients_do_not_depend_on_whether_statistics_are_wanted(rows, cols, kind, e, m):
+    gen = torch.Generator().manual_seed(rows + cols)
+    h, dy = values(gen, rows, cols, kind), values(gen, rows, cols, kind)
+    mean, rstd = saved(h)
+    w, _ = vectors(gen, cols)
+    stats = torch.full((qf.STATS_WORDS,), 5, dtype=torch.int64, device=DEV)
+    fmt = qf.make_format(e, m, 0)
+    plain = run_norm_backward(h, dy, mean, rstd, w, kind)
+    full = run_fused_backward(h, dy, None, mean, rstd, w, 0.1, 1, 2, kind)
+    for off, pad in ((0, 0), (3, 1)):
+        got = [run_norm_backward(h, dy, mean, rstd, w, kind, off, pad, fmt=fmt, stats=s) for s in (None, stats)]
+        for u, v, p in zip(*got, (None, *plain[1:])):
+            assert torch.equal(u, v) and (p is None or torch.equal(u, p))
+        got = [run_fused_backward(h, dy, None, mean, rstd, w, 0.1, 1, 2, kind, off, pad, fmt=fmt, stats=s) for s in (None, stats)]
+        for u, v, p in zip(*got, (None, *full[1:])):
+            assert torch.equal(u, v) and (p is None or torch.equal(u, p))
+        assert int(stats[qf.ST_TOTAL]) == rows * cols
+
+
 def test_norm_backward_against_differences():
     """The gradients against central differences of the 64-bit forward pass along random directions.  With step s the
     difference is off by O(s^2) = 1e-8 of the gradient's scale, single precision by less than 1e-5 of it."""
