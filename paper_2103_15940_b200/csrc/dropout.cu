@@ -25,6 +25,7 @@ struct DropArgs {
     Target<kType> out;
     int64_t cols;
     uint32_t rows, granules;  // per row
+    uint32_t inner;           // inner_rows()
     uint32_t turns;           // granules that a thread takes one after the other ...
     uint32_t step;            // ... this many rows apart, or in rows longer than the grid this many granules
     int64_t step_x, step_residual, step_out;  // the same step in elements
@@ -59,8 +60,8 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropArgs<kT
                 const int64_t left = a.cols - (int64_t)at_g * kGranule;
                 n[i] = !mine || at_row >= a.rows || left <= 0 ? 0 : kPlain || left > kGranule ? kGranule : (int)left;
                 const bool edge = at_edge(a.cols, at_g);
-                x[i] = start<kType, kPlain>(px + i * a.step_x, n[i], at_row, a.rows, edge);
-                if (kResidual) r[i] = start<kType, kPlain>(pr + i * a.step_residual, n[i], at_row, a.rows, edge);
+                x[i] = start<kType, kPlain>(px + i * a.step_x, n[i], at_row, a.rows, edge, a.inner);
+                if (kResidual) r[i] = start<kType, kPlain>(pr + i * a.step_residual, n[i], at_row, a.rows, edge, a.inner);
             }
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
@@ -91,6 +92,7 @@ int launch_dropout(const void* d_x, int64_t ld_x, const void* d_residual, int64_
     a.out = make_target<kType>(d_out, ld_out);
     a.cols = cols;
     a.rows = (uint32_t)rows;
+    a.inner = inner_rows(cols, rows);
     a.granules = (uint32_t)((cols + kGranule - 1) / kGranule);
     a.drop = drop;
     const bool plain = cols % kGranule == 0 && a.x.whole && a.residual.whole && a.out.whole;

@@ -202,12 +202,16 @@ struct Pieces {
     bool inside;  // they lie in the matrix
 };
 
-// Whether the pieces of granule g can reach beyond the matrix in its first or last row.
-__device__ __forceinline__ bool at_edge(int64_t cols, int64_t g) { return g == 0 || (g + 2) * kGranule > cols + 1; }
+// The pieces of a granule hold up to 7 elements on either side of it, so they can reach beyond the matrix where it lies at an
+// edge of its row (at_edge) in the first or last row, or, where rows may lie closer together than that, in any row.  Rows 1 ..
+// inner_rows() are those whose pieces cannot.
+__host__ __device__ __forceinline__ bool at_edge(int64_t cols, int64_t g) { return g == 0 || (g + 2) * kGranule > cols + 1; }
+__host__ __device__ __forceinline__ uint32_t inner_rows(int64_t cols, int64_t rows) { return cols < kGranule || rows < 3 ? 0u : (uint32_t)rows - 2u; }
+__host__ __device__ __forceinline__ bool pieces_inside(bool edge, uint32_t row, uint32_t inner) { return !edge || row - 1u < inner; }
 
 // Starts to load `n` columns (0..8) of a granule at p: loads under a predicate, nothing waits and nothing branches.
 // What the pieces hold beyond the columns is thrown away later; where they could reach beyond the matrix (`inside`
-// false: at the edges of its first and last row) the granule is left to arrive().
+// false) the granule is left to arrive().
 template <int kType>
 __device__ __forceinline__ Pieces<kType> start_any(const typename Word<kType>::type* p, int n, bool inside) {
     constexpr int kPer = kType == QFMT_F32 ? 4 : 8;
@@ -348,13 +352,14 @@ __device__ __forceinline__ Raw<kType> finish_format(const Granule& v, int n, con
 }
 
 // A granule of n columns at p, in row `row` of `rows`, on its way, and its words: zeros where there is nothing.
-// kPlain: whole and aligned, or not there at all.  edge: at_edge() of the granule.
+// kPlain: whole and aligned, or not there at all.  edge: at_edge() of the granule, inner: inner_rows().
 template <int kType, bool kPlain>
 using OnItsWay = std::conditional_t<kPlain, Raw<kType>, Pieces<kType>>;
 template <int kType, bool kPlain>
-__device__ __forceinline__ OnItsWay<kType, kPlain> start(const typename Word<kType>::type* p, int n, uint32_t row, uint32_t rows, bool edge) {
+__device__ __forceinline__ OnItsWay<kType, kPlain> start(const typename Word<kType>::type* p, int n, uint32_t row, uint32_t rows, bool edge,
+                                                           uint32_t inner) {
     if constexpr (kPlain) return load_raw<kType>(p, n, row, rows);
-    else return start_any<kType>(p, row < rows ? n : 0, !(edge && (row == 0 || row + 1 >= rows)));
+    else return start_any<kType>(p, row < rows ? n : 0, pieces_inside(edge, row, inner));
 }
 template <int kType, bool kPlain>
 __device__ __forceinline__ Raw<kType> words(const OnItsWay<kType, kPlain>& q, const typename Word<kType>::type* p, int n) {

@@ -30,6 +30,7 @@ struct BackwardArgs {
     float* dweight;  // where a single part goes at once; both NULL with several parts
     float* dbias;
     int64_t rows, cols;
+    uint32_t inner;  // inner_rows()
     float inverse;
     bool fmt;
     DropParams drop;
@@ -83,7 +84,7 @@ __device__ __forceinline__ void store_gradients(const BackwardArgs<kType>& a, co
         if (a.dh.p != nullptr) {
             const auto* p = to.dh + i * a.dh.ld + at;
             const Granule more = widen_raw<kType>(kPlain ? load_raw<kType>(p, n, 0, 1)
-                                                         : load_any<kType>(p, n, !(at_edge(a.cols, g) && (row == 0 || row + 1 >= (uint32_t)a.rows))));
+                                                         : load_any<kType>(p, n, pieces_inside(at_edge(a.cols, g), row, a.inner)));
 #pragma unroll
             for (int j = 0; j < 4; ++j) d.p[j] = add2(d.p[j], more.p[j]);
         }
@@ -107,7 +108,7 @@ __global__ void __launch_bounds__(kLoopThreads) norm_backward_loop_kernel(const 
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const float mean = a.mean[row], rstd = a.rstd[row];
         const auto load = [&](uint32_t g, int n, Granule& dy, Granule& xhat, Granule& w) {
-            const bool inside = (row != 0 && row + 1 != a.rows) || !at_edge(a.cols, g);
+            const bool inside = pieces_inside(at_edge(a.cols, g), (uint32_t)row, a.inner);
             dy = widen_raw<kType>(load_any<kType>(a.dy.p + row * a.dy.ld + (int64_t)g * kGranule, n, inside));
             xhat = normalise<false>(widen_raw<kType>(load_any<kType>(a.h.p + row * a.h.ld + (int64_t)g * kGranule, n, inside)), mean, rstd, n);
             w = load_columns(a.weight, g, n, 1.0f);
@@ -142,7 +143,7 @@ __global__ void __launch_bounds__(32 * kColumnWarps) norm_column_sums_kernel(con
     Granule dw = splat(0.0f), db = splat(0.0f);
     if (n > 0) {
         for (int64_t row = (int64_t)blockIdx.y * kColumnWarps + warp; row < a.rows; row += (int64_t)gridDim.y * kColumnWarps) {
-            const bool inside = (row != 0 && row + 1 != a.rows) || !at_edge(a.cols, g);
+            const bool inside = pieces_inside(at_edge(a.cols, g), (uint32_t)row, a.inner);
             const Granule dy = widen_raw<kType>(load_any<kType>(a.dy.p + row * a.dy.ld + (int64_t)g * kGranule, n, inside));
             const Granule xhat = normalise<false>(widen_raw<kType>(load_any<kType>(a.h.p + row * a.h.ld + (int64_t)g * kGranule, n, inside)), a.mean[row], a.rstd[row], n);
 #pragma unroll
@@ -287,8 +288,8 @@ norm_backward_rows_kernel(const BackwardArgs<kType> a, int team, int group, cons
 #pragma unroll
                 for (int k = 0; k < V; ++k) {
                     const bool edge = at_edge(a.cols, k * team + t);
-                    raw_dy[i][k] = start<kType, kPlain>(pdy + i * a.dy.ld + k * next, n[k], at + i, rows, edge);
-                    raw_h[i][k] = start<kType, kPlain>(ph + i * a.h.ld + k * next, n[k], at + i, rows, edge);
+                    raw_dy[i][k] = start<kType, kPlain>(pdy + i * a.dy.ld + k * next, n[k], at + i, rows, edge, a.inner);
+                    raw_h[i][k] = start<kType, kPlain>(ph + i * a.h.ld + k * next, n[k], at + i, rows, edge, a.inner);
                 }
             }
         }
@@ -606,6 +607,7 @@ int backward(const Call& c, const void* d_dy, const void* d_dh, const void* d_h,
     a.dweight = a.dbias = nullptr;
     a.rows = s.rows;
     a.cols = s.cols;
+    a.inner = inner_rows(s.cols, s.rows);
     a.inverse = 1.0f / (float)a.cols;
     a.fmt = c.fmt;
     a.drop = c.drop;

@@ -28,6 +28,7 @@ struct ForwardArgs {
     float* mean;
     float* rstd;
     int64_t rows, cols;
+    uint32_t inner;  // inner_rows()
     float eps;
     float inverse;  // 1 / cols
     bool fmt;       // quant holds a format to round to
@@ -92,7 +93,7 @@ __global__ void __launch_bounds__(kLoopThreads) norm_forward_loop_kernel(const F
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const auto h = [&](uint32_t g, int n) {
             const int64_t col = (int64_t)g * kGranule;
-            const bool inside = (row != 0 && row + 1 != a.rows) || !at_edge(a.cols, g);
+            const bool inside = pieces_inside(at_edge(a.cols, g), (uint32_t)row, a.inner);
             const Raw<kType> res = kFused && a.residual.p != nullptr
                                        ? load_any<kType>(a.residual.p + row * a.residual.ld + col, n, inside) : Raw<kType>();
             return join_h<kType, kFused>(a, load_any<kType>(a.x.p + row * a.x.ld + col, n, inside), res, offset, (uint32_t)row, g);
@@ -224,9 +225,9 @@ norm_forward_rows_kernel(const ForwardArgs<kType> a, int team, const ForwardStep
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 const bool edge = at_edge(a.cols, k * team + t);
-                x[i][k] = start<kType, kPlain || kStaged>(px + i * a.x.ld + k * next, n[k], at + i, rows, edge);
+                x[i][k] = start<kType, kPlain || kStaged>(px + i * a.x.ld + k * next, n[k], at + i, rows, edge, a.inner);
                 if (kFused)
-                    r[i][k] = start<kType, kPlain || kStaged>(pr + i * a.residual.ld + k * next, residual ? n[k] : 0, at + i, rows, edge);
+                    r[i][k] = start<kType, kPlain || kStaged>(pr + i * a.residual.ld + k * next, residual ? n[k] : 0, at + i, rows, edge, a.inner);
             }
         }
         if (kAhead) px += step.x, pr += step.residual;
@@ -405,6 +406,7 @@ int forward(const Call& c, const void* d_x, const void* d_residual, const float*
     a.rstd = d_rstd;
     a.rows = s.rows;
     a.cols = s.cols;
+    a.inner = inner_rows(s.cols, s.rows);
     a.eps = s.eps;
     a.inverse = 1.0f / (float)a.cols;
     a.fmt = c.fmt;

@@ -42,3 +42,35 @@ def test_joined_columns(joined):
     for cols, i, second, c in joined:
         padded = -(-cols // 8) * 8
         assert (second, c) == divmod(i, padded), (cols, i)
+
+
+def test_pieces_of_ragged_rows_stay_inside_the_matrix(tmp_path):
+    """Every aligned 16-byte piece that a granule is loaded in, for small matrices of every alignment and spacing of rows; inner
+    rows of eight columns and more are always loaded in pieces."""
+    out = run(tmp_path, r"""
+#include "elements.cuh"
+int main() {
+    long pieces = 0, outside = 0, by_element = 0;
+    for (int per : {4, 8})  // elements of a piece: containers, codes
+        for (int off = 0; off < per; ++off)
+            for (int rows = 1; rows <= 9; ++rows)
+                for (int cols = 1; cols <= 41; ++cols)
+                    for (int ld = cols; ld <= cols + 9; ++ld)
+                        for (int row = 0; row < rows; ++row)
+                            for (int g = 0; g * 8 < cols; ++g) {
+                                const int n = cols - 8 * g < 8 ? cols - 8 * g : 8, at = off + row * ld + 8 * g, first = at % per;
+                                if (!qfmt::pieces_inside(qfmt::at_edge(cols, g), row, qfmt::inner_rows(cols, rows))) {
+                                    by_element += cols >= 8 && row != 0 && row + 1 != rows;
+                                    continue;
+                                }
+                                for (int i = 0; first + n > i * per; ++i) {
+                                    const int begin = at - first + i * per;
+                                    ++pieces;
+                                    outside += begin < off || begin + per > off + (rows - 1) * ld + cols;
+                                }
+                            }
+    std::printf("%ld %ld %ld\n", pieces, outside, by_element);
+}
+""")
+    pieces, outside, by_element = (int(v) for v in out[0].split())
+    assert pieces > 100000 and outside == 0 and by_element == 0
