@@ -622,6 +622,63 @@ def test_rounded_gradients_of_several_teams_with_two_granules(rows, cols, kind, 
     test_rounded_gradients_of_wide_rows(rows, cols, kind, e, m)
 
 
+# ---- tensors of one call that lie differently -----------------------------------------------------------------------------
+
+
+MIXED = [((0, 0), (1, 1), (2, 3), (0, 0), (3, 0)), ((1, 2), (0, 0), (0, 0), (2, 1), (0, 0)), ((3, 1), (2, 1), (1, 0), (0, 8), (5, 2)),
+         ((0, 8), (0, 0), (1, 0), (1, 0), (0, 16)), ((2, 5), (2, 3), (6, 1), (7, 0), (4, 4))]
+
+
+def whole_rows(t):
+    """Every tensor aligned: rows padded to whole granules."""
+    return 0, -t.shape[1] % 8
+
+
+@pytest.mark.parametrize("kind", ref.KINDS)
+@pytest.mark.parametrize("rows,cols", [(3, 5), (70, 64), (41, 203), (50, 260), (300, 511), (33, 1024), (29, 1913), (2400, 1283), (9, 4093), (7, 8200),
+                                       (5, 13001), (3, 20001)])
+def test_every_tensor_has_its_own_alignment(rows, cols, kind):
+    """Offsets and leading dimensions that differ from tensor to tensor of a call (aligned sources with ragged targets, two
+    skews in one staged row) give the bits of the aligned layout."""
+    gen = torch.Generator().manual_seed(rows * 11 + cols)
+    dt, p, seed, offset = ref.KINDS[kind], 0.2, 17, 1 << 33
+    x, r, dy, dh = (values(gen, rows, cols, kind) for _ in range(4))
+    w, b = (t.to(DEV) for t in vectors(gen, cols))
+    drop = qf.make_dropout(p, seed, offset)
+    mean, rstd = (t.to(DEV) for t in saved(x))
+
+    def passes(layout):
+        """All outputs of every pass; layout: offset and padding of five tensors, inputs first."""
+        put = lambda i, data=None: Buffer(rows, cols, kind, *layout[i], data)
+        out = []
+        bx, br, bo = put(0, x), put(1, r), put(3)
+        qf.qfmt_dropout(bx.ptr, bx.ld, br.ptr, br.ld, bo.ptr, bo.ld, rows, cols, dt, drop)
+        out += [bo.get(), bx.get(), br.get()]
+        by, m, s = put(3), *torch.empty(2, rows, device=DEV).unbind(0)
+        qf.qfmt_layer_norm(qf.make_norm(rows, cols, dt, EPS, ld_x=bx.ld, ld_y=by.ld), bx.ptr, w, b, by.ptr, m, s)
+        out += [by.get(), m.cpu(), s.cpu()]
+        bh, by = put(2), put(4)
+        norm = qf.make_norm(rows, cols, dt, EPS, ld_x=bx.ld, ld_residual=br.ld, ld_h=bh.ld, ld_y=by.ld)
+        qf.qfmt_dropout_add_layer_norm(norm, drop, bx.ptr, br.ptr, w, b, bh.ptr, by.ptr, m, s)
+        out += [bh.get(), by.get(), m.cpu(), s.cpu()]
+        bdy, bh, bdx = put(1, dy), put(0, x), put(3)
+        norm = qf.make_norm(rows, cols, dt, EPS, ld_x=bh.ld, ld_dy=bdy.ld, ld_dx=bdx.ld)
+        ws = torch.full((qf.qfmt_layer_norm_workspace_bytes(norm),), 0xFF, dtype=torch.uint8, device=DEV)
+        dw, db = torch.empty(2, cols, device=DEV).unbind(0)
+        qf.qfmt_layer_norm_backward(norm, bdy.ptr, bh.ptr, mean, rstd, w, bdx.ptr, dw, db, ws, ws.numel())
+        out += [bdx.get(), dw.cpu(), db.cpu()]
+        bdh, bdx, bdr = put(2, dh), put(3), put(4)
+        norm = qf.make_norm(rows, cols, dt, EPS, ld_h=bh.ld, ld_dy=bdy.ld, ld_dh=bdh.ld, ld_dx=bdx.ld, ld_dresidual=bdr.ld)
+        qf.qfmt_dropout_add_layer_norm_backward(norm, drop, bdy.ptr, bdh.ptr, bh.ptr, mean, rstd, w, bdx.ptr, bdr.ptr, dw, db, ws, ws.numel())
+        return out + [bdx.get(), bdr.get(), dw.cpu(), db.cpu()]
+
+    want = passes([whole_rows(x)] * 5)
+    same_bits(want[0], expect_dropout(x, r, p, seed, offset, kind))
+    for layout in MIXED:
+        for u, v in zip(want, passes(layout)):
+            assert torch.equal(u, v), layout
+
+
 # ---- how calls sit in a program ---------------------------------------------------------------------------------------
 
 
