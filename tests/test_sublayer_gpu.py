@@ -622,6 +622,45 @@ def test_rounded_gradients_of_several_teams_with_two_granules(rows, cols, kind, 
     test_rounded_gradients_of_wide_rows(rows, cols, kind, e, m)
 
 
+# ---- how large errors are on the whole --------------------------------------------------------------------------------
+
+
+def rms(t):
+    return float(t.double().square().mean().sqrt())
+
+
+@pytest.mark.parametrize("rows,cols", [(4000, 64), (900, 203), (500, 768), (600, 1021), (300, 1024), (2400, 1283), (120, 4096), (70, 4093),
+                                       (60, 8200), (40, 16384), (9, 70001)])
+def test_errors_of_single_precision_are_those_of_a_few_roundings(rows, cols):
+    """Root mean squares over whole tensors of ordinary rows, which the worst-case bounds above leave six bits for.
+
+    One rounding is at most U of its result, U / sqrt(3) in the mean square, and they add up in squares.  y: three at full size (the
+    difference, the two products) are U together, the inverse root's error is at most 2^-22.9 = 2.2 U, sums over a row that
+    end near zero or are halved add less than U: below 4 U of |xhat w| + |b|.  dx: g, two products, the factor rstd: below 4 U of its three terms.
+    Column sums: a chain of k roundings of a growing sum is U sqrt(k) / 2.4 of its final size; at most 8 rows a granule's owner ahead of
+    5 parts of a warp's and 32 warps' (k < 64, 3.3 U), and the products: below 8 U of the terms' root sum of squares."""
+    gen = torch.Generator().manual_seed(rows + 3 * cols)
+    x, r, dy = (torch.randn(rows, cols, generator=gen) for _ in range(3))
+    w, b = vectors(gen, cols)
+    h = h32(x, r, 0.1, 3, 4)
+    for got, t in ((run_norm(x, w, b, "f32"), x), (run_fused(x, r, w, b, 0.1, 3, 4, "f32"), h)):
+        y, mean, rstd = ref.forward(t.double(), w.double(), b.double(), EPS)[:3]
+        size = (t.double() - mean[:, None]) * rstd[:, None] * w.double()
+        assert rms(got[0].double() - y) <= 4 * ref.U * rms(size.abs() + b.double().abs())
+        assert rms(got[1].double() - mean) <= 4 * ref.U * rms(t) and rms(got[2].double() / rstd - 1) <= 4 * ref.U
+    mean, rstd = saved(h)
+    dh, dw, db = ref.backward(h.double(), dy.double(), mean.double(), rstd.double(), w.double())[:3]
+    xhat, g = (h.double() - mean.double()[:, None]) * rstd.double()[:, None], dy.double() * w.double()
+    size = rstd.double()[:, None] * (g.abs() + g.mean(1, keepdim=True).abs() + (xhat * (g * xhat).mean(1, keepdim=True)).abs())
+    keep = ref.keep_mask(rows, cols, 0.1, 3, 4).double() * 65536 / (65536 - ref.threshold(0.1))
+    one, two = run_norm_backward(h, dy, mean, rstd, w, "f32"), run_fused_backward(h, dy, None, mean, rstd, w, 0.1, 3, 4, "f32")
+    for got, want in ((one[0], dh), (two[1], dh), (two[0], dh * keep)):
+        assert rms(got.double() - want) <= 4 * ref.U * rms(size * (keep if want is not dh else 1.0))
+    for dwk, dbk in ((one[1], one[2]), (two[2], two[3])):
+        assert rms(dwk.double() - dw) <= 8 * ref.U * rms((dy.double() * xhat).square().sum(0).sqrt())
+        assert rms(dbk.double() - db) <= 8 * ref.U * rms(dy.double().square().sum(0).sqrt())
+
+
 # ---- tensors of one call that lie differently -----------------------------------------------------------------------------
 
 
