@@ -457,11 +457,13 @@ norm_join_parts_kernel(const float4* partial, int parts, int64_t padded, int64_t
     grid_launch_dependents();
     grid_dependency_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t quads = padded / 2, q = (int64_t)blockIdx.x * 32 + lane;
+    const uint32_t quads = (uint32_t)(padded / 2), q = blockIdx.x * 32 + lane;  // at most 2^30
     float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     if (q < quads) {
+        const float4* p = partial + (int64_t)warp * quads + q;
+        const int64_t step = (int64_t)kJoinWarps * quads;
 #pragma unroll 5
-        for (int k = warp; k < parts; k += kJoinWarps) s = sum_of(s, partial[k * quads + q]);
+        for (int k = warp; k < parts; k += kJoinWarps, p += step) s = sum_of(s, *p);
     }
     sums[warp][lane] = s;
     __syncthreads();
