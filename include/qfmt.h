@@ -498,7 +498,11 @@ typedef struct {
 int qfmt_dropout(const void* d_x, int64_t ld_x, const void* d_residual, int64_t ld_residual, void* d_out, int64_t ld_out,
                  int64_t rows, int64_t cols, int32_t dtype, const qfmt_dropout_t* drop, void* stream);
 
-/* Geometry of a normalisation; ld_t is the leading dimension of the tensor d_t below, 0 for cols. */
+/*
+ * Geometry of a normalisation; ld_t is the leading dimension of the tensor d_t below, 0 for cols.  One record serves
+ * the forward and the backward pass; every leading dimension is checked (0 or at least cols) in every call, whether or not it
+ * takes that tensor.
+ */
 typedef struct {
     int64_t rows, cols;
     int64_t ld_x, ld_residual, ld_h, ld_y;
@@ -517,7 +521,7 @@ typedef struct {
  *            qfmt_quantize_stats (containers) or the codes of qfmt_quantize_stats_pack16 on the 32-bit results.
  *            loss_scale must be 1, and QFMT_F16 / QFMT_BF16 take {5, 10} / {8, 7} only (QFMT_ERR_BAD_FORMAT)
  *   d_stats  device, 8-byte aligned, or NULL: statistics of that rounding (fmt is then required);
- *            accumulate as in qfmt_quantize_stats
+ *            accumulate as in qfmt_quantize_stats.  No other output depends on whether they are wanted
  * d_y may equal d_x when their leading dimensions agree; other overlap is an error the library cannot detect.
  * The backward pass, from dy = dL/dy, with xhat = (x - mean) rstd and g = weight dy:
  *     dx = rstd (g - sum g / n - xhat sum (g xhat) / n),  dweight = sum over rows of dy xhat,  dbias = ... of dy.

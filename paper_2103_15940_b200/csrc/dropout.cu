@@ -7,7 +7,8 @@
 // came as constants, 28 us against 24 on 8192 x 4096 bfloat16).  Sixteen bits an element, not 32, because two blocks a
 // granule would make the integer pipe the bound; so p is held in steps of 2^-16 and the scale belongs to the step taken.
 // Measured: 8192 x 4096 bfloat16 24.0 us (5.6 TB/s, 0.87 of the measured copy rate), 16384 x 4096 fp32 92 us (5.8 TB/s),
-// 16 Mi elements in one row of bfloat16 11.4 us, 4099 x 1021 fp32 with a residual into dense rows 10.7 us (4.7 TB/s).
+// 16 Mi elements in one row of bfloat16 13.5 us, 4099 x 1021 fp32 with a residual into dense rows 10.7 us (4.7 TB/s); all on sets
+// of tensors larger than L2 in turn.
 #include <cuda_runtime.h>
 #include <stdint.h>
 

@@ -2,15 +2,16 @@
 //
 // Bound by memory: dy and h are read once, each gradient is written once.  The sums over rows for the weight and the
 // bias run along with the rows, in the registers of the thread that owns the columns, so nothing is read again for
-// them; each SM's one block of 512 threads leaves one part of 2 n sums and a second kernel joins the 148 parts, in an
-// order that depends on sizes alone.  Measured choices:
+// them; each SM's one block of 512 threads leaves one part of 2 n sums and a second kernel joins them (up to 148; the one part
+// of a few rows is the result), in an order that depends on sizes alone.  Measured choices:
 //   * up to 1280 columns one granule a thread and two rows at a time: 35.5 us for dx and the sums of 16384 x 1024 fp32; wider
 //     rows by the rule at backward_plan;
 //   * teams of one block, joined through its shared memory: small blocks in clusters that add up their sums through
 //     distributed shared memory took 4 to 5 us more at the end of every call;
 //   * with one granule a thread the sums are registers; with more, the registers hold the row and the sums lie in shared memory.
-// Measured: fused 8192 x 1024 fp32 26.5 us (5.1 TB/s, 0.78 of the measured copy rate), fused 8192 x 4096 bfloat16 52.7 us
-// (5.1 TB/s), fused 16384 x 4096 fp32 186 us (5.8 TB/s), 4096 x 768 binary16 7.6 us, of which joining takes 3.
+// Measured (replayed from a graph, on sets of tensors larger than L2 in turn, as all figures here that do not say otherwise):
+// fused 8192 x 1024 fp32 26.6 us (5.0 TB/s, 0.78 of the measured copy rate), fused 8192 x 4096 bfloat16 53.0 us (5.1 TB/s), fused
+// 16384 x 4096 fp32 187 us (5.8 TB/s), 4096 x 768 binary16 9.1 us (7.8 with three sets, partly in L2), of which joining takes 3.
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -233,8 +234,8 @@ static_assert((255 + kExtraBins) * backward_hist_lanes(QFMT_F32, 4) * 4 + 4 * kM
 // kParts: a team is a part of a warp (or all of it), otherwise whole warps; a block has 512 threads' worth of teams.
 // V > 1 (wide rows): the column sums lie in shared memory, each thread's its own, since the registers hold V granules of
 // dy and h; V > 2: the team is the block; with V = 4 the weight is read from the cache as well.
-// kPlain and kStaged as in the forward pass (staged bfloat16 rows took 75 us where shifted pieces take 44); with
-// registers to spare (kAhead) the next rows are on their way while these are worked on.  Staged rows have two
+// kPlain and kStaged as in the forward pass (16384 x 1021 bfloat16 takes 43 us in shifted pieces; staged word by word, before rows
+// were staged in pieces, 75); with registers to spare (kAhead) the next rows are on their way while these are worked on.  Staged rows have two
 // places a team, or one for h and dy in turn; the next ones are copied as soon as they have been read.
 // A team takes `group` neighbouring rows (R, or R = 1 at a time), then the group that is a step away.
 template <int kType, int V, int R, bool kParts, bool kFused, bool kPlain>
@@ -479,12 +480,12 @@ norm_join_parts_kernel(const float4* partial, int parts, int64_t padded, int64_t
 // One granule a thread; two and more, teams half as large, beyond 1280 columns where there are enough rows (16 a block of
 // containers, 32 of codes) and it pays: with containers (fused: unless the larger teams fill 512 threads), with codes where the
 // larger teams leave three eighths of 512 without work (2049 to 2560 columns).  dx and the sums / fused, two granules against
-// one, us: fp32 16384 x 1536 50 against 57 / 73 against 75, x 2048 64 against 68 / 97 against 90, x 2560 79 against 110 / 119
-// against 145, ragged x 2556 121 against 194 / 159 against 215, x 3496 110 against 136 / 158 against 177, x 4096 121 against 143
-// / 190 against 186, x 1024 36 against 36 / 49 against 46; 3000 x 2560 17 against 23 / 24 against 33, 2048 x 2560 13.7 against
-// 12.8 / 16.4 against 18.3, 400 x 2560 8.1 against 7.6 / 8.9 against 8.3.  bfloat16 16384 x 2560 54 against 62 / 67 against 76,
-// ragged x 2556 114 against 139 / 202 against 178 (registers spill), 9899 x 2816 41.7 against 40.1 / 52 against 50, 16384 x 4096
-// 79 against 77 / 100 against 99, 2000 x 2560 11.4 against 10.4 / 14.6 against 13.9.
+// one, us: fp32 16384 x 1536 50 against 57 / 72 against 75, x 2048 63 against 68 / 97 against 89, x 2560 78 against 110 / 118
+// against 145, ragged x 2556 121 against 198 / 159 against 202, x 3496 109 against 134 / 157 against 175, x 4096 120 against 143
+// / 190 against 187, 3000 x 2560 20 against 27 / 25 against 33.  bfloat16 16384 x 2560 53 against 62 / 67 against 75, ragged
+// x 2556 113 against 131 / 185 against 161 (registers spill).  Where the rule keeps one, in L2: fp32 16384 x 1024 36 against 36 / 49
+// against 46, 2048 x 2560 13.7 against 12.8 / 16.4 against 18.3, 400 x 2560 8.1 against 7.6 / 8.9 against 8.3; bfloat16 9899 x 2816
+// 41.7 against 40.1 / 52 against 50, 16384 x 4096 79 against 77 / 100 against 99, 2000 x 2560 11.4 against 10.4 / 14.6 against 13.9.
 constexpr int kMaxParts = 148;  // the blocks of the rows kernel, one on each of a B200's SMs
 Plan backward_plan(const qfmt_norm_t& s, bool fused) {
     const Plan one = make_plan(s.cols, 1, 4);
@@ -551,13 +552,14 @@ int launch_backward(const Call& c, const BackwardArgs<kType>& a, float* d_dweigh
         // Two neighbouring rows to a team where every team gets some: a rule on sizes alone, since it decides the order
         // of the sums over rows.  Whether the two are worked on at once does not.
         // So is a single block where that takes one turn of pairs, or two of narrow rows: its part is the result, and no
-        // second kernel runs (16 rows of 1024: 3.9 us against 4.1, and 6.1 against 8.7 when calls are launched one by one; four
-        // turns would take 5.5).
+        // second kernel runs (8 rows of 1024 fp32 3.6 us against 4.1 in a graph; 16 rows 4.7 against 4.2, bfloat16 3.9 against 4.0, but
+        // 6.1 against 8.7 when calls are launched one by one; four turns would take 5.5).
         const int teams = kMaxTeam / plan.team, cap = std::min(c.dev.sm_count, kMaxParts);
         const bool few = plan.granules == 1 && a.partial != nullptr && a.rows <= (plan.team <= 128 ? 4 : 2) * teams;
         const int group = plan.granules == 1 && (few || a.rows > 2 * ((int64_t)teams * cap - 1)) ? 2 : 1;
-        // With one granule as few blocks as take no more turns, so fewer parts are joined (5000 x 256 bfloat16 6.6 -> 5.8 us, 700 x
-        // 2048 6.9 -> 6.5, 400 x 4096 fp32 9.0 -> 8.7, 8192 x 1024 bfloat16 11.0 -> 11.2; wide rows mixed: 331 x 8192 11.4 -> 11.8).
+        // With one granule as few blocks as take no more turns, so fewer parts are joined (in L2: 5000 x 256 bfloat16 6.6 -> 5.8 us,
+        // 700 x 2048 6.9 -> 6.5, 400 x 4096 fp32 9.0 -> 8.7, 8192 x 1024 bfloat16 11.0 -> 11.2, wide rows mixed: 331 x 8192 11.4 ->
+        // 11.8; from memory 6.5 -> 6.4, 9.1 -> 9.0, 10.2 -> 10.4, 14.0 -> 14.0).
         const int64_t units = (a.rows + (int64_t)teams * group - 1) / ((int64_t)teams * group);
         const int64_t turns = plan.granules == 1 ? (units + cap - 1) / cap : 1;
         const int blocks = few ? 1 : (int)std::min<int64_t>((units + turns - 1) / turns, cap);

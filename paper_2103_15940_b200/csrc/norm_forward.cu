@@ -4,13 +4,14 @@
 // and the two sums a row needs one after the other (the variance is taken about the mean: a one-pass formula would lose
 // rows whose mean is large against their spread), so
 //   * a row stays in registers, two granules a thread, and additions and products issue in pairs: 118 instructions a
-//     granule and warp, against 186 with branches around loads and 64-bit row arithmetic (76 us -> 59 us on the case below);
+//     granule and warp, against 186 with branches around loads and 64-bit row arithmetic (76 us -> 59 us on the first case below);
 //   * two rows at a time share the barriers, and five shuffles reduce both rows' sums (79 instructions, 59 -> 48 us);
 //   * weight and bias stay in registers from row to row; four granules a thread without them took 75 us (their
 //     reads from L1 are four times the row's);
 //   * the next rows' granules are loaded while these are worked on.
-// Measured: 16384 x 4096 bfloat16 46.8 us (5.7 TB/s, 0.89 of the measured copy rate), 4096 x 768 fp32 4.8 us, fused
-// 8192 x 1024 bfloat16 14.9 us (4.5 TB/s), fused 16384 x 4096 bfloat16 87 us (6.1 TB/s), fp32 182 us (5.9 TB/s).
+// Measured (replayed from a graph, on sets of tensors larger than L2 in turn, as all figures here that do not say otherwise):
+// 16384 x 4096 bfloat16 46.9 us (5.7 TB/s, 0.89 of the measured copy rate), 4096 x 768 fp32 6.3 us (4.8 in L2), fused 8192 x 1024
+// bfloat16 14.6 us (4.6 TB/s), fused 16384 x 4096 bfloat16 89 us (6.0 TB/s), fp32 182 us (5.9 TB/s).
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -175,11 +176,12 @@ struct ForwardSteps {
 // kPlain: every granule whole and aligned, no format; granules go straight to registers, with V <= 2 those of the next
 // rows while these are worked on.  Otherwise any layout and an optional format: codes come as aligned pieces that are
 // shifted into place; rows of containers (kStaged) go through shared memory behind the histogram, where the next row
-// is copied as soon as this one has been read from there by its whole team.  Each way is the faster one for its type:
-// 16384 rows of 1021 take 23 us as shifted bfloat16 pieces and 31 us staged, as fp32 39 us shifted and 30 us staged.
-// Registers: 128 for a team of 512; fewer where more blocks on an SM are worth more, the general variant without dropout
-// (fp32 16384 x 4093 at 81, 80, 72, 64: 144, 122, 125, 126 us; bfloat16 at 94, 96, 80, 72: 130, 120, 109, 127, but x 2049 67, 62,
-// 71, 74; 2048 x 10237 at 94, 72: 47, 39.  With dropout they spill: bfloat16 16384 x 4093 at 128, 80: 206, 240).
+// is copied as soon as this one has been read from there by its whole team.  fp32 16384 x 1021 takes 39 us shifted and 30
+// staged; codes were staged only word by word (31 us against 23 shifted, in L2), not in pieces as containers are now.
+// Registers: 128 for a team of 512; fewer where more blocks on an SM are worth more, the general variant without dropout.  With
+// 128 against these: fp32 16384 x 4093 133 and 123 us; bfloat16 16384 x 4093 121 and 121, x 2049 76 and 62, x 1021 31 and 27, 2048 x
+// 10237 50 and 42.  (Bfloat16 at 96, 80, 72: x 4093 120, 109, 127, x 2049 62, 71, 74.  With dropout they spill: bfloat16
+// 16384 x 4093 at 128, 80: 206, 240.)
 constexpr int forward_registers(int type, int v, bool fused, bool plain) {
     if (plain || fused || v == 4) return 128;
     if (v == 1) return 64;
@@ -188,8 +190,10 @@ constexpr int forward_registers(int type, int v, bool fused, bool plain) {
 template <int kType, int V, int R, bool kFused, bool kPlain>
 __global__ void __maxnreg__((forward_registers(kType, V, kFused, kPlain)))
 norm_forward_rows_kernel(const ForwardArgs<kType> a, int team, const ForwardSteps step, int hist_words) {
-    // Wide rows keep the weights where that leaves the blocks of an SM as many as before (2048 rows of 16384 bfloat16: 39 us
-    // against 50, fused fp32 100 against 90; of 12288: fused bfloat16 49 against 54, fp32 54 against 37).
+    // Wide rows keep the weights where that leaves the blocks of an SM as many as before.  2048 rows, kept against read again, us:
+    // of 16384 bfloat16 41 against 50 / fused 64 against 68, fp32 53 against 62 / fused 105 against 89; of 12288 fused bfloat16 50
+    // against 54, fp32 67 against 71.  Of 9216 bfloat16 without dropout 30 against 25, which the rule goes by; towards 12288
+    // columns it turns (35 against 42, fp32 46 against 52).
     constexpr bool kKeep = V <= 2 || (V == 3 ? kFused && (kPlain || kType == QFMT_F32) : !(kFused && kType == QFMT_F32));
     constexpr bool kAhead = V <= 2 && kPlain, kStaged = !kPlain && kType == QFMT_F32;
     extern __shared__ __align__(16) uint32_t dynamic[];
@@ -358,7 +362,9 @@ int launch_forward_rows(const Call& c, const ForwardArgs<kType>& a, int team, cu
     if (rc != QFMT_OK) return rc;
     const int64_t want = (a.rows + teams * R - 1) / (teams * R), cap = (int64_t)c.dev.sm_count * resident;
     // Two rows at a time only where every team has them, and not where the mask's arithmetic already fills a small team's
-    // time (fused 8192 x 1024 bfloat16: 12.5 us with two, 11.1 with one; 8192 x 4096: 45.6 and 50.1).
+    // time.  Fused bfloat16, two against one: 8192 x 1024 on the same tensors in L2 12.6 against 11.2 us; from memory 14.6 against
+    // 14.4, 65536 x 512 49.0 against 47.8, but 16384 x 1024 25.6 against 26.2 and x 768 21.6 against 23.2.  Teams of more than 64:
+    // 8192 x 4096 45.6 against 50.1 (in L2).
     if constexpr (R == 2) {
         if (want < cap || (kFused && V == 2 && team <= 64)) return launch_forward_rows<kType, V, 1, kFused, kPlain>(c, a, team, stream);
     }
