@@ -96,7 +96,8 @@ __device__ __forceinline__ void store_gradients(const BackwardArgs<kType>& a, co
         put<kType, kPlain>(to.dx + i * a.dx.ld + at, n, a.dx, finish_output<kType, kPlain, kLanes>(a, d, n, hist), from, after);
 }
 
-// Long rows: a block takes a row at a time and reads it twice.
+// Long rows: a block takes a row at a time and reads it twice; a thread adds up its granules' sums in 64 bits, as in the forward
+// pass.
 template <int kType, bool kFused>
 __global__ void __launch_bounds__(kLoopThreads) norm_backward_loop_kernel(const BackwardArgs<kType> a) {
     extern __shared__ uint32_t lane_hist[];
@@ -114,13 +115,15 @@ __global__ void __launch_bounds__(kLoopThreads) norm_backward_loop_kernel(const 
             xhat = normalise<false>(widen_raw<kType>(load_any<kType>(a.h.p + row * a.h.ld + (int64_t)g * kGranule, n, inside)), mean, rstd, n);
             w = load_columns(a.weight, g, n, 1.0f);
         };
-        float2 s = make_float2(0.0f, 0.0f);
+        double sum_g = 0.0, sum_gx = 0.0;
         Granule dy, xhat, w;
         for (uint32_t g = threadIdx.x; g < granules; g += kLoopThreads) {
             load(g, granule_columns(a.cols, g), dy, xhat, w);
-            s = add2(s, row_sums(dy, xhat, w));
+            const float2 one = row_sums(dy, xhat, w);
+            sum_g += (double)one.x;
+            sum_gx += (double)one.y;
         }
-        s = block_sum(s, scratch);
+        const float2 s = block_sum(make_float2((float)sum_g, (float)sum_gx), scratch);
         for (uint32_t g0 = 0; g0 < granules; g0 += kLoopThreads) {  // whole warps
             const uint32_t g = g0 + threadIdx.x;
             const int n = granule_columns(a.cols, g);

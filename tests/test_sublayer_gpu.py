@@ -251,6 +251,34 @@ def test_large_centre_loses_nothing(cols):
     check_norm(run_norm(x, w, b, "f32"), x, w, b, "f32")
 
 
+def test_sums_of_very_long_rows():
+    """Rows of 4 Mi equal columns, or equal gradients: whatever a thread adds up one after the other must not be lost in a growing
+    sum.  At most 16 roundings on any path: three in a granule, nine in the tree over the block, the division, the rest for the
+    conversion from a thread's own sum."""
+    cols = (1 << 22) + 3
+    gen = torch.Generator().manual_seed(1)
+    x = torch.full((3, cols), 1.1)
+    x[1] = -0.3
+    x[2] = torch.randn(cols, generator=gen)
+    w, b = torch.ones(cols), torch.zeros(cols)
+    y, mean, rstd = run_norm(x, w, b, "f32")
+    want = x.double().mean(dim=1)
+    d_mean = 16 * ref.U * x.double().abs().mean(dim=1)
+    assert torch.all((mean.double() - want).abs() <= d_mean)
+    assert torch.all(y[:2].double().abs() <= (d_mean * EPS ** -0.5 * 1.01)[:2, None])
+    dy = torch.full((3, cols), 0.3)
+    dy[2] = x[2] * 0.7 + 0.1
+    h = torch.stack((x[2], x[2].flip(0), x[2]))
+    mean, rstd = saved(h)
+    dx = run_norm_backward(h, dy, mean, rstd, w, "f32")[0].double()
+    xhat = (h.double() - mean.double()[:, None]) * rstd.double()[:, None]
+    g = dy.double()
+    c1, c2 = g.mean(dim=1, keepdim=True), (g * xhat).mean(dim=1, keepdim=True)
+    d_c1, d_c2 = 16 * ref.U * g.abs().mean(dim=1, keepdim=True), 20 * ref.U * (g * xhat).abs().mean(dim=1, keepdim=True)
+    tol = rstd.double()[:, None] * (d_c1 + xhat.abs() * d_c2 + 6 * ref.U * (g.abs() + c1.abs() + (xhat * c2).abs()))
+    assert torch.all((dx - rstd.double()[:, None] * (g - c1 - xhat * c2)).abs() <= 1.01 * tol)
+
+
 def test_rows_that_do_not_vary_and_special_rows():
     x = torch.randn(6, 520, generator=torch.Generator().manual_seed(1))
     x[0], x[1] = 0.0, 3.0
