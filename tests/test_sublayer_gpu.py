@@ -797,6 +797,64 @@ def test_column_sums_of_more_than_two_to_the_thirty_columns():
         assert torch.all(edge == SENTINEL)
 
 
+def test_passes_over_a_row_of_more_than_two_to_the_thirty_columns():
+    """Every pass over one row of 2^30 + 8 columns (byte offsets pass 2^31): results by chunks against 64 bits, masks against the
+    generator at both ends and around 2^29 and 2^30."""
+    cols, kind, p, seed, offset = (1 << 30) + 8, torch.bfloat16, 0.25, 5, 1 << 40
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    x, r = (torch.empty(cols, dtype=kind, device=DEV).normal_(generator=gen) for _ in range(2))
+    h, y = torch.empty_like(x), torch.empty_like(x)
+    drop = qf.make_dropout(p, seed, offset)
+    scale = 65536 / (65536 - ref.threshold(p))
+
+    def chunks(*tensors):
+        for i in range(0, cols, 1 << 27):
+            yield [t[i:i + (1 << 27)].double() for t in tensors]
+
+    def near(got, want, extra):
+        """Within one rounding to bfloat16 and `extra`."""
+        return bool(torch.all((got - want).abs() <= ref.UNIT["bf16"] * (want.abs() + extra) + extra))
+
+    def kept(i, n):
+        """The mask of columns i .. i + n (i a multiple of 8)."""
+        words = ref.philox((np.arange(i // 8, (i + n) // 8, dtype=np.uint64),) + tuple(np.full(n // 8, v, dtype=np.uint64)
+                           for v in (0, offset & 0xFFFFFFFF, offset >> 32)), (seed, 0))
+        bits = np.stack([v for w in words for v in (w & np.uint64(0xFFFF), w >> np.uint64(16))], axis=1).reshape(-1)
+        return torch.from_numpy(bits >= ref.threshold(p)).to(DEV)
+
+    y.fill_(1.0)
+    qf.qfmt_dropout(y, 0, None, 0, y, 0, 1, cols, kind, drop)
+    mask = y != 0
+    for i in (0, (1 << 29) - 64, (1 << 30) - 1024, cols - 4096):
+        assert torch.equal(mask[i:i + 4096], kept(i, min(4096, cols - i)))
+    qf.qfmt_dropout(x, 0, None, 0, y, 0, 1, cols, kind, drop)
+    assert all(near(d, v * m * scale, 2.0 ** -20) for d, v, m in chunks(y, x, mask))
+    norm = qf.make_norm(1, cols, kind, EPS)
+    stat = torch.empty(2, device=DEV)
+    qf.qfmt_dropout_add_layer_norm(norm, drop, x, r, None, None, h, y, stat[:1], stat[1:])
+    total = square = 0.0
+    for v, u, m in chunks(x, r, mask):
+        t = u + v * m * scale
+        total, square = total + float(t.sum()), square + float(t.square().sum())
+    mean = total / cols
+    rstd = (square / cols - mean * mean + EPS) ** -0.5
+    assert abs(float(stat[0]) - mean) < 1e-6 and abs(float(stat[1]) / rstd - 1) < 1e-6
+    for v, u, m, hh, yy in chunks(x, r, mask, h, y):
+        t = u + v * m * scale
+        assert near(hh, t, 2.0 ** -20) and near(yy, (t - mean) * rstd, 2.0 ** -18)
+    qf.qfmt_layer_norm(norm, h, None, None, y, stat[:1], stat[1:])
+    mean, rstd = float(stat[0]), float(stat[1])
+    assert all(near(yy, (hh - mean) * rstd, 2.0 ** -18) for yy, hh in chunks(y, h))
+    dy, dres = r, x                                            # the residual serves as a gradient; dresidual takes x's place
+    c1 = c2 = 0.0
+    for g, hh in chunks(dy, h):
+        c1, c2 = c1 + float(g.sum()) / cols, c2 + float((g * (hh - mean)).sum()) * rstd / cols
+    qf.qfmt_dropout_add_layer_norm_backward(norm, drop, dy, None, h, stat[:1], stat[1:], None, y, dres, None, None, None, 0)
+    for g, hh, m, dx, dr in chunks(dy, h, mask, y, dres):
+        want = rstd * (g - c1 - (hh - mean) * rstd * c2)
+        assert near(dr, want, 2.0 ** -18) and near(dx, want * m * scale, 2.0 ** -17)
+
+
 def test_column_sums_of_no_rows_of_the_widest_matrix():
     cols = (1 << 31) - 1
     norm = qf.make_norm(0, cols, torch.bfloat16, EPS)
