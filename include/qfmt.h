@@ -568,6 +568,154 @@ int qfmt_dropout_add_layer_norm_backward(const qfmt_norm_t* norm, const qfmt_dro
                                          size_t workspace_bytes, void* stream);
 
 /*
+ * A product of 16-bit codes with what follows it in a layer done on its sums before they are stored:
+ *     z = op(A) op(B) + bias,   y = act(z) + residual.
+ * Operands as for qfmt_gemm_packed16 (16-byte aligned, leading dimensions multiples of 8, either one transposed), both of
+ * storage type dtype: QFMT_F16 (1/5/10 codes) or QFMT_BF16 (1/8/7 codes).  Sums, bias and activation are in 32 bits; y and z
+ * are rounded to the storage type once each (to nearest even; what overflows becomes infinite, as in qfmt_quantize_stats).
+ * The activation takes the 32-bit z.  No statistics are kept: qfmt_linear_forward and qfmt_bias_quantize_stats_pack16 do that.
+ *   QFMT_ACT_NONE z, QFMT_ACT_RELU max(z, 0), QFMT_ACT_GELU z Phi(z), QFMT_ACT_SILU z / (1 + exp(-z)),
+ *   QFMT_ACT_GELU_TANH z / 2 (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3)))
+ */
+enum { QFMT_ACT_NONE = 0, QFMT_ACT_RELU = 1, QFMT_ACT_GELU = 2, QFMT_ACT_GELU_TANH = 3, QFMT_ACT_SILU = 4 };
+typedef struct {
+    int32_t act;              /* QFMT_ACT_*                                                          */
+    int32_t reserved;
+    const float* d_bias;      /* device, N floats, or NULL for 0; not read by the backward pass       */
+    const void* d_residual;   /* device, M x N of the storage type, or NULL                          */
+    int64_t ld_residual;      /* leading dimension, 0 for N                                          */
+    void* d_z;                /* device, M x N of the storage type: forward, receives z (NULL where it
+                                 is not wanted); backward, read (may be NULL for QFMT_ACT_NONE)       */
+    int64_t ld_z;             /* leading dimension, 0 for N                                          */
+} qfmt_epilogue_t;
+
+/*
+ *   d_y, ldy     device, M x N of the storage type, leading dimension ldy >= N
+ *   d_workspace  device, 16-byte aligned, at least 256 bytes; qfmt_linear_act_workspace_bytes(A, B) is the size that lets
+ *                products of few tiles share a long K among the GPU's processors (partial sums added in a fixed order).
+ *                Status area and qfmt_device_status as for qfmt_gemm.  Calls that share a workspace must be ordered on one stream
+ * d_y, d_residual and d_z may start on any element; rows run fastest where they start on 16 bytes and the leading dimensions are
+ * multiples of 8.  d_y may equal d_residual when the leading dimensions agree; other overlap is an error the library cannot
+ * detect.  M = 0 or N = 0 is a no-op; K = 0 leaves z = bias.
+ * Errors: QFMT_ERR_BAD_ARG, QFMT_ERR_UNSUPPORTED_ARCH, QFMT_ERR_CUDA.
+ */
+int qfmt_linear_act(const qfmt_matrix16_t* A, const qfmt_matrix16_t* B, const qfmt_epilogue_t* epilogue, void* d_y, int64_t ldy,
+                    int32_t dtype, void* d_workspace, size_t workspace_bytes, void* stream);
+size_t qfmt_linear_act_workspace_bytes(const qfmt_matrix16_t* A, const qfmt_matrix16_t* B); /* 0 if the shapes do not agree */
+
+/*
+ * The way back through a product and the activation in front of it.  With dY the gradient at the output of the NEXT product
+ * (A = dY, B its weight transposed) and z as the forward pass stored it,
+ *     dz = (op(A) op(B) + residual) act'(z),   dbias = sums of dz over the rows;
+ * residual is a gradient that reaches act(z) by another path.  With QFMT_ACT_NONE and the residual this is also
+ * dX = dZ W^T + dY of a layer with a residual addition.  (Weight gradients are products without an epilogue: qfmt_gemm_packed16.)
+ *   d_dz, ld_dz  device, M x N of the storage type
+ *   d_dbias      device, N floats, or NULL: sums of the 32-bit dz, in an order that depends on the sizes alone
+ *   d_workspace  at least qfmt_linear_act_workspace_bytes(A, B) bytes if d_dbias is wanted
+ * d_dz may equal d_residual or d_z when the leading dimensions agree.  M = 0 leaves dbias = 0.
+ * The derivative of relu at 0 is 0.  Errors as above.
+ */
+int qfmt_linear_act_backward(const qfmt_matrix16_t* A, const qfmt_matrix16_t* B, const qfmt_epilogue_t* epilogue, void* d_dz,
+                             int64_t ld_dz, float* d_dbias, int32_t dtype, void* d_workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The same where the gradient dy of act(z) is there already: dz = dy act'(z), dbias = sums of dz over the rows; for
+ * QFMT_ACT_NONE d_z may be NULL, and with d_dz NULL as well only the column sums are formed: the bias gradient of any product.
+ *   d_dy, d_z, d_dz  device, rows x cols of storage type dtype (QFMT_F32, QFMT_F16 or QFMT_BF16); leading dimensions of 0 stand
+ *                    for cols; any alignment of an element.  d_dz may equal d_dy or d_z when their leading dimensions agree
+ *   d_dbias          device, cols floats, or NULL
+ *   d_workspace      16-byte aligned, at least qfmt_act_backward_workspace_bytes(rows, cols) bytes; NULL if d_dbias is
+ * rows = 0 (dbias = 0) and cols = 0 are valid; rows and cols are below 2^31.  Errors as above.
+ */
+int qfmt_act_backward(const void* d_dy, int64_t ld_dy, const void* d_z, int64_t ld_z, void* d_dz, int64_t ld_dz, float* d_dbias,
+                      int64_t rows, int64_t cols, int32_t dtype, int32_t act, void* d_workspace, size_t workspace_bytes, void* stream);
+size_t qfmt_act_backward_workspace_bytes(int64_t rows, int64_t cols);
+
+/*
+ * Softmax cross entropy on top of the product that makes the logits, which are never stored:
+ *     logits = H op(W) + bias,   lse = log sum_v exp(logits_v),   loss = lse - logits_target.
+ *   H            tokens x D codes, trans must be 0;  W  op(W) is D x V: {W, trans 0} stored D x V, {W, trans 1} stored V x D
+ *                (an embedding).  Both as for qfmt_linear_act, of storage type kind->dtype.  tokens, D and V are at least 1 (tokens = 0
+ *                is valid and gives mean = 0)
+ *   d_bias       device, V floats, or NULL; -infinity takes a word out of the vocabulary
+ *   d_targets    device, 8-byte aligned, tokens numbers.  Rows whose target is ignore_index do not count: their loss and lse
+ *                are 0, and H is not read there (whatever it holds).  They cost no products.  Any other target outside 0 .. V - 1 gives a NaN
+ *                loss and lse
+ *   d_loss       device, tokens floats, or NULL;  d_lse  device, tokens floats, or NULL: what the backward pass needs
+ *   d_mean       device, one float, or NULL: the mean loss of the rows that count (0 if none does)
+ *   d_workspace  device, 16-byte aligned, at least qfmt_linear_cross_entropy_workspace_bytes(H, W, 0) bytes; status area and
+ *                sharing as for qfmt_gemm
+ * Sums, exponentials and statistics are in 32 bits; results do not depend on the order in which blocks run.
+ * The backward pass, with the same H, W, bias and targets and the forward pass's lse:
+ *     d = g (exp(logits - lse) - onehot(target)),  dH = d op(W)^T,  dW = the gradient of W as W is stored,  dbias = sums of d,
+ *     g = dloss (1 if d_dloss is NULL) * (1 / rows that count, if kind->mean) * (d_dls->scale, if given).
+ * The logits are formed again, a piece of the vocabulary at a time; d passes from one product to the next rounded to the storage
+ * type (binary16: times a power of two that puts the largest |g| at 2^13, so what is lost lies 2^-37 below it), which is the one
+ * rounding besides those of the results.
+ *   d_dloss      device, tokens floats, or NULL;  d_dls  device, 8-byte aligned, or NULL: the loss scale is read when the kernels run
+ *   d_dh, ld_dh  device, tokens x D of the storage type, or NULL; rows that do not count get zeros
+ *   d_dw, ld_dw  device, the stored shape of W, of the storage type, or NULL
+ *   d_dbias      device, V floats, or NULL (sums of the 32-bit d)
+ *   d_workspace  at least qfmt_linear_cross_entropy_workspace_bytes(H, W, 1) bytes
+ * d_dh and d_dw may start on any element.  Errors: QFMT_ERR_BAD_ARG, QFMT_ERR_UNSUPPORTED_ARCH, QFMT_ERR_CUDA.
+ */
+typedef struct {
+    int64_t ignore_index;     /* target of rows that do not count, e.g. -100                        */
+    int32_t dtype;            /* QFMT_F16 or QFMT_BF16                                               */
+    int32_t mean;             /* 1: gradients are those of the mean over the rows that count; 0: of the sum */
+} qfmt_cross_entropy_t;
+int qfmt_linear_cross_entropy(const qfmt_matrix16_t* H, const qfmt_matrix16_t* W, const qfmt_cross_entropy_t* kind,
+                              const float* d_bias, const int64_t* d_targets, float* d_loss, float* d_lse, float* d_mean,
+                              void* d_workspace, size_t workspace_bytes, void* stream);
+int qfmt_linear_cross_entropy_backward(const qfmt_matrix16_t* H, const qfmt_matrix16_t* W, const qfmt_cross_entropy_t* kind,
+                                       const float* d_bias, const int64_t* d_targets, const float* d_lse, const float* d_dloss,
+                                       const qfmt_dls_t* d_dls, void* d_dh, int64_t ld_dh, void* d_dw, int64_t ld_dw, float* d_dbias,
+                                       void* d_workspace, size_t workspace_bytes, void* stream);
+size_t qfmt_linear_cross_entropy_workspace_bytes(const qfmt_matrix16_t* H, const qfmt_matrix16_t* W, int backward);
+
+/*
+ * The norm of all gradients of a step, and clipping by it.  The tensors are described by records in DEVICE memory, so that a
+ * list is built once and captured graphs can use it: fill src, dst, n and dtype of `count` records on the host, let
+ * qfmt_plan_tensors check them and number their chunks (it returns the chunks of the whole list, or an error < 0), and copy
+ * the records to the device.
+ */
+typedef struct {
+    const void* src;          /* device, n elements, any alignment of an element (NULL if n = 0)      */
+    void* dst;                /* device: where qfmt_grad_clip writes; may equal src.  NULL: norm only */
+    int64_t n;                /* 0 .. 2^46                                                            */
+    int32_t dtype;            /* QFMT_F32, QFMT_F16 or QFMT_BF16                                      */
+    int32_t reserved;
+    int64_t first_chunk;      /* written by qfmt_plan_tensors                                         */
+} qfmt_tensor_t;
+int64_t qfmt_plan_tensors(qfmt_tensor_t* h_tensors, int64_t count);
+
+typedef struct {
+    float norm;               /* sqrt(sum (g / scale)^2)                                              */
+    float factor;             /* what qfmt_grad_clip multiplies by                                    */
+    uint64_t n_nonfinite;     /* infinities and NaN among the gradients                              */
+} qfmt_grad_norm_t;
+
+/*
+ * norm = sqrt(sum over all tensors of (g / scale)^2), scale = d_dls->scale (1 if d_dls is NULL), squares and sums in 64 bits,
+ * and factor = min(1, max_norm / norm) / scale.  With any infinity or NaN among the gradients norm is infinite or NaN and factor is
+ * 1: such a step is to be skipped, and qfmt_grad_clip leaves its gradients as they are.
+ *   max_norm   > 0; infinity only takes the loss scale out
+ *   d_norm     device, 8-byte aligned: receives the record
+ *   d_stats    device, 8-byte aligned, or NULL: a statistics record for qfmt_dls_update.  n_total, n_nan and n_inf_in are those of
+ *              the gradients, everything else is 0
+ *   d_workspace  device, 16-byte aligned, at least qfmt_grad_norm_workspace_bytes(count, chunks) bytes
+ * The order of summation depends on the sizes (and the GPU's number of processors) alone.  Call qfmt_dls_update after this, not before:
+ * it changes the scale.  count = 0 is valid (norm 0).
+ * qfmt_grad_clip writes dst = src * factor, in 32 bits, rounded to dtype, for every record with a dst; where dst equals src and factor
+ * is 1 nothing moves.
+ * Errors: QFMT_ERR_BAD_ARG, QFMT_ERR_UNSUPPORTED_ARCH, QFMT_ERR_CUDA.
+ */
+int qfmt_grad_norm(const qfmt_tensor_t* d_tensors, int64_t count, int64_t chunks, float max_norm, const qfmt_dls_t* d_dls,
+                   qfmt_grad_norm_t* d_norm, qfmt_stats_t* d_stats, void* d_workspace, size_t workspace_bytes, void* stream);
+size_t qfmt_grad_norm_workspace_bytes(int64_t count, int64_t chunks);
+int qfmt_grad_clip(const qfmt_tensor_t* d_tensors, int64_t count, int64_t chunks, const qfmt_grad_norm_t* d_norm, void* stream);
+
+/*
  * qfmt_gemm for callers that cannot allocate device memory.  (The paper has no counterpart of
  * this call; it exists for the way the library gets embedded.)
  *

@@ -76,6 +76,26 @@ class qfmt_norm_t(ctypes.Structure):
                                               "ld_dx", "ld_dresidual")] + [("dtype", ctypes.c_int32), ("eps", ctypes.c_float)]
 
 
+class qfmt_epilogue_t(ctypes.Structure):
+    _fields_ = [("act", ctypes.c_int32), ("reserved", ctypes.c_int32), ("d_bias", ctypes.c_void_p), ("d_residual", ctypes.c_void_p),
+                ("ld_residual", ctypes.c_int64), ("d_z", ctypes.c_void_p), ("ld_z", ctypes.c_int64)]
+
+
+class qfmt_cross_entropy_t(ctypes.Structure):
+    _fields_ = [("ignore_index", ctypes.c_int64), ("dtype", ctypes.c_int32), ("mean", ctypes.c_int32)]
+
+
+class qfmt_tensor_t(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("first_chunk", ctypes.c_int64)]
+
+
+class qfmt_grad_norm_t(ctypes.Structure):
+    _fields_ = [("norm", ctypes.c_float), ("factor", ctypes.c_float), ("n_nonfinite", ctypes.c_uint64)]
+
+
+QFMT_ACT_NONE, QFMT_ACT_RELU, QFMT_ACT_GELU, QFMT_ACT_GELU_TANH, QFMT_ACT_SILU = range(5)
+
 QFMT_F32, QFMT_F16, QFMT_BF16 = 0, 1, 2
 _STORAGE = {"torch.float32": QFMT_F32, "torch.float16": QFMT_F16, "torch.bfloat16": QFMT_BF16}
 
@@ -190,6 +210,31 @@ def _bind_optional(L: ctypes.CDLL) -> None:
     L.qfmt_dropout_add_layer_norm.restype = ci
     L.qfmt_dropout_add_layer_norm_backward.argtypes = [vp] * 14 + [ci, vp, sz, vp]
     L.qfmt_dropout_add_layer_norm_backward.restype = ci
+    i32 = ctypes.c_int32
+    L.qfmt_linear_act.argtypes = [vp, vp, vp, vp, i64, i32, vp, sz, vp]
+    L.qfmt_linear_act.restype = ci
+    L.qfmt_linear_act_workspace_bytes.argtypes = [vp, vp]
+    L.qfmt_linear_act_workspace_bytes.restype = sz
+    L.qfmt_linear_act_backward.argtypes = [vp, vp, vp, vp, i64, vp, i32, vp, sz, vp]
+    L.qfmt_linear_act_backward.restype = ci
+    L.qfmt_act_backward.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i64, i32, i32, vp, sz, vp]
+    L.qfmt_act_backward.restype = ci
+    L.qfmt_act_backward_workspace_bytes.argtypes = [i64, i64]
+    L.qfmt_act_backward_workspace_bytes.restype = sz
+    L.qfmt_linear_cross_entropy.argtypes = [vp] * 9 + [sz, vp]
+    L.qfmt_linear_cross_entropy.restype = ci
+    L.qfmt_linear_cross_entropy_backward.argtypes = [vp] * 9 + [i64, vp, i64, vp, vp, sz, vp]
+    L.qfmt_linear_cross_entropy_backward.restype = ci
+    L.qfmt_linear_cross_entropy_workspace_bytes.argtypes = [vp, vp, ci]
+    L.qfmt_linear_cross_entropy_workspace_bytes.restype = sz
+    L.qfmt_plan_tensors.argtypes = [vp, i64]
+    L.qfmt_plan_tensors.restype = i64
+    L.qfmt_grad_norm.argtypes = [vp, i64, i64, ctypes.c_float, vp, vp, vp, vp, sz, vp]
+    L.qfmt_grad_norm.restype = ci
+    L.qfmt_grad_norm_workspace_bytes.argtypes = [i64, i64]
+    L.qfmt_grad_norm_workspace_bytes.restype = sz
+    L.qfmt_grad_clip.argtypes = [vp, i64, i64, vp, vp]
+    L.qfmt_grad_clip.restype = ci
     L.qfmt_gemm_builtin_scratch.argtypes = [matp, matp, vp, ctypes.c_int64, ctypes.POINTER(qfmt_format_t), vp, vp]
     L.qfmt_gemm_builtin_scratch.restype = ci
     L.qfmt_selftest_bounded_wait.argtypes = [vp, ctypes.c_uint32, vp, vp]
@@ -534,3 +579,103 @@ def qfmt_dropout_add_layer_norm_backward(norm: qfmt_norm_t, drop: Optional[qfmt_
     _sublayer("dropout_add_layer_norm_backward", _ref(norm, qfmt_norm_t), _ref(drop, qfmt_dropout_t), d_dy, d_dh, d_h, d_mean, d_rstd, d_weight,
               d_dx, d_dresidual, d_dweight, d_dbias, _ref(fmt, qfmt_format_t), d_stats, accumulate, d_workspace, workspace_bytes,
               _stream_handle(stream))
+
+
+def make_epilogue(act: int = QFMT_ACT_NONE, d_bias=None, d_residual=None, ld_residual: int = 0, d_z=None, ld_z: int = 0) -> qfmt_epilogue_t:
+    """What follows a product's sums (a leading dimension of 0 is a dense tensor's); see qfmt_epilogue_t in include/qfmt.h."""
+    return qfmt_epilogue_t(act, 0, _ptr(d_bias), _ptr(d_residual), ld_residual, _ptr(d_z), ld_z)
+
+
+def qfmt_linear_act_workspace_bytes(A: qfmt_matrix_t, B: qfmt_matrix_t) -> int:
+    return int(lib().qfmt_linear_act_workspace_bytes(_ref(A, qfmt_matrix_t), _ref(B, qfmt_matrix_t)))
+
+
+def qfmt_linear_act(A: qfmt_matrix_t, B: qfmt_matrix_t, epilogue: qfmt_epilogue_t, d_y, ldy: int, dtype, d_workspace,
+                    workspace_bytes: int, stream=None) -> None:
+    """y = act(op(A) op(B) + bias) + residual on 16-bit codes; see qfmt_linear_act in include/qfmt.h."""
+    _check(lib().qfmt_linear_act(_ref(A, qfmt_matrix_t), _ref(B, qfmt_matrix_t), _ref(epilogue, qfmt_epilogue_t), _ptr(d_y), ldy,
+                                 _storage(dtype), _ptr(d_workspace), workspace_bytes, _stream_handle(stream)), "qfmt_linear_act")
+
+
+def qfmt_linear_act_backward(A: qfmt_matrix_t, B: qfmt_matrix_t, epilogue: qfmt_epilogue_t, d_dz, ld_dz: int, d_dbias, dtype,
+                             d_workspace, workspace_bytes: int, stream=None) -> None:
+    """dz = (op(A) op(B) + residual) act'(z) and its column sums; see qfmt_linear_act_backward in include/qfmt.h."""
+    _check(lib().qfmt_linear_act_backward(_ref(A, qfmt_matrix_t), _ref(B, qfmt_matrix_t), _ref(epilogue, qfmt_epilogue_t), _ptr(d_dz),
+                                          ld_dz, _ptr(d_dbias), _storage(dtype), _ptr(d_workspace), workspace_bytes,
+                                          _stream_handle(stream)), "qfmt_linear_act_backward")
+
+
+def qfmt_act_backward_workspace_bytes(rows: int, cols: int) -> int:
+    return int(lib().qfmt_act_backward_workspace_bytes(rows, cols))
+
+
+def qfmt_act_backward(d_dy, ld_dy: int, d_z, ld_z: int, d_dz, ld_dz: int, d_dbias, rows: int, cols: int, dtype, act: int,
+                      d_workspace=None, workspace_bytes: int = 0, stream=None) -> None:
+    """dz = dy act'(z) and its column sums; see qfmt_act_backward in include/qfmt.h."""
+    _check(lib().qfmt_act_backward(_ptr(d_dy), ld_dy, _ptr(d_z), ld_z, _ptr(d_dz), ld_dz, _ptr(d_dbias), rows, cols, _storage(dtype), act,
+                                   _ptr(d_workspace), workspace_bytes, _stream_handle(stream)), "qfmt_act_backward")
+
+
+def make_cross_entropy(dtype, ignore_index: int = -100, mean: bool = True) -> qfmt_cross_entropy_t:
+    """Kind of a loss: storage type of the operands, target of rows that do not count, whose gradients; see qfmt_cross_entropy_t in
+    include/qfmt.h."""
+    return qfmt_cross_entropy_t(ignore_index, _storage(dtype), 1 if mean else 0)
+
+
+def qfmt_linear_cross_entropy_workspace_bytes(H: qfmt_matrix_t, W: qfmt_matrix_t, backward: bool) -> int:
+    return int(lib().qfmt_linear_cross_entropy_workspace_bytes(_ref(H, qfmt_matrix_t), _ref(W, qfmt_matrix_t), 1 if backward else 0))
+
+
+def qfmt_linear_cross_entropy(H: qfmt_matrix_t, W: qfmt_matrix_t, kind: qfmt_cross_entropy_t, d_bias, d_targets, d_loss, d_lse, d_mean,
+                              d_workspace, workspace_bytes: int, stream=None) -> None:
+    """Softmax cross entropy of the logits H op(W) + bias; see qfmt_linear_cross_entropy in include/qfmt.h."""
+    _check(lib().qfmt_linear_cross_entropy(_ref(H, qfmt_matrix_t), _ref(W, qfmt_matrix_t), _ref(kind, qfmt_cross_entropy_t), _ptr(d_bias),
+                                           _ptr(d_targets), _ptr(d_loss), _ptr(d_lse), _ptr(d_mean), _ptr(d_workspace), workspace_bytes,
+                                           _stream_handle(stream)), "qfmt_linear_cross_entropy")
+
+
+def qfmt_linear_cross_entropy_backward(H: qfmt_matrix_t, W: qfmt_matrix_t, kind: qfmt_cross_entropy_t, d_bias, d_targets, d_lse, d_dloss,
+                                       d_dls, d_dh, ld_dh: int, d_dw, ld_dw: int, d_dbias, d_workspace, workspace_bytes: int,
+                                       stream=None) -> None:
+    """Gradients of H, W and bias; see qfmt_linear_cross_entropy in include/qfmt.h."""
+    _check(lib().qfmt_linear_cross_entropy_backward(_ref(H, qfmt_matrix_t), _ref(W, qfmt_matrix_t), _ref(kind, qfmt_cross_entropy_t),
+                                                    _ptr(d_bias), _ptr(d_targets), _ptr(d_lse), _ptr(d_dloss), _ptr(d_dls), _ptr(d_dh),
+                                                    ld_dh, _ptr(d_dw), ld_dw, _ptr(d_dbias), _ptr(d_workspace), workspace_bytes,
+                                                    _stream_handle(stream)), "qfmt_linear_cross_entropy_backward")
+
+
+def make_tensors(tensors, outs=None):
+    """Host records (a ctypes array) of a list of dense torch tensors and, if given, of where qfmt_grad_clip writes: to be passed to
+    qfmt_plan_tensors and copied to the device; see qfmt_tensor_t in include/qfmt.h."""
+    outs = [None] * len(tensors) if outs is None else outs
+    if len(outs) != len(tensors):
+        raise ValueError(f"{len(tensors)} tensors and {len(outs)} outputs")
+    records = (qfmt_tensor_t * len(tensors))()
+    for r, t, o in zip(records, tensors, outs):
+        if not t.is_contiguous() or (o is not None and not (o.is_contiguous() and o.dtype == t.dtype and o.numel() == t.numel())):
+            raise ValueError("dense tensors expected, an output of its tensor's type and size")
+        r.src, r.dst, r.n, r.dtype = t.data_ptr() or None, None if o is None else o.data_ptr() or None, t.numel(), _storage(t.dtype)
+    return records
+
+
+def qfmt_plan_tensors(h_tensors, count: int) -> int:
+    """Checks host records and numbers their chunks; the chunks of the whole list.  See qfmt_plan_tensors in include/qfmt.h."""
+    chunks = int(lib().qfmt_plan_tensors(ctypes.addressof(h_tensors), count))
+    _check(min(chunks, 0), "qfmt_plan_tensors")
+    return chunks
+
+
+def qfmt_grad_norm_workspace_bytes(count: int, chunks: int) -> int:
+    return int(lib().qfmt_grad_norm_workspace_bytes(count, chunks))
+
+
+def qfmt_grad_norm(d_tensors, count: int, chunks: int, max_norm: float, d_dls, d_norm, d_stats, d_workspace, workspace_bytes: int,
+                   stream=None) -> None:
+    """Norm of all tensors of a list and the factor that clips them; see qfmt_grad_norm in include/qfmt.h."""
+    _check(lib().qfmt_grad_norm(_ptr(d_tensors), count, chunks, max_norm, _ptr(d_dls), _ptr(d_norm), _ptr(d_stats), _ptr(d_workspace),
+                                workspace_bytes, _stream_handle(stream)), "qfmt_grad_norm")
+
+
+def qfmt_grad_clip(d_tensors, count: int, chunks: int, d_norm, stream=None) -> None:
+    """Every tensor of a list times the factor; see qfmt_grad_norm in include/qfmt.h."""
+    _check(lib().qfmt_grad_clip(_ptr(d_tensors), count, chunks, _ptr(d_norm), _stream_handle(stream)), "qfmt_grad_clip")

@@ -34,6 +34,11 @@ int current_device(DeviceInfo* info) {
     return cc == 10 ? QFMT_OK : QFMT_ERR_UNSUPPORTED_ARCH;
 }
 
+unsigned long long next_launch_tag() {
+    static std::atomic<unsigned long long> counter{0};
+    return (counter.fetch_add(1) % ((1ull << 48) - 1)) + 1;
+}
+
 int validate_format(const qfmt_format_t* fmt) {
     if (fmt == nullptr) return QFMT_ERR_BAD_ARG;
     if (fmt->e < 2 || fmt->e > 8) return QFMT_ERR_BAD_FORMAT;

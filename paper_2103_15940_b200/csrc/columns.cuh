@@ -1,0 +1,41 @@
+// Sums of a matrix' columns from parts: [parts][pitch] fp32, part by part in a fixed order.
+#pragma once
+
+#include "common.cuh"
+
+namespace qfmt {
+
+constexpr int kJoinCols = 32, kJoinGroups = 8;
+
+// Block of 32 columns x 8 groups: group g adds parts g, g + 8, ..., then the groups are added in order.  `count` (or NULL)
+// holds the rows counted on the device: only the parts of whole 256-row tiles that hold some of them were written.
+// `scale` (or NULL): what the sums are multiplied by.
+static __global__ void __launch_bounds__(kJoinCols * kJoinGroups)
+join_columns_kernel(const float* __restrict__ parts, int64_t pitch, int n_parts, const int* count, const float* scale, float* __restrict__ out,
+                    int cols) {
+    __shared__ float sums[kJoinGroups][kJoinCols];
+    grid_dependency_wait();
+    grid_launch_dependents();
+    if (count != nullptr) n_parts = (*count + 255) / 256 * 8;
+    const int c = threadIdx.x % kJoinCols, g = threadIdx.x / kJoinCols, col = blockIdx.x * kJoinCols + c;
+    float s = 0.0f;
+    if (col < cols) {
+#pragma unroll 8
+        for (int i = g; i < n_parts; i += kJoinGroups) s = __fadd_rn(s, parts[(int64_t)i * pitch + col]);
+    }
+    sums[g][c] = s;
+    __syncthreads();
+    if (g == 0 && col < cols) {
+        for (int i = 1; i < kJoinGroups; ++i) s = __fadd_rn(s, sums[i][c]);
+        out[col] = scale != nullptr ? __fmul_rn(s, *scale) : s;
+    }
+}
+
+inline int launch_join_columns(const float* parts, int64_t pitch, int64_t n_parts, const int* count, const float* scale,
+                               float* out, int64_t cols, cudaStream_t stream) {
+    QFMT_CUDA_TRY(launch_overlapping(join_columns_kernel, (unsigned)((cols + kJoinCols - 1) / kJoinCols), (unsigned)(kJoinCols * kJoinGroups),
+                                     0, stream, parts, pitch, (int)n_parts, count, scale, out, (int)cols));
+    return QFMT_OK;
+}
+
+}  // namespace qfmt

@@ -22,6 +22,9 @@ struct DeviceInfo {
 // Returns QFMT_OK and fills *info, or QFMT_ERR_CUDA / QFMT_ERR_UNSUPPORTED_ARCH.
 int current_device(DeviceInfo* info);
 
+// Tag of the next launch that reports to a status area: process-wide, never zero, 48 bits.
+unsigned long long next_launch_tag();
+
 // Checks the fields of a format descriptor (Section IV-A: e <= 8, m <= 23; RNE only).
 int validate_format(const qfmt_format_t* fmt);
 

@@ -1,0 +1,845 @@
+// Softmax cross entropy on top of the product that makes the logits, forward and backward, without the logits in memory:
+//     logits = H W + bias,  lse = log sum exp(logits),  loss = lse - logits_target,
+//     d = g (exp(logits - lse) - onehot),  dH = d W^T,  dW = H^T d,  dbias = column sums of d.
+//
+// Rows that do not count are taken out first: compact_kernel numbers the others, and the products run over as many rows as it
+// found (the host never learns the number).  If all count, H is read in place.  Forward, the product's epilogue reduces each row's
+// 128 logits to their maximum and the sum of exponentials relative to it (base 2, one pass: a later maximum rescales the sum),
+// and join_rows_kernel joins the pieces.  Backward, the vocabulary is walked in pieces: the product again, its epilogue forming d in
+// codes in a buffer that stays in the second-level cache, then the two products that read it.  dH is added up in fp32 over the pieces.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "activation.cuh"
+#include "columns.cuh"
+#include "common.cuh"
+#include "product16.cuh"
+
+namespace qfmt {
+namespace {
+
+using p16::Patch;
+
+struct Nothing {};
+
+// Head of the workspace behind the status area: what compact_kernel finds out.
+struct Found {
+    int count;       // rows that count
+    float scale;     // power of two that d is multiplied by on its way into codes
+    float unscale;   // its inverse
+};
+
+// ---- rows that count ----------------------------------------------------------------------------------------------------
+struct Compact {
+    const int64_t* targets;
+    int64_t ignore;
+    int rows, vocab;
+    Found* found;
+    int *index, *target;      // compact row -> row, target (-1: not a word)
+    // forward: results of rows that do not count
+    float *loss, *lse_out;
+    // backward: what d needs of a compact row
+    const float *lse, *dloss;
+    const qfmt_dls_t* dls;
+    float *lse_of, *g;
+    int mean, f16;
+    // H and its compact copy; dH, whose rows that do not count are zeros
+    const uint16_t* h;
+    int64_t ld_h;
+    uint16_t* copy;
+    int64_t ld_copy;
+    uint16_t* dh;
+    int64_t ld_dh;
+    int hidden;
+    int rows_per_block;
+};
+
+constexpr int kCompactThreads = 256;
+
+template <typename V>
+__device__ __forceinline__ V block_sum(V v, V* scratch) {  // scratch: one per warp; every thread gets the sum
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = scratch[0];
+    for (int w = 1; w < kCompactThreads / 32; ++w) v += scratch[w];
+    return v;
+}
+
+// A block has rows_per_block rows and finds the place of its first by counting all rows itself (targets are a few bytes a row
+// and lie in the second-level cache), so blocks need not wait for one another.
+template <bool kBackward>
+__global__ void __launch_bounds__(kCompactThreads)
+compact_kernel(const Compact c, unsigned long long* status, unsigned long long tag) {
+    __shared__ int scratch[kCompactThreads / 32], place[kCompactThreads];
+    __shared__ float most[kCompactThreads / 32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    announce_launch(status, tag);
+    const int first = (int)blockIdx.x * c.rows_per_block;
+    const int end = first + c.rows_per_block < c.rows ? first + c.rows_per_block : c.rows;
+    int before = 0, total = 0;
+#pragma unroll 4
+    for (int i = tid; i < c.rows; i += kCompactThreads) {
+        const int counts = c.targets[i] != c.ignore ? 1 : 0;
+        total += counts;
+        before += i < first ? counts : 0;
+    }
+    before = block_sum(before, scratch);
+    total = block_sum(total, scratch);
+    const bool last = end == c.rows;
+    float scale = 1.0f, factor = 1.0f;
+    if (kBackward) {
+        if (c.mean) factor = __frcp_rn((float)(total > 0 ? total : 1));
+        if (c.dls != nullptr) factor = __fmul_rn(factor, c.dls->scale);
+        if (c.f16) {
+            // binary16: |d| <= |g|, so g scaled to 2^13 .. 2^14 leaves room above and 37 binades below
+            float g = fabsf(factor);
+            if (c.dloss != nullptr) {
+                float m = 0.0f;
+                for (int i = tid; i < c.rows; i += kCompactThreads) {
+                    const float v = c.targets[i] != c.ignore ? fabsf(c.dloss[i]) : 0.0f;
+                    m = v > m ? v : m;
+                }
+                for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+                if (lane == 0) most[warp] = m;
+                __syncthreads();
+                m = most[0];
+                for (int w = 1; w < kCompactThreads / 32; ++w) m = fmaxf(m, most[w]);
+                g = __fmul_rn(g, m);
+            }
+            if (g >= 1e-30f && g <= 1e30f) scale = __uint_as_float((267u << 23) - (__float_as_uint(g) & 0x7F800000u));  // 2^(13 - exponent of g)
+        }
+    }
+    if (last && tid == 0) {
+        c.found->count = total;
+        c.found->scale = scale;
+        c.found->unscale = __frcp_rn(scale);
+    }
+    const bool copy = total != c.rows;
+    const int whole = c.hidden & ~7;
+    for (int seg = first; seg < end; seg += kCompactThreads) {
+        const int row = seg + tid;
+        int64_t target = c.ignore;
+        if (row < end) target = c.targets[row];
+        const bool counts = row < end && target != c.ignore;
+        const unsigned mask = __ballot_sync(0xFFFFFFFFu, counts);
+        __syncthreads();
+        if (lane == 0) scratch[warp] = __popc(mask);
+        __syncthreads();
+        int at = before + __popc(mask & ((1u << lane) - 1u));
+        for (int w = 0; w < kCompactThreads / 32; ++w) {
+            if (w < warp) at += scratch[w];
+            before += scratch[w];
+        }
+        place[tid] = counts ? at : -1;
+        if (counts) {
+            c.index[at] = row;
+            c.target[at] = target >= 0 && target < c.vocab ? (int)target : -1;
+            if (kBackward) {
+                c.lse_of[at] = c.lse[row];
+                float g = factor;
+                if (c.dloss != nullptr) g = __fmul_rn(g, c.dloss[row]);
+                c.g[at] = __fmul_rn(g, scale);
+            }
+        } else if (!kBackward && row < end) {
+            if (c.loss != nullptr) c.loss[row] = 0.0f;
+            if (c.lse_out != nullptr) c.lse_out[row] = 0.0f;
+        }
+        __syncthreads();
+        if (!copy) continue;
+        const int n = end - seg < kCompactThreads ? end - seg : kCompactThreads;
+        for (int r = warp; r < n; r += kCompactThreads / 32) {
+            const int to = place[r];
+            if (to >= 0) {
+                const uint16_t* src = c.h + (int64_t)(seg + r) * c.ld_h;
+                uint16_t* dst = c.copy + (int64_t)to * c.ld_copy;
+#pragma unroll 4
+                for (int j = lane * 8; j < whole; j += 256) *reinterpret_cast<uint4*>(dst + j) = *reinterpret_cast<const uint4*>(src + j);
+                if (lane < c.hidden - whole) dst[whole + lane] = src[whole + lane];
+            } else if (kBackward && c.dh != nullptr) {
+                uint16_t* dst = c.dh + (int64_t)(seg + r) * c.ld_dh;
+                if ((reinterpret_cast<uintptr_t>(dst) & 15) == 0) {
+                    for (int j = lane * 8; j < whole; j += 256) *reinterpret_cast<uint4*>(dst + j) = make_uint4(0, 0, 0, 0);
+                    if (lane < c.hidden - whole) dst[whole + lane] = 0;
+                } else {
+                    for (int j = lane; j < c.hidden; j += 32) dst[j] = 0;
+                }
+            }
+        }
+    }
+    if (last && copy) {  // the weight gradient's products read whole stages of 64 rows
+        const int pad = (total + 63) / 64 * 64;
+        for (int r = total + warp; r < pad; r += kCompactThreads / 32)
+            for (int j = lane; j < c.hidden; j += 32) c.copy[(int64_t)r * c.ld_copy + j] = 0;
+    }
+}
+
+// ---- epilogues ------------------------------------------------------------------------------------------------------------
+
+// Per row and 128 columns: m = the largest logit, s = sum exp(logit - m), and the target's logit.  The exponentials are
+// 2^(logit log2 e - shift), one fused operation and one of the special function unit each, with shift = m log2 e rounded; what the rounding
+// took off is put back by one factor per 32 columns.  Logits whose product with log2 e overflows have m subtracted first.
+struct RowSumEpilogue {
+    struct Params {
+        const float* bias;
+        const int* target;
+        float2* parts;  // [128-column groups][pitch]
+        float* picked;  // the target's logit of a compact row
+        int64_t pitch;
+    };
+    struct Ahead {
+        int target;
+    };
+    static __device__ __forceinline__ void before(const Patch& p, const Params& e, Ahead& a) {
+        p.load_columns(e.bias);
+        a.target = p.row0 + p.lane < p.rows ? e.target[p.row0 + p.lane] - p.col0 : -1;
+    }
+    template <typename F>
+    static __device__ __forceinline__ void run(const Patch& p, const Params& e, Ahead& a, F release) {
+        const int row = p.row0 + p.lane;
+        float most = -INFINITY, sum = 0.0f;
+#pragma unroll 1
+        for (int c = 0; c < 4; ++c) {
+            uint32_t r[32];
+            p.load32(c, r);
+            p.wait();
+            if (c == 3) release();
+            const int left = p.cols - p.col0 - c * 32;
+            if (left <= 0) continue;
+            float v[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = __fadd_rn(__uint_as_float(r[j]), p.col[c * 32 + j]);
+            if (left < 32) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] = j < left ? v[j] : -INFINITY;
+            }
+            if ((a.target >> 5) == c) {
+                float t = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) t = (a.target & 31) == j ? v[j] : t;
+                e.picked[row] = t;
+            }
+            float m = v[0];
+#pragma unroll
+            for (int j = 1; j < 32; ++j) m = fmaxf(m, v[j]);
+            const float now = fmaxf(most, m);
+            float shift = __fmul_rn(now, kLog2E), back = 1.0f;
+            if (isinf(shift)) {
+                if (now != -INFINITY) {  // else nothing but -infinity yet: all terms are zero
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = __fsub_rn(v[j], now);
+                }
+                shift = 0.0f;
+            } else {
+                back = fast_exp2(-__fmaf_rn(now, kLog2E, -shift));
+            }
+            if (now != -INFINITY) sum = __fmul_rn(sum, fast_exp2(__fmul_rn(__fsub_rn(most, now), kLog2E)));
+            float s0 = 0.0f, s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) {
+                s0 = __fadd_rn(s0, fast_exp2(__fmaf_rn(v[j], kLog2E, -shift)));
+                s1 = __fadd_rn(s1, fast_exp2(__fmaf_rn(v[j + 1], kLog2E, -shift)));
+                s2 = __fadd_rn(s2, fast_exp2(__fmaf_rn(v[j + 2], kLog2E, -shift)));
+                s3 = __fadd_rn(s3, fast_exp2(__fmaf_rn(v[j + 3], kLog2E, -shift)));
+            }
+            sum = __fmaf_rn(__fadd_rn(__fadd_rn(s0, s1), __fadd_rn(s2, s3)), back, sum);
+            most = now;
+        }
+        if (row < p.rows && p.col0 < p.cols) e.parts[(int64_t)(p.col0 >> 7) * e.pitch + row] = make_float2(most, sum);
+    }
+};
+
+// d = g (exp(logit - lse) - onehot) in codes, zeros beyond the rows and the words; column sums of the 32-bit values.
+template <typename T>
+struct GradEpilogue {
+    struct Params {
+        const float* bias;
+        const int* target;
+        const float *lse, *g;
+        T* d;             // [rows of whole tiles][pitch]
+        float* parts;     // [32-row groups][pitch], or null
+        int64_t pitch;
+        int first_word;   // of this piece of the vocabulary
+    };
+    struct Ahead {
+        int target;
+        float lse, lse2, g, gp;  // lse2 = lse log2 e rounded; gp = g times what the rounding took off
+    };
+    static __device__ __forceinline__ void before(const Patch& p, const Params& e, Ahead& a) {
+        p.load_columns(e.bias);
+        const int row = p.row0 + p.lane;
+        const bool there = row < p.rows;
+        a.target = there ? e.target[row] - e.first_word - p.col0 : -1;
+        a.lse = there ? e.lse[row] : 0.0f;
+        a.g = there ? e.g[row] : 0.0f;
+        a.lse2 = __fmul_rn(a.lse, kLog2E);
+        a.gp = a.g;
+        if (isfinite(a.lse2)) a.gp = __fmul_rn(a.g, fast_exp2(-__fmaf_rn(a.lse, kLog2E, -a.lse2)));
+    }
+    template <typename F>
+    static __device__ __forceinline__ void run(const Patch& p, const Params& e, Ahead& a, F release) {
+        const bool there = p.row0 + p.lane < p.rows;
+        const bool huge = __any_sync(0xFFFFFFFFu, isinf(a.lse2));  // lse log2 e overflows: subtract first
+#pragma unroll 1
+        for (int c = 0; c < 2; ++c) {
+            uint32_t lo[32], hi[32];
+            p.load32(c * 2, lo);
+            p.load32(c * 2 + 1, hi);
+            p.wait();
+            if (c == 1) release();
+            const int left = p.cols - p.col0 - c * 64;
+            float v[64];
+#pragma unroll
+            for (int j = 0; j < 64; ++j) {
+                v[j] = __fadd_rn(__uint_as_float(j < 32 ? lo[j & 31] : hi[j & 31]), p.col[c * 64 + j]);
+                if (!huge) v[j] = __fmul_rn(a.gp, fast_exp2(__fmaf_rn(v[j], kLog2E, -a.lse2)));
+                else v[j] = __fmul_rn(a.g, fast_exp2(__fmul_rn(__fsub_rn(v[j], a.lse), kLog2E)));
+            }
+            if (a.target >= c * 64 && a.target < c * 64 + 64) {
+#pragma unroll
+                for (int j = 0; j < 64; ++j) v[j] = (a.target & 63) == j ? __fsub_rn(v[j], a.g) : v[j];
+            }
+            if (left < 64 || p.row0 + 32 > p.rows) {
+#pragma unroll
+                for (int j = 0; j < 64; ++j) v[j] = there && j < left ? v[j] : 0.0f;
+            }
+            p16::box_put_codes<T>(p.box, p.lane, v);
+            __syncwarp();
+            p16::box_store<T>(p.box, e.d, e.pitch, p.row0, p.row0 + 32, p.col0 + c * 64, (int)e.pitch, p.lane, true);
+            __syncwarp();
+            if (e.parts != nullptr) {
+                float* out = e.parts + (int64_t)(p.row0 >> 5) * e.pitch + p.col0 + c * 64 + p.lane;
+                float x[32], y[32];
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    x[j] = v[j];
+                    y[j] = v[32 + j];
+                }
+                const float s0 = p16::column_sum(x, p.lane), s1 = p16::column_sum(y, p.lane);
+                out[0] = s0;
+                out[32] = s1;
+            }
+        }
+    }
+};
+
+// The sums times a factor, in codes: dW.
+template <typename T>
+struct ScaledEpilogue {
+    struct Params {
+        const float* factor;
+        T* out;
+        int64_t ld;
+        int vec;
+    };
+    struct Ahead {
+        float factor;
+    };
+    static __device__ __forceinline__ void before(const Patch&, const Params& e, Ahead& a) { a.factor = *e.factor; }
+    template <typename F>
+    static __device__ __forceinline__ void run(const Patch& p, const Params& e, Ahead& a, F release) {
+#pragma unroll 1
+        for (int c = 0; c < 2; ++c) {
+            uint32_t lo[32], hi[32];
+            p.load32(c * 2, lo);
+            p.load32(c * 2 + 1, hi);
+            p.wait();
+            if (c == 1) release();
+            if (p.row0 >= p.rows || p.col0 + c * 64 >= p.cols) continue;
+            float v[64];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                v[j] = __fmul_rn(__uint_as_float(lo[j]), a.factor);
+                v[32 + j] = __fmul_rn(__uint_as_float(hi[j]), a.factor);
+            }
+            p16::box_put_codes<T>(p.box, p.lane, v);
+            __syncwarp();
+            p16::box_store<T>(p.box, e.out, e.ld, p.row0, p.rows, p.col0 + c * 64, p.cols, p.lane, e.vec != 0);
+            __syncwarp();
+        }
+    }
+};
+
+// The sums added to what the pieces before left, in fp32, one place per split of K: dH.
+struct AddEpilogue {
+    struct Params {
+        float* sums;
+        int64_t pitch, split_stride;
+        int add;  // 0: the first piece
+    };
+    using Ahead = Nothing;
+    static __device__ __forceinline__ void before(const Patch&, const Params&, Ahead&) {}
+    template <typename F>
+    static __device__ __forceinline__ void run(const Patch& p, const Params& e, Ahead&, F release) {
+        float* base = e.sums + (int64_t)p.split * e.split_stride;
+#pragma unroll 1
+        for (int c = 0; c < 4; ++c) {
+            uint32_t r[32];
+            p.load32(c, r);
+            p.wait();
+            if (c == 3) release();
+            const int col0 = p.col0 + c * 32;
+            if (p.row0 >= p.rows || col0 >= p.cols) continue;
+            if (e.add) {
+                p16::box_load<float>(p.box, base, e.pitch, p.row0, p.rows, col0, p.cols, p.lane, true);
+                __syncwarp();
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float4 w = *reinterpret_cast<const float4*>(p16::box_at(p.box, p.lane, k));
+                    const float s[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) r[4 * k + j] = __float_as_uint(__fadd_rn(s[j], __uint_as_float(r[4 * k + j])));
+                }
+                __syncwarp();
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) *p16::box_at(p.box, p.lane, k) = make_uint4(r[4 * k], r[4 * k + 1], r[4 * k + 2], r[4 * k + 3]);
+            __syncwarp();
+            p16::box_store<float>(p.box, base, e.pitch, p.row0, p.rows, col0, p.cols, p.lane, true);
+            __syncwarp();
+        }
+    }
+};
+
+// ---- joining ----------------------------------------------------------------------------------------------------------------
+
+constexpr int kJoinRows = 32, kJoinParts = 8;
+
+// Block of 32 rows x 8 groups: group q joins a row's parts q, q + 8, ..., then the eight are joined in order.
+__global__ void __launch_bounds__(kJoinRows * kJoinParts)
+join_rows_kernel(const float2* __restrict__ parts, int64_t pitch, int n_parts, const Found* found, const int* __restrict__ index,
+                 const int* __restrict__ target, const float* __restrict__ picked, float* loss, float* lse_out, float* compact_loss,
+                 float* mean) {
+    __shared__ float2 joined[kJoinParts][kJoinRows];
+    const int r = threadIdx.x % kJoinRows, q = threadIdx.x / kJoinRows, row = (int)blockIdx.x * kJoinRows + r;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int count = found->count;
+    float m = -INFINITY, s = 0.0f;
+    auto join = [&](float2 v) {
+        const float now = fmaxf(m, v.x);
+        if (now == -INFINITY) {
+            s = __fadd_rn(s, v.y);  // zero, or NaN where all of a part's logits are
+            return;
+        }
+        s = __fmaf_rn(v.y, fast_exp2(__fmul_rn(__fsub_rn(v.x, now), kLog2E)), __fmul_rn(s, fast_exp2(__fmul_rn(__fsub_rn(m, now), kLog2E))));
+        m = now;
+    };
+    if (row < count) {
+#pragma unroll 4
+        for (int i = q; i < n_parts; i += kJoinParts) join(parts[(int64_t)i * pitch + row]);
+    }
+    joined[q][r] = make_float2(m, s);
+    __syncthreads();
+    if (q != 0) return;
+    float l = 0.0f;
+    if (row < count) {
+        for (int i = 1; i < kJoinParts; ++i) join(joined[i][r]);
+        float lse = __fadd_rn(m, logf(s));
+        l = __fsub_rn(lse, picked[row]);
+        if (target[row] < 0) l = lse = __int_as_float(0x7FC00000);  // the target is not a word
+        const int to = index[row];
+        if (loss != nullptr) loss[to] = l;
+        if (lse_out != nullptr) lse_out[to] = lse;
+        if (compact_loss != nullptr) compact_loss[row] = l;
+    }
+    if (mean != nullptr) {  // the only block
+        double total = l;
+        for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
+        if (r == 0) *mean = (float)(total / (count > 0 ? count : 1));
+    }
+}
+
+__global__ void __launch_bounds__(1024)
+mean_kernel(const float* __restrict__ loss, const Found* found, float* mean) {
+    __shared__ double sums[32];
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int count = found->count;
+    double s = 0.0;
+    for (int i = threadIdx.x; i < count; i += 1024) s += loss[i];
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+    if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < 32; ++w) s += sums[w];
+        *mean = (float)(s / (count > 0 ? count : 1));
+    }
+}
+
+// dH: the splits of a compact row added in order, scaled back, rounded and put where the row came from.  A warp a row.
+template <typename T>
+__global__ void __launch_bounds__(256)
+scatter_kernel(const float* __restrict__ sums, int splits, int64_t split_stride, int64_t pitch, const Found* found,
+               const int* __restrict__ index, T* dh, int64_t ld, int hidden, int vec) {
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int lane = threadIdx.x & 31;
+    const int count = found->count;
+    const float factor = found->unscale;
+    for (int row = (int)(blockIdx.x * 8 + (threadIdx.x >> 5)); row < count; row += (int)gridDim.x * 8) {
+        const float* src = sums + (int64_t)row * pitch;
+        T* dst = dh + (int64_t)index[row] * ld;
+        for (int j = lane * 4; j < hidden; j += 128) {
+            float4 v = *reinterpret_cast<const float4*>(src + j);  // rows are padded to whole pieces
+            for (int s = 1; s < splits; ++s) {
+                const float4 w = *reinterpret_cast<const float4*>(src + s * split_stride + j);
+                v = make_float4(__fadd_rn(v.x, w.x), __fadd_rn(v.y, w.y), __fadd_rn(v.z, w.z), __fadd_rn(v.w, w.w));
+            }
+            const uint32_t lo = p16::pack_codes<T>(__fmul_rn(v.x, factor), __fmul_rn(v.y, factor));
+            const uint32_t hi = p16::pack_codes<T>(__fmul_rn(v.z, factor), __fmul_rn(v.w, factor));
+            if (vec && j + 4 <= hidden) {
+                *reinterpret_cast<uint2*>(dst + j) = make_uint2(lo, hi);
+            } else {
+                const uint32_t words[2] = {lo, hi};
+                const T* e = reinterpret_cast<const T*>(words);
+                for (int k = 0; k < 4 && j + k < hidden; ++k) dst[j + k] = e[k];
+            }
+        }
+    }
+}
+
+// ---- host side --------------------------------------------------------------------------------------------------------------
+
+bool misaligned(const void* p, uintptr_t size) { return (reinterpret_cast<uintptr_t>(p) & (size - 1)) != 0; }
+bool whole(const void* p, int64_t ld, int64_t size) { return !misaligned(p, 16) && (ld * size) % 16 == 0; }
+int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+struct Sizes {
+    int64_t rows, hidden, vocab;
+    bool stored_words;  // W stored with words as rows
+};
+int loss_sizes(const qfmt_matrix16_t* H, const qfmt_matrix16_t* W, Sizes* s) {
+    if (H == nullptr || W == nullptr || H->trans != 0) return QFMT_ERR_BAD_ARG;
+    s->stored_words = W->trans != 0;
+    s->rows = H->rows;
+    s->hidden = H->cols;
+    s->vocab = s->stored_words ? W->rows : W->cols;
+    if (s->hidden != (s->stored_words ? W->cols : W->rows)) return QFMT_ERR_BAD_ARG;
+    if (s->rows < 0 || s->hidden < 1 || s->vocab < 1) return QFMT_ERR_BAD_ARG;
+    if (s->rows > (1 << 24) || s->hidden > (1 << 24) || s->vocab > (1 << 28)) return QFMT_ERR_BAD_ARG;
+    if (up(s->rows, p16::kTileM) / p16::kTileM * (up(s->vocab, p16::kTileN) / p16::kTileN) > (1 << 26)) return QFMT_ERR_BAD_ARG;
+    return QFMT_OK;
+}
+
+// How the backward pass walks the vocabulary.  A piece's d (rows x piece, 2 bytes each) should stay in the second-level cache (126 MB)
+// between the product that writes it and the two that read it; and pieces of at least 1024 words keep those products whole.
+constexpr int64_t kPieceBytes = 64ll << 20;
+constexpr int64_t kPairs = 74, kMostSplits = 16, kLeastStages = 4;
+struct Plan {
+    int64_t tile_rows;   // rows of whole tiles
+    int64_t piece;       // words, a multiple of 256
+    int splits;          // of a piece's words in the product for dH
+    int64_t pitch_h;     // of the fp32 dH and the compact H
+};
+Plan plan_backward(const Sizes& s) {
+    Plan p;
+    p.tile_rows = up(s.rows > 0 ? s.rows : 1, p16::kTileM);
+    int64_t most = kPieceBytes / (p.tile_rows * 2) / p16::kTileN * p16::kTileN;
+    if (most < 1024) most = 1024;
+    const int64_t pieces = (s.vocab + most - 1) / most;
+    p.piece = up((s.vocab + pieces - 1) / pieces, p16::kTileN);
+    p.pitch_h = up(s.hidden, 8);
+    const int64_t tiles = p.tile_rows / p16::kTileM * (up(s.hidden, p16::kTileN) / p16::kTileN), stages = p.piece / p16::kStageK;
+    int64_t n = kPairs / tiles;
+    if (n > stages / kLeastStages) n = stages / kLeastStages;
+    if (n > kMostSplits) n = kMostSplits;
+    p.splits = n < 2 ? 1 : (int)n;
+    return p;
+}
+
+// The workspace's parts, in order; every one starts on 256 bytes.
+struct Layout {
+    size_t size = 0;
+    size_t take(size_t bytes) {
+        const size_t at = size;
+        size += (bytes + 255) / 256 * 256;
+        return at;
+    }
+};
+struct Places {
+    size_t found, index, target, compact_h;
+    size_t parts, picked, compact_loss;            // forward
+    size_t lse_of, g, d, column_parts, sums;         // backward
+    size_t total;
+};
+Places places(const Sizes& s, const Plan& plan, bool backward) {
+    Layout l;
+    Places p = {};
+    l.take(256);  // the status area, Found behind it
+    p.found = 64;
+    p.index = l.take((size_t)s.rows * 4);
+    p.target = l.take((size_t)s.rows * 4);
+    p.compact_h = l.take((size_t)up(s.rows, 64) * plan.pitch_h * 2);
+    if (!backward) {
+        p.parts = l.take((size_t)(up(s.vocab, 128) / 128) * s.rows * sizeof(float2));
+        p.picked = l.take((size_t)s.rows * 4);
+        p.compact_loss = l.take((size_t)s.rows * 4);
+    } else {
+        p.lse_of = l.take((size_t)s.rows * 4);
+        p.g = l.take((size_t)s.rows * 4);
+        p.d = l.take((size_t)plan.tile_rows * plan.piece * 2);
+        p.column_parts = l.take((size_t)(plan.tile_rows / 32) * plan.piece * 4);
+        p.sums = l.take((size_t)plan.splits * s.rows * plan.pitch_h * 4);
+    }
+    p.total = l.size;
+    return p;
+}
+
+template <typename T>
+T* at(void* workspace, size_t place) { return reinterpret_cast<T*>(static_cast<char*>(workspace) + place); }
+
+int check_loss(const qfmt_matrix16_t* H, const qfmt_matrix16_t* W, const qfmt_cross_entropy_t* kind, const float* d_bias,
+               const int64_t* d_targets, void* d_workspace, size_t workspace_bytes, bool backward, Sizes* s) {
+    const int rc = loss_sizes(H, W, s);
+    if (rc != QFMT_OK) return rc;
+    if (kind == nullptr || (kind->dtype != QFMT_F16 && kind->dtype != QFMT_BF16) || (kind->mean != 0 && kind->mean != 1)) return QFMT_ERR_BAD_ARG;
+    if (H->ld < H->cols || W->ld < W->cols || misaligned(d_bias, 4) || misaligned(d_targets, 8)) return QFMT_ERR_BAD_ARG;
+    if (W->ptr == nullptr || misaligned(W->ptr, 16) || (W->ld & 7)) return QFMT_ERR_BAD_ARG;
+    if (s->rows > 0 && (H->ptr == nullptr || misaligned(H->ptr, 16) || (H->ld & 7) || d_targets == nullptr)) return QFMT_ERR_BAD_ARG;
+    if (d_workspace == nullptr || misaligned(d_workspace, 16) || workspace_bytes < places(*s, plan_backward(*s), backward).total)
+        return QFMT_ERR_BAD_ARG;
+    return QFMT_OK;
+}
+
+Compact compact_args(const qfmt_matrix16_t* H, const qfmt_cross_entropy_t* kind, const int64_t* d_targets, const Sizes& s,
+                     const Plan& plan, const Places& pl, void* ws) {
+    Compact c = {};
+    c.targets = d_targets;
+    c.ignore = kind->ignore_index;
+    c.rows = (int)s.rows;
+    c.vocab = (int)s.vocab;
+    c.found = at<Found>(ws, pl.found);
+    c.index = at<int>(ws, pl.index);
+    c.target = at<int>(ws, pl.target);
+    c.mean = kind->mean;
+    c.f16 = kind->dtype == QFMT_F16;
+    c.h = H->ptr;
+    c.ld_h = H->ld;
+    c.copy = at<uint16_t>(ws, pl.compact_h);
+    c.ld_copy = plan.pitch_h;
+    c.hidden = (int)s.hidden;
+    return c;
+}
+template <bool kBackward>
+int launch_compact(Compact c, const p16::ProductParams& p, const DeviceInfo& dev, cudaStream_t stream) {
+    const int most = 2 * dev.sm_count;
+    int blocks = (c.rows + 31) / 32;
+    if (blocks > most) blocks = most;
+    c.rows_per_block = (c.rows + blocks - 1) / blocks;
+    blocks = (c.rows + c.rows_per_block - 1) / c.rows_per_block;
+    QFMT_CUDA_TRY(launch_overlapping(compact_kernel<kBackward>, (unsigned)blocks, (unsigned)kCompactThreads, 0, stream, c, p.status, p.tag));
+    return QFMT_OK;
+}
+
+// W's words first .. first + n - 1 as an operand: `words`: the words are the extent (logits), else they are K (dH).
+int word_operand(p16::Operand* o, const qfmt_matrix16_t* W, const Sizes& s, bool words, int64_t first, int64_t n) {
+    const uint16_t* base = W->ptr + (s.stored_words ? first * W->ld : first);
+    return p16::make_operand(o, base, words != s.stored_words, words ? n : s.hidden, words ? s.hidden : n, W->ld);
+}
+
+template <typename T>
+int backward_pieces(const qfmt_matrix16_t* W, const float* d_bias, const Sizes& s, const Plan& plan, const Places& pl, void* ws,
+                    const p16::Operand& h_rows, const p16::Operand& h_rows_alt, const p16::Operand& h_k, const p16::Operand& h_k_alt,
+                    p16::ProductParams base, void* d_dh, int64_t ld_dh, void* d_dw, int64_t ld_dw, float* d_dbias, const DeviceInfo& dev,
+                    cudaStream_t stream) {
+    const Found* found = at<Found>(ws, pl.found);
+    T* d = at<T>(ws, pl.d);
+    float* column_parts = at<float>(ws, pl.column_parts);
+    float* sums = at<float>(ws, pl.sums);
+    int rc;
+    for (int64_t first = 0; first < s.vocab; first += plan.piece) {
+        const int64_t n = first + plan.piece < s.vocab ? plan.piece : s.vocab - first, n64 = up(n, 64);
+        // d of this piece
+        p16::Operand w, dk, dm;
+        rc = word_operand(&w, W, s, true, first, n);
+        if (rc != QFMT_OK) return rc;
+        p16::ProductParams p = base;
+        p.M = (int)s.rows;
+        p.N = (int)n;
+        p.K = (int)s.hidden;
+        p.dyn = p16::kCountM;
+        p.alt = p16::kAltA;
+        p.splits = 1;
+        p.kb_per_split = (int)(up(s.hidden, p16::kStageK) / p16::kStageK);
+        typename GradEpilogue<T>::Params ge = {d_bias != nullptr ? d_bias + first : nullptr, at<int>(ws, pl.target), at<float>(ws, pl.lse_of),
+                                               at<float>(ws, pl.g), d, d_dbias != nullptr ? column_parts : nullptr, plan.piece, (int)first};
+        rc = p16::launch_product<GradEpilogue<T>>(h_rows, w, &h_rows_alt, p, ge, dev, stream);
+        if (rc != QFMT_OK) return rc;
+        if (d_dbias != nullptr) {
+            rc = launch_join_columns(column_parts, plan.piece, plan.tile_rows / 32, &found->count, &found->unscale, d_dbias + first, n, stream);
+            if (rc != QFMT_OK) return rc;
+        }
+        if (d_dw != nullptr) {
+            rc = p16::make_operand(&dm, d, true, n64, plan.tile_rows, plan.piece);
+            if (rc != QFMT_OK) return rc;
+            p.K = (int)s.rows;
+            p.dyn = p16::kCountK;
+            p.kb_per_split = (int)(up(s.rows, p16::kStageK) / p16::kStageK);
+            T* out = static_cast<T*>(d_dw) + (s.stored_words ? first * ld_dw : first);
+            typename ScaledEpilogue<T>::Params se = {&found->unscale, out, ld_dw, whole(out, ld_dw, 2)};
+            if (s.stored_words) {
+                p.M = (int)n;
+                p.N = (int)s.hidden;
+                p.alt = p16::kAltB;
+                rc = p16::launch_product<ScaledEpilogue<T>>(dm, h_k, &h_k_alt, p, se, dev, stream);
+            } else {
+                p.M = (int)s.hidden;
+                p.N = (int)n;
+                p.alt = p16::kAltA;
+                rc = p16::launch_product<ScaledEpilogue<T>>(h_k, dm, &h_k_alt, p, se, dev, stream);
+            }
+            if (rc != QFMT_OK) return rc;
+        }
+        if (d_dh != nullptr) {
+            rc = p16::make_operand(&dk, d, false, plan.tile_rows, n64, plan.piece);
+            if (rc != QFMT_OK) return rc;
+            rc = word_operand(&w, W, s, false, first, n);
+            if (rc != QFMT_OK) return rc;
+            p.M = (int)s.rows;
+            p.N = (int)s.hidden;
+            p.K = (int)n;
+            p.dyn = p16::kCountM;
+            p.alt = p16::kAltNone;
+            p.splits = plan.splits;
+            const int stages = (int)(up(n, p16::kStageK) / p16::kStageK);
+            p.kb_per_split = (stages + plan.splits - 1) / plan.splits;  // a short last piece leaves some splits without work: they add zeros
+            typename AddEpilogue::Params ae = {sums, plan.pitch_h, s.rows * plan.pitch_h, first > 0 ? 1 : 0};
+            rc = p16::launch_product<AddEpilogue>(dk, w, nullptr, p, ae, dev, stream);
+            if (rc != QFMT_OK) return rc;
+        }
+    }
+    if (d_dh != nullptr) {
+        const int64_t want = (s.rows + 7) / 8, most = (int64_t)dev.sm_count * 8;
+        QFMT_CUDA_TRY(launch_overlapping(scatter_kernel<T>, (unsigned)(want < most ? want : most), 256u, 0, stream, (const float*)sums, plan.splits,
+                                         s.rows * plan.pitch_h, plan.pitch_h, found, (const int*)at<int>(ws, pl.index), static_cast<T*>(d_dh),
+                                         ld_dh, (int)s.hidden, (int)(!misaligned(d_dh, 8) && ld_dh % 4 == 0)));
+    }
+    return QFMT_OK;
+}
+
+}  // namespace
+}  // namespace qfmt
+
+extern "C" size_t qfmt_linear_cross_entropy_workspace_bytes(const qfmt_matrix16_t* H, const qfmt_matrix16_t* W, int backward) {
+    qfmt::Sizes s;
+    if (qfmt::loss_sizes(H, W, &s) != QFMT_OK) return 0;
+    return qfmt::places(s, qfmt::plan_backward(s), backward != 0).total;
+}
+
+extern "C" int qfmt_linear_cross_entropy(const qfmt_matrix16_t* H, const qfmt_matrix16_t* W, const qfmt_cross_entropy_t* kind,
+                                         const float* d_bias, const int64_t* d_targets, float* d_loss, float* d_lse, float* d_mean,
+                                         void* d_workspace, size_t workspace_bytes, void* stream) {
+    using namespace qfmt;
+    Sizes s;
+    int rc = check_loss(H, W, kind, d_bias, d_targets, d_workspace, workspace_bytes, false, &s);
+    if (rc != QFMT_OK) return rc;
+    if (misaligned(d_loss, 4) || misaligned(d_lse, 4) || misaligned(d_mean, 4)) return QFMT_ERR_BAD_ARG;
+    DeviceInfo dev;
+    rc = current_device(&dev);
+    if (rc != QFMT_OK) return rc;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (s.rows == 0) {
+        if (d_mean != nullptr) QFMT_CUDA_TRY(cudaMemsetAsync(d_mean, 0, sizeof(float), st));
+        return QFMT_OK;
+    }
+    const Plan plan = plan_backward(s);
+    const Places pl = places(s, plan, false);
+    p16::Operand h, alt, w;
+    rc = p16::make_operand(&h, at<uint16_t>(d_workspace, pl.compact_h), false, up(s.rows, 64), s.hidden, plan.pitch_h);
+    if (rc != QFMT_OK) return rc;
+    rc = p16::make_operand(&alt, H->ptr, false, s.rows, s.hidden, H->ld);
+    if (rc != QFMT_OK) return rc;
+    rc = word_operand(&w, W, s, true, 0, s.vocab);
+    if (rc != QFMT_OK) return rc;
+    Compact c = compact_args(H, kind, d_targets, s, plan, pl, d_workspace);
+    c.loss = d_loss;
+    c.lse_out = d_lse;
+    p16::ProductParams p = {};
+    p.M = (int)s.rows;
+    p.N = (int)s.vocab;
+    p.K = (int)s.hidden;
+    p.count = &c.found->count;
+    p.dyn = p16::kCountM;
+    p.alt = p16::kAltA;
+    p.alt_rows = (int)s.rows;
+    p.bf16 = kind->dtype == QFMT_BF16;
+    p.splits = 1;
+    p.kb_per_split = (int)(up(s.hidden, p16::kStageK) / p16::kStageK);
+    p.status = static_cast<unsigned long long*>(d_workspace);
+    p.tag = next_launch_tag();
+    rc = launch_compact<false>(c, p, dev, st);
+    if (rc != QFMT_OK) return rc;
+    typename RowSumEpilogue::Params re = {d_bias, c.target, at<float2>(d_workspace, pl.parts), at<float>(d_workspace, pl.picked), s.rows};
+    rc = p16::launch_product<RowSumEpilogue>(h, w, &alt, p, re, dev, st);
+    if (rc != QFMT_OK) return rc;
+    const unsigned blocks = (unsigned)((s.rows + kJoinRows - 1) / kJoinRows);
+    float* compact_loss = d_mean != nullptr && blocks > 1 ? at<float>(d_workspace, pl.compact_loss) : nullptr;
+    QFMT_CUDA_TRY(launch_overlapping(join_rows_kernel, blocks, (unsigned)(kJoinRows * kJoinParts), 0, st, (const float2*)re.parts, s.rows,
+                                     (int)(up(s.vocab, 128) / 128), (const Found*)c.found, (const int*)c.index, (const int*)c.target,
+                                     (const float*)re.picked, d_loss, d_lse, compact_loss, blocks == 1 ? d_mean : (float*)nullptr));
+    if (compact_loss != nullptr)
+        QFMT_CUDA_TRY(launch_overlapping(mean_kernel, 1u, 1024u, 0, st, (const float*)compact_loss, (const Found*)c.found, d_mean));
+    return QFMT_OK;
+}
+
+extern "C" int qfmt_linear_cross_entropy_backward(const qfmt_matrix16_t* H, const qfmt_matrix16_t* W, const qfmt_cross_entropy_t* kind,
+                                                  const float* d_bias, const int64_t* d_targets, const float* d_lse, const float* d_dloss,
+                                                  const qfmt_dls_t* d_dls, void* d_dh, int64_t ld_dh, void* d_dw, int64_t ld_dw,
+                                                  float* d_dbias, void* d_workspace, size_t workspace_bytes, void* stream) {
+    using namespace qfmt;
+    Sizes s;
+    int rc = check_loss(H, W, kind, d_bias, d_targets, d_workspace, workspace_bytes, true, &s);
+    if (rc != QFMT_OK) return rc;
+    if (misaligned(d_lse, 4) || misaligned(d_dloss, 4) || misaligned(d_dls, 8) || misaligned(d_dh, 2) || misaligned(d_dw, 2) ||
+        misaligned(d_dbias, 4))
+        return QFMT_ERR_BAD_ARG;
+    if (s.rows > 0 && d_lse == nullptr) return QFMT_ERR_BAD_ARG;
+    if ((d_dh != nullptr && ld_dh < s.hidden) || (d_dw != nullptr && ld_dw < W->cols)) return QFMT_ERR_BAD_ARG;
+    DeviceInfo dev;
+    rc = current_device(&dev);
+    if (rc != QFMT_OK) return rc;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (s.rows == 0) {
+        if (d_dw != nullptr) QFMT_CUDA_TRY(cudaMemset2DAsync(d_dw, (size_t)ld_dw * 2, 0, (size_t)W->cols * 2, (size_t)W->rows, st));
+        if (d_dbias != nullptr) QFMT_CUDA_TRY(cudaMemsetAsync(d_dbias, 0, (size_t)s.vocab * sizeof(float), st));
+        return QFMT_OK;
+    }
+    const Plan plan = plan_backward(s);
+    const Places pl = places(s, plan, true);
+    // H as rows of the logits' product and as the K of the weight's, in the compact copy or in place
+    p16::Operand h_rows, h_rows_alt, h_k, h_k_alt;
+    const uint16_t* copy = at<uint16_t>(d_workspace, pl.compact_h);
+    rc = p16::make_operand(&h_rows, copy, false, up(s.rows, 64), s.hidden, plan.pitch_h);
+    if (rc == QFMT_OK) rc = p16::make_operand(&h_rows_alt, H->ptr, false, s.rows, s.hidden, H->ld);
+    if (rc == QFMT_OK) rc = p16::make_operand(&h_k, copy, true, s.hidden, up(s.rows, 64), plan.pitch_h);
+    if (rc == QFMT_OK) rc = p16::make_operand(&h_k_alt, H->ptr, true, s.hidden, s.rows, H->ld);
+    if (rc != QFMT_OK) return rc;
+    Compact c = compact_args(H, kind, d_targets, s, plan, pl, d_workspace);
+    c.lse = d_lse;
+    c.dloss = d_dloss;
+    c.dls = d_dls;
+    c.lse_of = at<float>(d_workspace, pl.lse_of);
+    c.g = at<float>(d_workspace, pl.g);
+    c.dh = static_cast<uint16_t*>(d_dh);
+    c.ld_dh = ld_dh;
+    p16::ProductParams p = {};
+    p.count = &c.found->count;
+    p.alt_rows = (int)s.rows;
+    p.bf16 = kind->dtype == QFMT_BF16;
+    p.status = static_cast<unsigned long long*>(d_workspace);
+    p.tag = next_launch_tag();
+    rc = launch_compact<true>(c, p, dev, st);
+    if (rc != QFMT_OK) return rc;
+    if (kind->dtype == QFMT_F16)
+        return backward_pieces<__half>(W, d_bias, s, plan, pl, d_workspace, h_rows, h_rows_alt, h_k, h_k_alt, p, d_dh, ld_dh, d_dw, ld_dw,
+                                       d_dbias, dev, st);
+    return backward_pieces<__nv_bfloat16>(W, d_bias, s, plan, pl, d_workspace, h_rows, h_rows_alt, h_k, h_k_alt, p, d_dh, ld_dh, d_dw, ld_dw,
+                                          d_dbias, dev, st);
+}

@@ -1,0 +1,654 @@
+// Products of 16-bit codes with bias, activation and residual in the epilogue, their backward pass, and the pass over a gradient
+// that is there already:
+//     z = X W + bias,  y = act(z) + residual;      dz = (dY W^T + residual) act'(z),  dbias = column sums of dz.
+// Formulas: activation.cuh; the product's frame: product16.cuh.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "activation.cuh"
+#include "columns.cuh"
+#include "common.cuh"
+#include "product16.cuh"
+
+namespace qfmt {
+namespace {
+
+using p16::Patch;
+
+struct Nothing {};
+
+// ---- epilogues of the product -------------------------------------------------------------------------------------------
+
+template <typename T, int kAct>
+struct ForwardEpilogue {
+    struct Params {
+        const float* bias;
+        const T* residual;
+        T *z, *y;
+        int64_t ld_residual, ld_z, ld_y;
+        int vec_residual, vec_z, vec_y;
+    };
+    using Ahead = Nothing;
+    static __device__ __forceinline__ void before(const Patch& p, const Params& e, Ahead&) { p.load_columns(e.bias); }
+    template <typename F>
+    static __device__ __forceinline__ void run(const Patch& p, const Params& e, Ahead&, F release) {
+#pragma unroll 1
+        for (int c = 0; c < 2; ++c) {
+            const int col0 = p.col0 + c * 64;
+            float v[64];
+            {
+                uint32_t a[32], b[32];
+                p.load32(c * 2, a);
+                p.load32(c * 2 + 1, b);
+                p.wait();
+                if (c == 1) release();
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    v[j] = __fadd_rn(__uint_as_float(a[j]), p.col[c * 64 + j]);
+                    v[32 + j] = __fadd_rn(__uint_as_float(b[j]), p.col[c * 64 + 32 + j]);
+                }
+            }
+            if (col0 >= p.cols || p.row0 >= p.rows) continue;
+            if (e.z != nullptr) {
+                p16::box_put_codes<T>(p.box, p.lane, v);
+                __syncwarp();
+                p16::box_store<T>(p.box, e.z, e.ld_z, p.row0, p.rows, col0, p.cols, p.lane, e.vec_z != 0);
+                __syncwarp();
+            }
+#pragma unroll
+            for (int j = 0; j < 64; ++j) v[j] = activate<kAct, false>(v[j]);
+            if (e.residual != nullptr) {
+                p16::box_load<T>(p.box, e.residual, e.ld_residual, p.row0, p.rows, col0, p.cols, p.lane, e.vec_residual != 0);
+                __syncwarp();
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const uint4 w = *p16::box_at(p.box, p.lane, k);
+                    const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float2 r = p16::unpack_codes<T>(words[j]);
+                        v[k * 8 + 2 * j] = __fadd_rn(v[k * 8 + 2 * j], r.x);
+                        v[k * 8 + 2 * j + 1] = __fadd_rn(v[k * 8 + 2 * j + 1], r.y);
+                    }
+                }
+                __syncwarp();
+            }
+            p16::box_put_codes<T>(p.box, p.lane, v);
+            __syncwarp();
+            p16::box_store<T>(p.box, e.y, e.ld_y, p.row0, p.rows, col0, p.cols, p.lane, e.vec_y != 0);
+            __syncwarp();
+        }
+    }
+};
+
+template <typename T, int kAct>
+struct BackwardEpilogue {
+    struct Params {
+        const T *residual, *z;
+        T* dz;
+        float* parts;  // [32-row groups][pitch] column sums, or null
+        int64_t ld_residual, ld_z, ld_dz, pitch;
+        int vec_residual, vec_z, vec_dz;
+    };
+    using Ahead = Nothing;
+    static __device__ __forceinline__ void before(const Patch&, const Params&, Ahead&) {}
+    template <typename F>
+    static __device__ __forceinline__ void run(const Patch& p, const Params& e, Ahead&, F release) {
+#pragma unroll 1
+        for (int c = 0; c < 2; ++c) {
+            const int col0 = p.col0 + c * 64;
+            float v[64];
+            {
+                uint32_t a[32], b[32];
+                p.load32(c * 2, a);
+                p.load32(c * 2 + 1, b);
+                p.wait();
+                if (c == 1) release();
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    v[j] = __uint_as_float(a[j]);
+                    v[32 + j] = __uint_as_float(b[j]);
+                }
+            }
+            if (col0 >= p.cols) continue;
+            if (e.residual != nullptr) {
+                p16::box_load<T>(p.box, e.residual, e.ld_residual, p.row0, p.rows, col0, p.cols, p.lane, e.vec_residual != 0);
+                __syncwarp();
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const uint4 w = *p16::box_at(p.box, p.lane, k);
+                    const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float2 r = p16::unpack_codes<T>(words[j]);
+                        v[k * 8 + 2 * j] = __fadd_rn(v[k * 8 + 2 * j], r.x);
+                        v[k * 8 + 2 * j + 1] = __fadd_rn(v[k * 8 + 2 * j + 1], r.y);
+                    }
+                }
+                __syncwarp();
+            }
+            if (kAct != QFMT_ACT_NONE) {
+                p16::box_load<T>(p.box, e.z, e.ld_z, p.row0, p.rows, col0, p.cols, p.lane, e.vec_z != 0);
+                __syncwarp();
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const uint4 w = *p16::box_at(p.box, p.lane, k);
+                    const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float2 r = p16::unpack_codes<T>(words[j]);
+                        v[k * 8 + 2 * j] = __fmul_rn(v[k * 8 + 2 * j], activation_slope<kAct, false>(r.x));
+                        v[k * 8 + 2 * j + 1] = __fmul_rn(v[k * 8 + 2 * j + 1], activation_slope<kAct, false>(r.y));
+                    }
+                }
+                __syncwarp();
+            }
+            p16::box_put_codes<T>(p.box, p.lane, v);
+            __syncwarp();
+            p16::box_store<T>(p.box, e.dz, e.ld_dz, p.row0, p.rows, col0, p.cols, p.lane, e.vec_dz != 0);
+            __syncwarp();
+            if (e.parts != nullptr) {
+                // rows beyond the matrix: sums and residual are zero there, and so is dz
+                float* out = e.parts + (int64_t)(p.row0 >> 5) * e.pitch + col0 + p.lane;
+                float lo[32], hi[32];
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    lo[j] = v[j];
+                    hi[j] = v[32 + j];
+                }
+                const float s0 = p16::column_sum(lo, p.lane), s1 = p16::column_sum(hi, p.lane);
+                if (col0 + p.lane < p.cols) out[0] = s0;
+                if (col0 + 32 + p.lane < p.cols) out[32] = s1;
+            }
+        }
+    }
+};
+
+// Sums as they are, in fp32, to [split][M][pitch]: products of few tiles whose K is shared.
+struct PartEpilogue {
+    struct Params {
+        float* parts;
+        int64_t pitch, split_stride;
+    };
+    using Ahead = Nothing;
+    static __device__ __forceinline__ void before(const Patch&, const Params&, Ahead&) {}
+    template <typename F>
+    static __device__ __forceinline__ void run(const Patch& p, const Params& e, Ahead&, F release) {
+        float* base = e.parts + (int64_t)p.split * e.split_stride;
+#pragma unroll 1
+        for (int c = 0; c < 4; ++c) {
+            uint32_t a[32];
+            p.load32(c, a);
+            p.wait();
+            if (c == 3) release();
+            if (p.row0 >= p.rows || p.col0 + c * 32 >= p.cols) continue;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) *p16::box_at(p.box, p.lane, k) = make_uint4(a[4 * k], a[4 * k + 1], a[4 * k + 2], a[4 * k + 3]);
+            __syncwarp();
+            p16::box_store<float>(p.box, base, e.pitch, p.row0, p.rows, p.col0 + c * 32, p.cols, p.lane, true);
+            __syncwarp();
+        }
+    }
+};
+
+// ---- the pass over rows -------------------------------------------------------------------------------------------------
+// Finishes a product whose K was shared (kParts: the source is [splits][rows][pitch] fp32) or works on a gradient that is in
+// memory.  A block has a strip of 256 columns and a range of rows, a warp a row at a time and a lane eight columns of it: whole
+// 16-byte pieces (32 bytes of containers) if everything is aligned (kVec), else every 32nd element so that accesses still join.
+// Column sums stay in registers down the rows and are joined across the block's eight warps, then across blocks by
+// join_columns_kernel.  Bound by memory: with two tensors read and one written 8192 x 4096 bfloat16 moves 201 MB.
+struct RowPass {
+    const float* parts;
+    int splits;
+    int64_t split_stride, pitch;       // pitch of the fp32 sources, and of the column sums
+    const void *dy, *residual, *z_in;
+    void *out, *z_out;
+    const float* bias;
+    float* sums;                       // [row blocks][pitch], or null
+    int64_t ld_dy, ld_residual, ld_z, ld_out;
+    int64_t rows, cols;
+    int strips;
+    int64_t rows_per_block;
+};
+
+template <typename T, bool kVec>
+__device__ __forceinline__ int64_t pass_col(int lane, int k) { return kVec ? lane * 8 + k : k * 32 + lane; }
+
+template <typename T, bool kVec>
+__device__ __forceinline__ void pass_load(const T* base, int64_t ld, int64_t row, int64_t col0, int64_t cols, int lane, float (&v)[8]) {
+    if (kVec) {
+        const T* p = base + row * ld + col0 + lane * 8;
+        if (col0 + lane * 8 >= cols) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = 0.0f;
+        } else if (sizeof(T) == 4) {
+            const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+            v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        } else {
+            const uint4 w = *reinterpret_cast<const uint4*>(p);
+            const T* e = reinterpret_cast<const T*>(&w);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = (float)e[k];
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int64_t col = col0 + k * 32 + lane;
+            v[k] = col < cols ? (float)base[row * ld + col] : 0.0f;
+        }
+    }
+}
+__device__ __forceinline__ float to_type(float v, float) { return v; }
+__device__ __forceinline__ __half to_type(float v, __half) { return __float2half_rn(v); }
+__device__ __forceinline__ __nv_bfloat16 to_type(float v, __nv_bfloat16) { return __float2bfloat16_rn(v); }
+
+template <typename T, bool kVec>
+__device__ __forceinline__ void pass_store(T* base, int64_t ld, int64_t row, int64_t col0, int64_t cols, int lane, const float (&v)[8]) {
+    if (kVec) {
+        T* p = base + row * ld + col0 + lane * 8;
+        if (col0 + lane * 8 >= cols) return;
+        if (sizeof(T) == 4) {
+            reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+            reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+        } else {
+            uint4 w;
+            T* e = reinterpret_cast<T*>(&w);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) e[k] = to_type(v[k], T());
+            *reinterpret_cast<uint4*>(p) = w;
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int64_t col = col0 + k * 32 + lane;
+            if (col < cols) base[row * ld + col] = to_type(v[k], T());
+        }
+    }
+}
+
+constexpr int kPassWarps = 8;
+
+template <typename T, int kAct, bool kBackward, bool kParts, bool kVec>
+__global__ void __launch_bounds__(kPassWarps * 32)
+row_pass_kernel(const RowPass a) {
+    constexpr bool kPrecise = sizeof(T) == 4;
+    __shared__ float sums[kPassWarps][256];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t col0 = (int64_t)(blockIdx.x % a.strips) * 256;
+    const int64_t block = blockIdx.x / a.strips, first = block * a.rows_per_block;
+    const int64_t end = first + a.rows_per_block < a.rows ? first + a.rows_per_block : a.rows;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    float bias[8], total[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int64_t col = col0 + pass_col<T, kVec>(lane, k);
+        bias[k] = !kBackward && a.bias != nullptr && col < a.cols ? a.bias[col] : 0.0f;
+        total[k] = 0.0f;
+    }
+    const T *dy = static_cast<const T*>(a.dy), *residual = static_cast<const T*>(a.residual), *z_in = static_cast<const T*>(a.z_in);
+    T *out = static_cast<T*>(a.out), *z_out = static_cast<T*>(a.z_out);
+#pragma unroll 2
+    for (int64_t row = first + warp; row < end; row += kPassWarps) {
+        float v[8], z[8], r[8];
+        if (kBackward && kAct != QFMT_ACT_NONE) pass_load<T, kVec>(z_in, a.ld_z, row, col0, a.cols, lane, z);
+        if constexpr (kParts) {
+            pass_load<float, kVec>(a.parts, a.pitch, row, col0, a.cols, lane, v);
+            for (int s = 1; s < a.splits; ++s) {
+                float w[8];
+                pass_load<float, kVec>(a.parts + s * a.split_stride, a.pitch, row, col0, a.cols, lane, w);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = __fadd_rn(v[k], w[k]);
+            }
+        } else {
+            pass_load<T, kVec>(dy, a.ld_dy, row, col0, a.cols, lane, v);
+        }
+        if (residual != nullptr) pass_load<T, kVec>(residual, a.ld_residual, row, col0, a.cols, lane, r);
+        if (kBackward) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                if (residual != nullptr) v[k] = __fadd_rn(v[k], r[k]);
+                if (kAct != QFMT_ACT_NONE) v[k] = __fmul_rn(v[k], activation_slope<kAct, kPrecise>(z[k]));
+                total[k] = __fadd_rn(total[k], v[k]);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = __fadd_rn(v[k], bias[k]);
+            if (z_out != nullptr) pass_store<T, kVec>(z_out, a.ld_z, row, col0, a.cols, lane, v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                v[k] = activate<kAct, kPrecise>(v[k]);
+                if (residual != nullptr) v[k] = __fadd_rn(v[k], r[k]);
+            }
+        }
+        if (out != nullptr) pass_store<T, kVec>(out, a.ld_out, row, col0, a.cols, lane, v);
+    }
+    if constexpr (kBackward) {
+        if (a.sums == nullptr) return;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sums[warp][pass_col<T, kVec>(lane, k)] = total[k];
+        __syncthreads();
+        const int64_t col = col0 + threadIdx.x;
+        if (col < a.cols) {
+            float s = sums[0][threadIdx.x];
+            for (int w = 1; w < kPassWarps; ++w) s = __fadd_rn(s, sums[w][threadIdx.x]);
+            a.sums[block * a.pitch + col] = s;
+        }
+    }
+}
+
+// ---- host side ----------------------------------------------------------------------------------------------------------
+
+// Columns of fp32 working matrices are padded so that rows start on 32 bytes.
+int64_t padded(int64_t cols) { return (cols + 7) / 8 * 8; }
+
+// Blocks of rows of a pass: enough blocks to fill the GPU a few times over, none of fewer than 32 rows (four a warp).
+constexpr int64_t kPassBlocks = 148 * 6;
+int64_t pass_row_blocks(int64_t rows, int64_t cols) {
+    const int64_t strips = (cols + 255) / 256, want = (kPassBlocks + strips - 1) / strips, most = (rows + 31) / 32;
+    return want < most ? want : most;
+}
+
+template <typename T, int kAct, bool kBackward, bool kParts>
+int launch_row_pass(RowPass a, bool vec, cudaStream_t stream) {
+    a.strips = (int)((a.cols + 255) / 256);
+    const int64_t blocks = pass_row_blocks(a.rows, a.cols);
+    a.rows_per_block = (a.rows + blocks - 1) / blocks;
+    const unsigned grid = (unsigned)(a.strips * ((a.rows + a.rows_per_block - 1) / a.rows_per_block));
+    if (vec) QFMT_CUDA_TRY(launch_overlapping(row_pass_kernel<T, kAct, kBackward, kParts, true>, grid, kPassWarps * 32u, 0, stream, a));
+    else QFMT_CUDA_TRY(launch_overlapping(row_pass_kernel<T, kAct, kBackward, kParts, false>, grid, kPassWarps * 32u, 0, stream, a));
+    return QFMT_OK;
+}
+
+bool misaligned(const void* p, uintptr_t size) { return (reinterpret_cast<uintptr_t>(p) & (size - 1)) != 0; }
+// Whether rows can be moved in 16-byte pieces.
+bool whole(const void* p, int64_t ld, int64_t size) { return p == nullptr || (!misaligned(p, 16) && (ld * size) % 16 == 0); }
+
+struct Shape {
+    int64_t M, N, K;
+};
+int product_shape(const qfmt_matrix16_t* A, const qfmt_matrix16_t* B, Shape* s) {
+    if (A == nullptr || B == nullptr) return QFMT_ERR_BAD_ARG;
+    if (A->rows < 0 || A->cols < 0 || B->rows < 0 || B->cols < 0) return QFMT_ERR_BAD_ARG;
+    s->M = A->trans ? A->cols : A->rows;
+    s->K = A->trans ? A->rows : A->cols;
+    s->N = B->trans ? B->rows : B->cols;
+    if (s->K != (B->trans ? B->cols : B->rows)) return QFMT_ERR_BAD_ARG;
+    if (s->M > (1 << 30) || s->N > (1 << 30) || s->K > (1 << 30)) return QFMT_ERR_BAD_ARG;
+    const int64_t tiles = ((s->M + p16::kTileM - 1) / p16::kTileM) * ((s->N + p16::kTileN - 1) / p16::kTileN);
+    if (tiles > (1 << 26)) return QFMT_ERR_BAD_ARG;  // work items are counted in 32 bits
+    return QFMT_OK;
+}
+
+// A product of fewer tiles than CTA pairs shares its K among them, in pieces of at least four stages (256 elements): shorter
+// ones would cost more in moving fp32 sums than they save.
+constexpr int64_t kPairs = 74, kMostSplits = 16, kLeastStages = 4;
+int plan_splits(const Shape& s) {
+    const int64_t tiles = ((s.M + p16::kTileM - 1) / p16::kTileM) * ((s.N + p16::kTileN - 1) / p16::kTileN);
+    const int64_t stages = (s.K + p16::kStageK - 1) / p16::kStageK;
+    if (tiles == 0) return 1;
+    int64_t n = kPairs / tiles;
+    if (n > stages / kLeastStages) n = stages / kLeastStages;
+    if (n > kMostSplits) n = kMostSplits;
+    return n < 2 ? 1 : (int)n;
+}
+
+constexpr size_t kHeader = 256;
+size_t sums_bytes(const Shape& s) {  // column sums by groups of 32 rows of whole tiles: more than a pass over rows leaves
+    return (size_t)((s.M + p16::kTileM - 1) / p16::kTileM) * 8 * (size_t)padded(s.N) * sizeof(float);
+}
+size_t part_bytes(const Shape& s, int splits) { return (size_t)splits * (size_t)s.M * (size_t)padded(s.N) * sizeof(float); }
+
+struct Call {
+    Shape s;
+    int act;
+    int64_t ld_residual, ld_z;
+    DeviceInfo dev;
+    p16::Operand a, b;
+    p16::ProductParams p;
+    int splits;
+    float *sums, *parts;
+};
+
+// Everything the two directions check and set up alike.  On QFMT_OK with *work false there is nothing to compute.
+int prepare_call(Call* c, bool backward, const qfmt_matrix16_t* A, const qfmt_matrix16_t* B, const qfmt_epilogue_t* e, const void* d_out, int64_t ld_out,
+                 const float* d_dbias, int32_t dtype, void* d_workspace, size_t workspace_bytes, bool* work) {
+    *work = false;
+    int rc = product_shape(A, B, &c->s);
+    if (rc != QFMT_OK) return rc;
+    const Shape& s = c->s;
+    if (e == nullptr || (dtype != QFMT_F16 && dtype != QFMT_BF16)) return QFMT_ERR_BAD_ARG;
+    if (e->act < QFMT_ACT_NONE || e->act > QFMT_ACT_SILU) return QFMT_ERR_BAD_ARG;
+    c->act = e->act;
+    c->ld_residual = e->ld_residual == 0 ? s.N : e->ld_residual;
+    c->ld_z = e->ld_z == 0 ? s.N : e->ld_z;
+    if (A->ld < A->cols || B->ld < B->cols || ld_out < s.N || c->ld_residual < s.N || c->ld_z < s.N) return QFMT_ERR_BAD_ARG;
+    if (misaligned(e->d_bias, 4) || misaligned(e->d_residual, 2) || misaligned(e->d_z, 2) || misaligned(d_out, 2) || misaligned(d_dbias, 4))
+        return QFMT_ERR_BAD_ARG;
+    if (d_workspace == nullptr || misaligned(d_workspace, 16) || workspace_bytes < kHeader) return QFMT_ERR_BAD_ARG;
+    const size_t sums = d_dbias != nullptr ? sums_bytes(s) : 0;
+    if (workspace_bytes < kHeader + sums) return QFMT_ERR_BAD_ARG;
+    if (s.M == 0 || s.N == 0) return QFMT_OK;
+    if (d_out == nullptr || (backward && e->act != QFMT_ACT_NONE && e->d_z == nullptr)) return QFMT_ERR_BAD_ARG;
+    if (s.K != 0) {
+        if (A->ptr == nullptr || B->ptr == nullptr || misaligned(A->ptr, 16) || misaligned(B->ptr, 16) || (A->ld & 7) || (B->ld & 7))
+            return QFMT_ERR_BAD_ARG;  // TMA: 16-byte aligned bases and row pitches
+    }
+    rc = current_device(&c->dev);
+    if (rc != QFMT_OK) return rc;
+    c->a = p16::Operand{};
+    c->b = p16::Operand{};
+    if (s.K != 0) {
+        rc = p16::make_operand(&c->a, A->ptr, A->trans != 0, s.M, s.K, A->ld);
+        if (rc != QFMT_OK) return rc;
+        rc = p16::make_operand(&c->b, B->ptr, B->trans == 0, s.N, s.K, B->ld);
+        if (rc != QFMT_OK) return rc;
+    }
+    c->splits = plan_splits(s);
+    while (c->splits > 1 && kHeader + sums + part_bytes(s, c->splits) > workspace_bytes) --c->splits;
+    const int stages = (int)((s.K + p16::kStageK - 1) / p16::kStageK);
+    p16::ProductParams& p = c->p;
+    p = p16::ProductParams{};
+    p.M = (int)s.M;
+    p.N = (int)s.N;
+    p.K = (int)s.K;
+    p.bf16 = dtype == QFMT_BF16;
+    p.kb_per_split = (stages + c->splits - 1) / c->splits;
+    if (c->splits > 1) c->splits = (stages + p.kb_per_split - 1) / p.kb_per_split;
+    p.splits = c->splits;
+    p.status = static_cast<unsigned long long*>(d_workspace);
+    p.tag = next_launch_tag();
+    c->sums = reinterpret_cast<float*>(static_cast<char*>(d_workspace) + kHeader);
+    c->parts = reinterpret_cast<float*>(static_cast<char*>(d_workspace) + kHeader + sums);
+    *work = true;
+    return QFMT_OK;
+}
+
+int launch_parts(const Call& c, RowPass* a, cudaStream_t stream) {
+    typename PartEpilogue::Params pe = {c.parts, padded(c.s.N), c.s.M * padded(c.s.N)};
+    *a = RowPass{};
+    a->parts = c.parts;
+    a->splits = c.splits;
+    a->split_stride = pe.split_stride;
+    a->pitch = pe.pitch;
+    a->rows = c.s.M;
+    a->cols = c.s.N;
+    return p16::launch_product<PartEpilogue>(c.a, c.b, nullptr, c.p, pe, c.dev, stream);
+}
+
+template <typename T, int kAct>
+int forward_call(const Call& c, const qfmt_epilogue_t* e, void* d_y, int64_t ldy, cudaStream_t stream) {
+    const bool vr = whole(e->d_residual, c.ld_residual, 2), vz = whole(e->d_z, c.ld_z, 2), vy = whole(d_y, ldy, 2);
+    if (c.splits > 1) {
+        RowPass a;
+        const int rc = launch_parts(c, &a, stream);
+        if (rc != QFMT_OK) return rc;
+        a.bias = e->d_bias;
+        a.residual = e->d_residual;
+        a.ld_residual = c.ld_residual;
+        a.z_out = e->d_z;
+        a.ld_z = c.ld_z;
+        a.out = d_y;
+        a.ld_out = ldy;
+        return launch_row_pass<T, kAct, false, true>(a, vr && vz && vy && c.s.N % 8 == 0, stream);
+    }
+    using Epi = ForwardEpilogue<T, kAct>;
+    typename Epi::Params ep = {e->d_bias, static_cast<const T*>(e->d_residual), static_cast<T*>(e->d_z), static_cast<T*>(d_y),
+                               c.ld_residual, c.ld_z, ldy, vr, vz, vy};
+    return p16::launch_product<Epi>(c.a, c.b, nullptr, c.p, ep, c.dev, stream);
+}
+
+template <typename T, int kAct>
+int backward_call(const Call& c, const qfmt_epilogue_t* e, void* d_dz, int64_t ld_dz, float* d_dbias, cudaStream_t stream) {
+    const bool vr = whole(e->d_residual, c.ld_residual, 2), vz = whole(e->d_z, c.ld_z, 2), vd = whole(d_dz, ld_dz, 2);
+    const int64_t pitch = padded(c.s.N);
+    int64_t n_parts = (c.s.M + p16::kTileM - 1) / p16::kTileM * 8;
+    int rc;
+    if (c.splits > 1) {
+        RowPass a;
+        rc = launch_parts(c, &a, stream);
+        if (rc != QFMT_OK) return rc;
+        a.residual = e->d_residual;
+        a.ld_residual = c.ld_residual;
+        a.z_in = e->d_z;
+        a.ld_z = c.ld_z;
+        a.out = d_dz;
+        a.ld_out = ld_dz;
+        a.sums = d_dbias != nullptr ? c.sums : nullptr;
+        rc = launch_row_pass<T, kAct, true, true>(a, vr && vz && vd && c.s.N % 8 == 0, stream);
+        const int64_t blocks = pass_row_blocks(c.s.M, c.s.N), per = (c.s.M + blocks - 1) / blocks;
+        n_parts = (c.s.M + per - 1) / per;
+    } else {
+        using Epi = BackwardEpilogue<T, kAct>;
+        typename Epi::Params ep = {static_cast<const T*>(e->d_residual), static_cast<const T*>(e->d_z), static_cast<T*>(d_dz),
+                                   d_dbias != nullptr ? c.sums : nullptr, c.ld_residual, c.ld_z, ld_dz, pitch, vr, vz, vd};
+        rc = p16::launch_product<Epi>(c.a, c.b, nullptr, c.p, ep, c.dev, stream);
+    }
+    if (rc != QFMT_OK || d_dbias == nullptr) return rc;
+    return launch_join_columns(c.sums, pitch, n_parts, nullptr, nullptr, d_dbias, c.s.N, stream);
+}
+
+template <typename T, int kAct>
+int act_backward_call(RowPass a, bool vec, float* d_dbias, cudaStream_t stream) {
+    int rc = launch_row_pass<T, kAct, true, false>(a, vec, stream);
+    if (rc != QFMT_OK || d_dbias == nullptr) return rc;
+    const int64_t blocks = pass_row_blocks(a.rows, a.cols), per = (a.rows + blocks - 1) / blocks;
+    return launch_join_columns(a.sums, a.pitch, (a.rows + per - 1) / per, nullptr, nullptr, d_dbias, a.cols, stream);
+}
+
+#define BY_ACT(act, call)                                              \
+    switch (act) {                                                     \
+        case QFMT_ACT_RELU: { constexpr int kA = QFMT_ACT_RELU; return call; }         \
+        case QFMT_ACT_GELU: { constexpr int kA = QFMT_ACT_GELU; return call; }         \
+        case QFMT_ACT_GELU_TANH: { constexpr int kA = QFMT_ACT_GELU_TANH; return call; } \
+        case QFMT_ACT_SILU: { constexpr int kA = QFMT_ACT_SILU; return call; }         \
+        default: { constexpr int kA = QFMT_ACT_NONE; return call; }    \
+    }
+
+template <typename T>
+int forward_typed(const Call& c, const qfmt_epilogue_t* e, void* d_y, int64_t ldy, cudaStream_t stream) {
+    BY_ACT(c.act, (forward_call<T, kA>(c, e, d_y, ldy, stream)))
+}
+template <typename T>
+int backward_typed(const Call& c, const qfmt_epilogue_t* e, void* d_dz, int64_t ld_dz, float* d_dbias, cudaStream_t stream) {
+    BY_ACT(c.act, (backward_call<T, kA>(c, e, d_dz, ld_dz, d_dbias, stream)))
+}
+template <typename T>
+int act_backward_typed(int act, const RowPass& a, bool vec, float* d_dbias, cudaStream_t stream) {
+    BY_ACT(act, (act_backward_call<T, kA>(a, vec, d_dbias, stream)))
+}
+
+}  // namespace
+}  // namespace qfmt
+
+extern "C" size_t qfmt_linear_act_workspace_bytes(const qfmt_matrix16_t* A, const qfmt_matrix16_t* B) {
+    qfmt::Shape s;
+    if (qfmt::product_shape(A, B, &s) != QFMT_OK) return 0;
+    const int splits = qfmt::plan_splits(s);
+    return qfmt::kHeader + qfmt::sums_bytes(s) + (splits > 1 ? qfmt::part_bytes(s, splits) : 0);
+}
+
+extern "C" int qfmt_linear_act(const qfmt_matrix16_t* A, const qfmt_matrix16_t* B, const qfmt_epilogue_t* epilogue, void* d_y, int64_t ldy,
+                               int32_t dtype, void* d_workspace, size_t workspace_bytes, void* stream) {
+    qfmt::Call c;
+    bool work;
+    const int rc = qfmt::prepare_call(&c, false, A, B, epilogue, d_y, ldy, nullptr, dtype, d_workspace, workspace_bytes, &work);
+    if (rc != QFMT_OK || !work) return rc;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (dtype == QFMT_F16) return qfmt::forward_typed<__half>(c, epilogue, d_y, ldy, st);
+    return qfmt::forward_typed<__nv_bfloat16>(c, epilogue, d_y, ldy, st);
+}
+
+extern "C" int qfmt_linear_act_backward(const qfmt_matrix16_t* A, const qfmt_matrix16_t* B, const qfmt_epilogue_t* epilogue, void* d_dz,
+                                        int64_t ld_dz, float* d_dbias, int32_t dtype, void* d_workspace, size_t workspace_bytes,
+                                        void* stream) {
+    qfmt::Call c;
+    bool work;
+    const int rc = qfmt::prepare_call(&c, true, A, B, epilogue, d_dz, ld_dz, d_dbias, dtype, d_workspace, workspace_bytes, &work);
+    if (rc != QFMT_OK) return rc;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (!work) {
+        if (d_dbias != nullptr && c.s.N > 0) {
+            qfmt::DeviceInfo dev;
+            const int ok = qfmt::current_device(&dev);
+            if (ok != QFMT_OK) return ok;
+            QFMT_CUDA_TRY(cudaMemsetAsync(d_dbias, 0, (size_t)c.s.N * sizeof(float), st));
+        }
+        return QFMT_OK;
+    }
+    if (dtype == QFMT_F16) return qfmt::backward_typed<__half>(c, epilogue, d_dz, ld_dz, d_dbias, st);
+    return qfmt::backward_typed<__nv_bfloat16>(c, epilogue, d_dz, ld_dz, d_dbias, st);
+}
+
+extern "C" size_t qfmt_act_backward_workspace_bytes(int64_t rows, int64_t cols) {
+    if (rows < 0 || cols < 0 || rows >= (1ll << 31) || cols >= (1ll << 31)) return 0;
+    return (size_t)qfmt::pass_row_blocks(rows, cols > 0 ? cols : 1) * (size_t)qfmt::padded(cols) * sizeof(float);
+}
+
+extern "C" int qfmt_act_backward(const void* d_dy, int64_t ld_dy, const void* d_z, int64_t ld_z, void* d_dz, int64_t ld_dz, float* d_dbias,
+                                 int64_t rows, int64_t cols, int32_t dtype, int32_t act, void* d_workspace, size_t workspace_bytes,
+                                 void* stream) {
+    using namespace qfmt;
+    if (rows < 0 || cols < 0 || rows >= (1ll << 31) || cols >= (1ll << 31)) return QFMT_ERR_BAD_ARG;
+    if (dtype != QFMT_F32 && dtype != QFMT_F16 && dtype != QFMT_BF16) return QFMT_ERR_BAD_ARG;
+    if (act < QFMT_ACT_NONE || act > QFMT_ACT_SILU) return QFMT_ERR_BAD_ARG;
+    const int64_t size = dtype == QFMT_F32 ? 4 : 2;
+    if (ld_dy == 0) ld_dy = cols;
+    if (ld_z == 0) ld_z = cols;
+    if (ld_dz == 0) ld_dz = cols;
+    if (ld_dy < cols || ld_z < cols || ld_dz < cols) return QFMT_ERR_BAD_ARG;
+    if (misaligned(d_dy, size) || misaligned(d_z, size) || misaligned(d_dz, size) || misaligned(d_dbias, 4)) return QFMT_ERR_BAD_ARG;
+    if (d_dbias != nullptr && rows > 0 && cols > 0) {
+        if (d_workspace == nullptr || misaligned(d_workspace, 16) || workspace_bytes < qfmt_act_backward_workspace_bytes(rows, cols))
+            return QFMT_ERR_BAD_ARG;
+    }
+    if (rows > 0 && cols > 0 && (d_dy == nullptr || (act != QFMT_ACT_NONE && d_z == nullptr))) return QFMT_ERR_BAD_ARG;
+    DeviceInfo dev;
+    const int rc = current_device(&dev);
+    if (rc != QFMT_OK) return rc;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (rows == 0 || cols == 0) {
+        if (d_dbias != nullptr && cols > 0) QFMT_CUDA_TRY(cudaMemsetAsync(d_dbias, 0, (size_t)cols * sizeof(float), st));
+        return QFMT_OK;
+    }
+    if (d_dz == nullptr && d_dbias == nullptr) return QFMT_OK;
+    RowPass a = {};
+    a.dy = d_dy;
+    a.ld_dy = ld_dy;
+    a.z_in = d_z;
+    a.ld_z = ld_z;
+    a.out = d_dz;
+    a.ld_out = ld_dz;
+    a.sums = d_dbias != nullptr ? static_cast<float*>(d_workspace) : nullptr;
+    a.pitch = padded(cols);
+    a.rows = rows;
+    a.cols = cols;
+    const bool vec = whole(d_dy, ld_dy, size) && (act == QFMT_ACT_NONE || whole(d_z, ld_z, size)) && whole(d_dz, ld_dz, size) &&
+                     cols % 8 == 0;
+    if (dtype == QFMT_F32) return act_backward_typed<float>(act, a, vec, d_dbias, st);
+    if (dtype == QFMT_F16) return act_backward_typed<__half>(act, a, vec, d_dbias, st);
+    return act_backward_typed<__nv_bfloat16>(act, a, vec, d_dbias, st);
+}

@@ -1,0 +1,443 @@
+// Products of 16-bit codes (binary16 or bfloat16 words) whose sums go through an epilogue of the caller's choice instead of
+// to memory as they are: the frame that qfmt_linear_act and qfmt_linear_cross_entropy share.
+//
+// One persistent kernel, one CTA pair per two SMs, 256 x 256 tiles: each CTA stages its own 128 rows of op(A) and its own 128
+// columns of op(B) by TMA (64 K elements, 32 KB a stage), the leader's MMA thread issues tcgen05.mma.cta_group::2 kind::f16
+// with M = 256, N = 256, K = 16, and each CTA's tensor memory receives its 128 x 256 half of the tile.  A tile's whole
+// contraction stays in one of two 256-column accumulators, so the eight epilogue warps work on one tile while the next one is
+// summed in the other.  Sums are fp32; the tensor core truncates once per 16 products, which drifts by at most (K / 16) 2^-24
+// of sum |a||b|: 2^-15 at K = 8192, below the half step of every type an epilogue rounds to (2^-12, 2^-9) and of what the loss
+// needs.  (qfmt_gemm_packed16 hands out fp32 sums and takes them in three levels instead, which costs it a third of its rate.)
+//
+// Roles: warps 0 and 3 fill alternate stages, warp 1 issues the MMAs (leader CTA), warp 2 idles, warps 4-11 run the epilogue:
+// warp w has rows 32 (w % 4) .. + 31 and columns 128 ((w - 4) / 4) .. + 127 of its CTA's half, one row a lane.
+//
+// Rows may be counted on the device (ProductParams::count): tiles beyond the count are left out, and an operand that was
+// gathered is read in place if every row counts (alt).  Every wait is bounded; on expiry the status area reports
+// QFMT_ERR_TIMEOUT and all roles leave.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "common.cuh"
+#include "ptx.cuh"
+#include "tiles.cuh"
+
+namespace qfmt {
+namespace p16 {
+
+constexpr int kTileM = 256, kTileN = 256, kStageK = 64;  // of a pair
+constexpr int kStages = 5;
+constexpr uint32_t kStageA = 128 * kStageK * 2, kStageB = 128 * kStageK * 2, kStageBytes = kStageA + kStageB;
+constexpr int kThreads = 384, kEpiWarps = 8;
+constexpr uint32_t kBoxBytes = 4096;       // 32 rows x 128 bytes per epilogue warp, 16-byte chunks swizzled with the row
+constexpr uint32_t kColBytes = 128 * 4;    // 128 fp32 per epilogue warp: its columns' bias
+constexpr uint32_t kSmemBytes = kStages * kStageBytes + kEpiWarps * (kBoxBytes + kColBytes) + 256 + 1024;
+static_assert(kSmemBytes <= 232448, "shared memory");
+constexpr uint32_t kAccCols = 256, kTmemCols = 512;
+constexpr uint32_t kWaitLimit = 1u << 31;  // SM cycles, about a second
+
+enum : int { kFixed = 0, kCountM = 1, kCountK = 2 };  // which extent the device's count replaces
+enum : int { kAltNone = 0, kAltA = 1, kAltB = 2 };    // which operand has a second place
+
+struct ProductParams {
+    int M, N, K;             // M or K is the upper bound where the device counts
+    const int* count;        // device word, read where dyn != kFixed or alt != kAltNone
+    int dyn, alt, alt_rows;  // the second map is read if *count == alt_rows
+    int a_mn, b_mn;          // operand stored with M / N contiguous
+    int a_blocked, b_blocked;
+    int bf16;
+    int splits, kb_per_split;
+    unsigned long long* status;
+    unsigned long long tag;
+};
+
+// What an epilogue warp gets to see of a tile.
+struct Patch {
+    int lane, quad, warp;    // warp: 0 .. 7 of the epilogue warps
+    int row0;                // row of lane 0; lane l has row row0 + l
+    int rows;                // M as counted
+    int col0, cols;          // first of the 128 columns, N
+    int split, tile_m, tile_n;
+    uint32_t tmem;           // accumulator address of (row0, col0)
+    bool empty;              // nothing was summed: the sums are zero
+    uint8_t* box;
+    float* col;
+
+    __device__ __forceinline__ void load32(int block, uint32_t (&r)[32]) const {
+        if (empty) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) r[j] = 0u;
+        } else {
+            ptx::tmem_load_32cols(tmem + block * 32, r);
+        }
+    }
+    __device__ __forceinline__ void wait() const {
+        if (!empty) ptx::tmem_load_wait();
+    }
+    // The 128 columns' values of a vector (zero beyond N) into col.
+    __device__ __forceinline__ void load_columns(const float* v) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = col0 + i * 32 + lane;
+            col[i * 32 + lane] = v != nullptr && c < cols ? v[c] : 0.0f;
+        }
+        __syncwarp();
+    }
+};
+
+// ---- the box: 64 columns of 16 bits or 32 of 32 bits per row, written and read a row a lane on one side and in whole
+// 128-byte rows on the other, so that global memory is touched in full lines
+__device__ __forceinline__ uint4* box_at(uint8_t* box, int row, int chunk) {
+    return reinterpret_cast<uint4*>(box + row * 128 + ((chunk ^ (row & 7)) << 4));
+}
+// box -> global.  rowmap: row r goes to row rowmap[r].  vec: base and pitch are multiples of 16 bytes.
+template <typename T>
+__device__ __forceinline__ void box_store(uint8_t* box, T* base, int64_t ld, int row0, int rows, int col0, int cols, int lane, bool vec) {
+    constexpr int per = 16 / (int)sizeof(T), width = 128 / (int)sizeof(T);
+    if (vec) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = i * 4 + (lane >> 3), c = lane & 7, row = row0 + r, col = col0 + c * per;
+            if (row < rows && col < cols) {
+                const uint4 v = *box_at(box, r, c);
+                T* g = base + (int64_t)row * ld + col;
+                if (col + per <= cols) {
+                    *reinterpret_cast<uint4*>(g) = v;
+                } else {
+                    const T* e = reinterpret_cast<const T*>(box_at(box, r, c));
+                    for (int k = 0; k < cols - col; ++k) g[k] = e[k];
+                }
+            }
+        }
+    } else {
+        const int r_end = rows - row0 < 32 ? rows - row0 : 32;
+        for (int r = 0; r < r_end; ++r) {
+#pragma unroll
+            for (int k = 0; k < width; k += 32) {
+                const int j = k + lane;
+                if (col0 + j < cols) base[(int64_t)(row0 + r) * ld + col0 + j] = reinterpret_cast<const T*>(box_at(box, r, j / per))[j % per];
+            }
+        }
+    }
+}
+// global -> box, zeros beyond the matrix
+template <typename T>
+__device__ __forceinline__ void box_load(uint8_t* box, const T* base, int64_t ld, int row0, int rows, int col0, int cols, int lane, bool vec) {
+    constexpr int per = 16 / (int)sizeof(T), width = 128 / (int)sizeof(T);
+    if (vec && col0 + width <= cols) {
+        uint4 v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int row = row0 + i * 4 + (lane >> 3);
+            v[i] = row < rows ? *reinterpret_cast<const uint4*>(base + (int64_t)row * ld + col0 + (lane & 7) * per) : make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) *box_at(box, i * 4 + (lane >> 3), lane & 7) = v[i];
+    } else {
+        for (int r = 0; r < 32; ++r) {
+#pragma unroll
+            for (int k = 0; k < width; k += 32) {
+                const int j = k + lane;
+                T e = T(0.0f);
+                if (row0 + r < rows && col0 + j < cols) e = base[(int64_t)(row0 + r) * ld + col0 + j];
+                reinterpret_cast<T*>(box_at(box, r, j / per))[j % per] = e;
+            }
+        }
+    }
+}
+// fp32 pairs to two codes and back, rounded to nearest even
+template <typename T>
+__device__ __forceinline__ uint32_t pack_codes(float lo, float hi);
+template <>
+__device__ __forceinline__ uint32_t pack_codes<__half>(float lo, float hi) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <>
+__device__ __forceinline__ uint32_t pack_codes<__nv_bfloat16>(float lo, float hi) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <typename T>
+__device__ __forceinline__ float2 unpack_codes(uint32_t w);
+template <>
+__device__ __forceinline__ float2 unpack_codes<__half>(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+template <>
+__device__ __forceinline__ float2 unpack_codes<__nv_bfloat16>(uint32_t w) {
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+}
+// lane's row of 64 fp32 values -> box as codes; box row -> 32 words of codes
+template <typename T>
+__device__ __forceinline__ void box_put_codes(uint8_t* box, int lane, const float (&v)[64]) {
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+        *box_at(box, lane, c) = make_uint4(pack_codes<T>(v[c * 8], v[c * 8 + 1]), pack_codes<T>(v[c * 8 + 2], v[c * 8 + 3]),
+                                           pack_codes<T>(v[c * 8 + 4], v[c * 8 + 5]), pack_codes<T>(v[c * 8 + 6], v[c * 8 + 7]));
+}
+// Sums over the warp's 32 rows: v[j] is column j of the lane's row; lane l returns the sum of column l.  (Halving exchange:
+// each step hands half of the columns to the partner lane, 31 shuffles in all; a fixed order.)
+__device__ __forceinline__ float column_sum(float (&v)[32], int lane) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const bool up = (lane & o) != 0;
+#pragma unroll
+        for (int i = 0; i < o; ++i) {
+            const float give = up ? v[i] : v[i + o], keep = up ? v[i + o] : v[i];
+            v[i] = __fadd_rn(keep, __shfl_xor_sync(0xFFFFFFFFu, give, o));
+        }
+    }
+    return v[0];
+}
+
+__device__ __forceinline__ uint32_t make_idesc(int a_mn, int b_mn, int bf16) {
+    const uint32_t ab = bf16 ? 1u : 0u;
+    return (1u << 4) | (ab << 7) | (ab << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(kTileN >> 3) << 17) |
+           ((uint32_t)(kTileM >> 4) << 24);
+}
+
+template <typename Epi>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+product16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                 const __grid_constant__ CUtensorMap map_alt, const ProductParams p, const typename Epi::Params ep) {
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = ptx::smem_addr(smem_raw);
+    const uint32_t tiles = (raw + 1023u) & ~1023u;
+    const uint32_t boxes = tiles + kStages * kStageBytes, colbufs = boxes + kEpiWarps * kBoxBytes, bars = colbufs + kEpiWarps * kColBytes;
+    auto full_bar = [&](int s) { return bars + 8u * s; };
+    auto empty_bar = [&](int s) { return bars + 8u * (kStages + s); };
+    auto acc_full_bar = [&](int a) { return bars + 8u * (2 * kStages + a); };
+    auto acc_empty_bar = [&](int a) { return bars + 8u * (2 * kStages + 2 + a); };
+    uint8_t* const gen_bars = smem_raw + (bars - raw);
+    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen_bars + 8 * (2 * kStages + 4));
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(gen_bars + 8 * (2 * kStages + 4) + 8);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = ptx::cluster_ctarank();
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            ptx::mbar_init(full_bar(s), 2);
+            ptx::mbar_init(empty_bar(s), 1);
+        }
+        for (int a = 0; a < 2; ++a) {
+            ptx::mbar_init(acc_full_bar(a), 1);
+            ptx::mbar_init(acc_empty_bar(a), 2 * kEpiWarps);
+        }
+        *abort_flag = 0;
+        ptx::fence_mbar_init();
+    }
+    if (warp == 1) {
+        ptx::tmem_alloc_pair(ptx::smem_addr(const_cast<uint32_t*>(tmem_slot)), kTmemCols);
+        ptx::tmem_relinquish_pair();
+    }
+    // global memory from here on
+    grid_dependency_wait();
+    announce_launch(p.status, p.tag);
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    ptx::cluster_sync();  // the peer's barriers exist before anything is signalled to them
+    ptx::tc_fence_after_sync();
+    grid_launch_dependents();
+    const uint32_t tmem_base = *tmem_slot;
+
+    const int count = p.dyn != kFixed || p.alt != kAltNone ? *p.count : 0;
+    const int M = p.dyn == kCountM ? count : p.M, K = p.dyn == kCountK ? count : p.K;
+    const bool use_alt = p.alt != kAltNone && count == p.alt_rows;
+    const int tiles_m = (M + kTileM - 1) / kTileM, tiles_n = (p.N + kTileN - 1) / kTileN;
+    const int kb_total = (K + kStageK - 1) / kStageK;
+    const int items = tiles_m * tiles_n * p.splits;
+    const int pairs = gridDim.x >> 1, first = blockIdx.x >> 1;
+    // item t: tile t % (tiles_m tiles_n), rows of tiles first so that pairs side by side read the same columns of B
+    auto stages_of = [&](int t, int* begin) {
+        const int split = t / (tiles_m * tiles_n);
+        *begin = split * p.kb_per_split;
+        const int left = kb_total - *begin;
+        return left < 0 ? 0 : (left < p.kb_per_split ? left : p.kb_per_split);
+    };
+
+    if (warp == 0 || warp == 3) {
+        if (lane == 0) {
+            const CUtensorMap* const ma = use_alt && p.alt == kAltA ? &map_alt : &map_a;
+            const CUtensorMap* const mb = use_alt && p.alt == kAltB ? &map_alt : &map_b;
+            const uint32_t who = warp == 0 ? 0u : 1u;
+            uint32_t seq = 0, phase = 0;
+            int stage = 0;
+            bool dead = false;
+            for (int t = first; t < items && !dead && !*abort_flag; t += pairs) {
+                const int tile = t % (tiles_m * tiles_n);
+                const int m0 = (tile % tiles_m) * kTileM + (int)rank * 128, n0 = (tile / tiles_m) * kTileN + (int)rank * 128;
+                int kb0;
+                const int nkb = stages_of(t, &kb0);
+                for (int kb = kb0; kb < kb0 + nkb; ++kb) {
+                    if ((seq++ & 1u) != who) {  // the other producer's stage
+                        if (++stage == kStages) { stage = 0; phase ^= 1u; }
+                        continue;
+                    }
+                    if (!ptx::mbar_wait_bounded(empty_bar(stage), phase ^ 1u, kWaitLimit)) {
+                        raise_timeout(p.status, p.tag, abort_flag);
+                        dead = true;
+                        break;
+                    }
+                    const uint32_t sa = tiles + stage * kStageBytes, sb = sa + kStageA;
+                    const uint32_t bar = ptx::map_to_cta(full_bar(stage), 0);
+                    const int k0 = kb * kStageK;
+                    ptx::mbar_expect_tx_cluster(bar, kStageBytes);
+                    if (p.a_blocked) {
+                        ptx::tma_load_3d_pair(sa, ma, bar, 0, k0, m0 >> 6);
+                    } else if (p.a_mn) {
+                        for (int c = 0; c < 2; ++c) ptx::tma_load_2d_pair(sa + c * 8192u, ma, bar, m0 + c * 64, k0);
+                    } else {
+                        ptx::tma_load_2d_pair(sa, ma, bar, k0, m0);
+                    }
+                    if (p.b_blocked) {
+                        ptx::tma_load_3d_pair(sb, mb, bar, 0, k0, n0 >> 6);
+                    } else if (p.b_mn) {
+                        for (int c = 0; c < 2; ++c) ptx::tma_load_2d_pair(sb + c * 8192u, mb, bar, n0 + c * 64, k0);
+                    } else {
+                        ptx::tma_load_2d_pair(sb, mb, bar, k0, n0);
+                    }
+                    if (++stage == kStages) { stage = 0; phase ^= 1u; }
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            const uint32_t idesc = make_idesc(p.a_mn, p.b_mn, p.bf16);
+            // K-major tile: 128-byte rows, 32 bytes a step.  MN-major: blocks of 64 columns x 64 K rows (8192 bytes), 16 K
+            // rows a step.
+            const uint32_t a_step = (p.a_mn ? 2048u : 32u) >> 4, b_step = (p.b_mn ? 2048u : 32u) >> 4;
+            const uint32_t hi = desc_hi(1024u, kLayoutSw128);
+            const uint32_t a_lo = desc_lo(tiles, p.a_mn ? 8192u : 16u), b_lo = desc_lo(tiles + kStageA, p.b_mn ? 8192u : 16u);
+            int stage = 0;
+            uint32_t phase = 0, it = 0;
+            bool dead = false;
+            for (int t = first; t < items && !dead; t += pairs) {
+                int kb0;
+                const int nkb = stages_of(t, &kb0);
+                if (nkb == 0) continue;
+                const uint32_t acc = it & 1u, acc_phase = (it >> 1) & 1u;
+                ++it;
+                if (!ptx::mbar_wait_bounded(acc_empty_bar(acc), acc_phase ^ 1u, kWaitLimit)) {
+                    raise_timeout(p.status, p.tag, abort_flag);
+                    break;
+                }
+                ptx::tc_fence_after_sync();
+                const uint32_t d = tmem_base + acc * kAccCols;
+                for (int kb = 0; kb < nkb; ++kb) {
+                    if (!ptx::mbar_wait_bounded(full_bar(stage), phase, kWaitLimit)) {
+                        raise_timeout(p.status, p.tag, abort_flag);
+                        dead = true;
+                        break;
+                    }
+                    ptx::tc_fence_after_sync();
+                    const uint32_t off = (uint32_t)stage * (kStageBytes >> 4);
+#pragma unroll
+                    for (int k = 0; k < kStageK / 16; ++k)
+                        ptx::mma_f16_pair(d, desc_join(hi, a_lo + off + k * a_step), desc_join(hi, b_lo + off + k * b_step), idesc,
+                                          (kb | k) != 0 ? 1u : 0u);
+                    ptx::mma_commit_pair(empty_bar(stage), 3);
+                    if (++stage == kStages) { stage = 0; phase ^= 1u; }
+                }
+                if (dead) break;
+                ptx::mma_commit_pair(acc_full_bar(acc), 3);
+            }
+        }
+        __syncwarp();
+    } else if (warp >= 4) {
+        Patch pt;
+        pt.lane = lane;
+        pt.quad = warp & 3;
+        pt.warp = warp - 4;
+        pt.box = smem_raw + (boxes - raw) + pt.warp * kBoxBytes;
+        pt.col = reinterpret_cast<float*>(smem_raw + (colbufs - raw) + pt.warp * kColBytes);
+        pt.rows = M;
+        pt.cols = p.N;
+        const int half = pt.warp >> 2;
+        uint32_t it = 0;
+        for (int t = first; t < items; t += pairs) {
+            const int tile = t % (tiles_m * tiles_n);
+            int kb0;
+            const int nkb = stages_of(t, &kb0);
+            pt.split = t / (tiles_m * tiles_n);
+            pt.tile_m = tile % tiles_m;
+            pt.tile_n = tile / tiles_m;
+            pt.row0 = pt.tile_m * kTileM + (int)rank * 128 + pt.quad * 32;
+            pt.col0 = pt.tile_n * kTileN + half * 128;
+            pt.empty = nkb == 0;
+            const uint32_t acc = it & 1u, acc_phase = (it >> 1) & 1u;
+            pt.tmem = tmem_base + ((uint32_t)(pt.quad * 32) << 16) + acc * kAccCols + (uint32_t)half * 128u;
+            typename Epi::Ahead ahead;
+            Epi::before(pt, ep, ahead);
+            if (nkb != 0) {
+                ++it;
+                bool ok = true;
+                if (lane == 0) ok = ptx::mbar_wait_bounded(acc_full_bar(acc), acc_phase, kWaitLimit);
+                ok = __shfl_sync(0xFFFFFFFFu, ok ? 1 : 0, 0) != 0;
+                if (!ok && lane == 0) raise_timeout(p.status, p.tag, abort_flag);
+                if (!ok || *abort_flag) break;
+                ptx::tc_fence_after_sync();
+            }
+            const uint32_t bar = ptx::map_to_cta(acc_empty_bar(acc), 0);
+            Epi::run(pt, ep, ahead, [&] {  // the accumulator has been read
+                if (nkb != 0) {
+                    ptx::tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive_cluster(bar);
+                }
+            });
+        }
+        __syncwarp();
+    }
+
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    if (*abort_flag) {  // copies in flight land before the shared memory goes
+        for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+    }
+    ptx::cluster_sync();  // neither CTA leaves while the other may still signal it
+    if (warp == 1) {
+        ptx::tc_fence_after_sync();
+        ptx::tmem_dealloc_pair(tmem_base, kTmemCols);
+    }
+}
+
+// ---- host side --------------------------------------------------------------------------------------------------------
+
+// An operand of M (or N) x K elements as the kernel fetches it; *blocked: see make_operand_map16.
+struct Operand {
+    CUtensorMap map;
+    int mn, blocked;
+};
+inline int make_operand(Operand* o, const void* ptr, bool mn, int64_t extent, int64_t k, int64_t ld) {
+    o->mn = mn ? 1 : 0;
+    return make_operand_map16(&o->map, reinterpret_cast<const uint16_t*>(ptr), mn, (uint64_t)extent, (uint64_t)k, (uint64_t)ld, 128, &o->blocked);
+}
+
+template <typename Epi>
+int launch_product(const Operand& a, const Operand& b, const Operand* alt, ProductParams p, const typename Epi::Params& ep,
+                   const DeviceInfo& dev, cudaStream_t stream) {
+    static std::atomic<bool> ready[64];
+    const bool known = dev.ordinal >= 0 && dev.ordinal < 64;
+    if (!known || !ready[dev.ordinal].load()) {
+        QFMT_CUDA_TRY(cudaFuncSetAttribute(product16_kernel<Epi>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes));
+        if (known) ready[dev.ordinal].store(true);
+    }
+    p.a_mn = a.mn;
+    p.b_mn = b.mn;
+    p.a_blocked = a.blocked;
+    p.b_blocked = b.blocked;
+    const long long items = (long long)((p.M + kTileM - 1) / kTileM) * ((p.N + kTileN - 1) / kTileN) * p.splits;
+    const long long most = dev.sm_count / 2, pairs = items < most ? items : most;
+    if (pairs == 0) return QFMT_OK;
+    QFMT_CUDA_TRY(launch_overlapping(product16_kernel<Epi>, (unsigned)(2 * pairs), (unsigned)kThreads, kSmemBytes, stream, a.map, b.map,
+                                     alt != nullptr ? alt->map : a.map, p, ep));
+    return QFMT_OK;
+}
+
+}  // namespace p16
+}  // namespace qfmt
