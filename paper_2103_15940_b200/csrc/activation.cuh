@@ -19,90 +19,142 @@ __device__ __forceinline__ float fast_rcp(float x) {
     return r;
 }
 
+// Two fp32 values in one register pair, and one instruction for two operations (each rounded to nearest even).
+typedef unsigned long long pair_t;
+__device__ __forceinline__ pair_t make_pair(float lo, float hi) {
+    pair_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 split_pair(pair_t v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ pair_t both(float v) { return make_pair(v, v); }
+__device__ __forceinline__ pair_t fma2(pair_t a, pair_t b, pair_t c) {
+    pair_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ pair_t mul2(pair_t a, pair_t b) {
+    pair_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ pair_t add2(pair_t a, pair_t b) {
+    pair_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// min(|x|, most), NaN where x is
+__device__ __forceinline__ float least_abs(float x, float most) {
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(fabsf(x)), "f"(most));
+    return r;
+}
+
 // GELU needs Phi(-|x|) = exp(-x^2 / 2) R(|x|).  R falls smoothly from 1/2 like 1 / (|x| sqrt(2 pi)), so in t = 1 / (1 + 0.24 |x|) it
 // is a short polynomial without a constant term: least squares of relative error on 0 <= |x| <= 40, reweighted until even, gave
 // |error| < 4.4e-7 (2^-21), far below the half step of the codes it is rounded to (2^-9, 2^-12).  The same exponential gives the
 // density that the derivative needs.
 struct NormalTail {
-    float q;  // Phi(-|x|)
-    float e;  // exp(-x^2 / 2)
+    pair_t ax;  // |x|, at most 100: beyond, nothing changes, and infinities would meet zeros
+    pair_t r;   // R(|x|)
+    pair_t e;   // exp(-x^2 / 2)
 };
-__device__ __forceinline__ NormalTail normal_tail(float x) {
-    const float t = fast_rcp(__fmaf_rn(0.24f, fabsf(x), 1.0f));
-    float r = -0.05299483f;
-    r = __fmaf_rn(r, t, 0.15280514f);
-    r = __fmaf_rn(r, t, -0.06571881f);
-    r = __fmaf_rn(r, t, 0.1184004f);
-    r = __fmaf_rn(r, t, 0.06339276f);
-    r = __fmaf_rn(r, t, 0.09283971f);
-    r = __fmaf_rn(r, t, 0.09552203f);
-    r = __fmaf_rn(r, t, 0.0957538f);
+__device__ __forceinline__ NormalTail normal_tail(float x0, float x1) {
     NormalTail n;
-    n.e = fast_exp2(__fmul_rn(__fmul_rn(x, x), -0.72134752f));
-    n.q = __fmul_rn(__fmul_rn(r, t), n.e);
+    n.ax = make_pair(least_abs(x0, 100.0f), least_abs(x1, 100.0f));
+    const float2 d = split_pair(fma2(both(0.24f), n.ax, both(1.0f)));
+    const pair_t t = make_pair(fast_rcp(d.x), fast_rcp(d.y));
+    pair_t r = both(-0.05299483f);
+    r = fma2(r, t, both(0.15280514f));
+    r = fma2(r, t, both(-0.06571881f));
+    r = fma2(r, t, both(0.1184004f));
+    r = fma2(r, t, both(0.06339276f));
+    r = fma2(r, t, both(0.09283971f));
+    r = fma2(r, t, both(0.09552203f));
+    r = fma2(r, t, both(0.0957538f));
+    n.r = mul2(r, t);
+    const float2 s = split_pair(mul2(mul2(n.ax, both(-0.72134752f)), n.ax));
+    n.e = make_pair(fast_exp2(s.x), fast_exp2(s.y));
     return n;
 }
 
 constexpr float kGeluTanhC = 1.5957691216f;  // 2 sqrt(2 / pi): 1/2 (1 + tanh u) = 1 / (1 + exp(-2 u))
 constexpr float kLog2E = 1.4426950409f;
 
-// kPrecise: for fp32 results, with the math library's functions; otherwise for results that are rounded to codes.
-template <bool kPrecise>
-__device__ __forceinline__ float logistic(float u) {
-    if (kPrecise) return __frcp_rn(__fadd_rn(1.0f, expf(-u)));
-    return fast_rcp(__fadd_rn(1.0f, fast_exp2(__fmul_rn(u, -kLog2E))));
-}
-
-// The same with p (1 - p), its derivative, from exp(-|u|): 1 - p would cancel where p is close to 1.
-struct Logistic {
-    float p, slope;
-};
-template <bool kPrecise>
-__device__ __forceinline__ Logistic logistic_slope(float u) {
-    const float a = kPrecise ? expf(-fabsf(u)) : fast_exp2(__fmul_rn(fabsf(u), -kLog2E));
-    const float r = kPrecise ? __frcp_rn(__fadd_rn(1.0f, a)) : fast_rcp(__fadd_rn(1.0f, a));
-    const float q = __fmul_rn(a, r);
-    Logistic l;
-    l.p = u < 0.0f ? q : r;
-    l.slope = __fmul_rn(q, r);
-    return l;
-}
-
-template <int kAct, bool kPrecise>
-__device__ __forceinline__ float activate(float x) {
-    if (kAct == QFMT_ACT_RELU) return x > 0.0f ? x : (x != x ? x : 0.0f);
-    if (kAct == QFMT_ACT_GELU) {
-        if (kPrecise) return __fmul_rn(__fmul_rn(0.5f, x), erfcf(__fmul_rn(x, -0.70710678f)));
-        const float q = normal_tail(x).q;
-        return __fmul_rn(x, x < 0.0f ? q : __fsub_rn(1.0f, q));
+// For results that are rounded to codes, two values at a time.  1 / (1 + exp(-u)) and its derivative from a = exp(-|u|): with
+// r = 1 / (1 + a) they are r or a r, and a r r (1 - p would cancel where p is close to 1).
+template <int kAct>
+__device__ __forceinline__ pair_t activate2(pair_t x) {
+    const float2 v = split_pair(x);
+    if (kAct == QFMT_ACT_RELU) return make_pair(v.x > 0.0f ? v.x : (v.x != v.x ? v.x : 0.0f), v.y > 0.0f ? v.y : (v.y != v.y ? v.y : 0.0f));
+    if (kAct == QFMT_ACT_GELU) {  // x Phi(x) = max(x, 0) - |x| Phi(-|x|), without cancellation on either side
+        const NormalTail n = normal_tail(v.x, v.y);
+        const pair_t low = mul2(mul2(n.ax, n.r), n.e);
+        return fma2(low, both(-1.0f), make_pair(fmaxf(v.x, 0.0f), fmaxf(v.y, 0.0f)));
     }
-    if (kAct == QFMT_ACT_GELU_TANH) {
-        const float u = __fmul_rn(__fmul_rn(kGeluTanhC, x), __fmaf_rn(__fmul_rn(0.044715f, x), x, 1.0f));
-        return __fmul_rn(x, logistic<kPrecise>(u));
+    if (kAct == QFMT_ACT_GELU_TANH || kAct == QFMT_ACT_SILU) {
+        pair_t u = mul2(x, both(-kLog2E));
+        if (kAct == QFMT_ACT_GELU_TANH)
+            u = mul2(mul2(x, both(-kGeluTanhC * kLog2E)), fma2(mul2(x, x), both(0.044715f), both(1.0f)));
+        const float2 w = split_pair(u);
+        const float2 d = split_pair(add2(make_pair(fast_exp2(w.x), fast_exp2(w.y)), both(1.0f)));
+        return mul2(x, make_pair(fast_rcp(d.x), fast_rcp(d.y)));
     }
-    if (kAct == QFMT_ACT_SILU) return __fmul_rn(x, logistic<kPrecise>(x));
     return x;
 }
 
-// Beyond +-100 every slope is 0 or 1 to the last bit; the squares of larger values would overflow.
-template <int kAct, bool kPrecise>
-__device__ __forceinline__ float activation_slope(float x) {
-    if (kAct != QFMT_ACT_RELU && kAct != QFMT_ACT_NONE) x = fabsf(x) > 100.0f ? copysignf(100.0f, x) : x;
+template <int kAct>
+__device__ __forceinline__ pair_t slope2(float x0, float x1) {
+    if (kAct == QFMT_ACT_RELU) return make_pair(x0 > 0.0f ? 1.0f : (x0 != x0 ? x0 : 0.0f), x1 > 0.0f ? 1.0f : (x1 != x1 ? x1 : 0.0f));
+    if (kAct == QFMT_ACT_GELU) {  // h = Phi(-|x|) - |x| phi(x) is the slope at -|x|, 1 - h the one at |x|
+        const NormalTail n = normal_tail(x0, x1);
+        const pair_t h = mul2(fma2(n.ax, both(-0.39894228f), n.r), n.e);
+        const float2 lo = split_pair(h), hi = split_pair(fma2(h, both(-1.0f), both(1.0f)));
+        return make_pair(x0 < 0.0f ? lo.x : hi.x, x1 < 0.0f ? lo.y : hi.y);
+    }
+    if (kAct == QFMT_ACT_GELU_TANH || kAct == QFMT_ACT_SILU) {
+        // at -|x| the slope is a r - |x| u'(x) a r r, at |x| it is 1 minus that; |x| at most 100 as above
+        const pair_t ax = make_pair(least_abs(x0, 100.0f), least_abs(x1, 100.0f));
+        pair_t u = ax, xdu = ax;
+        if (kAct == QFMT_ACT_GELU_TANH) {
+            const pair_t xx = mul2(ax, ax), cx = mul2(ax, both(kGeluTanhC));
+            u = mul2(cx, fma2(xx, both(0.044715f), both(1.0f)));
+            xdu = mul2(cx, fma2(xx, both(3.0f * 0.044715f), both(1.0f)));
+        }
+        const float2 w = split_pair(mul2(u, both(-kLog2E)));
+        const pair_t a = make_pair(fast_exp2(w.x), fast_exp2(w.y));
+        const float2 d = split_pair(add2(a, both(1.0f)));
+        const pair_t r = make_pair(fast_rcp(d.x), fast_rcp(d.y)), ar = mul2(a, r);
+        const pair_t h = mul2(ar, fma2(mul2(xdu, r), both(-1.0f), both(1.0f)));
+        const float2 lo = split_pair(h), hi = split_pair(fma2(h, both(-1.0f), both(1.0f)));
+        return make_pair(x0 < 0.0f ? lo.x : hi.x, x1 < 0.0f ? lo.y : hi.y);
+    }
+    return both(1.0f);
+}
+
+// The derivative for fp32 results, with the math library's functions.
+template <int kAct>
+__device__ __forceinline__ float slope(float x) {
     if (kAct == QFMT_ACT_RELU) return x > 0.0f ? 1.0f : (x != x ? x : 0.0f);
+    const float ax = least_abs(x, 100.0f);
     if (kAct == QFMT_ACT_GELU) {
-        if (kPrecise) return __fmaf_rn(__fmul_rn(x, 0.39894228f), expf(__fmul_rn(__fmul_rn(-0.5f, x), x)), __fmul_rn(0.5f, erfcf(__fmul_rn(x, -0.70710678f))));
-        const NormalTail n = normal_tail(x);
-        return __fmaf_rn(__fmul_rn(x, 0.39894228f), n.e, x < 0.0f ? n.q : __fsub_rn(1.0f, n.q));
+        const float h = __fmaf_rn(__fmul_rn(ax, -0.39894228f), expf(__fmul_rn(__fmul_rn(-0.5f, ax), ax)), __fmul_rn(0.5f, erfcf(__fmul_rn(ax, 0.70710678f))));
+        return x < 0.0f ? h : __fsub_rn(1.0f, h);
     }
-    if (kAct == QFMT_ACT_GELU_TANH) {
-        const float xx = __fmul_rn(x, x);
-        const Logistic l = logistic_slope<kPrecise>(__fmul_rn(__fmul_rn(kGeluTanhC, x), __fmaf_rn(0.044715f, xx, 1.0f)));
-        const float du = __fmul_rn(kGeluTanhC, __fmaf_rn(3.0f * 0.044715f, xx, 1.0f));
-        return __fmaf_rn(__fmul_rn(x, l.slope), du, l.p);
-    }
-    if (kAct == QFMT_ACT_SILU) {
-        const Logistic l = logistic_slope<kPrecise>(x);
-        return __fmaf_rn(x, l.slope, l.p);
+    if (kAct == QFMT_ACT_GELU_TANH || kAct == QFMT_ACT_SILU) {
+        float u = ax, xdu = ax;
+        if (kAct == QFMT_ACT_GELU_TANH) {
+            const float xx = __fmul_rn(ax, ax), cx = __fmul_rn(ax, kGeluTanhC);
+            u = __fmul_rn(cx, __fmaf_rn(0.044715f, xx, 1.0f));
+            xdu = __fmul_rn(cx, __fmaf_rn(3.0f * 0.044715f, xx, 1.0f));
+        }
+        const float a = expf(-u), r = __frcp_rn(__fadd_rn(1.0f, a));
+        const float h = __fmul_rn(__fmul_rn(a, r), __fmaf_rn(-xdu, r, 1.0f));
+        return x < 0.0f ? h : __fsub_rn(1.0f, h);
     }
     return 1.0f;
 }

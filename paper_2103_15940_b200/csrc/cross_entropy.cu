@@ -4,7 +4,7 @@
 //
 // Rows that do not count are taken out first: compact_kernel numbers the others, and the products run over as many rows as it
 // found (the host never learns the number).  If all count, H is read in place.  Forward, the product's epilogue reduces each row's
-// 128 logits to their maximum and the sum of exponentials relative to it (base 2, one pass: a later maximum rescales the sum),
+// 64 logits to their maximum and the sum of exponentials relative to it (base 2, one pass: a later maximum rescales the sum),
 // and join_rows_kernel joins the pieces.  Backward, the vocabulary is walked in pieces: the product again, its epilogue forming d in
 // codes in a buffer that stays in the second-level cache, then the two products that read it.  dH is added up in fp32 over the pieces.
 #include <cuda_bf16.h>
@@ -182,14 +182,14 @@ compact_kernel(const Compact c, unsigned long long* status, unsigned long long t
 
 // ---- epilogues ------------------------------------------------------------------------------------------------------------
 
-// Per row and 128 columns: m = the largest logit, s = sum exp(logit - m), and the target's logit.  The exponentials are
+// Per row and 64 columns: m = the largest logit, s = sum exp(logit - m), and the target's logit.  The exponentials are
 // 2^(logit log2 e - shift), one fused operation and one of the special function unit each, with shift = m log2 e rounded; what the rounding
 // took off is put back by one factor per 32 columns.  Logits whose product with log2 e overflows have m subtracted first.
 struct RowSumEpilogue {
     struct Params {
         const float* bias;
         const int* target;
-        float2* parts;  // [128-column groups][pitch]
+        float2* parts;  // [64-column groups][pitch]
         float* picked;  // the target's logit of a compact row
         int64_t pitch;
     };
@@ -205,53 +205,61 @@ struct RowSumEpilogue {
         const int row = p.row0 + p.lane;
         float most = -INFINITY, sum = 0.0f;
 #pragma unroll 1
-        for (int c = 0; c < 4; ++c) {
-            uint32_t r[32];
-            p.load32(c, r);
-            p.wait();
-            if (c == 3) release();
+        for (int c = 0; c < 2; ++c) {
+            pair_t v[16];
+            p.load_pairs<true>(c, v);
+            if (c == 1) release();
             const int left = p.cols - p.col0 - c * 32;
             if (left <= 0) continue;
-            float v[32];
-#pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = __fadd_rn(__uint_as_float(r[j]), p.col[c * 32 + j]);
             if (left < 32) {
 #pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] = j < left ? v[j] : -INFINITY;
+                for (int j = 0; j < 16; ++j) {
+                    const float2 f = split_pair(v[j]);
+                    v[j] = make_pair(2 * j < left ? f.x : -INFINITY, 2 * j + 1 < left ? f.y : -INFINITY);
+                }
             }
-            if ((a.target >> 5) == c) {
-                float t = 0.0f;
+            if ((a.target >> 5) == c) {  // by halves: an index would put the values into memory
+                pair_t w[8];
 #pragma unroll
-                for (int j = 0; j < 32; ++j) t = (a.target & 31) == j ? v[j] : t;
-                e.picked[row] = t;
+                for (int j = 0; j < 8; ++j) w[j] = (a.target & 16) ? v[j + 8] : v[j];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[j] = (a.target & 8) ? w[j + 4] : w[j];
+                w[0] = (a.target & 4) ? w[2] : w[0];
+                w[1] = (a.target & 4) ? w[3] : w[1];
+                const float2 f = split_pair((a.target & 2) ? w[1] : w[0]);
+                e.picked[row] = (a.target & 1) ? f.y : f.x;
             }
-            float m = v[0];
+            float m0 = -INFINITY, m1 = -INFINITY;
 #pragma unroll
-            for (int j = 1; j < 32; ++j) m = fmaxf(m, v[j]);
-            const float now = fmaxf(most, m);
+            for (int j = 0; j < 16; ++j) {
+                const float2 f = split_pair(v[j]);
+                m0 = fmaxf(m0, f.x);
+                m1 = fmaxf(m1, f.y);
+            }
+            const float now = fmaxf(most, fmaxf(m0, m1));
             float shift = __fmul_rn(now, kLog2E), back = 1.0f;
             if (isinf(shift)) {
                 if (now != -INFINITY) {  // else nothing but -infinity yet: all terms are zero
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] = __fsub_rn(v[j], now);
+                    for (int j = 0; j < 16; ++j) v[j] = add2(v[j], both(-now));
                 }
                 shift = 0.0f;
             } else {
                 back = fast_exp2(-__fmaf_rn(now, kLog2E, -shift));
             }
             if (now != -INFINITY) sum = __fmul_rn(sum, fast_exp2(__fmul_rn(__fsub_rn(most, now), kLog2E)));
-            float s0 = 0.0f, s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
+            pair_t s0 = 0ull, s1 = 0ull;
 #pragma unroll
-            for (int j = 0; j < 32; j += 4) {
-                s0 = __fadd_rn(s0, fast_exp2(__fmaf_rn(v[j], kLog2E, -shift)));
-                s1 = __fadd_rn(s1, fast_exp2(__fmaf_rn(v[j + 1], kLog2E, -shift)));
-                s2 = __fadd_rn(s2, fast_exp2(__fmaf_rn(v[j + 2], kLog2E, -shift)));
-                s3 = __fadd_rn(s3, fast_exp2(__fmaf_rn(v[j + 3], kLog2E, -shift)));
+            for (int j = 0; j < 16; j += 2) {
+                const float2 x = split_pair(fma2(v[j], both(kLog2E), both(-shift))), y = split_pair(fma2(v[j + 1], both(kLog2E), both(-shift)));
+                s0 = add2(s0, make_pair(fast_exp2(x.x), fast_exp2(x.y)));
+                s1 = add2(s1, make_pair(fast_exp2(y.x), fast_exp2(y.y)));
             }
-            sum = __fmaf_rn(__fadd_rn(__fadd_rn(s0, s1), __fadd_rn(s2, s3)), back, sum);
+            const float2 s = split_pair(add2(s0, s1));
+            sum = __fmaf_rn(__fadd_rn(s.x, s.y), back, sum);
             most = now;
         }
-        if (row < p.rows && p.col0 < p.cols) e.parts[(int64_t)(p.col0 >> 7) * e.pitch + row] = make_float2(most, sum);
+        if (row < p.rows && p.col0 < p.cols) e.parts[(int64_t)(p.col0 >> 6) * e.pitch + row] = make_float2(most, sum);
     }
 };
 
@@ -288,42 +296,43 @@ struct GradEpilogue {
         const bool huge = __any_sync(0xFFFFFFFFu, isinf(a.lse2));  // lse log2 e overflows: subtract first
 #pragma unroll 1
         for (int c = 0; c < 2; ++c) {
-            uint32_t lo[32], hi[32];
-            p.load32(c * 2, lo);
-            p.load32(c * 2 + 1, hi);
-            p.wait();
+            pair_t v[16];
+            p.load_pairs<true>(c, v);
             if (c == 1) release();
-            const int left = p.cols - p.col0 - c * 64;
-            float v[64];
+            const int col0 = p.col0 + c * 32, left = p.cols - col0;
+            if (!huge) {
 #pragma unroll
-            for (int j = 0; j < 64; ++j) {
-                v[j] = __fadd_rn(__uint_as_float(j < 32 ? lo[j & 31] : hi[j & 31]), p.col[c * 64 + j]);
-                if (!huge) v[j] = __fmul_rn(a.gp, fast_exp2(__fmaf_rn(v[j], kLog2E, -a.lse2)));
-                else v[j] = __fmul_rn(a.g, fast_exp2(__fmul_rn(__fsub_rn(v[j], a.lse), kLog2E)));
+                for (int j = 0; j < 16; ++j) {
+                    const float2 x = split_pair(fma2(v[j], both(kLog2E), both(-a.lse2)));
+                    v[j] = mul2(make_pair(fast_exp2(x.x), fast_exp2(x.y)), both(a.gp));
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const float2 x = split_pair(mul2(add2(v[j], both(-a.lse)), both(kLog2E)));
+                    v[j] = mul2(make_pair(fast_exp2(x.x), fast_exp2(x.y)), both(a.g));
+                }
             }
-            if (a.target >= c * 64 && a.target < c * 64 + 64) {
+            if ((a.target >> 5) == c) {
+                const int at = (a.target & 31) >> 1;
+                const pair_t minus = (a.target & 1) ? make_pair(0.0f, -a.g) : make_pair(-a.g, 0.0f);
 #pragma unroll
-                for (int j = 0; j < 64; ++j) v[j] = (a.target & 63) == j ? __fsub_rn(v[j], a.g) : v[j];
+                for (int j = 0; j < 16; ++j) v[j] = at == j ? add2(v[j], minus) : v[j];
             }
-            if (left < 64 || p.row0 + 32 > p.rows) {
+            if (left < 32 || p.row0 + 32 > p.rows) {
 #pragma unroll
-                for (int j = 0; j < 64; ++j) v[j] = there && j < left ? v[j] : 0.0f;
+                for (int j = 0; j < 16; ++j) {
+                    const float2 x = split_pair(v[j]);
+                    v[j] = make_pair(there && 2 * j < left ? x.x : 0.0f, there && 2 * j + 1 < left ? x.y : 0.0f);
+                }
             }
             p16::box_put_codes<T>(p.box, p.lane, v);
             __syncwarp();
-            p16::box_store<T>(p.box, e.d, e.pitch, p.row0, p.row0 + 32, p.col0 + c * 64, (int)e.pitch, p.lane, true);
+            p16::box_store<T>(p.box, e.d, e.pitch, p.row0, p.row0 + 32, col0, (int)e.pitch, p.lane, true);
             __syncwarp();
             if (e.parts != nullptr) {
-                float* out = e.parts + (int64_t)(p.row0 >> 5) * e.pitch + p.col0 + c * 64 + p.lane;
-                float x[32], y[32];
-#pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    x[j] = v[j];
-                    y[j] = v[32 + j];
-                }
-                const float s0 = p16::column_sum(x, p.lane), s1 = p16::column_sum(y, p.lane);
-                out[0] = s0;
-                out[32] = s1;
+                const float s = p16::column_sum(p.box, p.lane, v);
+                e.parts[(int64_t)(p.row0 >> 5) * e.pitch + col0 + p.lane] = s;
             }
         }
     }
@@ -346,21 +355,16 @@ struct ScaledEpilogue {
     static __device__ __forceinline__ void run(const Patch& p, const Params& e, Ahead& a, F release) {
 #pragma unroll 1
         for (int c = 0; c < 2; ++c) {
-            uint32_t lo[32], hi[32];
-            p.load32(c * 2, lo);
-            p.load32(c * 2 + 1, hi);
-            p.wait();
+            pair_t v[16];
+            p.load_pairs<false>(c, v);
             if (c == 1) release();
-            if (p.row0 >= p.rows || p.col0 + c * 64 >= p.cols) continue;
-            float v[64];
+            const int col0 = p.col0 + c * 32;
+            if (p.row0 >= p.rows || col0 >= p.cols) continue;
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
-                v[j] = __fmul_rn(__uint_as_float(lo[j]), a.factor);
-                v[32 + j] = __fmul_rn(__uint_as_float(hi[j]), a.factor);
-            }
+            for (int j = 0; j < 16; ++j) v[j] = mul2(v[j], both(a.factor));
             p16::box_put_codes<T>(p.box, p.lane, v);
             __syncwarp();
-            p16::box_store<T>(p.box, e.out, e.ld, p.row0, p.rows, p.col0 + c * 64, p.cols, p.lane, e.vec != 0);
+            p16::box_store<T>(p.box, e.out, e.ld, p.row0, p.rows, col0, p.cols, p.lane, e.vec != 0);
             __syncwarp();
         }
     }
@@ -379,30 +383,40 @@ struct AddEpilogue {
     static __device__ __forceinline__ void run(const Patch& p, const Params& e, Ahead&, F release) {
         float* base = e.sums + (int64_t)p.split * e.split_stride;
 #pragma unroll 1
-        for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < 2; ++c) {
+            p16::Fetched f[2];
+            if (e.add) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    p16::box_fetch<float>(f[h], base, e.pitch, p.row0, p.rows, p.col0 + c * 32 + h * 16, p.cols, p.lane, true);
+            }
             uint32_t r[32];
             p.load32(c, r);
             p.wait();
-            if (c == 3) release();
-            const int col0 = p.col0 + c * 32;
-            if (p.row0 >= p.rows || col0 >= p.cols) continue;
-            if (e.add) {
-                p16::box_load<float>(p.box, base, e.pitch, p.row0, p.rows, col0, p.cols, p.lane, true);
-                __syncwarp();
+            if (c == 1) release();
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const float4 w = *reinterpret_cast<const float4*>(p16::box_at(p.box, p.lane, k));
-                    const float s[4] = {w.x, w.y, w.z, w.w};
+            for (int h = 0; h < 2; ++h) {
+                const int col0 = p.col0 + c * 32 + h * 16;
+                if (p.row0 >= p.rows || col0 >= p.cols) continue;
+                if (e.add) {
+                    p16::box_put<float>(p.box, f[h], base, e.pitch, p.row0, p.rows, col0, p.cols, p.lane, true);
+                    __syncwarp();
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) r[4 * k + j] = __float_as_uint(__fadd_rn(s[j], __uint_as_float(r[4 * k + j])));
+                    for (int k = 0; k < 4; ++k) {
+                        const float4 w = *reinterpret_cast<const float4*>(p16::box_at(p.box, p.lane, k));
+                        const float s[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) r[16 * h + 4 * k + j] = __float_as_uint(__fadd_rn(s[j], __uint_as_float(r[16 * h + 4 * k + j])));
+                    }
+                    __syncwarp();
                 }
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    *p16::box_at(p.box, p.lane, k) = make_uint4(r[16 * h + 4 * k], r[16 * h + 4 * k + 1], r[16 * h + 4 * k + 2], r[16 * h + 4 * k + 3]);
+                __syncwarp();
+                p16::box_store<float>(p.box, base, e.pitch, p.row0, p.rows, col0, p.cols, p.lane, true);
                 __syncwarp();
             }
-#pragma unroll
-            for (int k = 0; k < 8; ++k) *p16::box_at(p.box, p.lane, k) = make_uint4(r[4 * k], r[4 * k + 1], r[4 * k + 2], r[4 * k + 3]);
-            __syncwarp();
-            p16::box_store<float>(p.box, base, e.pitch, p.row0, p.rows, col0, p.cols, p.lane, true);
-            __syncwarp();
         }
     }
 };
@@ -578,7 +592,7 @@ Places places(const Sizes& s, const Plan& plan, bool backward) {
     p.target = l.take((size_t)s.rows * 4);
     p.compact_h = l.take((size_t)up(s.rows, 64) * plan.pitch_h * 2);
     if (!backward) {
-        p.parts = l.take((size_t)(up(s.vocab, 128) / 128) * s.rows * sizeof(float2));
+        p.parts = l.take((size_t)(up(s.vocab, 64) / 64) * s.rows * sizeof(float2));
         p.picked = l.take((size_t)s.rows * 4);
         p.compact_loss = l.take((size_t)s.rows * 4);
     } else {
@@ -782,7 +796,7 @@ extern "C" int qfmt_linear_cross_entropy(const qfmt_matrix16_t* H, const qfmt_ma
     const unsigned blocks = (unsigned)((s.rows + kJoinRows - 1) / kJoinRows);
     float* compact_loss = d_mean != nullptr && blocks > 1 ? at<float>(d_workspace, pl.compact_loss) : nullptr;
     QFMT_CUDA_TRY(launch_overlapping(join_rows_kernel, blocks, (unsigned)(kJoinRows * kJoinParts), 0, st, (const float2*)re.parts, s.rows,
-                                     (int)(up(s.vocab, 128) / 128), (const Found*)c.found, (const int*)c.index, (const int*)c.target,
+                                     (int)(up(s.vocab, 64) / 64), (const Found*)c.found, (const int*)c.index, (const int*)c.target,
                                      (const float*)re.picked, d_loss, d_lse, compact_loss, blocks == 1 ? d_mean : (float*)nullptr));
     if (compact_loss != nullptr)
         QFMT_CUDA_TRY(launch_overlapping(mean_kernel, 1u, 1024u, 0, st, (const float*)compact_loss, (const Found*)c.found, d_mean));

@@ -30,26 +30,25 @@ struct ForwardEpilogue {
         int64_t ld_residual, ld_z, ld_y;
         int vec_residual, vec_z, vec_y;
     };
-    using Ahead = Nothing;
-    static __device__ __forceinline__ void before(const Patch& p, const Params& e, Ahead&) { p.load_columns(e.bias); }
+    struct Ahead {
+        p16::Fetched residual;
+    };
+    static __device__ __forceinline__ void fetch(const Patch& p, const Params& e, Ahead& a, int col0) {
+        if (e.residual != nullptr)
+            p16::box_fetch<T>(a.residual, e.residual, e.ld_residual, p.row0, p.rows, col0, p.cols, p.lane, e.vec_residual != 0);
+    }
+    static __device__ __forceinline__ void before(const Patch& p, const Params& e, Ahead& a) {
+        p.load_columns(e.bias);
+        fetch(p, e, a, p.col0);
+    }
     template <typename F>
-    static __device__ __forceinline__ void run(const Patch& p, const Params& e, Ahead&, F release) {
+    static __device__ __forceinline__ void run(const Patch& p, const Params& e, Ahead& a, F release) {
 #pragma unroll 1
         for (int c = 0; c < 2; ++c) {
-            const int col0 = p.col0 + c * 64;
-            float v[64];
-            {
-                uint32_t a[32], b[32];
-                p.load32(c * 2, a);
-                p.load32(c * 2 + 1, b);
-                p.wait();
-                if (c == 1) release();
-#pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    v[j] = __fadd_rn(__uint_as_float(a[j]), p.col[c * 64 + j]);
-                    v[32 + j] = __fadd_rn(__uint_as_float(b[j]), p.col[c * 64 + 32 + j]);
-                }
-            }
+            const int col0 = p.col0 + c * 32;
+            pair_t v[16];
+            p.load_pairs<true>(c, v);
+            if (c == 1) release();
             if (col0 >= p.cols || p.row0 >= p.rows) continue;
             if (e.z != nullptr) {
                 p16::box_put_codes<T>(p.box, p.lane, v);
@@ -58,21 +57,12 @@ struct ForwardEpilogue {
                 __syncwarp();
             }
 #pragma unroll
-            for (int j = 0; j < 64; ++j) v[j] = activate<kAct, false>(v[j]);
+            for (int j = 0; j < 16; ++j) v[j] = activate2<kAct>(v[j]);
             if (e.residual != nullptr) {
-                p16::box_load<T>(p.box, e.residual, e.ld_residual, p.row0, p.rows, col0, p.cols, p.lane, e.vec_residual != 0);
+                p16::box_put<T>(p.box, a.residual, e.residual, e.ld_residual, p.row0, p.rows, col0, p.cols, p.lane, e.vec_residual != 0);
                 __syncwarp();
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const uint4 w = *p16::box_at(p.box, p.lane, k);
-                    const uint32_t words[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float2 r = p16::unpack_codes<T>(words[j]);
-                        v[k * 8 + 2 * j] = __fadd_rn(v[k * 8 + 2 * j], r.x);
-                        v[k * 8 + 2 * j + 1] = __fadd_rn(v[k * 8 + 2 * j + 1], r.y);
-                    }
-                }
+                if (c == 0) fetch(p, e, a, col0 + 32);
+                p16::box_each<T>(p.box, p.lane, [&](int j, float2 r) { v[j] = add2(v[j], make_pair(r.x, r.y)); });
                 __syncwarp();
             }
             p16::box_put_codes<T>(p.box, p.lane, v);
@@ -92,57 +82,43 @@ struct BackwardEpilogue {
         int64_t ld_residual, ld_z, ld_dz, pitch;
         int vec_residual, vec_z, vec_dz;
     };
-    using Ahead = Nothing;
-    static __device__ __forceinline__ void before(const Patch&, const Params&, Ahead&) {}
+    // z is on its way while the tile is summed; the residual where there is no z (both would not fit the registers)
+    struct Ahead {
+        p16::Fetched f;
+    };
+    static __device__ __forceinline__ void fetch_residual(const Patch& p, const Params& e, p16::Fetched& f, int col0) {
+        p16::box_fetch<T>(f, e.residual, e.ld_residual, p.row0, p.rows, col0, p.cols, p.lane, e.vec_residual != 0);
+    }
+    static __device__ __forceinline__ void fetch(const Patch& p, const Params& e, Ahead& a, int col0) {
+        if (kAct != QFMT_ACT_NONE) p16::box_fetch<T>(a.f, e.z, e.ld_z, p.row0, p.rows, col0, p.cols, p.lane, e.vec_z != 0);
+        else if (e.residual != nullptr) fetch_residual(p, e, a.f, col0);
+    }
+    static __device__ __forceinline__ void before(const Patch& p, const Params& e, Ahead& a) { fetch(p, e, a, p.col0); }
     template <typename F>
-    static __device__ __forceinline__ void run(const Patch& p, const Params& e, Ahead&, F release) {
+    static __device__ __forceinline__ void run(const Patch& p, const Params& e, Ahead& a, F release) {
 #pragma unroll 1
         for (int c = 0; c < 2; ++c) {
-            const int col0 = p.col0 + c * 64;
-            float v[64];
-            {
-                uint32_t a[32], b[32];
-                p.load32(c * 2, a);
-                p.load32(c * 2 + 1, b);
-                p.wait();
-                if (c == 1) release();
-#pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    v[j] = __uint_as_float(a[j]);
-                    v[32 + j] = __uint_as_float(b[j]);
-                }
-            }
+            const int col0 = p.col0 + c * 32;
+            pair_t v[16];
+            p.load_pairs<false>(c, v);
+            if (c == 1) release();
             if (col0 >= p.cols) continue;
             if (e.residual != nullptr) {
-                p16::box_load<T>(p.box, e.residual, e.ld_residual, p.row0, p.rows, col0, p.cols, p.lane, e.vec_residual != 0);
+                p16::Fetched late;
+                if (kAct != QFMT_ACT_NONE) fetch_residual(p, e, late, col0);
+                p16::box_put<T>(p.box, kAct != QFMT_ACT_NONE ? late : a.f, e.residual, e.ld_residual, p.row0, p.rows, col0, p.cols, p.lane,
+                                e.vec_residual != 0);
                 __syncwarp();
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const uint4 w = *p16::box_at(p.box, p.lane, k);
-                    const uint32_t words[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float2 r = p16::unpack_codes<T>(words[j]);
-                        v[k * 8 + 2 * j] = __fadd_rn(v[k * 8 + 2 * j], r.x);
-                        v[k * 8 + 2 * j + 1] = __fadd_rn(v[k * 8 + 2 * j + 1], r.y);
-                    }
-                }
+                p16::box_each<T>(p.box, p.lane, [&](int j, float2 r) { v[j] = add2(v[j], make_pair(r.x, r.y)); });
                 __syncwarp();
             }
             if (kAct != QFMT_ACT_NONE) {
-                p16::box_load<T>(p.box, e.z, e.ld_z, p.row0, p.rows, col0, p.cols, p.lane, e.vec_z != 0);
+                p16::box_put<T>(p.box, a.f, e.z, e.ld_z, p.row0, p.rows, col0, p.cols, p.lane, e.vec_z != 0);
                 __syncwarp();
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const uint4 w = *p16::box_at(p.box, p.lane, k);
-                    const uint32_t words[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float2 r = p16::unpack_codes<T>(words[j]);
-                        v[k * 8 + 2 * j] = __fmul_rn(v[k * 8 + 2 * j], activation_slope<kAct, false>(r.x));
-                        v[k * 8 + 2 * j + 1] = __fmul_rn(v[k * 8 + 2 * j + 1], activation_slope<kAct, false>(r.y));
-                    }
-                }
+            }
+            if (c == 0) fetch(p, e, a, col0 + 32);
+            if (kAct != QFMT_ACT_NONE) {
+                p16::box_each<T>(p.box, p.lane, [&](int j, float2 z) { v[j] = mul2(v[j], slope2<kAct>(z.x, z.y)); });
                 __syncwarp();
             }
             p16::box_put_codes<T>(p.box, p.lane, v);
@@ -151,16 +127,8 @@ struct BackwardEpilogue {
             __syncwarp();
             if (e.parts != nullptr) {
                 // rows beyond the matrix: sums and residual are zero there, and so is dz
-                float* out = e.parts + (int64_t)(p.row0 >> 5) * e.pitch + col0 + p.lane;
-                float lo[32], hi[32];
-#pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    lo[j] = v[j];
-                    hi[j] = v[32 + j];
-                }
-                const float s0 = p16::column_sum(lo, p.lane), s1 = p16::column_sum(hi, p.lane);
-                if (col0 + p.lane < p.cols) out[0] = s0;
-                if (col0 + 32 + p.lane < p.cols) out[32] = s1;
+                const float s = p16::column_sum(p.box, p.lane, v);
+                if (col0 + p.lane < p.cols) e.parts[(int64_t)(p.row0 >> 5) * e.pitch + col0 + p.lane] = s;
             }
         }
     }
@@ -178,17 +146,22 @@ struct PartEpilogue {
     static __device__ __forceinline__ void run(const Patch& p, const Params& e, Ahead&, F release) {
         float* base = e.parts + (int64_t)p.split * e.split_stride;
 #pragma unroll 1
-        for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < 2; ++c) {
             uint32_t a[32];
             p.load32(c, a);
             p.wait();
-            if (c == 3) release();
-            if (p.row0 >= p.rows || p.col0 + c * 32 >= p.cols) continue;
+            if (c == 1) release();
 #pragma unroll
-            for (int k = 0; k < 8; ++k) *p16::box_at(p.box, p.lane, k) = make_uint4(a[4 * k], a[4 * k + 1], a[4 * k + 2], a[4 * k + 3]);
-            __syncwarp();
-            p16::box_store<float>(p.box, base, e.pitch, p.row0, p.rows, p.col0 + c * 32, p.cols, p.lane, true);
-            __syncwarp();
+            for (int h = 0; h < 2; ++h) {
+                const int col0 = p.col0 + c * 32 + h * 16;
+                if (p.row0 >= p.rows || col0 >= p.cols) continue;
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    *p16::box_at(p.box, p.lane, k) = make_uint4(a[16 * h + 4 * k], a[16 * h + 4 * k + 1], a[16 * h + 4 * k + 2], a[16 * h + 4 * k + 3]);
+                __syncwarp();
+                p16::box_store<float>(p.box, base, e.pitch, p.row0, p.rows, col0, p.cols, p.lane, true);
+                __syncwarp();
+            }
         }
     }
 };
@@ -311,17 +284,30 @@ row_pass_kernel(const RowPass a) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 if (residual != nullptr) v[k] = __fadd_rn(v[k], r[k]);
-                if (kAct != QFMT_ACT_NONE) v[k] = __fmul_rn(v[k], activation_slope<kAct, kPrecise>(z[k]));
-                total[k] = __fadd_rn(total[k], v[k]);
             }
+            if constexpr (kAct != QFMT_ACT_NONE) {
+#pragma unroll
+                for (int k = 0; k < 8; k += 2) {
+                    const float2 s = kPrecise ? make_float2(slope<kAct>(z[k]), slope<kAct>(z[k + 1])) : split_pair(slope2<kAct>(z[k], z[k + 1]));
+                    v[k] = __fmul_rn(v[k], s.x);
+                    v[k + 1] = __fmul_rn(v[k + 1], s.y);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) total[k] = __fadd_rn(total[k], v[k]);
         } else {
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] = __fadd_rn(v[k], bias[k]);
             if (z_out != nullptr) pass_store<T, kVec>(z_out, a.ld_z, row, col0, a.cols, lane, v);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                v[k] = activate<kAct, kPrecise>(v[k]);
-                if (residual != nullptr) v[k] = __fadd_rn(v[k], r[k]);
+            for (int k = 0; k < 8; k += 2) {
+                const float2 f = split_pair(activate2<kAct>(make_pair(v[k], v[k + 1])));
+                v[k] = f.x;
+                v[k + 1] = f.y;
+            }
+            if (residual != nullptr) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = __fadd_rn(v[k], r[k]);
             }
         }
         if (out != nullptr) pass_store<T, kVec>(out, a.ld_out, row, col0, a.cols, lane, v);

@@ -4,13 +4,15 @@
 // One persistent kernel, one CTA pair per two SMs, 256 x 256 tiles: each CTA stages its own 128 rows of op(A) and its own 128
 // columns of op(B) by TMA (64 K elements, 32 KB a stage), the leader's MMA thread issues tcgen05.mma.cta_group::2 kind::f16
 // with M = 256, N = 256, K = 16, and each CTA's tensor memory receives its 128 x 256 half of the tile.  A tile's whole
-// contraction stays in one of two 256-column accumulators, so the eight epilogue warps work on one tile while the next one is
+// contraction stays in one of two 256-column accumulators, so the sixteen epilogue warps work on one tile while the next one is
 // summed in the other.  Sums are fp32; the tensor core truncates once per 16 products, which drifts by at most (K / 16) 2^-24
 // of sum |a||b|: 2^-15 at K = 8192, below the half step of every type an epilogue rounds to (2^-12, 2^-9) and of what the loss
 // needs.  (qfmt_gemm_packed16 hands out fp32 sums and takes them in three levels instead, which costs it a third of its rate.)
 //
-// Roles: warps 0 and 3 fill alternate stages, warp 1 issues the MMAs (leader CTA), warp 2 idles, warps 4-11 run the epilogue:
-// warp w has rows 32 (w % 4) .. + 31 and columns 128 ((w - 4) / 4) .. + 127 of its CTA's half, one row a lane.
+// Roles: warps 0 and 3 fill alternate stages, warp 1 issues the MMAs (leader CTA), warp 2 idles, warps 4-19 run the epilogue:
+// warp w has rows 32 (w % 4) .. + 31 and columns 64 ((w - 4) / 4) .. + 63 of its CTA's half, one row a lane, 32 columns at a time.  (With
+// eight epilogue warps of 128 columns each an activation's epilogue took longer than a contraction over 1024 elements, waiting on its own
+// loads and conversions; 96 registers a thread are enough for 32 columns.)
 //
 // Rows may be counted on the device (ProductParams::count): tiles beyond the count are left out, and an operand that was
 // gathered is read in place if every row counts (alt).  Every wait is bounded; on expiry the status area reports
@@ -23,6 +25,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "activation.cuh"
 #include "common.cuh"
 #include "ptx.cuh"
 #include "tiles.cuh"
@@ -33,9 +36,9 @@ namespace p16 {
 constexpr int kTileM = 256, kTileN = 256, kStageK = 64;  // of a pair
 constexpr int kStages = 5;
 constexpr uint32_t kStageA = 128 * kStageK * 2, kStageB = 128 * kStageK * 2, kStageBytes = kStageA + kStageB;
-constexpr int kThreads = 384, kEpiWarps = 8;
-constexpr uint32_t kBoxBytes = 4096;       // 32 rows x 128 bytes per epilogue warp, 16-byte chunks swizzled with the row
-constexpr uint32_t kColBytes = 128 * 4;    // 128 fp32 per epilogue warp: its columns' bias
+constexpr int kThreads = 640, kEpiWarps = 16;
+constexpr uint32_t kBoxBytes = 2048;       // 32 rows x 64 bytes per epilogue warp, 16-byte chunks swizzled with the row
+constexpr uint32_t kColBytes = 64 * 4;     // 64 fp32 per epilogue warp: its columns' bias
 constexpr uint32_t kSmemBytes = kStages * kStageBytes + kEpiWarps * (kBoxBytes + kColBytes) + 256 + 1024;
 static_assert(kSmemBytes <= 232448, "shared memory");
 constexpr uint32_t kAccCols = 256, kTmemCols = 512;
@@ -58,10 +61,10 @@ struct ProductParams {
 
 // What an epilogue warp gets to see of a tile.
 struct Patch {
-    int lane, quad, warp;    // warp: 0 .. 7 of the epilogue warps
+    int lane, quad, warp;    // warp: 0 .. 15 of the epilogue warps
     int row0;                // row of lane 0; lane l has row row0 + l
     int rows;                // M as counted
-    int col0, cols;          // first of the 128 columns, N
+    int col0, cols;          // first of the 64 columns, N
     int split, tile_m, tile_n;
     uint32_t tmem;           // accumulator address of (row0, col0)
     bool empty;              // nothing was summed: the sums are zero
@@ -79,10 +82,27 @@ struct Patch {
     __device__ __forceinline__ void wait() const {
         if (!empty) ptx::tmem_load_wait();
     }
-    // The 128 columns' values of a vector (zero beyond N) into col.
+    // Block of 32 columns in pairs, complete on return; kBias: plus the columns' values.
+    template <bool kBias>
+    __device__ __forceinline__ void load_pairs(int block, pair_t (&v)[16]) const {
+        uint32_t r[32];
+        load32(block, r);
+        wait();
+#pragma unroll
+        for (int j = 0; j < 32; j += 4) {
+            v[j / 2] = make_pair(__uint_as_float(r[j]), __uint_as_float(r[j + 1]));
+            v[j / 2 + 1] = make_pair(__uint_as_float(r[j + 2]), __uint_as_float(r[j + 3]));
+            if (kBias) {
+                const float4 b = *reinterpret_cast<const float4*>(col + block * 32 + j);
+                v[j / 2] = add2(v[j / 2], make_pair(b.x, b.y));
+                v[j / 2 + 1] = add2(v[j / 2 + 1], make_pair(b.z, b.w));
+            }
+        }
+    }
+    // The 64 columns' values of a vector (zero beyond N) into col.
     __device__ __forceinline__ void load_columns(const float* v) const {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 2; ++i) {
             const int c = col0 + i * 32 + lane;
             col[i * 32 + lane] = v != nullptr && c < cols ? v[c] : 0.0f;
         }
@@ -90,24 +110,24 @@ struct Patch {
     }
 };
 
-// ---- the box: 64 columns of 16 bits or 32 of 32 bits per row, written and read a row a lane on one side and in whole
-// 128-byte rows on the other, so that global memory is touched in full lines
+// ---- the box: 32 columns of 16 bits or 16 of 32 bits per row, written and read a row a lane on one side and in whole
+// 64-byte rows on the other, so that global memory is touched in full sectors
 __device__ __forceinline__ uint4* box_at(uint8_t* box, int row, int chunk) {
-    return reinterpret_cast<uint4*>(box + row * 128 + ((chunk ^ (row & 7)) << 4));
+    return reinterpret_cast<uint4*>(box + row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4));
 }
-// box -> global.  rowmap: row r goes to row rowmap[r].  vec: base and pitch are multiples of 16 bytes.
+// box -> global.  vec: base and pitch are multiples of 16 bytes.
 template <typename T>
 __device__ __forceinline__ void box_store(uint8_t* box, T* base, int64_t ld, int row0, int rows, int col0, int cols, int lane, bool vec) {
-    constexpr int per = 16 / (int)sizeof(T), width = 128 / (int)sizeof(T);
+    constexpr int per = 16 / (int)sizeof(T), width = 64 / (int)sizeof(T);
     if (vec) {
+        const int c = lane & 3, col = col0 + c * per;
+        T* g = base + (int64_t)(row0 + (lane >> 2)) * ld + col;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int r = i * 4 + (lane >> 3), c = lane & 7, row = row0 + r, col = col0 + c * per;
-            if (row < rows && col < cols) {
-                const uint4 v = *box_at(box, r, c);
-                T* g = base + (int64_t)row * ld + col;
+        for (int i = 0; i < 4; ++i, g += 8 * ld) {
+            const int r = i * 8 + (lane >> 2);
+            if (row0 + r < rows && col < cols) {
                 if (col + per <= cols) {
-                    *reinterpret_cast<uint4*>(g) = v;
+                    *reinterpret_cast<uint4*>(g) = *box_at(box, r, c);
                 } else {
                     const T* e = reinterpret_cast<const T*>(box_at(box, r, c));
                     for (int k = 0; k < cols - col; ++k) g[k] = e[k];
@@ -115,38 +135,47 @@ __device__ __forceinline__ void box_store(uint8_t* box, T* base, int64_t ld, int
             }
         }
     } else {
-        const int r_end = rows - row0 < 32 ? rows - row0 : 32;
-        for (int r = 0; r < r_end; ++r) {
-#pragma unroll
-            for (int k = 0; k < width; k += 32) {
-                const int j = k + lane;
-                if (col0 + j < cols) base[(int64_t)(row0 + r) * ld + col0 + j] = reinterpret_cast<const T*>(box_at(box, r, j / per))[j % per];
-            }
+        constexpr int rows_at_once = 32 / width;  // one (codes) or two (fp32)
+        const int j = lane % width, r_end = rows - row0 < 32 ? rows - row0 : 32;
+        if (col0 + j < cols) {
+            T* g = base + (int64_t)(row0 + lane / width) * ld + col0 + j;
+            for (int r = lane / width; r < r_end; r += rows_at_once, g += rows_at_once * ld)
+                *g = reinterpret_cast<const T*>(box_at(box, r, j / per))[j % per];
         }
     }
 }
-// global -> box, zeros beyond the matrix
+// global -> box in two steps, so that the loads are on their way while something else is done: pieces of 16 bytes in registers (vec
+// and a whole row of the box inside the matrix), else elements when they are put.  Zeros beyond the matrix.
+struct Fetched {
+    uint4 v[4];
+};
 template <typename T>
-__device__ __forceinline__ void box_load(uint8_t* box, const T* base, int64_t ld, int row0, int rows, int col0, int cols, int lane, bool vec) {
-    constexpr int per = 16 / (int)sizeof(T), width = 128 / (int)sizeof(T);
-    if (vec && col0 + width <= cols) {
-        uint4 v[8];
+__device__ __forceinline__ bool fetch_whole(int col0, int cols, bool vec) { return vec && col0 + 64 / (int)sizeof(T) <= cols; }
+template <typename T>
+__device__ __forceinline__ void box_fetch(Fetched& f, const T* base, int64_t ld, int row0, int rows, int col0, int cols, int lane, bool vec) {
+    if (!fetch_whole<T>(col0, cols, vec)) return;
+    const T* g = base + (int64_t)(row0 + (lane >> 2)) * ld + col0 + (lane & 3) * (16 / (int)sizeof(T));
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int row = row0 + i * 4 + (lane >> 3);
-            v[i] = row < rows ? *reinterpret_cast<const uint4*>(base + (int64_t)row * ld + col0 + (lane & 7) * per) : make_uint4(0, 0, 0, 0);
-        }
+    for (int i = 0; i < 4; ++i, g += 8 * ld)
+        f.v[i] = row0 + i * 8 + (lane >> 2) < rows ? *reinterpret_cast<const uint4*>(g) : make_uint4(0, 0, 0, 0);
+}
+template <typename T>
+__device__ __forceinline__ void box_put(uint8_t* box, const Fetched& f, const T* base, int64_t ld, int row0, int rows, int col0, int cols,
+                                        int lane, bool vec) {
+    constexpr int per = 16 / (int)sizeof(T), width = 64 / (int)sizeof(T);
+    if (fetch_whole<T>(col0, cols, vec)) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) *box_at(box, i * 4 + (lane >> 3), lane & 7) = v[i];
+        for (int i = 0; i < 4; ++i) *box_at(box, i * 8 + (lane >> 2), lane & 3) = f.v[i];
     } else {
-        for (int r = 0; r < 32; ++r) {
-#pragma unroll
-            for (int k = 0; k < width; k += 32) {
-                const int j = k + lane;
-                T e = T(0.0f);
-                if (row0 + r < rows && col0 + j < cols) e = base[(int64_t)(row0 + r) * ld + col0 + j];
-                reinterpret_cast<T*>(box_at(box, r, j / per))[j % per] = e;
-            }
+        constexpr int rows_at_once = 32 / width;
+        const int j = lane % width;
+        const bool there = col0 + j < cols;
+        const T* g = base + (int64_t)(row0 + lane / width) * ld + col0 + j;
+#pragma unroll 8
+        for (int r = lane / width; r < 32; r += rows_at_once, g += rows_at_once * ld) {
+            T e = T(0.0f);
+            if (there && row0 + r < rows) e = *g;
+            reinterpret_cast<T*>(box_at(box, r, j / per))[j % per] = e;
         }
     }
 }
@@ -171,27 +200,63 @@ template <>
 __device__ __forceinline__ float2 unpack_codes<__nv_bfloat16>(uint32_t w) {
     return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
 }
-// lane's row of 64 fp32 values -> box as codes; box row -> 32 words of codes
+// the lane's row of 32 fp32 values, in pairs -> box, as codes
 template <typename T>
-__device__ __forceinline__ void box_put_codes(uint8_t* box, int lane, const float (&v)[64]) {
-#pragma unroll
-    for (int c = 0; c < 8; ++c)
-        *box_at(box, lane, c) = make_uint4(pack_codes<T>(v[c * 8], v[c * 8 + 1]), pack_codes<T>(v[c * 8 + 2], v[c * 8 + 3]),
-                                           pack_codes<T>(v[c * 8 + 4], v[c * 8 + 5]), pack_codes<T>(v[c * 8 + 6], v[c * 8 + 7]));
+__device__ __forceinline__ uint32_t pack_pair(pair_t v) {
+    const float2 f = split_pair(v);
+    return pack_codes<T>(f.x, f.y);
 }
-// Sums over the warp's 32 rows: v[j] is column j of the lane's row; lane l returns the sum of column l.  (Halving exchange:
-// each step hands half of the columns to the partner lane, 31 shuffles in all; a fixed order.)
-__device__ __forceinline__ float column_sum(float (&v)[32], int lane) {
+template <typename T>
+__device__ __forceinline__ void box_put_codes(uint8_t* box, int lane, const pair_t (&v)[16]) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const bool up = (lane & o) != 0;
+    for (int c = 0; c < 4; ++c)
+        *box_at(box, lane, c) = make_uint4(pack_pair<T>(v[c * 4]), pack_pair<T>(v[c * 4 + 1]), pack_pair<T>(v[c * 4 + 2]), pack_pair<T>(v[c * 4 + 3]));
+}
+// box -> the lane's row of 32 codes, two at a time: f(pair's index, values)
+template <typename T, typename F>
+__device__ __forceinline__ void box_each(uint8_t* box, int lane, F f) {
 #pragma unroll
-        for (int i = 0; i < o; ++i) {
-            const float give = up ? v[i] : v[i + o], keep = up ? v[i + o] : v[i];
-            v[i] = __fadd_rn(keep, __shfl_xor_sync(0xFFFFFFFFu, give, o));
-        }
+    for (int c = 0; c < 4; ++c) {
+        const uint4 w = *box_at(box, lane, c);
+        f(c * 4, unpack_codes<T>(w.x));
+        f(c * 4 + 1, unpack_codes<T>(w.y));
+        f(c * 4 + 2, unpack_codes<T>(w.z));
+        f(c * 4 + 3, unpack_codes<T>(w.w));
     }
-    return v[0];
+}
+// Sums over the warp's 32 rows of its 32 columns; lane l returns the sum of column l, in a fixed order.  Through the box, 16 columns
+// at a time: a lane puts its row, then adds two columns of eight rows, and three other lanes have the other rows.  (56 instructions;
+// exchanging halves by shuffles takes 124.)
+__device__ __forceinline__ float column_sum(uint8_t* box, int lane, const pair_t (&v)[16]) {
+    float mine = 0.0f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float2 a = split_pair(v[h * 8 + k * 2]), b = split_pair(v[h * 8 + k * 2 + 1]);
+            *reinterpret_cast<float4*>(box_at(box, lane, k)) = make_float4(a.x, a.y, b.x, b.y);
+        }
+        __syncwarp();
+        // columns 2 (lane % 8), + 1; rows lane / 8, + 4, ...: the eight lanes of a row read its 64 bytes
+        const int two = lane & 7;
+        pair_t s = 0ull;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int row = (lane >> 3) + i * 4;
+            const pair_t w = reinterpret_cast<const pair_t*>(box_at(box, row, two >> 1))[two & 1];
+            s = i == 0 ? w : add2(s, w);
+        }
+        float2 f = split_pair(s);
+        f.x = __fadd_rn(f.x, __shfl_xor_sync(0xFFFFFFFFu, f.x, 8));
+        f.y = __fadd_rn(f.y, __shfl_xor_sync(0xFFFFFFFFu, f.y, 8));
+        f.x = __fadd_rn(f.x, __shfl_xor_sync(0xFFFFFFFFu, f.x, 16));
+        f.y = __fadd_rn(f.y, __shfl_xor_sync(0xFFFFFFFFu, f.y, 16));
+        // column 16 h + c to lane 16 h + c: it is with lane c / 2, as its c % 2
+        const float x = __shfl_sync(0xFFFFFFFFu, f.x, (lane & 15) >> 1), y = __shfl_sync(0xFFFFFFFFu, f.y, (lane & 15) >> 1);
+        if ((lane >> 4) == h) mine = (lane & 1) ? y : x;
+        __syncwarp();
+    }
+    return mine;
 }
 
 __device__ __forceinline__ uint32_t make_idesc(int a_mn, int b_mn, int bf16) {
@@ -357,7 +422,7 @@ product16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         pt.col = reinterpret_cast<float*>(smem_raw + (colbufs - raw) + pt.warp * kColBytes);
         pt.rows = M;
         pt.cols = p.N;
-        const int half = pt.warp >> 2;
+        const int quarter = pt.warp >> 2;
         uint32_t it = 0;
         for (int t = first; t < items; t += pairs) {
             const int tile = t % (tiles_m * tiles_n);
@@ -367,10 +432,10 @@ product16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             pt.tile_m = tile % tiles_m;
             pt.tile_n = tile / tiles_m;
             pt.row0 = pt.tile_m * kTileM + (int)rank * 128 + pt.quad * 32;
-            pt.col0 = pt.tile_n * kTileN + half * 128;
+            pt.col0 = pt.tile_n * kTileN + quarter * 64;
             pt.empty = nkb == 0;
             const uint32_t acc = it & 1u, acc_phase = (it >> 1) & 1u;
-            pt.tmem = tmem_base + ((uint32_t)(pt.quad * 32) << 16) + acc * kAccCols + (uint32_t)half * 128u;
+            pt.tmem = tmem_base + ((uint32_t)(pt.quad * 32) << 16) + acc * kAccCols + (uint32_t)quarter * 64u;
             typename Epi::Ahead ahead;
             Epi::before(pt, ep, ahead);
             if (nkb != 0) {
