@@ -696,7 +696,8 @@ typedef struct {
 } qfmt_grad_norm_t;
 
 /*
- * norm = sqrt(sum over all tensors of (g / scale)^2), scale = d_dls->scale (1 if d_dls is NULL), squares and sums in 64 bits,
+ * norm = sqrt(sum over all tensors of (g / scale)^2), scale = d_dls->scale (1 if d_dls is NULL), summed in 64 bits (nothing overflows
+ * or vanishes on the way, relative error below 2^-21),
  * and factor = min(1, max_norm / norm) / scale.  With any infinity or NaN among the gradients norm is infinite or NaN and factor is
  * 1: such a step is to be skipped, and qfmt_grad_clip leaves its gradients as they are.
  *   max_norm   > 0; infinity only takes the loss scale out

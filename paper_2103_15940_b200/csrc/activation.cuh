@@ -63,21 +63,24 @@ struct NormalTail {
     pair_t r;   // R(|x|)
     pair_t e;   // exp(-x^2 / 2)
 };
+// (Operations with a constant are done one value at a time: a constant is part of the instruction there, a pair of them would have to
+// be put into registers first.)
+__device__ __forceinline__ float tail_polynomial(float t) {
+    float r = __fmaf_rn(-0.05299483f, t, 0.15280514f);
+    r = __fmaf_rn(r, t, -0.06571881f);
+    r = __fmaf_rn(r, t, 0.1184004f);
+    r = __fmaf_rn(r, t, 0.06339276f);
+    r = __fmaf_rn(r, t, 0.09283971f);
+    r = __fmaf_rn(r, t, 0.09552203f);
+    return __fmaf_rn(r, t, 0.0957538f);
+}
 __device__ __forceinline__ NormalTail normal_tail(float x0, float x1) {
+    const float a0 = least_abs(x0, 100.0f), a1 = least_abs(x1, 100.0f);
+    const float t0 = fast_rcp(__fmaf_rn(0.24f, a0, 1.0f)), t1 = fast_rcp(__fmaf_rn(0.24f, a1, 1.0f));
     NormalTail n;
-    n.ax = make_pair(least_abs(x0, 100.0f), least_abs(x1, 100.0f));
-    const float2 d = split_pair(fma2(both(0.24f), n.ax, both(1.0f)));
-    const pair_t t = make_pair(fast_rcp(d.x), fast_rcp(d.y));
-    pair_t r = both(-0.05299483f);
-    r = fma2(r, t, both(0.15280514f));
-    r = fma2(r, t, both(-0.06571881f));
-    r = fma2(r, t, both(0.1184004f));
-    r = fma2(r, t, both(0.06339276f));
-    r = fma2(r, t, both(0.09283971f));
-    r = fma2(r, t, both(0.09552203f));
-    r = fma2(r, t, both(0.0957538f));
-    n.r = mul2(r, t);
-    const float2 s = split_pair(mul2(mul2(n.ax, both(-0.72134752f)), n.ax));
+    n.ax = make_pair(a0, a1);
+    n.r = mul2(make_pair(tail_polynomial(t0), tail_polynomial(t1)), make_pair(t0, t1));
+    const float2 s = split_pair(mul2(make_pair(__fmul_rn(a0, -0.72134752f), __fmul_rn(a1, -0.72134752f)), n.ax));
     n.e = make_pair(fast_exp2(s.x), fast_exp2(s.y));
     return n;
 }
@@ -93,16 +96,17 @@ __device__ __forceinline__ pair_t activate2(pair_t x) {
     if (kAct == QFMT_ACT_RELU) return make_pair(v.x > 0.0f ? v.x : (v.x != v.x ? v.x : 0.0f), v.y > 0.0f ? v.y : (v.y != v.y ? v.y : 0.0f));
     if (kAct == QFMT_ACT_GELU) {  // x Phi(x) = max(x, 0) - |x| Phi(-|x|), without cancellation on either side
         const NormalTail n = normal_tail(v.x, v.y);
-        const pair_t low = mul2(mul2(n.ax, n.r), n.e);
-        return fma2(low, both(-1.0f), make_pair(fmaxf(v.x, 0.0f), fmaxf(v.y, 0.0f)));
+        const float2 low = split_pair(mul2(mul2(n.ax, n.r), n.e));
+        return make_pair(__fsub_rn(fmaxf(v.x, 0.0f), low.x), __fsub_rn(fmaxf(v.y, 0.0f), low.y));
     }
     if (kAct == QFMT_ACT_GELU_TANH || kAct == QFMT_ACT_SILU) {
-        pair_t u = mul2(x, both(-kLog2E));
-        if (kAct == QFMT_ACT_GELU_TANH)
-            u = mul2(mul2(x, both(-kGeluTanhC * kLog2E)), fma2(mul2(x, x), both(0.044715f), both(1.0f)));
-        const float2 w = split_pair(u);
-        const float2 d = split_pair(add2(make_pair(fast_exp2(w.x), fast_exp2(w.y)), both(1.0f)));
-        return mul2(x, make_pair(fast_rcp(d.x), fast_rcp(d.y)));
+        float2 u = make_float2(__fmul_rn(v.x, -kLog2E), __fmul_rn(v.y, -kLog2E));
+        if (kAct == QFMT_ACT_GELU_TANH) {
+            const float2 xx = split_pair(mul2(x, x));
+            u = split_pair(mul2(x, make_pair(__fmaf_rn(-0.044715f * kGeluTanhC * kLog2E, xx.x, -kGeluTanhC * kLog2E),
+                                             __fmaf_rn(-0.044715f * kGeluTanhC * kLog2E, xx.y, -kGeluTanhC * kLog2E))));
+        }
+        return mul2(x, make_pair(fast_rcp(__fadd_rn(1.0f, fast_exp2(u.x))), fast_rcp(__fadd_rn(1.0f, fast_exp2(u.y)))));
     }
     return x;
 }
@@ -112,26 +116,27 @@ __device__ __forceinline__ pair_t slope2(float x0, float x1) {
     if (kAct == QFMT_ACT_RELU) return make_pair(x0 > 0.0f ? 1.0f : (x0 != x0 ? x0 : 0.0f), x1 > 0.0f ? 1.0f : (x1 != x1 ? x1 : 0.0f));
     if (kAct == QFMT_ACT_GELU) {  // h = Phi(-|x|) - |x| phi(x) is the slope at -|x|, 1 - h the one at |x|
         const NormalTail n = normal_tail(x0, x1);
-        const pair_t h = mul2(fma2(n.ax, both(-0.39894228f), n.r), n.e);
-        const float2 lo = split_pair(h), hi = split_pair(fma2(h, both(-1.0f), both(1.0f)));
-        return make_pair(x0 < 0.0f ? lo.x : hi.x, x1 < 0.0f ? lo.y : hi.y);
+        const float2 ax = split_pair(n.ax), r = split_pair(n.r);
+        const float2 h = split_pair(mul2(make_pair(__fmaf_rn(ax.x, -0.39894228f, r.x), __fmaf_rn(ax.y, -0.39894228f, r.y)), n.e));
+        return make_pair(x0 < 0.0f ? h.x : __fsub_rn(1.0f, h.x), x1 < 0.0f ? h.y : __fsub_rn(1.0f, h.y));
     }
     if (kAct == QFMT_ACT_GELU_TANH || kAct == QFMT_ACT_SILU) {
         // at -|x| the slope is a r - |x| u'(x) a r r, at |x| it is 1 minus that; |x| at most 100 as above
-        const pair_t ax = make_pair(least_abs(x0, 100.0f), least_abs(x1, 100.0f));
-        pair_t u = ax, xdu = ax;
+        const float a0 = least_abs(x0, 100.0f), a1 = least_abs(x1, 100.0f);
+        const pair_t ax = make_pair(a0, a1);
+        pair_t xdu = ax;
+        float2 w = make_float2(__fmul_rn(a0, -kLog2E), __fmul_rn(a1, -kLog2E));
         if (kAct == QFMT_ACT_GELU_TANH) {
-            const pair_t xx = mul2(ax, ax), cx = mul2(ax, both(kGeluTanhC));
-            u = mul2(cx, fma2(xx, both(0.044715f), both(1.0f)));
-            xdu = mul2(cx, fma2(xx, both(3.0f * 0.044715f), both(1.0f)));
+            const float2 xx = split_pair(mul2(ax, ax));
+            w = split_pair(mul2(ax, make_pair(__fmaf_rn(-0.044715f * kGeluTanhC * kLog2E, xx.x, -kGeluTanhC * kLog2E),
+                                              __fmaf_rn(-0.044715f * kGeluTanhC * kLog2E, xx.y, -kGeluTanhC * kLog2E))));
+            xdu = mul2(ax, make_pair(__fmaf_rn(3.0f * 0.044715f * kGeluTanhC, xx.x, kGeluTanhC), __fmaf_rn(3.0f * 0.044715f * kGeluTanhC, xx.y, kGeluTanhC)));
         }
-        const float2 w = split_pair(mul2(u, both(-kLog2E)));
-        const pair_t a = make_pair(fast_exp2(w.x), fast_exp2(w.y));
-        const float2 d = split_pair(add2(a, both(1.0f)));
-        const pair_t r = make_pair(fast_rcp(d.x), fast_rcp(d.y)), ar = mul2(a, r);
-        const pair_t h = mul2(ar, fma2(mul2(xdu, r), both(-1.0f), both(1.0f)));
-        const float2 lo = split_pair(h), hi = split_pair(fma2(h, both(-1.0f), both(1.0f)));
-        return make_pair(x0 < 0.0f ? lo.x : hi.x, x1 < 0.0f ? lo.y : hi.y);
+        const float e0 = fast_exp2(w.x), e1 = fast_exp2(w.y);
+        const pair_t r = make_pair(fast_rcp(__fadd_rn(1.0f, e0)), fast_rcp(__fadd_rn(1.0f, e1)));
+        const float2 xr = split_pair(mul2(xdu, r));
+        const float2 h = split_pair(mul2(mul2(make_pair(e0, e1), r), make_pair(__fsub_rn(1.0f, xr.x), __fsub_rn(1.0f, xr.y))));
+        return make_pair(x0 < 0.0f ? h.x : __fsub_rn(1.0f, h.x), x1 < 0.0f ? h.y : __fsub_rn(1.0f, h.y));
     }
     return both(1.0f);
 }

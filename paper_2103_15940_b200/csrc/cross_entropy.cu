@@ -57,7 +57,7 @@ struct Compact {
     int rows_per_block;
 };
 
-constexpr int kCompactThreads = 256;
+constexpr int kCompactThreads = 1024;  // a warp a row of a block's 32, so that the copies of all are on their way at once
 
 template <typename V>
 __device__ __forceinline__ V block_sum(V v, V* scratch) {  // scratch: one per warp; every thread gets the sum
@@ -65,8 +65,8 @@ __device__ __forceinline__ V block_sum(V v, V* scratch) {  // scratch: one per w
     __syncthreads();
     if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
     __syncthreads();
-    v = scratch[0];
-    for (int w = 1; w < kCompactThreads / 32; ++w) v += scratch[w];
+    v = scratch[threadIdx.x & 31];
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
     return v;
 }
 
@@ -84,7 +84,7 @@ compact_kernel(const Compact c, unsigned long long* status, unsigned long long t
     const int first = (int)blockIdx.x * c.rows_per_block;
     const int end = first + c.rows_per_block < c.rows ? first + c.rows_per_block : c.rows;
     int before = 0, total = 0;
-#pragma unroll 4
+#pragma unroll 8
     for (int i = tid; i < c.rows; i += kCompactThreads) {
         const int counts = c.targets[i] != c.ignore ? 1 : 0;
         total += counts;
@@ -132,11 +132,13 @@ compact_kernel(const Compact c, unsigned long long* status, unsigned long long t
         __syncthreads();
         if (lane == 0) scratch[warp] = __popc(mask);
         __syncthreads();
-        int at = before + __popc(mask & ((1u << lane) - 1u));
-        for (int w = 0; w < kCompactThreads / 32; ++w) {
-            if (w < warp) at += scratch[w];
-            before += scratch[w];
+        int sum = scratch[lane];  // of the warps up to this lane's
+        for (int o = 1; o < 32; o <<= 1) {
+            const int below = __shfl_up_sync(0xFFFFFFFFu, sum, o);
+            if (lane >= o) sum += below;
         }
+        const int at = before + __shfl_sync(0xFFFFFFFFu, sum, warp) - __popc(mask) + __popc(mask & ((1u << lane) - 1u));
+        before += __shfl_sync(0xFFFFFFFFu, sum, 31);
         place[tid] = counts ? at : -1;
         if (counts) {
             c.index[at] = row;
@@ -423,14 +425,15 @@ struct AddEpilogue {
 
 // ---- joining ----------------------------------------------------------------------------------------------------------------
 
-constexpr int kJoinRows = 32, kJoinParts = 8;
+constexpr int kJoinRows = 32, kJoinParts = 32;
 
-// Block of 32 rows x 8 groups: group q joins a row's parts q, q + 8, ..., then the eight are joined in order.
+// Block of 32 rows x 32 groups: group q joins a row's parts q, q + 32, ..., then a warp a row joins the groups' (halves onto halves).
 __global__ void __launch_bounds__(kJoinRows * kJoinParts)
 join_rows_kernel(const float2* __restrict__ parts, int64_t pitch, int n_parts, const Found* found, const int* __restrict__ index,
                  const int* __restrict__ target, const float* __restrict__ picked, float* loss, float* lse_out, float* compact_loss,
                  float* mean) {
-    __shared__ float2 joined[kJoinParts][kJoinRows];
+    __shared__ float2 joined[kJoinParts][kJoinRows + 1];
+    __shared__ float losses[kJoinRows];
     const int r = threadIdx.x % kJoinRows, q = threadIdx.x / kJoinRows, row = (int)blockIdx.x * kJoinRows + r;
     grid_dependency_wait();
     grid_launch_dependents();
@@ -451,20 +454,29 @@ join_rows_kernel(const float2* __restrict__ parts, int64_t pitch, int n_parts, c
     }
     joined[q][r] = make_float2(m, s);
     __syncthreads();
-    if (q != 0) return;
-    float l = 0.0f;
-    if (row < count) {
-        for (int i = 1; i < kJoinParts; ++i) join(joined[i][r]);
-        float lse = __fadd_rn(m, logf(s));
-        l = __fsub_rn(lse, picked[row]);
-        if (target[row] < 0) l = lse = __int_as_float(0x7FC00000);  // the target is not a word
-        const int to = index[row];
-        if (loss != nullptr) loss[to] = l;
-        if (lse_out != nullptr) lse_out[to] = lse;
-        if (compact_loss != nullptr) compact_loss[row] = l;
+    // now thread (r, q) is lane r of warp q: the warp has row q of the block, the lane group r
+    const int mine = (int)blockIdx.x * kJoinRows + q;
+    float2 v = joined[r][q];
+    m = v.x;
+    s = v.y;
+    for (int o = 16; o > 0; o >>= 1) join(make_float2(__shfl_xor_sync(0xFFFFFFFFu, m, o), __shfl_xor_sync(0xFFFFFFFFu, s, o)));
+    if (r == 0) {
+        float l = 0.0f;
+        if (mine < count) {
+            float lse = __fadd_rn(m, logf(s));
+            l = __fsub_rn(lse, picked[mine]);
+            if (target[mine] < 0) l = lse = __int_as_float(0x7FC00000);  // the target is not a word
+            const int to = index[mine];
+            if (loss != nullptr) loss[to] = l;
+            if (lse_out != nullptr) lse_out[to] = lse;
+            if (compact_loss != nullptr) compact_loss[mine] = l;
+        }
+        losses[q] = l;
     }
-    if (mean != nullptr) {  // the only block
-        double total = l;
+    if (mean == nullptr) return;  // else this is the only block
+    __syncthreads();
+    if (q == 0) {
+        double total = losses[r];
         for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
         if (r == 0) *mean = (float)(total / (count > 0 ? count : 1));
     }
@@ -487,34 +499,36 @@ mean_kernel(const float* __restrict__ loss, const Found* found, float* mean) {
     }
 }
 
-// dH: the splits of a compact row added in order, scaled back, rounded and put where the row came from.  A warp a row.
+// dH: the splits of a compact row added in order, scaled back, rounded and put where the row came from.  A warp 128 columns of a row
+// at a time.
 template <typename T>
 __global__ void __launch_bounds__(256)
 scatter_kernel(const float* __restrict__ sums, int splits, int64_t split_stride, int64_t pitch, const Found* found,
                const int* __restrict__ index, T* dh, int64_t ld, int hidden, int vec) {
     grid_dependency_wait();
     grid_launch_dependents();
-    const int lane = threadIdx.x & 31;
-    const int count = found->count;
+    const int lane = threadIdx.x & 31, chunks = (hidden + 127) / 128;
+    const int64_t units = (int64_t)found->count * chunks;
     const float factor = found->unscale;
-    for (int row = (int)(blockIdx.x * 8 + (threadIdx.x >> 5)); row < count; row += (int)gridDim.x * 8) {
-        const float* src = sums + (int64_t)row * pitch;
-        T* dst = dh + (int64_t)index[row] * ld;
-        for (int j = lane * 4; j < hidden; j += 128) {
-            float4 v = *reinterpret_cast<const float4*>(src + j);  // rows are padded to whole pieces
-            for (int s = 1; s < splits; ++s) {
-                const float4 w = *reinterpret_cast<const float4*>(src + s * split_stride + j);
-                v = make_float4(__fadd_rn(v.x, w.x), __fadd_rn(v.y, w.y), __fadd_rn(v.z, w.z), __fadd_rn(v.w, w.w));
-            }
-            const uint32_t lo = p16::pack_codes<T>(__fmul_rn(v.x, factor), __fmul_rn(v.y, factor));
-            const uint32_t hi = p16::pack_codes<T>(__fmul_rn(v.z, factor), __fmul_rn(v.w, factor));
-            if (vec && j + 4 <= hidden) {
-                *reinterpret_cast<uint2*>(dst + j) = make_uint2(lo, hi);
-            } else {
-                const uint32_t words[2] = {lo, hi};
-                const T* e = reinterpret_cast<const T*>(words);
-                for (int k = 0; k < 4 && j + k < hidden; ++k) dst[j + k] = e[k];
-            }
+    for (int64_t u = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); u < units; u += (int64_t)gridDim.x * 8) {
+        const int row = (int)(u / chunks), j = (int)(u % chunks) * 128 + lane * 4;
+        if (j >= hidden) continue;
+        const float* src = sums + (int64_t)row * pitch + j;  // rows are padded to whole pieces
+        T* dst = dh + (int64_t)index[row] * ld + j;
+        float4 v = *reinterpret_cast<const float4*>(src);
+#pragma unroll 8
+        for (int s = 1; s < splits; ++s) {
+            const float4 w = *reinterpret_cast<const float4*>(src + s * split_stride);
+            v = make_float4(__fadd_rn(v.x, w.x), __fadd_rn(v.y, w.y), __fadd_rn(v.z, w.z), __fadd_rn(v.w, w.w));
+        }
+        const uint32_t lo = p16::pack_codes<T>(__fmul_rn(v.x, factor), __fmul_rn(v.y, factor));
+        const uint32_t hi = p16::pack_codes<T>(__fmul_rn(v.z, factor), __fmul_rn(v.w, factor));
+        if (vec && j + 4 <= hidden) {
+            *reinterpret_cast<uint2*>(dst) = make_uint2(lo, hi);
+        } else {
+            const uint32_t words[2] = {lo, hi};
+            const T* e = reinterpret_cast<const T*>(words);
+            for (int k = 0; k < 4 && j + k < hidden; ++k) dst[k] = e[k];
         }
     }
 }
@@ -543,8 +557,9 @@ int loss_sizes(const qfmt_matrix16_t* H, const qfmt_matrix16_t* W, Sizes* s) {
 }
 
 // How the backward pass walks the vocabulary.  A piece's d (rows x piece, 2 bytes each) should stay in the second-level cache (126 MB)
-// between the product that writes it and the two that read it; and pieces of at least 1024 words keep those products whole.
-constexpr int64_t kPieceBytes = 64ll << 20;
+// between the product that writes it and the two that read it; and pieces of at least 1024 words keep those products whole.  Within
+// that a piece has as many 256-word tiles as let the weight gradient's tiles fill whole rounds of the CTA pairs.
+constexpr int64_t kPieceBytes = 80ll << 20;
 constexpr int64_t kPairs = 74, kMostSplits = 16, kLeastStages = 4;
 struct Plan {
     int64_t tile_rows;   // rows of whole tiles
@@ -555,10 +570,15 @@ struct Plan {
 Plan plan_backward(const Sizes& s) {
     Plan p;
     p.tile_rows = up(s.rows > 0 ? s.rows : 1, p16::kTileM);
-    int64_t most = kPieceBytes / (p.tile_rows * 2) / p16::kTileN * p16::kTileN;
-    if (most < 1024) most = 1024;
-    const int64_t pieces = (s.vocab + most - 1) / most;
-    p.piece = up((s.vocab + pieces - 1) / pieces, p16::kTileN);
+    int64_t most = kPieceBytes / (p.tile_rows * 2) / p16::kTileN;  // tiles of words
+    if (most < 4) most = 4;
+    const int64_t all = (s.vocab + p16::kTileN - 1) / p16::kTileN, across = up(s.hidden, p16::kTileN) / p16::kTileN;
+    if (most < all) {
+        const int64_t fill = most * across / kPairs * kPairs / across;  // the most whose tiles make whole rounds
+        if (fill > 0) most = fill;
+    }
+    const int64_t pieces = (all + most - 1) / most;
+    p.piece = (all + pieces - 1) / pieces * p16::kTileN;
     p.pitch_h = up(s.hidden, 8);
     const int64_t tiles = p.tile_rows / p16::kTileM * (up(s.hidden, p16::kTileN) / p16::kTileN), stages = p.piece / p16::kStageK;
     int64_t n = kPairs / tiles;
@@ -730,7 +750,7 @@ int backward_pieces(const qfmt_matrix16_t* W, const float* d_bias, const Sizes& 
         }
     }
     if (d_dh != nullptr) {
-        const int64_t want = (s.rows + 7) / 8, most = (int64_t)dev.sm_count * 8;
+        const int64_t want = (s.rows * ((s.hidden + 127) / 128) + 7) / 8, most = (int64_t)dev.sm_count * 8;
         QFMT_CUDA_TRY(launch_overlapping(scatter_kernel<T>, (unsigned)(want < most ? want : most), 256u, 0, stream, (const float*)sums, plan.splits,
                                          s.rows * plan.pitch_h, plan.pitch_h, found, (const int*)at<int>(ws, pl.index), static_cast<T*>(d_dh),
                                          ld_dh, (int)s.hidden, (int)(!misaligned(d_dh, 8) && ld_dh % 4 == 0)));

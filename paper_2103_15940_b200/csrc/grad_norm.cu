@@ -1,8 +1,8 @@
 // The global norm of a list of tensors and clipping by it:
 //     norm = sqrt(sum (g / scale)^2),  dst = src min(1, max_norm / norm) / scale.
 //
-// Squares and sums are in 64 bits: the square of any 32-bit value is exact and finite there, so nothing overflows or vanishes and a
-// sum is not finite exactly if an element is not.  Only then are elements looked at one by one for the counts.
+// Sums are in 64 bits, and squares too unless eight of codes add up in 32 bits without leaving its range: the square of any 32-bit
+// value is exact and finite in 64 bits, so nothing overflows or vanishes and a sum is not finite exactly if an element is not.  Only then are elements looked at one by one for the counts.
 //
 // The list's chunks (at most 8192 elements of one tensor) form one sequence, cut into equal ranges among the blocks; a block finds its
 // first tensor by bisection and walks on from there.  Every block leaves one partial sum and one more block adds those up, so the order
@@ -19,7 +19,7 @@
 namespace qfmt {
 namespace {
 
-constexpr int kChunk = 8192, kThreads = 256, kBlocksPerSm = 8;
+constexpr int kChunk = 8192, kThreads = 256, kBlocksPerSm = 6;
 
 struct Partial {
     double sum;
@@ -63,12 +63,17 @@ struct Walk {
     long long chunk, end;
     int tensor;
 };
+// The last tensor whose first chunk is not behind `chunk` (empty tensors share theirs with the next).  Each step of the search looks at
+// 32 places at once, a lane each: a list of a thousand tensors takes two dependent loads, not ten.
 __device__ __forceinline__ int tensor_of(const qfmt_tensor_t* tensors, int count, long long chunk) {
-    int lo = 0, hi = count - 1;  // the last tensor whose first chunk is not behind `chunk` (empty tensors share theirs with the next)
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (tensors[mid].first_chunk <= chunk) lo = mid;
-        else hi = mid - 1;
+    const int lane = threadIdx.x & 31;
+    int lo = 0, n = count;  // the answer is in lo .. lo + n - 1
+    while (n > 1) {
+        const int step = (n + 31) / 32, at = lane * step;
+        const bool here = at < n && tensors[lo + at].first_chunk <= chunk;
+        const int last = 31 - __clz(__ballot_sync(0xFFFFFFFFu, here) | 1u);
+        lo += last * step;
+        n = n - last * step < step ? n - last * step : step;
     }
     return lo;
 }
@@ -90,15 +95,36 @@ __device__ __forceinline__ void chunk_square(const T* p, int n, Partial& total) 
         const double x = (double)(float)p[tail + tid];
         s1 = x * x;
     }
-#pragma unroll 4
-    for (int i = tid; i < pieces; i += kThreads) {
-        float v[per];
-        unpack16<T>(body[i], v);
+    for (int i0 = tid; i0 < pieces; i0 += 4 * kThreads) {
+        uint4 w[4];
 #pragma unroll
-        for (int k = 0; k < per; k += 2) {
-            const double a = (double)v[k], b = (double)v[k + 1];
-            s0 = __fma_rn(a, a, s0);
-            s1 = __fma_rn(b, b, s1);
+        for (int j = 0; j < 4; ++j) w[j] = i0 + j * kThreads < pieces ? body[i0 + j * kThreads] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float v[per];
+            unpack16<T>(w[j], v);
+            if constexpr (sizeof(T) == 2) {
+                // Eight squares in 32 bits (a code's square is exact there, the sum off by 2^-22 at most) where they are in range:
+                // conversions to 64 bits take eight times as long as the additions, and one for eight codes keeps up with memory.
+                float q0 = __fmul_rn(v[0], v[0]), q1 = __fmul_rn(v[1], v[1]);
+#pragma unroll
+                for (int k = 2; k < per; k += 2) {
+                    q0 = __fmaf_rn(v[k], v[k], q0);
+                    q1 = __fmaf_rn(v[k + 1], v[k + 1], q1);
+                }
+                const float q = __fadd_rn(q0, q1);
+                const bool zero = ((w[j].x | w[j].y | w[j].z | w[j].w) & 0x7FFF7FFFu) == 0u;
+                if ((q >= 1e-25f && q <= 1e37f) || zero) {
+                    s0 += (double)q;
+                    continue;
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < per; k += 2) {
+                const double a = (double)v[k], b = (double)v[k + 1];
+                s0 = __fma_rn(a, a, s0);
+                s1 = __fma_rn(b, b, s1);
+            }
         }
     }
     const double s = s0 + s1;
@@ -115,7 +141,7 @@ __device__ __forceinline__ void chunk_square(const T* p, int n, Partial& total) 
     total.sum += s;
 }
 
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm)
 norm_kernel(const qfmt_tensor_t* __restrict__ tensors, int count, long long chunks, Partial* __restrict__ partials) {
     __shared__ Partial sums[kThreads / 32];
     grid_dependency_wait();
@@ -230,7 +256,7 @@ __device__ __forceinline__ void chunk_scale(const T* p, T* q, int n, float facto
     }
 }
 
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm)
 clip_kernel(const qfmt_tensor_t* tensors, int count, long long chunks, const qfmt_grad_norm_t* norm) {
     grid_dependency_wait();
     grid_launch_dependents();

@@ -189,29 +189,26 @@ struct RowPass {
 template <typename T, bool kVec>
 __device__ __forceinline__ int64_t pass_col(int lane, int k) { return kVec ? lane * 8 + k : k * 32 + lane; }
 
+// A lane's eight elements of a row; `p` is the row's first element of the strip and `there` says which of them exist (bit k; in
+// whole pieces all or none).
 template <typename T, bool kVec>
-__device__ __forceinline__ void pass_load(const T* base, int64_t ld, int64_t row, int64_t col0, int64_t cols, int lane, float (&v)[8]) {
+__device__ __forceinline__ void pass_load(const T* p, unsigned there, int lane, float (&v)[8]) {
     if (kVec) {
-        const T* p = base + row * ld + col0 + lane * 8;
-        if (col0 + lane * 8 >= cols) {
+        if (!there) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] = 0.0f;
-        } else if (sizeof(T) == 4) {
-            const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-            v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
         } else {
-            const uint4 w = *reinterpret_cast<const uint4*>(p);
-            const T* e = reinterpret_cast<const T*>(&w);
+            const uint4* q = reinterpret_cast<const uint4*>(p + lane * 8);
+            uint4 w[sizeof(T) / 2];
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = q[i];
+            const T* e = reinterpret_cast<const T*>(w);
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] = (float)e[k];
         }
     } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int64_t col = col0 + k * 32 + lane;
-            v[k] = col < cols ? (float)base[row * ld + col] : 0.0f;
-        }
+        for (int k = 0; k < 8; ++k) v[k] = (there >> k) & 1u ? (float)p[k * 32 + lane] : 0.0f;
     }
 }
 __device__ __forceinline__ float to_type(float v, float) { return v; }
@@ -219,33 +216,29 @@ __device__ __forceinline__ __half to_type(float v, __half) { return __float2half
 __device__ __forceinline__ __nv_bfloat16 to_type(float v, __nv_bfloat16) { return __float2bfloat16_rn(v); }
 
 template <typename T, bool kVec>
-__device__ __forceinline__ void pass_store(T* base, int64_t ld, int64_t row, int64_t col0, int64_t cols, int lane, const float (&v)[8]) {
+__device__ __forceinline__ void pass_store(T* p, unsigned there, int lane, const float (&v)[8]) {
     if (kVec) {
-        T* p = base + row * ld + col0 + lane * 8;
-        if (col0 + lane * 8 >= cols) return;
-        if (sizeof(T) == 4) {
-            reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-            reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
-        } else {
-            uint4 w;
-            T* e = reinterpret_cast<T*>(&w);
+        if (!there) return;
+        uint4 w[sizeof(T) / 2];
+        T* e = reinterpret_cast<T*>(w);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) e[k] = to_type(v[k], T());
-            *reinterpret_cast<uint4*>(p) = w;
-        }
+        for (int k = 0; k < 8; ++k) e[k] = to_type(v[k], T());
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(p + lane * 8)[i] = w[i];
     } else {
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const int64_t col = col0 + k * 32 + lane;
-            if (col < cols) base[row * ld + col] = to_type(v[k], T());
+            if ((there >> k) & 1u) p[k * 32 + lane] = to_type(v[k], T());
         }
     }
 }
 
-constexpr int kPassWarps = 8;
+constexpr int kPassWarps = 8, kPassPerSm = 6;
 
+// At most 40 registers for whole pieces of a gradient: forty-eight warps an SM hide the loads behind one another's arithmetic, and a row fetched ahead or two rows at a
+// time, with fewer warps, do not (54 us of 8192 x 4096 bfloat16 with the next row in registers).
 template <typename T, int kAct, bool kBackward, bool kParts, bool kVec>
-__global__ void __launch_bounds__(kPassWarps * 32)
+__global__ void __launch_bounds__(kPassWarps * 32, kVec && !kParts ? kPassPerSm : 4)
 row_pass_kernel(const RowPass a) {
     constexpr bool kPrecise = sizeof(T) == 4;
     __shared__ float sums[kPassWarps][256];
@@ -253,52 +246,64 @@ row_pass_kernel(const RowPass a) {
     const int64_t col0 = (int64_t)(blockIdx.x % a.strips) * 256;
     const int64_t block = blockIdx.x / a.strips, first = block * a.rows_per_block;
     const int64_t end = first + a.rows_per_block < a.rows ? first + a.rows_per_block : a.rows;
+    unsigned there = 0u;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) there |= col0 + pass_col<T, kVec>(lane, k) < a.cols ? 1u << k : 0u;
     grid_dependency_wait();
     grid_launch_dependents();
     float bias[8], total[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        const int64_t col = col0 + pass_col<T, kVec>(lane, k);
-        bias[k] = !kBackward && a.bias != nullptr && col < a.cols ? a.bias[col] : 0.0f;
+        bias[k] = !kBackward && a.bias != nullptr && ((there >> k) & 1u) ? a.bias[col0 + pass_col<T, kVec>(lane, k)] : 0.0f;
         total[k] = 0.0f;
     }
-    const T *dy = static_cast<const T*>(a.dy), *residual = static_cast<const T*>(a.residual), *z_in = static_cast<const T*>(a.z_in);
+    const T *residual = static_cast<const T*>(a.residual), *z_in = static_cast<const T*>(a.z_in);
     T *out = static_cast<T*>(a.out), *z_out = static_cast<T*>(a.z_out);
-#pragma unroll 2
+#pragma unroll 1
     for (int64_t row = first + warp; row < end; row += kPassWarps) {
-        float v[8], z[8], r[8];
-        if (kBackward && kAct != QFMT_ACT_NONE) pass_load<T, kVec>(z_in, a.ld_z, row, col0, a.cols, lane, z);
+        float v[8];
         if constexpr (kParts) {
-            pass_load<float, kVec>(a.parts, a.pitch, row, col0, a.cols, lane, v);
+            const float* part = a.parts + row * a.pitch + col0;
+            pass_load<float, kVec>(part, there, lane, v);
+#pragma unroll 2
             for (int s = 1; s < a.splits; ++s) {
                 float w[8];
-                pass_load<float, kVec>(a.parts + s * a.split_stride, a.pitch, row, col0, a.cols, lane, w);
+                part += a.split_stride;
+                pass_load<float, kVec>(part, there, lane, w);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) v[k] = __fadd_rn(v[k], w[k]);
             }
         } else {
-            pass_load<T, kVec>(dy, a.ld_dy, row, col0, a.cols, lane, v);
+            pass_load<T, kVec>(static_cast<const T*>(a.dy) + row * a.ld_dy + col0, there, lane, v);
         }
-        if (residual != nullptr) pass_load<T, kVec>(residual, a.ld_residual, row, col0, a.cols, lane, r);
+        float r[8];
         if (kBackward) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                if (residual != nullptr) v[k] = __fadd_rn(v[k], r[k]);
-            }
             if constexpr (kAct != QFMT_ACT_NONE) {
+                float z[8];
+                pass_load<T, kVec>(z_in + row * a.ld_z + col0, there, lane, z);
+                if (residual != nullptr) {
+                    pass_load<T, kVec>(residual + row * a.ld_residual + col0, there, lane, r);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) v[k] = __fadd_rn(v[k], r[k]);
+                }
 #pragma unroll
                 for (int k = 0; k < 8; k += 2) {
                     const float2 s = kPrecise ? make_float2(slope<kAct>(z[k]), slope<kAct>(z[k + 1])) : split_pair(slope2<kAct>(z[k], z[k + 1]));
                     v[k] = __fmul_rn(v[k], s.x);
                     v[k + 1] = __fmul_rn(v[k + 1], s.y);
                 }
+            } else if (residual != nullptr) {
+                pass_load<T, kVec>(residual + row * a.ld_residual + col0, there, lane, r);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = __fadd_rn(v[k], r[k]);
             }
 #pragma unroll
             for (int k = 0; k < 8; ++k) total[k] = __fadd_rn(total[k], v[k]);
         } else {
+            if (residual != nullptr) pass_load<T, kVec>(residual + row * a.ld_residual + col0, there, lane, r);
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] = __fadd_rn(v[k], bias[k]);
-            if (z_out != nullptr) pass_store<T, kVec>(z_out, a.ld_z, row, col0, a.cols, lane, v);
+            if (z_out != nullptr) pass_store<T, kVec>(z_out + row * a.ld_z + col0, there, lane, v);
 #pragma unroll
             for (int k = 0; k < 8; k += 2) {
                 const float2 f = split_pair(activate2<kAct>(make_pair(v[k], v[k + 1])));
@@ -310,7 +315,7 @@ row_pass_kernel(const RowPass a) {
                 for (int k = 0; k < 8; ++k) v[k] = __fadd_rn(v[k], r[k]);
             }
         }
-        if (out != nullptr) pass_store<T, kVec>(out, a.ld_out, row, col0, a.cols, lane, v);
+        if (out != nullptr) pass_store<T, kVec>(out + row * a.ld_out + col0, there, lane, v);
     }
     if constexpr (kBackward) {
         if (a.sums == nullptr) return;
@@ -331,10 +336,12 @@ row_pass_kernel(const RowPass a) {
 // Columns of fp32 working matrices are padded so that rows start on 32 bytes.
 int64_t padded(int64_t cols) { return (cols + 7) / 8 * 8; }
 
-// Blocks of rows of a pass: enough blocks to fill the GPU a few times over, none of fewer than 32 rows (four a warp).
-constexpr int64_t kPassBlocks = 148 * 6;
+// Blocks of rows of a pass: as many blocks as are on the GPU at a time, none of fewer than eight rows (one a warp).
+constexpr int64_t kPassBlocks = 148 * kPassPerSm;
 int64_t pass_row_blocks(int64_t rows, int64_t cols) {
-    const int64_t strips = (cols + 255) / 256, want = (kPassBlocks + strips - 1) / strips, most = (rows + 31) / 32;
+    const int64_t strips = (cols + 255) / 256, most = (rows + 7) / 8;
+    int64_t want = kPassBlocks / strips;
+    if (want < 1) want = 1;
     return want < most ? want : most;
 }
 
@@ -383,8 +390,9 @@ int plan_splits(const Shape& s) {
 }
 
 constexpr size_t kHeader = 256;
-size_t sums_bytes(const Shape& s) {  // column sums by groups of 32 rows of whole tiles: more than a pass over rows leaves
-    return (size_t)((s.M + p16::kTileM - 1) / p16::kTileM) * 8 * (size_t)padded(s.N) * sizeof(float);
+size_t sums_bytes(const Shape& s) {  // column sums by groups of 32 rows of whole tiles, or by the row blocks of a pass
+    const int64_t groups = (s.M + p16::kTileM - 1) / p16::kTileM * 8, blocks = s.N > 0 ? pass_row_blocks(s.M, s.N) : 0;
+    return (size_t)(groups > blocks ? groups : blocks) * (size_t)padded(s.N) * sizeof(float);
 }
 size_t part_bytes(const Shape& s, int splits) { return (size_t)splits * (size_t)s.M * (size_t)padded(s.N) * sizeof(float); }
 
