@@ -17,6 +17,7 @@
 #include "columns.cuh"
 #include "common.cuh"
 #include "product16.cuh"
+#include "skinny16.cuh"
 
 namespace qfmt {
 namespace {
@@ -533,6 +534,163 @@ scatter_kernel(const float* __restrict__ sums, int splits, int64_t split_stride,
     }
 }
 
+// ---- at most 32 rows --------------------------------------------------------------------------------------------------------
+// The forward pass as a pass over W: a warp takes 16 words (W stored by word) or 64 at a time and the whole of K, and keeps a maximum
+// and a sum for every row that a lane's words belong to; the block leaves one pair a row.  Rows that do not count ride along.
+struct FewRows {
+    skinny::Operands o;
+    const float* bias;
+    const int64_t* targets;
+    float2* parts;  // [blocks][rows]
+    float* picked;
+    unsigned long long* status;
+    unsigned long long tag;
+};
+constexpr int kFewWarps = 2, kFirst = 256;  // K elements that are asked for ahead of the kernel before
+
+struct Running {  // sum exp(logit - most)
+    float most = -INFINITY, sum = 0.0f;
+    __device__ __forceinline__ void join(float m, float s) {
+        const float now = fmaxf(most, m);
+        if (now == -INFINITY) {
+            sum = __fadd_rn(sum, s);  // zero, or NaN where all logits are
+            return;
+        }
+        sum = __fmaf_rn(s, fast_exp2(__fmul_rn(__fsub_rn(m, now), kLog2E)), __fmul_rn(sum, fast_exp2(__fmul_rn(__fsub_rn(most, now), kLog2E))));
+        most = now;
+    }
+    __device__ __forceinline__ void add(float logit) { join(logit, logit == -INFINITY ? 0.0f : logit != logit ? logit : 1.0f); }
+};
+
+template <bool kBf16, bool kByK, int kBlocks>
+__global__ void __launch_bounds__(kFewWarps * 32, 8)
+few_rows_kernel(const FewRows f) {
+    constexpr int kWords = kByK ? 64 : 16, kRows = kByK ? 16 * kBlocks : 8 * kBlocks, kLane = 2 * kBlocks;  // rows of a lane
+    __shared__ float2 joined[kFewWarps][kRows];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    const int groups = (f.o.n + kWords - 1) / kWords;
+    {
+        const int n0 = ((int)blockIdx.x * kFewWarps + warp) * kWords;
+        if (n0 < f.o.n) skinny::prefetch_weights<kByK>(f.o, n0, 0, f.o.k < kFirst ? f.o.k : kFirst, lane);
+    }
+    grid_dependency_wait();
+    grid_launch_dependents();
+    announce_launch(f.status, f.tag);
+    auto row_of = [&](int j) { return kByK ? (j >> 1) * 16 + (j & 1) * 8 + g : (j >> 1) * 8 + 2 * t + (j & 1); };
+    int target[kLane];
+    Running run[kLane];
+#pragma unroll
+    for (int j = 0; j < kLane; ++j) {
+        const int64_t word = row_of(j) < f.o.rows ? f.targets[row_of(j)] : -1;
+        target[j] = word >= 0 && word < f.o.n ? (int)word : -1;
+    }
+    auto take = [&](int j, int word, float sum) {
+        if (word >= f.o.n) return;
+        const float logit = f.bias != nullptr ? __fadd_rn(sum, f.bias[word]) : sum;
+        run[j].add(logit);
+        if (word == target[j]) f.picked[row_of(j)] = logit;
+    };
+    for (int group = (int)blockIdx.x * kFewWarps + warp; group < groups; group += (int)gridDim.x * kFewWarps) {
+        const int n0 = group * kWords;
+        if constexpr (kByK) {
+            float d[kBlocks][8][4] = {};
+            skinny::by_k<kBf16, kBlocks>(f.o, n0, 0, f.o.k, lane, d);
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) take(2 * b + (q >> 1), n0 + 16 * t + 8 * (q & 1) + i, d[b][i][q]);
+                }
+            }
+        } else {
+            float d[kBlocks][4] = {};
+            skinny::by_output<kBf16, kBlocks, (kBlocks > 1 ? 2 : 4)>(f.o, n0, 0, f.o.k, lane, d);
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) take(2 * b + (q & 1), n0 + g + 8 * (q >> 1), d[b][q]);
+            }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < kLane; ++j) {  // over the lanes that have other words of the same row
+#pragma unroll
+        for (int o = kByK ? 1 : 4; o < (kByK ? 4 : 32); o <<= 1)
+            run[j].join(__shfl_xor_sync(0xFFFFFFFFu, run[j].most, o), __shfl_xor_sync(0xFFFFFFFFu, run[j].sum, o));
+        if ((kByK ? t : g) == 0) joined[warp][row_of(j)] = make_float2(run[j].most, run[j].sum);
+    }
+    __syncthreads();
+    if ((int)threadIdx.x < f.o.rows) {  // at most 32
+        Running all;
+        for (int w = 0; w < kFewWarps; ++w) all.join(joined[w][threadIdx.x].x, joined[w][threadIdx.x].y);
+        f.parts[(int64_t)blockIdx.x * f.o.rows + threadIdx.x] = make_float2(all.most, all.sum);
+    }
+}
+
+// A team of warps a row over the blocks' pairs (`team` warps: 32 for one row, one for 32 rows), then a warp a row over its team's; the
+// mean of the rows that count.
+__global__ void __launch_bounds__(1024)
+few_rows_join_kernel(const float2* __restrict__ parts, int n_parts, int rows, int team, int vocab, const int64_t* __restrict__ targets,
+                     int64_t ignore, const float* __restrict__ picked, float* loss, float* lse_out, float* mean) {
+    __shared__ float2 joined[32];
+    __shared__ float losses[32];
+    __shared__ int counted[32];
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, mine = warp / team, member = warp % team;
+    Running run;
+    if (mine < rows) {
+#pragma unroll 4
+        for (int i = member * 32 + lane; i < n_parts; i += team * 32) {
+            const float2 v = parts[(int64_t)i * rows + mine];
+            run.join(v.x, v.y);
+        }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) run.join(__shfl_xor_sync(0xFFFFFFFFu, run.most, o), __shfl_xor_sync(0xFFFFFFFFu, run.sum, o));
+    if (lane == 0) {
+        joined[warp] = make_float2(run.most, run.sum);
+        losses[warp] = 0.0f;
+        counted[warp] = 0;
+    }
+    __syncthreads();
+    const int row = warp;
+    if (row < rows) {
+        Running all;
+        if (lane < team) {
+            all.most = joined[row * team + lane].x;
+            all.sum = joined[row * team + lane].y;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) all.join(__shfl_xor_sync(0xFFFFFFFFu, all.most, o), __shfl_xor_sync(0xFFFFFFFFu, all.sum, o));
+        if (lane == 0) {
+            const int64_t target = targets[row];
+            float lse = 0.0f, l = 0.0f;
+            if (target != ignore) {
+                lse = __fadd_rn(all.most, logf(all.sum));
+                if (target >= 0 && target < vocab) l = __fsub_rn(lse, picked[row]);
+                else l = lse = __int_as_float(0x7FC00000);  // the target is not a word
+                counted[row] = 1;
+            }
+            if (loss != nullptr) loss[row] = l;
+            if (lse_out != nullptr) lse_out[row] = lse;
+            losses[row] = l;
+        }
+    }
+    if (mean == nullptr) return;
+    __syncthreads();
+    if (row == 0) {
+        double total = losses[lane];
+        int count = counted[lane];
+        for (int o = 16; o > 0; o >>= 1) {
+            total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
+            count += __shfl_xor_sync(0xFFFFFFFFu, count, o);
+        }
+        if (lane == 0) *mean = (float)(total / (count > 0 ? count : 1));
+    }
+}
+
 // ---- host side --------------------------------------------------------------------------------------------------------------
 
 bool misaligned(const void* p, uintptr_t size) { return (reinterpret_cast<uintptr_t>(p) & (size - 1)) != 0; }
@@ -612,7 +770,9 @@ Places places(const Sizes& s, const Plan& plan, bool backward) {
     p.target = l.take((size_t)s.rows * 4);
     p.compact_h = l.take((size_t)up(s.rows, 64) * plan.pitch_h * 2);
     if (!backward) {
-        p.parts = l.take((size_t)(up(s.vocab, 64) / 64) * s.rows * sizeof(float2));
+        // a pair a row for every 64 words of a tile, or for every block of at least 16 words
+        const int64_t words = s.rows <= skinny::kMostRows ? 16 : 64;
+        p.parts = l.take((size_t)(up(s.vocab, words) / words) * s.rows * sizeof(float2));
         p.picked = l.take((size_t)s.rows * 4);
         p.compact_loss = l.take((size_t)s.rows * 4);
     } else {
@@ -676,6 +836,25 @@ int launch_compact(Compact c, const p16::ProductParams& p, const DeviceInfo& dev
 int word_operand(p16::Operand* o, const qfmt_matrix16_t* W, const Sizes& s, bool words, int64_t first, int64_t n) {
     const uint16_t* base = W->ptr + (s.stored_words ? first * W->ld : first);
     return p16::make_operand(o, base, words != s.stored_words, words ? n : s.hidden, words ? s.hidden : n, W->ld);
+}
+
+template <bool kBf16, bool kByK, int kBlocks>
+int launch_few_rows(const FewRows& f, const DeviceInfo& dev, unsigned* blocks, cudaStream_t stream) {
+    constexpr int kWords = kByK ? 64 : 16;
+    const unsigned groups = (unsigned)((f.o.n + kWords - 1) / kWords), want = (groups + kFewWarps - 1) / kFewWarps, most = 8u * dev.sm_count;
+    *blocks = want < most ? want : most;
+    QFMT_CUDA_TRY(launch_overlapping(few_rows_kernel<kBf16, kByK, kBlocks>, *blocks, kFewWarps * 32u, 0, stream, f));
+    return QFMT_OK;
+}
+template <bool kBf16>
+int few_rows_blocks(const FewRows& f, bool by_word, const DeviceInfo& dev, unsigned* blocks, cudaStream_t stream) {
+    if (by_word) {
+        if (f.o.rows <= 8) return launch_few_rows<kBf16, false, 1>(f, dev, blocks, stream);
+        if (f.o.rows <= 16) return launch_few_rows<kBf16, false, 2>(f, dev, blocks, stream);
+        return launch_few_rows<kBf16, false, 4>(f, dev, blocks, stream);
+    }
+    if (f.o.rows <= 16) return launch_few_rows<kBf16, true, 1>(f, dev, blocks, stream);
+    return launch_few_rows<kBf16, true, 2>(f, dev, blocks, stream);
 }
 
 template <typename T>
@@ -785,6 +964,20 @@ extern "C" int qfmt_linear_cross_entropy(const qfmt_matrix16_t* H, const qfmt_ma
     }
     const Plan plan = plan_backward(s);
     const Places pl = places(s, plan, false);
+    if (s.rows <= skinny::kMostRows) {
+        FewRows f = {skinny::Operands{H->ptr, W->ptr, H->ld, W->ld, (int)s.rows, (int)s.vocab, (int)s.hidden}, d_bias, d_targets,
+                     at<float2>(d_workspace, pl.parts), at<float>(d_workspace, pl.picked), static_cast<unsigned long long*>(d_workspace),
+                     next_launch_tag()};
+        unsigned blocks = 0;
+        if (kind->dtype == QFMT_BF16) rc = few_rows_blocks<true>(f, s.stored_words, dev, &blocks, st);
+        else rc = few_rows_blocks<false>(f, s.stored_words, dev, &blocks, st);
+        if (rc != QFMT_OK) return rc;
+        int team = 32;
+        while (team * s.rows > 32) team /= 2;
+        QFMT_CUDA_TRY(launch_overlapping(few_rows_join_kernel, 1u, 1024u, 0, st, (const float2*)f.parts, (int)blocks, (int)s.rows, team, (int)s.vocab,
+                                         d_targets, kind->ignore_index, (const float*)f.picked, d_loss, d_lse, d_mean));
+        return QFMT_OK;
+    }
     p16::Operand h, alt, w;
     rc = p16::make_operand(&h, at<uint16_t>(d_workspace, pl.compact_h), false, up(s.rows, 64), s.hidden, plan.pitch_h);
     if (rc != QFMT_OK) return rc;

@@ -7,10 +7,13 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "activation.cuh"
 #include "columns.cuh"
 #include "common.cuh"
 #include "product16.cuh"
+#include "skinny16.cuh"
 
 namespace qfmt {
 namespace {
@@ -331,6 +334,168 @@ row_pass_kernel(const RowPass a) {
     }
 }
 
+// ---- products of at most 32 rows ------------------------------------------------------------------------------------------
+// One launch: a block takes 16 (weights stored by output) or 64 outputs (by K), its warps share K, and up to eight blocks of a cluster share
+// it again where that leaves more of the GPU with work.  The warps' sums meet in shared memory and the blocks' in the first one's, both
+// in order; the epilogue takes two outputs a thread.
+struct FewRows {
+    skinny::Operands o;
+    const float* bias;
+    const void* residual;
+    const void* z_in;
+    void *out, *z_out;
+    float* dbias;
+    int64_t ld_residual, ld_z, ld_out;
+    int k_warp;  // K elements of a warp, a multiple of 32
+    unsigned long long* status;
+    unsigned long long tag;
+};
+constexpr int kFewWarps = 8;
+
+template <typename T, int kAct, bool kBackward, bool kByK, int kBlocks>
+__global__ void __launch_bounds__(kFewWarps * 32, kByK || kBlocks > 2 ? 2 : 3)
+few_rows_kernel(const FewRows f) {
+    constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
+    constexpr int kOutputs = kByK ? 64 : 16, kRows = kByK ? 16 * kBlocks : 8 * kBlocks, kPitch = kOutputs + 2, kElements = kRows * kPitch;
+    extern __shared__ float few_sums[];  // [warps][rows][outputs]
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    uint32_t rank, size;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(size));
+    const int n0 = (int)(blockIdx.x / size) * kOutputs;
+    const int k0 = ((int)rank * kFewWarps + warp) * f.k_warp;
+    skinny::prefetch_weights<kByK>(f.o, n0, k0, k0 + f.k_warp, lane);
+    grid_dependency_wait();
+    grid_launch_dependents();
+    announce_launch(f.status, f.tag);
+    float* mine = few_sums + warp * kElements;
+    // what the epilogue of the thread's first two outputs needs is on its way meanwhile
+    const T *residual = static_cast<const T*>(f.residual), *z_in = static_cast<const T*>(f.z_in);
+    struct Two {
+        float b0, b1, r0, r1, z0, z1;
+    };
+    auto operands = [&](int e) {
+        Two v = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        const int row = e / (kOutputs / 2), n = n0 + e % (kOutputs / 2) * 2;
+        if (row >= f.o.rows || n >= f.o.n) return v;
+        const bool second = n + 1 < f.o.n;
+        if (!kBackward && f.bias != nullptr) {
+            v.b0 = f.bias[n];
+            if (second) v.b1 = f.bias[n + 1];
+        }
+        if (residual != nullptr) {
+            v.r0 = (float)residual[row * f.ld_residual + n];
+            if (second) v.r1 = (float)residual[row * f.ld_residual + n + 1];
+        }
+        if (kBackward && kAct != QFMT_ACT_NONE) {
+            v.z0 = (float)z_in[row * f.ld_z + n];
+            if (second) v.z1 = (float)z_in[row * f.ld_z + n + 1];
+        }
+        return v;
+    };
+    Two first_two = operands(threadIdx.x);
+    if constexpr (kByK) {
+        float d[kBlocks][8][4] = {};
+        skinny::by_k<kBf16, kBlocks>(f.o, n0, k0, k0 + f.k_warp, lane, d);
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float* p = mine + (b * 16 + g) * kPitch + 16 * t + i;
+                p[0] = d[b][i][0];
+                p[8] = d[b][i][1];
+                p[8 * kPitch] = d[b][i][2];
+                p[8 * kPitch + 8] = d[b][i][3];
+            }
+        }
+    } else {
+        float d[kBlocks][4] = {};
+        skinny::by_output<kBf16, kBlocks, (kBlocks == 1 ? 4 : 2)>(f.o, n0, k0, k0 + f.k_warp, lane, d);
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) {
+            float* p = mine + (b * 8 + 2 * t) * kPitch + g;
+            p[0] = d[b][0];
+            p[kPitch] = d[b][1];
+            p[8] = d[b][2];
+            p[kPitch + 8] = d[b][3];
+        }
+    }
+    __syncthreads();
+    const int rows = f.o.rows;
+    for (int e = threadIdx.x; e < rows * kOutputs; e += kFewWarps * 32) {  // every element is one thread's
+        float* p = few_sums + e / kOutputs * kPitch + e % kOutputs;
+        float s = p[0];
+#pragma unroll
+        for (int w = 1; w < kFewWarps; ++w) s = __fadd_rn(s, p[w * kElements]);
+        p[0] = s;
+    }
+    if (size > 1) {
+        ptx::cluster_sync();
+        if (rank == 0) {
+            for (int e = threadIdx.x; e < rows * kOutputs; e += kFewWarps * 32) {
+                float* p = few_sums + e / kOutputs * kPitch + e % kOutputs;
+                const uint32_t at = ptx::smem_addr(p);
+                float part[8], s = *p;
+#pragma unroll
+                for (int r = 1; r < 8; ++r) {
+                    part[r] = 0.0f;
+                    if (r < (int)size) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(part[r]) : "r"(ptx::map_to_cta(at, r)) : "memory");
+                }
+#pragma unroll
+                for (int r = 1; r < 8; ++r) {
+                    if (r < (int)size) s = __fadd_rn(s, part[r]);
+                }
+                *p = s;
+            }
+        }
+        ptx::cluster_sync();  // the other blocks' shared memory has been read
+        if (rank != 0) return;
+    }
+    __syncthreads();
+    T *out = static_cast<T*>(f.out), *z_out = static_cast<T*>(f.z_out);
+    for (int e = threadIdx.x; e < rows * (kOutputs / 2); e += kFewWarps * 32) {
+        const int row = e / (kOutputs / 2), c = e % (kOutputs / 2) * 2, n = n0 + c;
+        if (n >= f.o.n) continue;
+        const Two w = e < kFewWarps * 32 ? first_two : operands(e);
+        const bool second = n + 1 < f.o.n;
+        float* p = few_sums + row * kPitch + c;
+        float v0 = p[0], v1 = p[1];
+        if (kBackward) {
+            v0 = __fadd_rn(v0, w.r0);
+            v1 = __fadd_rn(v1, w.r1);
+            if constexpr (kAct != QFMT_ACT_NONE) {
+                const float2 s = split_pair(slope2<kAct>(w.z0, w.z1));
+                v0 = __fmul_rn(v0, s.x);
+                v1 = __fmul_rn(v1, s.y);
+            }
+            p[0] = v0;
+            p[1] = v1;
+        } else {
+            v0 = __fadd_rn(v0, w.b0);
+            v1 = __fadd_rn(v1, w.b1);
+            if (z_out != nullptr) {
+                T* z = z_out + row * f.ld_z + n;
+                z[0] = to_type(v0, T());
+                if (second) z[1] = to_type(v1, T());
+            }
+            const float2 a = split_pair(activate2<kAct>(make_pair(v0, v1)));
+            v0 = residual != nullptr ? __fadd_rn(a.x, w.r0) : a.x;
+            v1 = residual != nullptr ? __fadd_rn(a.y, w.r1) : a.y;
+        }
+        T* y = out + row * f.ld_out + n;
+        y[0] = to_type(v0, T());
+        if (second) y[1] = to_type(v1, T());
+    }
+    if (kBackward && f.dbias != nullptr) {
+        __syncthreads();
+        if (threadIdx.x < kOutputs && n0 + (int)threadIdx.x < f.o.n) {
+            float s = few_sums[threadIdx.x];
+            for (int row = 1; row < rows; ++row) s = __fadd_rn(s, few_sums[row * kPitch + threadIdx.x]);
+            f.dbias[n0 + threadIdx.x] = s;
+        }
+    }
+}
+
 // ---- host side ----------------------------------------------------------------------------------------------------------
 
 // Columns of fp32 working matrices are padded so that rows start on 32 bytes.
@@ -375,6 +540,9 @@ int product_shape(const qfmt_matrix16_t* A, const qfmt_matrix16_t* B, Shape* s) 
     if (tiles > (1 << 26)) return QFMT_ERR_BAD_ARG;  // work items are counted in 32 bits
     return QFMT_OK;
 }
+
+// Products of at most 32 rows whose A has its K contiguous go over the weights in few_rows_kernel.
+bool few_rows(const qfmt_matrix16_t* A, const Shape& s) { return s.M <= skinny::kMostRows && A->trans == 0; }
 
 // A product of fewer tiles than CTA pairs shares its K among them, in pieces of at least four stages (256 elements): shorter
 // ones would cost more in moving fp32 sums than they save.
@@ -435,7 +603,7 @@ int prepare_call(Call* c, bool backward, const qfmt_matrix16_t* A, const qfmt_ma
     if (rc != QFMT_OK) return rc;
     c->a = p16::Operand{};
     c->b = p16::Operand{};
-    if (s.K != 0) {
+    if (s.K != 0 && !few_rows(A, s)) {
         rc = p16::make_operand(&c->a, A->ptr, A->trans != 0, s.M, s.K, A->ld);
         if (rc != QFMT_OK) return rc;
         rc = p16::make_operand(&c->b, B->ptr, B->trans == 0, s.N, s.K, B->ld);
@@ -473,8 +641,69 @@ int launch_parts(const Call& c, RowPass* a, cudaStream_t stream) {
     return p16::launch_product<PartEpilogue>(c.a, c.b, nullptr, c.p, pe, c.dev, stream);
 }
 
+template <typename T, int kAct, bool kBackward, bool kByK, int kBlocks>
+int launch_few_rows(FewRows f, const DeviceInfo& dev, cudaStream_t stream) {
+    constexpr int kOutputs = kByK ? 64 : 16, kRows = kByK ? 16 * kBlocks : 8 * kBlocks;
+    constexpr size_t smem = (size_t)kFewWarps * kRows * (kOutputs + 2) * sizeof(float);
+    auto* kernel = few_rows_kernel<T, kAct, kBackward, kByK, kBlocks>;
+    if (smem > 48 * 1024) {
+        static std::atomic<bool> ready[64];
+        const bool known = dev.ordinal >= 0 && dev.ordinal < 64;
+        if (!known || !ready[dev.ordinal].load()) {
+            QFMT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+            if (known) ready[dev.ordinal].store(true);
+        }
+    }
+    // blocks to a cluster: while there are processors without a block and a warp keeps 64 elements of K
+    const int groups = (f.o.n + kOutputs - 1) / kOutputs;
+    int size = 1;
+    while (size < 8 && groups * size * 2 <= dev.sm_count && f.o.k >= size * 2 * kFewWarps * 64) size *= 2;
+    const int per = (f.o.k + size * kFewWarps - 1) / (size * kFewWarps);
+    f.k_warp = (per + 31) / 32 * 32;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(groups * size), 1, 1);
+    cfg.blockDim = dim3(kFewWarps * 32, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)size;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    QFMT_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, f));
+    return QFMT_OK;
+}
+
+template <typename T, int kAct, bool kBackward>
+int few_rows_call(const Call& c, const qfmt_matrix16_t* A, const qfmt_matrix16_t* B, const qfmt_epilogue_t* e, void* d_out, int64_t ld_out,
+                  float* d_dbias, cudaStream_t stream) {
+    FewRows f = {};
+    f.o = skinny::Operands{A->ptr, B->ptr, A->ld, B->ld, (int)c.s.M, (int)c.s.N, (int)c.s.K};
+    f.bias = e->d_bias;
+    f.residual = e->d_residual;
+    f.ld_residual = c.ld_residual;
+    f.z_in = f.z_out = e->d_z;
+    f.ld_z = c.ld_z;
+    f.out = d_out;
+    f.ld_out = ld_out;
+    f.dbias = d_dbias;
+    f.status = c.p.status;
+    f.tag = c.p.tag;
+    if (B->trans != 0) {
+        if (c.s.M <= 8) return launch_few_rows<T, kAct, kBackward, false, 1>(f, c.dev, stream);
+        if (c.s.M <= 16) return launch_few_rows<T, kAct, kBackward, false, 2>(f, c.dev, stream);
+        return launch_few_rows<T, kAct, kBackward, false, 4>(f, c.dev, stream);
+    }
+    if (c.s.M <= 16) return launch_few_rows<T, kAct, kBackward, true, 1>(f, c.dev, stream);
+    return launch_few_rows<T, kAct, kBackward, true, 2>(f, c.dev, stream);
+}
+
 template <typename T, int kAct>
-int forward_call(const Call& c, const qfmt_epilogue_t* e, void* d_y, int64_t ldy, cudaStream_t stream) {
+int forward_call(const Call& c, const qfmt_matrix16_t* A, const qfmt_matrix16_t* B, const qfmt_epilogue_t* e, void* d_y, int64_t ldy, cudaStream_t stream) {
+    if (few_rows(A, c.s)) return few_rows_call<T, kAct, false>(c, A, B, e, d_y, ldy, nullptr, stream);
     const bool vr = whole(e->d_residual, c.ld_residual, 2), vz = whole(e->d_z, c.ld_z, 2), vy = whole(d_y, ldy, 2);
     if (c.splits > 1) {
         RowPass a;
@@ -496,7 +725,9 @@ int forward_call(const Call& c, const qfmt_epilogue_t* e, void* d_y, int64_t ldy
 }
 
 template <typename T, int kAct>
-int backward_call(const Call& c, const qfmt_epilogue_t* e, void* d_dz, int64_t ld_dz, float* d_dbias, cudaStream_t stream) {
+int backward_call(const Call& c, const qfmt_matrix16_t* A, const qfmt_matrix16_t* B, const qfmt_epilogue_t* e, void* d_dz, int64_t ld_dz,
+                  float* d_dbias, cudaStream_t stream) {
+    if (few_rows(A, c.s)) return few_rows_call<T, kAct, true>(c, A, B, e, d_dz, ld_dz, d_dbias, stream);
     const bool vr = whole(e->d_residual, c.ld_residual, 2), vz = whole(e->d_z, c.ld_z, 2), vd = whole(d_dz, ld_dz, 2);
     const int64_t pitch = padded(c.s.N);
     int64_t n_parts = (c.s.M + p16::kTileM - 1) / p16::kTileM * 8;
@@ -543,12 +774,14 @@ int act_backward_call(RowPass a, bool vec, float* d_dbias, cudaStream_t stream) 
     }
 
 template <typename T>
-int forward_typed(const Call& c, const qfmt_epilogue_t* e, void* d_y, int64_t ldy, cudaStream_t stream) {
-    BY_ACT(c.act, (forward_call<T, kA>(c, e, d_y, ldy, stream)))
+int forward_typed(const Call& c, const qfmt_matrix16_t* A, const qfmt_matrix16_t* B, const qfmt_epilogue_t* e, void* d_y, int64_t ldy,
+                  cudaStream_t stream) {
+    BY_ACT(c.act, (forward_call<T, kA>(c, A, B, e, d_y, ldy, stream)))
 }
 template <typename T>
-int backward_typed(const Call& c, const qfmt_epilogue_t* e, void* d_dz, int64_t ld_dz, float* d_dbias, cudaStream_t stream) {
-    BY_ACT(c.act, (backward_call<T, kA>(c, e, d_dz, ld_dz, d_dbias, stream)))
+int backward_typed(const Call& c, const qfmt_matrix16_t* A, const qfmt_matrix16_t* B, const qfmt_epilogue_t* e, void* d_dz, int64_t ld_dz,
+                   float* d_dbias, cudaStream_t stream) {
+    BY_ACT(c.act, (backward_call<T, kA>(c, A, B, e, d_dz, ld_dz, d_dbias, stream)))
 }
 template <typename T>
 int act_backward_typed(int act, const RowPass& a, bool vec, float* d_dbias, cudaStream_t stream) {
@@ -572,8 +805,8 @@ extern "C" int qfmt_linear_act(const qfmt_matrix16_t* A, const qfmt_matrix16_t* 
     const int rc = qfmt::prepare_call(&c, false, A, B, epilogue, d_y, ldy, nullptr, dtype, d_workspace, workspace_bytes, &work);
     if (rc != QFMT_OK || !work) return rc;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (dtype == QFMT_F16) return qfmt::forward_typed<__half>(c, epilogue, d_y, ldy, st);
-    return qfmt::forward_typed<__nv_bfloat16>(c, epilogue, d_y, ldy, st);
+    if (dtype == QFMT_F16) return qfmt::forward_typed<__half>(c, A, B, epilogue, d_y, ldy, st);
+    return qfmt::forward_typed<__nv_bfloat16>(c, A, B, epilogue, d_y, ldy, st);
 }
 
 extern "C" int qfmt_linear_act_backward(const qfmt_matrix16_t* A, const qfmt_matrix16_t* B, const qfmt_epilogue_t* epilogue, void* d_dz,
@@ -593,8 +826,8 @@ extern "C" int qfmt_linear_act_backward(const qfmt_matrix16_t* A, const qfmt_mat
         }
         return QFMT_OK;
     }
-    if (dtype == QFMT_F16) return qfmt::backward_typed<__half>(c, epilogue, d_dz, ld_dz, d_dbias, st);
-    return qfmt::backward_typed<__nv_bfloat16>(c, epilogue, d_dz, ld_dz, d_dbias, st);
+    if (dtype == QFMT_F16) return qfmt::backward_typed<__half>(c, A, B, epilogue, d_dz, ld_dz, d_dbias, st);
+    return qfmt::backward_typed<__nv_bfloat16>(c, A, B, epilogue, d_dz, ld_dz, d_dbias, st);
 }
 
 extern "C" size_t qfmt_act_backward_workspace_bytes(int64_t rows, int64_t cols) {

@@ -355,3 +355,30 @@ def test_captured_graphs_share_a_workspace():
             torch.cuda.synchronize()
             for x, y in zip(got, out):
                 assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("words", [True, False])
+@pytest.mark.parametrize("rows", [1, 3, 8, 9, 16, 17, 32, 33])
+def test_few_rows(rows, words, dtype):
+    for hidden, vocab in ((64, 1), (8, 65), (1024, 3001), (100, 40000)):
+        Problem(rows, hidden, vocab, dtype, words, 0.2 if rows > 4 else 0.0, seed=rows).check_forward()
+
+
+def test_few_rows_with_words_taken_out_and_targets_that_are_none():
+    p = Problem(20, 72, 900, "bf16")
+    p.bias[100:800] = float("-inf")
+    p.targets[:] = torch.arange(20, device="cuda")
+    p.check_forward()
+    p.targets[3], p.targets[4], p.targets[5] = 900, -1, IGNORED
+    p.h[5] = float("nan")
+    loss, lse, mean = p.forward()
+    bad = torch.zeros(20, dtype=torch.bool, device="cuda")
+    bad[3] = bad[4] = True
+    assert torch.equal(torch.isnan(loss), bad) and torch.equal(torch.isnan(lse), bad) and bool(torch.isnan(mean))
+    assert float(loss[5]) == 0.0 == float(lse[5])
+    p.bias[:] = float("-inf")
+    assert bool((p.forward()[1][:3] == float("-inf")).all())
+    p.bias[:] = -3.4e38
+    p.h[:] = 0.0
+    assert bool((p.forward()[1][:3] == p.bias[0]).all())

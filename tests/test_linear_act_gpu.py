@@ -309,3 +309,33 @@ def test_less_workspace_gives_fewer_splits():
         ws, y = workspace(size), torch.empty(m, n, device="cuda", dtype=t)
         qf.qfmt_linear_act(A, B, qf.make_epilogue(), y, n, t, ws, size)
         close(y, want, sum_bound(a64, b64, k) + half_step(want.abs() * (1 + 2.0 ** -10), t))
+
+
+@pytest.mark.parametrize("ta", [False, True])
+@pytest.mark.parametrize("tb", [False, True])
+@pytest.mark.parametrize("m", [1, 7, 8, 9, 16, 17, 31, 32, 33, 40, 100])
+def test_few_rows(m, ta, tb):
+    """Up to 32 rows the weights are walked in one launch, beyond that tiles share a long K."""
+    for n, k in ((1000, 2056), (64, 16), (4099, 64), (15, 4100), (80, 9000)):
+        if not (ta and m % 8):  # a transposed operand's rows are m long
+            forward(m, n, k, "bf16" if m % 2 else "f16", "gelu", ta, tb, seed=m)
+        backward(m, n, k, "f16" if m % 2 else "bf16", "silu", ta, tb, seed=m)
+
+
+@pytest.mark.parametrize("act", ACTS)
+def test_activations_behind_shared_sums(act):
+    for n in (328, 325):
+        forward(40, n, 2000, "bf16", act)
+        backward(40, n, 2000, "f16", act)
+
+
+def test_less_workspace_shares_less():
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    t, m, n, k = torch.float16, 70, 520, 4096
+    A, B, a64, b64, held = product(gen, m, n, k, t, False, True)
+    full = qf.qfmt_linear_act_workspace_bytes(A, B)
+    want = a64 @ b64
+    for size in (256, full // 2, full):
+        ws, y = workspace(size), torch.empty(m, n, device="cuda", dtype=t)
+        qf.qfmt_linear_act(A, B, qf.make_epilogue(), y, n, t, ws, size)
+        close(y, want, sum_bound(a64, b64, k) + half_step(want.abs() * (1 + 2.0 ** -10), t))
