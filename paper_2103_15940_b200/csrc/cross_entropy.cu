@@ -198,9 +198,10 @@ struct RowSumEpilogue {
     };
     struct Ahead {
         int target;
+        float bias[2];
     };
     static __device__ __forceinline__ void before(const Patch& p, const Params& e, Ahead& a) {
-        p.load_columns(e.bias);
+        p.columns(e.bias, a.bias);
         a.target = p.row0 + p.lane < p.rows ? e.target[p.row0 + p.lane] - p.col0 : -1;
     }
     template <typename F>
@@ -210,7 +211,7 @@ struct RowSumEpilogue {
 #pragma unroll 1
         for (int c = 0; c < 2; ++c) {
             pair_t v[16];
-            p.load_pairs<true>(c, v);
+            p.load_pairs<true>(c, v, c == 0 ? a.bias[0] : a.bias[1]);
             if (c == 1) release();
             const int left = p.cols - p.col0 - c * 32;
             if (left <= 0) continue;
@@ -281,9 +282,10 @@ struct GradEpilogue {
     struct Ahead {
         int target;
         float lse, lse2, g, gp;  // lse2 = lse log2 e rounded; gp = g times what the rounding took off
+        float bias[2];
     };
     static __device__ __forceinline__ void before(const Patch& p, const Params& e, Ahead& a) {
-        p.load_columns(e.bias);
+        p.columns(e.bias, a.bias);
         const int row = p.row0 + p.lane;
         const bool there = row < p.rows;
         a.target = there ? e.target[row] - e.first_word - p.col0 : -1;
@@ -300,7 +302,7 @@ struct GradEpilogue {
 #pragma unroll 1
         for (int c = 0; c < 2; ++c) {
             pair_t v[16];
-            p.load_pairs<true>(c, v);
+            p.load_pairs<true>(c, v, c == 0 ? a.bias[0] : a.bias[1]);
             if (c == 1) release();
             const int col0 = p.col0 + c * 32, left = p.cols - col0;
             if (!huge) {

@@ -35,13 +35,14 @@ struct ForwardEpilogue {
     };
     struct Ahead {
         p16::Fetched residual;
+        float bias[2];
     };
     static __device__ __forceinline__ void fetch(const Patch& p, const Params& e, Ahead& a, int col0) {
         if (e.residual != nullptr)
             p16::box_fetch<T>(a.residual, e.residual, e.ld_residual, p.row0, p.rows, col0, p.cols, p.lane, e.vec_residual != 0);
     }
     static __device__ __forceinline__ void before(const Patch& p, const Params& e, Ahead& a) {
-        p.load_columns(e.bias);
+        p.columns(e.bias, a.bias);
         fetch(p, e, a, p.col0);
     }
     template <typename F>
@@ -50,7 +51,7 @@ struct ForwardEpilogue {
         for (int c = 0; c < 2; ++c) {
             const int col0 = p.col0 + c * 32;
             pair_t v[16];
-            p.load_pairs<true>(c, v);
+            p.load_pairs<true>(c, v, c == 0 ? a.bias[0] : a.bias[1]);
             if (c == 1) release();
             if (col0 >= p.cols || p.row0 >= p.rows) continue;
             if (e.z != nullptr) {

@@ -34,12 +34,13 @@ namespace qfmt {
 namespace p16 {
 
 constexpr int kTileM = 256, kTileN = 256, kStageK = 64;  // of a pair
-constexpr int kStages = 5;
+constexpr int kStages = 5;                 // (three: 64 us for 8192 x 1024 x 4096 without an activation, four 58.6, five 56.9, six 56.4, at
+                                           // the expense of what the epilogues' loads keep in the first-level cache: 84 against 91 us for
+                                           // the backward pass through GELU)
 constexpr uint32_t kStageA = 128 * kStageK * 2, kStageB = 128 * kStageK * 2, kStageBytes = kStageA + kStageB;
 constexpr int kThreads = 640, kEpiWarps = 16;
 constexpr uint32_t kBoxBytes = 2048;       // 32 rows x 64 bytes per epilogue warp, 16-byte chunks swizzled with the row
-constexpr uint32_t kColBytes = 64 * 4;     // 64 fp32 per epilogue warp: its columns' bias
-constexpr uint32_t kSmemBytes = kStages * kStageBytes + kEpiWarps * (kBoxBytes + kColBytes) + 256 + 1024;
+constexpr uint32_t kSmemBytes = kStages * kStageBytes + kEpiWarps * kBoxBytes + 256 + 1024;
 static_assert(kSmemBytes <= 232448, "shared memory");
 constexpr uint32_t kAccCols = 256, kTmemCols = 512;
 constexpr uint32_t kWaitLimit = 1u << 31;  // SM cycles, about a second
@@ -69,7 +70,6 @@ struct Patch {
     uint32_t tmem;           // accumulator address of (row0, col0)
     bool empty;              // nothing was summed: the sums are zero
     uint8_t* box;
-    float* col;
 
     __device__ __forceinline__ void load32(int block, uint32_t (&r)[32]) const {
         if (empty) {
@@ -82,31 +82,36 @@ struct Patch {
     __device__ __forceinline__ void wait() const {
         if (!empty) ptx::tmem_load_wait();
     }
-    // Block of 32 columns in pairs, complete on return; kBias: plus the columns' values.
+    // Block of 32 columns in pairs, complete on return; kBias: plus a vector of the columns, of which the lane brings its column's value.
+    // (It goes round through the box.)
     template <bool kBias>
-    __device__ __forceinline__ void load_pairs(int block, pair_t (&v)[16]) const {
+    __device__ __forceinline__ void load_pairs(int block, pair_t (&v)[16], float bias = 0.0f) const {
         uint32_t r[32];
         load32(block, r);
+        if (kBias) {
+            reinterpret_cast<float*>(box)[lane] = bias;
+            __syncwarp();
+        }
         wait();
 #pragma unroll
         for (int j = 0; j < 32; j += 4) {
             v[j / 2] = make_pair(__uint_as_float(r[j]), __uint_as_float(r[j + 1]));
             v[j / 2 + 1] = make_pair(__uint_as_float(r[j + 2]), __uint_as_float(r[j + 3]));
             if (kBias) {
-                const float4 b = *reinterpret_cast<const float4*>(col + block * 32 + j);
+                const float4 b = *reinterpret_cast<const float4*>(box + j * 4);
                 v[j / 2] = add2(v[j / 2], make_pair(b.x, b.y));
                 v[j / 2 + 1] = add2(v[j / 2 + 1], make_pair(b.z, b.w));
             }
         }
+        if (kBias) __syncwarp();
     }
-    // The 64 columns' values of a vector (zero beyond N) into col.
-    __device__ __forceinline__ void load_columns(const float* v) const {
+    // The lane's value of a vector of columns in each of the two blocks; zero beyond N and without a vector.
+    __device__ __forceinline__ void columns(const float* v, float (&out)[2]) const {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int c = col0 + i * 32 + lane;
-            col[i * 32 + lane] = v != nullptr && c < cols ? v[c] : 0.0f;
+            out[i] = v != nullptr && c < cols ? v[c] : 0.0f;
         }
-        __syncwarp();
     }
 };
 
@@ -272,7 +277,7 @@ product16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = ptx::smem_addr(smem_raw);
     const uint32_t tiles = (raw + 1023u) & ~1023u;
-    const uint32_t boxes = tiles + kStages * kStageBytes, colbufs = boxes + kEpiWarps * kBoxBytes, bars = colbufs + kEpiWarps * kColBytes;
+    const uint32_t boxes = tiles + kStages * kStageBytes, bars = boxes + kEpiWarps * kBoxBytes;
     auto full_bar = [&](int s) { return bars + 8u * s; };
     auto empty_bar = [&](int s) { return bars + 8u * (kStages + s); };
     auto acc_full_bar = [&](int a) { return bars + 8u * (2 * kStages + a); };
@@ -419,7 +424,6 @@ product16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         pt.quad = warp & 3;
         pt.warp = warp - 4;
         pt.box = smem_raw + (boxes - raw) + pt.warp * kBoxBytes;
-        pt.col = reinterpret_cast<float*>(smem_raw + (colbufs - raw) + pt.warp * kColBytes);
         pt.rows = M;
         pt.cols = p.N;
         const int quarter = pt.warp >> 2;
