@@ -8,15 +8,15 @@ namespace qfmt {
 constexpr int kJoinCols = 32, kJoinGroups = 8;
 
 // Block of 32 columns x 8 groups: group g adds parts g, g + 8, ..., then the groups are added in order.  `count` (or NULL)
-// holds the rows counted on the device: only the parts of whole 256-row tiles that hold some of them were written.
+// holds the rows counted on the device: only the parts of whole tiles of tile_rows that hold some of them were written, one for 32 rows.
 // `scale` (or NULL): what the sums are multiplied by.
 static __global__ void __launch_bounds__(kJoinCols * kJoinGroups)
-join_columns_kernel(const float* __restrict__ parts, int64_t pitch, int n_parts, const int* count, const float* scale, float* __restrict__ out,
-                    int cols) {
+join_columns_kernel(const float* __restrict__ parts, int64_t pitch, int n_parts, const int* count, int tile_rows,
+                    const float* scale, float* __restrict__ out, int cols) {
     __shared__ float sums[kJoinGroups][kJoinCols];
     grid_dependency_wait();
     grid_launch_dependents();
-    if (count != nullptr) n_parts = (*count + 255) / 256 * 8;
+    if (count != nullptr) n_parts = (*count + tile_rows - 1) / tile_rows * (tile_rows / 32);
     const int c = threadIdx.x % kJoinCols, g = threadIdx.x / kJoinCols, col = blockIdx.x * kJoinCols + c;
     float s = 0.0f;
     if (col < cols) {
@@ -31,10 +31,10 @@ join_columns_kernel(const float* __restrict__ parts, int64_t pitch, int n_parts,
     }
 }
 
-inline int launch_join_columns(const float* parts, int64_t pitch, int64_t n_parts, const int* count, const float* scale,
-                               float* out, int64_t cols, cudaStream_t stream) {
+inline int launch_join_columns(const float* parts, int64_t pitch, int64_t n_parts, const int* count, int tile_rows,
+                               const float* scale, float* out, int64_t cols, cudaStream_t stream) {
     QFMT_CUDA_TRY(launch_overlapping(join_columns_kernel, (unsigned)((cols + kJoinCols - 1) / kJoinCols), (unsigned)(kJoinCols * kJoinGroups),
-                                     0, stream, parts, pitch, (int)n_parts, count, scale, out, (int)cols));
+                                     0, stream, parts, pitch, (int)n_parts, count, tile_rows, scale, out, (int)cols));
     return QFMT_OK;
 }
 

@@ -712,7 +712,7 @@ int loss_sizes(const qfmt_matrix16_t* H, const qfmt_matrix16_t* W, Sizes* s) {
     if (s->hidden != (s->stored_words ? W->cols : W->rows)) return QFMT_ERR_BAD_ARG;
     if (s->rows < 0 || s->hidden < 1 || s->vocab < 1) return QFMT_ERR_BAD_ARG;
     if (s->rows > (1 << 24) || s->hidden > (1 << 24) || s->vocab > (1 << 28)) return QFMT_ERR_BAD_ARG;
-    if (up(s->rows, p16::kTileM) / p16::kTileM * (up(s->vocab, p16::kTileN) / p16::kTileN) > (1 << 26)) return QFMT_ERR_BAD_ARG;
+    if (p16::single_tiles(s->rows, s->vocab) > (1 << 26)) return QFMT_ERR_BAD_ARG;
     return QFMT_OK;
 }
 
@@ -720,7 +720,6 @@ int loss_sizes(const qfmt_matrix16_t* H, const qfmt_matrix16_t* W, Sizes* s) {
 // between the product that writes it and the two that read it; and pieces of at least 1024 words keep those products whole.  Within
 // that a piece has as many 256-word tiles as let the weight gradient's tiles fill whole rounds of the CTA pairs.
 constexpr int64_t kPieceBytes = 80ll << 20;
-constexpr int64_t kPairs = 74, kMostSplits = 16, kLeastStages = 4;
 struct Plan {
     int64_t tile_rows;   // rows of whole tiles
     int64_t piece;       // words, a multiple of 256
@@ -729,22 +728,18 @@ struct Plan {
 };
 Plan plan_backward(const Sizes& s) {
     Plan p;
-    p.tile_rows = up(s.rows > 0 ? s.rows : 1, p16::kTileM);
+    p.tile_rows = up(s.rows > 0 ? s.rows : 1, 2 * p16::kRows);
     int64_t most = kPieceBytes / (p.tile_rows * 2) / p16::kTileN;  // tiles of words
     if (most < 4) most = 4;
     const int64_t all = (s.vocab + p16::kTileN - 1) / p16::kTileN, across = up(s.hidden, p16::kTileN) / p16::kTileN;
     if (most < all) {
-        const int64_t fill = most * across / kPairs * kPairs / across;  // the most whose tiles make whole rounds
+        const int64_t fill = most * across / p16::kPairs * p16::kPairs / across;  // the most whose tiles make whole rounds
         if (fill > 0) most = fill;
     }
     const int64_t pieces = (all + most - 1) / most;
     p.piece = (all + pieces - 1) / pieces * p16::kTileN;
     p.pitch_h = up(s.hidden, 8);
-    const int64_t tiles = p.tile_rows / p16::kTileM * (up(s.hidden, p16::kTileN) / p16::kTileN), stages = p.piece / p16::kStageK;
-    int64_t n = kPairs / tiles;
-    if (n > stages / kLeastStages) n = stages / kLeastStages;
-    if (n > kMostSplits) n = kMostSplits;
-    p.splits = n < 2 ? 1 : (int)n;
+    p.splits = p16::plan_product(s.rows, s.hidden, p.piece, true).splits;
     return p;
 }
 
@@ -835,9 +830,9 @@ int launch_compact(Compact c, const p16::ProductParams& p, const DeviceInfo& dev
 }
 
 // W's words first .. first + n - 1 as an operand: `words`: the words are the extent (logits), else they are K (dH).
-int word_operand(p16::Operand* o, const qfmt_matrix16_t* W, const Sizes& s, bool words, int64_t first, int64_t n) {
+int word_operand(p16::Operand* o, bool pair, const qfmt_matrix16_t* W, const Sizes& s, bool words, int64_t first, int64_t n) {
     const uint16_t* base = W->ptr + (s.stored_words ? first * W->ld : first);
-    return p16::make_operand(o, base, words != s.stored_words, words ? n : s.hidden, words ? s.hidden : n, W->ld);
+    return p16::make_operand(o, true, pair, base, words != s.stored_words, words ? n : s.hidden, words ? s.hidden : n, W->ld);
 }
 
 template <bool kBf16, bool kByK, int kBlocks>
@@ -859,12 +854,23 @@ int few_rows_blocks(const FewRows& f, bool by_word, const DeviceInfo& dev, unsig
     return launch_few_rows<kBf16, true, 2>(f, dev, blocks, stream);
 }
 
+// H in the compact copy or in place, as rows of the logits' product or as the K of the weight gradient's.
+struct Tokens {
+    p16::Operand copy, whole;
+};
+int token_operand(Tokens* o, bool is_b, bool pair, const qfmt_matrix16_t* H, const Sizes& s, const Plan& plan, const uint16_t* copy, bool rows) {
+    const int64_t n = rows ? up(s.rows, 64) : s.hidden, k = rows ? s.hidden : up(s.rows, 64);
+    const int rc = p16::make_operand(&o->copy, is_b, pair, copy, !rows, n, k, plan.pitch_h);
+    if (rc != QFMT_OK) return rc;
+    return p16::make_operand(&o->whole, is_b, pair, H->ptr, !rows, rows ? s.rows : s.hidden, rows ? s.hidden : s.rows, H->ld);
+}
+
 template <typename T>
-int backward_pieces(const qfmt_matrix16_t* W, const float* d_bias, const Sizes& s, const Plan& plan, const Places& pl, void* ws,
-                    const p16::Operand& h_rows, const p16::Operand& h_rows_alt, const p16::Operand& h_k, const p16::Operand& h_k_alt,
-                    p16::ProductParams base, void* d_dh, int64_t ld_dh, void* d_dw, int64_t ld_dw, float* d_dbias, const DeviceInfo& dev,
-                    cudaStream_t stream) {
+int backward_pieces(const qfmt_matrix16_t* H, const qfmt_matrix16_t* W, const float* d_bias, const Sizes& s, const Plan& plan, const Places& pl,
+                    void* ws, p16::ProductParams base, void* d_dh, int64_t ld_dh, void* d_dw, int64_t ld_dw, float* d_dbias,
+                    const DeviceInfo& dev, cudaStream_t stream) {
     const Found* found = at<Found>(ws, pl.found);
+    const uint16_t* copy = at<uint16_t>(ws, pl.compact_h);
     T* d = at<T>(ws, pl.d);
     float* column_parts = at<float>(ws, pl.column_parts);
     float* sums = at<float>(ws, pl.sums);
@@ -872,8 +878,11 @@ int backward_pieces(const qfmt_matrix16_t* W, const float* d_bias, const Sizes& 
     for (int64_t first = 0; first < s.vocab; first += plan.piece) {
         const int64_t n = first + plan.piece < s.vocab ? plan.piece : s.vocab - first, n64 = up(n, 64);
         // d of this piece
-        p16::Operand w, dk, dm;
-        rc = word_operand(&w, W, s, true, first, n);
+        Tokens h;
+        p16::Operand w, g;
+        p16::ProductPlan pp = p16::plan_product(s.rows, n, s.hidden, false);
+        rc = token_operand(&h, false, pp.pair, H, s, plan, copy, true);
+        if (rc == QFMT_OK) rc = word_operand(&w, pp.pair, W, s, true, first, n);
         if (rc != QFMT_OK) return rc;
         p16::ProductParams p = base;
         p.M = (int)s.rows;
@@ -882,51 +891,48 @@ int backward_pieces(const qfmt_matrix16_t* W, const float* d_bias, const Sizes& 
         p.dyn = p16::kCountM;
         p.alt = p16::kAltA;
         p.splits = 1;
-        p.kb_per_split = (int)(up(s.hidden, p16::kStageK) / p16::kStageK);
+        p.kb_per_split = pp.kb_per_split;
         typename GradEpilogue<T>::Params ge = {d_bias != nullptr ? d_bias + first : nullptr, at<int>(ws, pl.target), at<float>(ws, pl.lse_of),
                                                at<float>(ws, pl.g), d, d_dbias != nullptr ? column_parts : nullptr, plan.piece, (int)first};
-        rc = p16::launch_product<GradEpilogue<T>>(h_rows, w, &h_rows_alt, p, ge, dev, stream);
+        rc = p16::launch_product<GradEpilogue<T>>(pp.pair, h.copy, w, &h.whole, p, ge, dev, stream);
         if (rc != QFMT_OK) return rc;
         if (d_dbias != nullptr) {
-            rc = launch_join_columns(column_parts, plan.piece, plan.tile_rows / 32, &found->count, &found->unscale, d_dbias + first, n, stream);
+            rc = launch_join_columns(column_parts, plan.piece, plan.tile_rows / 32, &found->count, pp.pair ? 2 * p16::kRows : p16::kRows,
+                                     &found->unscale, d_dbias + first, n, stream);
             if (rc != QFMT_OK) return rc;
         }
         if (d_dw != nullptr) {
-            rc = p16::make_operand(&dm, d, true, n64, plan.tile_rows, plan.piece);
-            if (rc != QFMT_OK) return rc;
+            p.M = (int)(s.stored_words ? n : s.hidden);
+            p.N = (int)(s.stored_words ? s.hidden : n);
             p.K = (int)s.rows;
             p.dyn = p16::kCountK;
-            p.kb_per_split = (int)(up(s.rows, p16::kStageK) / p16::kStageK);
+            p.alt = s.stored_words ? p16::kAltB : p16::kAltA;
+            pp = p16::plan_product(p.M, p.N, s.rows, false);
+            p.kb_per_split = pp.kb_per_split;
+            rc = token_operand(&h, s.stored_words, pp.pair, H, s, plan, copy, false);
+            if (rc == QFMT_OK) rc = p16::make_operand(&g, !s.stored_words, pp.pair, d, true, n64, plan.tile_rows, plan.piece);
+            if (rc != QFMT_OK) return rc;
             T* out = static_cast<T*>(d_dw) + (s.stored_words ? first * ld_dw : first);
             typename ScaledEpilogue<T>::Params se = {&found->unscale, out, ld_dw, whole(out, ld_dw, 2)};
-            if (s.stored_words) {
-                p.M = (int)n;
-                p.N = (int)s.hidden;
-                p.alt = p16::kAltB;
-                rc = p16::launch_product<ScaledEpilogue<T>>(dm, h_k, &h_k_alt, p, se, dev, stream);
-            } else {
-                p.M = (int)s.hidden;
-                p.N = (int)n;
-                p.alt = p16::kAltA;
-                rc = p16::launch_product<ScaledEpilogue<T>>(h_k, dm, &h_k_alt, p, se, dev, stream);
-            }
+            if (s.stored_words) rc = p16::launch_product<ScaledEpilogue<T>>(pp.pair, g, h.copy, &h.whole, p, se, dev, stream);
+            else rc = p16::launch_product<ScaledEpilogue<T>>(pp.pair, h.copy, g, &h.whole, p, se, dev, stream);
             if (rc != QFMT_OK) return rc;
         }
         if (d_dh != nullptr) {
-            rc = p16::make_operand(&dk, d, false, plan.tile_rows, n64, plan.piece);
-            if (rc != QFMT_OK) return rc;
-            rc = word_operand(&w, W, s, false, first, n);
-            if (rc != QFMT_OK) return rc;
             p.M = (int)s.rows;
             p.N = (int)s.hidden;
             p.K = (int)n;
             p.dyn = p16::kCountM;
             p.alt = p16::kAltNone;
+            pp = p16::plan_product(s.rows, s.hidden, plan.piece, true);
             p.splits = plan.splits;
-            const int stages = (int)(up(n, p16::kStageK) / p16::kStageK);
-            p.kb_per_split = (stages + plan.splits - 1) / plan.splits;  // a short last piece leaves some splits without work: they add zeros
+            // a short last piece is shared as finely: some splits may be left without work and add zeros
+            p.kb_per_split = (int)p16::ceil_div(p16::ceil_div(n, p16::kStageK), plan.splits);
+            rc = p16::make_operand(&g, false, pp.pair, d, false, plan.tile_rows, n64, plan.piece);
+            if (rc == QFMT_OK) rc = word_operand(&w, pp.pair, W, s, false, first, n);
+            if (rc != QFMT_OK) return rc;
             typename AddEpilogue::Params ae = {sums, plan.pitch_h, s.rows * plan.pitch_h, first > 0 ? 1 : 0};
-            rc = p16::launch_product<AddEpilogue>(dk, w, nullptr, p, ae, dev, stream);
+            rc = p16::launch_product<AddEpilogue>(pp.pair, g, w, nullptr, p, ae, dev, stream);
             if (rc != QFMT_OK) return rc;
         }
     }
@@ -980,12 +986,11 @@ extern "C" int qfmt_linear_cross_entropy(const qfmt_matrix16_t* H, const qfmt_ma
                                          d_targets, kind->ignore_index, (const float*)f.picked, d_loss, d_lse, d_mean));
         return QFMT_OK;
     }
-    p16::Operand h, alt, w;
-    rc = p16::make_operand(&h, at<uint16_t>(d_workspace, pl.compact_h), false, up(s.rows, 64), s.hidden, plan.pitch_h);
-    if (rc != QFMT_OK) return rc;
-    rc = p16::make_operand(&alt, H->ptr, false, s.rows, s.hidden, H->ld);
-    if (rc != QFMT_OK) return rc;
-    rc = word_operand(&w, W, s, true, 0, s.vocab);
+    const p16::ProductPlan pp = p16::plan_product(s.rows, s.vocab, s.hidden, false);
+    Tokens h;
+    p16::Operand w;
+    rc = token_operand(&h, false, pp.pair, H, s, plan, at<uint16_t>(d_workspace, pl.compact_h), true);
+    if (rc == QFMT_OK) rc = word_operand(&w, pp.pair, W, s, true, 0, s.vocab);
     if (rc != QFMT_OK) return rc;
     Compact c = compact_args(H, kind, d_targets, s, plan, pl, d_workspace);
     c.loss = d_loss;
@@ -1006,7 +1011,7 @@ extern "C" int qfmt_linear_cross_entropy(const qfmt_matrix16_t* H, const qfmt_ma
     rc = launch_compact<false>(c, p, dev, st);
     if (rc != QFMT_OK) return rc;
     typename RowSumEpilogue::Params re = {d_bias, c.target, at<float2>(d_workspace, pl.parts), at<float>(d_workspace, pl.picked), s.rows};
-    rc = p16::launch_product<RowSumEpilogue>(h, w, &alt, p, re, dev, st);
+    rc = p16::launch_product<RowSumEpilogue>(pp.pair, h.copy, w, &h.whole, p, re, dev, st);
     if (rc != QFMT_OK) return rc;
     const unsigned blocks = (unsigned)((s.rows + kJoinRows - 1) / kJoinRows);
     float* compact_loss = d_mean != nullptr && blocks > 1 ? at<float>(d_workspace, pl.compact_loss) : nullptr;
@@ -1042,14 +1047,6 @@ extern "C" int qfmt_linear_cross_entropy_backward(const qfmt_matrix16_t* H, cons
     }
     const Plan plan = plan_backward(s);
     const Places pl = places(s, plan, true);
-    // H as rows of the logits' product and as the K of the weight's, in the compact copy or in place
-    p16::Operand h_rows, h_rows_alt, h_k, h_k_alt;
-    const uint16_t* copy = at<uint16_t>(d_workspace, pl.compact_h);
-    rc = p16::make_operand(&h_rows, copy, false, up(s.rows, 64), s.hidden, plan.pitch_h);
-    if (rc == QFMT_OK) rc = p16::make_operand(&h_rows_alt, H->ptr, false, s.rows, s.hidden, H->ld);
-    if (rc == QFMT_OK) rc = p16::make_operand(&h_k, copy, true, s.hidden, up(s.rows, 64), plan.pitch_h);
-    if (rc == QFMT_OK) rc = p16::make_operand(&h_k_alt, H->ptr, true, s.hidden, s.rows, H->ld);
-    if (rc != QFMT_OK) return rc;
     Compact c = compact_args(H, kind, d_targets, s, plan, pl, d_workspace);
     c.lse = d_lse;
     c.dloss = d_dloss;
@@ -1067,8 +1064,6 @@ extern "C" int qfmt_linear_cross_entropy_backward(const qfmt_matrix16_t* H, cons
     rc = launch_compact<true>(c, p, dev, st);
     if (rc != QFMT_OK) return rc;
     if (kind->dtype == QFMT_F16)
-        return backward_pieces<__half>(W, d_bias, s, plan, pl, d_workspace, h_rows, h_rows_alt, h_k, h_k_alt, p, d_dh, ld_dh, d_dw, ld_dw,
-                                       d_dbias, dev, st);
-    return backward_pieces<__nv_bfloat16>(W, d_bias, s, plan, pl, d_workspace, h_rows, h_rows_alt, h_k, h_k_alt, p, d_dh, ld_dh, d_dw, ld_dw,
-                                          d_dbias, dev, st);
+        return backward_pieces<__half>(H, W, d_bias, s, plan, pl, d_workspace, p, d_dh, ld_dh, d_dw, ld_dw, d_dbias, dev, st);
+    return backward_pieces<__nv_bfloat16>(H, W, d_bias, s, plan, pl, d_workspace, p, d_dh, ld_dh, d_dw, ld_dw, d_dbias, dev, st);
 }

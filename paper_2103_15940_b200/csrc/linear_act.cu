@@ -537,30 +537,16 @@ int product_shape(const qfmt_matrix16_t* A, const qfmt_matrix16_t* B, Shape* s) 
     s->N = B->trans ? B->rows : B->cols;
     if (s->K != (B->trans ? B->cols : B->rows)) return QFMT_ERR_BAD_ARG;
     if (s->M > (1 << 30) || s->N > (1 << 30) || s->K > (1 << 30)) return QFMT_ERR_BAD_ARG;
-    const int64_t tiles = ((s->M + p16::kTileM - 1) / p16::kTileM) * ((s->N + p16::kTileN - 1) / p16::kTileN);
-    if (tiles > (1 << 26)) return QFMT_ERR_BAD_ARG;  // work items are counted in 32 bits
+    if (p16::single_tiles(s->M, s->N) > (1 << 26)) return QFMT_ERR_BAD_ARG;  // work items are counted in 32 bits
     return QFMT_OK;
 }
 
 // Products of at most 32 rows whose A has its K contiguous go over the weights in few_rows_kernel.
 bool few_rows(const qfmt_matrix16_t* A, const Shape& s) { return s.M <= skinny::kMostRows && A->trans == 0; }
 
-// A product of fewer tiles than CTA pairs shares its K among them, in pieces of at least four stages (256 elements): shorter
-// ones would cost more in moving fp32 sums than they save.
-constexpr int64_t kPairs = 74, kMostSplits = 16, kLeastStages = 4;
-int plan_splits(const Shape& s) {
-    const int64_t tiles = ((s.M + p16::kTileM - 1) / p16::kTileM) * ((s.N + p16::kTileN - 1) / p16::kTileN);
-    const int64_t stages = (s.K + p16::kStageK - 1) / p16::kStageK;
-    if (tiles == 0) return 1;
-    int64_t n = kPairs / tiles;
-    if (n > stages / kLeastStages) n = stages / kLeastStages;
-    if (n > kMostSplits) n = kMostSplits;
-    return n < 2 ? 1 : (int)n;
-}
-
 constexpr size_t kHeader = 256;
 size_t sums_bytes(const Shape& s) {  // column sums by groups of 32 rows of whole tiles, or by the row blocks of a pass
-    const int64_t groups = (s.M + p16::kTileM - 1) / p16::kTileM * 8, blocks = s.N > 0 ? pass_row_blocks(s.M, s.N) : 0;
+    const int64_t groups = p16::ceil_div(s.M, 2 * p16::kRows) * 2 * p16::kRows / 32, blocks = s.N > 0 ? pass_row_blocks(s.M, s.N) : 0;
     return (size_t)(groups > blocks ? groups : blocks) * (size_t)padded(s.N) * sizeof(float);
 }
 size_t part_bytes(const Shape& s, int splits) { return (size_t)splits * (size_t)s.M * (size_t)padded(s.N) * sizeof(float); }
@@ -572,6 +558,7 @@ struct Call {
     DeviceInfo dev;
     p16::Operand a, b;
     p16::ProductParams p;
+    bool pair;
     int splits;
     float *sums, *parts;
 };
@@ -602,26 +589,29 @@ int prepare_call(Call* c, bool backward, const qfmt_matrix16_t* A, const qfmt_ma
     }
     rc = current_device(&c->dev);
     if (rc != QFMT_OK) return rc;
+    p16::ProductPlan plan = p16::plan_product(s.M, s.N, s.K, true);
+    while (plan.splits > 1 && kHeader + sums + part_bytes(s, plan.splits) > workspace_bytes) --plan.splits;
+    const int stages = (int)p16::ceil_div(s.K, p16::kStageK);
+    plan.kb_per_split = (stages + plan.splits - 1) / plan.splits;
+    if (plan.splits > 1) plan.splits = (stages + plan.kb_per_split - 1) / plan.kb_per_split;
+    c->pair = plan.pair;
+    c->splits = plan.splits;
     c->a = p16::Operand{};
     c->b = p16::Operand{};
     if (s.K != 0 && !few_rows(A, s)) {
-        rc = p16::make_operand(&c->a, A->ptr, A->trans != 0, s.M, s.K, A->ld);
+        rc = p16::make_operand(&c->a, false, plan.pair, A->ptr, A->trans != 0, s.M, s.K, A->ld);
         if (rc != QFMT_OK) return rc;
-        rc = p16::make_operand(&c->b, B->ptr, B->trans == 0, s.N, s.K, B->ld);
+        rc = p16::make_operand(&c->b, true, plan.pair, B->ptr, B->trans == 0, s.N, s.K, B->ld);
         if (rc != QFMT_OK) return rc;
     }
-    c->splits = plan_splits(s);
-    while (c->splits > 1 && kHeader + sums + part_bytes(s, c->splits) > workspace_bytes) --c->splits;
-    const int stages = (int)((s.K + p16::kStageK - 1) / p16::kStageK);
     p16::ProductParams& p = c->p;
     p = p16::ProductParams{};
     p.M = (int)s.M;
     p.N = (int)s.N;
     p.K = (int)s.K;
     p.bf16 = dtype == QFMT_BF16;
-    p.kb_per_split = (stages + c->splits - 1) / c->splits;
-    if (c->splits > 1) c->splits = (stages + p.kb_per_split - 1) / p.kb_per_split;
-    p.splits = c->splits;
+    p.kb_per_split = plan.kb_per_split;
+    p.splits = plan.splits;
     p.status = static_cast<unsigned long long*>(d_workspace);
     p.tag = next_launch_tag();
     c->sums = reinterpret_cast<float*>(static_cast<char*>(d_workspace) + kHeader);
@@ -639,7 +629,7 @@ int launch_parts(const Call& c, RowPass* a, cudaStream_t stream) {
     a->pitch = pe.pitch;
     a->rows = c.s.M;
     a->cols = c.s.N;
-    return p16::launch_product<PartEpilogue>(c.a, c.b, nullptr, c.p, pe, c.dev, stream);
+    return p16::launch_product<PartEpilogue>(c.pair, c.a, c.b, nullptr, c.p, pe, c.dev, stream);
 }
 
 template <typename T, int kAct, bool kBackward, bool kByK, int kBlocks>
@@ -722,7 +712,7 @@ int forward_call(const Call& c, const qfmt_matrix16_t* A, const qfmt_matrix16_t*
     using Epi = ForwardEpilogue<T, kAct>;
     typename Epi::Params ep = {e->d_bias, static_cast<const T*>(e->d_residual), static_cast<T*>(e->d_z), static_cast<T*>(d_y),
                                c.ld_residual, c.ld_z, ldy, vr, vz, vy};
-    return p16::launch_product<Epi>(c.a, c.b, nullptr, c.p, ep, c.dev, stream);
+    return p16::launch_product<Epi>(c.pair, c.a, c.b, nullptr, c.p, ep, c.dev, stream);
 }
 
 template <typename T, int kAct>
@@ -731,7 +721,8 @@ int backward_call(const Call& c, const qfmt_matrix16_t* A, const qfmt_matrix16_t
     if (few_rows(A, c.s)) return few_rows_call<T, kAct, true>(c, A, B, e, d_dz, ld_dz, d_dbias, stream);
     const bool vr = whole(e->d_residual, c.ld_residual, 2), vz = whole(e->d_z, c.ld_z, 2), vd = whole(d_dz, ld_dz, 2);
     const int64_t pitch = padded(c.s.N);
-    int64_t n_parts = (c.s.M + p16::kTileM - 1) / p16::kTileM * 8;
+    const int64_t tile_rows = c.pair ? 2 * p16::kRows : p16::kRows;
+    int64_t n_parts = p16::ceil_div(c.s.M, tile_rows) * tile_rows / 32;
     int rc;
     if (c.splits > 1) {
         RowPass a;
@@ -751,10 +742,10 @@ int backward_call(const Call& c, const qfmt_matrix16_t* A, const qfmt_matrix16_t
         using Epi = BackwardEpilogue<T, kAct>;
         typename Epi::Params ep = {static_cast<const T*>(e->d_residual), static_cast<const T*>(e->d_z), static_cast<T*>(d_dz),
                                    d_dbias != nullptr ? c.sums : nullptr, c.ld_residual, c.ld_z, ld_dz, pitch, vr, vz, vd};
-        rc = p16::launch_product<Epi>(c.a, c.b, nullptr, c.p, ep, c.dev, stream);
+        rc = p16::launch_product<Epi>(c.pair, c.a, c.b, nullptr, c.p, ep, c.dev, stream);
     }
     if (rc != QFMT_OK || d_dbias == nullptr) return rc;
-    return launch_join_columns(c.sums, pitch, n_parts, nullptr, nullptr, d_dbias, c.s.N, stream);
+    return launch_join_columns(c.sums, pitch, n_parts, nullptr, 0, nullptr, d_dbias, c.s.N, stream);
 }
 
 template <typename T, int kAct>
@@ -762,7 +753,7 @@ int act_backward_call(RowPass a, bool vec, float* d_dbias, cudaStream_t stream) 
     int rc = launch_row_pass<T, kAct, true, false>(a, vec, stream);
     if (rc != QFMT_OK || d_dbias == nullptr) return rc;
     const int64_t blocks = pass_row_blocks(a.rows, a.cols), per = (a.rows + blocks - 1) / blocks;
-    return launch_join_columns(a.sums, a.pitch, (a.rows + per - 1) / per, nullptr, nullptr, d_dbias, a.cols, stream);
+    return launch_join_columns(a.sums, a.pitch, (a.rows + per - 1) / per, nullptr, 0, nullptr, d_dbias, a.cols, stream);
 }
 
 #define BY_ACT(act, call)                                              \
@@ -795,7 +786,7 @@ int act_backward_typed(int act, const RowPass& a, bool vec, float* d_dbias, cuda
 extern "C" size_t qfmt_linear_act_workspace_bytes(const qfmt_matrix16_t* A, const qfmt_matrix16_t* B) {
     qfmt::Shape s;
     if (qfmt::product_shape(A, B, &s) != QFMT_OK) return 0;
-    const int splits = qfmt::plan_splits(s);
+    const int splits = qfmt::p16::plan_product(s.M, s.N, s.K, true).splits;
     return qfmt::kHeader + qfmt::sums_bytes(s) + (splits > 1 ? qfmt::part_bytes(s, splits) : 0);
 }
 

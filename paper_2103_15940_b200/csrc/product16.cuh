@@ -1,13 +1,16 @@
 // Products of 16-bit codes (binary16 or bfloat16 words) whose sums go through an epilogue of the caller's choice instead of
 // to memory as they are: the frame that qfmt_linear_act and qfmt_linear_cross_entropy share.
 //
-// One persistent kernel, one CTA pair per two SMs, 256 x 256 tiles: each CTA stages its own 128 rows of op(A) and its own 128
+// One persistent kernel.  For large products one CTA pair per two SMs and 256 x 256 tiles: each CTA stages its own 128 rows of op(A) and its own 128
 // columns of op(B) by TMA (64 K elements, 32 KB a stage), the leader's MMA thread issues tcgen05.mma.cta_group::2 kind::f16
 // with M = 256, N = 256, K = 16, and each CTA's tensor memory receives its 128 x 256 half of the tile.  A tile's whole
 // contraction stays in one of two 256-column accumulators, so the sixteen epilogue warps work on one tile while the next one is
 // summed in the other.  Sums are fp32; the tensor core truncates once per 16 products, which drifts by at most (K / 16) 2^-24
 // of sum |a||b|: 2^-15 at K = 8192, below the half step of every type an epilogue rounds to (2^-12, 2^-9) and of what the loss
 // needs.  (qfmt_gemm_packed16 hands out fp32 sums and takes them in three levels instead, which costs it a third of its rate.)
+//
+// Products that leave pairs without a tile run on single CTAs with 128 x 256 tiles (cta_group::1, 48 KB a stage): twice as many workers
+// for half the rows each, at one and a half times the operand traffic (rule: plan_product).
 //
 // Roles: warps 0 and 3 fill alternate stages, warp 1 issues the MMAs (leader CTA), warp 2 idles, warps 4-19 run the epilogue:
 // warp w has rows 32 (w % 4) .. + 31 and columns 64 ((w - 4) / 4) .. + 63 of its CTA's half, one row a lane, 32 columns at a time.  (With
@@ -33,15 +36,20 @@
 namespace qfmt {
 namespace p16 {
 
-constexpr int kTileM = 256, kTileN = 256, kStageK = 64;  // of a pair
-constexpr int kStages = 5;                 // (three: 64 us for 8192 x 1024 x 4096 without an activation, four 58.6, five 56.9, six 56.4, at
-                                           // the expense of what the epilogues' loads keep in the first-level cache: 84 against 91 us for
-                                           // the backward pass through GELU)
-constexpr uint32_t kStageA = 128 * kStageK * 2, kStageB = 128 * kStageK * 2, kStageBytes = kStageA + kStageB;
+constexpr int kRows = 128, kTileN = 256, kStageK = 64;  // rows of a CTA's tile, columns of a tile, K elements of a stage
+// kPair: shared memory holds half of a tile's columns of B and five stages (three: 64 us for 8192 x 1024 x 4096 without an activation, four
+// 58.6, five 56.9, six 56.4, at the expense of what the epilogues' loads keep in the first-level cache: 84 against 91 us for the backward
+// pass through GELU); otherwise all of them and four stages.
+template <bool kPair>
+struct Staging {
+    static constexpr int kStages = kPair ? 5 : 4, kColumns = kPair ? 128 : 256;
+    static constexpr uint32_t kA = kRows * kStageK * 2, kB = kColumns * kStageK * 2, kBytes = kA + kB;
+};
 constexpr int kThreads = 640, kEpiWarps = 16;
 constexpr uint32_t kBoxBytes = 2048;       // 32 rows x 64 bytes per epilogue warp, 16-byte chunks swizzled with the row
-constexpr uint32_t kSmemBytes = kStages * kStageBytes + kEpiWarps * kBoxBytes + 256 + 1024;
-static_assert(kSmemBytes <= 232448, "shared memory");
+template <bool kPair>
+constexpr uint32_t smem_bytes() { return Staging<kPair>::kStages * Staging<kPair>::kBytes + kEpiWarps * kBoxBytes + 256 + 1024; }
+static_assert(smem_bytes<true>() <= 232448 && smem_bytes<false>() <= 232448, "shared memory");
 constexpr uint32_t kAccCols = 256, kTmemCols = 512;
 constexpr uint32_t kWaitLimit = 1u << 31;  // SM cycles, about a second
 
@@ -264,16 +272,19 @@ __device__ __forceinline__ float column_sum(uint8_t* box, int lane, const pair_t
     return mine;
 }
 
+template <bool kPair>
 __device__ __forceinline__ uint32_t make_idesc(int a_mn, int b_mn, int bf16) {
     const uint32_t ab = bf16 ? 1u : 0u;
     return (1u << 4) | (ab << 7) | (ab << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(kTileN >> 3) << 17) |
-           ((uint32_t)(kTileM >> 4) << 24);
+           ((uint32_t)((kPair ? 2 * kRows : kRows) >> 4) << 24);
 }
 
-template <typename Epi>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
-product16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                 const __grid_constant__ CUtensorMap map_alt, const ProductParams p, const typename Epi::Params ep) {
+template <typename Epi, bool kPair>
+__device__ __forceinline__ void product16_body(const CUtensorMap& map_a, const CUtensorMap& map_b, const CUtensorMap& map_alt,
+                                               const ProductParams& p, const typename Epi::Params& ep) {
+    using S = Staging<kPair>;
+    constexpr int kStages = S::kStages, kTileM = kPair ? 2 * kRows : kRows;
+    constexpr uint32_t kStageBytes = S::kBytes, kStageA = S::kA;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = ptx::smem_addr(smem_raw);
     const uint32_t tiles = (raw + 1023u) & ~1023u;
@@ -287,29 +298,35 @@ product16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     volatile int* abort_flag = reinterpret_cast<volatile int*>(gen_bars + 8 * (2 * kStages + 4) + 8);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = ptx::cluster_ctarank();
+    const uint32_t rank = kPair ? ptx::cluster_ctarank() : 0u;
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
-            ptx::mbar_init(full_bar(s), 2);
+            ptx::mbar_init(full_bar(s), kPair ? 2 : 1);
             ptx::mbar_init(empty_bar(s), 1);
         }
         for (int a = 0; a < 2; ++a) {
             ptx::mbar_init(acc_full_bar(a), 1);
-            ptx::mbar_init(acc_empty_bar(a), 2 * kEpiWarps);
+            ptx::mbar_init(acc_empty_bar(a), (kPair ? 2 : 1) * kEpiWarps);
         }
         *abort_flag = 0;
         ptx::fence_mbar_init();
     }
     if (warp == 1) {
-        ptx::tmem_alloc_pair(ptx::smem_addr(const_cast<uint32_t*>(tmem_slot)), kTmemCols);
-        ptx::tmem_relinquish_pair();
+        const uint32_t slot = ptx::smem_addr(const_cast<uint32_t*>(tmem_slot));
+        if (kPair) {
+            ptx::tmem_alloc_pair(slot, kTmemCols);
+            ptx::tmem_relinquish_pair();
+        } else {
+            ptx::tmem_alloc(slot, kTmemCols);
+            ptx::tmem_relinquish();
+        }
     }
     // global memory from here on
     grid_dependency_wait();
     announce_launch(p.status, p.tag);
     ptx::tc_fence_before_sync();
     __syncthreads();
-    ptx::cluster_sync();  // the peer's barriers exist before anything is signalled to them
+    if (kPair) ptx::cluster_sync();  // the peer's barriers exist before anything is signalled to them
     ptx::tc_fence_after_sync();
     grid_launch_dependents();
     const uint32_t tmem_base = *tmem_slot;
@@ -320,7 +337,7 @@ product16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     const int tiles_m = (M + kTileM - 1) / kTileM, tiles_n = (p.N + kTileN - 1) / kTileN;
     const int kb_total = (K + kStageK - 1) / kStageK;
     const int items = tiles_m * tiles_n * p.splits;
-    const int pairs = gridDim.x >> 1, first = blockIdx.x >> 1;
+    const int workers = kPair ? gridDim.x >> 1 : gridDim.x, first = kPair ? blockIdx.x >> 1 : blockIdx.x;
     // item t: tile t % (tiles_m tiles_n), rows of tiles first so that pairs side by side read the same columns of B
     auto stages_of = [&](int t, int* begin) {
         const int split = t / (tiles_m * tiles_n);
@@ -337,9 +354,9 @@ product16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             uint32_t seq = 0, phase = 0;
             int stage = 0;
             bool dead = false;
-            for (int t = first; t < items && !dead && !*abort_flag; t += pairs) {
+            for (int t = first; t < items && !dead && !*abort_flag; t += workers) {
                 const int tile = t % (tiles_m * tiles_n);
-                const int m0 = (tile % tiles_m) * kTileM + (int)rank * 128, n0 = (tile / tiles_m) * kTileN + (int)rank * 128;
+                const int m0 = (tile % tiles_m) * kTileM + (int)rank * kRows, n0 = (tile / tiles_m) * kTileN + (int)rank * S::kColumns;
                 int kb0;
                 const int nkb = stages_of(t, &kb0);
                 for (int kb = kb0; kb < kb0 + nkb; ++kb) {
@@ -353,23 +370,26 @@ product16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                         break;
                     }
                     const uint32_t sa = tiles + stage * kStageBytes, sb = sa + kStageA;
-                    const uint32_t bar = ptx::map_to_cta(full_bar(stage), 0);
+                    const uint32_t bar = kPair ? ptx::map_to_cta(full_bar(stage), 0) : full_bar(stage);
                     const int k0 = kb * kStageK;
-                    ptx::mbar_expect_tx_cluster(bar, kStageBytes);
-                    if (p.a_blocked) {
-                        ptx::tma_load_3d_pair(sa, ma, bar, 0, k0, m0 >> 6);
-                    } else if (p.a_mn) {
-                        for (int c = 0; c < 2; ++c) ptx::tma_load_2d_pair(sa + c * 8192u, ma, bar, m0 + c * 64, k0);
-                    } else {
-                        ptx::tma_load_2d_pair(sa, ma, bar, k0, m0);
-                    }
-                    if (p.b_blocked) {
-                        ptx::tma_load_3d_pair(sb, mb, bar, 0, k0, n0 >> 6);
-                    } else if (p.b_mn) {
-                        for (int c = 0; c < 2; ++c) ptx::tma_load_2d_pair(sb + c * 8192u, mb, bar, n0 + c * 64, k0);
-                    } else {
-                        ptx::tma_load_2d_pair(sb, mb, bar, k0, n0);
-                    }
+                    if (kPair) ptx::mbar_expect_tx_cluster(bar, kStageBytes);
+                    else ptx::mbar_expect_tx(bar, kStageBytes);
+                    auto load = [&](uint32_t dst, const CUtensorMap* m, int columns, int x0, bool mn, bool blocked) {
+                        if (blocked) {
+                            if (kPair) ptx::tma_load_3d_pair(dst, m, bar, 0, k0, x0 >> 6);
+                            else ptx::tma_load_3d(dst, m, bar, 0, k0, x0 >> 6);
+                        } else if (mn) {
+                            for (int c = 0; c < columns / 64; ++c) {
+                                if (kPair) ptx::tma_load_2d_pair(dst + c * 8192u, m, bar, x0 + c * 64, k0);
+                                else ptx::tma_load_2d(dst + c * 8192u, m, bar, x0 + c * 64, k0);
+                            }
+                        } else {
+                            if (kPair) ptx::tma_load_2d_pair(dst, m, bar, k0, x0);
+                            else ptx::tma_load_2d(dst, m, bar, k0, x0);
+                        }
+                    };
+                    load(sa, ma, kRows, m0, p.a_mn != 0, p.a_blocked != 0);
+                    load(sb, mb, S::kColumns, n0, p.b_mn != 0, p.b_blocked != 0);
                     if (++stage == kStages) { stage = 0; phase ^= 1u; }
                 }
             }
@@ -377,7 +397,7 @@ product16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         __syncwarp();
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
-            const uint32_t idesc = make_idesc(p.a_mn, p.b_mn, p.bf16);
+            const uint32_t idesc = make_idesc<kPair>(p.a_mn, p.b_mn, p.bf16);
             // K-major tile: 128-byte rows, 32 bytes a step.  MN-major: blocks of 64 columns x 64 K rows (8192 bytes), 16 K
             // rows a step.
             const uint32_t a_step = (p.a_mn ? 2048u : 32u) >> 4, b_step = (p.b_mn ? 2048u : 32u) >> 4;
@@ -386,7 +406,7 @@ product16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             int stage = 0;
             uint32_t phase = 0, it = 0;
             bool dead = false;
-            for (int t = first; t < items && !dead; t += pairs) {
+            for (int t = first; t < items && !dead; t += workers) {
                 int kb0;
                 const int nkb = stages_of(t, &kb0);
                 if (nkb == 0) continue;
@@ -407,14 +427,18 @@ product16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                     ptx::tc_fence_after_sync();
                     const uint32_t off = (uint32_t)stage * (kStageBytes >> 4);
 #pragma unroll
-                    for (int k = 0; k < kStageK / 16; ++k)
-                        ptx::mma_f16_pair(d, desc_join(hi, a_lo + off + k * a_step), desc_join(hi, b_lo + off + k * b_step), idesc,
-                                          (kb | k) != 0 ? 1u : 0u);
-                    ptx::mma_commit_pair(empty_bar(stage), 3);
+                    for (int k = 0; k < kStageK / 16; ++k) {
+                        const uint64_t da = desc_join(hi, a_lo + off + k * a_step), db = desc_join(hi, b_lo + off + k * b_step);
+                        if (kPair) ptx::mma_f16_pair(d, da, db, idesc, (kb | k) != 0 ? 1u : 0u);
+                        else ptx::mma_f16(d, da, db, idesc, (kb | k) != 0 ? 1u : 0u);
+                    }
+                    if (kPair) ptx::mma_commit_pair(empty_bar(stage), 3);
+                    else ptx::mma_commit(empty_bar(stage));
                     if (++stage == kStages) { stage = 0; phase ^= 1u; }
                 }
                 if (dead) break;
-                ptx::mma_commit_pair(acc_full_bar(acc), 3);
+                if (kPair) ptx::mma_commit_pair(acc_full_bar(acc), 3);
+                else ptx::mma_commit(acc_full_bar(acc));
             }
         }
         __syncwarp();
@@ -428,14 +452,14 @@ product16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         pt.cols = p.N;
         const int quarter = pt.warp >> 2;
         uint32_t it = 0;
-        for (int t = first; t < items; t += pairs) {
+        for (int t = first; t < items; t += workers) {
             const int tile = t % (tiles_m * tiles_n);
             int kb0;
             const int nkb = stages_of(t, &kb0);
             pt.split = t / (tiles_m * tiles_n);
             pt.tile_m = tile % tiles_m;
             pt.tile_n = tile / tiles_m;
-            pt.row0 = pt.tile_m * kTileM + (int)rank * 128 + pt.quad * 32;
+            pt.row0 = pt.tile_m * kTileM + (int)rank * kRows + pt.quad * 32;
             pt.col0 = pt.tile_n * kTileN + quarter * 64;
             pt.empty = nkb == 0;
             const uint32_t acc = it & 1u, acc_phase = (it >> 1) & 1u;
@@ -451,12 +475,15 @@ product16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 if (!ok || *abort_flag) break;
                 ptx::tc_fence_after_sync();
             }
-            const uint32_t bar = ptx::map_to_cta(acc_empty_bar(acc), 0);
+            const uint32_t bar = kPair ? ptx::map_to_cta(acc_empty_bar(acc), 0) : acc_empty_bar(acc);
             Epi::run(pt, ep, ahead, [&] {  // the accumulator has been read
                 if (nkb != 0) {
                     ptx::tc_fence_before_sync();
                     __syncwarp();
-                    if (lane == 0) ptx::mbar_arrive_cluster(bar);
+                    if (lane == 0) {
+                        if (kPair) ptx::mbar_arrive_cluster(bar);
+                        else ptx::mbar_arrive(bar);
+                    }
                 }
             });
         }
@@ -468,43 +495,93 @@ product16_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     if (*abort_flag) {  // copies in flight land before the shared memory goes
         for (int i = 0; i < 2000; ++i) __nanosleep(1000);
     }
-    ptx::cluster_sync();  // neither CTA leaves while the other may still signal it
+    if (kPair) ptx::cluster_sync();  // neither CTA leaves while the other may still signal it
     if (warp == 1) {
         ptx::tc_fence_after_sync();
-        ptx::tmem_dealloc_pair(tmem_base, kTmemCols);
+        if (kPair) ptx::tmem_dealloc_pair(tmem_base, kTmemCols);
+        else ptx::tmem_dealloc(tmem_base, kTmemCols);
     }
 }
 
+template <typename Epi>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+product16_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                      const __grid_constant__ CUtensorMap map_alt, const ProductParams p, const typename Epi::Params ep) {
+    product16_body<Epi, true>(map_a, map_b, map_alt, p, ep);
+}
+template <typename Epi>
+__global__ void __launch_bounds__(kThreads, 1)
+product16_single_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                        const __grid_constant__ CUtensorMap map_alt, const ProductParams p, const typename Epi::Params ep) {
+    product16_body<Epi, false>(map_a, map_b, map_alt, p, ep);
+}
+
 // ---- host side --------------------------------------------------------------------------------------------------------
+
+// How a product is laid over the GPU: CTA pairs or single CTAs, and parts of K.
+struct ProductPlan {
+    bool pair;
+    int splits, kb_per_split;
+};
+constexpr int64_t kPairs = 74, kSingles = 148;  // the plan goes by a whole GPU, so that workspaces are sized without asking a device
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline int64_t pair_tiles(int64_t M, int64_t N) { return ceil_div(M, 2 * kRows) * ceil_div(N, kTileN); }
+inline int64_t single_tiles(int64_t M, int64_t N) { return ceil_div(M, kRows) * ceil_div(N, kTileN); }
+
+// Single CTAs where every tile of theirs is worked on at once, or where they need at least a quarter fewer rounds.
+// A product of fewer tiles than workers shares its K among them (if `share`), in pieces of at least four stages (256 elements) and at most
+// 16: shorter ones would cost more in moving fp32 sums than they save.
+inline ProductPlan plan_product(int64_t M, int64_t N, int64_t K, bool share) {
+    ProductPlan plan;
+    const int64_t pairs = pair_tiles(M, N), singles = single_tiles(M, N), stages = ceil_div(K, kStageK);
+    const int64_t pair_rounds = ceil_div(pairs, kPairs), single_rounds = ceil_div(singles, kSingles);
+    plan.pair = singles > kSingles && 4 * single_rounds > 3 * pair_rounds;
+    const int64_t tiles = plan.pair ? pairs : singles, workers = plan.pair ? kPairs : kSingles;
+    int64_t n = !share || tiles == 0 ? 1 : workers / tiles;
+    if (n > stages / 4) n = stages / 4;
+    if (n > 16) n = 16;
+    if (n < 1) n = 1;
+    plan.kb_per_split = (int)ceil_div(stages, n);
+    plan.splits = plan.kb_per_split > 0 ? (int)ceil_div(stages, plan.kb_per_split) : 1;
+    return plan;
+}
 
 // An operand of M (or N) x K elements as the kernel fetches it; *blocked: see make_operand_map16.
 struct Operand {
     CUtensorMap map;
     int mn, blocked;
 };
-inline int make_operand(Operand* o, const void* ptr, bool mn, int64_t extent, int64_t k, int64_t ld) {
+inline int make_operand(Operand* o, bool is_b, bool pair, const void* ptr, bool mn, int64_t extent, int64_t k, int64_t ld) {
     o->mn = mn ? 1 : 0;
-    return make_operand_map16(&o->map, reinterpret_cast<const uint16_t*>(ptr), mn, (uint64_t)extent, (uint64_t)k, (uint64_t)ld, 128, &o->blocked);
+    return make_operand_map16(&o->map, reinterpret_cast<const uint16_t*>(ptr), mn, (uint64_t)extent, (uint64_t)k, (uint64_t)ld,
+                              is_b && !pair ? kTileN : kRows, &o->blocked);
 }
 
+// Workspace words, statuses and operands are the caller's; the plan's splits are in p.
 template <typename Epi>
-int launch_product(const Operand& a, const Operand& b, const Operand* alt, ProductParams p, const typename Epi::Params& ep,
+int launch_product(bool pair, const Operand& a, const Operand& b, const Operand* alt, ProductParams p, const typename Epi::Params& ep,
                    const DeviceInfo& dev, cudaStream_t stream) {
     static std::atomic<bool> ready[64];
     const bool known = dev.ordinal >= 0 && dev.ordinal < 64;
     if (!known || !ready[dev.ordinal].load()) {
-        QFMT_CUDA_TRY(cudaFuncSetAttribute(product16_kernel<Epi>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes));
+        QFMT_CUDA_TRY(cudaFuncSetAttribute(product16_pair_kernel<Epi>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<true>()));
+        QFMT_CUDA_TRY(cudaFuncSetAttribute(product16_single_kernel<Epi>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<false>()));
         if (known) ready[dev.ordinal].store(true);
     }
     p.a_mn = a.mn;
     p.b_mn = b.mn;
     p.a_blocked = a.blocked;
     p.b_blocked = b.blocked;
-    const long long items = (long long)((p.M + kTileM - 1) / kTileM) * ((p.N + kTileN - 1) / kTileN) * p.splits;
-    const long long most = dev.sm_count / 2, pairs = items < most ? items : most;
-    if (pairs == 0) return QFMT_OK;
-    QFMT_CUDA_TRY(launch_overlapping(product16_kernel<Epi>, (unsigned)(2 * pairs), (unsigned)kThreads, kSmemBytes, stream, a.map, b.map,
-                                     alt != nullptr ? alt->map : a.map, p, ep));
+    const int64_t items = (pair ? pair_tiles(p.M, p.N) : single_tiles(p.M, p.N)) * p.splits;
+    const int64_t most = pair ? dev.sm_count / 2 : dev.sm_count, workers = items < most ? items : most;
+    if (workers == 0) return QFMT_OK;
+    const CUtensorMap& other = alt != nullptr ? alt->map : a.map;
+    if (pair)
+        QFMT_CUDA_TRY(launch_overlapping(product16_pair_kernel<Epi>, (unsigned)(2 * workers), (unsigned)kThreads, smem_bytes<true>(), stream, a.map,
+                                         b.map, other, p, ep));
+    else
+        QFMT_CUDA_TRY(launch_overlapping(product16_single_kernel<Epi>, (unsigned)workers, (unsigned)kThreads, smem_bytes<false>(), stream, a.map,
+                                         b.map, other, p, ep));
     return QFMT_OK;
 }
 
