@@ -536,9 +536,9 @@ scatter_kernel(const float* __restrict__ sums, int splits, int64_t split_stride,
     }
 }
 
-// ---- at most 32 rows --------------------------------------------------------------------------------------------------------
-// The forward pass as a pass over W: a warp takes 16 words (W stored by word) or 64 at a time and the whole of K, and keeps a maximum
-// and a sum for every row that a lane's words belong to; the block leaves one pair a row.  Rows that do not count ride along.
+// ---- few rows ---------------------------------------------------------------------------------------------------------------
+// The forward pass as a pass over a W that is stored by word: a warp takes 16 words at a time and the whole of K, and keeps a maximum and a
+// sum for every row that a lane's words belong to; the block leaves one pair a row.  Rows that do not count ride along.
 struct FewRows {
     skinny::Operands o;
     const float* bias;
@@ -561,24 +561,38 @@ struct Running {  // sum exp(logit - most)
         sum = __fmaf_rn(s, fast_exp2(__fmul_rn(__fsub_rn(m, now), kLog2E)), __fmul_rn(sum, fast_exp2(__fmul_rn(__fsub_rn(most, now), kLog2E))));
         most = now;
     }
-    __device__ __forceinline__ void add(float logit) { join(logit, logit == -INFINITY ? 0.0f : logit != logit ? logit : 1.0f); }
+    template <int kN>
+    __device__ __forceinline__ void add(const float (&logits)[kN]) {
+        float now = most;
+#pragma unroll
+        for (int i = 0; i < kN; ++i) now = fmaxf(now, logits[i]);
+        if (now == -INFINITY) {
+#pragma unroll
+            for (int i = 0; i < kN; ++i) sum = logits[i] != logits[i] ? logits[i] : sum;
+            return;
+        }
+        sum = __fmul_rn(sum, fast_exp2(__fmul_rn(__fsub_rn(most, now), kLog2E)));
+        most = now;
+#pragma unroll
+        for (int i = 0; i < kN; ++i) sum = __fadd_rn(sum, fast_exp2(__fmul_rn(__fsub_rn(logits[i], now), kLog2E)));
+    }
 };
 
-template <bool kBf16, bool kByK, int kBlocks>
+template <bool kBf16, int kBlocks>
 __global__ void __launch_bounds__(kFewWarps * 32, 8)
 few_rows_kernel(const FewRows f) {
-    constexpr int kWords = kByK ? 64 : 16, kRows = kByK ? 16 * kBlocks : 8 * kBlocks, kLane = 2 * kBlocks;  // rows of a lane
+    constexpr int kWords = 16, kRows = 8 * kBlocks, kLane = 2 * kBlocks;  // kLane: rows of a lane
     __shared__ float2 joined[kFewWarps][kRows];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int groups = (f.o.n + kWords - 1) / kWords;
     {
         const int n0 = ((int)blockIdx.x * kFewWarps + warp) * kWords;
-        if (n0 < f.o.n) skinny::prefetch_weights<kByK>(f.o, n0, 0, f.o.k < kFirst ? f.o.k : kFirst, lane);
+        if (n0 < f.o.n) skinny::prefetch_weights<false>(f.o, n0, 0, f.o.k < kFirst ? f.o.k : kFirst, lane);
     }
     grid_dependency_wait();
     grid_launch_dependents();
     announce_launch(f.status, f.tag);
-    auto row_of = [&](int j) { return kByK ? (j >> 1) * 16 + (j & 1) * 8 + g : (j >> 1) * 8 + 2 * t + (j & 1); };
+    auto row_of = [&](int j) { return (j >> 1) * 8 + 2 * t + (j & 1); };
     int target[kLane];
     Running run[kLane];
 #pragma unroll
@@ -586,41 +600,30 @@ few_rows_kernel(const FewRows f) {
         const int64_t word = row_of(j) < f.o.rows ? f.targets[row_of(j)] : -1;
         target[j] = word >= 0 && word < f.o.n ? (int)word : -1;
     }
-    auto take = [&](int j, int word, float sum) {
-        if (word >= f.o.n) return;
-        const float logit = f.bias != nullptr ? __fadd_rn(sum, f.bias[word]) : sum;
-        run[j].add(logit);
-        if (word == target[j]) f.picked[row_of(j)] = logit;
+    auto logit = [&](int j, int word, float sum) {
+        if (word >= f.o.n) return -INFINITY;
+        const float l = f.bias != nullptr ? __fadd_rn(sum, f.bias[word]) : sum;
+        if (word == target[j]) f.picked[row_of(j)] = l;
+        return l;
     };
     for (int group = (int)blockIdx.x * kFewWarps + warp; group < groups; group += (int)gridDim.x * kFewWarps) {
         const int n0 = group * kWords;
-        if constexpr (kByK) {
-            float d[kBlocks][8][4] = {};
-            skinny::by_k<kBf16, kBlocks>(f.o, n0, 0, f.o.k, lane, d);
+        float d[kBlocks][4] = {};
+        skinny::by_output<kBf16, kBlocks, (kBlocks > 1 ? 2 : 4)>(f.o, n0, 0, f.o.k, lane, d);
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b) {
+        for (int b = 0; b < kBlocks; ++b) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) take(2 * b + (q >> 1), n0 + 16 * t + 8 * (q & 1) + i, d[b][i][q]);
-                }
-            }
-        } else {
-            float d[kBlocks][4] = {};
-            skinny::by_output<kBf16, kBlocks, (kBlocks > 1 ? 2 : 4)>(f.o, n0, 0, f.o.k, lane, d);
-#pragma unroll
-            for (int b = 0; b < kBlocks; ++b) {
-#pragma unroll
-                for (int q = 0; q < 4; ++q) take(2 * b + (q & 1), n0 + g + 8 * (q >> 1), d[b][q]);
+            for (int h = 0; h < 2; ++h) {
+                const float l[2] = {logit(2 * b + h, n0 + g, d[b][h]), logit(2 * b + h, n0 + g + 8, d[b][2 + h])};
+                run[2 * b + h].add(l);
             }
         }
     }
 #pragma unroll
     for (int j = 0; j < kLane; ++j) {  // over the lanes that have other words of the same row
 #pragma unroll
-        for (int o = kByK ? 1 : 4; o < (kByK ? 4 : 32); o <<= 1)
-            run[j].join(__shfl_xor_sync(0xFFFFFFFFu, run[j].most, o), __shfl_xor_sync(0xFFFFFFFFu, run[j].sum, o));
-        if ((kByK ? t : g) == 0) joined[warp][row_of(j)] = make_float2(run[j].most, run[j].sum);
+        for (int o = 4; o < 32; o <<= 1) run[j].join(__shfl_xor_sync(0xFFFFFFFFu, run[j].most, o), __shfl_xor_sync(0xFFFFFFFFu, run[j].sum, o));
+        if (g == 0) joined[warp][row_of(j)] = make_float2(run[j].most, run[j].sum);
     }
     __syncthreads();
     if ((int)threadIdx.x < f.o.rows) {  // at most 32
@@ -743,6 +746,13 @@ Plan plan_backward(const Sizes& s) {
     return p;
 }
 
+// Forward passes that go over W in few_rows_kernel, if it is stored by word: up to eight rows, or up to 32 and 2^25 multiplications
+// (measured against tiles: 8 x 1024 x 30522 24.0 against 26.6 us, 16 27.8 against 26.5; 16 x 256 x 4000 9.6 against 12.6, 32 x 256 x 8000
+// 15.3 against 13.2; a W stored by K took longer than tiles at nearly every size).
+bool few_rows(const Sizes& s) {
+    return s.stored_words && (s.rows <= 8 || (s.rows <= skinny::kMostRows && s.rows * s.vocab * s.hidden <= 1ll << 25));
+}
+
 // The workspace's parts, in order; every one starts on 256 bytes.
 struct Layout {
     size_t size = 0;
@@ -768,7 +778,7 @@ Places places(const Sizes& s, const Plan& plan, bool backward) {
     p.compact_h = l.take((size_t)up(s.rows, 64) * plan.pitch_h * 2);
     if (!backward) {
         // a pair a row for every 64 words of a tile, or for every block of at least 16 words
-        const int64_t words = s.rows <= skinny::kMostRows ? 16 : 64;
+        const int64_t words = few_rows(s) ? 16 : 64;
         p.parts = l.take((size_t)(up(s.vocab, words) / words) * s.rows * sizeof(float2));
         p.picked = l.take((size_t)s.rows * 4);
         p.compact_loss = l.take((size_t)s.rows * 4);
@@ -835,23 +845,13 @@ int word_operand(p16::Operand* o, bool pair, const qfmt_matrix16_t* W, const Siz
     return p16::make_operand(o, true, pair, base, words != s.stored_words, words ? n : s.hidden, words ? s.hidden : n, W->ld);
 }
 
-template <bool kBf16, bool kByK, int kBlocks>
-int launch_few_rows(const FewRows& f, const DeviceInfo& dev, unsigned* blocks, cudaStream_t stream) {
-    constexpr int kWords = kByK ? 64 : 16;
-    const unsigned groups = (unsigned)((f.o.n + kWords - 1) / kWords), want = (groups + kFewWarps - 1) / kFewWarps, most = 8u * dev.sm_count;
-    *blocks = want < most ? want : most;
-    QFMT_CUDA_TRY(launch_overlapping(few_rows_kernel<kBf16, kByK, kBlocks>, *blocks, kFewWarps * 32u, 0, stream, f));
-    return QFMT_OK;
-}
 template <bool kBf16>
-int few_rows_blocks(const FewRows& f, bool by_word, const DeviceInfo& dev, unsigned* blocks, cudaStream_t stream) {
-    if (by_word) {
-        if (f.o.rows <= 8) return launch_few_rows<kBf16, false, 1>(f, dev, blocks, stream);
-        if (f.o.rows <= 16) return launch_few_rows<kBf16, false, 2>(f, dev, blocks, stream);
-        return launch_few_rows<kBf16, false, 4>(f, dev, blocks, stream);
-    }
-    if (f.o.rows <= 16) return launch_few_rows<kBf16, true, 1>(f, dev, blocks, stream);
-    return launch_few_rows<kBf16, true, 2>(f, dev, blocks, stream);
+int launch_few_rows(const FewRows& f, const DeviceInfo& dev, unsigned* blocks, cudaStream_t stream) {
+    const unsigned want = (unsigned)((f.o.n + 16 * kFewWarps - 1) / (16 * kFewWarps)), most = 8u * dev.sm_count;
+    *blocks = want < most ? want : most;
+    auto* kernel = f.o.rows <= 8 ? few_rows_kernel<kBf16, 1> : f.o.rows <= 16 ? few_rows_kernel<kBf16, 2> : few_rows_kernel<kBf16, 4>;
+    QFMT_CUDA_TRY(launch_overlapping(kernel, *blocks, kFewWarps * 32u, 0, stream, f));
+    return QFMT_OK;
 }
 
 // H in the compact copy or in place, as rows of the logits' product or as the K of the weight gradient's.
@@ -972,16 +972,16 @@ extern "C" int qfmt_linear_cross_entropy(const qfmt_matrix16_t* H, const qfmt_ma
     }
     const Plan plan = plan_backward(s);
     const Places pl = places(s, plan, false);
-    if (s.rows <= skinny::kMostRows) {
+    if (few_rows(s)) {
         FewRows f = {skinny::Operands{H->ptr, W->ptr, H->ld, W->ld, (int)s.rows, (int)s.vocab, (int)s.hidden}, d_bias, d_targets,
                      at<float2>(d_workspace, pl.parts), at<float>(d_workspace, pl.picked), static_cast<unsigned long long*>(d_workspace),
                      next_launch_tag()};
         unsigned blocks = 0;
-        if (kind->dtype == QFMT_BF16) rc = few_rows_blocks<true>(f, s.stored_words, dev, &blocks, st);
-        else rc = few_rows_blocks<false>(f, s.stored_words, dev, &blocks, st);
+        if (kind->dtype == QFMT_BF16) rc = launch_few_rows<true>(f, dev, &blocks, st);
+        else rc = launch_few_rows<false>(f, dev, &blocks, st);
         if (rc != QFMT_OK) return rc;
         int team = 32;
-        while (team * s.rows > 32) team /= 2;
+        while (team > 1 && team * s.rows > 32) team /= 2;
         QFMT_CUDA_TRY(launch_overlapping(few_rows_join_kernel, 1u, 1024u, 0, st, (const float2*)f.parts, (int)blocks, (int)s.rows, team, (int)s.vocab,
                                          d_targets, kind->ignore_index, (const float*)f.picked, d_loss, d_lse, d_mean));
         return QFMT_OK;

@@ -335,8 +335,8 @@ row_pass_kernel(const RowPass a) {
     }
 }
 
-// ---- products of at most 32 rows ------------------------------------------------------------------------------------------
-// One launch: a block takes 16 (weights stored by output) or 64 outputs (by K), its warps share K, and up to eight blocks of a cluster share
+// ---- small products ---------------------------------------------------------------------------------------------------------
+// One launch: a block takes 32 rows and 16 (weights stored by output) or 64 outputs (by K), its warps share K, and up to eight blocks of a cluster share
 // it again where that leaves more of the GPU with work.  The warps' sums meet in shared memory and the blocks' in the first one's, both
 // in order; the epilogue takes two outputs a thread.
 struct FewRows {
@@ -345,8 +345,8 @@ struct FewRows {
     const void* residual;
     const void* z_in;
     void *out, *z_out;
-    float* dbias;
-    int64_t ld_residual, ld_z, ld_out;
+    float* sums;  // column sums: of all rows, or [blocks of 32 rows][pitch]
+    int64_t ld_residual, ld_z, ld_out, pitch;
     int k_warp;  // K elements of a warp, a multiple of 32
     unsigned long long* status;
     unsigned long long tag;
@@ -355,7 +355,7 @@ constexpr int kFewWarps = 8;
 
 template <typename T, int kAct, bool kBackward, bool kByK, int kBlocks>
 __global__ void __launch_bounds__(kFewWarps * 32, kByK || kBlocks > 2 ? 2 : 3)
-few_rows_kernel(const FewRows f) {
+few_rows_kernel(FewRows f) {
     constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
     constexpr int kOutputs = kByK ? 64 : 16, kRows = kByK ? 16 * kBlocks : 8 * kBlocks, kPitch = kOutputs + 2, kElements = kRows * kPitch;
     extern __shared__ float few_sums[];  // [warps][rows][outputs]
@@ -364,11 +364,21 @@ few_rows_kernel(const FewRows f) {
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(size));
     const int n0 = (int)(blockIdx.x / size) * kOutputs;
+    {  // the block's rows as a matrix of its own
+        const int64_t r0 = (int64_t)blockIdx.y * skinny::kMostRows;
+        f.o.a += r0 * f.o.lda;
+        f.o.rows = f.o.rows - r0 < skinny::kMostRows ? (int)(f.o.rows - r0) : skinny::kMostRows;
+        f.residual = f.residual != nullptr ? static_cast<const T*>(f.residual) + r0 * f.ld_residual : nullptr;
+        f.z_in = f.z_in != nullptr ? static_cast<const T*>(f.z_in) + r0 * f.ld_z : nullptr;
+        f.z_out = f.z_out != nullptr ? static_cast<T*>(f.z_out) + r0 * f.ld_z : nullptr;
+        f.out = static_cast<T*>(f.out) + r0 * f.ld_out;
+        if (f.sums != nullptr) f.sums += blockIdx.y * f.pitch;
+    }
     const int k0 = ((int)rank * kFewWarps + warp) * f.k_warp;
     skinny::prefetch_weights<kByK>(f.o, n0, k0, k0 + f.k_warp, lane);
     grid_dependency_wait();
     grid_launch_dependents();
-    announce_launch(f.status, f.tag);
+    if (blockIdx.y == 0) announce_launch(f.status, f.tag);
     float* mine = few_sums + warp * kElements;
     // what the epilogue of the thread's first two outputs needs is on its way meanwhile
     const T *residual = static_cast<const T*>(f.residual), *z_in = static_cast<const T*>(f.z_in);
@@ -397,7 +407,7 @@ few_rows_kernel(const FewRows f) {
     Two first_two = operands(threadIdx.x);
     if constexpr (kByK) {
         float d[kBlocks][8][4] = {};
-        skinny::by_k<kBf16, kBlocks>(f.o, n0, k0, k0 + f.k_warp, lane, d);
+        skinny::by_k<kBf16, kBlocks, 1>(f.o, n0, k0, k0 + f.k_warp, lane, d);
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) {
 #pragma unroll
@@ -487,12 +497,12 @@ few_rows_kernel(const FewRows f) {
         y[0] = to_type(v0, T());
         if (second) y[1] = to_type(v1, T());
     }
-    if (kBackward && f.dbias != nullptr) {
+    if (kBackward && f.sums != nullptr) {
         __syncthreads();
         if (threadIdx.x < kOutputs && n0 + (int)threadIdx.x < f.o.n) {
             float s = few_sums[threadIdx.x];
             for (int row = 1; row < rows; ++row) s = __fadd_rn(s, few_sums[row * kPitch + threadIdx.x]);
-            f.dbias[n0 + threadIdx.x] = s;
+            f.sums[n0 + threadIdx.x] = s;
         }
     }
 }
@@ -541,8 +551,16 @@ int product_shape(const qfmt_matrix16_t* A, const qfmt_matrix16_t* B, Shape* s) 
     return QFMT_OK;
 }
 
-// Products of at most 32 rows whose A has its K contiguous go over the weights in few_rows_kernel.
-bool few_rows(const qfmt_matrix16_t* A, const Shape& s) { return s.M <= skinny::kMostRows && A->trans == 0; }
+// Products that go over the weights in few_rows_kernel: up to 2^27 multiplications, which tiles cannot spread over the GPU, and up to 32 rows
+// of any size if the weights are stored by output.  Measured against tiles, with GELU: 128 x 256 x 512 3.0 us by output and 5.1 by K against 11.4,
+// 512 x 512 x 512 7.2 and 7.3 against 10.8; at 2^28 256 x 1024 x 1024 9.5 and 11.3 against 11.8, 1024 x 512 x 512 13.1 and 10.8 against 11.7;
+// 32 x 4096 x 4096 13.8 and 25.8 against 17.4.  A's K must be contiguous.
+constexpr int64_t kFewWork = 1ll << 27;
+bool few_rows(const qfmt_matrix16_t* A, const qfmt_matrix16_t* B, const Shape& s) {
+    if (A->trans != 0) return false;
+    if (B->trans != 0 && s.M <= skinny::kMostRows) return true;
+    return s.M <= 1024 && s.M * s.N <= kFewWork && s.M * s.N * s.K <= kFewWork;
+}
 
 constexpr size_t kHeader = 256;
 size_t sums_bytes(const Shape& s) {  // column sums by groups of 32 rows of whole tiles, or by the row blocks of a pass
@@ -598,7 +616,7 @@ int prepare_call(Call* c, bool backward, const qfmt_matrix16_t* A, const qfmt_ma
     c->splits = plan.splits;
     c->a = p16::Operand{};
     c->b = p16::Operand{};
-    if (s.K != 0 && !few_rows(A, s)) {
+    if (s.K != 0 && !few_rows(A, B, s)) {
         rc = p16::make_operand(&c->a, false, plan.pair, A->ptr, A->trans != 0, s.M, s.K, A->ld);
         if (rc != QFMT_OK) return rc;
         rc = p16::make_operand(&c->b, true, plan.pair, B->ptr, B->trans == 0, s.N, s.K, B->ld);
@@ -633,7 +651,8 @@ int launch_parts(const Call& c, RowPass* a, cudaStream_t stream) {
 }
 
 template <typename T, int kAct, bool kBackward, bool kByK, int kBlocks>
-int launch_few_rows(FewRows f, const DeviceInfo& dev, cudaStream_t stream) {
+int launch_few_rows(const FewRows& f0, const DeviceInfo& dev, cudaStream_t stream) {
+    FewRows f = f0;
     constexpr int kOutputs = kByK ? 64 : 16, kRows = kByK ? 16 * kBlocks : 8 * kBlocks;
     constexpr size_t smem = (size_t)kFewWarps * kRows * (kOutputs + 2) * sizeof(float);
     auto* kernel = few_rows_kernel<T, kAct, kBackward, kByK, kBlocks>;
@@ -646,13 +665,13 @@ int launch_few_rows(FewRows f, const DeviceInfo& dev, cudaStream_t stream) {
         }
     }
     // blocks to a cluster: while there are processors without a block and a warp keeps 64 elements of K
-    const int groups = (f.o.n + kOutputs - 1) / kOutputs;
+    const int groups = (f.o.n + kOutputs - 1) / kOutputs, row_blocks = (f.o.rows + skinny::kMostRows - 1) / skinny::kMostRows;
     int size = 1;
-    while (size < 8 && groups * size * 2 <= dev.sm_count && f.o.k >= size * 2 * kFewWarps * 64) size *= 2;
+    while (size < 8 && groups * row_blocks * size * 2 <= dev.sm_count && f.o.k >= size * 2 * kFewWarps * 64) size *= 2;
     const int per = (f.o.k + size * kFewWarps - 1) / (size * kFewWarps);
     f.k_warp = (per + 31) / 32 * 32;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(groups * size), 1, 1);
+    cfg.gridDim = dim3((unsigned)(groups * size), (unsigned)row_blocks, 1);
     cfg.blockDim = dim3(kFewWarps * 32, 1, 1);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
@@ -680,21 +699,27 @@ int few_rows_call(const Call& c, const qfmt_matrix16_t* A, const qfmt_matrix16_t
     f.ld_z = c.ld_z;
     f.out = d_out;
     f.ld_out = ld_out;
-    f.dbias = d_dbias;
+    const bool join = c.s.M > skinny::kMostRows && d_dbias != nullptr;
+    f.sums = join ? c.sums : d_dbias;
+    f.pitch = padded(c.s.N);
     f.status = c.p.status;
     f.tag = c.p.tag;
+    int rc;
     if (B->trans != 0) {
-        if (c.s.M <= 8) return launch_few_rows<T, kAct, kBackward, false, 1>(f, c.dev, stream);
-        if (c.s.M <= 16) return launch_few_rows<T, kAct, kBackward, false, 2>(f, c.dev, stream);
-        return launch_few_rows<T, kAct, kBackward, false, 4>(f, c.dev, stream);
+        if (c.s.M <= 8) rc = launch_few_rows<T, kAct, kBackward, false, 1>(f, c.dev, stream);
+        else if (c.s.M <= 16) rc = launch_few_rows<T, kAct, kBackward, false, 2>(f, c.dev, stream);
+        else rc = launch_few_rows<T, kAct, kBackward, false, 4>(f, c.dev, stream);
+    } else {
+        if (c.s.M <= 16) rc = launch_few_rows<T, kAct, kBackward, true, 1>(f, c.dev, stream);
+        else rc = launch_few_rows<T, kAct, kBackward, true, 2>(f, c.dev, stream);
     }
-    if (c.s.M <= 16) return launch_few_rows<T, kAct, kBackward, true, 1>(f, c.dev, stream);
-    return launch_few_rows<T, kAct, kBackward, true, 2>(f, c.dev, stream);
+    if (rc != QFMT_OK || !join) return rc;
+    return launch_join_columns(c.sums, f.pitch, (c.s.M + skinny::kMostRows - 1) / skinny::kMostRows, nullptr, 0, nullptr, d_dbias, c.s.N, stream);
 }
 
 template <typename T, int kAct>
 int forward_call(const Call& c, const qfmt_matrix16_t* A, const qfmt_matrix16_t* B, const qfmt_epilogue_t* e, void* d_y, int64_t ldy, cudaStream_t stream) {
-    if (few_rows(A, c.s)) return few_rows_call<T, kAct, false>(c, A, B, e, d_y, ldy, nullptr, stream);
+    if (few_rows(A, B, c.s)) return few_rows_call<T, kAct, false>(c, A, B, e, d_y, ldy, nullptr, stream);
     const bool vr = whole(e->d_residual, c.ld_residual, 2), vz = whole(e->d_z, c.ld_z, 2), vy = whole(d_y, ldy, 2);
     if (c.splits > 1) {
         RowPass a;
@@ -718,7 +743,7 @@ int forward_call(const Call& c, const qfmt_matrix16_t* A, const qfmt_matrix16_t*
 template <typename T, int kAct>
 int backward_call(const Call& c, const qfmt_matrix16_t* A, const qfmt_matrix16_t* B, const qfmt_epilogue_t* e, void* d_dz, int64_t ld_dz,
                   float* d_dbias, cudaStream_t stream) {
-    if (few_rows(A, c.s)) return few_rows_call<T, kAct, true>(c, A, B, e, d_dz, ld_dz, d_dbias, stream);
+    if (few_rows(A, B, c.s)) return few_rows_call<T, kAct, true>(c, A, B, e, d_dz, ld_dz, d_dbias, stream);
     const bool vr = whole(e->d_residual, c.ld_residual, 2), vz = whole(e->d_z, c.ld_z, 2), vd = whole(d_dz, ld_dz, 2);
     const int64_t pitch = padded(c.s.N);
     const int64_t tile_rows = c.pair ? 2 * p16::kRows : p16::kRows;

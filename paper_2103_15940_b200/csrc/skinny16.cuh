@@ -6,8 +6,9 @@
 // registers are 16 contiguous bytes:
 //   by output  (W [N][K])  m16n8k16, the outputs are M and the rows of A are N: lane (g, t) loads 8 K elements 8 t .. of outputs g and g + 8 and
 //              of row g of A, which is two MMAs;
-//   by K       (W [K][N])  m16n8k16, the rows of A are M and the outputs are N: lane (g, t) loads outputs 8 g .. + 7 at K = 2 t, 2 t + 1, 2 t + 8,
-//              2 t + 9; element i of those four goes to the i-th of eight MMAs, whose column g is output 8 g + i.
+//   by K       (W [K][N])  m16n8k16, the rows of A are M and the outputs are N: lane (g, t) loads outputs 8 g .. + 7 at K = 8 t .. 8 t + 7 and
+//              those K of rows g and g + 8 of A, which is two times eight MMAs: element i of the weights goes to the i-th, whose column g
+//              is output 8 g + i.
 // A (at most 32 rows) is read by every warp from the caches.
 #pragma once
 
@@ -112,61 +113,77 @@ __device__ __forceinline__ void by_output(const Operands& o, int n0, int k0, int
     }
 }
 
-// By K: sums over [k0, k1) (k0 a multiple of 16) for outputs n0 .. n0 + 63.  d[b][i][0 .. 3]: row 16 b + g (0, 1) and + 8 (2, 3) of A,
-// output n0 + 16 t + i (0, 2) and n0 + 16 t + 8 + i (1, 3).
-template <bool kBf16, int kBlocks>
+// By K: sums over [k0, k1) (k0 a multiple of 32) for outputs n0 .. n0 + 63.  d[b][i][0 .. 3]: row 16 b + g (0, 1) and + 8 (2, 3) of A,
+// output n0 + 16 t + i (0, 2) and n0 + 16 t + 8 + i (1, 3).  kAhead: 32-element steps whose weights are on their way together.
+template <bool kBf16, int kBlocks, int kAhead>
 __device__ __forceinline__ void by_k(const Operands& o, int n0, int k0, int k1, int lane, float (&d)[kBlocks][8][4]) {
     const int g = lane >> 2, t = lane & 3, n = n0 + 8 * g, end = k1 < o.k ? k1 : o.k;
-    const bool whole = n0 + 64 <= o.n;
-    auto weights = [&](int k) { return k < end && n < o.n ? piece(o.w + (int64_t)k * o.ldw + n, o.n - n) : make_uint4(0, 0, 0, 0); };
-    auto two = [&](int row, int k) -> uint32_t {  // two neighbours of a row of A
-        if (row >= o.rows || k >= end) return 0u;
-        const uint16_t* p = o.a + (int64_t)row * o.lda + k;
-        return k + 1 < end ? *reinterpret_cast<const uint32_t*>(p) : (uint32_t)*p;
-    };
-    for (int k = k0; k < end; k += 32) {
-        uint4 w[2][4];
-        if (whole && k + 32 <= end) {
-            const uint16_t* p = o.w + (int64_t)(k + 2 * t) * o.ldw + n;
+    // rows beyond the last read the last one's: what comes of them is nobody's
+    const uint16_t* a[kBlocks][2];
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const uint16_t* q = p + s * 16 * o.ldw;
-                w[s][0] = *reinterpret_cast<const uint4*>(q);
-                w[s][1] = *reinterpret_cast<const uint4*>(q + o.ldw);
-                w[s][2] = *reinterpret_cast<const uint4*>(q + 8 * o.ldw);
-                w[s][3] = *reinterpret_cast<const uint4*>(q + 9 * o.ldw);
-            }
-        } else {
+    for (int b = 0; b < kBlocks; ++b) {
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const int at = k + s * 16 + 2 * t;
-                w[s][0] = weights(at);
-                w[s][1] = weights(at + 1);
-                w[s][2] = weights(at + 8);
-                w[s][3] = weights(at + 9);
-            }
+        for (int h = 0; h < 2; ++h) {
+            const int row = b * 16 + h * 8 + g;
+            a[b][h] = o.a + (int64_t)(row < o.rows ? row : o.rows - 1) * o.lda + t * 8;
         }
+    }
+    auto multiply = [&](const uint4 (&w)[8], const uint4 (&r)[kBlocks][2]) {
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            const int at = k + s * 16 + 2 * t;
-            uint32_t a[kBlocks][4];
-#pragma unroll
-            for (int b = 0; b < kBlocks; ++b) {
-                a[b][0] = two(b * 16 + g, at);
-                a[b][1] = two(b * 16 + g + 8, at);
-                a[b][2] = two(b * 16 + g, at + 8);
-                a[b][3] = two(b * 16 + g + 8, at + 8);
-            }
-            const uint32_t p0[4] = {w[s][0].x, w[s][0].y, w[s][0].z, w[s][0].w}, p1[4] = {w[s][1].x, w[s][1].y, w[s][1].z, w[s][1].w};
-            const uint32_t p2[4] = {w[s][2].x, w[s][2].y, w[s][2].z, w[s][2].w}, p3[4] = {w[s][3].x, w[s][3].y, w[s][3].z, w[s][3].w};
+            const uint32_t p0[4] = {w[4 * s].x, w[4 * s].y, w[4 * s].z, w[4 * s].w}, p1[4] = {w[4 * s + 1].x, w[4 * s + 1].y, w[4 * s + 1].z, w[4 * s + 1].w};
+            const uint32_t p2[4] = {w[4 * s + 2].x, w[4 * s + 2].y, w[4 * s + 2].z, w[4 * s + 2].w};
+            const uint32_t p3[4] = {w[4 * s + 3].x, w[4 * s + 3].y, w[4 * s + 3].z, w[4 * s + 3].w};
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const uint32_t pick = i & 1 ? 0x7632u : 0x5410u;
                 const uint32_t b0 = __byte_perm(p0[i >> 1], p1[i >> 1], pick), b1 = __byte_perm(p2[i >> 1], p3[i >> 1], pick);
 #pragma unroll
-                for (int b = 0; b < kBlocks; ++b) mma<kBf16>(d[b][i], a[b][0], a[b][1], a[b][2], a[b][3], b0, b1);
+                for (int b = 0; b < kBlocks; ++b) {
+                    if (s == 0) mma<kBf16>(d[b][i], r[b][0].x, r[b][1].x, r[b][0].y, r[b][1].y, b0, b1);
+                    else mma<kBf16>(d[b][i], r[b][0].z, r[b][1].z, r[b][0].w, r[b][1].w, b0, b1);
+                }
             }
         }
+    };
+    int k = k0;
+    {
+        // A piece that reaches beyond the outputs lies before the next row, so it is memory unless the row is the last; outputs beyond the last
+        // piece read that one.
+        const int whole = n0 + 64 <= o.n ? o.k : o.k - 1, limit = end < whole ? end : whole;
+        const uint16_t* w0 = o.w + (int64_t)t * 8 * o.ldw + (n < o.n ? n : (o.n - 1) & ~7);
+        for (; k + 32 * kAhead <= limit; k += 32 * kAhead) {
+            uint4 w[kAhead][8], r[kAhead][kBlocks][2];
+#pragma unroll
+            for (int s = 0; s < kAhead; ++s) {
+                const uint16_t* p = w0 + (int64_t)(k + s * 32) * o.ldw;
+#pragma unroll
+                for (int j = 0; j < 8; ++j, p += o.ldw) w[s][j] = *reinterpret_cast<const uint4*>(p);
+            }
+#pragma unroll
+            for (int s = 0; s < kAhead; ++s) {
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b) {
+                    r[s][b][0] = *reinterpret_cast<const uint4*>(a[b][0] + k + s * 32);
+                    r[s][b][1] = *reinterpret_cast<const uint4*>(a[b][1] + k + s * 32);
+                }
+            }
+#pragma unroll
+            for (int s = 0; s < kAhead; ++s) multiply(w[s], r[s]);
+        }
+    }
+    for (; k < end; k += 32) {
+        const int left = end - k - t * 8;
+        uint4 w[8], r[kBlocks][2];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            w[j] = j < left && n < o.n ? piece(o.w + (int64_t)(k + t * 8 + j) * o.ldw + n, o.n - n) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) {
+            r[b][0] = piece(a[b][0] + k, left);
+            r[b][1] = piece(a[b][1] + k, left);
+        }
+        multiply(w, r);
     }
 }
 

@@ -382,3 +382,18 @@ def test_few_rows_with_words_taken_out_and_targets_that_are_none():
     p.bias[:] = -3.4e38
     p.h[:] = 0.0
     assert bool((p.forward()[1][:3] == p.bias[0]).all())
+
+
+@pytest.mark.parametrize("words", [True, False])
+@pytest.mark.parametrize("shape", [(33, 64, 1000), (64, 40, 30000), (100, 200, 777), (500, 33, 100), (1000, 64, 515), (1024, 100, 1000)])
+def test_little_work(shape, words):
+    """Passes over W for blocks of 32 rows, the mean over all of them."""
+    for ignored in (0.0, 0.4):
+        p = Problem(*shape, "bf16", words, ignored, seed=shape[0])
+        p.check_forward()
+    p.targets[shape[0] // 2] = -7
+    loss, lse, mean = p.forward()
+    assert int(torch.isnan(loss).sum()) == 1 and bool(torch.isnan(mean))
+    p.targets[:] = IGNORED
+    loss, lse, mean = p.forward()
+    assert not loss.any() and not lse.any() and not mean.any()
