@@ -237,15 +237,20 @@ __device__ __forceinline__ void pass_store(T* p, unsigned there, int lane, const
     }
 }
 
-constexpr int kPassWarps = 8, kPassPerSm = 6;
+constexpr int kPassWarps = 8, kPassPerSm = 4;
 
-// At most 40 registers for whole pieces of a gradient: forty-eight warps an SM hide the loads behind one another's arithmetic, and a row fetched ahead or two rows at a
-// time, with fewer warps, do not (54 us of 8192 x 4096 bfloat16 with the next row in registers).
+//
+// Whole pieces of a gradient come through a ring in shared memory, a lane's own pieces at its own place, so that several rows of every warp
+// are on their way at all times without holding registers: with the loads of one row at a time 8192 x 4096 bfloat16 takes 54 to 56 us,
+// whether with 16, 32 or 48 warps an SM.
 template <typename T, int kAct, bool kBackward, bool kParts, bool kVec>
-__global__ void __launch_bounds__(kPassWarps * 32, kVec && !kParts ? kPassPerSm : 4)
+__global__ void __launch_bounds__(kPassWarps * 32, 4)
 row_pass_kernel(const RowPass a) {
-    constexpr bool kPrecise = sizeof(T) == 4;
+    constexpr bool kPrecise = sizeof(T) == 4, kRing = kVec && !kParts, kZ = kAct != QFMT_ACT_NONE;
+    constexpr int kPieces = (int)sizeof(T) / 2 * (kZ ? 2 : 1);   // 16-byte pieces of a row and lane
+    constexpr int kDepth = 8 / kPieces;                          // rows on their way
     __shared__ float sums[kPassWarps][256];
+    __shared__ uint4 ring[kRing ? kDepth : 1][kPieces][kPassWarps * 32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t col0 = (int64_t)(blockIdx.x % a.strips) * 256;
     const int64_t block = blockIdx.x / a.strips, first = block * a.rows_per_block;
@@ -263,10 +268,41 @@ row_pass_kernel(const RowPass a) {
     }
     const T *residual = static_cast<const T*>(a.residual), *z_in = static_cast<const T*>(a.z_in);
     T *out = static_cast<T*>(a.out), *z_out = static_cast<T*>(a.z_out);
+    const T* const dy = static_cast<const T*>(a.dy);
+    auto ask = [&](int64_t row, int slot) {
+        if (row < end && there) {
+            const T* p = dy + row * a.ld_dy + col0 + lane * 8;
+            const T* q = kZ ? z_in + row * a.ld_z + col0 + lane * 8 : nullptr;
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const uint4* from = i < (int)sizeof(T) / 2 ? reinterpret_cast<const uint4*>(p) + i : reinterpret_cast<const uint4*>(q) + (i - (int)sizeof(T) / 2);
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ptx::smem_addr(&ring[slot][i][threadIdx.x])), "l"(from) : "memory");
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");  // committed even when empty: the waits count groups
+    };
+    int slot = 0;
+    if constexpr (kRing) {
+#pragma unroll
+        for (int i = 0; i < kDepth; ++i) ask(first + warp + i * kPassWarps, i);
+    }
 #pragma unroll 1
     for (int64_t row = first + warp; row < end; row += kPassWarps) {
-        float v[8];
-        if constexpr (kParts) {
+        float v[8], z[8];
+        if constexpr (kRing) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
+            uint4 w[kPieces];
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) w[i] = ring[slot][i][threadIdx.x];
+            ask(row + kDepth * kPassWarps, slot);
+            slot = slot + 1 == kDepth ? 0 : slot + 1;
+            const T* e = reinterpret_cast<const T*>(w);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                v[k] = (float)e[k];
+                if (kZ) z[k] = (float)e[8 + k];
+            }
+        } else if constexpr (kParts) {
             const float* part = a.parts + row * a.pitch + col0;
             pass_load<float, kVec>(part, there, lane, v);
 #pragma unroll 2
@@ -278,13 +314,12 @@ row_pass_kernel(const RowPass a) {
                 for (int k = 0; k < 8; ++k) v[k] = __fadd_rn(v[k], w[k]);
             }
         } else {
-            pass_load<T, kVec>(static_cast<const T*>(a.dy) + row * a.ld_dy + col0, there, lane, v);
+            pass_load<T, kVec>(dy + row * a.ld_dy + col0, there, lane, v);
         }
         float r[8];
         if (kBackward) {
             if constexpr (kAct != QFMT_ACT_NONE) {
-                float z[8];
-                pass_load<T, kVec>(z_in + row * a.ld_z + col0, there, lane, z);
+                if constexpr (!kRing) pass_load<T, kVec>(z_in + row * a.ld_z + col0, there, lane, z);
                 if (residual != nullptr) {
                     pass_load<T, kVec>(residual + row * a.ld_residual + col0, there, lane, r);
 #pragma unroll
