@@ -146,8 +146,8 @@ _calls_error: Optional[ImportError] = None
 
 
 def _bind_calls(L: ctypes.CDLL) -> None:
-    """The sub-layer calls go through a module of their own, since generic conversion takes as long as their GPU work.  Without
-    it they raise; nothing else needs it."""
+    """The sub-layer calls and those around a step's last products go through a module of their own, since generic conversion takes
+    as long as their GPU work.  Without it they raise; nothing else needs it."""
     global _calls, _calls_error
     try:
         from . import _calls
@@ -157,6 +157,9 @@ def _bind_calls(L: ctypes.CDLL) -> None:
     _calls.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
         L.qfmt_dropout, L.qfmt_layer_norm, L.qfmt_layer_norm_backward, L.qfmt_dropout_add_layer_norm,
         L.qfmt_dropout_add_layer_norm_backward)))
+    _calls.bind_step(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+        L.qfmt_linear_act, L.qfmt_linear_act_backward, L.qfmt_act_backward, L.qfmt_linear_cross_entropy,
+        L.qfmt_linear_cross_entropy_backward, L.qfmt_grad_norm, L.qfmt_grad_clip)))
 
 
 def _bind_optional(L: ctypes.CDLL) -> None:
@@ -524,8 +527,8 @@ def _ref(record, kind):
     return ctypes.addressof(record)
 
 
-def _sublayer(name: str, *args) -> None:
-    """One of the sub-layer calls: integers, tensors or None, in the order of include/qfmt.h."""
+def _module_call(name: str, *args) -> None:
+    """One of the calls that go through the C module: numbers, tensors or None, in the order of include/qfmt.h."""
     if _lib is None:
         lib()
     if _calls is None:
@@ -539,14 +542,14 @@ def _sublayer(name: str, *args) -> None:
 def qfmt_dropout(d_x, ld_x: int, d_residual, ld_residual: int, d_out, ld_out: int, rows: int, cols: int, dtype,
                  drop: qfmt_dropout_t, stream=None) -> None:
     """out = residual + D(x), and D's own backward pass; see qfmt_dropout in include/qfmt.h."""
-    _sublayer("dropout", d_x, ld_x, d_residual, ld_residual, d_out, ld_out, rows, cols, _storage(dtype),
+    _module_call("dropout", d_x, ld_x, d_residual, ld_residual, d_out, ld_out, rows, cols, _storage(dtype),
               _ref(drop, qfmt_dropout_t), _stream_handle(stream))
 
 
 def qfmt_layer_norm(norm: qfmt_norm_t, d_x, d_weight, d_bias, d_y, d_mean=None, d_rstd=None,
                     fmt: Optional[qfmt_format_t] = None, d_stats=None, accumulate: int = 0, stream=None) -> None:
     """y = LN(x), rounded to fmt with statistics if one is given; see qfmt_layer_norm in include/qfmt.h."""
-    _sublayer("layer_norm", _ref(norm, qfmt_norm_t), d_x, d_weight, d_bias, d_y, d_mean, d_rstd, _ref(fmt, qfmt_format_t),
+    _module_call("layer_norm", _ref(norm, qfmt_norm_t), d_x, d_weight, d_bias, d_y, d_mean, d_rstd, _ref(fmt, qfmt_format_t),
               d_stats, accumulate, _stream_handle(stream))
 
 
@@ -558,7 +561,7 @@ def qfmt_layer_norm_backward(norm: qfmt_norm_t, d_dy, d_x, d_mean, d_rstd, d_wei
                              workspace_bytes: int, fmt: Optional[qfmt_format_t] = None, d_stats=None, accumulate: int = 0,
                              stream=None) -> None:
     """Gradients of LN's input, weight and bias; see qfmt_layer_norm_backward in include/qfmt.h."""
-    _sublayer("layer_norm_backward", _ref(norm, qfmt_norm_t), d_dy, d_x, d_mean, d_rstd, d_weight, d_dx, d_dweight, d_dbias,
+    _module_call("layer_norm_backward", _ref(norm, qfmt_norm_t), d_dy, d_x, d_mean, d_rstd, d_weight, d_dx, d_dweight, d_dbias,
               _ref(fmt, qfmt_format_t), d_stats, accumulate, d_workspace, workspace_bytes, _stream_handle(stream))
 
 
@@ -566,7 +569,7 @@ def qfmt_dropout_add_layer_norm(norm: qfmt_norm_t, drop: Optional[qfmt_dropout_t
                                 d_mean=None, d_rstd=None, fmt: Optional[qfmt_format_t] = None, d_stats=None,
                                 accumulate: int = 0, stream=None) -> None:
     """h = residual + D(x), y = LN(h) in one pass; see qfmt_dropout_add_layer_norm in include/qfmt.h."""
-    _sublayer("dropout_add_layer_norm", _ref(norm, qfmt_norm_t), _ref(drop, qfmt_dropout_t), d_x, d_residual, d_weight, d_bias, d_h,
+    _module_call("dropout_add_layer_norm", _ref(norm, qfmt_norm_t), _ref(drop, qfmt_dropout_t), d_x, d_residual, d_weight, d_bias, d_h,
               d_y, d_mean, d_rstd, _ref(fmt, qfmt_format_t), d_stats, accumulate, _stream_handle(stream))
 
 
@@ -576,7 +579,7 @@ def qfmt_dropout_add_layer_norm_backward(norm: qfmt_norm_t, drop: Optional[qfmt_
                                          stream=None) -> None:
     """dresidual = dh + LN's gradient, dx = D(dresidual), dweight, dbias; see
     qfmt_dropout_add_layer_norm_backward in include/qfmt.h."""
-    _sublayer("dropout_add_layer_norm_backward", _ref(norm, qfmt_norm_t), _ref(drop, qfmt_dropout_t), d_dy, d_dh, d_h, d_mean, d_rstd, d_weight,
+    _module_call("dropout_add_layer_norm_backward", _ref(norm, qfmt_norm_t), _ref(drop, qfmt_dropout_t), d_dy, d_dh, d_h, d_mean, d_rstd, d_weight,
               d_dx, d_dresidual, d_dweight, d_dbias, _ref(fmt, qfmt_format_t), d_stats, accumulate, d_workspace, workspace_bytes,
               _stream_handle(stream))
 
@@ -593,16 +596,15 @@ def qfmt_linear_act_workspace_bytes(A: qfmt_matrix_t, B: qfmt_matrix_t) -> int:
 def qfmt_linear_act(A: qfmt_matrix_t, B: qfmt_matrix_t, epilogue: qfmt_epilogue_t, d_y, ldy: int, dtype, d_workspace,
                     workspace_bytes: int, stream=None) -> None:
     """y = act(op(A) op(B) + bias) + residual on 16-bit codes; see qfmt_linear_act in include/qfmt.h."""
-    _check(lib().qfmt_linear_act(_ref(A, qfmt_matrix_t), _ref(B, qfmt_matrix_t), _ref(epilogue, qfmt_epilogue_t), _ptr(d_y), ldy,
-                                 _storage(dtype), _ptr(d_workspace), workspace_bytes, _stream_handle(stream)), "qfmt_linear_act")
+    _module_call("linear_act", _ref(A, qfmt_matrix_t), _ref(B, qfmt_matrix_t), _ref(epilogue, qfmt_epilogue_t), d_y, ldy, _storage(dtype),
+                 d_workspace, workspace_bytes, _stream_handle(stream))
 
 
 def qfmt_linear_act_backward(A: qfmt_matrix_t, B: qfmt_matrix_t, epilogue: qfmt_epilogue_t, d_dz, ld_dz: int, d_dbias, dtype,
                              d_workspace, workspace_bytes: int, stream=None) -> None:
     """dz = (op(A) op(B) + residual) act'(z) and its column sums; see qfmt_linear_act_backward in include/qfmt.h."""
-    _check(lib().qfmt_linear_act_backward(_ref(A, qfmt_matrix_t), _ref(B, qfmt_matrix_t), _ref(epilogue, qfmt_epilogue_t), _ptr(d_dz),
-                                          ld_dz, _ptr(d_dbias), _storage(dtype), _ptr(d_workspace), workspace_bytes,
-                                          _stream_handle(stream)), "qfmt_linear_act_backward")
+    _module_call("linear_act_backward", _ref(A, qfmt_matrix_t), _ref(B, qfmt_matrix_t), _ref(epilogue, qfmt_epilogue_t), d_dz, ld_dz, d_dbias,
+                 _storage(dtype), d_workspace, workspace_bytes, _stream_handle(stream))
 
 
 def qfmt_act_backward_workspace_bytes(rows: int, cols: int) -> int:
@@ -612,8 +614,8 @@ def qfmt_act_backward_workspace_bytes(rows: int, cols: int) -> int:
 def qfmt_act_backward(d_dy, ld_dy: int, d_z, ld_z: int, d_dz, ld_dz: int, d_dbias, rows: int, cols: int, dtype, act: int,
                       d_workspace=None, workspace_bytes: int = 0, stream=None) -> None:
     """dz = dy act'(z) and its column sums; see qfmt_act_backward in include/qfmt.h."""
-    _check(lib().qfmt_act_backward(_ptr(d_dy), ld_dy, _ptr(d_z), ld_z, _ptr(d_dz), ld_dz, _ptr(d_dbias), rows, cols, _storage(dtype), act,
-                                   _ptr(d_workspace), workspace_bytes, _stream_handle(stream)), "qfmt_act_backward")
+    _module_call("act_backward", d_dy, ld_dy, d_z, ld_z, d_dz, ld_dz, d_dbias, rows, cols, _storage(dtype), act, d_workspace, workspace_bytes,
+                 _stream_handle(stream))
 
 
 def make_cross_entropy(dtype, ignore_index: int = -100, mean: bool = True) -> qfmt_cross_entropy_t:
@@ -629,19 +631,16 @@ def qfmt_linear_cross_entropy_workspace_bytes(H: qfmt_matrix_t, W: qfmt_matrix_t
 def qfmt_linear_cross_entropy(H: qfmt_matrix_t, W: qfmt_matrix_t, kind: qfmt_cross_entropy_t, d_bias, d_targets, d_loss, d_lse, d_mean,
                               d_workspace, workspace_bytes: int, stream=None) -> None:
     """Softmax cross entropy of the logits H op(W) + bias; see qfmt_linear_cross_entropy in include/qfmt.h."""
-    _check(lib().qfmt_linear_cross_entropy(_ref(H, qfmt_matrix_t), _ref(W, qfmt_matrix_t), _ref(kind, qfmt_cross_entropy_t), _ptr(d_bias),
-                                           _ptr(d_targets), _ptr(d_loss), _ptr(d_lse), _ptr(d_mean), _ptr(d_workspace), workspace_bytes,
-                                           _stream_handle(stream)), "qfmt_linear_cross_entropy")
+    _module_call("linear_cross_entropy", _ref(H, qfmt_matrix_t), _ref(W, qfmt_matrix_t), _ref(kind, qfmt_cross_entropy_t), d_bias, d_targets,
+                 d_loss, d_lse, d_mean, d_workspace, workspace_bytes, _stream_handle(stream))
 
 
 def qfmt_linear_cross_entropy_backward(H: qfmt_matrix_t, W: qfmt_matrix_t, kind: qfmt_cross_entropy_t, d_bias, d_targets, d_lse, d_dloss,
                                        d_dls, d_dh, ld_dh: int, d_dw, ld_dw: int, d_dbias, d_workspace, workspace_bytes: int,
                                        stream=None) -> None:
     """Gradients of H, W and bias; see qfmt_linear_cross_entropy in include/qfmt.h."""
-    _check(lib().qfmt_linear_cross_entropy_backward(_ref(H, qfmt_matrix_t), _ref(W, qfmt_matrix_t), _ref(kind, qfmt_cross_entropy_t),
-                                                    _ptr(d_bias), _ptr(d_targets), _ptr(d_lse), _ptr(d_dloss), _ptr(d_dls), _ptr(d_dh),
-                                                    ld_dh, _ptr(d_dw), ld_dw, _ptr(d_dbias), _ptr(d_workspace), workspace_bytes,
-                                                    _stream_handle(stream)), "qfmt_linear_cross_entropy_backward")
+    _module_call("linear_cross_entropy_backward", _ref(H, qfmt_matrix_t), _ref(W, qfmt_matrix_t), _ref(kind, qfmt_cross_entropy_t), d_bias,
+                 d_targets, d_lse, d_dloss, d_dls, d_dh, ld_dh, d_dw, ld_dw, d_dbias, d_workspace, workspace_bytes, _stream_handle(stream))
 
 
 def make_tensors(tensors, outs=None):
@@ -672,10 +671,9 @@ def qfmt_grad_norm_workspace_bytes(count: int, chunks: int) -> int:
 def qfmt_grad_norm(d_tensors, count: int, chunks: int, max_norm: float, d_dls, d_norm, d_stats, d_workspace, workspace_bytes: int,
                    stream=None) -> None:
     """Norm of all tensors of a list and the factor that clips them; see qfmt_grad_norm in include/qfmt.h."""
-    _check(lib().qfmt_grad_norm(_ptr(d_tensors), count, chunks, max_norm, _ptr(d_dls), _ptr(d_norm), _ptr(d_stats), _ptr(d_workspace),
-                                workspace_bytes, _stream_handle(stream)), "qfmt_grad_norm")
+    _module_call("grad_norm", d_tensors, count, chunks, max_norm, d_dls, d_norm, d_stats, d_workspace, workspace_bytes, _stream_handle(stream))
 
 
 def qfmt_grad_clip(d_tensors, count: int, chunks: int, d_norm, stream=None) -> None:
     """Every tensor of a list times the factor; see qfmt_grad_norm in include/qfmt.h."""
-    _check(lib().qfmt_grad_clip(_ptr(d_tensors), count, chunks, _ptr(d_norm), _stream_handle(stream)), "qfmt_grad_clip")
+    _module_call("grad_clip", d_tensors, count, chunks, d_norm, _stream_handle(stream))
