@@ -573,7 +573,9 @@ int qfmt_dropout_add_layer_norm_backward(const qfmt_norm_t* norm, const qfmt_dro
  * Operands as for qfmt_gemm_packed16 (16-byte aligned, leading dimensions multiples of 8, either one transposed), both of
  * storage type dtype: QFMT_F16 (1/5/10 codes) or QFMT_BF16 (1/8/7 codes).  Sums, bias and activation are in 32 bits; y and z
  * are rounded to the storage type once each (to nearest even; what overflows becomes infinite, as in qfmt_quantize_stats).
- * The activation takes the 32-bit z.  No statistics are kept: qfmt_linear_forward and qfmt_bias_quantize_stats_pack16 do that.
+ * The activation takes the 32-bit z.  A sum over K may be off by (K / 16 + 24) 2^-23 sum |a||b| (the tensor core truncates each of its
+ * additions of 16 products, where qfmt_gemm_packed16 takes sums in levels): far below the half step of a code, and relative errors of
+ * 10^-6 (K = 1024) to 5 10^-6 (K = 4096) are what bias gradients show of it.  No statistics are kept: qfmt_linear_forward and qfmt_bias_quantize_stats_pack16 do that.
  *   QFMT_ACT_NONE z, QFMT_ACT_RELU max(z, 0), QFMT_ACT_GELU z Phi(z), QFMT_ACT_SILU z / (1 + exp(-z)),
  *   QFMT_ACT_GELU_TANH z / 2 (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3)))
  */
@@ -657,7 +659,8 @@ size_t qfmt_act_backward_workspace_bytes(int64_t rows, int64_t cols);
  *   d_dw, ld_dw  device, the stored shape of W, of the storage type, or NULL
  *   d_dbias      device, V floats, or NULL (sums of the 32-bit d)
  *   d_workspace  at least qfmt_linear_cross_entropy_workspace_bytes(H, W, 1) bytes
- * d_dh and d_dw may start on any element.  Errors: QFMT_ERR_BAD_ARG, QFMT_ERR_UNSUPPORTED_ARCH, QFMT_ERR_CUDA.
+ * d_dh and d_dw may start on any element; no output may overlap an input (an error the library cannot detect).  Sums over D as in
+ * qfmt_linear_act.  Errors: QFMT_ERR_BAD_ARG, QFMT_ERR_UNSUPPORTED_ARCH, QFMT_ERR_CUDA.
  */
 typedef struct {
     int64_t ignore_index;     /* target of rows that do not count, e.g. -100                        */
@@ -677,7 +680,7 @@ size_t qfmt_linear_cross_entropy_workspace_bytes(const qfmt_matrix16_t* H, const
  * The norm of all gradients of a step, and clipping by it.  The tensors are described by records in DEVICE memory, so that a
  * list is built once and captured graphs can use it: fill src, dst, n and dtype of `count` records on the host, let
  * qfmt_plan_tensors check them and number their chunks (it returns the chunks of the whole list, or an error < 0), and copy
- * the records to the device.
+ * the records to the device.  count and chunks of the calls below are those of that plan (the kernels walk the list by them).
  */
 typedef struct {
     const void* src;          /* device, n elements, any alignment of an element (NULL if n = 0)      */

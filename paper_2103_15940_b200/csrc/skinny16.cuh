@@ -1,5 +1,5 @@
-// Products of 16-bit codes with at most 32 rows: every weight is used for a few rows only, so the product is a pass over the weights,
-// bound by memory, and 256 x 256 tiles would leave most of the GPU idle.
+// Products of 16-bit codes with few rows, or with little work at all: a weight is used for at most 32 rows at a time, so the product is a
+// pass over the weights, bound by memory or by latency, and tiles of 128 x 256 would leave most of the GPU idle.
 //
 // A warp takes 16 (weights stored by output) or 64 (stored by K) outputs and walks K; the weights go from memory straight into the
 // registers that mma.sync reads.  The order of K within an MMA is free as long as both operands agree, so it is chosen such that a lane's
