@@ -652,8 +652,8 @@ size_t qfmt_act_backward_workspace_bytes(int64_t rows, int64_t cols);
  *     d = g (exp(logits - lse) - onehot(target)),  dH = d op(W)^T,  dW = the gradient of W as W is stored,  dbias = sums of d,
  *     g = dloss (1 if d_dloss is NULL) * (1 / rows that count, if kind->mean) * (d_dls->scale, if given).
  * The logits are formed again, a piece of the vocabulary at a time; d passes from one product to the next rounded to the storage
- * type (binary16: times a power of two that puts the largest |g| at 2^13, so what is lost lies 2^-37 below it), which is the one
- * rounding besides those of the results.
+ * type, which is the one rounding besides those of the results.  It does so without the factors that all rows share, which multiply the
+ * sums in 32 bits, and times a power of two that puts the largest |dloss| at 2^13 (in binary16 what is lost lies 2^-37 below it).
  *   d_dloss      device, tokens floats, or NULL;  d_dls  device, 8-byte aligned, or NULL: the loss scale is read when the kernels run
  *   d_dh, ld_dh  device, tokens x D of the storage type, or NULL; rows that do not count get zeros
  *   d_dw, ld_dw  device, the stored shape of W, of the storage type, or NULL
