@@ -647,7 +647,8 @@ size_t qfmt_act_backward_workspace_bytes(int64_t rows, int64_t cols);
  *   d_mean       device, one float, or NULL: the mean loss of the rows that count (0 if none does)
  *   d_workspace  device, 16-byte aligned, at least qfmt_linear_cross_entropy_workspace_bytes(H, W, 0) bytes; status area and
  *                sharing as for qfmt_gemm
- * Sums, exponentials and statistics are in 32 bits; results do not depend on the order in which blocks run.
+ * Sums, exponentials and statistics are in 32 bits, the loss is subtracted in 64 (lse is rounded to 32); results do not depend on the
+ * order in which blocks run.
  * The backward pass, with the same H, W, bias and targets and the forward pass's lse:
  *     d = g (exp(logits - lse) - onehot(target)),  dH = d op(W)^T,  dW = the gradient of W as W is stored,  dbias = sums of d,
  *     g = dloss (1 if d_dloss is NULL) * (1 / rows that count, if kind->mean) * (d_dls->scale, if given).

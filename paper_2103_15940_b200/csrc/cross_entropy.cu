@@ -427,6 +427,10 @@ struct AddEpilogue {
 
 // ---- joining ----------------------------------------------------------------------------------------------------------------
 
+// lse - logit in 64 bits: rounded to 32 before the subtraction, lse takes half a step of the largest logit's size from every loss (2e-6 where
+// logits are around 50, all of a small loss).
+__device__ __forceinline__ float loss_of(float most, float log, float picked) { return (float)((double)most + (double)log - (double)picked); }
+
 constexpr int kJoinRows = 32, kJoinParts = 32;
 
 // Block of 32 rows x 32 groups: group q joins a row's parts q, q + 32, ..., then a warp a row joins the groups' (halves onto halves).
@@ -465,8 +469,9 @@ join_rows_kernel(const float2* __restrict__ parts, int64_t pitch, int n_parts, c
     if (r == 0) {
         float l = 0.0f;
         if (mine < count) {
-            float lse = __fadd_rn(m, logf(s));
-            l = __fsub_rn(lse, picked[mine]);
+            const float log = logf(s);
+            float lse = __fadd_rn(m, log);
+            l = loss_of(m, log, picked[mine]);
             if (target[mine] < 0) l = lse = __int_as_float(0x7FC00000);  // the target is not a word
             const int to = index[mine];
             if (loss != nullptr) loss[to] = l;
@@ -672,8 +677,9 @@ few_rows_join_kernel(const float2* __restrict__ parts, int n_parts, int rows, in
             const int64_t target = targets[row];
             float lse = 0.0f, l = 0.0f;
             if (target != ignore) {
-                lse = __fadd_rn(all.most, logf(all.sum));
-                if (target >= 0 && target < vocab) l = __fsub_rn(lse, picked[row]);
+                const float log = logf(all.sum);
+                lse = __fadd_rn(all.most, log);
+                if (target >= 0 && target < vocab) l = loss_of(all.most, log, picked[row]);
                 else l = lse = __int_as_float(0x7FC00000);  // the target is not a word
                 counted[row] = 1;
             }

@@ -10,6 +10,44 @@ from test_cross_entropy_gpu import IGNORED, Problem
 pytestmark = pytest.mark.gpu
 
 
+def definition(p):
+    """lse and loss of all rows in 64 bits; a row's largest logit taken out of both before they are subtracted."""
+    logits = p.h.double() @ (p.w.t() if p.words else p.w).double() + p.bias.double()
+    most = logits.amax(dim=1, keepdim=True)
+    log = torch.log(torch.exp(logits - most).sum(dim=1))
+    return most[:, 0] + log, (most[:, 0] - logits.gather(1, p.targets[:, None])[:, 0]) + log
+
+
+@pytest.mark.parametrize("rows", [3, 8, 40, 130])
+@pytest.mark.parametrize("level", [50.0, 1000.0, -3.0e4])
+def test_a_loss_is_not_rounded_to_the_logits_steps(rows, level):
+    """Logits far from zero whose differences are small: the loss is formed from differences.  With H = 0 the logits are the bias, exactly."""
+    p = Problem(rows, 64, 300, "bf16", scale=0.0)
+    p.bias.mul_(0.25).add_(level)
+    p.targets[:] = torch.arange(rows, device="cuda") * 2
+    p.bias[0] = level + 10.0  # of the first row's target: its loss is small
+    loss, lse, mean = p.forward()
+    lse64, loss64 = definition(p)
+    assert float(loss64[0]) < 0.05 and float(loss64[1]) > 1.0
+    # exponentials and their sum 2^-19 of the sum, whose logarithm has as large an absolute error; the logarithm's and the result's rounding
+    close(loss, loss64, loss64 * 2.0 ** -22 + 2.0 ** -19)
+    close(lse, lse64, 2.0 ** -19 + lse64.abs() * 2.0 ** -23)
+    close(mean, loss64.mean().view(1), loss64.mean().view(1) * 2.0 ** -22 + 2.0 ** -19)
+
+
+@pytest.mark.parametrize("rows", [3, 40])
+def test_the_least_loss(rows):
+    """A word with all but 10^-4 of the probability, logits around 50.  The sum of exponentials is near 1 and takes at most 16 additions on its
+    way, half a step of 2^-23 each; a step of the logits' is 2^-18."""
+    p = Problem(rows, 64, 295, "f16", scale=0.0)
+    p.bias[:] = 35.0
+    p.bias[7] = 50.0 + 2.0 ** -10
+    p.targets[:] = 7
+    loss = p.forward()[0]
+    _, loss64 = definition(p)
+    close(loss, loss64, loss64 * 2.0 ** -19 + 2.0 ** -20)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("words", [True, False])
 @pytest.mark.parametrize("times,more,scale", [(5, 19, None), (7, 11, None), (5, 19, 3.0), (7, 11, 1000.0)])
