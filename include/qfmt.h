@@ -573,9 +573,13 @@ int qfmt_dropout_add_layer_norm_backward(const qfmt_norm_t* norm, const qfmt_dro
  * Operands as for qfmt_gemm_packed16 (16-byte aligned, leading dimensions multiples of 8, either one transposed), both of
  * storage type dtype: QFMT_F16 (1/5/10 codes) or QFMT_BF16 (1/8/7 codes).  Sums, bias and activation are in 32 bits; y and z
  * are rounded to the storage type once each (to nearest even; what overflows becomes infinite, as in qfmt_quantize_stats).
- * The activation takes the 32-bit z.  A sum over K may be off by (K / 16 + 24) 2^-23 sum |a||b| (the tensor core truncates each of its
- * additions of 16 products, where qfmt_gemm_packed16 takes sums in levels): far below the half step of a code, and relative errors of
- * 10^-6 (K = 1024) to 5 10^-6 (K = 4096) are what bias gradients show of it.  No statistics are kept: qfmt_linear_forward and qfmt_bias_quantize_stats_pack16 do that.
+ * The activation takes the 32-bit z.  No statistics are kept: qfmt_linear_forward and qfmt_bias_quantize_stats_pack16 do that.
+ * Accuracy.  A sum over K may be off by (min(K, 8192) / 16 + K / 16384 + 24) 2^-23 sum |a||b|: the tensor core truncates each of its
+ * additions of 16 products, and sums are closed after 8192 elements and the closed ones added up (qfmt_gemm_packed16 takes its sums in levels,
+ * 2^-20).  That is 2^-16.5 at K = 1024, 2^-13.9 at 8192, 2^-13.7 at 2^20 and 2^-12.3 at 2^24, where half a step of a code is 2^-12
+ * (binary16) or 2^-9 of the result; where a sum cancels, so that sum |a||b| is many times the result, it is as many times more of it.  Results
+ * in 32 bits (column sums; the loss and lse below) show it: relative errors of 10^-6 at K = 1024, 10^-5 at 8192.  Activations and
+ * their slopes go through the exponential and reciprocal of the special function unit and are within 2^-18 of their value, or of 1.
  *   QFMT_ACT_NONE z, QFMT_ACT_RELU max(z, 0), QFMT_ACT_GELU z Phi(z), QFMT_ACT_SILU z / (1 + exp(-z)),
  *   QFMT_ACT_GELU_TANH z / 2 (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3)))
  */
@@ -648,7 +652,8 @@ size_t qfmt_act_backward_workspace_bytes(int64_t rows, int64_t cols);
  *   d_workspace  device, 16-byte aligned, at least qfmt_linear_cross_entropy_workspace_bytes(H, W, 0) bytes; status area and
  *                sharing as for qfmt_gemm
  * Sums, exponentials and statistics are in 32 bits, the loss is subtracted in 64 (lse is rounded to 32); results do not depend on the
- * order in which blocks run.
+ * order in which blocks run.  Sums over D are as accurate as those of qfmt_linear_act, exponentials come from the special function unit (2^-19 of a
+ * sum of them, and as much of lse and the loss in absolute terms).
  * The backward pass, with the same H, W, bias and targets and the forward pass's lse:
  *     d = g (exp(logits - lse) - onehot(target)),  dH = d op(W)^T,  dW = the gradient of W as W is stored,  dbias = sums of d,
  *     g = dloss (1 if d_dloss is NULL) * (1 / rows that count, if kind->mean) * (d_dls->scale, if given).
@@ -660,8 +665,8 @@ size_t qfmt_act_backward_workspace_bytes(int64_t rows, int64_t cols);
  *   d_dw, ld_dw  device, the stored shape of W, of the storage type, or NULL
  *   d_dbias      device, V floats, or NULL (sums of the 32-bit d)
  *   d_workspace  at least qfmt_linear_cross_entropy_workspace_bytes(H, W, 1) bytes
- * d_dh and d_dw may start on any element; no output may overlap an input (an error the library cannot detect).  Sums over D as in
- * qfmt_linear_act.  Errors: QFMT_ERR_BAD_ARG, QFMT_ERR_UNSUPPORTED_ARCH, QFMT_ERR_CUDA.
+ * d_dh and d_dw may start on any element; no output may overlap an input (an error the library cannot detect).  Sums over D, words
+ * and rows as in qfmt_linear_act.  Errors: QFMT_ERR_BAD_ARG, QFMT_ERR_UNSUPPORTED_ARCH, QFMT_ERR_CUDA.
  */
 typedef struct {
     int64_t ignore_index;     /* target of rows that do not count, e.g. -100                        */

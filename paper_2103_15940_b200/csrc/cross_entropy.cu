@@ -396,7 +396,7 @@ struct AddEpilogue {
             }
             uint32_t r[32];
             p.load32(c, r);
-            p.wait();
+            p.finish(c, r);
             if (c == 1) release();
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -582,7 +582,8 @@ struct Running {  // sum exp(logit - most)
     }
 };
 
-template <bool kBf16, int kBlocks>
+// kLong: sums over K are closed as those of tiles are (product16.cuh); on its own since the loop costs the others up to a tenth of their time.
+template <bool kBf16, int kBlocks, bool kLong>
 __global__ void __launch_bounds__(kFewWarps * 32, 8)
 few_rows_kernel(const FewRows f) {
     constexpr int kWords = 16, kRows = 8 * kBlocks, kLane = 2 * kBlocks;  // kLane: rows of a lane
@@ -613,7 +614,20 @@ few_rows_kernel(const FewRows f) {
     for (int group = (int)blockIdx.x * kFewWarps + warp; group < groups; group += (int)gridDim.x * kFewWarps) {
         const int n0 = group * kWords;
         float d[kBlocks][4] = {};
-        skinny::by_output<kBf16, kBlocks, (kBlocks > 1 ? 2 : 4)>(f.o, n0, 0, f.o.k, lane, d);
+        if constexpr (kLong) {
+#pragma unroll 1
+            for (int k = 0; k < f.o.k; k += p16::kCloseK) {
+                float part[kBlocks][4] = {};
+                skinny::by_output<kBf16, kBlocks, (kBlocks > 1 ? 2 : 4)>(f.o, n0, k, k + p16::kCloseK, lane, part);
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) d[b][i] = __fadd_rn(d[b][i], part[b][i]);
+                }
+            }
+        } else {
+            skinny::by_output<kBf16, kBlocks, (kBlocks > 1 ? 2 : 4)>(f.o, n0, 0, f.o.k, lane, d);
+        }
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) {
 #pragma unroll
@@ -753,9 +767,10 @@ Plan plan_backward(const Sizes& s) {
 
 // Forward passes that go over W in few_rows_kernel, if it is stored by word: up to eight rows, or up to 32 and 2^25 multiplications
 // (measured against tiles: 8 x 1024 x 30522 24.0 against 26.6 us, 16 27.8 against 26.5; 16 x 256 x 4000 9.6 against 12.6, 32 x 256 x 8000
-// 15.3 against 13.2; a W stored by K took longer than tiles at nearly every size).
+// 15.3 against 13.2; a W stored by K took longer than tiles at nearly every size).  D of at most 2^15: a warp then has
+// four closed sums at most.
 bool few_rows(const Sizes& s) {
-    return s.stored_words && (s.rows <= 8 || (s.rows <= skinny::kMostRows && s.rows * s.vocab * s.hidden <= 1ll << 25));
+    return s.stored_words && s.hidden <= 1 << 15 && (s.rows <= 8 || (s.rows <= skinny::kMostRows && s.rows * s.vocab * s.hidden <= 1ll << 25));
 }
 
 // The workspace's parts, in order; every one starts on 256 bytes.
@@ -849,11 +864,13 @@ int word_operand(p16::Operand* o, bool pair, const qfmt_matrix16_t* W, const Siz
     return p16::make_operand(o, true, pair, base, words != s.stored_words, words ? n : s.hidden, words ? s.hidden : n, W->ld);
 }
 
-template <bool kBf16>
+template <bool kBf16, bool kLong>
 int launch_few_rows(const FewRows& f, const DeviceInfo& dev, unsigned* blocks, cudaStream_t stream) {
     const unsigned want = (unsigned)((f.o.n + 16 * kFewWarps - 1) / (16 * kFewWarps)), most = 8u * dev.sm_count;
     *blocks = want < most ? want : most;
-    auto* kernel = f.o.rows <= 8 ? few_rows_kernel<kBf16, 1> : f.o.rows <= 16 ? few_rows_kernel<kBf16, 2> : few_rows_kernel<kBf16, 4>;
+    auto* kernel = f.o.rows <= 8    ? few_rows_kernel<kBf16, 1, kLong>
+                   : f.o.rows <= 16 ? few_rows_kernel<kBf16, 2, kLong>
+                                    : few_rows_kernel<kBf16, 4, kLong>;
     QFMT_CUDA_TRY(launch_overlapping(kernel, *blocks, kFewWarps * 32u, 0, stream, f));
     return QFMT_OK;
 }
@@ -981,8 +998,9 @@ extern "C" int qfmt_linear_cross_entropy(const qfmt_matrix16_t* H, const qfmt_ma
                      at<float2>(d_workspace, pl.parts), at<float>(d_workspace, pl.picked), static_cast<unsigned long long*>(d_workspace),
                      next_launch_tag()};
         unsigned blocks = 0;
-        if (kind->dtype == QFMT_BF16) rc = launch_few_rows<true>(f, dev, &blocks, st);
-        else rc = launch_few_rows<false>(f, dev, &blocks, st);
+        const bool closed = s.hidden > p16::kCloseK;
+        if (kind->dtype == QFMT_BF16) rc = closed ? launch_few_rows<true, true>(f, dev, &blocks, st) : launch_few_rows<true, false>(f, dev, &blocks, st);
+        else rc = closed ? launch_few_rows<false, true>(f, dev, &blocks, st) : launch_few_rows<false, false>(f, dev, &blocks, st);
         if (rc != QFMT_OK) return rc;
         int team = 32;
         while (team > 1 && team * s.rows > 32) team /= 2;

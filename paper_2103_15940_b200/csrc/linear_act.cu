@@ -153,7 +153,7 @@ struct PartEpilogue {
         for (int c = 0; c < 2; ++c) {
             uint32_t a[32];
             p.load32(c, a);
-            p.wait();
+            p.finish(c, a);
             if (c == 1) release();
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -589,10 +589,11 @@ int product_shape(const qfmt_matrix16_t* A, const qfmt_matrix16_t* B, Shape* s) 
 // Products that go over the weights in few_rows_kernel: up to 2^27 multiplications, which tiles cannot spread over the GPU, and up to 32 rows
 // of any size if the weights are stored by output.  Measured against tiles, with GELU: 128 x 256 x 512 3.0 us by output and 5.1 by K against 11.4,
 // 512 x 512 x 512 7.2 and 7.3 against 10.8; at 2^28 256 x 1024 x 1024 9.5 and 11.3 against 11.8, 1024 x 512 x 512 13.1 and 10.8 against 11.7;
-// 32 x 4096 x 4096 13.8 and 25.8 against 17.4.  A's K must be contiguous.
+// 32 x 4096 x 4096 13.8 and 25.8 against 17.4.  A's K must be contiguous, and short enough that none of the eight warps sums more than
+// tiles do before they close a sum.
 constexpr int64_t kFewWork = 1ll << 27;
 bool few_rows(const qfmt_matrix16_t* A, const qfmt_matrix16_t* B, const Shape& s) {
-    if (A->trans != 0) return false;
+    if (A->trans != 0 || s.K > kFewWarps * p16::kCloseK) return false;
     if (B->trans != 0 && s.M <= skinny::kMostRows) return true;
     return s.M <= 1024 && s.M * s.N <= kFewWork && s.M * s.N * s.K <= kFewWork;
 }

@@ -3,11 +3,17 @@
 //
 // One persistent kernel.  For large products one CTA pair per two SMs and 256 x 256 tiles: each CTA stages its own 128 rows of op(A) and its own 128
 // columns of op(B) by TMA (64 K elements, 32 KB a stage), the leader's MMA thread issues tcgen05.mma.cta_group::2 kind::f16
-// with M = 256, N = 256, K = 16, and each CTA's tensor memory receives its 128 x 256 half of the tile.  A tile's whole
-// contraction stays in one of two 256-column accumulators, so the sixteen epilogue warps work on one tile while the next one is
-// summed in the other.  Sums are fp32; the tensor core truncates once per 16 products, which drifts by at most (K / 16) 2^-24
-// of sum |a||b|: 2^-15 at K = 8192, below the half step of every type an epilogue rounds to (2^-12, 2^-9) and of what the loss
-// needs.  (qfmt_gemm_packed16 hands out fp32 sums and takes them in three levels instead, which costs it a third of its rate.)
+// with M = 256, N = 256, K = 16, and each CTA's tensor memory receives its 128 x 256 half of the tile, in one of two 256-column
+// accumulators, so the sixteen epilogue warps work on one tile while the next one is summed in the other.
+//
+// Accuracy.  Sums are fp32, and the tensor core truncates one once per 16 products, by at most 2^-23 of sum |a||b| and always towards zero, so
+// a sum of one sign drifts by its length.  After 8192 elements it is closed (kLong): its epilogue warps add it to what the ones before it
+// came to, rounded to nearest, while the next 8192 are summed in the other accumulator.  So a sum is off by at most
+//     (min(K, 8192) / 16 + K / 16384) 2^-23 of sum |a||b|
+// and what the few additions of an epilogue lose: 2^-14 at K = 8192, 2^-13.8 at 2^20, 2^-12.4 at 2^24, against the half step of 2^-12 that
+// binary16 has.  (qfmt_gemm_packed16 hands out fp32 sums and takes them in three levels instead, 2^-20, which costs it a third of its
+// rate.)  The closed sums are 256 bytes a thread of local memory.  Kernels of their own, since the epilogues have no registers to spare: with
+// the same code for all, 8192 x 1024 x 4096 with GELU took 86 instead of 81 us.
 //
 // Products that leave pairs without a tile run on single CTAs with 128 x 256 tiles (cta_group::1, 48 KB a stage): twice as many workers
 // for half the rows each, at one and a half times the operand traffic (rule: plan_product).
@@ -52,6 +58,7 @@ constexpr uint32_t smem_bytes() { return Staging<kPair>::kStages * Staging<kPair
 static_assert(smem_bytes<true>() <= 232448 && smem_bytes<false>() <= 232448, "shared memory");
 constexpr uint32_t kAccCols = 256, kTmemCols = 512;
 constexpr uint32_t kWaitLimit = 1u << 31;  // SM cycles, about a second
+constexpr int kCloseK = 8192, kCloseStages = kCloseK / kStageK;  // elements and stages of a sum before it is closed
 
 enum : int { kFixed = 0, kCountM = 1, kCountK = 2 };  // which extent the device's count replaces
 enum : int { kAltNone = 0, kAltA = 1, kAltB = 2 };    // which operand has a second place
@@ -77,6 +84,7 @@ struct Patch {
     int split, tile_m, tile_n;
     uint32_t tmem;           // accumulator address of (row0, col0)
     bool empty;              // nothing was summed: the sums are zero
+    float* closed;           // the closed sums of the lane's row, 64 columns; null without any
     uint8_t* box;
 
     __device__ __forceinline__ void load32(int block, uint32_t (&r)[32]) const {
@@ -87,8 +95,25 @@ struct Patch {
             ptx::tmem_load_32cols(tmem + block * 32, r);
         }
     }
-    __device__ __forceinline__ void wait() const {
-        if (!empty) ptx::tmem_load_wait();
+    // Waits for what load32 has asked for and adds the closed sums.
+    __device__ __forceinline__ void finish(int block, uint32_t (&r)[32]) const {
+        if (!empty) ptx::tmem_load_wait_for(r);
+        if (closed != nullptr) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__fadd_rn(closed[block * 32 + j], __uint_as_float(r[j])));
+        }
+    }
+    // Puts the accumulator on top of the closed sums.
+    __device__ __forceinline__ void close(float (&sums)[64]) {
+#pragma unroll 1
+        for (int block = 0; block < 2; ++block) {
+            uint32_t r[32];
+            load32(block, r);
+            finish(block, r);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) sums[block * 32 + j] = __uint_as_float(r[j]);
+        }
+        closed = sums;
     }
     // Block of 32 columns in pairs, complete on return; kBias: plus a vector of the columns, of which the lane brings its column's value.
     // (It goes round through the box.)
@@ -100,7 +125,7 @@ struct Patch {
             reinterpret_cast<float*>(box)[lane] = bias;
             __syncwarp();
         }
-        wait();
+        finish(block, r);
 #pragma unroll
         for (int j = 0; j < 32; j += 4) {
             v[j / 2] = make_pair(__uint_as_float(r[j]), __uint_as_float(r[j + 1]));
@@ -279,7 +304,7 @@ __device__ __forceinline__ uint32_t make_idesc(int a_mn, int b_mn, int bf16) {
            ((uint32_t)((kPair ? 2 * kRows : kRows) >> 4) << 24);
 }
 
-template <typename Epi, bool kPair>
+template <typename Epi, bool kPair, bool kLong>
 __device__ __forceinline__ void product16_body(const CUtensorMap& map_a, const CUtensorMap& map_b, const CUtensorMap& map_alt,
                                                const ProductParams& p, const typename Epi::Params& ep) {
     using S = Staging<kPair>;
@@ -409,36 +434,39 @@ __device__ __forceinline__ void product16_body(const CUtensorMap& map_a, const C
             for (int t = first; t < items && !dead; t += workers) {
                 int kb0;
                 const int nkb = stages_of(t, &kb0);
-                if (nkb == 0) continue;
-                const uint32_t acc = it & 1u, acc_phase = (it >> 1) & 1u;
-                ++it;
-                if (!ptx::mbar_wait_bounded(acc_empty_bar(acc), acc_phase ^ 1u, kWaitLimit)) {
-                    raise_timeout(p.status, p.tag, abort_flag);
-                    break;
-                }
-                ptx::tc_fence_after_sync();
-                const uint32_t d = tmem_base + acc * kAccCols;
-                for (int kb = 0; kb < nkb; ++kb) {
-                    if (!ptx::mbar_wait_bounded(full_bar(stage), phase, kWaitLimit)) {
+                for (int from = 0; from < nkb && !dead; from += kLong ? kCloseStages : nkb) {
+                    const int until = kLong && nkb - from > kCloseStages ? kCloseStages : nkb - from;
+                    const uint32_t acc = it & 1u, acc_phase = (it >> 1) & 1u;
+                    ++it;
+                    if (!ptx::mbar_wait_bounded(acc_empty_bar(acc), acc_phase ^ 1u, kWaitLimit)) {
                         raise_timeout(p.status, p.tag, abort_flag);
                         dead = true;
                         break;
                     }
                     ptx::tc_fence_after_sync();
-                    const uint32_t off = (uint32_t)stage * (kStageBytes >> 4);
+                    const uint32_t d = tmem_base + acc * kAccCols;
+                    for (int kb = 0; kb < until; ++kb) {
+                        if (!ptx::mbar_wait_bounded(full_bar(stage), phase, kWaitLimit)) {
+                            raise_timeout(p.status, p.tag, abort_flag);
+                            dead = true;
+                            break;
+                        }
+                        ptx::tc_fence_after_sync();
+                        const uint32_t off = (uint32_t)stage * (kStageBytes >> 4);
 #pragma unroll
-                    for (int k = 0; k < kStageK / 16; ++k) {
-                        const uint64_t da = desc_join(hi, a_lo + off + k * a_step), db = desc_join(hi, b_lo + off + k * b_step);
-                        if (kPair) ptx::mma_f16_pair(d, da, db, idesc, (kb | k) != 0 ? 1u : 0u);
-                        else ptx::mma_f16(d, da, db, idesc, (kb | k) != 0 ? 1u : 0u);
+                        for (int k = 0; k < kStageK / 16; ++k) {
+                            const uint64_t da = desc_join(hi, a_lo + off + k * a_step), db = desc_join(hi, b_lo + off + k * b_step);
+                            if (kPair) ptx::mma_f16_pair(d, da, db, idesc, (kb | k) != 0 ? 1u : 0u);
+                            else ptx::mma_f16(d, da, db, idesc, (kb | k) != 0 ? 1u : 0u);
+                        }
+                        if (kPair) ptx::mma_commit_pair(empty_bar(stage), 3);
+                        else ptx::mma_commit(empty_bar(stage));
+                        if (++stage == kStages) { stage = 0; phase ^= 1u; }
                     }
-                    if (kPair) ptx::mma_commit_pair(empty_bar(stage), 3);
-                    else ptx::mma_commit(empty_bar(stage));
-                    if (++stage == kStages) { stage = 0; phase ^= 1u; }
+                    if (dead) break;
+                    if (kPair) ptx::mma_commit_pair(acc_full_bar(acc), 3);
+                    else ptx::mma_commit(acc_full_bar(acc));
                 }
-                if (dead) break;
-                if (kPair) ptx::mma_commit_pair(acc_full_bar(acc), 3);
-                else ptx::mma_commit(acc_full_bar(acc));
             }
         }
         __syncwarp();
@@ -450,6 +478,8 @@ __device__ __forceinline__ void product16_body(const CUtensorMap& map_a, const C
         pt.box = smem_raw + (boxes - raw) + pt.warp * kBoxBytes;
         pt.rows = M;
         pt.cols = p.N;
+        float sums[kLong ? 64 : 1];
+        pt.closed = nullptr;
         const int quarter = pt.warp >> 2;
         uint32_t it = 0;
         for (int t = first; t < items; t += workers) {
@@ -462,29 +492,46 @@ __device__ __forceinline__ void product16_body(const CUtensorMap& map_a, const C
             pt.row0 = pt.tile_m * kTileM + (int)rank * kRows + pt.quad * 32;
             pt.col0 = pt.tile_n * kTileN + quarter * 64;
             pt.empty = nkb == 0;
-            const uint32_t acc = it & 1u, acc_phase = (it >> 1) & 1u;
+            uint32_t acc = it & 1u, acc_phase = (it >> 1) & 1u;
             pt.tmem = tmem_base + ((uint32_t)(pt.quad * 32) << 16) + acc * kAccCols + (uint32_t)quarter * 64u;
             typename Epi::Ahead ahead;
             Epi::before(pt, ep, ahead);
-            if (nkb != 0) {
+            auto complete = [&] {  // waits for the accumulator
                 ++it;
                 bool ok = true;
                 if (lane == 0) ok = ptx::mbar_wait_bounded(acc_full_bar(acc), acc_phase, kWaitLimit);
                 ok = __shfl_sync(0xFFFFFFFFu, ok ? 1 : 0, 0) != 0;
                 if (!ok && lane == 0) raise_timeout(p.status, p.tag, abort_flag);
-                if (!ok || *abort_flag) break;
+                if (!ok || *abort_flag) return false;
                 ptx::tc_fence_after_sync();
-            }
-            const uint32_t bar = kPair ? ptx::map_to_cta(acc_empty_bar(acc), 0) : acc_empty_bar(acc);
-            Epi::run(pt, ep, ahead, [&] {  // the accumulator has been read
-                if (nkb != 0) {
-                    ptx::tc_fence_before_sync();
-                    __syncwarp();
-                    if (lane == 0) {
-                        if (kPair) ptx::mbar_arrive_cluster(bar);
-                        else ptx::mbar_arrive(bar);
-                    }
+                return true;
+            };
+            auto release = [&](uint32_t bar) {  // the accumulator has been read
+                ptx::tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) {
+                    if (kPair) ptx::mbar_arrive_cluster(bar);
+                    else ptx::mbar_arrive(bar);
                 }
+            };
+            auto empty_of = [&] { return kPair ? ptx::map_to_cta(acc_empty_bar(acc), 0) : acc_empty_bar(acc); };
+            if (nkb != 0 && !complete()) break;
+            if constexpr (kLong) {
+                pt.closed = nullptr;
+                bool ok = true;
+                for (int left = nkb; left > kCloseStages && ok; left -= kCloseStages) {
+                    pt.close(sums);
+                    release(empty_of());
+                    acc = it & 1u;
+                    acc_phase = (it >> 1) & 1u;
+                    pt.tmem = tmem_base + ((uint32_t)(pt.quad * 32) << 16) + acc * kAccCols + (uint32_t)quarter * 64u;
+                    ok = complete();
+                }
+                if (!ok) break;
+            }
+            const uint32_t bar = empty_of();
+            Epi::run(pt, ep, ahead, [&] {
+                if (nkb != 0) release(bar);
             });
         }
         __syncwarp();
@@ -503,17 +550,17 @@ __device__ __forceinline__ void product16_body(const CUtensorMap& map_a, const C
     }
 }
 
-template <typename Epi>
+template <typename Epi, bool kLong>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 product16_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                       const __grid_constant__ CUtensorMap map_alt, const ProductParams p, const typename Epi::Params ep) {
-    product16_body<Epi, true>(map_a, map_b, map_alt, p, ep);
+    product16_body<Epi, true, kLong>(map_a, map_b, map_alt, p, ep);
 }
-template <typename Epi>
+template <typename Epi, bool kLong>
 __global__ void __launch_bounds__(kThreads, 1)
 product16_single_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                         const __grid_constant__ CUtensorMap map_alt, const ProductParams p, const typename Epi::Params ep) {
-    product16_body<Epi, false>(map_a, map_b, map_alt, p, ep);
+    product16_body<Epi, false, kLong>(map_a, map_b, map_alt, p, ep);
 }
 
 // ---- host side --------------------------------------------------------------------------------------------------------
@@ -557,32 +604,37 @@ inline int make_operand(Operand* o, bool is_b, bool pair, const void* ptr, bool 
                               is_b && !pair ? kTileN : kRows, &o->blocked);
 }
 
+template <typename Epi, bool kLong>
+int launch_product_of(bool pair, const Operand& a, const Operand& b, const CUtensorMap& alt, const ProductParams& p, const typename Epi::Params& ep,
+                      const DeviceInfo& dev, cudaStream_t stream) {
+    static std::atomic<bool> ready[64];
+    const bool known = dev.ordinal >= 0 && dev.ordinal < 64;
+    auto* const pairs = product16_pair_kernel<Epi, kLong>;
+    auto* const singles = product16_single_kernel<Epi, kLong>;
+    if (!known || !ready[dev.ordinal].load()) {
+        QFMT_CUDA_TRY(cudaFuncSetAttribute(pairs, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<true>()));
+        QFMT_CUDA_TRY(cudaFuncSetAttribute(singles, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<false>()));
+        if (known) ready[dev.ordinal].store(true);
+    }
+    const int64_t items = (pair ? pair_tiles(p.M, p.N) : single_tiles(p.M, p.N)) * p.splits;
+    const int64_t most = pair ? dev.sm_count / 2 : dev.sm_count, workers = items < most ? items : most;
+    if (workers == 0) return QFMT_OK;
+    if (pair) QFMT_CUDA_TRY(launch_overlapping(pairs, (unsigned)(2 * workers), (unsigned)kThreads, smem_bytes<true>(), stream, a.map, b.map, alt, p, ep));
+    else QFMT_CUDA_TRY(launch_overlapping(singles, (unsigned)workers, (unsigned)kThreads, smem_bytes<false>(), stream, a.map, b.map, alt, p, ep));
+    return QFMT_OK;
+}
+
 // Workspace words, statuses and operands are the caller's; the plan's splits are in p.
 template <typename Epi>
 int launch_product(bool pair, const Operand& a, const Operand& b, const Operand* alt, ProductParams p, const typename Epi::Params& ep,
                    const DeviceInfo& dev, cudaStream_t stream) {
-    static std::atomic<bool> ready[64];
-    const bool known = dev.ordinal >= 0 && dev.ordinal < 64;
-    if (!known || !ready[dev.ordinal].load()) {
-        QFMT_CUDA_TRY(cudaFuncSetAttribute(product16_pair_kernel<Epi>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<true>()));
-        QFMT_CUDA_TRY(cudaFuncSetAttribute(product16_single_kernel<Epi>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<false>()));
-        if (known) ready[dev.ordinal].store(true);
-    }
     p.a_mn = a.mn;
     p.b_mn = b.mn;
     p.a_blocked = a.blocked;
     p.b_blocked = b.blocked;
-    const int64_t items = (pair ? pair_tiles(p.M, p.N) : single_tiles(p.M, p.N)) * p.splits;
-    const int64_t most = pair ? dev.sm_count / 2 : dev.sm_count, workers = items < most ? items : most;
-    if (workers == 0) return QFMT_OK;
     const CUtensorMap& other = alt != nullptr ? alt->map : a.map;
-    if (pair)
-        QFMT_CUDA_TRY(launch_overlapping(product16_pair_kernel<Epi>, (unsigned)(2 * workers), (unsigned)kThreads, smem_bytes<true>(), stream, a.map,
-                                         b.map, other, p, ep));
-    else
-        QFMT_CUDA_TRY(launch_overlapping(product16_single_kernel<Epi>, (unsigned)workers, (unsigned)kThreads, smem_bytes<false>(), stream, a.map,
-                                         b.map, other, p, ep));
-    return QFMT_OK;
+    if (p.kb_per_split > kCloseStages) return launch_product_of<Epi, true>(pair, a, b, other, p, ep, dev, stream);
+    return launch_product_of<Epi, false>(pair, a, b, other, p, ep, dev, stream);
 }
 
 }  // namespace p16

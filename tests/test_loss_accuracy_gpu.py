@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import paper_2103_15940_b200 as qf
-from step_reference import TYPES, close, half_step, workspace
+from step_reference import TYPES, close, half_step, operand, workspace
 from test_cross_entropy_gpu import IGNORED, Problem
 
 pytestmark = pytest.mark.gpu
@@ -46,6 +46,48 @@ def test_the_least_loss(rows):
     loss = p.forward()[0]
     _, loss64 = definition(p)
     close(loss, loss64, loss64 * 2.0 ** -19 + 2.0 ** -20)
+
+
+@pytest.mark.parametrize("rows", [2, 8, 9, 32, 100])
+@pytest.mark.parametrize("words", [True, False])
+@pytest.mark.parametrize("hidden", [32768, 50000])
+def test_logits_of_one_sign_over_a_long_contraction(rows, words, hidden):
+    """Sums over D are closed after 8192 elements, wherever the product goes."""
+    p = Problem(rows, 64, 40, "f16", words, scale=1.0)
+    gen, t = p.gen, p.t
+    p.hidden = hidden
+    one = lambda *s: 0.5 + torch.rand(*s, generator=gen, device="cuda")
+    p.h = operand(one(rows, hidden), t)
+    w = one(40, hidden) * 2.0 ** -12
+    p.w = operand(w if words else w.t(), t)
+    loss, lse, _ = p.forward()
+    logits = p.h.double() @ (p.w.t() if words else p.w).double() + p.bias.double()
+    size = logits.abs().amax(dim=1)
+    want = torch.logsumexp(logits, dim=1)
+    tol = size * ((8192 / 16 + hidden / 16384 + 24) * 2.0 ** -23) + 2.0 ** -19 + want.abs() * 2.0 ** -22
+    close(lse, want, tol)
+    close(loss, want - logits.gather(1, p.targets[:, None])[:, 0], 2.0 * tol)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("words", [True, False])
+def test_weight_gradients_of_one_sign_over_many_tokens(words, dtype):
+    """Sums over tokens are closed after 8192: with W = 0 and 64 words every probability is 1/64, a code, so what the sums lose shows."""
+    rows = 1 << 18
+    p = Problem(rows, 40, 64, dtype, words, bias=False, scale=0.0)
+    p.h = operand(0.5 + torch.rand(rows, 40, generator=p.gen, device="cuda"), p.t)
+    p.targets[:] = 5
+    lse = p.forward()[1]
+    dh, dw, db = p.backward(lse, mean=False)
+    d = torch.full((64,), 1.0 / 64.0, device="cuda", dtype=torch.float64)
+    d[5] -= 1.0
+    want = d[:, None] * p.h.double().sum(dim=0)[None]
+    tol = want.abs() * ((8192 / 16 + rows / 16384 + 24) * 2.0 ** -23)
+    tol = tol + half_step(want.abs() + tol, p.t)
+    close(dw if words else dw.t(), want, tol)
+    # column sums: the exponential 2^-21; 32 rows, then a 32nd of the parts one after the other, half a step each
+    close(db, d * rows, (d * rows).abs() * (2.0 ** -21 + (rows / 1024 + 40) * 2.0 ** -24))
+    assert not dh.any()  # W is zero
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
