@@ -107,6 +107,10 @@ struct BackwardEpilogue {
             p.load_pairs<false>(c, v);
             if (c == 1) release();
             if (col0 >= p.cols) continue;
+            if (p.row0 + p.lane >= p.rows) {  // rows beyond the matrix are zeros, but not their products with infinite weights
+#pragma unroll
+                for (int j = 0; j < 16; ++j) v[j] = 0ull;
+            }
             if (e.residual != nullptr) {
                 p16::Fetched late;
                 if (kAct != QFMT_ACT_NONE) fetch_residual(p, e, late, col0);
@@ -130,7 +134,6 @@ struct BackwardEpilogue {
             p16::box_store<T>(p.box, e.dz, e.ld_dz, p.row0, p.rows, col0, p.cols, p.lane, e.vec_dz != 0);
             __syncwarp();
             if (e.parts != nullptr) {
-                // rows beyond the matrix: sums and residual are zero there, and so is dz
                 const float s = p16::column_sum(p.box, p.lane, v);
                 if (col0 + p.lane < p.cols) e.parts[(int64_t)(p.row0 >> 5) * e.pitch + col0 + p.lane] = s;
             }
