@@ -630,7 +630,8 @@ int qfmt_linear_act_backward(const qfmt_matrix16_t* A, const qfmt_matrix16_t* B,
  *   d_dy, d_z, d_dz  device, rows x cols of storage type dtype (QFMT_F32, QFMT_F16 or QFMT_BF16); leading dimensions of 0 stand
  *                    for cols; any alignment of an element.  d_dz may equal d_dy or d_z when their leading dimensions agree
  *   d_dbias          device, cols floats, or NULL
- *   d_workspace      16-byte aligned, at least qfmt_act_backward_workspace_bytes(rows, cols) bytes; NULL if d_dbias is
+ *   d_workspace      16-byte aligned, at least qfmt_act_backward_workspace_bytes(rows, cols) bytes; NULL if d_dbias is.  The pass has no
+ *                    waits that could run out: it leaves the status area of a shared workspace as it is
  * rows = 0 (dbias = 0) and cols = 0 are valid; rows and cols are below 2^31.  Errors as above.
  */
 int qfmt_act_backward(const void* d_dy, int64_t ld_dy, const void* d_z, int64_t ld_z, void* d_dz, int64_t ld_dz, float* d_dbias,
@@ -686,7 +687,9 @@ size_t qfmt_linear_cross_entropy_workspace_bytes(const qfmt_matrix16_t* H, const
  * The norm of all gradients of a step, and clipping by it.  The tensors are described by records in DEVICE memory, so that a
  * list is built once and captured graphs can use it: fill src, dst, n and dtype of `count` records on the host, let
  * qfmt_plan_tensors check them and number their chunks (it returns the chunks of the whole list, or an error < 0), and copy
- * the records to the device.  count and chunks of the calls below are those of that plan (the kernels walk the list by them).
+ * the records to the device.  count and chunks of the calls below are those of that plan (the kernels walk the list by them).  Where
+ * qfmt_grad_clip writes, records must not overlap, a tensor's own dst and src apart: a tensor that is listed twice would be clipped twice (an
+ * error the library cannot detect).
  */
 typedef struct {
     const void* src;          /* device, n elements, any alignment of an element (NULL if n = 0)      */
@@ -713,9 +716,11 @@ typedef struct {
  *   d_norm     device, 8-byte aligned: receives the record
  *   d_stats    device, 8-byte aligned, or NULL: a statistics record for qfmt_dls_update.  n_total, n_nan and n_inf_in are those of
  *              the gradients, everything else is 0
- *   d_workspace  device, 16-byte aligned, at least qfmt_grad_norm_workspace_bytes(count, chunks) bytes
+ *   d_workspace  device, 16-byte aligned, at least qfmt_grad_norm_workspace_bytes(count, chunks) bytes; the status area of a shared
+ *                workspace is left as it is
  * The order of summation depends on the sizes (and the GPU's number of processors) alone.  Call qfmt_dls_update after this, not before:
- * it changes the scale.  count = 0 is valid (norm 0).
+ * it changes the scale.  count = 0 is valid (norm 0).  A norm beyond the largest 32-bit number is infinite in the record; the factor is that of
+ * the norm in 64 bits.
  * qfmt_grad_clip writes dst = src * factor, in 32 bits, rounded to dtype, for every record with a dst; where dst equals src and factor
  * is 1 nothing moves.
  * Errors: QFMT_ERR_BAD_ARG, QFMT_ERR_UNSUPPORTED_ARCH, QFMT_ERR_CUDA.

@@ -283,6 +283,7 @@ int64_t list_blocks(int64_t chunks, const DeviceInfo& dev) {
     return chunks < most ? chunks : most;
 }
 constexpr int64_t kMostBlocks = 256 * kBlocksPerSm;  // workspaces are sized without asking a device
+constexpr size_t kHeader = 256;                      // the status area, which is another call's if the workspace is shared
 
 bool misaligned(const void* p, uintptr_t size) { return (reinterpret_cast<uintptr_t>(p) & (size - 1)) != 0; }
 bool list_ok(const qfmt_tensor_t* d_tensors, int64_t count, int64_t chunks) {
@@ -312,7 +313,7 @@ extern "C" int64_t qfmt_plan_tensors(qfmt_tensor_t* h_tensors, int64_t count) {
 extern "C" size_t qfmt_grad_norm_workspace_bytes(int64_t count, int64_t chunks) {
     if (count < 0 || chunks < 0) return 0;
     const int64_t blocks = chunks < qfmt::kMostBlocks ? chunks : qfmt::kMostBlocks;
-    return (size_t)(blocks > 0 ? blocks : 1) * sizeof(qfmt::Partial);
+    return qfmt::kHeader + (size_t)blocks * sizeof(qfmt::Partial);
 }
 
 extern "C" int qfmt_grad_norm(const qfmt_tensor_t* d_tensors, int64_t count, int64_t chunks, float max_norm, const qfmt_dls_t* d_dls,
@@ -328,7 +329,7 @@ extern "C" int qfmt_grad_norm(const qfmt_tensor_t* d_tensors, int64_t count, int
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     int64_t blocks = list_blocks(chunks, dev);
     if (blocks > kMostBlocks) blocks = kMostBlocks;
-    Partial* partials = static_cast<Partial*>(d_workspace);
+    Partial* partials = reinterpret_cast<Partial*>(static_cast<char*>(d_workspace) + kHeader);
     if (blocks > 0)
         QFMT_CUDA_TRY(launch_overlapping(norm_kernel, (unsigned)blocks, (unsigned)kThreads, 0, st, d_tensors, (int)count, (long long)chunks, partials));
     QFMT_CUDA_TRY(launch_overlapping(finish_kernel, 1u, (unsigned)kThreads, 0, st, (const Partial*)partials, (int)blocks, d_tensors, (int)count,

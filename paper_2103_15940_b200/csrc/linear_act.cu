@@ -888,7 +888,7 @@ extern "C" int qfmt_linear_act_backward(const qfmt_matrix16_t* A, const qfmt_mat
 
 extern "C" size_t qfmt_act_backward_workspace_bytes(int64_t rows, int64_t cols) {
     if (rows < 0 || cols < 0 || rows >= (1ll << 31) || cols >= (1ll << 31)) return 0;
-    return (size_t)qfmt::pass_row_blocks(rows, cols > 0 ? cols : 1) * (size_t)qfmt::padded(cols) * sizeof(float);
+    return qfmt::kHeader + (size_t)qfmt::pass_row_blocks(rows, cols > 0 ? cols : 1) * (size_t)qfmt::padded(cols) * sizeof(float);
 }
 
 extern "C" int qfmt_act_backward(const void* d_dy, int64_t ld_dy, const void* d_z, int64_t ld_z, void* d_dz, int64_t ld_dz, float* d_dbias,
@@ -925,7 +925,8 @@ extern "C" int qfmt_act_backward(const void* d_dy, int64_t ld_dy, const void* d_
     a.ld_z = ld_z;
     a.out = d_dz;
     a.ld_out = ld_dz;
-    a.sums = d_dbias != nullptr ? static_cast<float*>(d_workspace) : nullptr;
+    // behind the status area, which is another call's if the workspace is shared
+    a.sums = d_dbias != nullptr ? reinterpret_cast<float*>(static_cast<char*>(d_workspace) + kHeader) : nullptr;
     a.pitch = padded(cols);
     a.rows = rows;
     a.cols = cols;
