@@ -529,7 +529,8 @@ typedef struct {
  *            for rows = 0) and do not depend on the order in which blocks run
  *   fmt, d_stats, accumulate   as above, for dx (d_stats requires d_dx)
  *   d_workspace  device, 16-byte aligned, at least qfmt_layer_norm_workspace_bytes(norm) bytes; may be NULL if
- *            neither d_dweight nor d_dbias is wanted.  Calls that share a workspace must be ordered on one stream
+ *            neither d_dweight nor d_dbias is wanted.  Calls that share a workspace must be ordered on one stream; its
+ *            status area is left as it is
  * d_dx may equal d_dy when their leading dimensions agree.
  * Errors: QFMT_ERR_BAD_FORMAT, QFMT_ERR_BAD_ARG, QFMT_ERR_UNSUPPORTED_ARCH, QFMT_ERR_CUDA.
  */

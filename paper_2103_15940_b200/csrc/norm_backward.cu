@@ -623,6 +623,8 @@ int backward(const Call& c, const void* d_dy, const void* d_dh, const void* d_h,
     return launch_backward<kType, kFused>(c, a, d_dweight, d_dbias, stream);
 }
 
+constexpr size_t kStatusBytes = 256;  // head of a workspace: the status area of other calls that share it
+
 int backward_entry(const qfmt_norm_t* norm, const qfmt_dropout_t* drop, bool fused, const void* d_dy, const void* d_dh,
                    const void* d_h, const float* d_mean, const float* d_rstd, const float* d_weight, void* d_dx,
                    void* d_dresidual, float* d_dweight, float* d_dbias, const qfmt_format_t* fmt, qfmt_stats_t* d_stats,
@@ -653,7 +655,7 @@ int backward_entry(const qfmt_norm_t* norm, const qfmt_dropout_t* drop, bool fus
     const auto run = fused ? (t == QFMT_F32 ? backward<QFMT_F32, true> : t == QFMT_F16 ? backward<QFMT_F16, true> : backward<QFMT_BF16, true>)
                            : (t == QFMT_F32 ? backward<QFMT_F32, false> : t == QFMT_F16 ? backward<QFMT_F16, false> : backward<QFMT_BF16, false>);
     return run(c, d_dy, d_dh, d_h, ld_h, d_mean, d_rstd, d_weight, d_dx, d_dresidual, d_dweight, d_dbias, d_stats,
-               columns ? static_cast<float*>(d_workspace) : nullptr, stream);
+               columns ? reinterpret_cast<float*>(static_cast<char*>(d_workspace) + kStatusBytes) : nullptr, stream);
 }
 
 }  // namespace
@@ -661,7 +663,7 @@ int backward_entry(const qfmt_norm_t* norm, const qfmt_dropout_t* drop, bool fus
 
 extern "C" size_t qfmt_layer_norm_workspace_bytes(const qfmt_norm_t* norm) {
     if (norm == nullptr || norm->rows < 0 || norm->cols < 0 || norm->rows > 0x7FFFFFFF || norm->cols > 0x7FFFFFFF) return 0;
-    return (size_t)qfmt::row_parts(*norm) * 2 * (size_t)qfmt::padded_columns(norm->cols) * sizeof(float);
+    return qfmt::kStatusBytes + (size_t)qfmt::row_parts(*norm) * 2 * (size_t)qfmt::padded_columns(norm->cols) * sizeof(float);
 }
 
 extern "C" int qfmt_layer_norm_backward(const qfmt_norm_t* norm, const void* d_dy, const void* d_x, const float* d_mean,

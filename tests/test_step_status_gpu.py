@@ -40,6 +40,21 @@ def test_pass_over_a_gradient(shape):
     assert bool((db == float(rows)).all())
 
 
+@pytest.mark.parametrize("shape", [(3, 8), (4099, 520), (700, 20000)])
+def test_layer_norm_backward(shape):
+    rows, cols = shape
+    x, dy = torch.randn(rows, cols, device="cuda"), torch.ones(rows, cols, device="cuda")
+    mean, rstd, y = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda"), torch.empty_like(x)
+    dx, dw, db = torch.empty_like(x), torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda")
+    norm = qf.make_norm(rows, cols, qf.QFMT_F32)
+    qf.qfmt_layer_norm(norm, x, None, None, y, mean, rstd)
+    ws = workspace(qf.qfmt_layer_norm_workspace_bytes(norm))
+    timed_out(ws)
+    qf.qfmt_layer_norm_backward(norm, dy, x, mean, rstd, None, dx, dw, db, ws, ws.numel())
+    assert qf.qfmt_device_status(ws) == qf.QFMT_ERR_TIMEOUT
+    assert bool((db == float(rows)).all())
+
+
 def test_a_call_that_reports_there_starts_anew():
     a, b = (torch.ones(s, device="cuda", dtype=torch.bfloat16) for s in ((8, 16), (16, 24)))
     A, B, y = qf.make_matrix(a), qf.make_matrix(b), torch.empty(8, 24, device="cuda", dtype=torch.bfloat16)
