@@ -147,19 +147,21 @@ _calls_error: Optional[ImportError] = None
 
 def _bind_calls(L: ctypes.CDLL) -> None:
     """The sub-layer calls and those around a step's last products go through a module of their own, since generic conversion takes
-    as long as their GPU work.  Without it they raise; nothing else needs it."""
+    as long as their GPU work.  Without it, or with one that was built from other sources, they raise; nothing else needs it."""
     global _calls, _calls_error
+    address = lambda f: ctypes.cast(f, ctypes.c_void_p).value
     try:
         from . import _calls
+        _calls.bind(*(address(f) for f in (
+            L.qfmt_dropout, L.qfmt_layer_norm, L.qfmt_layer_norm_backward, L.qfmt_dropout_add_layer_norm,
+            L.qfmt_dropout_add_layer_norm_backward)))
+        _calls.bind_step(*(address(f) for f in (
+            L.qfmt_linear_act, L.qfmt_linear_act_backward, L.qfmt_act_backward, L.qfmt_linear_cross_entropy,
+            L.qfmt_linear_cross_entropy_backward, L.qfmt_grad_norm, L.qfmt_grad_clip)))
     except ImportError as e:
         _calls, _calls_error = None, e
-        return
-    _calls.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
-        L.qfmt_dropout, L.qfmt_layer_norm, L.qfmt_layer_norm_backward, L.qfmt_dropout_add_layer_norm,
-        L.qfmt_dropout_add_layer_norm_backward)))
-    _calls.bind_step(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
-        L.qfmt_linear_act, L.qfmt_linear_act_backward, L.qfmt_act_backward, L.qfmt_linear_cross_entropy,
-        L.qfmt_linear_cross_entropy_backward, L.qfmt_grad_norm, L.qfmt_grad_clip)))
+    except (AttributeError, TypeError) as e:
+        _calls, _calls_error = None, ImportError(f"it was built from other sources: {e}")
 
 
 def _bind_optional(L: ctypes.CDLL) -> None:

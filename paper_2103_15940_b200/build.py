@@ -70,8 +70,8 @@ def build_calls() -> None:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Builds what is missing or out of date: the library first, since all calls but the sub-layer ones do without the module
-    (which needs the interpreter's headers)."""
+    """Builds what is missing or out of date: the library first, since all calls but the sub-layer ones and those around a step's last
+    products do without the module (which needs the interpreter's headers)."""
     if force or library_needs_build():
         build_library(verbose)
     if force or calls_need_build():
