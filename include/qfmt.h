@@ -646,9 +646,9 @@ size_t qfmt_act_backward_workspace_bytes(int64_t rows, int64_t cols);
  *                (an embedding).  Both as for qfmt_linear_act, of storage type kind->dtype.  tokens, D and V are at least 1 (tokens = 0
  *                is valid and gives mean = 0)
  *   d_bias       device, V floats, or NULL; -infinity takes a word out of the vocabulary
- *   d_targets    device, 8-byte aligned, tokens numbers.  Rows whose target is ignore_index do not count: their loss and lse
- *                are 0, and H is not read there (whatever it holds).  They cost no products.  Any other target outside 0 .. V - 1 gives a NaN
- *                loss and lse
+ *   d_targets    device, 8-byte aligned, tokens numbers.  Rows whose target is ignore_index do not count: their loss and lse are 0, and
+ *                whatever H holds there has no effect on any result.  They cost no products, but for the forward pass of at most 32
+ *                rows, which may read and multiply them all the same.  Any other target outside 0 .. V - 1 gives a NaN loss and lse
  *   d_loss       device, tokens floats, or NULL;  d_lse  device, tokens floats, or NULL: what the backward pass needs
  *   d_mean       device, one float, or NULL: the mean loss of the rows that count (0 if none does)
  *   d_workspace  device, 16-byte aligned, at least qfmt_linear_cross_entropy_workspace_bytes(H, W, 0) bytes; status area and

@@ -48,9 +48,9 @@ __device__ __forceinline__ void grid_launch_dependents() { asm volatile("griddep
 
 // Launch with programmatic stream serialization: the grid may be placed on SMs that the kernel before it
 // in the stream has left (once all of that kernel's CTAs have passed their grid_launch_dependents), so its
-// prologue overlaps that kernel's tail.  Only for kernels that execute grid_dependency_wait before their
-// first access to global memory (the GEMM kernels, the split-K reduction, the layer-output pass).  After anything else in the
-// stream (a copy, a memset, a kernel without grid_launch_dependents) it is an ordinary launch.
+// prologue overlaps that kernel's tail.  Only for kernels that execute grid_dependency_wait before they first read or write global
+// memory (a prefetch into the second-level cache may come before: what it brings is not read then, and that cache sees all
+// writes).  After anything else in the stream (a copy, a memset, a kernel without grid_launch_dependents) it is an ordinary launch.
 template <typename... P, typename... A>
 cudaError_t launch_overlapping(void (*kernel)(P...), unsigned grid, unsigned block, size_t smem, cudaStream_t stream,
                                A&&... args) {

@@ -542,7 +542,8 @@ scatter_kernel(const float* __restrict__ sums, int splits, int64_t split_stride,
 
 // ---- few rows ---------------------------------------------------------------------------------------------------------------
 // The forward pass as a pass over a W that is stored by word: a warp takes 16 words at a time and the whole of K, and keeps a maximum and a
-// sum for every row that a lane's words belong to; the block leaves one pair a row.  Rows that do not count ride along.
+// sum for every row that a lane's words belong to; the block leaves one pair a row.  Rows that do not count ride along: they are read and
+// multiplied, and their results are left out.
 struct FewRows {
     skinny::Operands o;
     const float* bias;

@@ -2,7 +2,8 @@
 //     norm = sqrt(sum (g / scale)^2),  dst = src min(1, max_norm / norm) / scale.
 //
 // Sums are in 64 bits, and squares too unless eight of codes add up in 32 bits without leaving its range: the square of any 32-bit
-// value is exact and finite in 64 bits, so nothing overflows or vanishes and a sum is not finite exactly if an element is not.  Only then are elements looked at one by one for the counts.
+// value is exact and finite in 64 bits, so nothing overflows or vanishes and a sum is not finite exactly if an element is not.  Only then
+// are elements looked at one by one for the counts.
 //
 // The list's chunks (at most 8192 elements of one tensor) form one sequence, cut into equal ranges among the blocks; a block finds its
 // first tensor by bisection and walks on from there.  Every block leaves one partial sum and one more block adds those up, so the order
@@ -58,11 +59,6 @@ __device__ __forceinline__ float rounded(float v, float) { return v; }
 __device__ __forceinline__ __half rounded(float v, __half) { return __float2half_rn(v); }
 __device__ __forceinline__ __nv_bfloat16 rounded(float v, __nv_bfloat16) { return __float2bfloat16_rn(v); }
 
-// The block's range of chunks and its place in the list.
-struct Walk {
-    long long chunk, end;
-    int tensor;
-};
 // The last tensor whose first chunk is not behind `chunk` (empty tensors share theirs with the next).  Each step of the search looks at
 // 32 places at once, a lane each: a list of a thousand tensors takes two dependent loads, not ten.
 __device__ __forceinline__ int tensor_of(const qfmt_tensor_t* tensors, int count, long long chunk) {

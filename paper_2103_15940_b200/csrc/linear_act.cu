@@ -242,7 +242,6 @@ __device__ __forceinline__ void pass_store(T* p, unsigned there, int lane, const
 
 constexpr int kPassWarps = 8, kPassPerSm = 4;
 
-//
 // Whole pieces of a gradient come through a ring in shared memory, a lane's own pieces at its own place, so that several rows of every warp
 // are on their way at all times without holding registers: with the loads of one row at a time 8192 x 4096 bfloat16 takes 54 to 56 us,
 // whether with 16, 32 or 48 warps an SM.
