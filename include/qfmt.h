@@ -667,8 +667,8 @@ size_t qfmt_act_backward_workspace_bytes(int64_t rows, int64_t cols);
  *   d_dw, ld_dw  device, the stored shape of W, of the storage type, or NULL
  *   d_dbias      device, V floats, or NULL (sums of the 32-bit d)
  *   d_workspace  at least qfmt_linear_cross_entropy_workspace_bytes(H, W, 1) bytes
- * d_dh and d_dw may start on any element; no output may overlap an input (an error the library cannot detect).  Sums over D, words
- * and rows as in qfmt_linear_act.  Errors: QFMT_ERR_BAD_ARG, QFMT_ERR_UNSUPPORTED_ARCH, QFMT_ERR_CUDA.
+ * d_dh and d_dw may start on any element; no output may overlap an input (an error the library cannot detect).  Sums over D and
+ * rows as in qfmt_linear_act, over words too up to V = 2^20 (pieces of at least 1024 words add up in 32 bits).  Errors: QFMT_ERR_BAD_ARG, QFMT_ERR_UNSUPPORTED_ARCH, QFMT_ERR_CUDA.
  */
 typedef struct {
     int64_t ignore_index;     /* target of rows that do not count, e.g. -100                        */
